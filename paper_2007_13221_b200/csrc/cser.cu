@@ -25,6 +25,7 @@
 #include <new>
 
 #include "cser.h"
+#include "train_host.h"
 
 namespace {
 
@@ -648,6 +649,16 @@ size_t g_l2_limit_before[64] = {};
 }  // namespace
 
 // ------------------------------------------------------------------ C ABI
+// The other translation units of the library report through the same thread-local message.
+int cser_internal_fail(int code, const char *fmt, ...) {
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(g_err, sizeof(g_err), fmt, ap);
+    va_end(ap);
+    return code;
+}
+int cser_internal_check_ptr(const void *p, const char *what) { return check_device_ptr(p, what); }
+
 extern "C" {
 
 const char *cser_last_error(void) { return g_err; }

@@ -1,0 +1,828 @@
+// Orthogonalised updates (cser_orth_* of include/cser_train.h): Newton-Schulz products on the matrices inside the flat
+// gradients of n workers, grouped: one call is three kernels, whatever the number of matrices.
+//
+//   orth_norm_kernel     one pass over g (and m, which it updates): |u|_F^2 per matrix
+//   orth_convert_kernel  X = u / (|u|_F + 1e-7) as 16-bit panels (tensor_tiles.cuh)
+//   orth_products_kernel all products of all steps, persistent
+//
+// With s = the shorter side, l = the longer, a step is
+//     A = X X^T (or X^T X)        s x s, symmetric: tiles on and below the diagonal only          s^2 l flops
+//     B = b A + c A^2             s x s, symmetric, likewise                                       s^3
+//     X <- a X + B X (or X B)                                                                    2 s^2 l
+// 4 s^3 multiply-adds for a square: far over the tensor cores' balance point, so products are the bound for all but
+// small matrices, for which the chain of 3 * steps dependent products is.
+//
+// No transposes.  A tall matrix is not turned: its rows become the inner dimension instead.  The half of A and B above
+// the diagonal is not stored: a stage that needs it reads the mirrored block and takes it as the other majorness.
+//
+// Rounding.  Operands are fp16 (X, A, B times 2^12, which keeps entries of matrices with singular values in 0 .. 1.21 inside
+// fp16's range).  Rounding X, A and B alone would leave 1.5e-3 relative error for a random matrix and 2e-2 for a matrix of low
+// rank with little noise.  Two things take that away without another product: X's remainder is kept (a second fp16) for the
+// a X term (in fp32 where the result is 32-bit), and the diagonals of A and B, which dominate them once X is near orthogonal, are kept in fp32 and left out of
+// the operands:  A A = Ao Ao + (dA_i + dA_j) Ao_ij + dA_i^2 [i = j].  That leaves 3e-4 .. 1e-3.  For a 32-bit result every
+// operand is a pair of fp16 and a product is hi lo + lo hi + hi hi, small terms first.
+//
+// Order of work.  The list of all tiles of all phases of all steps is dealt out to the CTAs in order; a tile waits for
+// the tiles of its own matrix's earlier phases by a counter, so the phases of different matrices overlap.  The launch is cooperative:
+// every CTA is resident, a wait always has someone to end it.
+#include <cuda.h>
+#include <cuda_runtime.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <math.h>
+#include <stdint.h>
+#include <stdio.h>
+#include <new>
+#include <vector>
+
+#include "cser_train.h"
+#include "train_host.h"
+
+namespace {
+
+#include "tensor_tiles.cuh"
+
+constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f, kEps = 1e-7f;
+constexpr float kScale = 4096.f, kUnscale = 1.f / 4096.f, kUnscale2 = kUnscale * kUnscale;
+constexpr int kNormChunk = 8192;                   // elements per CTA of the norm kernel
+// Columns of a tile.
+constexpr int tile_n(bool split) { return split ? 128 : 256; }
+// The tensor cores truncate every partial sum, about 2^-24 of it for 16 terms: 2e-5 over an inner dimension of 4096.  So a
+// 32-bit result's accumulator is taken out and added up in registers, rounded, after this many stages of the leading
+// product (the two small ones share one accumulator).  X's product is the one whose error the steps after it do not
+// shrink: with a low-rank matrix 9e-6 at 4 stages.
+constexpr int kChunkAB = 4, kChunkX = 1;
+constexpr size_t kGroupBytes = 2ull << 30;         // workspace of one group of matrices
+
+struct OrthMat {
+    __half *xh[2], *xl[2], *ah, *al, *bh, *bl;     // panels; al, bl for 32-bit results only
+    float *xf[2];                                  // X in fp32, panels of 64 columns; for 32-bit results only
+    float *da, *db;                                // diagonals of A and B
+    long long offset, stride;                      // of the matrix in the [n, ld] arrays, worker included
+    int rows, cols, tall;
+    int rp, cp, sp;                                // rows, columns, short side, padded to the tile
+    int k_long, k_short;                           // inner dimensions in stages
+    unsigned tiles_sym, tiles_x;                   // signals that complete a phase
+    float scale;
+    int chunk0, chunks;                            // of the norm kernel
+};
+struct OrthTile {
+    uint32_t q;
+    uint16_t i, j;
+};
+struct ConvertUnit {
+    uint32_t q, r0, c0;                            // 32 rows, up to 4 panels
+};
+
+struct OrthArgs {
+    const OrthMat *mats;
+    const OrthTile *sym, *x;
+    int n_sym, n_x, steps;
+    unsigned *done;                                // [matrices] finished tiles
+    unsigned *ticket;                              // [matrices] norm kernel
+    float *partial, *inv;                          // [chunks], [matrices] 1 / (norm + eps)
+    const uint2 *chunk;                            // (matrix, chunk in it)
+    const ConvertUnit *unit;
+    const void *grad;
+    float *m;
+    float mu;
+    void *out;
+    int out_type;
+    unsigned *err;
+};
+
+// ------------------------------------------------------------------ element access
+template <typename T> __device__ __forceinline__ float to_f(T v);
+template <> __device__ __forceinline__ float to_f(float v) { return v; }
+template <> __device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <> __device__ __forceinline__ float to_f(__half v) { return __half2float(v); }
+
+// 8 consecutive elements, `n` of them wanted (the rest 0).
+template <typename T>
+__device__ __forceinline__ void load8(const T *p, int n, float (&v)[8]) {
+    if (n >= 8 && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
+        if constexpr (sizeof(T) == 4) {
+            const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
+            v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+        } else {
+            const uint4 a = *reinterpret_cast<const uint4 *>(p);
+            const T *e = reinterpret_cast<const T *>(&a);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = to_f<T>(e[k]);
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = k < n ? to_f<T>(p[k]) : 0.f;
+    }
+}
+
+// ------------------------------------------------------------------ |u|_F, momentum
+// HBM-bound: g read once (m read and written once).  The last CTA of a matrix adds the partial sums in their order.
+template <typename T>
+__global__ void __launch_bounds__(256) orth_norm_kernel(const OrthArgs a) {
+    __shared__ float red[8];
+    __shared__ int last;
+    const uint2 ck = a.chunk[blockIdx.x];
+    const OrthMat &M = a.mats[ck.x];
+    const T *g = static_cast<const T *>(a.grad) + M.offset;
+    float *m = a.m ? a.m + M.offset : nullptr;
+    const long long total = (long long)M.rows * M.cols, e0 = (long long)ck.y * kNormChunk;
+    const long long end = e0 + kNormChunk < total ? e0 + kNormChunk : total;
+    float sum = 0.f;
+    if (M.stride == M.cols) {
+        for (long long e = e0 + threadIdx.x * 8; e < end; e += 2048) {
+            const int n = end - e < 8 ? (int)(end - e) : 8;
+            float v[8], w[8];
+            load8(g + e, n, v);
+            if (m) {
+                load8(m + e, n, w);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) w[k] = __fadd_rn(__fmul_rn(a.mu, w[k]), v[k]), v[k] = __fadd_rn(v[k], __fmul_rn(a.mu, w[k]));
+                if (n == 8 && (reinterpret_cast<uintptr_t>(m + e) & 15) == 0) {
+                    reinterpret_cast<float4 *>(m + e)[0] = make_float4(w[0], w[1], w[2], w[3]);
+                    reinterpret_cast<float4 *>(m + e)[1] = make_float4(w[4], w[5], w[6], w[7]);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        if (k < n) m[e + k] = w[k];
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) sum = __fmaf_rn(v[k], v[k], sum);
+        }
+    } else {
+        for (long long e = e0 + threadIdx.x; e < end; e += 256) {
+            const long long r = e / M.cols, at = r * M.stride + (e - r * M.cols);
+            float v = to_f<T>(g[at]);
+            if (m) {
+                const float w = __fadd_rn(__fmul_rn(a.mu, m[at]), v);
+                m[at] = w;
+                v = __fadd_rn(v, __fmul_rn(a.mu, w));
+            }
+            sum = __fmaf_rn(v, v, sum);
+        }
+    }
+    for (int k = 16; k; k >>= 1) sum += __shfl_xor_sync(~0u, sum, k);
+    if (threadIdx.x % 32 == 0) red[threadIdx.x / 32] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        float s = 0.f;
+        for (int k = 0; k < 8; ++k) s += red[k];
+        a.partial[M.chunk0 + ck.y] = s;
+        __threadfence();
+        last = atomicAdd(&a.ticket[ck.x], 1u) == (unsigned)M.chunks - 1;
+        __threadfence();
+    }
+    __syncthreads();
+    if (!last) return;
+    float s = 0.f;
+    for (int k = threadIdx.x; k < M.chunks; k += 256) s += __ldcg(&a.partial[M.chunk0 + k]);
+    for (int k = 16; k; k >>= 1) s += __shfl_xor_sync(~0u, s, k);
+    __syncthreads();
+    if (threadIdx.x % 32 == 0) red[threadIdx.x / 32] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        s = 0.f;
+        for (int k = 0; k < 8; ++k) s += red[k];
+        a.inv[ck.x] = __fdiv_rn(1.f, __fadd_rn(__fsqrt_rn(s), kEps));
+        a.ticket[ck.x] = 0;                        // for the next call
+        a.done[ck.x] = 0;
+    }
+}
+
+// ------------------------------------------------------------------ X as panels
+__device__ __forceinline__ uint32_t pack_half2(float a, float b) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+// 8 values as one chunk of fp16 and one of what that leaves.
+__device__ __forceinline__ void split8(const float *v, uint4 &hi, uint4 &lo) {
+    uint32_t h[4], l[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        h[k] = pack_half2(v[2 * k], v[2 * k + 1]);
+        const float2 b = __half22float2(*reinterpret_cast<const __half2 *>(&h[k]));
+        l[k] = pack_half2(__fsub_rn(v[2 * k], b.x), __fsub_rn(v[2 * k + 1], b.y));
+    }
+    hi = make_uint4(h[0], h[1], h[2], h[3]);
+    lo = make_uint4(l[0], l[1], l[2], l[3]);
+}
+__device__ __forceinline__ void unpack8(const uint4 &p, float *v) {
+    const uint32_t w[4] = {p.x, p.y, p.z, p.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const float2 b = __half22float2(*reinterpret_cast<const __half2 *>(&w[k]));
+        v[2 * k] = b.x, v[2 * k + 1] = b.y;
+    }
+}
+__device__ __forceinline__ char *panel_at(__half *base, int rows, int panel) {
+    return reinterpret_cast<char *>(base) + (size_t)panel * rows * 128;
+}
+
+__device__ __forceinline__ float4 *wide_at(float *base, int rows, int row, int col) {
+    return reinterpret_cast<float4 *>(base + ((size_t)(col / 64) * rows + row) * 64 + col % 64);
+}
+
+// A thread makes one chunk of 8 columns per panel; the padding becomes 0.
+template <typename T>
+__global__ void __launch_bounds__(256) orth_convert_kernel(const OrthArgs a) {
+    const ConvertUnit u = a.unit[blockIdx.x];
+    const OrthMat &M = a.mats[u.q];
+    const int row = u.r0 + threadIdx.x / 8, c = threadIdx.x % 8;
+    if (row >= M.rp) return;
+    const float f = __fmul_rn(a.inv[u.q], kScale);
+    float v[4][8];
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+        const int col = u.c0 + p * 64 + c * 8;
+        const int n = row < M.rows ? M.cols - col : 0;
+        const long long at = M.offset + (long long)row * M.stride + col;
+        if (n > 0) {
+            load8(static_cast<const T *>(a.grad) + at, n, v[p]);
+            if (a.m) {
+                float w[8];
+                load8(a.m + at, n, w);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[p][k] = __fadd_rn(v[p][k], __fmul_rn(a.mu, w[k]));
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[p][k] = 0.f;
+        }
+    }
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+        const int col = u.c0 + p * 64;
+        if (col >= M.cp) break;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[p][k] = __fmul_rn(v[p][k], f);
+        uint4 hi, lo;
+        split8(v[p], hi, lo);
+        const uint32_t at = panel_chunk(row, c);
+        *reinterpret_cast<uint4 *>(panel_at(M.xh[0], M.rp, col / 64) + at) = hi;
+        *reinterpret_cast<uint4 *>(panel_at(M.xl[0], M.rp, col / 64) + at) = lo;
+        if (M.xf[0]) {
+            float4 *w = wide_at(M.xf[0], M.rp, row, col + c * 8);
+            w[0] = make_float4(v[p][0], v[p][1], v[p][2], v[p][3]);
+            w[1] = make_float4(v[p][4], v[p][5], v[p][6], v[p][7]);
+        }
+    }
+}
+
+// ------------------------------------------------------------------ products
+enum { kPhaseA = 0, kPhaseB = 1, kPhaseX = 2 };
+
+template <int CG, bool SPLIT>
+struct OrthJob {
+    const OrthArgs &a;
+    int first, every, per_step;
+    static constexpr int TN = tile_n(SPLIT);
+
+    struct Tile {
+        const OrthMat *M;
+        uint32_t q;
+        int i, j, n, phase, step, k_blocks, k_seg;
+        unsigned need;
+    };
+
+    __device__ __forceinline__ bool next(Tile &t, int k) const {
+        const long long at = first + (long long)k * every;
+        if (at >= (long long)per_step * a.steps) return false;
+        t.step = (int)(at / per_step);
+        int r = (int)(at - (long long)t.step * per_step);
+        const OrthTile *list = a.sym;
+        t.phase = kPhaseA;
+        if (r >= a.n_sym) r -= a.n_sym, t.phase = kPhaseB;
+        if (t.phase == kPhaseB && r >= a.n_sym) r -= a.n_sym, t.phase = kPhaseX, list = a.x;
+        const OrthTile e = list[r];
+        t.q = e.q, t.i = e.i, t.j = e.j;
+        t.M = a.mats + e.q;
+        const int width = t.phase == kPhaseX ? t.M->cp : t.M->sp;
+        t.n = width - t.j * TN < TN ? width - t.j * TN : TN;
+        t.k_seg = t.phase == kPhaseA ? t.M->k_long : t.M->k_short;
+        t.k_blocks = SPLIT ? 3 * t.k_seg : t.k_seg;
+        t.need = (unsigned)t.step * (2 * t.M->tiles_sym + t.M->tiles_x) + (unsigned)t.phase * t.M->tiles_sym;
+        return true;
+    }
+    __device__ __forceinline__ bool ready(Pipe<CG> &p, const Tile &t) const {
+        if (t.need && !p.wait_counter(a.done + t.q, t.need)) return false;
+        fence_async_proxy();
+        return true;
+    }
+    // Whether rows (in units of 256) of a symmetric matrix's panel are stored, or their mirror image is.
+    __device__ __forceinline__ static bool mirrored(int row256, int kb) { return row256 < (kb >> 2); }
+    __device__ __forceinline__ bool a_mn(const Tile &t, int kb) const {
+        const int k = SPLIT ? kb % t.k_seg : kb;
+        if (t.phase == kPhaseA) return t.M->tall;
+        if (t.phase == kPhaseX && t.M->tall) return false;
+        return mirrored(CG == 1 ? t.i >> 1 : t.i, k);
+    }
+    __device__ __forceinline__ bool b_mn(const Tile &t, int kb) const {
+        const int k = SPLIT ? kb % t.k_seg : kb;
+        if (t.phase == kPhaseA) return t.M->tall;
+        if (t.phase == kPhaseX && !t.M->tall) return true;
+        return mirrored(SPLIT ? t.j >> 1 : t.j, k);
+    }
+    __device__ __forceinline__ bool chunk_ends(const Tile &t, int kb) const {
+        if (kb + 1 == t.k_blocks) return true;
+        if (!SPLIT || kb + 1 < 2 * t.k_seg) return false;
+        return (kb + 1 - 2 * t.k_seg) % (t.phase == kPhaseX ? kChunkX : kChunkAB) == 0;
+    }
+    __device__ __forceinline__ int bf16() const { return 0; }
+    __device__ __forceinline__ uint32_t bytes(const Tile &t) const { return 128 * 128 + (uint32_t)(t.n / CG) * 128; }
+    // `count` rows from `row`, stage k, of a matrix with `rp` rows: either its panel k, or as columns of its rows 64 k..
+    __device__ __forceinline__ static void load_operand(__half *base, int rp, int row, int count, int k, bool mn,
+                                                        uint32_t dst, uint64_t *bar) {
+        if (!mn) {
+            bulk_copy_in(dst, panel_at(base, rp, k) + (size_t)row * 128, (uint32_t)count * 128, bar);
+        } else {
+            for (int p = 0; p < count / 64; ++p)
+                bulk_copy_in(dst + p * 8192, panel_at(base, rp, row / 64 + p) + (size_t)k * 8192, 8192, bar);
+        }
+    }
+    __device__ __forceinline__ void load(const Tile &t, int kb, uint32_t sa, uint32_t sb, uint64_t *bar) const {
+        const OrthMat &M = *t.M;
+        const int seg = SPLIT ? kb / t.k_seg : 2, k = SPLIT ? kb - seg * t.k_seg : kb;
+        const bool a_lo = seg == 1, b_lo = seg == 0;
+        const uint32_t rank = CG == 1 ? 0 : cluster_rank();
+        const int row_a = t.i * 128 * CG + (int)rank * 128, row_b = t.j * TN + (int)rank * (t.n / CG), nb = t.n / CG;
+        __half *xh = M.xh[t.step & 1], *xl = M.xl[t.step & 1];
+        const bool am = a_mn(t, kb), bm = b_mn(t, kb);
+        if (t.phase == kPhaseA) {
+            load_operand(a_lo ? xl : xh, M.rp, row_a, 128, k, am, sa, bar);
+            load_operand(b_lo ? xl : xh, M.rp, row_b, nb, k, bm, sb, bar);
+        } else if (t.phase == kPhaseB) {
+            load_operand(a_lo ? M.al : M.ah, M.sp, row_a, 128, k, am, sa, bar);
+            load_operand(b_lo ? M.al : M.ah, M.sp, row_b, nb, k, bm, sb, bar);
+        } else if (!M.tall) {
+            load_operand(a_lo ? M.bl : M.bh, M.sp, row_a, 128, k, am, sa, bar);
+            load_operand(b_lo ? xl : xh, M.rp, row_b, nb, k, bm, sb, bar);
+        } else {
+            load_operand(a_lo ? xl : xh, M.rp, row_a, 128, k, am, sa, bar);
+            load_operand(b_lo ? M.bl : M.bh, M.sp, row_b, nb, k, bm, sb, bar);
+        }
+    }
+
+    __device__ __forceinline__ void store_out(const OrthMat &M, int row, int col, const float (&v)[32]) const {
+        if (row >= M.rows || col >= M.cols) return;
+        const long long at = M.offset + (long long)row * M.stride + col;
+        const int n = M.cols - col < 32 ? M.cols - col : 32;
+        if (a.out_type == CSER_TYPE_F32) {
+            float *o = static_cast<float *>(a.out) + at;
+            if (n == 32 && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    reinterpret_cast<float4 *>(o)[k] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 32; ++k)
+                    if (k < n) o[k] = v[k];
+            }
+        } else {
+            uint32_t w[16];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+                if (a.out_type == CSER_TYPE_BF16) {
+                    const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * k], v[2 * k + 1]);
+                    w[k] = *reinterpret_cast<const uint32_t *>(&h);
+                } else {
+                    w[k] = pack_half2(v[2 * k], v[2 * k + 1]);
+                }
+            }
+            uint16_t *o = static_cast<uint16_t *>(a.out) + at;
+            if (n == 32 && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    reinterpret_cast<uint4 *>(o)[k] = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 32; ++k)
+                    if (k < n) o[k] = (uint16_t)(k & 1 ? w[k / 2] >> 16 : w[k / 2] & 0xffff);
+            }
+        }
+    }
+
+    __device__ __forceinline__ bool epilogue(Pipe<CG> &p, const Tile &t, typename Pipe<CG>::Turn &turn, int warp, int lane) const {
+        uint32_t tmem;
+        float sum[2][32];                                            // of a 32-bit result's chunks
+        const int half = t.n / 2, c0 = warp / 4 * half;              // this warp's columns of the tile
+        if (SPLIT) {
+            for (int kb = 0, done = 0; kb < t.k_blocks; ++kb) {
+                if (!chunk_ends(t, kb)) continue;
+                if (!p.take(turn, tmem)) return false;
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    float v[32];
+                    tmem_load32(tmem + c0 + b * 32, v);
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) sum[b][k] = __fadd_rn(done ? sum[b][k] : 0.f, v[k]);
+                }
+                p.release(turn, lane);
+                done = 1;
+            }
+        } else if (!p.take(turn, tmem)) {
+            return false;
+        }
+        const OrthMat &M = *t.M;
+        const int row = t.i * 128 * CG + (int)p.rank * 128 + warp % 4 * 32 + lane;
+        float d_row = 0.f;
+        if (t.phase != kPhaseA) {
+            unsigned seen;                                           // reached already: the products had to wait for it
+            asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(seen) : "l"(a.done + t.q) : "memory");
+            if (t.phase == kPhaseB) d_row = __ldcg(M.da + row);
+            else if (!M.tall) d_row = __ldcg(M.db + row);
+        }
+        const bool last = t.phase == kPhaseX && t.step == a.steps - 1;
+        __half *src_h = t.phase == kPhaseB ? M.ah : M.xh[t.step & 1], *src_l = t.phase == kPhaseB ? M.al : M.xl[t.step & 1];
+        __half *dst_h = t.phase == kPhaseA ? M.ah : t.phase == kPhaseB ? M.bh : M.xh[t.step & 1 ^ 1];
+        __half *dst_l = t.phase == kPhaseA ? M.al : t.phase == kPhaseB ? M.bl : M.xl[t.step & 1 ^ 1];
+        const int rp = t.phase == kPhaseX ? M.rp : M.sp;
+#pragma unroll(SPLIT ? 2 : 1)
+        for (int b = 0; b < (SPLIT ? 64 : half); b += 32) {
+            const int col = t.j * TN + c0 + b;
+            float v[32];
+            if (SPLIT) {
+#pragma unroll
+                for (int k = 0; k < 32; ++k) v[k] = sum[b / 32][k];
+            } else {
+                tmem_load32(tmem + c0 + b, v);
+                if (b + 32 >= half) p.release(turn, lane);
+            }
+            if (t.phase == kPhaseA) {
+#pragma unroll
+                for (int k = 0; k < 32; ++k) {
+                    if (col + k == row) {
+                        M.da[row] = v[k] * kUnscale2;
+                        v[k] = 0.f;
+                    }
+                    v[k] *= kUnscale;
+                }
+            } else {
+                float x[32];
+                if (SPLIT && t.phase == kPhaseX) {
+                    const float4 *w = wide_at(M.xf[t.step & 1], rp, row, col);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const float4 f = __ldcg(w + k);
+                        x[4 * k] = f.x, x[4 * k + 1] = f.y, x[4 * k + 2] = f.z, x[4 * k + 3] = f.w;
+                    }
+                } else
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const uint32_t at = panel_chunk(row, (col % 64) / 8 + k);
+                    unpack8(__ldcg(reinterpret_cast<const uint4 *>(panel_at(src_h, rp, col / 64) + at)), x + 8 * k);
+                    if (SPLIT || t.phase == kPhaseX) {
+                        float l[8];
+                        unpack8(__ldcg(reinterpret_cast<const uint4 *>(panel_at(src_l, rp, col / 64) + at)), l);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) x[8 * k + e] += l[e];
+                    }
+                }
+                if (t.phase == kPhaseB) {
+                    // x is A without its diagonal, times 2^12
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) {
+                        const float d = d_row + __ldcg(M.da + col + k);
+                        const float sq = __fmaf_rn(d, x[k], v[k] * kUnscale);
+                        if (col + k == row) {
+                            M.db[row] = __fmaf_rn(kC, __fmaf_rn(d_row, d_row, v[k] * kUnscale2), kB * d_row);
+                            v[k] = 0.f;
+                        } else {
+                            v[k] = __fmaf_rn(kC, sq, kB * x[k]);
+                        }
+                    }
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) {
+                        const float d = M.tall ? __ldcg(M.db + col + k) : d_row;
+                        v[k] = __fmaf_rn(kA + d, x[k], v[k] * kUnscale);
+                    }
+                }
+            }
+            if (last) {
+                const float f = kUnscale * M.scale;
+#pragma unroll
+                for (int k = 0; k < 32; ++k) v[k] *= f;
+                store_out(M, row, col, v);
+            } else {
+                if (SPLIT && t.phase == kPhaseX) {
+                    float4 *w = wide_at(M.xf[t.step & 1 ^ 1], rp, row, col);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) w[k] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    uint4 hi, lo;
+                    split8(v + 8 * k, hi, lo);
+                    const uint32_t at = panel_chunk(row, (col % 64) / 8 + k);
+                    *reinterpret_cast<uint4 *>(panel_at(dst_h, rp, col / 64) + at) = hi;
+                    if (SPLIT || t.phase == kPhaseX)
+                        *reinterpret_cast<uint4 *>(panel_at(dst_l, rp, col / 64) + at) = lo;
+                }
+            }
+        }
+        if (!last) {
+            __threadfence();
+            fence_async_proxy();                                     // the next phase reads through the copy engine
+            p.epi_sync();
+            if (warp == 0 && lane == 0)
+                asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(a.done + t.q) : "memory");
+        }
+        return true;
+    }
+};
+
+template <int CG, bool SPLIT>
+__global__ void __launch_bounds__(kThreads, 1) orth_products_kernel(const __grid_constant__ OrthArgs a) {
+    extern __shared__ unsigned char raw[];
+    Pipe<CG> p;
+    p.setup(raw, a.err);
+    OrthJob<CG, SPLIT> job{a, (int)blockIdx.x / CG, (int)gridDim.x / CG, 2 * a.n_sym + a.n_x};
+    p.run(job);
+    p.teardown();
+}
+
+}  // namespace
+
+// ------------------------------------------------------------------ host
+#define TRY(expr)                                                                                              \
+    do {                                                                                                       \
+        cudaError_t _e = (expr);                                                                               \
+        if (_e != cudaSuccess)                                                                                 \
+            return cser_internal_fail(_e == cudaErrorMemoryAllocation ? CSER_ERR_NOMEM : CSER_ERR_CUDA, "%s: %s", #expr, \
+                                      cudaGetErrorString(_e));                                                 \
+    } while (0)
+
+struct cser_orth {
+    struct Group {
+        int cg = 1, grid = 0, n_chunk = 0, n_unit = 0;
+        OrthArgs args{};
+        void *tables = nullptr;                    // one allocation for the lists and matrices
+    };
+    int device = 0, in_type = 0, out_type = 0;
+    bool split = false;
+    std::vector<Group> groups;
+    void *work = nullptr;                          // shared by the groups, which run one after the other
+    unsigned *err_host = nullptr;
+    long long launches = 0;
+};
+
+namespace {
+
+int type_size(int t) { return t == CSER_TYPE_F32 ? 4 : 2; }
+long long up(long long v, long long to) { return (v + to - 1) / to * to; }
+
+template <int CG, bool SPLIT>
+cudaError_t products_launch(const OrthArgs &a, int grid, cudaStream_t st) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = Pipe<CG>::kSharedBytes;
+    cfg.stream = st;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeCooperative;
+    at[0].val.cooperative = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = CG, at[1].val.clusterDim.y = 1, at[1].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = CG == 1 ? 1 : 2;
+    return cudaLaunchKernelEx(&cfg, orth_products_kernel<CG, SPLIT>, a);
+}
+template <int CG, bool SPLIT>
+cudaError_t products_setup(int &pairs) {
+    cudaError_t e = cudaFuncSetAttribute(orth_products_kernel<CG, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                         (int)Pipe<CG>::kSharedBytes);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(CG);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = Pipe<CG>::kSharedBytes;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = CG, at[0].val.clusterDim.y = 1, at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    return cudaOccupancyMaxActiveClusters(&pairs, orth_products_kernel<CG, SPLIT>, &cfg);
+}
+
+int orth_fail(cser_orth *h, int code, const char *what) {
+    cser_internal_fail(code, "cser_orth_create: %s", what);
+    cser_orth_destroy(h);
+    return code;
+}
+
+struct HostMat {
+    long long offset, rows, cols, stride;
+    float scale;
+    int worker;
+};
+
+// Padded dimensions and workspace of one matrix.
+void shape_of(const HostMat &m, int cg, OrthMat &M) {
+    M = OrthMat{};
+    M.rows = (int)m.rows, M.cols = (int)m.cols, M.tall = m.rows > m.cols;
+    M.rp = (int)up(m.rows, 128 * cg), M.cp = (int)up(m.cols, 128 * cg), M.sp = M.tall ? M.cp : M.rp;
+    M.k_long = (int)(up(M.tall ? m.rows : m.cols, 64) / 64), M.k_short = (int)(up(M.tall ? m.cols : m.rows, 64) / 64);
+    M.offset = m.offset, M.stride = m.stride, M.scale = m.scale;
+}
+size_t work_of(const OrthMat &M, bool split) {
+    return (size_t)M.rp * M.cp * 2 * (split ? 8 : 4) + (size_t)M.sp * M.sp * 2 * (split ? 4 : 2) + (size_t)M.sp * 8;
+}
+
+int build_group(cser_orth *h, cser_orth::Group &G, const std::vector<HostMat> &ms, int cg) {
+    std::vector<OrthMat> mats(ms.size());
+    std::vector<OrthTile> sym, xs;
+    std::vector<uint2> chunk;
+    std::vector<ConvertUnit> unit;
+    size_t at = 0;
+    char *base = static_cast<char *>(h->work);
+    int chunk0 = 0;
+    for (size_t q = 0; q < ms.size(); ++q) {
+        OrthMat &M = mats[q];
+        shape_of(ms[q], cg, M);
+        const size_t xb = (size_t)M.rp * M.cp * 2, ab = (size_t)M.sp * M.sp * 2;
+        auto take = [&](size_t b) { char *p = base + at; at += b; return reinterpret_cast<__half *>(p); };
+        M.xh[0] = take(xb), M.xl[0] = take(xb), M.xh[1] = take(xb), M.xl[1] = take(xb), M.ah = take(ab), M.bh = take(ab);
+        if (h->split) {
+            M.al = take(ab), M.bl = take(ab);
+            for (float *&x : M.xf) x = reinterpret_cast<float *>(take(2 * xb));
+        }
+        M.da = reinterpret_cast<float *>(take((size_t)M.sp * 4)), M.db = reinterpret_cast<float *>(take((size_t)M.sp * 4));
+        M.chunk0 = chunk0, M.chunks = (int)(up((long long)M.rows * M.cols, kNormChunk) / kNormChunk);
+        chunk0 += M.chunks;
+        for (int c = 0; c < M.chunks; ++c) chunk.push_back(make_uint2((unsigned)q, (unsigned)c));
+        for (int r = 0; r < M.rp; r += 32)
+            for (int c = 0; c < M.cp; c += 256) unit.push_back({(uint32_t)q, (uint32_t)r, (uint32_t)c});
+        const int tm = 128 * cg, tn = tile_n(h->split);
+        for (int j = 0; j * tn < M.sp; ++j)
+            for (int i = 0; i * tm < M.sp; ++i)
+                if (i * tm / 256 >= j * tn / 256) sym.push_back({(uint32_t)q, (uint16_t)i, (uint16_t)j}), M.tiles_sym += cg;
+        if (M.tall) {
+            for (int i = 0; i * tm < M.rp; ++i)
+                for (int j = 0; j * tn < M.cp; ++j) xs.push_back({(uint32_t)q, (uint16_t)i, (uint16_t)j}), M.tiles_x += cg;
+        } else {
+            for (int j = 0; j * tn < M.cp; ++j)
+                for (int i = 0; i * tm < M.rp; ++i) xs.push_back({(uint32_t)q, (uint16_t)i, (uint16_t)j}), M.tiles_x += cg;
+        }
+    }
+    const size_t n = ms.size();
+    size_t bytes = 0;
+    auto place = [&](size_t b) { const size_t p = bytes; bytes += (b + 255) / 256 * 256; return p; };
+    const size_t o_mat = place(n * sizeof(OrthMat)), o_sym = place(sym.size() * sizeof(OrthTile)),
+                 o_x = place(xs.size() * sizeof(OrthTile)), o_ck = place(chunk.size() * sizeof(uint2)),
+                 o_un = place(unit.size() * sizeof(ConvertUnit)), o_done = place(n * 4), o_tick = place(n * 4),
+                 o_inv = place(n * 4), o_part = place((size_t)chunk0 * 4);
+    TRY(cudaMalloc(&G.tables, bytes));
+    char *t = static_cast<char *>(G.tables);
+    TRY(cudaMemset(t + o_done, 0, bytes - o_done));
+    TRY(cudaMemcpy(t + o_mat, mats.data(), n * sizeof(OrthMat), cudaMemcpyHostToDevice));
+    TRY(cudaMemcpy(t + o_sym, sym.data(), sym.size() * sizeof(OrthTile), cudaMemcpyHostToDevice));
+    TRY(cudaMemcpy(t + o_x, xs.data(), xs.size() * sizeof(OrthTile), cudaMemcpyHostToDevice));
+    TRY(cudaMemcpy(t + o_ck, chunk.data(), chunk.size() * sizeof(uint2), cudaMemcpyHostToDevice));
+    TRY(cudaMemcpy(t + o_un, unit.data(), unit.size() * sizeof(ConvertUnit), cudaMemcpyHostToDevice));
+    OrthArgs &A = G.args;
+    A.mats = reinterpret_cast<OrthMat *>(t + o_mat);
+    A.sym = reinterpret_cast<OrthTile *>(t + o_sym), A.n_sym = (int)sym.size();
+    A.x = reinterpret_cast<OrthTile *>(t + o_x), A.n_x = (int)xs.size();
+    A.chunk = reinterpret_cast<uint2 *>(t + o_ck), A.unit = reinterpret_cast<ConvertUnit *>(t + o_un);
+    A.done = reinterpret_cast<unsigned *>(t + o_done), A.ticket = reinterpret_cast<unsigned *>(t + o_tick);
+    A.inv = reinterpret_cast<float *>(t + o_inv), A.partial = reinterpret_cast<float *>(t + o_part);
+    A.out_type = h->out_type;
+    G.n_chunk = (int)chunk.size(), G.n_unit = (int)unit.size(), G.cg = cg;
+    return CSER_OK;
+}
+
+template <typename T>
+void prologue_launch(const cser_orth::Group &G, const OrthArgs &a, cudaStream_t st) {
+    orth_norm_kernel<T><<<G.n_chunk, 256, 0, st>>>(a);
+    orth_convert_kernel<T><<<G.n_unit, 256, 0, st>>>(a);
+}
+
+}  // namespace
+
+extern "C" {
+
+cser_orth_handle cser_orth_create(int32_t n_workers, int64_t ld, int32_t n_matrices, const int64_t *offset,
+                                  const int64_t *rows, const int64_t *cols, const int64_t *row_stride,
+                                  const float *scale, int32_t steps, int32_t in_type, int32_t out_type) {
+    auto bad = [](const char *what) { cser_internal_fail(CSER_ERR_INVALID, "cser_orth_create: %s", what); return nullptr; };
+    if (n_workers < 1 || ld < 1 || n_matrices < 1) return bad("n_workers, ld and n_matrices must be positive");
+    if (!offset || !rows || !cols) return bad("offset, rows and cols must not be NULL");
+    if (steps < 1 || steps > 16) return bad("steps must be in 1..16");
+    if (in_type < 0 || in_type > 2 || out_type < 0 || out_type > 2) return bad("unknown element type");
+    if ((long long)n_workers * n_matrices > (1 << 20)) return bad("more than 2^20 matrices");
+    std::vector<HostMat> all;
+    cser_orth *h = nullptr;
+    try {
+        std::vector<std::pair<long long, long long>> span;
+        for (int k = 0; k < n_matrices; ++k) {
+            const long long st = row_stride ? row_stride[k] : cols[k];
+            if (rows[k] < 1 || cols[k] < 1 || rows[k] > 65536 || cols[k] > 65536) return bad("rows and cols must be in 1..65536");
+            if (st < cols[k] || st > ld) return bad("row_stride must be at least cols and at most ld");
+            if (offset[k] < 0 || offset[k] > ld || offset[k] + (rows[k] - 1) * st + cols[k] > ld)
+                return bad("a matrix reaches outside the vector");
+            if (scale && !isfinite(scale[k])) return bad("scale must be finite");
+        }
+        for (int w = 0; w < n_workers; ++w)
+            for (int k = 0; k < n_matrices; ++k)
+                all.push_back({(long long)w * ld + offset[k], rows[k], cols[k], row_stride ? row_stride[k] : cols[k],
+                               scale ? scale[k] : 1.f, w});
+        h = new cser_orth;
+        h->in_type = in_type, h->out_type = out_type, h->split = out_type == CSER_TYPE_F32;
+        if (cudaGetDevice(&h->device) != cudaSuccess) {
+            orth_fail(h, CSER_ERR_CUDA, "no CUDA device");
+            return nullptr;
+        }
+        int pairs[3] = {0, 0, 0};
+        cudaError_t er = h->split ? products_setup<1, true>(pairs[1]) : products_setup<1, false>(pairs[1]);
+        if (er == cudaSuccess) er = h->split ? products_setup<2, true>(pairs[2]) : products_setup<2, false>(pairs[2]);
+        if (er != cudaSuccess || pairs[1] < 1 || pairs[2] < 1) {
+            orth_fail(h, CSER_ERR_CUDA, er != cudaSuccess ? cudaGetErrorString(er) : "the kernel does not fit this GPU");
+            return nullptr;
+        }
+        const int cg = 1;
+        // Groups that fit the workspace, one after the other.
+        std::vector<std::vector<HostMat>> parts;
+        size_t most = 0, now = 0;
+        for (const HostMat &m : all) {
+            OrthMat M;
+            shape_of(m, cg, M);
+            const size_t need = work_of(M, h->split);
+            if (parts.empty() || now + need > kGroupBytes) parts.emplace_back(), now = 0;
+            parts.back().push_back(m);
+            now += need;
+            if (now > most) most = now;
+        }
+        er = cudaMalloc(&h->work, most);
+        if (er == cudaSuccess) er = cudaHostAlloc(reinterpret_cast<void **>(&h->err_host), 64, cudaHostAllocMapped | cudaHostAllocPortable);
+        unsigned *err_dev = nullptr;
+        if (er == cudaSuccess) *h->err_host = 0, er = cudaHostGetDevicePointer(reinterpret_cast<void **>(&err_dev), h->err_host, 0);
+        if (er != cudaSuccess) {
+            orth_fail(h, er == cudaErrorMemoryAllocation ? CSER_ERR_NOMEM : CSER_ERR_CUDA, cudaGetErrorString(er));
+            return nullptr;
+        }
+        h->groups.resize(parts.size());
+        for (size_t g = 0; g < parts.size(); ++g) {
+            cser_orth::Group &G = h->groups[g];
+            if (build_group(h, G, parts[g], cg) != CSER_OK) {
+                cser_orth_destroy(h);
+                return nullptr;
+            }
+            G.args.steps = steps, G.args.err = err_dev;
+            const int widest = G.args.n_sym > G.args.n_x ? G.args.n_sym : G.args.n_x;
+            G.grid = (widest < pairs[cg] ? widest : pairs[cg]) * cg;
+        }
+        return h;
+    } catch (const std::bad_alloc &) {
+        if (h) cser_orth_destroy(h);
+        cser_internal_fail(CSER_ERR_NOMEM, "cser_orth_create: host allocation failed");
+        return nullptr;
+    }
+}
+
+int cser_orth_apply(cser_orth_handle h, const void *grad, float *m, float mu, void *out, void *stream) {
+    if (!h) return cser_internal_fail(CSER_ERR_INVALID, "cser_orth_apply: NULL handle");
+    int dev = -1;
+    TRY(cudaGetDevice(&dev));
+    if (dev != h->device)
+        return cser_internal_fail(CSER_ERR_INVALID, "handle belongs to device %d, current device is %d", h->device, dev);
+    if (*reinterpret_cast<volatile unsigned *>(h->err_host))
+        return cser_internal_fail(CSER_ERR_CUDA, "a device-side wait ran out in an earlier cser_orth_apply: its results are incomplete");
+    if (int rc = cser_internal_check_ptr(grad, "cser_orth_apply: grad")) return rc;
+    if (int rc = cser_internal_check_ptr(out, "cser_orth_apply: out")) return rc;
+    if (m)
+        if (int rc = cser_internal_check_ptr(m, "cser_orth_apply: m")) return rc;
+    if (m && !(mu >= 0.f && mu < 1.f)) return cser_internal_fail(CSER_ERR_INVALID, "cser_orth_apply: mu must be in [0, 1)");
+    if ((uintptr_t)grad % type_size(h->in_type) || (uintptr_t)out % type_size(h->out_type) || (uintptr_t)m % 4)
+        return cser_internal_fail(CSER_ERR_INVALID, "cser_orth_apply: a pointer is not aligned to its element type");
+    if (grad == out && h->in_type != h->out_type)
+        return cser_internal_fail(CSER_ERR_INVALID, "cser_orth_apply: out may be grad only where the types are the same");
+    if (m && (static_cast<const void *>(m) == grad || static_cast<const void *>(m) == out))
+        return cser_internal_fail(CSER_ERR_INVALID, "cser_orth_apply: m must be an array of its own");
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    for (cser_orth::Group &G : h->groups) {
+        OrthArgs a = G.args;
+        a.grad = grad, a.m = m, a.mu = mu, a.out = out;
+        if (h->in_type == CSER_TYPE_F32) prologue_launch<float>(G, a, st);
+        else if (h->in_type == CSER_TYPE_BF16) prologue_launch<__nv_bfloat16>(G, a, st);
+        else prologue_launch<__half>(G, a, st);
+        TRY(cudaGetLastError());
+        if (h->split) TRY((products_launch<1, true>(a, G.grid, st)));
+        else TRY((products_launch<1, false>(a, G.grid, st)));
+        h->launches += 3;
+    }
+    return CSER_OK;
+}
+
+void cser_orth_destroy(cser_orth_handle h) {
+    if (!h) return;
+    for (cser_orth::Group &G : h->groups)
+        if (G.tables) cudaFree(G.tables);
+    if (h->work) cudaFree(h->work);
+    if (h->err_host) cudaFreeHost(h->err_host);
+    delete h;
+}
+
+int64_t cser_orth_launch_count(cser_orth_handle h) { return h ? h->launches : 0; }
+
+}  // extern "C"

@@ -1,0 +1,110 @@
+"""ctypes binding of the operators of ``include/cser_train.h`` - argument marshalling only.
+
+They live in the same ``libcser.so`` as the optimizer step (``binding``) and surround it in a training step:
+``LinearCrossEntropy`` gives the loss of a language model's head and its gradient, ``Orthogonalizer`` turns the
+matrices inside the flat [n_workers, d] gradient into orthogonalised updates that ``binding.CSER.step`` takes.
+"""
+import ctypes
+
+import torch
+
+from .binding import CSERError, _check, _ptr, _stream, cser_last_error
+from .binding import lib as _base_lib
+
+TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+_lib = None
+
+
+class _XentInputs(ctypes.Structure):
+    _fields_ = [("hidden", ctypes.c_void_p), ("hidden_row_stride", ctypes.c_int64),
+                ("hidden_worker_stride", ctypes.c_int64), ("weight", ctypes.c_void_p),
+                ("weight_row_stride", ctypes.c_int64), ("weight_worker_stride", ctypes.c_int64),
+                ("target", ctypes.c_void_p), ("ignore_index", ctypes.c_int64), ("tokens", ctypes.c_int64)]
+
+
+def lib():
+    """libcser.so with the signatures of cser_train.h."""
+    global _lib
+    if _lib is not None:
+        return _lib
+    L, c = _base_lib(), ctypes
+    p, i32, i64, f32 = c.c_void_p, c.c_int32, c.c_int64, c.c_float
+    for name, res, args in (
+            ("cser_orth_create", p, [i32, i64, i32, p, p, p, p, p, i32, i32, i32]),
+            ("cser_orth_apply", c.c_int, [p, p, p, f32, p, p]),
+            ("cser_orth_destroy", None, [p]),
+            ("cser_orth_launch_count", i64, [p]),
+            ("cser_xent_create", p, [i32, i64, i64, i64, i32, i64]),
+            ("cser_xent_loss", c.c_int, [p, c.POINTER(_XentInputs), p, p, p]),
+            ("cser_xent_grad", c.c_int, [p, c.POINTER(_XentInputs), p, p, p, p, i64, p]),
+            ("cser_xent_destroy", None, [p]),
+            ("cser_xent_launch_count", i64, [p])):
+        if not hasattr(L, name): continue
+        f = getattr(L, name)
+        f.restype, f.argtypes = res, args
+    _lib = L
+    return L
+
+
+def _want(ok, what):
+    if not ok:
+        raise CSERError(what)
+
+
+class Orthogonalizer:
+    """Plan for the matrices ``[(offset, rows, cols), ...]`` inside each row of an [n_workers, ld] array.
+
+    ``row_strides``: elements from one row of a matrix to the next (default: cols); ``scales``: factor of each
+    result (default: 1).  See cser_orth_create.
+    """
+
+    def __init__(self, matrices, n_workers, ld, in_dtype=torch.float32, out_dtype=torch.float32, row_strides=None,
+                 scales=None, steps=5):
+        self.h = None
+        _want(in_dtype in TYPES and out_dtype in TYPES, "Orthogonalizer: types are float32, bfloat16 and float16")
+        k = len(matrices)
+        i64 = ctypes.c_int64 * max(1, k)
+        for name, extra in (("row_strides", row_strides), ("scales", scales)):
+            _want(extra is None or len(extra) == k, f"Orthogonalizer: {name} needs one value per matrix")
+        self.n, self.ld, self.in_dtype, self.out_dtype = int(n_workers), int(ld), in_dtype, out_dtype
+        off, rows, cols = (i64(*(int(m[j]) for m in matrices)) for j in range(3))
+        stride = i64(*map(int, row_strides)) if row_strides is not None else None
+        scale = (ctypes.c_float * max(1, k))(*map(float, scales)) if scales is not None else None
+        h = lib().cser_orth_create(self.n, self.ld, k, off, rows, cols, stride, scale, int(steps), TYPES[in_dtype],
+                                   TYPES[out_dtype])
+        if not h:
+            raise CSERError(f"cser_orth_create failed: {cser_last_error()}")
+        self.h = ctypes.c_void_p(h)
+
+    def apply(self, grad, out=None, momentum=None, mu=0.0, stream=None):
+        """grad [n, ld] -> out [n, ld] (made if not given: zeros outside the matrices); momentum is updated in place."""
+        size = (self.n, self.ld)
+        _want(grad.is_cuda and grad.dtype == self.in_dtype and grad.shape == size and grad.is_contiguous(),
+              f"Orthogonalizer: grad must be a contiguous CUDA {self.in_dtype} tensor of shape {size}")
+        if out is None:
+            out = torch.zeros(size, dtype=self.out_dtype, device=grad.device)
+        _want(out.is_cuda and out.dtype == self.out_dtype and out.shape == size and out.is_contiguous(),
+              f"Orthogonalizer: out must be a contiguous CUDA {self.out_dtype} tensor of shape {size}")
+        if momentum is not None:
+            _want(momentum.is_cuda and momentum.dtype == torch.float32 and momentum.shape == size and
+                  momentum.is_contiguous(), f"Orthogonalizer: momentum must be a contiguous CUDA float32 tensor of shape {size}")
+        _check(_lib.cser_orth_apply(self.h, grad.data_ptr(), None if momentum is None else momentum.data_ptr(), mu,
+                                    out.data_ptr(), _stream(stream)), "cser_orth_apply")
+        return out
+
+    @property
+    def launches(self):
+        return int(lib().cser_orth_launch_count(self.h))
+
+    def close(self):
+        if self.h is not None:
+            torch.cuda.synchronize()
+            lib().cser_orth_destroy(self.h)
+            self.h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
