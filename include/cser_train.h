@@ -6,8 +6,8 @@
  * Same library (libcser.so), error codes, cser_last_error() and conventions as cser.h: pointers are device memory of
  * the GPU that was current when the handle was created; `stream` is a cudaStream_t as void* (NULL = legacy default
  * stream); a call only enqueues work and returns; calls on one handle must not overlap, on the host or on the GPU (a
- * handle's workspace serves one call at a time); nothing is allocated after creation.  Calls may be captured in a CUDA
- * graph and replayed.  No call aborts, throws or traps on the device.  Every wait inside a kernel is bounded to about a
+ * handle's workspace serves one call at a time).  Calls may be captured in a CUDA
+ * graph and replayed (but see cser_xent_create for unaligned inputs).  No call aborts, throws or traps on the device.  Every wait inside a kernel is bounded to about a
  * second; one that ran out (the GPU withheld from part of a launch, say) ends the kernel and every later call on the
  * handle returns CSER_ERR_CUDA, the results of that call being incomplete.
  */
@@ -95,7 +95,9 @@ typedef struct cser_xent_inputs {
 /*
  * Workspace for up to max_tokens tokens per worker.  piece: vocabulary entries per piece of the gradient (rounded up to
  * a multiple of 256), 0 = chosen so that a piece of dz takes at most 256 MB.  1 <= vocab <= 2^24, 1 <= dim <= 65536,
- * 1 <= n_workers * max_tokens <= 2^24.  Returns NULL on failure.
+ * 1 <= n_workers * max_tokens <= 2^24, n_workers * vocab and n_workers * ceil(max_tokens / 128) * ceil(vocab / 256) at most 2^30.
+ * hidden or weights whose rows are not 16 bytes apart (or not 16-byte aligned) are first copied: the buffer for that is
+ * allocated on the first such call, which must not be under stream capture.  Returns NULL on failure.
  */
 cser_xent_handle cser_xent_create(int32_t n_workers, int64_t max_tokens, int64_t vocab, int64_t dim, int32_t type,
                                   int64_t piece);

@@ -191,10 +191,6 @@ __global__ void __launch_bounds__(256) orth_norm_kernel(const OrthArgs a) {
 }
 
 // ------------------------------------------------------------------ X as panels
-__device__ __forceinline__ uint32_t pack_half2(float a, float b) {
-    const __half2 h = __floats2half2_rn(a, b);
-    return *reinterpret_cast<const uint32_t *>(&h);
-}
 // 8 values as one chunk of fp16 and one of what that leaves.
 __device__ __forceinline__ void split8(const float *v, uint4 &hi, uint4 &lo) {
     uint32_t h[4], l[4];
@@ -363,45 +359,6 @@ struct OrthJob {
         }
     }
 
-    __device__ __forceinline__ void store_out(const OrthMat &M, int row, int col, const float (&v)[32]) const {
-        if (row >= M.rows || col >= M.cols) return;
-        const long long at = M.offset + (long long)row * M.stride + col;
-        const int n = M.cols - col < 32 ? M.cols - col : 32;
-        if (a.out_type == CSER_TYPE_F32) {
-            float *o = static_cast<float *>(a.out) + at;
-            if (n == 32 && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
-#pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    reinterpret_cast<float4 *>(o)[k] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
-            } else {
-#pragma unroll
-                for (int k = 0; k < 32; ++k)
-                    if (k < n) o[k] = v[k];
-            }
-        } else {
-            uint32_t w[16];
-#pragma unroll
-            for (int k = 0; k < 16; ++k) {
-                if (a.out_type == CSER_TYPE_BF16) {
-                    const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * k], v[2 * k + 1]);
-                    w[k] = *reinterpret_cast<const uint32_t *>(&h);
-                } else {
-                    w[k] = pack_half2(v[2 * k], v[2 * k + 1]);
-                }
-            }
-            uint16_t *o = static_cast<uint16_t *>(a.out) + at;
-            if (n == 32 && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    reinterpret_cast<uint4 *>(o)[k] = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
-            } else {
-#pragma unroll
-                for (int k = 0; k < 32; ++k)
-                    if (k < n) o[k] = (uint16_t)(k & 1 ? w[k / 2] >> 16 : w[k / 2] & 0xffff);
-            }
-        }
-    }
-
     __device__ __forceinline__ bool epilogue(Pipe<CG> &p, const Tile &t, typename Pipe<CG>::Turn &turn, int warp, int lane) const {
         uint32_t tmem;
         float sum[2][32];                                            // of a 32-bit result's chunks
@@ -503,7 +460,8 @@ struct OrthJob {
                 const float f = kUnscale * M.scale;
 #pragma unroll
                 for (int k = 0; k < 32; ++k) v[k] *= f;
-                store_out(M, row, col, v);
+                if (row < M.rows && col < M.cols)
+                    store_row32(a.out, M.offset + (long long)row * M.stride + col, M.cols - col, a.out_type, v);
             } else {
                 if (SPLIT && t.phase == kPhaseX) {
                     float4 *w = wide_at(M.xf[t.step & 1 ^ 1], rp, row, col);

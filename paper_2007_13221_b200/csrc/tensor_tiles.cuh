@@ -155,6 +155,46 @@ __device__ __forceinline__ uint32_t instr_desc(int bf16, bool a_mn, bool b_mn, i
 // Byte offset of the 16-byte chunk `c` (0..7) of row r inside a panel.
 __device__ __forceinline__ uint32_t panel_chunk(uint32_t row, uint32_t c) { return row * 128 + ((c ^ (row & 7)) << 4); }
 
+// ------------------------------------------------------------------ rows of results
+__device__ __forceinline__ uint32_t pack_half2(float a, float b) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+__device__ __forceinline__ uint32_t pack_bf162(float a, float b) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+// min(n, 32) values to elements at, at + 1, ... of an array of CSER_TYPE_* `type`; 16 bytes at a time where they are aligned.
+__device__ __forceinline__ void store_row32(void *base, long long at, int n, int type, const float (&v)[32]) {
+    if (type == CSER_TYPE_F32) {
+        float *o = static_cast<float *>(base) + at;
+        if (n >= 32 && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                reinterpret_cast<float4 *>(o)[k] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 32; ++k)
+                if (k < n) o[k] = v[k];
+        }
+    } else {
+        uint32_t w[16];
+#pragma unroll
+        for (int k = 0; k < 16; ++k)
+            w[k] = type == CSER_TYPE_BF16 ? pack_bf162(v[2 * k], v[2 * k + 1]) : pack_half2(v[2 * k], v[2 * k + 1]);
+        uint16_t *o = static_cast<uint16_t *>(base) + at;
+        if (n >= 32 && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                reinterpret_cast<uint4 *>(o)[k] = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 32; ++k)
+                if (k < n) o[k] = (uint16_t)(k & 1 ? w[k / 2] >> 16 : w[k / 2] & 0xffff);
+        }
+    }
+}
+
 // ------------------------------------------------------------------ the pipeline
 template <int CG>
 struct Pipe {

@@ -1,0 +1,673 @@
+// Softmax cross entropy of a linear head over a large vocabulary and its gradient (cser_xent_* of include/cser_train.h).
+//
+//   z = h W^T,  lse = log sum exp z,  loss = lse - z[target];    dz = (exp(z - lse) - [target]) dloss,  dh = dz W,  dW = dz^T h
+//
+// The logits are never kept.  cser_xent_loss: one kernel of 128 x 256 tiles of z whose epilogue reduces its tile to a
+// maximum and a sum of exponentials per row and half tile, and one that joins them.  cser_xent_grad: for each piece of
+// the vocabulary a kernel computes the tiles of z again and leaves dz in 16 bits, as panels (tensor_tiles.cuh), and
+// one kernel makes from them the piece's rows of dW (inner dimension: tokens) and the piece's share of dh (inner dimension: the piece).
+// Every operand is read where it lies: the products that need dz, h or W the other way round take the same tiles with the other majorness.
+//
+// Bound.  6 T V D multiply-adds' flops (8 with z computed again) against 2 V D elements of W and dW moved: the tensor cores for
+// T above about 500, the read of W (and the write of dW) below.
+//
+// Rounding.  dz is rounded to the operands' type, 8 (bf16) or 11 (fp16) bits, as any product on these inputs has to.
+// It is held relative to the worker's largest |dloss| (times 2^12 for fp16, whose smallest normal number is above 1 / V for a
+// large vocabulary) and the factor is put back in fp32 at the end: for a mean over tokens dz is p - [target] itself, not p / T rounded.
+#include <cuda.h>
+#include <cuda_runtime.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <math.h>
+#include <stdint.h>
+#include <stdio.h>
+#include <new>
+
+#include "cser_train.h"
+#include "train_host.h"
+
+namespace {
+
+#include "tensor_tiles.cuh"
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLowest = -1e30f;                  // below every logit, and finite times log2(e)
+constexpr size_t kPieceBytes = 256ull << 20;
+
+// 2^x, flushing: the instruction.
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+struct XentArgs {
+    CUtensorMap h, w;                              // (dim, row, worker), boxes of 64 x 64
+    int n, tokens, vocab, dim;
+    int h_workers, w_workers;                      // 1: one array for all workers
+    int bf16, type;
+    int token_tiles, piece0, piece_n;              // vocabulary entries of this launch
+    int tp;                                        // rows of a dz panel
+    // loss
+    float2 *part;                                  // [n * tokens][parts] maximum and sum
+    int parts;
+    float *z_target;                               // [n * tokens]
+    const int64_t *target;
+    int64_t ignore;
+    float *loss, *lse_out;
+    // gradient
+    const float *lse, *dloss;
+    float *ratio;                                  // [n * tokens] dloss relative to the largest, times the type's scale
+    float *unscale;                                // [n] what takes that back
+    char *dz;                                      // [n][piece / 64 panels][tp rows][128 bytes]
+    size_t dz_worker;
+    float *acc;                                    // [n][splits][acc_rows][acc_cols] dh of the pieces so far
+    int acc_rows, acc_cols, splits, first_piece, last_piece;
+    void *dh, *dw;
+    long long dw_stride;
+    unsigned *err;
+};
+
+// ------------------------------------------------------------------ logits, tile by tile
+template <int CG, bool GRAD>
+struct LogitsJob {
+    const XentArgs &a;
+    int first, every, vocab_tiles;
+
+    struct Tile {
+        int w, i, j, n, k_blocks;
+    };
+    __device__ __forceinline__ bool next(Tile &t, int k) const {
+        const int at = first + k * every, per = a.token_tiles * vocab_tiles;
+        t.w = at / per;
+        if (t.w >= a.n) return false;
+        const int r = at - t.w * per;
+        t.j = r / a.token_tiles, t.i = r - t.j * a.token_tiles;
+        t.n = 256;
+        t.k_blocks = (a.dim + 63) / 64;
+        return true;
+    }
+    __device__ __forceinline__ bool ready(Pipe<CG> &, const Tile &) const { return true; }
+    __device__ __forceinline__ bool a_mn(const Tile &, int) const { return false; }
+    __device__ __forceinline__ bool b_mn(const Tile &, int) const { return false; }
+    __device__ __forceinline__ bool chunk_ends(const Tile &t, int kb) const { return kb + 1 == t.k_blocks; }
+    __device__ __forceinline__ int bf16() const { return a.bf16; }
+    __device__ __forceinline__ uint32_t bytes(const Tile &) const { return Pipe<CG>::kStageBytes; }
+    __device__ __forceinline__ void load(const Tile &t, int kb, uint32_t sa, uint32_t sb, uint64_t *bar) const {
+        const int rank = CG == 1 ? 0 : (int)cluster_rank();
+        const int hw = a.h_workers == 1 ? 0 : t.w, ww = a.w_workers == 1 ? 0 : t.w;
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            tensor_copy_in(sa + k * 8192, &a.h, kb * 64, t.i * 128 * CG + rank * 128 + k * 64, hw, bar);
+#pragma unroll
+        for (int k = 0; k < 4 / CG; ++k)
+            tensor_copy_in(sb + k * 8192, &a.w, kb * 64, a.piece0 + t.j * 256 + rank * 128 + k * 64, ww, bar);
+    }
+    __device__ __forceinline__ bool epilogue(Pipe<CG> &p, const Tile &t, typename Pipe<CG>::Turn &turn, int warp, int lane) const {
+        const int row = t.i * 128 * CG + (int)p.rank * 128 + warp % 4 * 32 + lane;
+        const int c0 = warp / 4 * 128;
+        const bool live = row < a.tokens;
+        const size_t at = (size_t)t.w * a.tokens + row;
+        int target = -1;
+        if (live) {
+            const int64_t y = a.target[at];
+            if (y >= 0 && y < a.vocab && y != a.ignore) target = (int)y;
+        }
+        uint32_t tmem;
+        if constexpr (!GRAD) {
+            if (!p.take(turn, tmem)) return false;
+            float m = kLowest, s = 0.f;
+#pragma unroll 1
+            for (int b = 0; b < 128; b += 32) {
+                const int col = t.j * 256 + c0 + b;
+                float v[32];
+                tmem_load32(tmem + c0 + b, v);
+                if (b == 96) p.release(turn, lane);
+                if (col + 32 > a.vocab) {
+#pragma unroll
+                    for (int k = 0; k < 32; ++k)
+                        if (col + k >= a.vocab) v[k] = -INFINITY;
+                }
+                float top = m;
+#pragma unroll
+                for (int k = 0; k < 32; ++k) top = fmaxf(top, v[k]);
+                float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int k = 0; k < 32; ++k) sum[k % 4] += exp2_fast((v[k] - top) * kLog2e);
+                s = __fmaf_rn(s, exp2_fast((m - top) * kLog2e), (sum[0] + sum[1]) + (sum[2] + sum[3]));
+                m = top;
+                const unsigned off = (unsigned)(target - col);
+                if (off < 32u) {
+#pragma unroll
+                    for (int k = 0; k < 32; ++k)
+                        if (off == (unsigned)k) a.z_target[at] = v[k];
+                }
+            }
+            if (live) a.part[at * a.parts + t.j * 2 + warp / 4] = make_float2(m, s);
+        } else {
+            float ratio = 0.f, lse = 0.f;
+            if (live) ratio = a.ratio[at], lse = a.lse[at];
+            if (!p.take(turn, tmem)) return false;
+            char *dz = a.dz + (size_t)t.w * a.dz_worker;
+#pragma unroll 1
+            for (int b = 0; b < 128; b += 32) {
+                const int in = t.j * 256 + c0 + b, col = a.piece0 + in;
+                float v[32];
+                tmem_load32(tmem + c0 + b, v);
+                if (b == 96) p.release(turn, lane);
+#pragma unroll
+                for (int k = 0; k < 32; ++k) v[k] = ratio * exp2_fast((v[k] - lse) * kLog2e);   // the difference first: it is exact where p is near 1
+                const unsigned off = (unsigned)(target - col);
+                if (off < 32u) {
+#pragma unroll
+                    for (int k = 0; k < 32; ++k)
+                        if (off == (unsigned)k) v[k] -= ratio;
+                }
+                if (col + 32 > a.vocab || !(ratio != 0.f)) {        // padding, and tokens that do not count
+#pragma unroll
+                    for (int k = 0; k < 32; ++k)
+                        if (col + k >= a.vocab || ratio == 0.f) v[k] = 0.f;
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float *e = v + 8 * k;
+                    uint4 o;
+                    if (a.bf16)
+                        o = make_uint4(pack_bf162(e[0], e[1]), pack_bf162(e[2], e[3]), pack_bf162(e[4], e[5]), pack_bf162(e[6], e[7]));
+                    else
+                        o = make_uint4(pack_half2(e[0], e[1]), pack_half2(e[2], e[3]), pack_half2(e[4], e[5]), pack_half2(e[6], e[7]));
+                    *reinterpret_cast<uint4 *>(dz + (size_t)(in / 64) * a.tp * 128 + panel_chunk(row, in % 64 / 8 + k)) = o;
+                }
+            }
+        }
+        return true;
+    }
+};
+
+template <int CG, bool GRAD>
+__global__ void __launch_bounds__(kThreads, 1) xent_logits_kernel(const __grid_constant__ XentArgs a) {
+    extern __shared__ unsigned char raw[];
+    if (threadIdx.x == 0) prefetch_tensor_map(&a.h), prefetch_tensor_map(&a.w);
+    Pipe<CG> p;
+    p.setup(raw, a.err);
+    LogitsJob<CG, GRAD> job{a, (int)blockIdx.x / CG, (int)gridDim.x / CG, (a.piece_n + 255) / 256};
+    p.run(job);
+    p.teardown();
+}
+
+// A warp joins the parts of one row.
+__global__ void __launch_bounds__(256) xent_join_kernel(const __grid_constant__ XentArgs a) {
+    const size_t at = (size_t)blockIdx.x * 8 + threadIdx.x / 32;
+    const int lane = threadIdx.x % 32;
+    if (at >= (size_t)a.n * a.tokens) return;
+    const float2 *p = a.part + at * a.parts;
+    float m = kLowest, s = 0.f;
+    for (int k = lane; k < a.parts; k += 32) {
+        const float2 q = p[k];
+        const float top = fmaxf(m, q.x);
+        s = s * exp2_fast((m - top) * kLog2e) + q.y * exp2_fast((q.x - top) * kLog2e);
+        m = top;
+    }
+    for (int k = 16; k; k >>= 1) {
+        const float qm = __shfl_xor_sync(~0u, m, k), qs = __shfl_xor_sync(~0u, s, k);
+        const float top = fmaxf(m, qm);
+        s = s * exp2_fast((m - top) * kLog2e) + qs * exp2_fast((qm - top) * kLog2e);
+        m = top;
+    }
+    if (lane == 0) {
+        const float lse = m + logf(s);
+        const int64_t y = a.target[at];
+        a.lse_out[at] = lse;
+        if (a.loss) a.loss[at] = y == a.ignore ? 0.f : y >= 0 && y < a.vocab ? lse - a.z_target[at] : NAN;
+    }
+}
+
+// One CTA per worker: the largest |dloss| of the tokens that count, and every token's dloss relative to it.
+__global__ void __launch_bounds__(1024) xent_ratio_kernel(const __grid_constant__ XentArgs a) {
+    __shared__ float red[32];
+    const size_t base = (size_t)blockIdx.x * a.tokens;
+    float top = 0.f;
+    for (int t = threadIdx.x; t < a.tokens; t += 1024)
+        if (a.target[base + t] != a.ignore) top = fmaxf(top, fabsf(a.dloss[base + t]));
+    for (int k = 16; k; k >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, k));
+    if (threadIdx.x % 32 == 0) red[threadIdx.x / 32] = top;
+    __syncthreads();
+    top = red[threadIdx.x % 32];
+    for (int k = 16; k; k >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, k));
+    const float scale = a.bf16 ? 1.f : 4096.f;
+    if (threadIdx.x == 0) a.unscale[blockIdx.x] = top / scale;
+    for (int t = threadIdx.x; t < a.tokens; t += 1024) {
+        const int64_t y = a.target[base + t];
+        float r = 0.f;
+        if (y != a.ignore) {
+            const float d = a.dloss[base + t];
+            if (d != 0.f) r = d / top * scale;                       // NaN stays NaN
+            if (y < 0 || y >= a.vocab) r = NAN;
+        }
+        a.ratio[base + t] = r;
+    }
+}
+
+// ------------------------------------------------------------------ dh and dW of a piece
+template <int CG>
+struct GradJob {
+    const XentArgs &a;
+    int first, every, n_dh, n_dw, dim_tiles, vocab_tiles;
+
+    struct Tile {
+        int w, i, j, n, k_blocks, k0, split, dw;
+    };
+    __device__ __forceinline__ bool next(Tile &t, int k) const {
+        int at = first + k * every;
+        t.dw = at >= n_dh;
+        if (t.dw) at -= n_dh;
+        if (t.dw && at >= n_dw) return false;
+        t.j = at % dim_tiles, at /= dim_tiles;
+        const int width = (a.dim + 64 * CG - 1) / (64 * CG) * (64 * CG);
+        t.n = width - t.j * 256 < 256 ? width - t.j * 256 : 256;
+        if (t.dw) {
+            t.i = at % vocab_tiles, t.w = at / vocab_tiles;
+            t.k0 = 0, t.k_blocks = (a.tokens + 63) / 64, t.split = 0;
+        } else {
+            t.split = at % a.splits, at /= a.splits;
+            t.i = at % a.token_tiles, t.w = at / a.token_tiles;
+            const int all = (a.piece_n + 63) / 64;
+            t.k0 = (int)((long long)all * t.split / a.splits);
+            t.k_blocks = (int)((long long)all * (t.split + 1) / a.splits) - t.k0;
+        }
+        return true;
+    }
+    __device__ __forceinline__ bool ready(Pipe<CG> &, const Tile &) const { return true; }
+    __device__ __forceinline__ bool a_mn(const Tile &t, int) const { return t.dw; }
+    __device__ __forceinline__ bool b_mn(const Tile &, int) const { return true; }
+    __device__ __forceinline__ bool chunk_ends(const Tile &t, int kb) const { return kb + 1 == t.k_blocks; }
+    __device__ __forceinline__ int bf16() const { return a.bf16; }
+    __device__ __forceinline__ uint32_t bytes(const Tile &t) const { return 128 * 128 + (uint32_t)(t.n / CG) * 128; }
+    __device__ __forceinline__ void load(const Tile &t, int kb, uint32_t sa, uint32_t sb, uint64_t *bar) const {
+        const int rank = CG == 1 ? 0 : (int)cluster_rank();
+        const char *dz = a.dz + (size_t)t.w * a.dz_worker;
+        const int row = t.i * 128 * CG + rank * 128, col = t.j * 256 + rank * (t.n / CG), k = t.k0 + kb;
+        if (t.dw) {
+#pragma unroll
+            for (int p = 0; p < 2; ++p)
+                bulk_copy_in(sa + p * 8192, dz + (size_t)(row / 64 + p) * a.tp * 128 + (size_t)k * 8192, 8192, bar);
+        } else {
+            bulk_copy_in(sa, dz + (size_t)k * a.tp * 128 + (size_t)row * 128, 16384, bar);
+        }
+        const int worker = (t.dw ? a.h_workers : a.w_workers) == 1 ? 0 : t.w;
+        for (int p = 0; p < t.n / CG / 64; ++p)
+            tensor_copy_in(sb + p * 8192, t.dw ? &a.h : &a.w, col + p * 64, t.dw ? k * 64 : a.piece0 + k * 64, worker, bar);
+    }
+    __device__ __forceinline__ bool epilogue(Pipe<CG> &p, const Tile &t, typename Pipe<CG>::Turn &turn, int warp, int lane) const {
+        uint32_t tmem;
+        const int row = t.i * 128 * CG + (int)p.rank * 128 + warp % 4 * 32 + lane;
+        const int half = t.n / 2, c0 = warp / 4 * half;
+        const float f = a.unscale[t.w];
+        if (!p.take(turn, tmem)) return false;
+#pragma unroll 1
+        for (int b = 0; b < half; b += 32) {
+            const int col = t.j * 256 + c0 + b;
+            float v[32];
+            tmem_load32(tmem + c0 + b, v);
+            if (b + 32 >= half) p.release(turn, lane);
+            if (t.dw) {
+                if (row < a.piece_n && col < a.dim) {
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) v[k] *= f;
+                    store_row32(a.dw, t.w * a.dw_stride + (long long)(a.piece0 + row) * a.dim + col, a.dim - col, a.type, v);
+                }
+                continue;
+            }
+            float4 *acc = reinterpret_cast<float4 *>(
+                a.acc + (((size_t)t.w * a.splits + t.split) * a.acc_rows + row) * a.acc_cols + col);
+            if (!a.first_piece) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const float4 q = acc[k];
+                    v[4 * k] += q.x, v[4 * k + 1] += q.y, v[4 * k + 2] += q.z, v[4 * k + 3] += q.w;
+                }
+            }
+            if (a.last_piece && a.splits == 1) {
+                if (row < a.tokens && col < a.dim) {
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) v[k] *= f;
+                    store_row32(a.dh, ((long long)t.w * a.tokens + row) * a.dim + col, a.dim - col, a.type, v);
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) acc[k] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+            }
+        }
+        return true;
+    }
+};
+
+template <int CG>
+__global__ void __launch_bounds__(kThreads, 1) xent_grad_kernel(const __grid_constant__ XentArgs a, int n_dh, int n_dw) {
+    extern __shared__ unsigned char raw[];
+    if (threadIdx.x == 0) prefetch_tensor_map(&a.h), prefetch_tensor_map(&a.w);
+    Pipe<CG> p;
+    p.setup(raw, a.err);
+    const int width = (a.dim + 64 * CG - 1) / (64 * CG) * (64 * CG);
+    GradJob<CG> job{a, (int)blockIdx.x / CG, (int)gridDim.x / CG, n_dh, n_dw, (width + 255) / 256,
+                    (a.piece_n + 128 * CG - 1) / (128 * CG)};
+    p.run(job);
+    p.teardown();
+}
+
+// Where the inner dimension was split: the shares of dh added in their order, four columns a thread.
+__global__ void __launch_bounds__(256) xent_join_dh_kernel(const __grid_constant__ XentArgs a) {
+    const int groups = (a.dim + 3) / 4;
+    const long long e = (long long)blockIdx.x * 256 + threadIdx.x, row_at = e / groups;
+    const int col = (int)(e - row_at * groups) * 4;
+    if (row_at >= (long long)a.n * a.tokens) return;
+    const int w = (int)(row_at / a.tokens), row = (int)(row_at - (long long)w * a.tokens);
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < a.splits; ++s) {
+        const float4 q = *reinterpret_cast<const float4 *>(a.acc + (((size_t)w * a.splits + s) * a.acc_rows + row) * a.acc_cols + col);
+        v[0] += q.x, v[1] += q.y, v[2] += q.z, v[3] += q.w;
+    }
+    const float f = a.unscale[w];
+    uint16_t *o = static_cast<uint16_t *>(a.dh) + row_at * a.dim + col;
+    const uint32_t lo = a.bf16 ? pack_bf162(v[0] * f, v[1] * f) : pack_half2(v[0] * f, v[1] * f);
+    const uint32_t hi = a.bf16 ? pack_bf162(v[2] * f, v[3] * f) : pack_half2(v[2] * f, v[3] * f);
+    if (col + 4 <= a.dim && (reinterpret_cast<uintptr_t>(o) & 7) == 0) {
+        *reinterpret_cast<uint2 *>(o) = make_uint2(lo, hi);
+    } else {
+        for (int k = 0; k < 4 && col + k < a.dim; ++k) o[k] = (uint16_t)((k < 2 ? lo : hi) >> (k % 2 * 16));
+    }
+}
+
+// Rows that no tensor copy can start at, as rows padded to a multiple of 8.
+__global__ void __launch_bounds__(256) xent_pack_kernel(const uint16_t *src, long long row_stride, long long worker_stride, int rows,
+                                                        int dim, int padded, uint16_t *dst) {
+    const long long row = blockIdx.x;
+    const uint16_t *s = src + (row / rows) * worker_stride + (row % rows) * row_stride;
+    uint16_t *d = dst + row * padded;
+    for (int c = threadIdx.x; c < padded; c += 256) d[c] = c < dim ? s[c] : 0;
+}
+
+}  // namespace
+
+// ------------------------------------------------------------------ host
+#define TRY(expr)                                                                                              \
+    do {                                                                                                       \
+        cudaError_t _e = (expr);                                                                               \
+        if (_e != cudaSuccess)                                                                                 \
+            return cser_internal_fail(_e == cudaErrorMemoryAllocation ? CSER_ERR_NOMEM : CSER_ERR_CUDA, "%s: %s", #expr, \
+                                      cudaGetErrorString(_e));                                                 \
+    } while (0)
+
+typedef CUresult (*encode_fn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                              const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                              CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+struct cser_xent {
+    int device = 0, n = 0, type = 0, sms = 0;
+    long long max_tokens = 0, vocab = 0, dim = 0, piece = 0;
+    int parts = 0, tp = 0, acc_cols = 0;
+    void *work = nullptr;
+    float2 *part = nullptr;
+    float *z_target = nullptr, *ratio = nullptr, *unscale = nullptr, *acc = nullptr;
+    char *dz = nullptr;
+    void *pack_h = nullptr, *pack_w = nullptr;     // made on the first call that needs them
+    encode_fn encode = nullptr;
+    unsigned *err_host = nullptr, *err_dev = nullptr;
+    long long launches = 0;
+};
+
+namespace {
+
+long long up(long long v, long long to) { return (v + to - 1) / to * to; }
+int splits_of(const cser_xent *h, long long tokens) {
+    // Few tiles of dh and a long inner dimension: the vocabulary is split so that every SM has a share, each of 16 stages at least.
+    const long long tiles = h->n * (up(tokens, 128) / 128) * (up(h->dim, 256) / 256), stages = up(h->piece < h->vocab ? h->piece : h->vocab, 64) / 64;
+    long long s = tiles >= h->sms ? 1 : h->sms / tiles;
+    if (s > stages / 16) s = stages / 16;
+    return s < 1 ? 1 : (int)s;
+}
+
+bool tensor_map(const cser_xent *h, CUtensorMap &m, const void *p, long long rows, long long row_stride, long long worker_stride,
+                int workers, long long dim) {
+    const cuuint64_t size[3] = {(cuuint64_t)dim, (cuuint64_t)rows, (cuuint64_t)workers};
+    const cuuint64_t stride[2] = {(cuuint64_t)row_stride * 2, (cuuint64_t)(workers == 1 ? up(row_stride * rows, 8) : worker_stride) * 2};
+    const cuuint32_t box[3] = {64, 64, 1}, step[3] = {1, 1, 1};
+    return h->encode(&m, h->type == CSER_TYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3,
+                     const_cast<void *>(p), size, stride, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                     CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// The map of an operand, of a packed copy where its rows cannot be read in place.
+int operand(cser_xent *h, CUtensorMap &m, int &workers, const void *p, long long rows, long long row_stride, long long worker_stride,
+            void *&pack, long long pack_rows, const char *what, cudaStream_t st) {
+    workers = h->n == 1 || worker_stride == 0 ? 1 : h->n;
+    if (rows == 1) row_stride = up(h->dim, 8);                      // no second row: its distance says nothing
+    const bool direct = (uintptr_t)p % 16 == 0 && row_stride % 8 == 0 && row_stride > 0 && (workers == 1 || worker_stride % 8 == 0);
+    if (!direct) {
+        const long long padded = up(h->dim, 8);
+        if (!pack) {
+            cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
+            TRY(cudaStreamIsCapturing(st, &cap));
+            if (cap != cudaStreamCaptureStatusNone)
+                return cser_internal_fail(CSER_ERR_INVALID, "%s needs a packing buffer: make the first such call outside a capture", what);
+            TRY(cudaMalloc(&pack, (size_t)h->n * pack_rows * padded * 2));
+        }
+        xent_pack_kernel<<<(unsigned)(workers * rows), 256, 0, st>>>(static_cast<const uint16_t *>(p), row_stride, worker_stride, (int)rows,
+                                                                     (int)h->dim, (int)padded, static_cast<uint16_t *>(pack));
+        TRY(cudaGetLastError());
+        h->launches++;
+        p = pack, row_stride = padded, worker_stride = padded * rows;
+    }
+    if (!tensor_map(h, m, p, rows, row_stride, worker_stride, workers, h->dim))
+        return cser_internal_fail(CSER_ERR_INVALID, "%s: no tensor map for this address and these strides", what);
+    return CSER_OK;
+}
+
+int prepare_call(cser_xent *h, const cser_xent_inputs *in, const char *what, XentArgs &a, cudaStream_t st) {
+    if (!h) return cser_internal_fail(CSER_ERR_INVALID, "%s: NULL handle", what);
+    if (!in) return cser_internal_fail(CSER_ERR_INVALID, "%s: NULL inputs", what);
+    int dev = -1;
+    TRY(cudaGetDevice(&dev));
+    if (dev != h->device)
+        return cser_internal_fail(CSER_ERR_INVALID, "handle belongs to device %d, current device is %d", h->device, dev);
+    if (*reinterpret_cast<volatile unsigned *>(h->err_host))
+        return cser_internal_fail(CSER_ERR_CUDA, "a device-side wait ran out in an earlier call: its results are incomplete");
+    if (in->tokens < 0 || in->tokens > h->max_tokens)
+        return cser_internal_fail(CSER_ERR_INVALID, "%s: tokens must be in 0..%lld", what, h->max_tokens);
+    a = XentArgs{};
+    a.n = h->n, a.tokens = (int)in->tokens, a.vocab = (int)h->vocab, a.dim = (int)h->dim;
+    if (in->tokens == 0) return CSER_OK;
+    if (in->hidden_row_stride < 0 || in->hidden_worker_stride < 0 || in->weight_row_stride < 0 || in->weight_worker_stride < 0)
+        return cser_internal_fail(CSER_ERR_INVALID, "%s: strides must not be negative", what);
+    if (int rc = cser_internal_check_ptr(in->hidden, "hidden")) return rc;
+    if (int rc = cser_internal_check_ptr(in->weight, "weight")) return rc;
+    if (int rc = cser_internal_check_ptr(in->target, "target")) return rc;
+    if ((uintptr_t)in->hidden % 2 || (uintptr_t)in->weight % 2 || (uintptr_t)in->target % 8)
+        return cser_internal_fail(CSER_ERR_INVALID, "%s: a pointer is not aligned to its element type", what);
+    if (int rc = operand(h, a.h, a.h_workers, in->hidden, in->tokens, in->hidden_row_stride, in->hidden_worker_stride, h->pack_h,
+                         h->max_tokens, "hidden", st))
+        return rc;
+    if (int rc = operand(h, a.w, a.w_workers, in->weight, h->vocab, in->weight_row_stride, in->weight_worker_stride, h->pack_w, h->vocab,
+                         "weight", st))
+        return rc;
+    a.type = h->type, a.bf16 = h->type == CSER_TYPE_BF16;
+    a.tp = h->tp, a.part = h->part, a.parts = h->parts, a.z_target = h->z_target, a.target = in->target, a.ignore = in->ignore_index;
+    a.ratio = h->ratio, a.unscale = h->unscale, a.dz = h->dz, a.dz_worker = (size_t)(h->piece / 64) * h->tp * 128;
+    a.acc = h->acc, a.acc_rows = (int)up(a.tokens, 256), a.acc_cols = h->acc_cols, a.err = h->err_dev;
+    return CSER_OK;
+}
+
+template <int CG, typename K, typename... Args>
+cudaError_t tiles_launch(cser_xent *h, K kernel, long long tiles, cudaStream_t st, Args... args) {
+    const long long most = h->sms / CG;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)((tiles < most ? tiles : most) * CG));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = Pipe<CG>::kSharedBytes;
+    cfg.stream = st;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = CG, at[0].val.clusterDim.y = 1, at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = CG == 1 ? 0 : 1;
+    h->launches++;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+template <int CG>
+cudaError_t kernels_setup() {
+    const int b = (int)Pipe<CG>::kSharedBytes;
+    cudaError_t e = cudaFuncSetAttribute(xent_logits_kernel<CG, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, b);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(xent_logits_kernel<CG, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, b);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(xent_grad_kernel<CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, b);
+    return e;
+}
+
+template <int CG>
+int loss_launch(cser_xent *h, XentArgs &a, cudaStream_t st) {
+    a.token_tiles = (int)(up(a.tokens, 128 * CG) / (128 * CG)), a.piece0 = 0, a.piece_n = a.vocab;
+    TRY((tiles_launch<CG>(h, xent_logits_kernel<CG, false>, (long long)a.n * a.token_tiles * ((a.vocab + 255) / 256), st, a)));
+    xent_join_kernel<<<(unsigned)(((long long)a.n * a.tokens + 7) / 8), 256, 0, st>>>(a);
+    TRY(cudaGetLastError());
+    h->launches++;
+    return CSER_OK;
+}
+
+template <int CG>
+int grad_launch(cser_xent *h, XentArgs &a, cudaStream_t st) {
+    a.token_tiles = (int)(up(a.tokens, 128 * CG) / (128 * CG));
+    a.splits = splits_of(h, a.tokens);
+    xent_ratio_kernel<<<(unsigned)a.n, 1024, 0, st>>>(a);
+    TRY(cudaGetLastError());
+    h->launches++;
+    const long long dim_tiles = up(a.dim, 256) / 256;
+    for (long long v = 0; v < h->vocab; v += h->piece) {
+        a.piece0 = (int)v, a.piece_n = (int)(h->vocab - v < h->piece ? h->vocab - v : h->piece);
+        a.first_piece = v == 0, a.last_piece = v + h->piece >= h->vocab;
+        const long long vt = up(a.piece_n, 128 * CG) / (128 * CG);
+        TRY((tiles_launch<CG>(h, xent_logits_kernel<CG, true>, (long long)a.n * a.token_tiles * ((a.piece_n + 255) / 256), st, a)));
+        const long long n_dh = a.dh ? (long long)a.n * a.token_tiles * a.splits * dim_tiles : 0, n_dw = a.dw ? a.n * vt * dim_tiles : 0;
+        TRY((tiles_launch<CG>(h, xent_grad_kernel<CG>, n_dh + n_dw, st, a, (int)n_dh, (int)n_dw)));
+    }
+    if (a.dh && a.splits > 1) {
+        const long long e = (long long)a.n * a.tokens * ((a.dim + 3) / 4);
+        xent_join_dh_kernel<<<(unsigned)((e + 255) / 256), 256, 0, st>>>(a);
+        TRY(cudaGetLastError());
+        h->launches++;
+    }
+    return CSER_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+cser_xent_handle cser_xent_create(int32_t n_workers, int64_t max_tokens, int64_t vocab, int64_t dim, int32_t type,
+                                  int64_t piece) {
+    auto bad = [](int code, const char *what) { cser_internal_fail(code, "cser_xent_create: %s", what); return nullptr; };
+    if (n_workers < 1 || max_tokens < 1 || n_workers > (1 << 24) / max_tokens)
+        return bad(CSER_ERR_INVALID, "n_workers and max_tokens must be positive and their product at most 2^24");
+    if (vocab < 1 || vocab > (1 << 24) || dim < 1 || dim > 65536)
+        return bad(CSER_ERR_INVALID, "vocab must be in 1..2^24, dim in 1..65536");
+    if ((long long)n_workers * vocab > (1 << 30) || up(max_tokens, 128) / 128 * n_workers * (up(vocab, 256) / 256) > (1 << 30))
+        return bad(CSER_ERR_INVALID, "n_workers * vocab, and the tiles of all logits, must be at most 2^30");
+    if (type != CSER_TYPE_BF16 && type != CSER_TYPE_F16) return bad(CSER_ERR_INVALID, "type must be CSER_TYPE_BF16 or CSER_TYPE_F16");
+    if (piece < 0) return bad(CSER_ERR_INVALID, "piece must not be negative");
+    cser_xent *h = new (std::nothrow) cser_xent;
+    if (!h) return bad(CSER_ERR_NOMEM, "host allocation failed");
+    auto drop = [&](cudaError_t e) {
+        cser_internal_fail(e == cudaErrorMemoryAllocation ? CSER_ERR_NOMEM : CSER_ERR_CUDA, "cser_xent_create: %s", cudaGetErrorString(e));
+        cser_xent_destroy(h);
+        return nullptr;
+    };
+    h->n = n_workers, h->max_tokens = max_tokens, h->vocab = vocab, h->dim = dim, h->type = type;
+    cudaError_t e = cudaGetDevice(&h->device);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&h->sms, cudaDevAttrMultiProcessorCount, h->device);
+    if (e == cudaSuccess) e = kernels_setup<1>();
+    if (e == cudaSuccess) e = kernels_setup<2>();
+    void *fn = nullptr;
+    cudaDriverEntryPointQueryResult found = cudaDriverEntryPointSymbolNotFound;
+    if (e == cudaSuccess) e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found);
+    if (e == cudaSuccess && (!fn || found != cudaDriverEntryPointSuccess)) e = cudaErrorNotSupported;
+    if (e != cudaSuccess) return drop(e);
+    h->encode = reinterpret_cast<encode_fn>(fn);
+    const long long rows = (long long)n_workers * max_tokens;
+    h->tp = (int)up(max_tokens, 256), h->acc_cols = (int)up(dim, 128), h->parts = (int)(2 * (up(vocab, 256) / 256));
+    const long long fit = (long long)(kPieceBytes / ((size_t)h->n * h->tp * 2)) / 256 * 256;
+    h->piece = piece ? up(piece, 256) : fit < 2048 ? 2048 : fit;
+    if (h->piece > up(vocab, 256)) h->piece = up(vocab, 256);
+    long long acc_rows = 0;                        // the most that any number of tokens asks for
+    for (long long t = 128; t < max_tokens + 128; t += 128) {
+        const int k = splits_of(h, t < max_tokens ? t : max_tokens);
+        if ((k > 1 || h->piece < vocab) && k * up(t, 256) > acc_rows) acc_rows = k * up(t, 256);
+    }
+    size_t at = 0;
+    auto place = [&](size_t b) { const size_t p = at; at += (b + 1023) / 1024 * 1024; return p; };
+    const size_t o_part = place((size_t)rows * h->parts * 8), o_zt = place((size_t)rows * 4), o_ratio = place((size_t)rows * 4),
+                 o_un = place((size_t)n_workers * 4), o_dz = place((size_t)n_workers * (h->piece / 64) * h->tp * 128),
+                 o_acc = place((size_t)n_workers * acc_rows * h->acc_cols * 4);
+    e = cudaMalloc(&h->work, at);
+    if (e == cudaSuccess) e = cudaHostAlloc(reinterpret_cast<void **>(&h->err_host), 64, cudaHostAllocMapped | cudaHostAllocPortable);
+    if (e == cudaSuccess) *h->err_host = 0, e = cudaHostGetDevicePointer(reinterpret_cast<void **>(&h->err_dev), h->err_host, 0);
+    if (e != cudaSuccess) return drop(e);
+    char *w = static_cast<char *>(h->work);
+    h->part = reinterpret_cast<float2 *>(w + o_part), h->z_target = reinterpret_cast<float *>(w + o_zt);
+    h->ratio = reinterpret_cast<float *>(w + o_ratio), h->unscale = reinterpret_cast<float *>(w + o_un);
+    h->dz = w + o_dz, h->acc = reinterpret_cast<float *>(w + o_acc);
+    return h;
+}
+
+int cser_xent_loss(cser_xent_handle h, const cser_xent_inputs *in, float *loss, float *lse, void *stream) {
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    XentArgs a;
+    if (int rc = prepare_call(h, in, "cser_xent_loss", a, st)) return rc;
+    if (a.tokens == 0) return CSER_OK;
+    if (int rc = cser_internal_check_ptr(lse, "cser_xent_loss: lse")) return rc;
+    if (loss)
+        if (int rc = cser_internal_check_ptr(loss, "cser_xent_loss: loss")) return rc;
+    if ((uintptr_t)lse % 4 || (uintptr_t)loss % 4)
+        return cser_internal_fail(CSER_ERR_INVALID, "cser_xent_loss: a pointer is not aligned to its element type");
+    a.loss = loss, a.lse_out = lse;
+    return loss_launch<1>(h, a, st);
+}
+
+int cser_xent_grad(cser_xent_handle h, const cser_xent_inputs *in, const float *lse, const float *dloss, void *dhidden,
+                   void *dweight, int64_t dweight_stride, void *stream) {
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    XentArgs a;
+    if (int rc = prepare_call(h, in, "cser_xent_grad", a, st)) return rc;
+    if (!dhidden && !dweight) return CSER_OK;
+    if (dweight) {
+        if (int rc = cser_internal_check_ptr(dweight, "cser_xent_grad: dweight")) return rc;
+        if (h->n > 1 && dweight_stride < h->vocab * h->dim)
+            return cser_internal_fail(CSER_ERR_INVALID, "cser_xent_grad: dweight_stride must be at least vocab * dim");
+    }
+    if ((uintptr_t)dweight % 2 || (uintptr_t)dhidden % 2)
+        return cser_internal_fail(CSER_ERR_INVALID, "cser_xent_grad: a pointer is not aligned to its element type");
+    if (a.tokens == 0) {
+        if (dweight)
+            for (int w = 0; w < h->n; ++w)
+                TRY(cudaMemsetAsync(static_cast<uint16_t *>(dweight) + w * dweight_stride, 0, (size_t)h->vocab * h->dim * 2, st));
+        return CSER_OK;
+    }
+    if (int rc = cser_internal_check_ptr(lse, "cser_xent_grad: lse")) return rc;
+    if (int rc = cser_internal_check_ptr(dloss, "cser_xent_grad: dloss")) return rc;
+    if (dhidden)
+        if (int rc = cser_internal_check_ptr(dhidden, "cser_xent_grad: dhidden")) return rc;
+    if ((uintptr_t)lse % 4 || (uintptr_t)dloss % 4)
+        return cser_internal_fail(CSER_ERR_INVALID, "cser_xent_grad: a pointer is not aligned to its element type");
+    a.lse = lse, a.dloss = dloss, a.dh = dhidden, a.dw = dweight, a.dw_stride = dweight_stride;
+    return grad_launch<1>(h, a, st);
+}
+
+void cser_xent_destroy(cser_xent_handle h) {
+    if (!h) return;
+    for (void *p : {h->work, h->pack_h, h->pack_w})
+        if (p) cudaFree(p);
+    if (h->err_host) cudaFreeHost(h->err_host);
+    delete h;
+}
+
+int64_t cser_xent_launch_count(cser_xent_handle h) { return h ? h->launches : 0; }
+
+}  // extern "C"

@@ -40,7 +40,6 @@ def lib():
             ("cser_xent_grad", c.c_int, [p, c.POINTER(_XentInputs), p, p, p, p, i64, p]),
             ("cser_xent_destroy", None, [p]),
             ("cser_xent_launch_count", i64, [p])):
-        if not hasattr(L, name): continue
         f = getattr(L, name)
         f.restype, f.argtypes = res, args
     _lib = L
@@ -101,6 +100,87 @@ class Orthogonalizer:
         if self.h is not None:
             torch.cuda.synchronize()
             lib().cser_orth_destroy(self.h)
+            self.h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class LinearCrossEntropy:
+    """Softmax cross entropy of hidden @ weight^T against targets, in pieces of the vocabulary, and its gradient.
+
+    Workspace for up to ``max_tokens`` tokens of each of ``n_workers`` workers; ``piece``: vocabulary entries per piece
+    of the gradient (0: chosen by size).  hidden is [n, tokens, dim], weight [n, vocab, dim] (an ``expand``ed leading
+    dimension shares one array), target int64 [n, tokens].  See cser_xent_create.
+    """
+
+    def __init__(self, n_workers, max_tokens, vocab, dim, dtype=torch.bfloat16, piece=0):
+        self.h = None
+        _want(dtype in TYPES, "LinearCrossEntropy: types are bfloat16 and float16")
+        self.n, self.max_tokens, self.vocab, self.dim = int(n_workers), int(max_tokens), int(vocab), int(dim)
+        self.dtype = dtype
+        h = lib().cser_xent_create(self.n, self.max_tokens, self.vocab, self.dim, TYPES[dtype], int(piece))
+        if not h:
+            raise CSERError(f"cser_xent_create failed: {cser_last_error()}")
+        self.h = ctypes.c_void_p(h)
+
+    def _inputs(self, hidden, weight, target, ignore_index):
+        t = target.shape[1] if target.dim() == 2 else -1
+        for name, a, shape in (("hidden", hidden, (self.n, t, self.dim)), ("weight", weight, (self.n, self.vocab, self.dim))):
+            _want(a.is_cuda and a.dtype == self.dtype and a.shape == shape and (a.stride(2) == 1 or self.dim == 1) and
+                  min(a.stride()) >= 0, f"LinearCrossEntropy: {name} must be a CUDA {self.dtype} tensor of shape {shape} "
+                  "with a contiguous last dimension")
+        _want(target.is_cuda and target.dtype == torch.int64 and target.shape == (self.n, t) and target.is_contiguous() and
+              0 <= t <= self.max_tokens, f"LinearCrossEntropy: target must be a contiguous CUDA int64 tensor "
+              f"[{self.n}, at most {self.max_tokens}]")
+        return _XentInputs(hidden.data_ptr(), hidden.stride(1), hidden.stride(0), weight.data_ptr(), weight.stride(1),
+                           weight.stride(0), target.data_ptr(), ignore_index, t)
+
+    def loss(self, hidden, weight, target, ignore_index=-100, stream=None):
+        """(loss, lse), each fp32 [n, tokens]; lse is what grad takes."""
+        args = self._inputs(hidden, weight, target, ignore_index)
+        both = torch.empty((2, *target.shape), dtype=torch.float32, device=target.device)
+        _check(_lib.cser_xent_loss(self.h, ctypes.byref(args), both[0].data_ptr(), both[1].data_ptr(), _stream(stream)),
+               "cser_xent_loss")
+        return both[0], both[1]
+
+    def grad(self, hidden, weight, target, lse, dloss, ignore_index=-100, dhidden=None, dweight=None, need_dhidden=True,
+             need_dweight=True, stream=None):
+        """(dhidden, dweight) of sum(dloss * loss); dweight may be a [n, vocab, dim] view of a larger [n, d] array."""
+        args = self._inputs(hidden, weight, target, ignore_index)
+        for name, a in (("lse", lse), ("dloss", dloss)):
+            _want(a.is_cuda and a.dtype == torch.float32 and a.shape == target.shape and a.is_contiguous(),
+                  f"LinearCrossEntropy: {name} must be a contiguous CUDA float32 tensor of target's shape")
+        if need_dhidden:
+            if dhidden is None:
+                dhidden = torch.empty(hidden.shape, dtype=self.dtype, device=hidden.device)
+            _want(dhidden.is_cuda and dhidden.dtype == self.dtype and dhidden.shape == hidden.shape and dhidden.is_contiguous(),
+                  f"LinearCrossEntropy: dhidden must be a contiguous CUDA {self.dtype} tensor of hidden's shape")
+        if need_dweight:
+            if dweight is None:
+                dweight = torch.empty(weight.shape, dtype=self.dtype, device=weight.device)
+            _want(dweight.is_cuda and dweight.dtype == self.dtype and dweight.shape == weight.shape and
+                  (self.dim == 1 or dweight.stride(2) == 1) and (self.vocab == 1 or dweight.stride(1) == self.dim) and
+                  (self.n == 1 or dweight.stride(0) >= self.vocab * self.dim),
+                  f"LinearCrossEntropy: dweight must be a CUDA {self.dtype} tensor of weight's shape, dense for each worker")
+        _check(_lib.cser_xent_grad(self.h, ctypes.byref(args), lse.data_ptr(), dloss.data_ptr(),
+                                   dhidden.data_ptr() if need_dhidden else None,
+                                   dweight.data_ptr() if need_dweight else None,
+                                   max(dweight.stride(0), self.vocab * self.dim) if need_dweight else 0, _stream(stream)),
+               "cser_xent_grad")
+        return dhidden if need_dhidden else None, dweight if need_dweight else None
+
+    @property
+    def launches(self):
+        return int(lib().cser_xent_launch_count(self.h))
+
+    def close(self):
+        if self.h is not None:
+            torch.cuda.synchronize()
+            lib().cser_xent_destroy(self.h)
             self.h = None
 
     def __del__(self):
