@@ -32,6 +32,7 @@
 #include <math.h>
 #include <stdint.h>
 #include <stdio.h>
+#include <stdlib.h>
 #include <new>
 #include <vector>
 
@@ -45,14 +46,15 @@ namespace {
 constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f, kEps = 1e-7f;
 constexpr float kScale = 4096.f, kUnscale = 1.f / 4096.f, kUnscale2 = kUnscale * kUnscale;
 constexpr int kNormChunk = 8192;                   // elements per CTA of the norm kernel
-// Columns of a tile.
-constexpr int tile_n(bool split) { return split ? 128 : 256; }
+// Columns of a tile, for CTAs in pairs (cg = 2) or single ones; a 32-bit result's sums must fit the epilogue's registers.
+constexpr int tile_n(int cg, bool split) { return cg == 2 && !split ? 256 : 128; }
 // The tensor cores truncate every partial sum, about 2^-24 of it for 16 terms: 2e-5 over an inner dimension of 4096.  So a
 // 32-bit result's accumulator is taken out and added up in registers, rounded, after this many stages of the leading
 // product (the two small ones share one accumulator).  X's product is the one whose error the steps after it do not
 // shrink: with a low-rank matrix 9e-6 at 4 stages.
 constexpr int kChunkAB = 4, kChunkX = 1;
 constexpr size_t kGroupBytes = 2ull << 30;         // workspace of one group of matrices
+constexpr size_t kBatchBytes = 96ull << 20;        // of it, what is worked on together
 
 struct OrthMat {
     __half *xh[2], *xl[2], *ah, *al, *bh, *bl;     // panels; al, bl for 32-bit results only
@@ -70,6 +72,11 @@ struct OrthTile {
     uint32_t q;
     uint16_t i, j;
 };
+// Matrices whose steps are worked on together, so that their X, A and B stay in L2: where their tiles are in the lists.
+struct OrthBatch {
+    int sym, n_sym, x, n_x;
+    long long first;                               // position of their first tile in the order of work
+};
 struct ConvertUnit {
     uint32_t q, r0, c0;                            // 32 rows, up to 4 panels
 };
@@ -77,7 +84,8 @@ struct ConvertUnit {
 struct OrthArgs {
     const OrthMat *mats;
     const OrthTile *sym, *x;
-    int n_sym, n_x, steps;
+    const OrthBatch *batch;                        // and one more, whose `first` is the number of all tiles
+    int steps;
     unsigned *done;                                // [matrices] finished tiles
     unsigned *ticket;                              // [matrices] norm kernel
     float *partial, *inv;                          // [chunks], [matrices] 1 / (norm + eps)
@@ -215,8 +223,10 @@ __device__ __forceinline__ char *panel_at(__half *base, int rows, int panel) {
     return reinterpret_cast<char *>(base) + (size_t)panel * rows * 128;
 }
 
-__device__ __forceinline__ float4 *wide_at(float *base, int rows, int row, int col) {
-    return reinterpret_cast<float4 *>(base + ((size_t)(col / 64) * rows + row) * 64 + col % 64);
+// X in fp32: panels of 64 columns, rows of 256 bytes, chunk c of 4 columns of row r at c ^ (r & 7).
+__device__ __forceinline__ uint32_t wide_chunk(uint32_t row, uint32_t c) { return row * 256 + ((c ^ (row & 7)) << 4); }
+__device__ __forceinline__ char *wide_at(float *base, int rows, int panel) {
+    return reinterpret_cast<char *>(base) + (size_t)panel * rows * 256;
 }
 
 // A thread makes one chunk of 8 columns per panel; the padding becomes 0.
@@ -258,9 +268,9 @@ __global__ void __launch_bounds__(256) orth_convert_kernel(const OrthArgs a) {
         *reinterpret_cast<uint4 *>(panel_at(M.xh[0], M.rp, col / 64) + at) = hi;
         *reinterpret_cast<uint4 *>(panel_at(M.xl[0], M.rp, col / 64) + at) = lo;
         if (M.xf[0]) {
-            float4 *w = wide_at(M.xf[0], M.rp, row, col + c * 8);
-            w[0] = make_float4(v[p][0], v[p][1], v[p][2], v[p][3]);
-            w[1] = make_float4(v[p][4], v[p][5], v[p][6], v[p][7]);
+            char *w = wide_at(M.xf[0], M.rp, col / 64);
+            *reinterpret_cast<float4 *>(w + wide_chunk(row, 2 * c)) = make_float4(v[p][0], v[p][1], v[p][2], v[p][3]);
+            *reinterpret_cast<float4 *>(w + wide_chunk(row, 2 * c + 1)) = make_float4(v[p][4], v[p][5], v[p][6], v[p][7]);
         }
     }
 }
@@ -269,110 +279,273 @@ __global__ void __launch_bounds__(256) orth_convert_kernel(const OrthArgs a) {
 enum { kPhaseA = 0, kPhaseB = 1, kPhaseX = 2 };
 
 template <int CG, bool SPLIT>
+using OrthPipe = Pipe<CG, tile_n(CG, SPLIT), SPLIT ? 65536 : 98304>;
+
+template <int CG, bool SPLIT>
 struct OrthJob {
+    using P = OrthPipe<CG, SPLIT>;
     const OrthArgs &a;
-    int first, every, per_step;
-    static constexpr int TN = tile_n(SPLIT);
+    int first, every;
+    int at_batch = 0;                                                // of the last tile asked for: positions only grow
+    static constexpr int TN = tile_n(CG, SPLIT);
+    static constexpr bool kCopier = true;
 
     struct Tile {
-        const OrthMat *M;
-        uint32_t q;
-        int i, j, n, phase, step, k_blocks, k_seg;
-        unsigned need;
+        int n, segs, k_seg, a_lim, b_lim;
+        int phase, tall, last, row0, panel0, rp;                     // row0: of this CTA; rp: rows of a panel of what is written
+        int row_a, row_b;                                            // first rows of the operands
+        unsigned need, *done;
+        const char *a_hi, *a_lo, *b_hi, *b_lo;                       // operands, their panels' bytes
+        size_t a_panel, b_panel;
+        char *dst_hi, *dst_lo, *dst_wide;
+        const char *src_hi, *src_lo, *src_wide;                      // A or X, for the epilogue
+        float *da, *db;
+        long long offset, stride;
+        int rows, cols;
+        float scale;
     };
 
-    __device__ __forceinline__ bool next(Tile &t, int k) const {
+    __device__ __forceinline__ void tile(Tile &t, int k, int rank) {
+        t.n = 0;
         const long long at = first + (long long)k * every;
-        if (at >= (long long)per_step * a.steps) return false;
-        t.step = (int)(at / per_step);
-        int r = (int)(at - (long long)t.step * per_step);
-        const OrthTile *list = a.sym;
-        t.phase = kPhaseA;
-        if (r >= a.n_sym) r -= a.n_sym, t.phase = kPhaseB;
-        if (t.phase == kPhaseB && r >= a.n_sym) r -= a.n_sym, t.phase = kPhaseX, list = a.x;
+        while (at >= a.batch[at_batch + 1].first)
+            if (a.batch[++at_batch].n_x == 0) return;                // the one behind the last
+        const OrthBatch B = a.batch[at_batch];
+        const int in = (int)(at - B.first), per_step = 2 * B.n_sym + B.n_x, step = in / per_step;
+        int r = in - step * per_step, phase = kPhaseA;
+        const OrthTile *list = a.sym + B.sym;
+        if (r >= B.n_sym) r -= B.n_sym, phase = kPhaseB;
+        if (phase == kPhaseB && r >= B.n_sym) r -= B.n_sym, phase = kPhaseX, list = a.x + B.x;
         const OrthTile e = list[r];
-        t.q = e.q, t.i = e.i, t.j = e.j;
-        t.M = a.mats + e.q;
-        const int width = t.phase == kPhaseX ? t.M->cp : t.M->sp;
-        t.n = width - t.j * TN < TN ? width - t.j * TN : TN;
-        t.k_seg = t.phase == kPhaseA ? t.M->k_long : t.M->k_short;
-        t.k_blocks = SPLIT ? 3 * t.k_seg : t.k_seg;
-        t.need = (unsigned)t.step * (2 * t.M->tiles_sym + t.M->tiles_x) + (unsigned)t.phase * t.M->tiles_sym;
-        return true;
+        const OrthMat &M = a.mats[e.q];
+        const int width = phase == kPhaseX ? M.cp : M.sp, from = step & 1, to = from ^ 1;
+        t.n = width - e.j * TN < TN ? width - e.j * TN : TN;
+        t.segs = SPLIT ? 3 : 1, t.k_seg = phase == kPhaseA ? M.k_long : M.k_short;
+        // Of a symmetric matrix the stages of the panels up to the row's own 256 are stored, the others as their mirror image.
+        const int tri_a = (e.i * 128 * CG / 256 + 1) * 4, tri_b = (e.j * TN / 256 + 1) * 4;
+        const bool sym_a = phase == kPhaseB || (phase == kPhaseX && !M.tall), sym_b = phase == kPhaseB || (phase == kPhaseX && M.tall);
+        t.a_lim = phase == kPhaseA ? (M.tall ? 0 : t.k_seg) : sym_a ? tri_a : t.k_seg;
+        t.b_lim = phase == kPhaseA ? (M.tall ? 0 : t.k_seg) : sym_b ? tri_b : 0;
+        t.phase = phase, t.tall = M.tall, t.last = phase == kPhaseX && step == a.steps - 1;
+        t.row0 = t.row_a = e.i * 128 * CG + rank * 128, t.row_b = e.j * TN + rank * (t.n / CG), t.panel0 = e.j * (TN / 64);
+        t.need = (unsigned)step * (2 * M.tiles_sym + M.tiles_x) + (unsigned)phase * M.tiles_sym, t.done = a.done + e.q;
+        __half *sym_hi = phase == kPhaseB ? M.ah : M.bh, *sym_lo = phase == kPhaseB ? M.al : M.bl;
+        t.a_hi = (const char *)(sym_a ? sym_hi : M.xh[from]), t.a_lo = (const char *)(sym_a ? sym_lo : M.xl[from]);
+        t.b_hi = (const char *)(sym_b ? sym_hi : M.xh[from]), t.b_lo = (const char *)(sym_b ? sym_lo : M.xl[from]);
+        t.a_panel = (size_t)(sym_a ? M.sp : M.rp) * 128, t.b_panel = (size_t)(sym_b ? M.sp : M.rp) * 128;
+        t.rp = phase == kPhaseX ? M.rp : M.sp;
+        t.dst_hi = (char *)(phase == kPhaseA ? M.ah : phase == kPhaseB ? M.bh : M.xh[to]);
+        t.dst_lo = (char *)(phase == kPhaseA ? M.al : phase == kPhaseB ? M.bl : M.xl[to]), t.dst_wide = (char *)M.xf[to];
+        t.src_hi = (const char *)(phase == kPhaseB ? M.ah : M.xh[from]), t.src_lo = (const char *)(phase == kPhaseB ? M.al : M.xl[from]);
+        t.src_wide = (const char *)M.xf[from], t.da = M.da, t.db = M.db;
+        t.offset = M.offset, t.stride = M.stride, t.rows = M.rows, t.cols = M.cols, t.scale = M.scale;
     }
-    __device__ __forceinline__ bool ready(Pipe<CG> &p, const Tile &t) const {
-        if (t.need && !p.wait_counter(a.done + t.q, t.need)) return false;
+    __device__ __forceinline__ bool ready(P &p, const Tile &t) const {
+        if (t.need && !p.wait_counter(t.done, t.need)) return false;
         fence_async_proxy();
         return true;
     }
-    // Whether rows (in units of 256) of a symmetric matrix's panel are stored, or their mirror image is.
-    __device__ __forceinline__ static bool mirrored(int row256, int kb) { return row256 < (kb >> 2); }
-    __device__ __forceinline__ bool a_mn(const Tile &t, int kb) const {
-        const int k = SPLIT ? kb % t.k_seg : kb;
-        if (t.phase == kPhaseA) return t.M->tall;
-        if (t.phase == kPhaseX && t.M->tall) return false;
-        return mirrored(CG == 1 ? t.i >> 1 : t.i, k);
-    }
-    __device__ __forceinline__ bool b_mn(const Tile &t, int kb) const {
-        const int k = SPLIT ? kb % t.k_seg : kb;
-        if (t.phase == kPhaseA) return t.M->tall;
-        if (t.phase == kPhaseX && !t.M->tall) return true;
-        return mirrored(SPLIT ? t.j >> 1 : t.j, k);
-    }
-    __device__ __forceinline__ bool chunk_ends(const Tile &t, int kb) const {
-        if (kb + 1 == t.k_blocks) return true;
-        if (!SPLIT || kb + 1 < 2 * t.k_seg) return false;
-        return (kb + 1 - 2 * t.k_seg) % (t.phase == kPhaseX ? kChunkX : kChunkAB) == 0;
+    __device__ __forceinline__ bool chunk_ends(const Tile &t, int seg, int k) const {
+        if (!SPLIT) return k + 1 == t.k_seg;
+        if (k + 1 == t.k_seg) return seg > 0;
+        return seg == 2 && ((k + 1) & ((t.phase == kPhaseX ? kChunkX : kChunkAB) - 1)) == 0;
     }
     __device__ __forceinline__ int bf16() const { return 0; }
-    __device__ __forceinline__ uint32_t bytes(const Tile &t) const { return 128 * 128 + (uint32_t)(t.n / CG) * 128; }
-    // `count` rows from `row`, stage k, of a matrix with `rp` rows: either its panel k, or as columns of its rows 64 k..
-    __device__ __forceinline__ static void load_operand(__half *base, int rp, int row, int count, int k, bool mn,
-                                                        uint32_t dst, uint64_t *bar) {
-        if (!mn) {
-            bulk_copy_in(dst, panel_at(base, rp, k) + (size_t)row * 128, (uint32_t)count * 128, bar);
-        } else {
-            for (int p = 0; p < count / 64; ++p)
-                bulk_copy_in(dst + p * 8192, panel_at(base, rp, row / 64 + p) + (size_t)k * 8192, 8192, bar);
+    // `count` rows from `row` on of a matrix of `rp` rows, stage by stage: its panel k, or, from stage `lim` on, as the columns of
+    // its rows 64 k .. 64 k + 63.
+    struct Operand {
+        const char *k_major, *mn_major;
+        size_t panel;
+        int lim;
+        __device__ __forceinline__ void at(const char *base, int row, size_t panel_bytes) {
+            panel = panel_bytes;
+            k_major = base + (size_t)row * 128;
+            mn_major = base + (size_t)(row / 64) * panel;
         }
-    }
-    __device__ __forceinline__ void load(const Tile &t, int kb, uint32_t sa, uint32_t sb, uint64_t *bar) const {
-        const OrthMat &M = *t.M;
-        const int seg = SPLIT ? kb / t.k_seg : 2, k = SPLIT ? kb - seg * t.k_seg : kb;
-        const bool a_lo = seg == 1, b_lo = seg == 0;
-        const uint32_t rank = CG == 1 ? 0 : cluster_rank();
-        const int row_a = t.i * 128 * CG + (int)rank * 128, row_b = t.j * TN + (int)rank * (t.n / CG), nb = t.n / CG;
-        __half *xh = M.xh[t.step & 1], *xl = M.xl[t.step & 1];
-        const bool am = a_mn(t, kb), bm = b_mn(t, kb);
+        template <int COUNT>
+        __device__ __forceinline__ void load(int k, int count, uint32_t dst, uint64_t *bar) const {
+            if (k < lim) {
+                bulk_copy_in(dst, k_major + (size_t)k * panel, (uint32_t)count * 128, bar);
+            } else {
+                const char *p = mn_major + (size_t)k * 8192;
+#pragma unroll
+                for (int e = 0; e < COUNT / 64; ++e)
+                    if (e * 64 < count) bulk_copy_in(dst + e * 8192, p + (size_t)e * panel, 8192, bar);
+            }
+        }
+    };
+    struct Loader {
+        const char *a_hi, *a_lo, *b_hi, *b_lo;
+        size_t a_panel, b_panel;
+        int row_a, row_b, nb;
+        Operand x, y;
+        __device__ __forceinline__ Loader(const OrthJob &, const Tile &t)
+            : a_hi(t.a_hi), a_lo(t.a_lo), b_hi(t.b_hi), b_lo(t.b_lo), a_panel(t.a_panel), b_panel(t.b_panel), row_a(t.row_a),
+              row_b(t.row_b), nb(t.n / CG) {
+            x.lim = t.a_lim, y.lim = t.b_lim;
+        }
+        __device__ __forceinline__ uint32_t bytes() const { return 128 * 128 + (uint32_t)nb * 128; }
+        // Small products first: hi lo, lo hi, hi hi.
+        __device__ __forceinline__ void seg(int g) {
+            x.at(SPLIT && g == 1 ? a_lo : a_hi, row_a, a_panel);
+            y.at(SPLIT && g == 0 ? b_lo : b_hi, row_b, b_panel);
+        }
+        __device__ __forceinline__ void load(int k, uint32_t sa, uint32_t sb, uint64_t *bar) const {
+            x.template load<128>(k, 128, sa, bar);
+            y.template load<TN / CG>(k, nb, sb, bar);
+        }
+    };
+
+    // The epilogue goes panel by panel (64 columns): a thread has 16 columns of a row.  What it needs of A or X, and what
+    // it makes, passes through shared memory, brought and taken away by bulk copies that a thread of its own issues: written
+    // from the registers, 16 bytes to a row, the same epilogue took twice the time of a tile's products at an inner dimension
+    // of 1024.  fp16 results have three buffers of 32 KB (operand, remainder), so that most of a tile's panels are
+    // there when its products end; 32-bit ones one of 64 KB.
+    static constexpr int kBufs = SPLIT ? 1 : 3;
+    static constexpr uint32_t kLo = 16384, kWide = 32768, kBufBytes = SPLIT ? 65536 : 32768;
+    // Next buffer, and the parity of each one's barriers: every role keeps its own.
+    struct Ring {
+        uint32_t buf = 0, ph = 0;
+        __device__ __forceinline__ uint32_t parity() const { return ph >> buf & 1; }
+        __device__ __forceinline__ void step() {
+            ph ^= 1u << buf;
+            if (++buf == kBufs) buf = 0;
+        }
+    };
+    Ring ring, ring_in;
+
+    __device__ __forceinline__ void load_panel(P &p, const Tile &t, int b) {
+        const uint32_t at = p.extra + ring_in.buf * kBufBytes;
+        uint64_t *bar = &p.sh->extra_full[ring_in.buf];
+        const size_t from = ((size_t)(t.panel0 + b) * t.rp + t.row0) * 128;
         if (t.phase == kPhaseA) {
-            load_operand(a_lo ? xl : xh, M.rp, row_a, 128, k, am, sa, bar);
-            load_operand(b_lo ? xl : xh, M.rp, row_b, nb, k, bm, sb, bar);
-        } else if (t.phase == kPhaseB) {
-            load_operand(a_lo ? M.al : M.ah, M.sp, row_a, 128, k, am, sa, bar);
-            load_operand(b_lo ? M.al : M.ah, M.sp, row_b, nb, k, bm, sb, bar);
-        } else if (!M.tall) {
-            load_operand(a_lo ? M.bl : M.bh, M.sp, row_a, 128, k, am, sa, bar);
-            load_operand(b_lo ? xl : xh, M.rp, row_b, nb, k, bm, sb, bar);
+            mbar_arrive(bar);
+        } else if (SPLIT && t.phase == kPhaseX) {
+            mbar_arrive_expect(bar, 32768);
+            bulk_copy_in(at + kWide, t.src_wide + 2 * from, 32768, bar);
         } else {
-            load_operand(a_lo ? xl : xh, M.rp, row_a, 128, k, am, sa, bar);
-            load_operand(b_lo ? M.bl : M.bh, M.sp, row_b, nb, k, bm, sb, bar);
+            const bool lo = SPLIT || t.phase == kPhaseX;
+            mbar_arrive_expect(bar, lo ? 32768 : 16384);
+            bulk_copy_in(at, t.src_hi + from, 16384, bar);
+            if (lo) bulk_copy_in(at + kLo, t.src_lo + from, 16384, bar);
+        }
+        ring_in.step();
+    }
+    __device__ __forceinline__ void store_panel(P &p, const Tile &t, int b) const {
+        const uint32_t at = p.extra + ring.buf * kBufBytes;
+        const size_t to = ((size_t)(t.panel0 + b) * t.rp + t.row0) * 128;
+        bulk_copy_out(t.dst_hi + to, at, 16384);
+        if (SPLIT || t.phase == kPhaseX) bulk_copy_out(t.dst_lo + to, at + kLo, 16384);
+        if (SPLIT && t.phase == kPhaseX) bulk_copy_out(t.dst_wide + 2 * to, at + kWide, 32768);
+        bulk_out_commit();
+    }
+    // The finished panel in the buffer, in the result's type, to the caller's rows: consecutive threads take consecutive chunks.
+    __device__ __forceinline__ void store_result(P &p, const Tile &t, int panel, int tid) const {
+        const uint32_t at = p.extra + ring.buf * kBufBytes;
+        constexpr int kChunk = SPLIT ? 4 : 8, kSize = SPLIT ? 4 : 2;  // columns of a chunk, bytes of an element
+#pragma unroll 4
+        for (int k = tid; k < 128 * 64 / kChunk; k += kEpiWarps * 32) {
+            const int r = k / (64 / kChunk), c = k % (64 / kChunk), col = panel * 64 + c * kChunk, n = t.cols - col;
+            if (t.row0 + r >= t.rows || n <= 0) continue;
+            const uint4 v = shared_load16(at + (SPLIT ? kWide + wide_chunk(r, c) : panel_chunk(r, c)));
+            char *o = static_cast<char *>(a.out) + (t.offset + (long long)(t.row0 + r) * t.stride + col) * kSize;
+            if (n >= kChunk && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
+                *reinterpret_cast<uint4 *>(o) = v;
+            } else {
+                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int e = 0; e < kChunk; ++e) {
+                    if (e >= n) break;
+                    if (SPLIT) reinterpret_cast<uint32_t *>(o)[e] = w[e];
+                    else reinterpret_cast<uint16_t *>(o)[e] = (uint16_t)(e & 1 ? w[e / 2] >> 16 : w[e / 2] & 0xffff);
+                }
+            }
         }
     }
 
-    __device__ __forceinline__ bool epilogue(Pipe<CG> &p, const Tile &t, typename Pipe<CG>::Turn &turn, int warp, int lane) const {
+    // The copying thread: loads panels in order as buffers come free and the earlier phases are done, tile after tile, takes
+    // each finished panel away, and tells the matrix's counter when a whole tile is in memory.  It never blocks on a later
+    // tile's loads (what they wait for may be this CTA's own tile) while there is a panel to take away.
+    __device__ __forceinline__ bool copier(P &p) {
+        typename P::Walk ahead, behind;                              // tile of the next load, of the next panel to take away
+        int b_in = 0, b_out = 0, used = 0;                           // panels of these, buffers in use
+        bool end = false, known = false, go = false, signal = false; // go: the tile `ahead` may be loaded; signal: one is due
+        long long t0 = clock64();
+        for (;;) {
+            bool moved = false;
+            while (!end && used < kBufs) {
+                if (!known) {
+                    if (!mbar_test(&p.sh->tile_full[ahead.slot], ahead.ph)) break;
+                    known = true;
+                    if (p.template tile_at<Tile>(ahead)->n == 0) {
+                        end = true;
+                        break;
+                    }
+                }
+                const Tile &t = *p.template tile_at<Tile>(ahead);
+                if (!go && t.phase != kPhaseA) {
+                    unsigned v;
+                    asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(t.done) : "memory");
+                    if (v < t.need) break;
+                    fence_async_proxy();
+                }
+                go = true;
+                bulk_out_read<0>();
+                load_panel(p, t, b_in);
+                ++used, moved = true;
+                if (++b_in == t.n / 64) b_in = 0, known = go = false, ahead.step();
+            }
+            if (signal) {
+                const Tile &t = *p.template tile_at<Tile>(behind);
+                bulk_out_done();
+                fence_async_proxy();                                 // the next phase reads through the copy engine
+                asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(t.done) : "memory");
+                signal = false, moved = true;
+                p.tile_done(behind);
+            }
+            if (used > 0) {
+                const Tile &t = *p.template tile_at<Tile>(behind);
+                if (mbar_test(t.last ? &p.sh->extra_free[ring.buf] : &p.sh->extra_done[ring.buf], ring.parity())) {
+                    if (!t.last) store_panel(p, t, b_out);
+                    ring.step();
+                    --used, moved = true;
+                    if (++b_out == t.n / 64) {
+                        b_out = 0;
+                        if (t.last) p.tile_done(behind);
+                        else signal = true;
+                    }
+                }
+            } else if (end && !signal) {
+                return true;
+            }
+            if (moved) {
+                t0 = clock64();
+            } else {
+                if (p.sh->dead) return false;
+                if (clock64() - t0 > kWaitCycles) {
+                    p.fail();
+                    return false;
+                }
+            }
+        }
+    }
+
+    __device__ __forceinline__ bool epilogue(P &p, const Tile &t, typename P::Turn &turn, int warp, int lane) {
+        const int tid = warp * 32 + lane, side = warp / 4, r = warp % 4 * 32 + lane, row = t.row0 + r, panels = t.n / 64;
+        const bool last = t.last;
+        float d_row = 0.f;
         uint32_t tmem;
-        float sum[2][32];                                            // of a 32-bit result's chunks
-        const int half = t.n / 2, c0 = warp / 4 * half;              // this warp's columns of the tile
+        float sum[2][16];                                            // of a 32-bit result's chunks
         if (SPLIT) {
-            for (int kb = 0, done = 0; kb < t.k_blocks; ++kb) {
-                if (!chunk_ends(t, kb)) continue;
+            const int each = t.phase == kPhaseX ? kChunkX : kChunkAB, chunks = 1 + (t.k_seg + each - 1) / each;
+            for (int c = 0, done = 0; c < chunks; ++c) {
                 if (!p.take(turn, tmem)) return false;
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
-                    float v[32];
-                    tmem_load32(tmem + c0 + b * 32, v);
+                    float v[16];
+                    tmem_load(tmem + b * 64 + side * 16, v);
 #pragma unroll
-                    for (int k = 0; k < 32; ++k) sum[b][k] = __fadd_rn(done ? sum[b][k] : 0.f, v[k]);
+                    for (int k = 0; k < 16; ++k) sum[b][k] = __fadd_rn(done ? sum[b][k] : 0.f, v[k]);
                 }
                 p.release(turn, lane);
                 done = 1;
@@ -380,111 +553,125 @@ struct OrthJob {
         } else if (!p.take(turn, tmem)) {
             return false;
         }
-        const OrthMat &M = *t.M;
-        const int row = t.i * 128 * CG + (int)p.rank * 128 + warp % 4 * 32 + lane;
-        float d_row = 0.f;
-        if (t.phase != kPhaseA) {
-            unsigned seen;                                           // reached already: the products had to wait for it
-            asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(seen) : "l"(a.done + t.q) : "memory");
-            if (t.phase == kPhaseB) d_row = __ldcg(M.da + row);
-            else if (!M.tall) d_row = __ldcg(M.db + row);
-        }
-        const bool last = t.phase == kPhaseX && t.step == a.steps - 1;
-        __half *src_h = t.phase == kPhaseB ? M.ah : M.xh[t.step & 1], *src_l = t.phase == kPhaseB ? M.al : M.xl[t.step & 1];
-        __half *dst_h = t.phase == kPhaseA ? M.ah : t.phase == kPhaseB ? M.bh : M.xh[t.step & 1 ^ 1];
-        __half *dst_l = t.phase == kPhaseA ? M.al : t.phase == kPhaseB ? M.bl : M.xl[t.step & 1 ^ 1];
-        const int rp = t.phase == kPhaseX ? M.rp : M.sp;
 #pragma unroll(SPLIT ? 2 : 1)
-        for (int b = 0; b < (SPLIT ? 64 : half); b += 32) {
-            const int col = t.j * TN + c0 + b;
-            float v[32];
+        for (int b = 0; b < (SPLIT ? 2 : panels); ++b) {
+            const int panel = t.panel0 + b, col = panel * 64 + side * 16;
+            if (!p.warp_wait(&p.sh->extra_full[ring.buf], ring.parity())) return false;
+            if (b == 0 && t.phase != kPhaseA) {
+                unsigned seen;                                       // reached already: the loads had to wait for it
+                asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(seen) : "l"(t.done) : "memory");
+                if (t.phase == kPhaseB) d_row = __ldcg(t.da + row);
+                else if (!t.tall) d_row = __ldcg(t.db + row);
+            }
+            const uint32_t at = p.extra + ring.buf * kBufBytes;
+            float v[16];
             if (SPLIT) {
 #pragma unroll
-                for (int k = 0; k < 32; ++k) v[k] = sum[b / 32][k];
+                for (int k = 0; k < 16; ++k) v[k] = sum[b][k];
             } else {
-                tmem_load32(tmem + c0 + b, v);
-                if (b + 32 >= half) p.release(turn, lane);
+                tmem_load(tmem + b * 64 + side * 16, v);
+                if (b + 1 == panels) p.release(turn, lane);
             }
+            const unsigned on = (unsigned)(row - col);               // the diagonal is at column `on` of the 16, if below 16
             if (t.phase == kPhaseA) {
+                if (on < 16u) {
 #pragma unroll
-                for (int k = 0; k < 32; ++k) {
-                    if (col + k == row) {
-                        M.da[row] = v[k] * kUnscale2;
-                        v[k] = 0.f;
-                    }
-                    v[k] *= kUnscale;
+                    for (int k = 0; k < 16; ++k)
+                        if (on == (unsigned)k) t.da[row] = v[k] * kUnscale2, v[k] = 0.f;
+                    __threadfence();
                 }
+#pragma unroll
+                for (int k = 0; k < 16; ++k) v[k] *= kUnscale;
             } else {
-                float x[32];
+                float x[16];
                 if (SPLIT && t.phase == kPhaseX) {
-                    const float4 *w = wide_at(M.xf[t.step & 1], rp, row, col);
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        const float4 f = __ldcg(w + k);
-                        x[4 * k] = f.x, x[4 * k + 1] = f.y, x[4 * k + 2] = f.z, x[4 * k + 3] = f.w;
+                    for (int k = 0; k < 4; ++k) {
+                        const uint4 f = shared_load16(at + kWide + wide_chunk(r, side * 4 + k));
+                        x[4 * k] = __uint_as_float(f.x), x[4 * k + 1] = __uint_as_float(f.y);
+                        x[4 * k + 2] = __uint_as_float(f.z), x[4 * k + 3] = __uint_as_float(f.w);
                     }
-                } else
+                } else {
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const uint32_t at = panel_chunk(row, (col % 64) / 8 + k);
-                    unpack8(__ldcg(reinterpret_cast<const uint4 *>(panel_at(src_h, rp, col / 64) + at)), x + 8 * k);
-                    if (SPLIT || t.phase == kPhaseX) {
-                        float l[8];
-                        unpack8(__ldcg(reinterpret_cast<const uint4 *>(panel_at(src_l, rp, col / 64) + at)), l);
+                    for (int k = 0; k < 2; ++k) {
+                        unpack8(shared_load16(at + panel_chunk(r, side * 2 + k)), x + 8 * k);
+                        if (SPLIT || t.phase == kPhaseX) {
+                            float l[8];
+                            unpack8(shared_load16(at + kLo + panel_chunk(r, side * 2 + k)), l);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) x[8 * k + e] += l[e];
+                            for (int e = 0; e < 8; ++e) x[8 * k + e] += l[e];
+                        }
                     }
                 }
                 if (t.phase == kPhaseB) {
                     // x is A without its diagonal, times 2^12
+                    if (on < 16u) {
 #pragma unroll
-                    for (int k = 0; k < 32; ++k) {
-                        const float d = d_row + __ldcg(M.da + col + k);
-                        const float sq = __fmaf_rn(d, x[k], v[k] * kUnscale);
-                        if (col + k == row) {
-                            M.db[row] = __fmaf_rn(kC, __fmaf_rn(d_row, d_row, v[k] * kUnscale2), kB * d_row);
-                            v[k] = 0.f;
-                        } else {
-                            v[k] = __fmaf_rn(kC, sq, kB * x[k]);
+                        for (int k = 0; k < 16; ++k)
+                            if (on == (unsigned)k)
+                                t.db[row] = __fmaf_rn(kC, __fmaf_rn(d_row, d_row, v[k] * kUnscale2), kB * d_row), v[k] = 0.f;
+                        __threadfence();
+                    }
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const float4 dc = __ldcg(reinterpret_cast<const float4 *>(t.da + col) + k);
+                        const float d[4] = {dc.x, dc.y, dc.z, dc.w};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const int i = 4 * k + e;
+                            const float sq = __fmaf_rn(d_row + d[e], x[i], v[i] * kUnscale);
+                            v[i] = on == (unsigned)i ? 0.f : __fmaf_rn(kC, sq, kB * x[i]);
                         }
                     }
-                } else {
+                } else if (t.tall) {
 #pragma unroll
-                    for (int k = 0; k < 32; ++k) {
-                        const float d = M.tall ? __ldcg(M.db + col + k) : d_row;
-                        v[k] = __fmaf_rn(kA + d, x[k], v[k] * kUnscale);
+                    for (int k = 0; k < 4; ++k) {
+                        const float4 dc = __ldcg(reinterpret_cast<const float4 *>(t.db + col) + k);
+                        const float d[4] = {dc.x, dc.y, dc.z, dc.w};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) v[4 * k + e] = __fmaf_rn(kA + d[e], x[4 * k + e], v[4 * k + e] * kUnscale);
                     }
+                } else {
+                    const float f = kA + d_row;
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) v[k] = __fmaf_rn(f, x[k], v[k] * kUnscale);
                 }
             }
             if (last) {
-                const float f = kUnscale * M.scale;
+                const float f = kUnscale * t.scale;
 #pragma unroll
-                for (int k = 0; k < 32; ++k) v[k] *= f;
-                if (row < M.rows && col < M.cols)
-                    store_row32(a.out, M.offset + (long long)row * M.stride + col, M.cols - col, a.out_type, v);
-            } else {
-                if (SPLIT && t.phase == kPhaseX) {
-                    float4 *w = wide_at(M.xf[t.step & 1 ^ 1], rp, row, col);
+                for (int k = 0; k < 16; ++k) v[k] *= f;
+            }
+            if (!(SPLIT && last)) {
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) w[k] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
-                }
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
+                for (int k = 0; k < 2; ++k) {
+                    const float *e = v + 8 * k;
                     uint4 hi, lo;
-                    split8(v + 8 * k, hi, lo);
-                    const uint32_t at = panel_chunk(row, (col % 64) / 8 + k);
-                    *reinterpret_cast<uint4 *>(panel_at(dst_h, rp, col / 64) + at) = hi;
-                    if (SPLIT || t.phase == kPhaseX)
-                        *reinterpret_cast<uint4 *>(panel_at(dst_l, rp, col / 64) + at) = lo;
+                    split8(e, hi, lo);
+                    if (last && a.out_type == CSER_TYPE_BF16)
+                        hi = make_uint4(pack_bf162(e[0], e[1]), pack_bf162(e[2], e[3]), pack_bf162(e[4], e[5]), pack_bf162(e[6], e[7]));
+                    shared_store16(at + panel_chunk(r, side * 2 + k), hi);
+                    if (SPLIT || t.phase == kPhaseX) shared_store16(at + kLo + panel_chunk(r, side * 2 + k), lo);
                 }
             }
-        }
-        if (!last) {
-            __threadfence();
-            fence_async_proxy();                                     // the next phase reads through the copy engine
-            p.epi_sync();
-            if (warp == 0 && lane == 0)
-                asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(a.done + t.q) : "memory");
+            if (SPLIT && t.phase == kPhaseX) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    shared_store16(at + kWide + wide_chunk(r, side * 4 + k),
+                                   make_uint4(__float_as_uint(v[4 * k]), __float_as_uint(v[4 * k + 1]), __float_as_uint(v[4 * k + 2]),
+                                              __float_as_uint(v[4 * k + 3])));
+            }
+            fence_async_proxy();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&p.sh->extra_done[ring.buf]);
+            if (last) {
+                if (!p.warp_wait(&p.sh->extra_done[ring.buf], ring.parity())) return false;
+                store_result(p, t, panel, tid);
+                fence_async_proxy();                                 // read before the copy engine writes here again
+                __syncwarp();
+            }
+            if (lane == 0) mbar_arrive(&p.sh->extra_free[ring.buf]);
+            ring.step();
         }
         return true;
     }
@@ -493,9 +680,9 @@ struct OrthJob {
 template <int CG, bool SPLIT>
 __global__ void __launch_bounds__(kThreads, 1) orth_products_kernel(const __grid_constant__ OrthArgs a) {
     extern __shared__ unsigned char raw[];
-    Pipe<CG> p;
-    p.setup(raw, a.err);
-    OrthJob<CG, SPLIT> job{a, (int)blockIdx.x / CG, (int)gridDim.x / CG, 2 * a.n_sym + a.n_x};
+    OrthPipe<CG, SPLIT> p;
+    p.template setup<OrthJob<CG, SPLIT>>(raw, a.err);
+    OrthJob<CG, SPLIT> job{a, (int)blockIdx.x / CG, (int)gridDim.x / CG};
     p.run(job);
     p.teardown();
 }
@@ -535,7 +722,7 @@ cudaError_t products_launch(const OrthArgs &a, int grid, cudaStream_t st) {
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)grid);
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = Pipe<CG>::kSharedBytes;
+    cfg.dynamicSmemBytes = OrthPipe<CG, SPLIT>::kSharedBytes;
     cfg.stream = st;
     cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeCooperative;
@@ -549,12 +736,12 @@ cudaError_t products_launch(const OrthArgs &a, int grid, cudaStream_t st) {
 template <int CG, bool SPLIT>
 cudaError_t products_setup(int &pairs) {
     cudaError_t e = cudaFuncSetAttribute(orth_products_kernel<CG, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                         (int)Pipe<CG>::kSharedBytes);
+                                         (int)OrthPipe<CG, SPLIT>::kSharedBytes);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(CG);
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = Pipe<CG>::kSharedBytes;
+    cfg.dynamicSmemBytes = OrthPipe<CG, SPLIT>::kSharedBytes;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = CG, at[0].val.clusterDim.y = 1, at[0].val.clusterDim.z = 1;
@@ -587,9 +774,36 @@ size_t work_of(const OrthMat &M, bool split) {
     return (size_t)M.rp * M.cp * 2 * (split ? 8 : 4) + (size_t)M.sp * M.sp * 2 * (split ? 4 : 2) + (size_t)M.sp * 8;
 }
 
-int build_group(cser_orth *h, cser_orth::Group &G, const std::vector<HostMat> &ms, int cg) {
+// Tiles of 256 rows by a pair of CTAs, or of 128 by one.
+bool pairs_pay(const std::vector<HostMat> &all, bool split, int pairs) {
+    if (getenv("CSER_CG")) return atoi(getenv("CSER_CG")) == 2;
+    double area[3] = {0, 0, 0};
+    for (const HostMat &m : all)
+        for (int cg = 1; cg <= 2; ++cg) {
+            OrthMat M;
+            shape_of(m, cg, M);
+            area[cg] += (double)M.rp * M.cp;
+        }
+    return area[2] <= 1.15 * area[1] && area[2] >= 65536.0 * pairs;
+}
+
+int build_group(cser_orth *h, cser_orth::Group &G, const std::vector<HostMat> &ms, int cg, int steps, int pairs) {
     std::vector<OrthMat> mats(ms.size());
     std::vector<OrthTile> sym, xs;
+    std::vector<OrthBatch> batch;
+    size_t in_batch = 0, widest = 0;
+    auto close_batch = [&](size_t next_bytes) {     // opens a batch at the lists' ends where this one is full
+        if (!batch.empty()) {
+            OrthBatch &B = batch.back();
+            B.n_sym = (int)sym.size() - B.sym, B.n_x = (int)xs.size() - B.x;
+            if (next_bytes && in_batch + next_bytes <= (getenv("CSER_BB") ? (size_t)atoi(getenv("CSER_BB")) << 20 : kBatchBytes)) return;
+            if ((size_t)B.n_sym > widest) widest = B.n_sym;
+            if ((size_t)B.n_x > widest) widest = B.n_x;
+        }
+        const long long from = batch.empty() ? 0 : batch.back().first + (long long)steps * (2 * batch.back().n_sym + batch.back().n_x);
+        batch.push_back({(int)sym.size(), 0, (int)xs.size(), 0, from});
+        in_batch = 0;
+    };
     std::vector<uint2> chunk;
     std::vector<ConvertUnit> unit;
     size_t at = 0;
@@ -598,6 +812,8 @@ int build_group(cser_orth *h, cser_orth::Group &G, const std::vector<HostMat> &m
     for (size_t q = 0; q < ms.size(); ++q) {
         OrthMat &M = mats[q];
         shape_of(ms[q], cg, M);
+        close_batch(work_of(M, h->split));
+        in_batch += work_of(M, h->split);
         const size_t xb = (size_t)M.rp * M.cp * 2, ab = (size_t)M.sp * M.sp * 2;
         auto take = [&](size_t b) { char *p = base + at; at += b; return reinterpret_cast<__half *>(p); };
         M.xh[0] = take(xb), M.xl[0] = take(xb), M.xh[1] = take(xb), M.xl[1] = take(xb), M.ah = take(ab), M.bh = take(ab);
@@ -611,7 +827,7 @@ int build_group(cser_orth *h, cser_orth::Group &G, const std::vector<HostMat> &m
         for (int c = 0; c < M.chunks; ++c) chunk.push_back(make_uint2((unsigned)q, (unsigned)c));
         for (int r = 0; r < M.rp; r += 32)
             for (int c = 0; c < M.cp; c += 256) unit.push_back({(uint32_t)q, (uint32_t)r, (uint32_t)c});
-        const int tm = 128 * cg, tn = tile_n(h->split);
+        const int tm = 128 * cg, tn = tile_n(cg, h->split);
         for (int j = 0; j * tn < M.sp; ++j)
             for (int i = 0; i * tm < M.sp; ++i)
                 if (i * tm / 256 >= j * tn / 256) sym.push_back({(uint32_t)q, (uint16_t)i, (uint16_t)j}), M.tiles_sym += cg;
@@ -623,12 +839,13 @@ int build_group(cser_orth *h, cser_orth::Group &G, const std::vector<HostMat> &m
                 for (int i = 0; i * tm < M.rp; ++i) xs.push_back({(uint32_t)q, (uint16_t)i, (uint16_t)j}), M.tiles_x += cg;
         }
     }
+    close_batch(0);
     const size_t n = ms.size();
     size_t bytes = 0;
     auto place = [&](size_t b) { const size_t p = bytes; bytes += (b + 255) / 256 * 256; return p; };
     const size_t o_mat = place(n * sizeof(OrthMat)), o_sym = place(sym.size() * sizeof(OrthTile)),
                  o_x = place(xs.size() * sizeof(OrthTile)), o_ck = place(chunk.size() * sizeof(uint2)),
-                 o_un = place(unit.size() * sizeof(ConvertUnit)), o_done = place(n * 4), o_tick = place(n * 4),
+                 o_un = place(unit.size() * sizeof(ConvertUnit)), o_ba = place(batch.size() * sizeof(OrthBatch)), o_done = place(n * 4), o_tick = place(n * 4),
                  o_inv = place(n * 4), o_part = place((size_t)chunk0 * 4);
     TRY(cudaMalloc(&G.tables, bytes));
     char *t = static_cast<char *>(G.tables);
@@ -638,15 +855,18 @@ int build_group(cser_orth *h, cser_orth::Group &G, const std::vector<HostMat> &m
     TRY(cudaMemcpy(t + o_x, xs.data(), xs.size() * sizeof(OrthTile), cudaMemcpyHostToDevice));
     TRY(cudaMemcpy(t + o_ck, chunk.data(), chunk.size() * sizeof(uint2), cudaMemcpyHostToDevice));
     TRY(cudaMemcpy(t + o_un, unit.data(), unit.size() * sizeof(ConvertUnit), cudaMemcpyHostToDevice));
+    TRY(cudaMemcpy(t + o_ba, batch.data(), batch.size() * sizeof(OrthBatch), cudaMemcpyHostToDevice));
     OrthArgs &A = G.args;
+    A.batch = reinterpret_cast<OrthBatch *>(t + o_ba), A.steps = steps;
     A.mats = reinterpret_cast<OrthMat *>(t + o_mat);
-    A.sym = reinterpret_cast<OrthTile *>(t + o_sym), A.n_sym = (int)sym.size();
-    A.x = reinterpret_cast<OrthTile *>(t + o_x), A.n_x = (int)xs.size();
+    A.sym = reinterpret_cast<OrthTile *>(t + o_sym);
+    A.x = reinterpret_cast<OrthTile *>(t + o_x);
     A.chunk = reinterpret_cast<uint2 *>(t + o_ck), A.unit = reinterpret_cast<ConvertUnit *>(t + o_un);
     A.done = reinterpret_cast<unsigned *>(t + o_done), A.ticket = reinterpret_cast<unsigned *>(t + o_tick);
     A.inv = reinterpret_cast<float *>(t + o_inv), A.partial = reinterpret_cast<float *>(t + o_part);
     A.out_type = h->out_type;
     G.n_chunk = (int)chunk.size(), G.n_unit = (int)unit.size(), G.cg = cg;
+    G.grid = (widest < (size_t)pairs ? (int)widest : pairs) * cg;
     return CSER_OK;
 }
 
@@ -698,7 +918,7 @@ cser_orth_handle cser_orth_create(int32_t n_workers, int64_t ld, int32_t n_matri
             orth_fail(h, CSER_ERR_CUDA, er != cudaSuccess ? cudaGetErrorString(er) : "the kernel does not fit this GPU");
             return nullptr;
         }
-        const int cg = 1;
+        const int cg = pairs_pay(all, h->split, pairs[2]) ? 2 : 1;
         // Groups that fit the workspace, one after the other.
         std::vector<std::vector<HostMat>> parts;
         size_t most = 0, now = 0;
@@ -722,13 +942,11 @@ cser_orth_handle cser_orth_create(int32_t n_workers, int64_t ld, int32_t n_matri
         h->groups.resize(parts.size());
         for (size_t g = 0; g < parts.size(); ++g) {
             cser_orth::Group &G = h->groups[g];
-            if (build_group(h, G, parts[g], cg) != CSER_OK) {
+            if (build_group(h, G, parts[g], cg, steps, pairs[cg]) != CSER_OK) {
                 cser_orth_destroy(h);
                 return nullptr;
             }
-            G.args.steps = steps, G.args.err = err_dev;
-            const int widest = G.args.n_sym > G.args.n_x ? G.args.n_sym : G.args.n_x;
-            G.grid = (widest < pairs[cg] ? widest : pairs[cg]) * cg;
+            G.args.err = err_dev;
         }
         return h;
     } catch (const std::bad_alloc &) {
@@ -765,8 +983,9 @@ int cser_orth_apply(cser_orth_handle h, const void *grad, float *m, float mu, vo
         else if (h->in_type == CSER_TYPE_BF16) prologue_launch<__nv_bfloat16>(G, a, st);
         else prologue_launch<__half>(G, a, st);
         TRY(cudaGetLastError());
-        if (h->split) TRY((products_launch<1, true>(a, G.grid, st)));
-        else TRY((products_launch<1, false>(a, G.grid, st)));
+        cudaError_t e = G.cg == 1 ? (h->split ? products_launch<1, true>(a, G.grid, st) : products_launch<1, false>(a, G.grid, st))
+                                  : (h->split ? products_launch<2, true>(a, G.grid, st) : products_launch<2, false>(a, G.grid, st));
+        TRY(e);
         h->launches += 3;
     }
     return CSER_OK;

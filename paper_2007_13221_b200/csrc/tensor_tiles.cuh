@@ -2,8 +2,10 @@
 // fifth-generation tensor cores with operands brought by asynchronous copies, accumulators in tensor memory, and
 // an epilogue of the operator's own.  Device code; included by orth.cu and xent.cu inside their unnamed namespaces.
 //
-// Roles.  A CTA is 12 warps: warp 0 issues the copies, warp 1 issues the matrix instructions, warps 4-11 are the
-// epilogue (warp w reads the tensor-memory lanes 32*(w%4)..+31, the half (w-4)/4 of a tile's columns).  Two
+// Roles.  A CTA is 20 warps: warp 0 issues the copies, warp 1 issues the matrix instructions, warp 2 works out what the next
+// tiles are and leaves that in shared memory, warp 3 may copy for the epilogue, warps 4-19 are the epilogue (warp w reads
+// the tensor-memory lanes 32*(w%4)..+31, the quarter (w-4)/4 of the columns; with 8 epilogue warps, two to a scheduler, the
+// latencies of their arithmetic showed: 3000 cycles for 128 x 64 values).  Two
 // accumulators of 256 columns take turns, so the epilogue of one tile runs under the products of the next.  With
 // CG = 2 the CTAs of a cluster of two work on one 256 x 256 tile: each brings half of both operands (half the
 // traffic per product of a single CTA's 128 x 256 tile), and the first one issues the instructions for both.
@@ -21,9 +23,8 @@
 #include "bulk_copy.cuh"
 
 constexpr int kStageK = 64;                        // inner dimension of one stage: one panel's width
-constexpr int kThreads = 384;
-constexpr int kEpiWarp0 = 4;
-constexpr int kEpiThreads = 256;
+constexpr int kEpiWarp0 = 4, kEpiWarps = 16;
+constexpr int kThreads = (kEpiWarp0 + kEpiWarps) * 32;
 
 // ------------------------------------------------------------------ small PTX
 __device__ __forceinline__ uint32_t cluster_rank() {
@@ -38,13 +39,14 @@ __device__ __forceinline__ void cluster_sync_all() {
 __device__ __forceinline__ void mbar_arrive_remote(uint64_t *bar, uint32_t rank) {
     uint32_t a;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_addr(bar)), "r"(rank));
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(a) : "memory");
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(a) : "memory");
 }
-__device__ __forceinline__ bool mbar_try_wait_cluster(uint64_t *bar, uint32_t parity) {
+// Whether the phase is over, without waiting.
+__device__ __forceinline__ bool mbar_test(uint64_t *bar, uint32_t parity) {
     uint32_t done;
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
         "selp.u32 %0, 1, 0, p;\n\t}"
         : "=r"(done)
         : "r"(smem_addr(bar)), "r"(parity)
@@ -56,6 +58,22 @@ __device__ __forceinline__ void bulk_copy_in(uint32_t dst, const void *src, uint
     asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
                  "l"(src), "r"(bytes), "r"(smem_addr(bar))
                  : "memory");
+}
+// `bytes` from shared memory to global; the thread's copies are counted in groups.
+__device__ __forceinline__ void bulk_copy_out(void *dst, uint32_t src, uint32_t bytes) {
+    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void bulk_out_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+// Until all but the last LEFT groups have read their source / are done.
+template <int LEFT> __device__ __forceinline__ void bulk_out_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(LEFT) : "memory"); }
+__device__ __forceinline__ void bulk_out_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+__device__ __forceinline__ uint4 shared_load16(uint32_t at) {
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ void shared_store16(uint32_t at, uint4 v) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
 // A box of a three-dimensional tensor (column, row, worker); the column is a multiple of 64 everywhere here.
 __device__ __forceinline__ void tensor_copy_in(uint32_t dst, const CUtensorMap *map, int col, int row, int worker,
@@ -122,8 +140,20 @@ __device__ __forceinline__ void mma_commit(uint64_t *bar) {
 __device__ __forceinline__ void tmem_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tmem_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 
-// 32 columns of this warp's 32 lanes: thread = lane (row), register = column.
-__device__ __forceinline__ void tmem_load32(uint32_t addr, float (&v)[32]) {
+// 16 or 32 columns of this warp's 32 lanes: thread = lane (row), register = column.
+__device__ __forceinline__ void tmem_load(uint32_t addr, float (&v)[16]) {
+    uint32_t r[16];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(addr)
+        : "memory");
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void tmem_load(uint32_t addr, float (&v)[32]) {
     uint32_t r[32];
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
@@ -140,16 +170,19 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, float (&v)[32]) {
     for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
 }
 
-// Shared-memory operand descriptor, 128-byte swizzle.  K-major: 8-row groups are 1024 bytes apart.  MN-major: panels
-// of 64 along M or N are 64 rows (8192 bytes) apart, 8-row groups along K 1024 bytes.
-__device__ __forceinline__ uint64_t operand_desc(uint32_t addr, bool mn) {
-    const uint64_t lead = mn ? 8192 / 16 : 1, stride = 1024 / 16;
-    return (uint64_t)((addr & 0x3ffff) >> 4) | (lead << 16) | (stride << 32) | (1ull << 46) | (2ull << 61);
+// Shared-memory operand descriptor, 128-byte swizzle, without the address (its bits 4..17 go into the lowest 14).  K-major:
+// 8-row groups are 1024 bytes apart.  MN-major: panels of 64 along M or N are 64 rows (8192 bytes) apart, 8-row groups
+// along K 1024 bytes.
+__device__ __forceinline__ constexpr uint64_t operand_desc(bool mn) {
+    return ((uint64_t)(mn ? 8192 / 16 : 1) << 16) | ((uint64_t)(1024 / 16) << 32) | (1ull << 46) | (2ull << 61);
 }
-// Instruction descriptor: fp32 accumulators, A and B both fp16 (0) or bf16 (1), M = 128 * CG.
-__device__ __forceinline__ uint32_t instr_desc(int bf16, bool a_mn, bool b_mn, int n, int cg) {
-    return (1u << 4) | ((uint32_t)bf16 << 7) | ((uint32_t)bf16 << 10) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) |
-           ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 * cg >> 4) << 24);
+// Descriptor units (16 bytes) from one 16 of the inner dimension to the next inside a stage.
+__device__ __forceinline__ constexpr uint32_t operand_step(bool mn) { return mn ? 2048 / 16 : 32 / 16; }
+// Instruction descriptor: fp32 accumulators, A and B both fp16 (0) or bf16 (1), M = 128 * CG; bits 15 and 16 say that A and
+// B are MN-major.
+__device__ __forceinline__ uint32_t instr_desc(int bf16, int n, int cg) {
+    return (1u << 4) | ((uint32_t)bf16 << 7) | ((uint32_t)bf16 << 10) | ((uint32_t)(n >> 3) << 17) |
+           ((uint32_t)(128 * cg >> 4) << 24);
 }
 
 // Byte offset of the 16-byte chunk `c` (0..7) of row r inside a panel.
@@ -164,54 +197,47 @@ __device__ __forceinline__ uint32_t pack_bf162(float a, float b) {
     const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
     return *reinterpret_cast<const uint32_t *>(&h);
 }
-// min(n, 32) values to elements at, at + 1, ... of an array of CSER_TYPE_* `type`; 16 bytes at a time where they are aligned.
-__device__ __forceinline__ void store_row32(void *base, long long at, int n, int type, const float (&v)[32]) {
-    if (type == CSER_TYPE_F32) {
-        float *o = static_cast<float *>(base) + at;
-        if (n >= 32 && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
+// min(n, N) values to 16-bit elements at, at + 1, ... ; 16 bytes at a time where they are aligned.
+template <int N>
+__device__ __forceinline__ void store_row(void *base, long long at, int n, bool bf16, const float (&v)[N]) {
+    uint32_t w[N / 2];
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
-                reinterpret_cast<float4 *>(o)[k] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
-        } else {
+    for (int k = 0; k < N / 2; ++k) w[k] = bf16 ? pack_bf162(v[2 * k], v[2 * k + 1]) : pack_half2(v[2 * k], v[2 * k + 1]);
+    uint16_t *o = static_cast<uint16_t *>(base) + at;
+    if (n >= N && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
 #pragma unroll
-            for (int k = 0; k < 32; ++k)
-                if (k < n) o[k] = v[k];
-        }
+        for (int k = 0; k < N / 8; ++k)
+            reinterpret_cast<uint4 *>(o)[k] = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
     } else {
-        uint32_t w[16];
 #pragma unroll
-        for (int k = 0; k < 16; ++k)
-            w[k] = type == CSER_TYPE_BF16 ? pack_bf162(v[2 * k], v[2 * k + 1]) : pack_half2(v[2 * k], v[2 * k + 1]);
-        uint16_t *o = static_cast<uint16_t *>(base) + at;
-        if (n >= 32 && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                reinterpret_cast<uint4 *>(o)[k] = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
-        } else {
-#pragma unroll
-            for (int k = 0; k < 32; ++k)
-                if (k < n) o[k] = (uint16_t)(k & 1 ? w[k / 2] >> 16 : w[k / 2] & 0xffff);
-        }
+        for (int k = 0; k < N; ++k)
+            if (k < n) o[k] = (uint16_t)(k & 1 ? w[k / 2] >> 16 : w[k / 2] & 0xffff);
     }
 }
 
 // ------------------------------------------------------------------ the pipeline
-template <int CG>
+// TN: columns of a tile (at most 256).  EXTRA: bytes of shared memory for the epilogue, a multiple of 1024.
+template <int CG, int TN = 256, int EXTRA = 0>
 struct Pipe {
     static constexpr int kABytes = 128 * 128;                       // this CTA's 128 rows of the first operand
-    static constexpr int kBBytes = (CG == 1 ? 256 : 128) * 128;     // this CTA's share of the second
+    static constexpr int kBBytes = TN / CG * 128;                   // this CTA's share of the second
     static constexpr int kStageBytes = kABytes + kBBytes;
-    static constexpr int kStages = CG == 1 ? 4 : 6;
-    static constexpr int kTileM = 128 * CG;
+    static constexpr int kStages = (225 * 1024 - EXTRA) / kStageBytes;
+
+    static constexpr int kTiles = 4, kTileBytes = 256;               // tiles known ahead
 
     struct Shared {
         uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2], drain;
+        uint64_t extra_full[3], extra_done[3], extra_free[3];         // the epilogue's buffers, see orth.cu
+        uint64_t tile_full[kTiles], tile_empty[kTiles];
         uint32_t tmem;
         volatile int dead;
+        alignas(16) unsigned char tile[kTiles][kTileBytes];
     };
-    static constexpr size_t kSharedBytes = 1024 + (size_t)kStages * kStageBytes + sizeof(Shared);
+    static constexpr size_t kSharedBytes = 1024 + (size_t)kStages * kStageBytes + EXTRA + sizeof(Shared);
+    static_assert(kSharedBytes <= 227 * 1024, "shared memory of a CTA");
 
-    uint32_t stage0;                                                // 1024-byte aligned shared address
+    uint32_t stage0, extra;                                         // 1024-byte aligned shared addresses
     Shared *sh;
     unsigned *err;                                                  // the handle's word, mapped host memory
     uint32_t rank;
@@ -224,12 +250,12 @@ struct Pipe {
         }
     }
     __device__ __forceinline__ bool wait(uint64_t *bar, uint32_t parity) {
-        if (CG == 1 ? mbar_try_wait(bar, parity) : mbar_try_wait_cluster(bar, parity)) return true;
+        if (mbar_try_wait(bar, parity)) return true;
         const long long t0 = clock64();
         for (;;) {
 #pragma unroll 1
             for (int k = 0; k < 64; ++k)
-                if (CG == 1 ? mbar_try_wait(bar, parity) : mbar_try_wait_cluster(bar, parity)) return true;
+                if (mbar_try_wait(bar, parity)) return true;
             if (sh->dead) return false;
             if (clock64() - t0 > kWaitCycles) {
                 fail();
@@ -252,9 +278,12 @@ struct Pipe {
         }
     }
 
+    template <class Job>
     __device__ __forceinline__ void setup(unsigned char *raw, unsigned *err_word) {
+        static_assert(sizeof(typename Job::Tile) <= kTileBytes && alignof(typename Job::Tile) <= 16, "a tile in shared memory");
         stage0 = (smem_addr(raw) + 1023u) & ~1023u;
-        sh = reinterpret_cast<Shared *>(raw + (stage0 - smem_addr(raw)) + (size_t)kStages * kStageBytes);
+        extra = stage0 + kStages * kStageBytes;
+        sh = reinterpret_cast<Shared *>(raw + (extra - smem_addr(raw)) + EXTRA);
         err = err_word;
         rank = CG == 1 ? 0 : cluster_rank();
         if (threadIdx.x == 0) {
@@ -262,7 +291,10 @@ struct Pipe {
                 mbar_init(&sh->full[s], CG == 2 && rank == 0 ? 2 : 1);   // the peer's copies are passed on by an arrival
                 mbar_init(&sh->empty[s], 1);
             }
-            for (int k = 0; k < 2; ++k) mbar_init(&sh->acc_full[k], 1), mbar_init(&sh->acc_empty[k], 8 * CG);
+            for (int k = 0; k < 2; ++k) mbar_init(&sh->acc_full[k], 1), mbar_init(&sh->acc_empty[k], kEpiWarps * CG);
+            for (int k = 0; k < 3; ++k)
+                mbar_init(&sh->extra_full[k], 1), mbar_init(&sh->extra_done[k], kEpiWarps), mbar_init(&sh->extra_free[k], kEpiWarps);
+            for (int k = 0; k < kTiles; ++k) mbar_init(&sh->tile_full[k], 1), mbar_init(&sh->tile_empty[k], 2 + kEpiWarps + Job::kCopier);
             mbar_init(&sh->drain, 1);
             sh->dead = 0;
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -280,35 +312,69 @@ struct Pipe {
         int acc = 0;
         uint32_t ph = 0;
     };
-    // Runs the tiles that `job` lists.  Job:
-    //   Tile                       what one tile is; fields k_blocks (stages) and n (columns, a multiple of 64 * CG)
-    //   bool chunk_ends(tile, kb)  after this stage the epilogue takes the accumulator (always after the last)
-    //   bool next(Tile &, int i)   the i-th tile of this CTA (pair); false after the last
+    // One role's way through the tiles.
+    struct Walk {
+        int slot = 0;
+        uint32_t ph = 0;
+        __device__ __forceinline__ void step() {
+            if (++slot == kTiles) slot = 0, ph ^= 1;
+        }
+    };
+    template <class T>
+    __device__ __forceinline__ const T *tile_at(const Walk &w) const { return reinterpret_cast<const T *>(sh->tile[w.slot]); }
+    __device__ __forceinline__ void tile_done(Walk &w) {
+        mbar_arrive(&sh->tile_empty[w.slot]);
+        w.step();
+    }
+
+    // Runs the tiles that `job` lists.  What a role does per stage is kept to a few instructions: one thread issues
+    // a stage's copies and one its products, about 500 cycles' worth, and address arithmetic there is what it waits for
+    // (a kernel that worked out descriptors and majorness anew in every stage ran at 1.08 instead of 1.5 PFLOP/s).  Nor does
+    // a role look up what the next tile is: a chain of loads from the lists in memory at each tile's start left
+    // the tensor cores idle for about 2 us a tile.  Job:
+    //   Tile                       all that the roles need of a tile; n: columns, a multiple of 64 * CG, 0: no more tiles; segs, k_seg: its inner
+    //                              dimension is `segs` times k_seg stages; a_lim, b_lim: from which stage of each segment on that
+    //                              operand is MN-major
+    //   void tile(Tile &, int i, int rank)   the i-th tile of this CTA (pair); each lane asks for growing i only
+    //   bool chunk_ends(tile, seg, k)   after this stage the epilogue takes the accumulator (always after the last)
     //   bool ready(pipe, tile)     producer: what the tile reads is there
-    //   void load(tile, kb, a, b, bar)       copies into a and b (shared addresses); must bring bytes(tile) bytes
-    //   uint32_t bytes(tile)
-    //   bool a_mn(tile, kb), b_mn(tile, kb)  majorness of the stage's operands
+    //   Loader                     made from a tile; uint32_t bytes(); void seg(int); void load(k, a, b, bar): copies of bytes() bytes into
+    //                              a and b (shared addresses)
     //   int bf16()
-    //   bool epilogue(pipe, tile, turn, warp, lane)   warp 0..7: for each chunk take(), read its columns, release();
-    //                              false once take() is
+    //   bool epilogue(pipe, tile, turn, warp, lane)   warp 0..15: for each chunk take(), read its columns, release();
+    //                              false once a wait was.  Its warps do not wait for one another but on bounded barriers
+    //   kCopier; bool copier(pipe)  a thread of its own for what the epilogue brings and takes away through shared memory; walks the
+    //                              tiles itself
     template <class Job>
     __device__ __forceinline__ void run(Job &job) {
+        typedef typename Job::Tile Tile;
         const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+        Walk walk;
+        bool ok = true;
         if (warp == 0 && lane == 0) {
             int s = 0, issued = 0;
             uint32_t ph = 0;
-            typename Job::Tile t;
-            bool ok = true;
-            for (int i = 0; ok && job.next(t, i); ++i) {
+            while (ok) {
+                ok = wait(&sh->tile_full[walk.slot], walk.ph);
+                const Tile &t = *tile_at<Tile>(walk);
+                if (!ok || t.n == 0) break;
                 ok = job.ready(*this, t);
-                for (int kb = 0; ok && kb < t.k_blocks; ++kb) {
-                    ok = wait(&sh->empty[s], ph ^ 1);
-                    if (!ok) break;
-                    mbar_arrive_expect(&sh->full[s], job.bytes(t));
-                    const uint32_t at = stage0 + (uint32_t)s * kStageBytes;
-                    job.load(t, kb, at, at + kABytes, &sh->full[s]);
-                    ++issued;
-                    if (++s == kStages) s = 0, ph ^= 1;
+                if (!ok) break;
+                typename Job::Loader from(job, t);
+                const uint32_t bytes = from.bytes();
+                const int segs = t.segs, k_seg = t.k_seg;
+                tile_done(walk);
+                for (int g = 0; ok && g < segs; ++g) {
+                    from.seg(g);
+                    for (int k = 0; k < k_seg; ++k) {
+                        ok = wait(&sh->empty[s], ph ^ 1);
+                        if (!ok) break;
+                        mbar_arrive_expect(&sh->full[s], bytes);
+                        const uint32_t at = stage0 + (uint32_t)s * kStageBytes;
+                        from.load(k, at, at + kABytes, &sh->full[s]);
+                        ++issued;
+                        if (++s == kStages) s = 0, ph ^= 1;
+                    }
                 }
             }
             if (!ok) {                                  // copies in flight land before the CTA's memory is given up
@@ -325,33 +391,41 @@ struct Pipe {
         } else if (warp == 1 && lane == 0 && rank == 0) {
             int s = 0, acc = 0;
             uint32_t ph = 0, acc_ph = 0;
-            typename Job::Tile t;
-            bool ok = true;
-            for (int i = 0; ok && job.next(t, i); ++i) {
+            const uint32_t tmem = sh->tmem;
+            while (ok) {
+                ok = wait(&sh->tile_full[walk.slot], walk.ph);
+                if (!ok || tile_at<Tile>(walk)->n == 0) break;
+                const Tile t = *tile_at<Tile>(walk);
+                tile_done(walk);
+                const uint32_t id = instr_desc(job.bf16(), t.n, CG);
                 bool fresh = true;
-                for (int kb = 0; kb < t.k_blocks; ++kb) {
-                    if (fresh) {
-                        ok = wait(&sh->acc_empty[acc], acc_ph ^ 1);
+                uint32_t d = 0;
+                for (int g = 0; ok && g < t.segs; ++g) {
+                    for (int k = 0; k < t.k_seg; ++k) {
+                        if (fresh) {
+                            ok = wait(&sh->acc_empty[acc], acc_ph ^ 1);
+                            if (!ok) break;
+                            d = tmem + (uint32_t)acc * 256;
+                        }
+                        ok = wait(&sh->full[s], ph);
                         if (!ok) break;
-                    }
-                    const uint32_t d = sh->tmem + (uint32_t)acc * 256;
-                    ok = wait(&sh->full[s], ph);
-                    if (!ok) break;
-                    tmem_fence_after();
-                    const bool a_mn = job.a_mn(t, kb), b_mn = job.b_mn(t, kb);
-                    const uint32_t at = stage0 + (uint32_t)s * kStageBytes;
-                    const uint64_t da = operand_desc(at, a_mn), db = operand_desc(at + kABytes, b_mn);
-                    const uint32_t id = instr_desc(job.bf16(), a_mn, b_mn, t.n, CG);
-                    const uint32_t sa = a_mn ? 2048 / 16 : 32 / 16, sb = b_mn ? 2048 / 16 : 32 / 16;
+                        tmem_fence_after();
+                        const bool a_mn = k >= t.a_lim, b_mn = k >= t.b_lim;
+                        const uint32_t at = (stage0 + (uint32_t)s * kStageBytes) >> 4;
+                        const uint64_t da = (a_mn ? operand_desc(true) : operand_desc(false)) + at;
+                        const uint64_t db = (b_mn ? operand_desc(true) : operand_desc(false)) + at + (kABytes >> 4);
+                        const uint32_t sa = operand_step(a_mn), sb = operand_step(b_mn);
+                        const uint32_t di = id | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16);
 #pragma unroll
-                    for (int k = 0; k < kStageK / 16; ++k)
-                        mma_f16<CG>(d, da + (uint64_t)k * sa, db + (uint64_t)k * sb, id, !(fresh && k == 0));
-                    mma_commit<CG>(&sh->empty[s]);
-                    if (++s == kStages) s = 0, ph ^= 1;
-                    fresh = job.chunk_ends(t, kb);
-                    if (fresh) {
-                        mma_commit<CG>(&sh->acc_full[acc]);
-                        if (++acc == 2) acc = 0, acc_ph ^= 1;
+                        for (int e = 0; e < kStageK / 16; ++e)
+                            mma_f16<CG>(d, da + e * sa, db + e * sb, di, e == 0 ? !fresh : 1);
+                        mma_commit<CG>(&sh->empty[s]);
+                        if (++s == kStages) s = 0, ph ^= 1;
+                        fresh = job.chunk_ends(t, g, k);
+                        if (fresh) {
+                            mma_commit<CG>(&sh->acc_full[acc]);
+                            if (++acc == 2) acc = 0, acc_ph ^= 1;
+                        }
                     }
                 }
             }
@@ -364,43 +438,61 @@ struct Pipe {
             // The pair's second CTA passes "this stage has landed" on to the first one's barrier.
             int s = 0;
             uint32_t ph = 0;
-            typename Job::Tile t;
-            bool ok = true;
-            for (int i = 0; ok && job.next(t, i); ++i)
-                for (int kb = 0; ok && kb < t.k_blocks; ++kb) {
+            while (ok) {
+                ok = wait(&sh->tile_full[walk.slot], walk.ph);
+                const Tile &t = *tile_at<Tile>(walk);
+                if (!ok || t.n == 0) break;
+                int k = t.segs * t.k_seg;
+                tile_done(walk);
+                for (; ok && k > 0; --k) {
                     ok = wait(&sh->full[s], ph);
                     if (ok) mbar_arrive_remote(&sh->full[s], 0);
                     if (++s == kStages) s = 0, ph ^= 1;
                 }
+            }
+        } else if (warp == 2 && lane < kTiles) {
+            // Lane l works out every kTiles-th tile, before its place is free.
+            Tile t;
+            for (int i = lane; ok; i += kTiles) {
+                job.tile(t, i, (int)rank);
+                ok = wait(&sh->tile_empty[lane], (uint32_t)(i / kTiles & 1) ^ 1);
+                if (!ok) break;
+                *reinterpret_cast<Tile *>(sh->tile[lane]) = t;
+                mbar_arrive(&sh->tile_full[lane]);
+                if (t.n == 0) break;
+            }
+        } else if (Job::kCopier && warp == 3 && lane == 0) {
+            if constexpr (Job::kCopier) {
+                if (!job.copier(*this)) {
+                    bulk_out_done();                    // its copies, and time for those into shared memory
+                    const long long t0 = clock64();
+                    while (clock64() - t0 < 2000000ll) {}
+                }
+            }
         } else if (warp >= kEpiWarp0) {
             Turn turn;
-            typename Job::Tile t;
-            for (int i = 0; job.next(t, i); ++i)
-                if (!job.epilogue(*this, t, turn, warp - kEpiWarp0, lane)) break;
+            while (ok) {
+                ok = warp_wait(&sh->tile_full[walk.slot], walk.ph);
+                const Tile &t = *tile_at<Tile>(walk);
+                if (!ok || t.n == 0) break;
+                ok = job.epilogue(*this, t, turn, warp - kEpiWarp0, lane);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sh->tile_empty[walk.slot]);
+                walk.step();
+            }
         }
         __syncwarp();
     }
-    // Vote of the 256 epilogue threads.
-    __device__ __forceinline__ bool epi_all(bool ok) {
-        int all;
-        asm volatile(
-            "{\n\t.reg .pred p, q;\n\tsetp.ne.s32 p, %1, 0;\n\t"
-            "barrier.red.and.pred q, 1, 256, p;\n\tselp.s32 %0, 1, 0, q;\n\t}"
-            : "=r"(all)
-            : "r"((int)ok)
-            : "memory");
-        return all != 0;
-    }
-    __device__ __forceinline__ void epi_sync() { asm volatile("barrier.sync 1, 256;" ::: "memory"); }
-    // Waits for the next accumulator; `at` is its address for this warp's lanes.  All epilogue threads get the same
-    // answer, so that none waits at a barrier for one that left.
+    // wait() by all lanes of a warp, which go on or leave together.
+    __device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity) { return __all_sync(~0u, wait(bar, parity)); }
+    // Waits for the next accumulator; `at` is its address for this warp's lanes.
     __device__ __forceinline__ bool take(Turn &t, uint32_t &at) {
-        if (!epi_all(wait(&sh->acc_full[t.acc], t.ph))) return false;
+        if (!warp_wait(&sh->acc_full[t.acc], t.ph)) return false;
         tmem_fence_after();
         at = sh->tmem + (uint32_t)t.acc * 256 + ((uint32_t)(threadIdx.x / 32 % 4) << 21);
         return true;
     }
-    // Called by every epilogue warp once it has read its part of the accumulator.
+    // Called by every epilogue warp once it has read its part of the accumulator for the last time.
     __device__ __forceinline__ void release(Turn &t, int lane) {
         tmem_fence_before();
         __syncwarp();

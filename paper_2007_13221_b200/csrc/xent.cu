@@ -3,7 +3,7 @@
 //   z = h W^T,  lse = log sum exp z,  loss = lse - z[target];    dz = (exp(z - lse) - [target]) dloss,  dh = dz W,  dW = dz^T h
 //
 // The logits are never kept.  cser_xent_loss: one kernel of 128 x 256 tiles of z whose epilogue reduces its tile to a
-// maximum and a sum of exponentials per row and half tile, and one that joins them.  cser_xent_grad: for each piece of
+// maximum and a sum of exponentials per row and quarter tile, and one that joins them.  cser_xent_grad: for each piece of
 // the vocabulary a kernel computes the tiles of z again and leaves dz in 16 bits, as panels (tensor_tiles.cuh), and
 // one kernel makes from them the piece's rows of dW (inner dimension: tokens) and the piece's share of dh (inner dimension: the piece).
 // Every operand is read where it lies: the products that need dz, h or W the other way round take the same tiles with the other majorness.
@@ -45,7 +45,7 @@ struct XentArgs {
     CUtensorMap h, w;                              // (dim, row, worker), boxes of 64 x 64
     int n, tokens, vocab, dim;
     int h_workers, w_workers;                      // 1: one array for all workers
-    int bf16, type;
+    int bf16;
     int token_tiles, piece0, piece_n;              // vocabulary entries of this launch
     int tp;                                        // rows of a dz panel
     // loss
@@ -73,39 +73,40 @@ template <int CG, bool GRAD>
 struct LogitsJob {
     const XentArgs &a;
     int first, every, vocab_tiles;
+    static constexpr bool kCopier = false;
 
     struct Tile {
-        int w, i, j, n, k_blocks;
+        int w, i, j, n, segs, k_seg, a_lim, b_lim;
     };
-    __device__ __forceinline__ bool next(Tile &t, int k) const {
+    __device__ __forceinline__ void tile(Tile &t, int k, int) const {
         const int at = first + k * every, per = a.token_tiles * vocab_tiles;
-        t.w = at / per;
-        if (t.w >= a.n) return false;
+        t.w = at / per, t.n = 0;
+        if (t.w >= a.n) return;
         const int r = at - t.w * per;
         t.j = r / a.token_tiles, t.i = r - t.j * a.token_tiles;
-        t.n = 256;
-        t.k_blocks = (a.dim + 63) / 64;
-        return true;
+        t.n = 256, t.segs = 1, t.k_seg = (a.dim + 63) / 64, t.a_lim = t.b_lim = t.k_seg;
     }
     __device__ __forceinline__ bool ready(Pipe<CG> &, const Tile &) const { return true; }
-    __device__ __forceinline__ bool a_mn(const Tile &, int) const { return false; }
-    __device__ __forceinline__ bool b_mn(const Tile &, int) const { return false; }
-    __device__ __forceinline__ bool chunk_ends(const Tile &t, int kb) const { return kb + 1 == t.k_blocks; }
+    __device__ __forceinline__ bool chunk_ends(const Tile &t, int, int k) const { return k + 1 == t.k_seg; }
     __device__ __forceinline__ int bf16() const { return a.bf16; }
-    __device__ __forceinline__ uint32_t bytes(const Tile &) const { return Pipe<CG>::kStageBytes; }
-    __device__ __forceinline__ void load(const Tile &t, int kb, uint32_t sa, uint32_t sb, uint64_t *bar) const {
-        const int rank = CG == 1 ? 0 : (int)cluster_rank();
-        const int hw = a.h_workers == 1 ? 0 : t.w, ww = a.w_workers == 1 ? 0 : t.w;
+    struct Loader {
+        const CUtensorMap *h, *w;
+        int row_a, row_b, wa, wb;
+        __device__ __forceinline__ Loader(const LogitsJob &job, const Tile &t, int rank = CG == 1 ? 0 : (int)cluster_rank())
+            : h(&job.a.h), w(&job.a.w), row_a(t.i * 128 * CG + rank * 128), row_b(job.a.piece0 + t.j * 256 + rank * 128),
+              wa(job.a.h_workers == 1 ? 0 : t.w), wb(job.a.w_workers == 1 ? 0 : t.w) {}
+        __device__ __forceinline__ uint32_t bytes() const { return Pipe<CG>::kStageBytes; }
+        __device__ __forceinline__ void seg(int) {}
+        __device__ __forceinline__ void load(int k, uint32_t sa, uint32_t sb, uint64_t *bar) const {
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
-            tensor_copy_in(sa + k * 8192, &a.h, kb * 64, t.i * 128 * CG + rank * 128 + k * 64, hw, bar);
+            for (int p = 0; p < 2; ++p) tensor_copy_in(sa + p * 8192, h, k * 64, row_a + p * 64, wa, bar);
 #pragma unroll
-        for (int k = 0; k < 4 / CG; ++k)
-            tensor_copy_in(sb + k * 8192, &a.w, kb * 64, a.piece0 + t.j * 256 + rank * 128 + k * 64, ww, bar);
-    }
+            for (int p = 0; p < 4 / CG; ++p) tensor_copy_in(sb + p * 8192, w, k * 64, row_b + p * 64, wb, bar);
+        }
+    };
     __device__ __forceinline__ bool epilogue(Pipe<CG> &p, const Tile &t, typename Pipe<CG>::Turn &turn, int warp, int lane) const {
         const int row = t.i * 128 * CG + (int)p.rank * 128 + warp % 4 * 32 + lane;
-        const int c0 = warp / 4 * 128;
+        const int c0 = warp / 4 * 64;
         const bool live = row < a.tokens;
         const size_t at = (size_t)t.w * a.tokens + row;
         int target = -1;
@@ -118,11 +119,11 @@ struct LogitsJob {
             if (!p.take(turn, tmem)) return false;
             float m = kLowest, s = 0.f;
 #pragma unroll 1
-            for (int b = 0; b < 128; b += 32) {
+            for (int b = 0; b < 64; b += 32) {
                 const int col = t.j * 256 + c0 + b;
                 float v[32];
-                tmem_load32(tmem + c0 + b, v);
-                if (b == 96) p.release(turn, lane);
+                tmem_load(tmem + c0 + b, v);
+                if (b == 32) p.release(turn, lane);
                 if (col + 32 > a.vocab) {
 #pragma unroll
                     for (int k = 0; k < 32; ++k)
@@ -143,18 +144,18 @@ struct LogitsJob {
                         if (off == (unsigned)k) a.z_target[at] = v[k];
                 }
             }
-            if (live) a.part[at * a.parts + t.j * 2 + warp / 4] = make_float2(m, s);
+            if (live) a.part[at * a.parts + t.j * 4 + warp / 4] = make_float2(m, s);
         } else {
             float ratio = 0.f, lse = 0.f;
             if (live) ratio = a.ratio[at], lse = a.lse[at];
             if (!p.take(turn, tmem)) return false;
             char *dz = a.dz + (size_t)t.w * a.dz_worker;
 #pragma unroll 1
-            for (int b = 0; b < 128; b += 32) {
+            for (int b = 0; b < 64; b += 32) {
                 const int in = t.j * 256 + c0 + b, col = a.piece0 + in;
                 float v[32];
-                tmem_load32(tmem + c0 + b, v);
-                if (b == 96) p.release(turn, lane);
+                tmem_load(tmem + c0 + b, v);
+                if (b == 32) p.release(turn, lane);
 #pragma unroll
                 for (int k = 0; k < 32; ++k) v[k] = ratio * exp2_fast((v[k] - lse) * kLog2e);   // the difference first: it is exact where p is near 1
                 const unsigned off = (unsigned)(target - col);
@@ -189,7 +190,7 @@ __global__ void __launch_bounds__(kThreads, 1) xent_logits_kernel(const __grid_c
     extern __shared__ unsigned char raw[];
     if (threadIdx.x == 0) prefetch_tensor_map(&a.h), prefetch_tensor_map(&a.w);
     Pipe<CG> p;
-    p.setup(raw, a.err);
+    p.template setup<LogitsJob<CG, GRAD>>(raw, a.err);
     LogitsJob<CG, GRAD> job{a, (int)blockIdx.x / CG, (int)gridDim.x / CG, (a.piece_n + 255) / 256};
     p.run(job);
     p.teardown();
@@ -253,68 +254,79 @@ template <int CG>
 struct GradJob {
     const XentArgs &a;
     int first, every, n_dh, n_dw, dim_tiles, vocab_tiles;
+    static constexpr bool kCopier = false;
 
     struct Tile {
-        int w, i, j, n, k_blocks, k0, split, dw;
+        int w, i, j, n, segs, k_seg, a_lim, b_lim, k0, split, dw;
     };
-    __device__ __forceinline__ bool next(Tile &t, int k) const {
+    __device__ __forceinline__ void tile(Tile &t, int k, int) const {
         int at = first + k * every;
-        t.dw = at >= n_dh;
+        t.n = 0, t.dw = at >= n_dh;
         if (t.dw) at -= n_dh;
-        if (t.dw && at >= n_dw) return false;
+        if (t.dw && at >= n_dw) return;
         t.j = at % dim_tiles, at /= dim_tiles;
         const int width = (a.dim + 64 * CG - 1) / (64 * CG) * (64 * CG);
         t.n = width - t.j * 256 < 256 ? width - t.j * 256 : 256;
         if (t.dw) {
             t.i = at % vocab_tiles, t.w = at / vocab_tiles;
-            t.k0 = 0, t.k_blocks = (a.tokens + 63) / 64, t.split = 0;
+            t.k0 = 0, t.k_seg = (a.tokens + 63) / 64, t.split = 0, t.a_lim = 0;
         } else {
             t.split = at % a.splits, at /= a.splits;
             t.i = at % a.token_tiles, t.w = at / a.token_tiles;
             const int all = (a.piece_n + 63) / 64;
             t.k0 = (int)((long long)all * t.split / a.splits);
-            t.k_blocks = (int)((long long)all * (t.split + 1) / a.splits) - t.k0;
+            t.k_seg = (int)((long long)all * (t.split + 1) / a.splits) - t.k0, t.a_lim = t.k_seg;
         }
-        return true;
+        t.segs = 1, t.b_lim = 0;
     }
     __device__ __forceinline__ bool ready(Pipe<CG> &, const Tile &) const { return true; }
-    __device__ __forceinline__ bool a_mn(const Tile &t, int) const { return t.dw; }
-    __device__ __forceinline__ bool b_mn(const Tile &, int) const { return true; }
-    __device__ __forceinline__ bool chunk_ends(const Tile &t, int kb) const { return kb + 1 == t.k_blocks; }
+    __device__ __forceinline__ bool chunk_ends(const Tile &t, int, int k) const { return k + 1 == t.k_seg; }
     __device__ __forceinline__ int bf16() const { return a.bf16; }
-    __device__ __forceinline__ uint32_t bytes(const Tile &t) const { return 128 * 128 + (uint32_t)(t.n / CG) * 128; }
-    __device__ __forceinline__ void load(const Tile &t, int kb, uint32_t sa, uint32_t sb, uint64_t *bar) const {
-        const int rank = CG == 1 ? 0 : (int)cluster_rank();
-        const char *dz = a.dz + (size_t)t.w * a.dz_worker;
-        const int row = t.i * 128 * CG + rank * 128, col = t.j * 256 + rank * (t.n / CG), k = t.k0 + kb;
-        if (t.dw) {
-#pragma unroll
-            for (int p = 0; p < 2; ++p)
-                bulk_copy_in(sa + p * 8192, dz + (size_t)(row / 64 + p) * a.tp * 128 + (size_t)k * 8192, 8192, bar);
-        } else {
-            bulk_copy_in(sa, dz + (size_t)k * a.tp * 128 + (size_t)row * 128, 16384, bar);
+    struct Loader {
+        const CUtensorMap *b;
+        const char *dz;
+        size_t panel;
+        int dw, col, row0, worker, boxes;
+        __device__ __forceinline__ Loader(const GradJob &job, const Tile &t) {
+            const int rank = CG == 1 ? 0 : (int)cluster_rank();
+            const XentArgs &a = job.a;
+            const int row = t.i * 128 * CG + rank * 128;
+            dw = t.dw, panel = (size_t)a.tp * 128, b = dw ? &a.h : &a.w, boxes = t.n / CG / 64;
+            dz = a.dz + (size_t)t.w * a.dz_worker + (dw ? (size_t)(row / 64) * panel : (size_t)t.k0 * panel + (size_t)row * 128);
+            col = t.j * 256 + rank * (t.n / CG), row0 = dw ? 0 : a.piece0 + t.k0 * 64;
+            worker = (dw ? a.h_workers : a.w_workers) == 1 ? 0 : t.w;
         }
-        const int worker = (t.dw ? a.h_workers : a.w_workers) == 1 ? 0 : t.w;
-        for (int p = 0; p < t.n / CG / 64; ++p)
-            tensor_copy_in(sb + p * 8192, t.dw ? &a.h : &a.w, col + p * 64, t.dw ? k * 64 : a.piece0 + k * 64, worker, bar);
-    }
+        __device__ __forceinline__ uint32_t bytes() const { return 128 * 128 + (uint32_t)boxes * 8192; }
+        __device__ __forceinline__ void seg(int) {}
+        __device__ __forceinline__ void load(int k, uint32_t sa, uint32_t sb, uint64_t *bar) const {
+            if (dw) {
+                bulk_copy_in(sa, dz + (size_t)k * 8192, 8192, bar);
+                bulk_copy_in(sa + 8192, dz + panel + (size_t)k * 8192, 8192, bar);
+            } else {
+                bulk_copy_in(sa, dz + (size_t)k * panel, 16384, bar);
+            }
+#pragma unroll
+            for (int p = 0; p < 4 / CG; ++p)
+                if (p < boxes) tensor_copy_in(sb + p * 8192, b, col + p * 64, row0 + k * 64, worker, bar);
+        }
+    };
     __device__ __forceinline__ bool epilogue(Pipe<CG> &p, const Tile &t, typename Pipe<CG>::Turn &turn, int warp, int lane) const {
         uint32_t tmem;
         const int row = t.i * 128 * CG + (int)p.rank * 128 + warp % 4 * 32 + lane;
-        const int half = t.n / 2, c0 = warp / 4 * half;
+        const int quarter = t.n / 4, c0 = warp / 4 * quarter;
         const float f = a.unscale[t.w];
         if (!p.take(turn, tmem)) return false;
 #pragma unroll 1
-        for (int b = 0; b < half; b += 32) {
+        for (int b = 0; b < quarter; b += 16) {
             const int col = t.j * 256 + c0 + b;
-            float v[32];
-            tmem_load32(tmem + c0 + b, v);
-            if (b + 32 >= half) p.release(turn, lane);
+            float v[16];
+            tmem_load(tmem + c0 + b, v);
+            if (b + 16 >= quarter) p.release(turn, lane);
             if (t.dw) {
                 if (row < a.piece_n && col < a.dim) {
 #pragma unroll
-                    for (int k = 0; k < 32; ++k) v[k] *= f;
-                    store_row32(a.dw, t.w * a.dw_stride + (long long)(a.piece0 + row) * a.dim + col, a.dim - col, a.type, v);
+                    for (int k = 0; k < 16; ++k) v[k] *= f;
+                    store_row(a.dw, t.w * a.dw_stride + (long long)(a.piece0 + row) * a.dim + col, a.dim - col, a.bf16, v);
                 }
                 continue;
             }
@@ -322,7 +334,7 @@ struct GradJob {
                 a.acc + (((size_t)t.w * a.splits + t.split) * a.acc_rows + row) * a.acc_cols + col);
             if (!a.first_piece) {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
+                for (int k = 0; k < 4; ++k) {
                     const float4 q = acc[k];
                     v[4 * k] += q.x, v[4 * k + 1] += q.y, v[4 * k + 2] += q.z, v[4 * k + 3] += q.w;
                 }
@@ -330,12 +342,12 @@ struct GradJob {
             if (a.last_piece && a.splits == 1) {
                 if (row < a.tokens && col < a.dim) {
 #pragma unroll
-                    for (int k = 0; k < 32; ++k) v[k] *= f;
-                    store_row32(a.dh, ((long long)t.w * a.tokens + row) * a.dim + col, a.dim - col, a.type, v);
+                    for (int k = 0; k < 16; ++k) v[k] *= f;
+                    store_row(a.dh, ((long long)t.w * a.tokens + row) * a.dim + col, a.dim - col, a.bf16, v);
                 }
             } else {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) acc[k] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+                for (int k = 0; k < 4; ++k) acc[k] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
             }
         }
         return true;
@@ -347,7 +359,7 @@ __global__ void __launch_bounds__(kThreads, 1) xent_grad_kernel(const __grid_con
     extern __shared__ unsigned char raw[];
     if (threadIdx.x == 0) prefetch_tensor_map(&a.h), prefetch_tensor_map(&a.w);
     Pipe<CG> p;
-    p.setup(raw, a.err);
+    p.template setup<GradJob<CG>>(raw, a.err);
     const int width = (a.dim + 64 * CG - 1) / (64 * CG) * (64 * CG);
     GradJob<CG> job{a, (int)blockIdx.x / CG, (int)gridDim.x / CG, n_dh, n_dw, (width + 255) / 256,
                     (a.piece_n + 128 * CG - 1) / (128 * CG)};
@@ -427,6 +439,11 @@ int splits_of(const cser_xent *h, long long tokens) {
     return s < 1 ? 1 : (int)s;
 }
 
+// Tiles of 256 tokens by a pair of CTAs, or of 128 by one.  Up to 128 tokens half of a pair's tile would be padding: loss of
+// one token x 30522 x 1024 13.7 us by single CTAs, 20.5 by pairs.  Above, pairs bring half the bytes per product: 4096 x 131072 x
+// 4096 2.63 ms against 2.82 (loss), 9.7 against 12.1 (gradient).
+bool wide_tiles(long long tokens) { return tokens > 128; }
+
 bool tensor_map(const cser_xent *h, CUtensorMap &m, const void *p, long long rows, long long row_stride, long long worker_stride,
                 int workers, long long dim) {
     const cuuint64_t size[3] = {(cuuint64_t)dim, (cuuint64_t)rows, (cuuint64_t)workers};
@@ -490,7 +507,7 @@ int prepare_call(cser_xent *h, const cser_xent_inputs *in, const char *what, Xen
     if (int rc = operand(h, a.w, a.w_workers, in->weight, h->vocab, in->weight_row_stride, in->weight_worker_stride, h->pack_w, h->vocab,
                          "weight", st))
         return rc;
-    a.type = h->type, a.bf16 = h->type == CSER_TYPE_BF16;
+    a.bf16 = h->type == CSER_TYPE_BF16;
     a.tp = h->tp, a.part = h->part, a.parts = h->parts, a.z_target = h->z_target, a.target = in->target, a.ignore = in->ignore_index;
     a.ratio = h->ratio, a.unscale = h->unscale, a.dz = h->dz, a.dz_worker = (size_t)(h->piece / 64) * h->tp * 128;
     a.acc = h->acc, a.acc_rows = (int)up(a.tokens, 256), a.acc_cols = h->acc_cols, a.err = h->err_dev;
@@ -592,7 +609,7 @@ cser_xent_handle cser_xent_create(int32_t n_workers, int64_t max_tokens, int64_t
     if (e != cudaSuccess) return drop(e);
     h->encode = reinterpret_cast<encode_fn>(fn);
     const long long rows = (long long)n_workers * max_tokens;
-    h->tp = (int)up(max_tokens, 256), h->acc_cols = (int)up(dim, 128), h->parts = (int)(2 * (up(vocab, 256) / 256));
+    h->tp = (int)up(max_tokens, 256), h->acc_cols = (int)up(dim, 128), h->parts = (int)(4 * (up(vocab, 256) / 256));
     const long long fit = (long long)(kPieceBytes / ((size_t)h->n * h->tp * 2)) / 256 * 256;
     h->piece = piece ? up(piece, 256) : fit < 2048 ? 2048 : fit;
     if (h->piece > up(vocab, 256)) h->piece = up(vocab, 256);
@@ -628,7 +645,7 @@ int cser_xent_loss(cser_xent_handle h, const cser_xent_inputs *in, float *loss, 
     if ((uintptr_t)lse % 4 || (uintptr_t)loss % 4)
         return cser_internal_fail(CSER_ERR_INVALID, "cser_xent_loss: a pointer is not aligned to its element type");
     a.loss = loss, a.lse_out = lse;
-    return loss_launch<1>(h, a, st);
+    return wide_tiles(a.tokens) ? loss_launch<2>(h, a, st) : loss_launch<1>(h, a, st);
 }
 
 int cser_xent_grad(cser_xent_handle h, const cser_xent_inputs *in, const float *lse, const float *dloss, void *dhidden,
@@ -657,7 +674,7 @@ int cser_xent_grad(cser_xent_handle h, const cser_xent_inputs *in, const float *
     if ((uintptr_t)lse % 4 || (uintptr_t)dloss % 4)
         return cser_internal_fail(CSER_ERR_INVALID, "cser_xent_grad: a pointer is not aligned to its element type");
     a.lse = lse, a.dloss = dloss, a.dh = dhidden, a.dw = dweight, a.dw_stride = dweight_stride;
-    return grad_launch<1>(h, a, st);
+    return wide_tiles(a.tokens) ? grad_launch<2>(h, a, st) : grad_launch<1>(h, a, st);
 }
 
 void cser_xent_destroy(cser_xent_handle h) {
