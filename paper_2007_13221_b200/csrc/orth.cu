@@ -340,11 +340,7 @@ struct OrthJob {
         t.src_wide = (const char *)M.xf[from], t.da = M.da, t.db = M.db;
         t.offset = M.offset, t.stride = M.stride, t.rows = M.rows, t.cols = M.cols, t.scale = M.scale;
     }
-    __device__ __forceinline__ bool ready(P &p, const Tile &t) const {
-        if (t.need && !p.wait_counter(t.done, t.need)) return false;
-        fence_async_proxy();
-        return true;
-    }
+    __device__ __forceinline__ bool ready(P &p, const Tile &t) const { return !t.need || p.wait_counter(t.done, t.need); }
     __device__ __forceinline__ bool chunk_ends(const Tile &t, int seg, int k) const {
         if (!SPLIT) return k + 1 == t.k_seg;
         if (k + 1 == t.k_seg) return seg > 0;
@@ -463,13 +459,13 @@ struct OrthJob {
         }
     }
 
-    // The copying thread: loads panels in order as buffers come free and the earlier phases are done, tile after tile, takes
-    // each finished panel away, and tells the matrix's counter when a whole tile is in memory.  It never blocks on a later
-    // tile's loads (what they wait for may be this CTA's own tile) while there is a panel to take away.
+    // The copying thread: loads panels in order as buffers come free, tile after tile, takes each finished panel away, and
+    // tells the matrix's counter when a whole tile is in memory.  It never blocks on a later tile (what that waits for may be this
+    // CTA's own) while there is a panel to take away.
     __device__ __forceinline__ bool copier(P &p) {
         typename P::Walk ahead, behind;                              // tile of the next load, of the next panel to take away
         int b_in = 0, b_out = 0, used = 0;                           // panels of these, buffers in use
-        bool end = false, known = false, go = false, signal = false; // go: the tile `ahead` may be loaded; signal: one is due
+        bool end = false, known = false, signal = false;
         long long t0 = clock64();
         for (;;) {
             bool moved = false;
@@ -481,19 +477,13 @@ struct OrthJob {
                         end = true;
                         break;
                     }
+                    fence_async_proxy();                             // what the tile's phase reads, for the copy engine
                 }
                 const Tile &t = *p.template tile_at<Tile>(ahead);
-                if (!go && t.phase != kPhaseA) {
-                    unsigned v;
-                    asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(t.done) : "memory");
-                    if (v < t.need) break;
-                    fence_async_proxy();
-                }
-                go = true;
                 bulk_out_read<0>();
                 load_panel(p, t, b_in);
                 ++used, moved = true;
-                if (++b_in == t.n / 64) b_in = 0, known = go = false, ahead.step();
+                if (++b_in == t.n / 64) b_in = 0, known = false, ahead.step();
             }
             if (signal) {
                 const Tile &t = *p.template tile_at<Tile>(behind);
@@ -533,7 +523,7 @@ struct OrthJob {
     __device__ __forceinline__ bool epilogue(P &p, const Tile &t, typename P::Turn &turn, int warp, int lane) {
         const int tid = warp * 32 + lane, side = warp / 4, r = warp % 4 * 32 + lane, row = t.row0 + r, panels = t.n / 64;
         const bool last = t.last;
-        float d_row = 0.f;
+        const float d_row = t.phase == kPhaseB ? __ldcg(t.da + row) : t.phase == kPhaseX && !t.tall ? __ldcg(t.db + row) : 0.f;
         uint32_t tmem;
         float sum[2][16];                                            // of a 32-bit result's chunks
         if (SPLIT) {
@@ -557,12 +547,6 @@ struct OrthJob {
         for (int b = 0; b < (SPLIT ? 2 : panels); ++b) {
             const int panel = t.panel0 + b, col = panel * 64 + side * 16;
             if (!p.warp_wait(&p.sh->extra_full[ring.buf], ring.parity())) return false;
-            if (b == 0 && t.phase != kPhaseA) {
-                unsigned seen;                                       // reached already: the loads had to wait for it
-                asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(seen) : "l"(t.done) : "memory");
-                if (t.phase == kPhaseB) d_row = __ldcg(t.da + row);
-                else if (!t.tall) d_row = __ldcg(t.db + row);
-            }
             const uint32_t at = p.extra + ring.buf * kBufBytes;
             float v[16];
             if (SPLIT) {

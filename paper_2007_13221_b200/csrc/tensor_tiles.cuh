@@ -337,7 +337,7 @@ struct Pipe {
     //                              operand is MN-major
     //   void tile(Tile &, int i, int rank)   the i-th tile of this CTA (pair); each lane asks for growing i only
     //   bool chunk_ends(tile, seg, k)   after this stage the epilogue takes the accumulator (always after the last)
-    //   bool ready(pipe, tile)     producer: what the tile reads is there
+    //   bool ready(pipe, tile)     waits until what the tile reads is in memory (before any role hears of the tile)
     //   Loader                     made from a tile; uint32_t bytes(); void seg(int); void load(k, a, b, bar): copies of bytes() bytes into
     //                              a and b (shared addresses)
     //   int bf16()
@@ -358,8 +358,7 @@ struct Pipe {
                 ok = wait(&sh->tile_full[walk.slot], walk.ph);
                 const Tile &t = *tile_at<Tile>(walk);
                 if (!ok || t.n == 0) break;
-                ok = job.ready(*this, t);
-                if (!ok) break;
+                fence_async_proxy();                    // what ready() saw written, for the copy engine
                 typename Job::Loader from(job, t);
                 const uint32_t bytes = from.bytes();
                 const int segs = t.segs, k_seg = t.k_seg;
@@ -456,6 +455,7 @@ struct Pipe {
             for (int i = lane; ok; i += kTiles) {
                 job.tile(t, i, (int)rank);
                 ok = wait(&sh->tile_empty[lane], (uint32_t)(i / kTiles & 1) ^ 1);
+                if (ok && t.n) ok = job.ready(*this, t);
                 if (!ok) break;
                 *reinterpret_cast<Tile *>(sh->tile[lane]) = t;
                 mbar_arrive(&sh->tile_full[lane]);

@@ -49,7 +49,7 @@ struct XentArgs {
     int token_tiles, piece0, piece_n;              // vocabulary entries of this launch
     int tp;                                        // rows of a dz panel
     // loss
-    float2 *part;                                  // [n * tokens][parts] maximum and sum
+    float2 *part;                                  // [parts][n * tokens] maximum and sum
     int parts;
     float *z_target;                               // [n * tokens]
     const int64_t *target;
@@ -144,7 +144,7 @@ struct LogitsJob {
                         if (off == (unsigned)k) a.z_target[at] = v[k];
                 }
             }
-            if (live) a.part[at * a.parts + t.j * 4 + warp / 4] = make_float2(m, s);
+            if (live) a.part[(size_t)(t.j * 4 + warp / 4) * a.n * a.tokens + at] = make_float2(m, s);
         } else {
             float ratio = 0.f, lse = 0.f;
             if (live) ratio = a.ratio[at], lse = a.lse[at];
@@ -196,26 +196,32 @@ __global__ void __launch_bounds__(kThreads, 1) xent_logits_kernel(const __grid_c
     p.teardown();
 }
 
-// A warp joins the parts of one row.
-__global__ void __launch_bounds__(256) xent_join_kernel(const __grid_constant__ XentArgs a) {
-    const size_t at = (size_t)blockIdx.x * 8 + threadIdx.x / 32;
-    const int lane = threadIdx.x % 32;
-    if (at >= (size_t)a.n * a.tokens) return;
-    const float2 *p = a.part + at * a.parts;
+// The parts of 32 rows joined by 32 warps: a lane takes a row, a warp every 32nd part, four of them at a time.
+__global__ void __launch_bounds__(1024) xent_join_kernel(const __grid_constant__ XentArgs a) {
+    __shared__ float2 red[32][32];
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const size_t rows = (size_t)a.n * a.tokens, at = (size_t)blockIdx.x * 32 + lane;
     float m = kLowest, s = 0.f;
-    for (int k = lane; k < a.parts; k += 32) {
-        const float2 q = p[k];
-        const float top = fmaxf(m, q.x);
-        s = s * exp2_fast((m - top) * kLog2e) + q.y * exp2_fast((q.x - top) * kLog2e);
-        m = top;
-    }
-    for (int k = 16; k; k >>= 1) {
-        const float qm = __shfl_xor_sync(~0u, m, k), qs = __shfl_xor_sync(~0u, s, k);
-        const float top = fmaxf(m, qm);
-        s = s * exp2_fast((m - top) * kLog2e) + qs * exp2_fast((qm - top) * kLog2e);
-        m = top;
-    }
-    if (lane == 0) {
+    if (at < rows)
+        for (int k = warp; k < a.parts; k += 128) {
+            float2 q[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) q[e] = k + 32 * e < a.parts ? a.part[(k + 32 * e) * rows + at] : make_float2(kLowest, 0.f);
+            const float top = fmaxf(fmaxf(m, fmaxf(q[0].x, q[1].x)), fmaxf(q[2].x, q[3].x));
+            s *= exp2_fast((m - top) * kLog2e);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s += q[e].y * exp2_fast((q[e].x - top) * kLog2e);
+            m = top;
+        }
+    red[warp][lane] = make_float2(m, s);
+    __syncthreads();
+    if (warp == 0 && at < rows) {
+        for (int k = 1; k < 32; ++k) {
+            const float2 q = red[k][lane];
+            const float top = fmaxf(m, q.x);
+            s = s * exp2_fast((m - top) * kLog2e) + q.y * exp2_fast((q.x - top) * kLog2e);
+            m = top;
+        }
         const float lse = m + logf(s);
         const int64_t y = a.target[at];
         a.lse_out[at] = lse;
@@ -544,7 +550,7 @@ template <int CG>
 int loss_launch(cser_xent *h, XentArgs &a, cudaStream_t st) {
     a.token_tiles = (int)(up(a.tokens, 128 * CG) / (128 * CG)), a.piece0 = 0, a.piece_n = a.vocab;
     TRY((tiles_launch<CG>(h, xent_logits_kernel<CG, false>, (long long)a.n * a.token_tiles * ((a.vocab + 255) / 256), st, a)));
-    xent_join_kernel<<<(unsigned)(((long long)a.n * a.tokens + 7) / 8), 256, 0, st>>>(a);
+    xent_join_kernel<<<(unsigned)(((long long)a.n * a.tokens + 31) / 32), 1024, 0, st>>>(a);
     TRY(cudaGetLastError());
     h->launches++;
     return CSER_OK;
