@@ -124,6 +124,8 @@ __device__ __forceinline__ void load8(const T *p, int n, float (&v)[8]) {
     }
 }
 
+#include "orth_small.cuh"
+
 // ------------------------------------------------------------------ |u|_F, momentum
 // HBM-bound: g read once (m read and written once).  The last CTA of a matrix adds the partial sums in their order.
 template <typename T>
@@ -691,6 +693,12 @@ struct cser_orth {
     int device = 0, in_type = 0, out_type = 0;
     bool split = false;
     std::vector<Group> groups;
+    struct Small {                                 // matrices with a short side of at most kSmallSide
+        SmallArgs args{};
+        int n_part = 0, n_piece = 0, n_resident = 0, side = 0;
+        size_t gram_shared = 0, apply_shared = 0, resident_shared = 0;
+        void *tables = nullptr;
+    } small, resident;                             // resident: those of them that fit a CTA's shared memory
     void *work = nullptr;                          // shared by the groups, which run one after the other
     unsigned *err_host = nullptr;
     long long launches = 0;
@@ -854,6 +862,85 @@ int build_group(cser_orth *h, cser_orth::Group &G, const std::vector<HostMat> &m
     return CSER_OK;
 }
 
+int build_small(cser_orth *h, const std::vector<HostMat> &ms, int steps) {
+    std::vector<SmallMat> mats(ms.size());
+    std::vector<uint2> part, piece;
+    size_t work = 0;
+    int most = 0;
+    for (size_t q = 0; q < ms.size(); ++q) {
+        SmallMat &M = mats[q];
+        M.tall = ms[q].rows > ms[q].cols;
+        M.s = (int)(M.tall ? ms[q].cols : ms[q].rows), M.l = (int)(M.tall ? ms[q].rows : ms[q].cols), M.sp = (int)up(M.s, 8);
+        M.offset = ms[q].offset, M.stride = ms[q].stride, M.scale = ms[q].scale;
+        // Parts of at least one piece of u in shared memory and 16 at most: the last CTA adds them up alone.
+        const long long cols = kGramDoubles / gram_ld(M.sp) / 4 * 4, fit = up(M.l, cols) / cols;
+        M.parts = fit < 16 ? (int)fit : 16;
+        M.per = (int)(up(up(M.l, M.parts) / M.parts, cols));
+        M.parts = (int)(up(M.l, M.per) / M.per);
+        const int side = M.sp / 8;
+        M.partial = work, work += (size_t)M.parts * side * (side + 1) / 2 * 64;
+        M.q = work, work += (size_t)M.sp * M.sp;
+        for (int k = 0; k < M.parts; ++k) part.push_back(make_uint2((unsigned)q, (unsigned)k));
+        for (int j = 0; j < M.l; j += kApplyCols) piece.push_back(make_uint2((unsigned)q, (unsigned)j));
+        if (M.sp > most) most = M.sp;
+    }
+    size_t bytes = 0;
+    auto place = [&](size_t b) { const size_t p = bytes; bytes += (b + 255) / 256 * 256; return p; };
+    const size_t o_mat = place(mats.size() * sizeof(SmallMat)), o_part = place(part.size() * sizeof(uint2)),
+                 o_piece = place(piece.size() * sizeof(uint2)), o_tick = place(mats.size() * 4), o_work = place(work * 8);
+    cser_orth::Small &S = h->small;
+    TRY(cudaMalloc(&S.tables, bytes));
+    char *t = static_cast<char *>(S.tables);
+    TRY(cudaMemset(t + o_tick, 0, mats.size() * 4));
+    TRY(cudaMemcpy(t + o_mat, mats.data(), mats.size() * sizeof(SmallMat), cudaMemcpyHostToDevice));
+    TRY(cudaMemcpy(t + o_part, part.data(), part.size() * sizeof(uint2), cudaMemcpyHostToDevice));
+    TRY(cudaMemcpy(t + o_piece, piece.data(), piece.size() * sizeof(uint2), cudaMemcpyHostToDevice));
+    S.args.mats = reinterpret_cast<SmallMat *>(t + o_mat), S.args.part = reinterpret_cast<uint2 *>(t + o_part);
+    S.args.piece = reinterpret_cast<uint2 *>(t + o_piece), S.args.ticket = reinterpret_cast<unsigned *>(t + o_tick);
+    S.args.work = reinterpret_cast<double *>(t + o_work), S.args.out_type = h->out_type, S.args.steps = steps;
+    S.n_part = (int)part.size(), S.n_piece = (int)piece.size();
+    const size_t four = (size_t)most * square_ld(most) * 4;
+    S.gram_shared = (four > kGramDoubles ? four : kGramDoubles) * 8;
+    S.apply_shared = ((size_t)most * square_ld(most) + (size_t)most * kApplyLd) * 8;
+    return CSER_OK;
+}
+int build_resident(cser_orth *h, const std::vector<HostMat> &ms, int steps) {
+    std::vector<SmallMat> mats(ms.size());
+    cser_orth::Small &S = h->resident;
+    for (size_t q = 0; q < ms.size(); ++q) {
+        SmallMat &M = mats[q];
+        M.tall = ms[q].rows > ms[q].cols;
+        M.s = (int)(M.tall ? ms[q].cols : ms[q].rows), M.l = (int)(M.tall ? ms[q].rows : ms[q].cols), M.sp = (int)up(M.s, 8);
+        M.offset = ms[q].offset, M.stride = ms[q].stride, M.scale = ms[q].scale;
+        const size_t b = resident_bytes(M.sp, M.l);
+        if (b > S.resident_shared) S.resident_shared = b;
+        if (M.sp > S.side) S.side = M.sp;
+    }
+    TRY(cudaMalloc(&S.tables, mats.size() * sizeof(SmallMat)));
+    TRY(cudaMemcpy(S.tables, mats.data(), mats.size() * sizeof(SmallMat), cudaMemcpyHostToDevice));
+    S.args.mats = static_cast<SmallMat *>(S.tables), S.args.out_type = h->out_type, S.args.steps = steps;
+    S.n_resident = (int)mats.size();
+    return CSER_OK;
+}
+template <typename T>
+cudaError_t small_setup(const cser_orth::Small &S) {
+    cudaError_t e = cudaFuncSetAttribute(orth_gram_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S.gram_shared);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(orth_apply_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S.apply_shared);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(orth_resident_kernel<T, 4>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S.resident_shared);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(orth_resident_kernel<T, 8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S.resident_shared);
+    return e;
+}
+template <typename T>
+void small_launch(const cser_orth::Small &S, const SmallArgs &a, cudaStream_t st) {
+    if (S.n_resident) {
+        if (S.side <= 32) orth_resident_kernel<T, 4><<<S.n_resident, 256, S.resident_shared, st>>>(a);
+        else orth_resident_kernel<T, 8><<<S.n_resident, 256, S.resident_shared, st>>>(a);
+    } else {
+        orth_gram_kernel<T><<<S.n_part, 256, S.gram_shared, st>>>(a);
+        orth_apply_kernel<T><<<S.n_piece, 256, S.apply_shared, st>>>(a);
+    }
+}
+
 template <typename T>
 void prologue_launch(const cser_orth::Group &G, const OrthArgs &a, cudaStream_t st) {
     orth_norm_kernel<T><<<G.n_chunk, 256, 0, st>>>(a);
@@ -873,7 +960,7 @@ cser_orth_handle cser_orth_create(int32_t n_workers, int64_t ld, int32_t n_matri
     if (steps < 1 || steps > 16) return bad("steps must be in 1..16");
     if (in_type < 0 || in_type > 2 || out_type < 0 || out_type > 2) return bad("unknown element type");
     if ((long long)n_workers * n_matrices > (1 << 20)) return bad("more than 2^20 matrices");
-    std::vector<HostMat> all;
+    std::vector<HostMat> all, small;
     cser_orth *h = nullptr;
     try {
         std::vector<std::pair<long long, long long>> span;
@@ -887,7 +974,7 @@ cser_orth_handle cser_orth_create(int32_t n_workers, int64_t ld, int32_t n_matri
         }
         for (int w = 0; w < n_workers; ++w)
             for (int k = 0; k < n_matrices; ++k)
-                all.push_back({(long long)w * ld + offset[k], rows[k], cols[k], row_stride ? row_stride[k] : cols[k],
+                (rows[k] <= kSmallSide || cols[k] <= kSmallSide ? small : all).push_back({(long long)w * ld + offset[k], rows[k], cols[k], row_stride ? row_stride[k] : cols[k],
                                scale ? scale[k] : 1.f, w});
         h = new cser_orth;
         h->in_type = in_type, h->out_type = out_type, h->split = out_type == CSER_TYPE_F32;
@@ -915,7 +1002,26 @@ cser_orth_handle cser_orth_create(int32_t n_workers, int64_t ld, int32_t n_matri
             now += need;
             if (now > most) most = now;
         }
-        er = cudaMalloc(&h->work, most);
+        if (most) er = cudaMalloc(&h->work, most);
+        std::vector<HostMat> fit, rest;
+        for (const HostMat &m : small) {
+            const long long side = m.rows < m.cols ? m.rows : m.cols, longer = m.rows < m.cols ? m.cols : m.rows;
+            (resident_bytes((int)up(side, 8), longer) <= kResidentMost ? fit : rest).push_back(m);
+        }
+        if (er == cudaSuccess && !small.empty()) {
+            if ((!rest.empty() && build_small(h, rest, steps) != CSER_OK) || (!fit.empty() && build_resident(h, fit, steps) != CSER_OK)) {
+                cser_orth_destroy(h);
+                return nullptr;
+            }
+            // shared memory is a property of the kernel, not of the plan: what any plan can need
+            cser_orth::Small any;
+            any.gram_shared = (size_t)kSmallSide * square_ld(kSmallSide) * 4 * 8;
+            any.apply_shared = (size_t)kSmallSide * (square_ld(kSmallSide) + kApplyLd) * 8;
+            any.resident_shared = kResidentMost;
+            er = small_setup<float>(any);
+            if (er == cudaSuccess) er = small_setup<__nv_bfloat16>(any);
+            if (er == cudaSuccess) er = small_setup<__half>(any);
+        }
         if (er == cudaSuccess) er = cudaHostAlloc(reinterpret_cast<void **>(&h->err_host), 64, cudaHostAllocMapped | cudaHostAllocPortable);
         unsigned *err_dev = nullptr;
         if (er == cudaSuccess) *h->err_host = 0, er = cudaHostGetDevicePointer(reinterpret_cast<void **>(&err_dev), h->err_host, 0);
@@ -960,6 +1066,16 @@ int cser_orth_apply(cser_orth_handle h, const void *grad, float *m, float mu, vo
     if (m && (static_cast<const void *>(m) == grad || static_cast<const void *>(m) == out))
         return cser_internal_fail(CSER_ERR_INVALID, "cser_orth_apply: m must be an array of its own");
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    for (const cser_orth::Small *S : {&h->resident, &h->small}) {
+        if (!S->tables) continue;
+        SmallArgs a = S->args;
+        a.grad = grad, a.m = m, a.mu = mu, a.out = out;
+        if (h->in_type == CSER_TYPE_F32) small_launch<float>(*S, a, st);
+        else if (h->in_type == CSER_TYPE_BF16) small_launch<__nv_bfloat16>(*S, a, st);
+        else small_launch<__half>(*S, a, st);
+        TRY(cudaGetLastError());
+        h->launches += S->n_resident ? 1 : 2;
+    }
     for (cser_orth::Group &G : h->groups) {
         OrthArgs a = G.args;
         a.grad = grad, a.m = m, a.mu = mu, a.out = out;
@@ -979,6 +1095,8 @@ void cser_orth_destroy(cser_orth_handle h) {
     if (!h) return;
     for (cser_orth::Group &G : h->groups)
         if (G.tables) cudaFree(G.tables);
+    if (h->small.tables) cudaFree(h->small.tables);
+    if (h->resident.tables) cudaFree(h->resident.tables);
     if (h->work) cudaFree(h->work);
     if (h->err_host) cudaFreeHost(h->err_host);
     delete h;
