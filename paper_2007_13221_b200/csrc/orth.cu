@@ -1006,7 +1006,10 @@ cser_orth_handle cser_orth_create(int32_t n_workers, int64_t ld, int32_t n_matri
         std::vector<HostMat> fit, rest;
         for (const HostMat &m : small) {
             const long long side = m.rows < m.cols ? m.rows : m.cols, longer = m.rows < m.cols ? m.cols : m.rows;
-            (resident_bytes((int)up(side, 8), longer) <= kResidentMost ? fit : rest).push_back(m);
+            // One CTA for a whole matrix pays where there are matrices for most SMs, or little to do: 33 x 1000 took 100 us alone,
+            // against 54 by two kernels that spread it; 384 of 16 x 1024 took 48 against 120.
+            const bool pays = (int)small.size() >= pairs[2] || side * side * longer <= 1 << 19;
+            (pays && resident_bytes((int)up(side, 8), longer) <= kResidentMost ? fit : rest).push_back(m);
         }
         if (er == cudaSuccess && !small.empty()) {
             if ((!rest.empty() && build_small(h, rest, steps) != CSER_OK) || (!fit.empty() && build_resident(h, fit, steps) != CSER_OK)) {

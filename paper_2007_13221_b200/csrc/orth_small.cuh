@@ -51,9 +51,9 @@ __host__ __device__ constexpr int gram_ld(int sp) { return sp % 16 ? sp : sp + 8
 // 8 x 8 += (8 x 4) (4 x 8).  a: row lane / 4, column lane % 4; b: row lane % 4, column lane / 4; c: row lane / 4,
 // columns lane % 4 * 2 and the next.
 __device__ __forceinline__ void mma_f64(double (&c)[2], double a, double b) {
-    asm volatile("mma.sync.aligned.m8n8k4.row.col.f64.f64.f64.f64 {%0, %1}, {%2}, {%3}, {%0, %1};"
-                 : "+d"(c[0]), "+d"(c[1])
-                 : "d"(a), "d"(b));
+    asm("mma.sync.aligned.m8n8k4.row.col.f64.f64.f64.f64 {%0, %1}, {%2}, {%3}, {%0, %1};"
+        : "+d"(c[0]), "+d"(c[1])
+        : "d"(a), "d"(b));
 }
 
 __device__ __forceinline__ float small_u(const SmallArgs &a, float g, long long at, bool update) {
@@ -76,31 +76,57 @@ __device__ __forceinline__ void triangle(int k, int &i, int &j) {
     while (i * (i + 1) / 2 > k) --i;
     j = k - i * (i + 1) / 2;
 }
-// out = x y for symmetric commuting x and y (rows of square_ld(sp)): 8 x 8 tiles of one triangle, mirrored.  out is neither.
-__device__ __forceinline__ void sym_product(double *out, const double *x, const double *y, int sp) {
-    const int side = sp / 8, tiles = side * (side + 1) / 2, ld = square_ld(sp), lane = threadIdx.x % 32;
-    for (int k = threadIdx.x / 32; k < tiles; k += 8) {
-        int ti, tj;
-        triangle(k, ti, tj);
-        const double *u = x + (ti * 8 + lane / 4) * ld + lane % 4, *v = y + (tj * 8 + lane / 4) * ld + lane % 4;
-        double c[2][2] = {};                                         // two chains
-#pragma unroll 4
-        for (int e = 0; e < sp; e += 8) {
-            mma_f64(c[0], u[e], v[e]);
-            mma_f64(c[1], u[e + 4], v[e + 4]);
-        }
+// A warp's 8 x 8 tiles of one triangle of an s x s matrix: every eighth one, at most N.
+template <int N>
+struct WarpTiles {
+    int i[N], j[N], n = 0;                                           // this lane's row of either operand's fragment
+    __device__ __forceinline__ explicit WarpTiles(int sp) {
+        const int side = sp / 8, tiles = side * (side + 1) / 2, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            const int i = ti * 8 + lane / 4, j = tj * 8 + lane % 4 * 2 + q;
-            if (j <= i) out[i * ld + j] = out[j * ld + i] = c[0][q] + c[1][q];
+        for (int b = 0; b < N; ++b) {
+            i[b] = j[b] = 0;
+            if (warp + 8 * b < tiles) {
+                triangle(warp + 8 * b, i[b], j[b]);
+                ++n;
+            }
+            i[b] = i[b] * 8 + lane / 4, j[b] = j[b] * 8 + lane / 4;
         }
     }
+};
+// out = x y (POLY: kA I + kB x + kC x y) for symmetric commuting x and y (rows of square_ld(sp)): one triangle, mirrored.
+// out is neither.  A product waits about 190 cycles for the one before it on the same accumulator: a warp's tiles go side by
+// side, each as two chains.
+template <int N, bool POLY>
+__device__ __forceinline__ void sym_product(double *out, const double *x, const double *y, int sp, const WarpTiles<N> &w) {
+    const int ld = square_ld(sp), k = threadIdx.x % 4;
+    double c[N][2][2] = {};
+#pragma unroll 2
+    for (int e = 0; e < sp; e += 8)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int b = 0; b < N; ++b)
+                if (b < w.n) mma_f64(c[b][h], x[w.i[b] * ld + k + e + 4 * h], y[w.j[b] * ld + k + e + 4 * h]);
+#pragma unroll
+    for (int b = 0; b < N; ++b)
+        if (b < w.n)
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const int i = w.i[b], j = w.j[b] / 8 * 8 + k * 2 + q;
+                double s = c[b][0][q] + c[b][1][q];
+                if (j <= i) {
+                    if (POLY) s = __fma_rn((double)kC, s, __fma_rn((double)kB, x[i * ld + j], i == j ? (double)kA : 0.0));
+                    out[i * ld + j] = out[j * ld + i] = s;
+                }
+            }
     __syncthreads();
 }
 
 // From the Gram matrix in A: Q with out = Q u; returns where it is (one of the four).
+template <int N>
 __device__ __forceinline__ double *small_steps(double *A, double *P, double *Q, double *W, int sp, int steps) {
     __shared__ double inv;
+    const WarpTiles<N> tiles(sp);
     const int sq = square_ld(sp), lane = threadIdx.x % 32;
     if (threadIdx.x < 32) {
         double tr = 0.0;
@@ -115,16 +141,13 @@ __device__ __forceinline__ double *small_steps(double *A, double *P, double *Q, 
     }
     __syncthreads();
     for (int step = 0; step < steps; ++step) {
-        sym_product(P, A, A, sp);
-        for (int e = threadIdx.x; e < sp * sq; e += 256)
-            P[e] = __fma_rn((double)kC, P[e], __fma_rn((double)kB, A[e], e % (sq + 1) == 0 ? (double)kA : 0.0));
-        __syncthreads();
-        sym_product(W, P, Q, sp);
+        sym_product<N, true>(P, A, A, sp, tiles);
+        sym_product<N, false>(W, P, Q, sp, tiles);
         double *t = Q;
         Q = W, W = t;
         if (step + 1 < steps) {
-            sym_product(W, P, A, sp);
-            sym_product(A, W, P, sp);
+            sym_product<N, false>(W, P, A, sp, tiles);
+            sym_product<N, false>(A, W, P, sp, tiles);
         }
     }
     return Q;
@@ -167,6 +190,7 @@ __global__ void __launch_bounds__(256) orth_gram_kernel(const SmallArgs a) {
         }
         __syncthreads();
         if (group < groups)
+#pragma unroll 2
             for (int c = group * 4; c < filled; c += groups * 4) {
                 const double *row = sh + (c + lane % 4) * ld;
 #pragma unroll
@@ -215,7 +239,7 @@ __global__ void __launch_bounds__(256) orth_gram_kernel(const SmallArgs a) {
         if (j <= i) A[i * sq + j] = A[j * sq + i] = s;
     }
     __syncthreads();
-    Q = small_steps(A, P, Q, W, sp, a.steps);
+    Q = sp <= 32 ? small_steps<2>(A, P, Q, W, sp, a.steps) : small_steps<5>(A, P, Q, W, sp, a.steps);
     double *q = a.work + M.q;
     for (int e = threadIdx.x; e < sp * sp; e += 256) q[e] = Q[e / sp * sq + e % sp] * (double)M.scale;
 }
@@ -286,7 +310,7 @@ __host__ __device__ constexpr int resident_ld(int sp) { return sp % 32 == 16 ? s
 __host__ __device__ constexpr size_t resident_bytes(int sp, long long l) {
     return (size_t)sp * square_ld(sp) * 32 + (size_t)((l + 15) / 16 * 16) * resident_ld(sp) * 4;
 }
-constexpr size_t kResidentMost = 200 * 1024;
+constexpr size_t kResidentMost = 224 * 1024;
 
 // MOST: eighths of the short side at most.
 template <typename T, int MOST>
@@ -301,7 +325,7 @@ __global__ void __launch_bounds__(256, MOST == 4 ? 3 : 2) orth_resident_kernel(c
     // Eight values at a time, along memory: of a row of a wide matrix (lanes take different rows, which keeps the
     // stores to shared memory apart), or of the short side of a tall one.
     const int chunks = M.tall ? cols * eighths : sp * (cols / 8);
-#pragma unroll 2
+#pragma unroll 4
     for (int e = threadIdx.x; e < chunks; e += 256) {
         int i, c, n;
         if (M.tall) c = e / eighths, i = (e - c * eighths) * 8, n = c < M.l ? M.s - i : 0;
@@ -333,18 +357,18 @@ __global__ void __launch_bounds__(256, MOST == 4 ? 3 : 2) orth_resident_kernel(c
     for (int b = tile0; b < tiles && group < groups; b += 8) {
         int ti, tj;
         triangle(b, ti, tj);
-        double acc[2][2] = {};
+        double acc[4][2] = {};
         const float *row = u + (group * 4 + lane % 4) * ld + lane / 4;
+        const int step = groups * 4 * ld;
         int c = group * 4;
-        for (; c + groups * 4 < cols; c += groups * 8, row += groups * 8 * ld) {
-            const float *next = row + groups * 4 * ld;
-            mma_f64(acc[0], (double)row[ti * 8], (double)row[tj * 8]);
-            mma_f64(acc[1], (double)next[ti * 8], (double)next[tj * 8]);
-        }
-        if (c < cols) mma_f64(acc[0], (double)row[ti * 8], (double)row[tj * 8]);
+        for (; c + groups * 12 < cols; c += groups * 16, row += 4 * step)
+#pragma unroll
+            for (int h = 0; h < 4; ++h) mma_f64(acc[h], (double)row[h * step + ti * 8], (double)row[h * step + tj * 8]);
+        for (; c < cols; c += groups * 4, row += step) mma_f64(acc[0], (double)row[ti * 8], (double)row[tj * 8]);
         // over P, Q and W: the groups' sums one after the other
         double *o = P + (group * tiles + b) * 64 + lane * 2;
-        o[0] = acc[0][0] + acc[1][0], o[1] = acc[0][1] + acc[1][1];
+#pragma unroll
+        for (int q = 0; q < 2; ++q) o[q] = (acc[0][q] + acc[1][q]) + (acc[2][q] + acc[3][q]);
     }
     __syncthreads();
     for (int e = threadIdx.x; e < tiles * 64; e += 256) {
@@ -357,10 +381,11 @@ __global__ void __launch_bounds__(256, MOST == 4 ? 3 : 2) orth_resident_kernel(c
         if (j <= i) A[i * sq + j] = A[j * sq + i] = s;
     }
     __syncthreads();
-    Q = small_steps(A, P, Q, W, sp, a.steps);
+    Q = small_steps<MOST == 4 ? 2 : 5>(A, P, Q, W, sp, a.steps);
     // out = scale Q u: a warp takes 16 columns and puts the results where they were.
     for (int c = warp * 16; c < cols; c += 128) {
         double acc[MOST][2][2] = {};
+#pragma unroll 2
         for (int k = 0; k < sp; k += 4) {
             const float *row = u + (c + lane / 4) * ld + k + lane % 4;
             const double b0 = (double)row[0], b1 = (double)row[8 * ld];

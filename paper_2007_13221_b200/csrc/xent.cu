@@ -256,8 +256,14 @@ __global__ void __launch_bounds__(1024) xent_ratio_kernel(const __grid_constant_
 }
 
 // ------------------------------------------------------------------ dh and dW of a piece
+// Results leave through 4 KB of shared memory per epilogue warp, 32 rows of up to 64 columns, so that a store instruction
+// covers whole lines of four rows (or one row, where rows are not 16 bytes apart) and not 16 bytes of 32 rows.
+template <int CG>
+using GradPipe = Pipe<CG, 256, kEpiWarps * 4096>;
+
 template <int CG>
 struct GradJob {
+    using P = GradPipe<CG>;
     const XentArgs &a;
     int first, every, n_dh, n_dw, dim_tiles, vocab_tiles;
     static constexpr bool kCopier = false;
@@ -285,7 +291,7 @@ struct GradJob {
         }
         t.segs = 1, t.b_lim = 0;
     }
-    __device__ __forceinline__ bool ready(Pipe<CG> &, const Tile &) const { return true; }
+    __device__ __forceinline__ bool ready(P &, const Tile &) const { return true; }
     __device__ __forceinline__ bool chunk_ends(const Tile &t, int, int k) const { return k + 1 == t.k_seg; }
     __device__ __forceinline__ int bf16() const { return a.bf16; }
     struct Loader {
@@ -316,46 +322,65 @@ struct GradJob {
                 if (p < boxes) tensor_copy_in(sb + p * 8192, b, col + p * 64, row0 + k * 64, worker, bar);
         }
     };
-    __device__ __forceinline__ bool epilogue(Pipe<CG> &p, const Tile &t, typename Pipe<CG>::Turn &turn, int warp, int lane) const {
+    __device__ __forceinline__ bool epilogue(P &p, const Tile &t, typename P::Turn &turn, int warp, int lane) const {
         uint32_t tmem;
-        const int row = t.i * 128 * CG + (int)p.rank * 128 + warp % 4 * 32 + lane;
-        const int quarter = t.n / 4, c0 = warp / 4 * quarter;
+        const int row0 = t.i * 128 * CG + (int)p.rank * 128 + warp % 4 * 32, row = row0 + lane;
+        const int quarter = t.n / 4, c0 = warp / 4 * quarter, col0 = t.j * 256 + c0;
+        const bool leaves = t.dw || (a.last_piece && a.splits == 1);
+        const uint32_t at = p.extra + (uint32_t)warp * 4096;
         const float f = a.unscale[t.w];
         if (!p.take(turn, tmem)) return false;
 #pragma unroll 1
         for (int b = 0; b < quarter; b += 16) {
-            const int col = t.j * 256 + c0 + b;
             float v[16];
             tmem_load(tmem + c0 + b, v);
             if (b + 16 >= quarter) p.release(turn, lane);
-            if (t.dw) {
-                if (row < a.piece_n && col < a.dim) {
+            if (!t.dw && (!a.first_piece || !leaves)) {
+                float4 *acc = reinterpret_cast<float4 *>(
+                    a.acc + (((size_t)t.w * a.splits + t.split) * a.acc_rows + row) * a.acc_cols + col0 + b);
+                if (!a.first_piece) {
 #pragma unroll
-                    for (int k = 0; k < 16; ++k) v[k] *= f;
-                    store_row(a.dw, t.w * a.dw_stride + (long long)(a.piece0 + row) * a.dim + col, a.dim - col, a.bf16, v);
+                    for (int k = 0; k < 4; ++k) {
+                        const float4 q = acc[k];
+                        v[4 * k] += q.x, v[4 * k + 1] += q.y, v[4 * k + 2] += q.z, v[4 * k + 3] += q.w;
+                    }
                 }
-                continue;
+                if (!leaves) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) acc[k] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+                    continue;
+                }
             }
-            float4 *acc = reinterpret_cast<float4 *>(
-                a.acc + (((size_t)t.w * a.splits + t.split) * a.acc_rows + row) * a.acc_cols + col);
-            if (!a.first_piece) {
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const float4 q = acc[k];
-                    v[4 * k] += q.x, v[4 * k + 1] += q.y, v[4 * k + 2] += q.z, v[4 * k + 3] += q.w;
-                }
-            }
-            if (a.last_piece && a.splits == 1) {
-                if (row < a.tokens && col < a.dim) {
+            for (int k = 0; k < 16; ++k) v[k] *= f;
 #pragma unroll
-                    for (int k = 0; k < 16; ++k) v[k] *= f;
-                    store_row(a.dh, ((long long)t.w * a.tokens + row) * a.dim + col, a.dim - col, a.bf16, v);
-                }
-            } else {
-#pragma unroll
-                for (int k = 0; k < 4; ++k) acc[k] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+            for (int k = 0; k < 2; ++k) {
+                const float *e = v + 8 * k;
+                shared_store16(at + panel_chunk(lane, b / 8 + k),
+                               a.bf16 ? make_uint4(pack_bf162(e[0], e[1]), pack_bf162(e[2], e[3]), pack_bf162(e[4], e[5]), pack_bf162(e[6], e[7]))
+                                      : make_uint4(pack_half2(e[0], e[1]), pack_half2(e[2], e[3]), pack_half2(e[4], e[5]), pack_half2(e[6], e[7])));
             }
         }
+        if (!leaves) return true;
+        __syncwarp();
+        const int rows = (t.dw ? a.piece_n : a.tokens) - row0, cols = a.dim - col0 < quarter ? a.dim - col0 : quarter;
+        uint16_t *o = t.dw ? static_cast<uint16_t *>(a.dw) + t.w * a.dw_stride + (long long)(a.piece0 + row0) * a.dim + col0
+                           : static_cast<uint16_t *>(a.dh) + ((long long)t.w * a.tokens + row0) * a.dim + col0;
+        if (cols > 0 && (a.dim & 7) == 0 && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
+            const int chunks = cols / 8;                             // whole ones: dim and quarter are multiples of 8
+            for (int e = lane; e < 32 * chunks; e += 32) {
+                const int r = e / chunks, c = e - r * chunks;
+                if (r < rows) *reinterpret_cast<uint4 *>(o + (long long)r * a.dim + c * 8) = shared_load16(at + panel_chunk(r, c));
+            }
+        } else {
+            for (int r = 0; r < 32 && r < rows; ++r)
+                for (int c = lane; c < cols; c += 32) {
+                    uint16_t v;
+                    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(at + panel_chunk(r, c / 8) + c % 8 * 2) : "memory");
+                    o[(long long)r * a.dim + c] = v;
+                }
+        }
+        __syncwarp();
         return true;
     }
 };
@@ -364,7 +389,7 @@ template <int CG>
 __global__ void __launch_bounds__(kThreads, 1) xent_grad_kernel(const __grid_constant__ XentArgs a, int n_dh, int n_dw) {
     extern __shared__ unsigned char raw[];
     if (threadIdx.x == 0) prefetch_tensor_map(&a.h), prefetch_tensor_map(&a.w);
-    Pipe<CG> p;
+    GradPipe<CG> p;
     p.template setup<GradJob<CG>>(raw, a.err);
     const int width = (a.dim + 64 * CG - 1) / (64 * CG) * (64 * CG);
     GradJob<CG> job{a, (int)blockIdx.x / CG, (int)gridDim.x / CG, n_dh, n_dw, (width + 255) / 256,
@@ -521,12 +546,12 @@ int prepare_call(cser_xent *h, const cser_xent_inputs *in, const char *what, Xen
 }
 
 template <int CG, typename K, typename... Args>
-cudaError_t tiles_launch(cser_xent *h, K kernel, long long tiles, cudaStream_t st, Args... args) {
+cudaError_t tiles_launch(cser_xent *h, K kernel, size_t shared, long long tiles, cudaStream_t st, Args... args) {
     const long long most = h->sms / CG;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)((tiles < most ? tiles : most) * CG));
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = Pipe<CG>::kSharedBytes;
+    cfg.dynamicSmemBytes = shared;
     cfg.stream = st;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
@@ -542,14 +567,14 @@ cudaError_t kernels_setup() {
     const int b = (int)Pipe<CG>::kSharedBytes;
     cudaError_t e = cudaFuncSetAttribute(xent_logits_kernel<CG, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, b);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(xent_logits_kernel<CG, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, b);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(xent_grad_kernel<CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, b);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(xent_grad_kernel<CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)GradPipe<CG>::kSharedBytes);
     return e;
 }
 
 template <int CG>
 int loss_launch(cser_xent *h, XentArgs &a, cudaStream_t st) {
     a.token_tiles = (int)(up(a.tokens, 128 * CG) / (128 * CG)), a.piece0 = 0, a.piece_n = a.vocab;
-    TRY((tiles_launch<CG>(h, xent_logits_kernel<CG, false>, (long long)a.n * a.token_tiles * ((a.vocab + 255) / 256), st, a)));
+    TRY((tiles_launch<CG>(h, xent_logits_kernel<CG, false>, Pipe<CG>::kSharedBytes, (long long)a.n * a.token_tiles * ((a.vocab + 255) / 256), st, a)));
     xent_join_kernel<<<(unsigned)(((long long)a.n * a.tokens + 31) / 32), 1024, 0, st>>>(a);
     TRY(cudaGetLastError());
     h->launches++;
@@ -568,9 +593,9 @@ int grad_launch(cser_xent *h, XentArgs &a, cudaStream_t st) {
         a.piece0 = (int)v, a.piece_n = (int)(h->vocab - v < h->piece ? h->vocab - v : h->piece);
         a.first_piece = v == 0, a.last_piece = v + h->piece >= h->vocab;
         const long long vt = up(a.piece_n, 128 * CG) / (128 * CG);
-        TRY((tiles_launch<CG>(h, xent_logits_kernel<CG, true>, (long long)a.n * a.token_tiles * ((a.piece_n + 255) / 256), st, a)));
+        TRY((tiles_launch<CG>(h, xent_logits_kernel<CG, true>, Pipe<CG>::kSharedBytes, (long long)a.n * a.token_tiles * ((a.piece_n + 255) / 256), st, a)));
         const long long n_dh = a.dh ? (long long)a.n * a.token_tiles * a.splits * dim_tiles : 0, n_dw = a.dw ? a.n * vt * dim_tiles : 0;
-        TRY((tiles_launch<CG>(h, xent_grad_kernel<CG>, n_dh + n_dw, st, a, (int)n_dh, (int)n_dw)));
+        TRY((tiles_launch<CG>(h, xent_grad_kernel<CG>, GradPipe<CG>::kSharedBytes, n_dh + n_dw, st, a, (int)n_dh, (int)n_dw)));
     }
     if (a.dh && a.splits > 1) {
         const long long e = (long long)a.n * a.tokens * ((a.dim + 3) / 4);
