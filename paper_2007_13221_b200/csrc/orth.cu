@@ -49,9 +49,8 @@ constexpr int kNormChunk = 8192;                   // elements per CTA of the no
 // Columns of a tile, for CTAs in pairs (cg = 2) or single ones; a 32-bit result's sums must fit the epilogue's registers.
 constexpr int tile_n(int cg, bool split) { return cg == 2 && !split ? 256 : 128; }
 // The tensor cores truncate every partial sum, about 2^-24 of it for 16 terms: 2e-5 over an inner dimension of 4096.  So a
-// 32-bit result's accumulator is taken out and added up in registers, rounded, after this many stages of the leading
-// product (the two small ones share one accumulator).  X's product is the one whose error the steps after it do not
-// shrink: with a low-rank matrix 9e-6 at 4 stages.
+// 32-bit result's accumulator of hi hi is taken out and added up in registers, rounded, after this many stages.  X's
+// product is the one whose error the steps after it do not shrink: with a low-rank matrix 9e-6 at 4 stages.
 constexpr int kChunkAB = 4, kChunkX = 1;
 constexpr size_t kGroupBytes = 2ull << 30;         // workspace of one group of matrices
 constexpr size_t kBatchBytes = 96ull << 20;        // of it, what is worked on together
@@ -281,7 +280,7 @@ __global__ void __launch_bounds__(256) orth_convert_kernel(const OrthArgs a) {
 enum { kPhaseA = 0, kPhaseB = 1, kPhaseX = 2 };
 
 template <int CG, bool SPLIT>
-using OrthPipe = Pipe<CG, tile_n(CG, SPLIT), SPLIT ? 65536 : 98304>;
+using OrthPipe = Pipe<CG, tile_n(CG, SPLIT), SPLIT ? 65536 : 98304, SPLIT>;
 
 template <int CG, bool SPLIT>
 struct OrthJob {
@@ -293,7 +292,7 @@ struct OrthJob {
     static constexpr bool kCopier = true;
 
     struct Tile {
-        int n, segs, k_seg, a_lim, b_lim;
+        int n, stages, a_lim, b_lim;
         int phase, tall, last, row0, panel0, rp;                     // row0: of this CTA; rp: rows of a panel of what is written
         int row_a, row_b;                                            // first rows of the operands
         unsigned need, *done;
@@ -322,12 +321,12 @@ struct OrthJob {
         const OrthMat &M = a.mats[e.q];
         const int width = phase == kPhaseX ? M.cp : M.sp, from = step & 1, to = from ^ 1;
         t.n = width - e.j * TN < TN ? width - e.j * TN : TN;
-        t.segs = SPLIT ? 3 : 1, t.k_seg = phase == kPhaseA ? M.k_long : M.k_short;
+        t.stages = phase == kPhaseA ? M.k_long : M.k_short;
         // Of a symmetric matrix the stages of the panels up to the row's own 256 are stored, the others as their mirror image.
         const int tri_a = (e.i * 128 * CG / 256 + 1) * 4, tri_b = (e.j * TN / 256 + 1) * 4;
         const bool sym_a = phase == kPhaseB || (phase == kPhaseX && !M.tall), sym_b = phase == kPhaseB || (phase == kPhaseX && M.tall);
-        t.a_lim = phase == kPhaseA ? (M.tall ? 0 : t.k_seg) : sym_a ? tri_a : t.k_seg;
-        t.b_lim = phase == kPhaseA ? (M.tall ? 0 : t.k_seg) : sym_b ? tri_b : 0;
+        t.a_lim = phase == kPhaseA ? (M.tall ? 0 : t.stages) : sym_a ? tri_a : t.stages;
+        t.b_lim = phase == kPhaseA ? (M.tall ? 0 : t.stages) : sym_b ? tri_b : 0;
         t.phase = phase, t.tall = M.tall, t.last = phase == kPhaseX && step == a.steps - 1;
         t.row0 = t.row_a = e.i * 128 * CG + rank * 128, t.row_b = e.j * TN + rank * (t.n / CG), t.panel0 = e.j * (TN / 64);
         t.need = (unsigned)step * (2 * M.tiles_sym + M.tiles_x) + (unsigned)phase * M.tiles_sym, t.done = a.done + e.q;
@@ -343,10 +342,8 @@ struct OrthJob {
         t.offset = M.offset, t.stride = M.stride, t.rows = M.rows, t.cols = M.cols, t.scale = M.scale;
     }
     __device__ __forceinline__ bool ready(P &p, const Tile &t) const { return !t.need || p.wait_counter(t.done, t.need); }
-    __device__ __forceinline__ bool chunk_ends(const Tile &t, int seg, int k) const {
-        if (!SPLIT) return k + 1 == t.k_seg;
-        if (k + 1 == t.k_seg) return seg > 0;
-        return seg == 2 && ((k + 1) & ((t.phase == kPhaseX ? kChunkX : kChunkAB) - 1)) == 0;
+    __device__ __forceinline__ bool chunk_ends(const Tile &t, int k) const {
+        return k + 1 == t.stages || (SPLIT && ((k + 1) & ((t.phase == kPhaseX ? kChunkX : kChunkAB) - 1)) == 0);
     }
     __device__ __forceinline__ int bf16() const { return 0; }
     // `count` rows from `row` on of a matrix of `rp` rows, stage by stage: its panel k, or, from stage `lim` on, as the columns of
@@ -354,40 +351,33 @@ struct OrthJob {
     struct Operand {
         const char *k_major, *mn_major;
         size_t panel;
+        long long lo;                                                // from hi to lo
         int lim;
-        __device__ __forceinline__ void at(const char *base, int row, size_t panel_bytes) {
-            panel = panel_bytes;
-            k_major = base + (size_t)row * 128;
-            mn_major = base + (size_t)(row / 64) * panel;
-        }
+        __device__ __forceinline__ Operand(const char *hi, const char *low, int row, size_t panel_bytes, int limit)
+            : k_major(hi + (size_t)row * 128), mn_major(hi + (size_t)(row / 64) * panel_bytes), panel(panel_bytes), lo(low - hi), lim(limit) {}
         template <int COUNT>
         __device__ __forceinline__ void load(int k, int count, uint32_t dst, uint64_t *bar) const {
             if (k < lim) {
-                bulk_copy_in(dst, k_major + (size_t)k * panel, (uint32_t)count * 128, bar);
+                const char *p = k_major + (size_t)k * panel;
+                bulk_copy_in(dst, p, (uint32_t)count * 128, bar);
+                if (SPLIT) bulk_copy_in(dst + P::kLoOffset, p + lo, (uint32_t)count * 128, bar);
             } else {
                 const char *p = mn_major + (size_t)k * 8192;
 #pragma unroll
                 for (int e = 0; e < COUNT / 64; ++e)
-                    if (e * 64 < count) bulk_copy_in(dst + e * 8192, p + (size_t)e * panel, 8192, bar);
+                    if (e * 64 < count) {
+                        bulk_copy_in(dst + e * 8192, p + (size_t)e * panel, 8192, bar);
+                        if (SPLIT) bulk_copy_in(dst + P::kLoOffset + e * 8192, p + (size_t)e * panel + lo, 8192, bar);
+                    }
             }
         }
     };
     struct Loader {
-        const char *a_hi, *a_lo, *b_hi, *b_lo;
-        size_t a_panel, b_panel;
-        int row_a, row_b, nb;
+        int nb;
         Operand x, y;
         __device__ __forceinline__ Loader(const OrthJob &, const Tile &t)
-            : a_hi(t.a_hi), a_lo(t.a_lo), b_hi(t.b_hi), b_lo(t.b_lo), a_panel(t.a_panel), b_panel(t.b_panel), row_a(t.row_a),
-              row_b(t.row_b), nb(t.n / CG) {
-            x.lim = t.a_lim, y.lim = t.b_lim;
-        }
-        __device__ __forceinline__ uint32_t bytes() const { return 128 * 128 + (uint32_t)nb * 128; }
-        // Small products first: hi lo, lo hi, hi hi.
-        __device__ __forceinline__ void seg(int g) {
-            x.at(SPLIT && g == 1 ? a_lo : a_hi, row_a, a_panel);
-            y.at(SPLIT && g == 0 ? b_lo : b_hi, row_b, b_panel);
-        }
+            : nb(t.n / CG), x(t.a_hi, t.a_lo, t.row_a, t.a_panel, t.a_lim), y(t.b_hi, t.b_lo, t.row_b, t.b_panel, t.b_lim) {}
+        __device__ __forceinline__ uint32_t bytes() const { return (128 * 128 + (uint32_t)nb * 128) * (SPLIT ? 2 : 1); }
         __device__ __forceinline__ void load(int k, uint32_t sa, uint32_t sb, uint64_t *bar) const {
             x.template load<128>(k, 128, sa, bar);
             y.template load<TN / CG>(k, nb, sb, bar);
@@ -529,18 +519,18 @@ struct OrthJob {
         uint32_t tmem;
         float sum[2][16];                                            // of a 32-bit result's chunks
         if (SPLIT) {
-            const int each = t.phase == kPhaseX ? kChunkX : kChunkAB, chunks = 1 + (t.k_seg + each - 1) / each;
-            for (int c = 0, done = 0; c < chunks; ++c) {
-                if (!p.take(turn, tmem)) return false;
+            const int each = t.phase == kPhaseX ? kChunkX : kChunkAB, chunks = (t.stages + each - 1) / each;
+            for (int c = 0; c <= chunks; ++c) {                      // hi hi, then the small products
+                if (c < chunks ? !p.take(turn, tmem) : !p.take_small(turn, tmem)) return false;
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
                     float v[16];
                     tmem_load(tmem + b * 64 + side * 16, v);
 #pragma unroll
-                    for (int k = 0; k < 16; ++k) sum[b][k] = __fadd_rn(done ? sum[b][k] : 0.f, v[k]);
+                    for (int k = 0; k < 16; ++k) sum[b][k] = __fadd_rn(c ? sum[b][k] : 0.f, v[k]);
                 }
-                p.release(turn, lane);
-                done = 1;
+                if (c < chunks) p.release(turn, lane);
+                else p.release_small(turn, lane);
             }
         } else if (!p.take(turn, tmem)) {
             return false;

@@ -216,18 +216,24 @@ __device__ __forceinline__ void store_row(void *base, long long at, int n, bool 
 }
 
 // ------------------------------------------------------------------ the pipeline
-// TN: columns of a tile (at most 256).  EXTRA: bytes of shared memory for the epilogue, a multiple of 1024.
-template <int CG, int TN = 256, int EXTRA = 0>
+// TN: columns of a tile (at most 256).  EXTRA: bytes of shared memory for the epilogue, a multiple of 1024.  PAIR: operands are
+// pairs hi + lo of 16-bit values: a stage holds all four and makes hi hi in one accumulator and hi lo + lo hi, 2^-11 of it, in
+// another (three products as three passes over the inner dimension brought half as many bytes again, and the copies were the
+// bound); TN is at most 128 then.
+template <int CG, int TN = 256, int EXTRA = 0, bool PAIR = false>
 struct Pipe {
     static constexpr int kABytes = 128 * 128;                       // this CTA's 128 rows of the first operand
     static constexpr int kBBytes = TN / CG * 128;                   // this CTA's share of the second
-    static constexpr int kStageBytes = kABytes + kBBytes;
+    static constexpr int kLoOffset = kABytes + kBBytes;             // of the lo halves in a stage
+    static constexpr int kStageBytes = (kABytes + kBBytes) * (PAIR ? 2 : 1);
+    static constexpr int kAccCols = PAIR ? 128 : 256;               // of an accumulator; two, and two more for the small products
+    static_assert(TN <= kAccCols, "an accumulator's columns");
     static constexpr int kStages = (225 * 1024 - EXTRA) / kStageBytes;
 
     static constexpr int kTiles = 4, kTileBytes = 256;               // tiles known ahead
 
     struct Shared {
-        uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2], drain;
+        uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2], small_full[2], small_empty[2], drain;
         uint64_t extra_full[3], extra_done[3], extra_free[3];         // the epilogue's buffers, see orth.cu
         uint64_t tile_full[kTiles], tile_empty[kTiles];
         uint32_t tmem;
@@ -291,7 +297,10 @@ struct Pipe {
                 mbar_init(&sh->full[s], CG == 2 && rank == 0 ? 2 : 1);   // the peer's copies are passed on by an arrival
                 mbar_init(&sh->empty[s], 1);
             }
-            for (int k = 0; k < 2; ++k) mbar_init(&sh->acc_full[k], 1), mbar_init(&sh->acc_empty[k], kEpiWarps * CG);
+            for (int k = 0; k < 2; ++k) {
+                mbar_init(&sh->acc_full[k], 1), mbar_init(&sh->acc_empty[k], kEpiWarps * CG);
+                mbar_init(&sh->small_full[k], 1), mbar_init(&sh->small_empty[k], kEpiWarps * CG);
+            }
             for (int k = 0; k < 3; ++k)
                 mbar_init(&sh->extra_full[k], 1), mbar_init(&sh->extra_done[k], kEpiWarps), mbar_init(&sh->extra_free[k], kEpiWarps);
             for (int k = 0; k < kTiles; ++k) mbar_init(&sh->tile_full[k], 1), mbar_init(&sh->tile_empty[k], 2 + kEpiWarps + Job::kCopier);
@@ -311,6 +320,8 @@ struct Pipe {
     struct Turn {
         int acc = 0;
         uint32_t ph = 0;
+        int small = 0;                                              // of the small products', one a tile
+        uint32_t small_ph = 0;
     };
     // One role's way through the tiles.
     struct Walk {
@@ -332,14 +343,13 @@ struct Pipe {
     // (a kernel that worked out descriptors and majorness anew in every stage ran at 1.08 instead of 1.5 PFLOP/s).  Nor does
     // a role look up what the next tile is: a chain of loads from the lists in memory at each tile's start left
     // the tensor cores idle for about 2 us a tile.  Job:
-    //   Tile                       all that the roles need of a tile; n: columns, a multiple of 64 * CG, 0: no more tiles; segs, k_seg: its inner
-    //                              dimension is `segs` times k_seg stages; a_lim, b_lim: from which stage of each segment on that
-    //                              operand is MN-major
+    //   Tile                       all that the roles need of a tile; n: columns, a multiple of 64 * CG, 0: no more tiles; stages: its inner
+    //                              dimension; a_lim, b_lim: from which stage on that operand is MN-major
     //   void tile(Tile &, int i, int rank)   the i-th tile of this CTA (pair); each lane asks for growing i only
-    //   bool chunk_ends(tile, seg, k)   after this stage the epilogue takes the accumulator (always after the last)
+    //   bool chunk_ends(tile, k)   after this stage the epilogue takes the accumulator (always after the last)
     //   bool ready(pipe, tile)     waits until what the tile reads is in memory (before any role hears of the tile)
-    //   Loader                     made from a tile; uint32_t bytes(); void seg(int); void load(k, a, b, bar): copies of bytes() bytes into
-    //                              a and b (shared addresses)
+    //   Loader                     made from a tile; uint32_t bytes(); void load(k, a, b, bar): copies of bytes() bytes into a and b (shared
+    //                              addresses; the lo halves of pairs kLoOffset behind)
     //   int bf16()
     //   bool epilogue(pipe, tile, turn, warp, lane)   warp 0..15: for each chunk take(), read its columns, release();
     //                              false once a wait was.  Its warps do not wait for one another but on bounded barriers
@@ -361,19 +371,16 @@ struct Pipe {
                 fence_async_proxy();                    // what ready() saw written, for the copy engine
                 typename Job::Loader from(job, t);
                 const uint32_t bytes = from.bytes();
-                const int segs = t.segs, k_seg = t.k_seg;
+                const int stages = t.stages;
                 tile_done(walk);
-                for (int g = 0; ok && g < segs; ++g) {
-                    from.seg(g);
-                    for (int k = 0; k < k_seg; ++k) {
-                        ok = wait(&sh->empty[s], ph ^ 1);
-                        if (!ok) break;
-                        mbar_arrive_expect(&sh->full[s], bytes);
-                        const uint32_t at = stage0 + (uint32_t)s * kStageBytes;
-                        from.load(k, at, at + kABytes, &sh->full[s]);
-                        ++issued;
-                        if (++s == kStages) s = 0, ph ^= 1;
-                    }
+                for (int k = 0; k < stages; ++k) {
+                    ok = wait(&sh->empty[s], ph ^ 1);
+                    if (!ok) break;
+                    mbar_arrive_expect(&sh->full[s], bytes);
+                    const uint32_t at = stage0 + (uint32_t)s * kStageBytes;
+                    from.load(k, at, at + kABytes, &sh->full[s]);
+                    ++issued;
+                    if (++s == kStages) s = 0, ph ^= 1;
                 }
             }
             if (!ok) {                                  // copies in flight land before the CTA's memory is given up
@@ -388,8 +395,9 @@ struct Pipe {
                     while (clock64() - t0 < 2000000ll) {}
             }
         } else if (warp == 1 && lane == 0 && rank == 0) {
-            int s = 0, acc = 0;
-            uint32_t ph = 0, acc_ph = 0;
+            int s = 0;
+            uint32_t ph = 0;
+            Turn turn;
             const uint32_t tmem = sh->tmem;
             while (ok) {
                 ok = wait(&sh->tile_full[walk.slot], walk.ph);
@@ -399,33 +407,45 @@ struct Pipe {
                 const uint32_t id = instr_desc(job.bf16(), t.n, CG);
                 bool fresh = true;
                 uint32_t d = 0;
-                for (int g = 0; ok && g < t.segs; ++g) {
-                    for (int k = 0; k < t.k_seg; ++k) {
-                        if (fresh) {
-                            ok = wait(&sh->acc_empty[acc], acc_ph ^ 1);
-                            if (!ok) break;
-                            d = tmem + (uint32_t)acc * 256;
-                        }
-                        ok = wait(&sh->full[s], ph);
+                const uint32_t d_small = tmem + 2 * kAccCols + (uint32_t)turn.small * kAccCols;
+                if (PAIR) ok = wait(&sh->small_empty[turn.small], turn.small_ph ^ 1);
+                for (int k = 0; ok && k < t.stages; ++k) {
+                    if (fresh) {
+                        ok = wait(&sh->acc_empty[turn.acc], turn.ph ^ 1);
                         if (!ok) break;
-                        tmem_fence_after();
-                        const bool a_mn = k >= t.a_lim, b_mn = k >= t.b_lim;
-                        const uint32_t at = (stage0 + (uint32_t)s * kStageBytes) >> 4;
-                        const uint64_t da = (a_mn ? operand_desc(true) : operand_desc(false)) + at;
-                        const uint64_t db = (b_mn ? operand_desc(true) : operand_desc(false)) + at + (kABytes >> 4);
-                        const uint32_t sa = operand_step(a_mn), sb = operand_step(b_mn);
-                        const uint32_t di = id | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16);
+                        d = tmem + (uint32_t)turn.acc * kAccCols;
+                    }
+                    ok = wait(&sh->full[s], ph);
+                    if (!ok) break;
+                    tmem_fence_after();
+                    const bool a_mn = k >= t.a_lim, b_mn = k >= t.b_lim;
+                    const uint32_t at = (stage0 + (uint32_t)s * kStageBytes) >> 4;
+                    const uint64_t da = (a_mn ? operand_desc(true) : operand_desc(false)) + at;
+                    const uint64_t db = (b_mn ? operand_desc(true) : operand_desc(false)) + at + (kABytes >> 4);
+                    const uint32_t sa = operand_step(a_mn), sb = operand_step(b_mn);
+                    const uint32_t di = id | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16);
 #pragma unroll
-                        for (int e = 0; e < kStageK / 16; ++e)
-                            mma_f16<CG>(d, da + e * sa, db + e * sb, di, e == 0 ? !fresh : 1);
-                        mma_commit<CG>(&sh->empty[s]);
-                        if (++s == kStages) s = 0, ph ^= 1;
-                        fresh = job.chunk_ends(t, g, k);
-                        if (fresh) {
-                            mma_commit<CG>(&sh->acc_full[acc]);
-                            if (++acc == 2) acc = 0, acc_ph ^= 1;
+                    for (int e = 0; e < kStageK / 16; ++e)
+                        mma_f16<CG>(d, da + e * sa, db + e * sb, di, e == 0 ? !fresh : 1);
+                    if (PAIR) {
+                        constexpr uint32_t lo = kLoOffset >> 4;
+#pragma unroll
+                        for (int e = 0; e < kStageK / 16; ++e) {
+                            mma_f16<CG>(d_small, da + e * sa, db + lo + e * sb, di, e == 0 ? k != 0 : 1);
+                            mma_f16<CG>(d_small, da + lo + e * sa, db + e * sb, di, 1);
                         }
                     }
+                    mma_commit<CG>(&sh->empty[s]);
+                    if (++s == kStages) s = 0, ph ^= 1;
+                    fresh = job.chunk_ends(t, k);
+                    if (fresh) {
+                        mma_commit<CG>(&sh->acc_full[turn.acc]);
+                        if (++turn.acc == 2) turn.acc = 0, turn.ph ^= 1;
+                    }
+                }
+                if (PAIR && ok) {
+                    mma_commit<CG>(&sh->small_full[turn.small]);
+                    if (++turn.small == 2) turn.small = 0, turn.small_ph ^= 1;
                 }
             }
             if (!ok) {                                  // products in flight end before tensor memory is given back
@@ -441,7 +461,7 @@ struct Pipe {
                 ok = wait(&sh->tile_full[walk.slot], walk.ph);
                 const Tile &t = *tile_at<Tile>(walk);
                 if (!ok || t.n == 0) break;
-                int k = t.segs * t.k_seg;
+                int k = t.stages;
                 tile_done(walk);
                 for (; ok && k > 0; --k) {
                     ok = wait(&sh->full[s], ph);
@@ -489,8 +509,24 @@ struct Pipe {
     __device__ __forceinline__ bool take(Turn &t, uint32_t &at) {
         if (!warp_wait(&sh->acc_full[t.acc], t.ph)) return false;
         tmem_fence_after();
-        at = sh->tmem + (uint32_t)t.acc * 256 + ((uint32_t)(threadIdx.x / 32 % 4) << 21);
+        at = sh->tmem + (uint32_t)t.acc * kAccCols + ((uint32_t)(threadIdx.x / 32 % 4) << 21);
         return true;
+    }
+    // The same for the tile's small products, after its last chunk.
+    __device__ __forceinline__ bool take_small(Turn &t, uint32_t &at) {
+        if (!warp_wait(&sh->small_full[t.small], t.small_ph)) return false;
+        tmem_fence_after();
+        at = sh->tmem + (uint32_t)(2 + t.small) * kAccCols + ((uint32_t)(threadIdx.x / 32 % 4) << 21);
+        return true;
+    }
+    __device__ __forceinline__ void release_small(Turn &t, int lane) {
+        tmem_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+            if (CG == 1) mbar_arrive(&sh->small_empty[t.small]);
+            else mbar_arrive_remote(&sh->small_empty[t.small], 0);
+        }
+        if (++t.small == 2) t.small = 0, t.small_ph ^= 1;
     }
     // Called by every epilogue warp once it has read its part of the accumulator for the last time.
     __device__ __forceinline__ void release(Turn &t, int lane) {

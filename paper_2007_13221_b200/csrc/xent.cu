@@ -76,7 +76,7 @@ struct LogitsJob {
     static constexpr bool kCopier = false;
 
     struct Tile {
-        int w, i, j, n, segs, k_seg, a_lim, b_lim;
+        int w, i, j, n, stages, a_lim, b_lim;
     };
     __device__ __forceinline__ void tile(Tile &t, int k, int) const {
         const int at = first + k * every, per = a.token_tiles * vocab_tiles;
@@ -84,10 +84,10 @@ struct LogitsJob {
         if (t.w >= a.n) return;
         const int r = at - t.w * per;
         t.j = r / a.token_tiles, t.i = r - t.j * a.token_tiles;
-        t.n = 256, t.segs = 1, t.k_seg = (a.dim + 63) / 64, t.a_lim = t.b_lim = t.k_seg;
+        t.n = 256, t.stages = (a.dim + 63) / 64, t.a_lim = t.b_lim = t.stages;
     }
     __device__ __forceinline__ bool ready(Pipe<CG> &, const Tile &) const { return true; }
-    __device__ __forceinline__ bool chunk_ends(const Tile &t, int, int k) const { return k + 1 == t.k_seg; }
+    __device__ __forceinline__ bool chunk_ends(const Tile &t, int k) const { return k + 1 == t.stages; }
     __device__ __forceinline__ int bf16() const { return a.bf16; }
     struct Loader {
         const CUtensorMap *h, *w;
@@ -96,7 +96,6 @@ struct LogitsJob {
             : h(&job.a.h), w(&job.a.w), row_a(t.i * 128 * CG + rank * 128), row_b(job.a.piece0 + t.j * 256 + rank * 128),
               wa(job.a.h_workers == 1 ? 0 : t.w), wb(job.a.w_workers == 1 ? 0 : t.w) {}
         __device__ __forceinline__ uint32_t bytes() const { return Pipe<CG>::kStageBytes; }
-        __device__ __forceinline__ void seg(int) {}
         __device__ __forceinline__ void load(int k, uint32_t sa, uint32_t sb, uint64_t *bar) const {
 #pragma unroll
             for (int p = 0; p < 2; ++p) tensor_copy_in(sa + p * 8192, h, k * 64, row_a + p * 64, wa, bar);
@@ -265,34 +264,49 @@ template <int CG>
 struct GradJob {
     using P = GradPipe<CG>;
     const XentArgs &a;
-    int first, every, n_dh, n_dw, dim_tiles, vocab_tiles;
+    int first, every, n_dh, n_dw, dim_tiles, vocab_tiles, early;
     static constexpr bool kCopier = false;
 
     struct Tile {
-        int w, i, j, n, segs, k_seg, a_lim, b_lim, k0, split, dw;
+        int w, i, j, n, stages, a_lim, b_lim, k0, split, dw;
     };
+    // dh's tiles are long (the piece), dW's short (the tokens).  All of dh's come first, dealt out in turn; the CTAs that got one
+    // less than the others take `early` tiles of dW in its place, the rest of dW is dealt out in turn again.
     __device__ __forceinline__ void tile(Tile &t, int k, int) const {
-        int at = first + k * every;
-        t.n = 0, t.dw = at >= n_dh;
-        if (t.dw) at -= n_dh;
-        if (t.dw && at >= n_dw) return;
+        const int extra = n_dh % every, mine = n_dh / every + (first < extra);
+        int at;
+        t.n = 0, t.dw = k >= mine;
+        if (!t.dw) {
+            at = k * every + first;
+        } else {
+            int rest = k - mine, begin = 0;
+            if (extra) {
+                begin = early * (every - extra);
+                if (first >= extra) {
+                    if (rest < early) begin = -1;
+                    else rest -= early;
+                }
+            }
+            at = begin < 0 ? rest * (every - extra) + first - extra : begin + rest * every + first;
+            if (at >= n_dw) return;
+        }
         t.j = at % dim_tiles, at /= dim_tiles;
         const int width = (a.dim + 64 * CG - 1) / (64 * CG) * (64 * CG);
         t.n = width - t.j * 256 < 256 ? width - t.j * 256 : 256;
         if (t.dw) {
             t.i = at % vocab_tiles, t.w = at / vocab_tiles;
-            t.k0 = 0, t.k_seg = (a.tokens + 63) / 64, t.split = 0, t.a_lim = 0;
+            t.k0 = 0, t.stages = (a.tokens + 63) / 64, t.split = 0, t.a_lim = 0;
         } else {
             t.split = at % a.splits, at /= a.splits;
             t.i = at % a.token_tiles, t.w = at / a.token_tiles;
             const int all = (a.piece_n + 63) / 64;
             t.k0 = (int)((long long)all * t.split / a.splits);
-            t.k_seg = (int)((long long)all * (t.split + 1) / a.splits) - t.k0, t.a_lim = t.k_seg;
+            t.stages = (int)((long long)all * (t.split + 1) / a.splits) - t.k0, t.a_lim = t.stages;
         }
-        t.segs = 1, t.b_lim = 0;
+        t.b_lim = 0;
     }
     __device__ __forceinline__ bool ready(P &, const Tile &) const { return true; }
-    __device__ __forceinline__ bool chunk_ends(const Tile &t, int, int k) const { return k + 1 == t.k_seg; }
+    __device__ __forceinline__ bool chunk_ends(const Tile &t, int k) const { return k + 1 == t.stages; }
     __device__ __forceinline__ int bf16() const { return a.bf16; }
     struct Loader {
         const CUtensorMap *b;
@@ -309,7 +323,6 @@ struct GradJob {
             worker = (dw ? a.h_workers : a.w_workers) == 1 ? 0 : t.w;
         }
         __device__ __forceinline__ uint32_t bytes() const { return 128 * 128 + (uint32_t)boxes * 8192; }
-        __device__ __forceinline__ void seg(int) {}
         __device__ __forceinline__ void load(int k, uint32_t sa, uint32_t sb, uint64_t *bar) const {
             if (dw) {
                 bulk_copy_in(sa, dz + (size_t)k * 8192, 8192, bar);
@@ -393,7 +406,14 @@ __global__ void __launch_bounds__(kThreads, 1) xent_grad_kernel(const __grid_con
     p.template setup<GradJob<CG>>(raw, a.err);
     const int width = (a.dim + 64 * CG - 1) / (64 * CG) * (64 * CG);
     GradJob<CG> job{a, (int)blockIdx.x / CG, (int)gridDim.x / CG, n_dh, n_dw, (width + 255) / 256,
-                    (a.piece_n + 128 * CG - 1) / (128 * CG)};
+                    (a.piece_n + 128 * CG - 1) / (128 * CG), 0};
+    if (n_dh && n_dw) {
+        // A tile of dh in tiles of dW, whose epilogue takes as long as 12 stages, and of which there may not be that many.
+        const int stages = ((a.piece_n + 63) / 64 + a.splits - 1) / a.splits, less = job.every - n_dh % job.every;
+        const int each = (a.tokens + 63) / 64, fits = n_dw / less;
+        job.early = stages / (each < 12 ? 12 : each);
+        if (job.early > fits) job.early = fits;
+    }
     p.run(job);
     p.teardown();
 }
