@@ -1,7 +1,7 @@
 // Orthogonalised updates (cser_orth_* of include/cser_train.h): Newton-Schulz products on the matrices inside the flat
 // gradients of n workers, grouped: one call is three kernels, whatever the number of matrices.
 //
-//   orth_norm_kernel     one pass over g (and m, which it updates): |u|_F^2 per matrix
+//   orth_norm_kernel     one pass over g (and m, which it updates): |u|_F per matrix
 //   orth_convert_kernel  X = u / (|u|_F + 1e-7) as 16-bit panels (tensor_tiles.cuh)
 //   orth_products_kernel all products of all steps, persistent
 //
@@ -32,7 +32,6 @@
 #include <math.h>
 #include <stdint.h>
 #include <stdio.h>
-#include <stdlib.h>
 #include <new>
 #include <vector>
 
@@ -45,15 +44,17 @@ namespace {
 
 constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f, kEps = 1e-7f;
 constexpr float kScale = 4096.f, kUnscale = 1.f / 4096.f, kUnscale2 = kUnscale * kUnscale;
-constexpr int kNormChunk = 8192;                   // elements per CTA of the norm kernel
-// Columns of a tile, for CTAs in pairs (cg = 2) or single ones; a 32-bit result's sums must fit the epilogue's registers.
-constexpr int tile_n(int cg, bool split) { return cg == 2 && !split ? 256 : 128; }
+constexpr int kNormChunk = 16384;                  // elements per CTA of the norm kernel
+// How tiles are cut: 128 x 64 or 128 x 128 by one CTA, or 256 rows by a pair of CTAs (by 256 columns; 128 for a 32-bit result, whose
+// sums must fit the epilogue's registers).
+enum { kNarrow = 0, kSingle = 1, kPaired = 2 };
+__host__ __device__ constexpr int mode_cg(int mode) { return mode == kPaired ? 2 : 1; }
+__host__ __device__ constexpr int tile_n(int mode, bool split) { return mode == kNarrow ? 64 : mode == kPaired && !split ? 256 : 128; }
 // The tensor cores truncate every partial sum, about 2^-24 of it for 16 terms: 2e-5 over an inner dimension of 4096.  So a
 // 32-bit result's accumulator of hi hi is taken out and added up in registers, rounded, after this many stages.  X's
 // product is the one whose error the steps after it do not shrink: with a low-rank matrix 9e-6 at 4 stages.
 constexpr int kChunkAB = 4, kChunkX = 1;
 constexpr size_t kGroupBytes = 2ull << 30;         // workspace of one group of matrices
-constexpr size_t kBatchBytes = 96ull << 20;        // of it, what is worked on together
 
 struct OrthMat {
     __half *xh[2], *xl[2], *ah, *al, *bh, *bl;     // panels; al, bl for 32-bit results only
@@ -71,25 +72,19 @@ struct OrthTile {
     uint32_t q;
     uint16_t i, j;
 };
-// Matrices whose steps are worked on together, so that their X, A and B stay in L2: where their tiles are in the lists.
-struct OrthBatch {
-    int sym, n_sym, x, n_x;
-    long long first;                               // position of their first tile in the order of work
-};
-struct ConvertUnit {
+struct PanelUnit {
     uint32_t q, r0, c0;                            // 32 rows, up to 4 panels
 };
 
 struct OrthArgs {
     const OrthMat *mats;
     const OrthTile *sym, *x;
-    const OrthBatch *batch;                        // and one more, whose `first` is the number of all tiles
-    int steps;
+    int n_sym, n_x, steps;
     unsigned *done;                                // [matrices] finished tiles
     unsigned *ticket;                              // [matrices] norm kernel
     float *partial, *inv;                          // [chunks], [matrices] 1 / (norm + eps)
     const uint2 *chunk;                            // (matrix, chunk in it)
-    const ConvertUnit *unit;
+    const PanelUnit *unit;
     const void *grad;
     float *m;
     float mu;
@@ -125,81 +120,7 @@ __device__ __forceinline__ void load8(const T *p, int n, float (&v)[8]) {
 
 #include "orth_small.cuh"
 
-// ------------------------------------------------------------------ |u|_F, momentum
-// HBM-bound: g read once (m read and written once).  The last CTA of a matrix adds the partial sums in their order.
-template <typename T>
-__global__ void __launch_bounds__(256) orth_norm_kernel(const OrthArgs a) {
-    __shared__ float red[8];
-    __shared__ int last;
-    const uint2 ck = a.chunk[blockIdx.x];
-    const OrthMat &M = a.mats[ck.x];
-    const T *g = static_cast<const T *>(a.grad) + M.offset;
-    float *m = a.m ? a.m + M.offset : nullptr;
-    const long long total = (long long)M.rows * M.cols, e0 = (long long)ck.y * kNormChunk;
-    const long long end = e0 + kNormChunk < total ? e0 + kNormChunk : total;
-    float sum = 0.f;
-    if (M.stride == M.cols) {
-        for (long long e = e0 + threadIdx.x * 8; e < end; e += 2048) {
-            const int n = end - e < 8 ? (int)(end - e) : 8;
-            float v[8], w[8];
-            load8(g + e, n, v);
-            if (m) {
-                load8(m + e, n, w);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) w[k] = __fadd_rn(__fmul_rn(a.mu, w[k]), v[k]), v[k] = __fadd_rn(v[k], __fmul_rn(a.mu, w[k]));
-                if (n == 8 && (reinterpret_cast<uintptr_t>(m + e) & 15) == 0) {
-                    reinterpret_cast<float4 *>(m + e)[0] = make_float4(w[0], w[1], w[2], w[3]);
-                    reinterpret_cast<float4 *>(m + e)[1] = make_float4(w[4], w[5], w[6], w[7]);
-                } else {
-#pragma unroll
-                    for (int k = 0; k < 8; ++k)
-                        if (k < n) m[e + k] = w[k];
-                }
-            }
-#pragma unroll
-            for (int k = 0; k < 8; ++k) sum = __fmaf_rn(v[k], v[k], sum);
-        }
-    } else {
-        for (long long e = e0 + threadIdx.x; e < end; e += 256) {
-            const long long r = e / M.cols, at = r * M.stride + (e - r * M.cols);
-            float v = to_f<T>(g[at]);
-            if (m) {
-                const float w = __fadd_rn(__fmul_rn(a.mu, m[at]), v);
-                m[at] = w;
-                v = __fadd_rn(v, __fmul_rn(a.mu, w));
-            }
-            sum = __fmaf_rn(v, v, sum);
-        }
-    }
-    for (int k = 16; k; k >>= 1) sum += __shfl_xor_sync(~0u, sum, k);
-    if (threadIdx.x % 32 == 0) red[threadIdx.x / 32] = sum;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        float s = 0.f;
-        for (int k = 0; k < 8; ++k) s += red[k];
-        a.partial[M.chunk0 + ck.y] = s;
-        __threadfence();
-        last = atomicAdd(&a.ticket[ck.x], 1u) == (unsigned)M.chunks - 1;
-        __threadfence();
-    }
-    __syncthreads();
-    if (!last) return;
-    float s = 0.f;
-    for (int k = threadIdx.x; k < M.chunks; k += 256) s += __ldcg(&a.partial[M.chunk0 + k]);
-    for (int k = 16; k; k >>= 1) s += __shfl_xor_sync(~0u, s, k);
-    __syncthreads();
-    if (threadIdx.x % 32 == 0) red[threadIdx.x / 32] = s;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        s = 0.f;
-        for (int k = 0; k < 8; ++k) s += red[k];
-        a.inv[ck.x] = __fdiv_rn(1.f, __fadd_rn(__fsqrt_rn(s), kEps));
-        a.ticket[ck.x] = 0;                        // for the next call
-        a.done[ck.x] = 0;
-    }
-}
-
-// ------------------------------------------------------------------ X as panels
+// ------------------------------------------------------------------ |u|_F, momentum, X as panels
 // 8 values as one chunk of fp16 and one of what that leaves.
 __device__ __forceinline__ void split8(const float *v, uint4 &hi, uint4 &lo) {
     uint32_t h[4], l[4];
@@ -230,18 +151,110 @@ __device__ __forceinline__ char *wide_at(float *base, int rows, int panel) {
     return reinterpret_cast<char *>(base) + (size_t)panel * rows * 256;
 }
 
-// A thread makes one chunk of 8 columns per panel; the padding becomes 0.
+// u = g, or m <- mu m + g, u = g + mu m, for 8 values.
+__device__ __forceinline__ void momentum8(float mu, float (&v)[8], float (&w)[8]) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) w[k] = __fadd_rn(__fmul_rn(mu, w[k]), v[k]), v[k] = __fadd_rn(v[k], __fmul_rn(mu, w[k]));
+}
+
+// A chunk of a matrix: g read (m read and written), the sum of u's squares.  The matrix's last chunk adds the
+// partial sums in their order.
 template <typename T>
-__global__ void __launch_bounds__(256) orth_convert_kernel(const OrthArgs a) {
-    const ConvertUnit u = a.unit[blockIdx.x];
-    const OrthMat &M = a.mats[u.q];
-    const int row = u.r0 + threadIdx.x / 8, c = threadIdx.x % 8;
-    if (row >= M.rp) return;
-    const float f = __fmul_rn(a.inv[u.q], kScale);
+__device__ __forceinline__ void norm_chunk(const OrthArgs &a, uint32_t q, uint32_t chunk, float *red, int &last) {
+    const OrthMat &M = a.mats[q];
+    const T *g = static_cast<const T *>(a.grad) + M.offset;
+    float *m = a.m ? a.m + M.offset : nullptr;
+    const long long total = (long long)M.rows * M.cols, e0 = (long long)chunk * kNormChunk;
+    const long long end = e0 + kNormChunk < total ? e0 + kNormChunk : total;
+    float sum = 0.f;
+    if (M.stride == M.cols && end - e0 == kNormChunk && (reinterpret_cast<uintptr_t>(g + e0) & 15) == 0 &&
+        (!m || (reinterpret_cast<uintptr_t>(m + e0) & 15) == 0)) {
+        for (long long e = e0 + threadIdx.x * 8; e < end; e += 4 * 2048) {
+            float v[4][8], w[4][8];                // four loads of each under way at a time
+#pragma unroll
+            for (int k = 0; k < 4; ++k) load8(g + e + k * 2048, 8, v[k]);
+            if (m) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) load8(m + e + k * 2048, 8, w[k]);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    momentum8(a.mu, v[k], w[k]);
+                    float4 *o = reinterpret_cast<float4 *>(m + e + k * 2048);
+                    o[0] = make_float4(w[k][0], w[k][1], w[k][2], w[k][3]), o[1] = make_float4(w[k][4], w[k][5], w[k][6], w[k][7]);
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int p = 0; p < 8; ++p) sum = __fmaf_rn(v[k][p], v[k][p], sum);
+        }
+    } else if (M.stride == M.cols) {
+        for (long long e = e0 + threadIdx.x * 8; e < end; e += 2048) {
+            const int n = end - e < 8 ? (int)(end - e) : 8;
+            float v[8], w[8];
+            load8(g + e, n, v);
+            if (m) {
+                load8(m + e, n, w);
+                momentum8(a.mu, v, w);
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (k < n) m[e + k] = w[k];
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (k < n) sum = __fmaf_rn(v[k], v[k], sum);
+        }
+    } else {
+        for (long long e = e0 + threadIdx.x; e < end; e += 256) {
+            const long long r = e / M.cols, at = r * M.stride + (e - r * M.cols);
+            float v = to_f<T>(g[at]);
+            if (m) {
+                const float w = __fadd_rn(__fmul_rn(a.mu, m[at]), v);
+                m[at] = w;
+                v = __fadd_rn(v, __fmul_rn(a.mu, w));
+            }
+            sum = __fmaf_rn(v, v, sum);
+        }
+    }
+    for (int k = 16; k; k >>= 1) sum += __shfl_xor_sync(~0u, sum, k);
+    if (threadIdx.x % 32 == 0) red[threadIdx.x / 32] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        float s = 0.f;
+        for (int k = 0; k < 8; ++k) s += red[k];
+        a.partial[M.chunk0 + chunk] = s;
+        __threadfence();
+        last = atomicAdd(&a.ticket[q], 1u) == (unsigned)M.chunks - 1;
+        __threadfence();
+    }
+    __syncthreads();
+    if (!last) return;
+    float s = 0.f;
+#pragma unroll 8
+    for (int k = threadIdx.x; k < M.chunks; k += 256) s += __ldcg(&a.partial[M.chunk0 + k]);
+    for (int k = 16; k; k >>= 1) s += __shfl_xor_sync(~0u, s, k);
+    __syncthreads();
+    if (threadIdx.x % 32 == 0) red[threadIdx.x / 32] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        s = 0.f;
+        for (int k = 0; k < 8; ++k) s += red[k];
+        a.inv[q] = __fdiv_rn(1.f, __fadd_rn(__fsqrt_rn(s), kEps));
+        a.ticket[q] = 0;                           // for the next call
+        a.done[q] = 0;
+    }
+}
+
+// 32 rows of up to 4 panels: a thread makes one chunk of 8 columns per panel; the padding becomes 0.
+template <typename T>
+__device__ __forceinline__ void make_panels(const OrthArgs &a, uint32_t q, int r0, int c0) {
+    const OrthMat &M = a.mats[q];
+    const int row = r0 + threadIdx.x / 8, c = threadIdx.x % 8;
+    const float f = __fmul_rn(__ldcg(a.inv + q), kScale);
     float v[4][8];
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
-        const int col = u.c0 + p * 64 + c * 8;
+        const int col = c0 + p * 64 + c * 8;
         const int n = row < M.rows ? M.cols - col : 0;
         const long long at = M.offset + (long long)row * M.stride + col;
         if (n > 0) {
@@ -259,7 +272,7 @@ __global__ void __launch_bounds__(256) orth_convert_kernel(const OrthArgs a) {
     }
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
-        const int col = u.c0 + p * 64;
+        const int col = c0 + p * 64;
         if (col >= M.cp) break;
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[p][k] = __fmul_rn(v[p][k], f);
@@ -276,19 +289,34 @@ __global__ void __launch_bounds__(256) orth_convert_kernel(const OrthArgs a) {
     }
 }
 
+// Both bound by memory: making X needs the whole matrix's norm, so g (and m) are read twice.  (One kernel that makes a batch's panels
+// while its g and m are still in L2 read less and was slower, 387 against 375 us for 8 x 12.6 M elements with momentum: its units'
+// chain of dependent loads outweighed it.)
+template <typename T>
+__global__ void __launch_bounds__(256) orth_norm_kernel(const OrthArgs a) {
+    __shared__ float red[8];
+    __shared__ int last;
+    const uint2 c = a.chunk[blockIdx.x];
+    norm_chunk<T>(a, c.x, c.y, red, last);
+}
+template <typename T>
+__global__ void __launch_bounds__(256) orth_convert_kernel(const OrthArgs a) {
+    const PanelUnit u = a.unit[blockIdx.x];
+    make_panels<T>(a, u.q, (int)u.r0, (int)u.c0);
+}
+
 // ------------------------------------------------------------------ products
 enum { kPhaseA = 0, kPhaseB = 1, kPhaseX = 2 };
 
-template <int CG, bool SPLIT>
-using OrthPipe = Pipe<CG, tile_n(CG, SPLIT), SPLIT ? 65536 : 98304, SPLIT>;
+template <int MODE, bool SPLIT>
+using OrthPipe = Pipe<mode_cg(MODE), tile_n(MODE, SPLIT), SPLIT ? 65536 : 98304, SPLIT>;
 
-template <int CG, bool SPLIT>
+template <int MODE, bool SPLIT>
 struct OrthJob {
-    using P = OrthPipe<CG, SPLIT>;
+    using P = OrthPipe<MODE, SPLIT>;
+    static constexpr int CG = mode_cg(MODE), TN = tile_n(MODE, SPLIT), kSums = SPLIT ? TN / 64 : 1;
     const OrthArgs &a;
     int first, every;
-    int at_batch = 0;                                                // of the last tile asked for: positions only grow
-    static constexpr int TN = tile_n(CG, SPLIT);
     static constexpr bool kCopier = true;
 
     struct Tile {
@@ -306,17 +334,16 @@ struct OrthJob {
         float scale;
     };
 
-    __device__ __forceinline__ void tile(Tile &t, int k, int rank) {
+    __device__ __forceinline__ void tile(Tile &t, int k, int rank) const {
         t.n = 0;
         const long long at = first + (long long)k * every;
-        while (at >= a.batch[at_batch + 1].first)
-            if (a.batch[++at_batch].n_x == 0) return;                // the one behind the last
-        const OrthBatch B = a.batch[at_batch];
-        const int in = (int)(at - B.first), per_step = 2 * B.n_sym + B.n_x, step = in / per_step;
+        const int per_step = 2 * a.n_sym + a.n_x;
+        if (at >= (long long)per_step * a.steps) return;
+        const int in = (int)at, step = in / per_step;
         int r = in - step * per_step, phase = kPhaseA;
-        const OrthTile *list = a.sym + B.sym;
-        if (r >= B.n_sym) r -= B.n_sym, phase = kPhaseB;
-        if (phase == kPhaseB && r >= B.n_sym) r -= B.n_sym, phase = kPhaseX, list = a.x + B.x;
+        const OrthTile *list = a.sym;
+        if (r >= a.n_sym) r -= a.n_sym, phase = kPhaseB;
+        if (phase == kPhaseB && r >= a.n_sym) r -= a.n_sym, phase = kPhaseX, list = a.x;
         const OrthTile e = list[r];
         const OrthMat &M = a.mats[e.q];
         const int width = phase == kPhaseX ? M.cp : M.sp, from = step & 1, to = from ^ 1;
@@ -517,13 +544,13 @@ struct OrthJob {
         const bool last = t.last;
         const float d_row = t.phase == kPhaseB ? __ldcg(t.da + row) : t.phase == kPhaseX && !t.tall ? __ldcg(t.db + row) : 0.f;
         uint32_t tmem;
-        float sum[2][16];                                            // of a 32-bit result's chunks
+        float sum[kSums][16];                                        // of a 32-bit result's chunks
         if (SPLIT) {
             const int each = t.phase == kPhaseX ? kChunkX : kChunkAB, chunks = (t.stages + each - 1) / each;
             for (int c = 0; c <= chunks; ++c) {                      // hi hi, then the small products
                 if (c < chunks ? !p.take(turn, tmem) : !p.take_small(turn, tmem)) return false;
 #pragma unroll
-                for (int b = 0; b < 2; ++b) {
+                for (int b = 0; b < kSums; ++b) {
                     float v[16];
                     tmem_load(tmem + b * 64 + side * 16, v);
 #pragma unroll
@@ -535,8 +562,8 @@ struct OrthJob {
         } else if (!p.take(turn, tmem)) {
             return false;
         }
-#pragma unroll(SPLIT ? 2 : 1)
-        for (int b = 0; b < (SPLIT ? 2 : panels); ++b) {
+#pragma unroll kSums
+        for (int b = 0; b < (SPLIT ? kSums : panels); ++b) {
             const int panel = t.panel0 + b, col = panel * 64 + side * 16;
             if (!p.warp_wait(&p.sh->extra_full[ring.buf], ring.parity())) return false;
             const uint32_t at = p.extra + ring.buf * kBufBytes;
@@ -653,12 +680,13 @@ struct OrthJob {
     }
 };
 
-template <int CG, bool SPLIT>
+template <int MODE, bool SPLIT>
 __global__ void __launch_bounds__(kThreads, 1) orth_products_kernel(const __grid_constant__ OrthArgs a) {
     extern __shared__ unsigned char raw[];
-    OrthPipe<CG, SPLIT> p;
-    p.template setup<OrthJob<CG, SPLIT>>(raw, a.err);
-    OrthJob<CG, SPLIT> job{a, (int)blockIdx.x / CG, (int)gridDim.x / CG};
+    constexpr int CG = mode_cg(MODE);
+    OrthPipe<MODE, SPLIT> p;
+    p.template setup<OrthJob<MODE, SPLIT>>(raw, a.err);
+    OrthJob<MODE, SPLIT> job{a, (int)blockIdx.x / CG, (int)gridDim.x / CG};
     p.run(job);
     p.teardown();
 }
@@ -676,7 +704,7 @@ __global__ void __launch_bounds__(kThreads, 1) orth_products_kernel(const __grid
 
 struct cser_orth {
     struct Group {
-        int cg = 1, grid = 0, n_chunk = 0, n_unit = 0;
+        int mode = kSingle, grid = 0, n_chunk = 0, n_unit = 0;
         OrthArgs args{};
         void *tables = nullptr;                    // one allocation for the lists and matrices
     };
@@ -689,6 +717,9 @@ struct cser_orth {
         size_t gram_shared = 0, apply_shared = 0, resident_shared = 0;
         void *tables = nullptr;
     } small, resident;                             // resident: those of them that fit a CTA's shared memory
+    // Small matrices run beside the large ones, on a stream of the plan's own.
+    cudaStream_t side = nullptr;
+    cudaEvent_t fork = nullptr, join = nullptr;
     void *work = nullptr;                          // shared by the groups, which run one after the other
     unsigned *err_host = nullptr;
     long long launches = 0;
@@ -699,12 +730,13 @@ namespace {
 int type_size(int t) { return t == CSER_TYPE_F32 ? 4 : 2; }
 long long up(long long v, long long to) { return (v + to - 1) / to * to; }
 
-template <int CG, bool SPLIT>
+template <int MODE, bool SPLIT>
 cudaError_t products_launch(const OrthArgs &a, int grid, cudaStream_t st) {
+    constexpr int CG = mode_cg(MODE);
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)grid);
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = OrthPipe<CG, SPLIT>::kSharedBytes;
+    cfg.dynamicSmemBytes = OrthPipe<MODE, SPLIT>::kSharedBytes;
     cfg.stream = st;
     cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeCooperative;
@@ -713,23 +745,24 @@ cudaError_t products_launch(const OrthArgs &a, int grid, cudaStream_t st) {
     at[1].val.clusterDim.x = CG, at[1].val.clusterDim.y = 1, at[1].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = CG == 1 ? 1 : 2;
-    return cudaLaunchKernelEx(&cfg, orth_products_kernel<CG, SPLIT>, a);
+    return cudaLaunchKernelEx(&cfg, orth_products_kernel<MODE, SPLIT>, a);
 }
-template <int CG, bool SPLIT>
+template <int MODE, bool SPLIT>
 cudaError_t products_setup(int &pairs) {
-    cudaError_t e = cudaFuncSetAttribute(orth_products_kernel<CG, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                         (int)OrthPipe<CG, SPLIT>::kSharedBytes);
+    constexpr int CG = mode_cg(MODE);
+    cudaError_t e = cudaFuncSetAttribute(orth_products_kernel<MODE, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                         (int)OrthPipe<MODE, SPLIT>::kSharedBytes);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(CG);
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = OrthPipe<CG, SPLIT>::kSharedBytes;
+    cfg.dynamicSmemBytes = OrthPipe<MODE, SPLIT>::kSharedBytes;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = CG, at[0].val.clusterDim.y = 1, at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    return cudaOccupancyMaxActiveClusters(&pairs, orth_products_kernel<CG, SPLIT>, &cfg);
+    return cudaOccupancyMaxActiveClusters(&pairs, orth_products_kernel<MODE, SPLIT>, &cfg);
 }
 
 int orth_fail(cser_orth *h, int code, const char *what) {
@@ -756,9 +789,12 @@ size_t work_of(const OrthMat &M, bool split) {
     return (size_t)M.rp * M.cp * 2 * (split ? 8 : 4) + (size_t)M.sp * M.sp * 2 * (split ? 4 : 2) + (size_t)M.sp * 8;
 }
 
-// Tiles of 256 rows by a pair of CTAs, or of 128 by one.
-bool pairs_pay(const std::vector<HostMat> &all, bool split, int pairs) {
-    if (getenv("CSER_CG")) return atoi(getenv("CSER_CG")) == 2;
+// How a plan's tiles are cut, by the padded elements of all its matrices.  Pairs bring half the bytes per product: two of 2048 x
+// 4096 548 us, single CTAs 744, narrow tiles 1317 (16-bit results; 32-bit 1726, 1817, 2684).  They need tiles for all SMs
+// (1024 x 4096: 314, 303, 327) and matrices that 256 rows do not pad much.  Where there are few tiles the chain of phases is the
+// bound and narrow ones shorten its links (512 x 512: 193, 141, 125; 8 workers' 256 x 256 and 256 x 1024: 205, 157, 143; 8 of 768 x
+// 768, 288 tiles of 128 x 128: 235, 204, 220).
+int choose_mode(const std::vector<HostMat> &all, bool split, int pairs, int sms) {
     double area[3] = {0, 0, 0};
     for (const HostMat &m : all)
         for (int cg = 1; cg <= 2; ++cg) {
@@ -766,36 +802,22 @@ bool pairs_pay(const std::vector<HostMat> &all, bool split, int pairs) {
             shape_of(m, cg, M);
             area[cg] += (double)M.rp * M.cp;
         }
-    return area[2] <= 1.15 * area[1] && area[2] >= 65536.0 * pairs;
+    if (area[2] <= 1.15 * area[1] && area[2] >= 256.0 * tile_n(kPaired, split) * pairs) return kPaired;
+    return area[1] < 1.5 * 16384.0 * sms ? kNarrow : kSingle;
 }
 
-int build_group(cser_orth *h, cser_orth::Group &G, const std::vector<HostMat> &ms, int cg, int steps, int pairs) {
+int build_group(cser_orth *h, cser_orth::Group &G, const std::vector<HostMat> &ms, int mode, int steps, int ctas) {
+    const int cg = mode_cg(mode);
     std::vector<OrthMat> mats(ms.size());
     std::vector<OrthTile> sym, xs;
-    std::vector<OrthBatch> batch;
-    size_t in_batch = 0, widest = 0;
-    auto close_batch = [&](size_t next_bytes) {     // opens a batch at the lists' ends where this one is full
-        if (!batch.empty()) {
-            OrthBatch &B = batch.back();
-            B.n_sym = (int)sym.size() - B.sym, B.n_x = (int)xs.size() - B.x;
-            if (next_bytes && in_batch + next_bytes <= (getenv("CSER_BB") ? (size_t)atoi(getenv("CSER_BB")) << 20 : kBatchBytes)) return;
-            if ((size_t)B.n_sym > widest) widest = B.n_sym;
-            if ((size_t)B.n_x > widest) widest = B.n_x;
-        }
-        const long long from = batch.empty() ? 0 : batch.back().first + (long long)steps * (2 * batch.back().n_sym + batch.back().n_x);
-        batch.push_back({(int)sym.size(), 0, (int)xs.size(), 0, from});
-        in_batch = 0;
-    };
     std::vector<uint2> chunk;
-    std::vector<ConvertUnit> unit;
+    std::vector<PanelUnit> unit;
     size_t at = 0;
     char *base = static_cast<char *>(h->work);
     int chunk0 = 0;
     for (size_t q = 0; q < ms.size(); ++q) {
         OrthMat &M = mats[q];
         shape_of(ms[q], cg, M);
-        close_batch(work_of(M, h->split));
-        in_batch += work_of(M, h->split);
         const size_t xb = (size_t)M.rp * M.cp * 2, ab = (size_t)M.sp * M.sp * 2;
         auto take = [&](size_t b) { char *p = base + at; at += b; return reinterpret_cast<__half *>(p); };
         M.xh[0] = take(xb), M.xl[0] = take(xb), M.xh[1] = take(xb), M.xl[1] = take(xb), M.ah = take(ab), M.bh = take(ab);
@@ -809,7 +831,7 @@ int build_group(cser_orth *h, cser_orth::Group &G, const std::vector<HostMat> &m
         for (int c = 0; c < M.chunks; ++c) chunk.push_back(make_uint2((unsigned)q, (unsigned)c));
         for (int r = 0; r < M.rp; r += 32)
             for (int c = 0; c < M.cp; c += 256) unit.push_back({(uint32_t)q, (uint32_t)r, (uint32_t)c});
-        const int tm = 128 * cg, tn = tile_n(cg, h->split);
+        const int tm = 128 * cg, tn = tile_n(mode, h->split);
         for (int j = 0; j * tn < M.sp; ++j)
             for (int i = 0; i * tm < M.sp; ++i)
                 if (i * tm / 256 >= j * tn / 256) sym.push_back({(uint32_t)q, (uint16_t)i, (uint16_t)j}), M.tiles_sym += cg;
@@ -821,13 +843,13 @@ int build_group(cser_orth *h, cser_orth::Group &G, const std::vector<HostMat> &m
                 for (int i = 0; i * tm < M.rp; ++i) xs.push_back({(uint32_t)q, (uint16_t)i, (uint16_t)j}), M.tiles_x += cg;
         }
     }
-    close_batch(0);
     const size_t n = ms.size();
     size_t bytes = 0;
     auto place = [&](size_t b) { const size_t p = bytes; bytes += (b + 255) / 256 * 256; return p; };
     const size_t o_mat = place(n * sizeof(OrthMat)), o_sym = place(sym.size() * sizeof(OrthTile)),
                  o_x = place(xs.size() * sizeof(OrthTile)), o_ck = place(chunk.size() * sizeof(uint2)),
-                 o_un = place(unit.size() * sizeof(ConvertUnit)), o_ba = place(batch.size() * sizeof(OrthBatch)), o_done = place(n * 4), o_tick = place(n * 4),
+                 o_un = place(unit.size() * sizeof(PanelUnit)),
+                 o_done = place(n * 4), o_tick = place(n * 4),
                  o_inv = place(n * 4), o_part = place((size_t)chunk0 * 4);
     TRY(cudaMalloc(&G.tables, bytes));
     char *t = static_cast<char *>(G.tables);
@@ -835,20 +857,20 @@ int build_group(cser_orth *h, cser_orth::Group &G, const std::vector<HostMat> &m
     TRY(cudaMemcpy(t + o_mat, mats.data(), n * sizeof(OrthMat), cudaMemcpyHostToDevice));
     TRY(cudaMemcpy(t + o_sym, sym.data(), sym.size() * sizeof(OrthTile), cudaMemcpyHostToDevice));
     TRY(cudaMemcpy(t + o_x, xs.data(), xs.size() * sizeof(OrthTile), cudaMemcpyHostToDevice));
+    TRY(cudaMemcpy(t + o_un, unit.data(), unit.size() * sizeof(PanelUnit), cudaMemcpyHostToDevice));
     TRY(cudaMemcpy(t + o_ck, chunk.data(), chunk.size() * sizeof(uint2), cudaMemcpyHostToDevice));
-    TRY(cudaMemcpy(t + o_un, unit.data(), unit.size() * sizeof(ConvertUnit), cudaMemcpyHostToDevice));
-    TRY(cudaMemcpy(t + o_ba, batch.data(), batch.size() * sizeof(OrthBatch), cudaMemcpyHostToDevice));
     OrthArgs &A = G.args;
-    A.batch = reinterpret_cast<OrthBatch *>(t + o_ba), A.steps = steps;
+    A.n_sym = (int)sym.size(), A.n_x = (int)xs.size(), A.steps = steps;
     A.mats = reinterpret_cast<OrthMat *>(t + o_mat);
     A.sym = reinterpret_cast<OrthTile *>(t + o_sym);
     A.x = reinterpret_cast<OrthTile *>(t + o_x);
-    A.chunk = reinterpret_cast<uint2 *>(t + o_ck), A.unit = reinterpret_cast<ConvertUnit *>(t + o_un);
+    A.chunk = reinterpret_cast<uint2 *>(t + o_ck), A.unit = reinterpret_cast<PanelUnit *>(t + o_un);
     A.done = reinterpret_cast<unsigned *>(t + o_done), A.ticket = reinterpret_cast<unsigned *>(t + o_tick);
     A.inv = reinterpret_cast<float *>(t + o_inv), A.partial = reinterpret_cast<float *>(t + o_part);
     A.out_type = h->out_type;
-    G.n_chunk = (int)chunk.size(), G.n_unit = (int)unit.size(), G.cg = cg;
-    G.grid = (widest < (size_t)pairs ? (int)widest : pairs) * cg;
+    G.n_chunk = (int)chunk.size(), G.n_unit = (int)unit.size(), G.mode = mode;
+    const int widest = A.n_sym > A.n_x ? A.n_sym : A.n_x;
+    G.grid = (widest < ctas ? widest : ctas) * cg;
     return CSER_OK;
 }
 
@@ -972,14 +994,17 @@ cser_orth_handle cser_orth_create(int32_t n_workers, int64_t ld, int32_t n_matri
             orth_fail(h, CSER_ERR_CUDA, "no CUDA device");
             return nullptr;
         }
-        int pairs[3] = {0, 0, 0};
-        cudaError_t er = h->split ? products_setup<1, true>(pairs[1]) : products_setup<1, false>(pairs[1]);
-        if (er == cudaSuccess) er = h->split ? products_setup<2, true>(pairs[2]) : products_setup<2, false>(pairs[2]);
-        if (er != cudaSuccess || pairs[1] < 1 || pairs[2] < 1) {
+        int fit_ctas[3] = {0, 0, 0};               // CTAs (pairs) of each mode that are resident together
+        cudaError_t er = h->split ? products_setup<kNarrow, true>(fit_ctas[kNarrow]) : products_setup<kNarrow, false>(fit_ctas[kNarrow]);
+        if (er == cudaSuccess)
+            er = h->split ? products_setup<kSingle, true>(fit_ctas[kSingle]) : products_setup<kSingle, false>(fit_ctas[kSingle]);
+        if (er == cudaSuccess)
+            er = h->split ? products_setup<kPaired, true>(fit_ctas[kPaired]) : products_setup<kPaired, false>(fit_ctas[kPaired]);
+        if (er != cudaSuccess || fit_ctas[kNarrow] < 1 || fit_ctas[kSingle] < 1 || fit_ctas[kPaired] < 1) {
             orth_fail(h, CSER_ERR_CUDA, er != cudaSuccess ? cudaGetErrorString(er) : "the kernel does not fit this GPU");
             return nullptr;
         }
-        const int cg = pairs_pay(all, h->split, pairs[2]) ? 2 : 1;
+        const int mode = choose_mode(all, h->split, fit_ctas[kPaired], fit_ctas[kSingle]), cg = mode_cg(mode);
         // Groups that fit the workspace, one after the other.
         std::vector<std::vector<HostMat>> parts;
         size_t most = 0, now = 0;
@@ -998,7 +1023,7 @@ cser_orth_handle cser_orth_create(int32_t n_workers, int64_t ld, int32_t n_matri
             const long long side = m.rows < m.cols ? m.rows : m.cols, longer = m.rows < m.cols ? m.cols : m.rows;
             // One CTA for a whole matrix pays where there are matrices for most SMs, or little to do: 33 x 1000 took 100 us alone,
             // against 54 by two kernels that spread it; 384 of 16 x 1024 took 48 against 120.
-            const bool pays = (int)small.size() >= pairs[2] || side * side * longer <= 1 << 19;
+            const bool pays = (int)small.size() >= fit_ctas[kPaired] || side * side * longer <= 1 << 19;
             (pays && resident_bytes((int)up(side, 8), longer) <= kResidentMost ? fit : rest).push_back(m);
         }
         if (er == cudaSuccess && !small.empty()) {
@@ -1015,6 +1040,11 @@ cser_orth_handle cser_orth_create(int32_t n_workers, int64_t ld, int32_t n_matri
             if (er == cudaSuccess) er = small_setup<__nv_bfloat16>(any);
             if (er == cudaSuccess) er = small_setup<__half>(any);
         }
+        if (!all.empty() && !small.empty()) {
+            if (er == cudaSuccess) er = cudaStreamCreateWithFlags(&h->side, cudaStreamNonBlocking);
+            if (er == cudaSuccess) er = cudaEventCreateWithFlags(&h->fork, cudaEventDisableTiming);
+            if (er == cudaSuccess) er = cudaEventCreateWithFlags(&h->join, cudaEventDisableTiming);
+        }
         if (er == cudaSuccess) er = cudaHostAlloc(reinterpret_cast<void **>(&h->err_host), 64, cudaHostAllocMapped | cudaHostAllocPortable);
         unsigned *err_dev = nullptr;
         if (er == cudaSuccess) *h->err_host = 0, er = cudaHostGetDevicePointer(reinterpret_cast<void **>(&err_dev), h->err_host, 0);
@@ -1025,7 +1055,7 @@ cser_orth_handle cser_orth_create(int32_t n_workers, int64_t ld, int32_t n_matri
         h->groups.resize(parts.size());
         for (size_t g = 0; g < parts.size(); ++g) {
             cser_orth::Group &G = h->groups[g];
-            if (build_group(h, G, parts[g], cg, steps, pairs[cg]) != CSER_OK) {
+            if (build_group(h, G, parts[g], mode, steps, fit_ctas[mode]) != CSER_OK) {
                 cser_orth_destroy(h);
                 return nullptr;
             }
@@ -1059,13 +1089,19 @@ int cser_orth_apply(cser_orth_handle h, const void *grad, float *m, float mu, vo
     if (m && (static_cast<const void *>(m) == grad || static_cast<const void *>(m) == out))
         return cser_internal_fail(CSER_ERR_INVALID, "cser_orth_apply: m must be an array of its own");
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const bool both = !h->groups.empty() && (h->resident.tables || h->small.tables);
+    cudaStream_t small_st = both ? h->side : st;
+    if (both) {
+        TRY(cudaEventRecord(h->fork, st));
+        TRY(cudaStreamWaitEvent(small_st, h->fork, 0));
+    }
     for (const cser_orth::Small *S : {&h->resident, &h->small}) {
         if (!S->tables) continue;
         SmallArgs a = S->args;
         a.grad = grad, a.m = m, a.mu = mu, a.out = out;
-        if (h->in_type == CSER_TYPE_F32) small_launch<float>(*S, a, st);
-        else if (h->in_type == CSER_TYPE_BF16) small_launch<__nv_bfloat16>(*S, a, st);
-        else small_launch<__half>(*S, a, st);
+        if (h->in_type == CSER_TYPE_F32) small_launch<float>(*S, a, small_st);
+        else if (h->in_type == CSER_TYPE_BF16) small_launch<__nv_bfloat16>(*S, a, small_st);
+        else small_launch<__half>(*S, a, small_st);
         TRY(cudaGetLastError());
         h->launches += S->n_resident ? 1 : 2;
     }
@@ -1076,16 +1112,25 @@ int cser_orth_apply(cser_orth_handle h, const void *grad, float *m, float mu, vo
         else if (h->in_type == CSER_TYPE_BF16) prologue_launch<__nv_bfloat16>(G, a, st);
         else prologue_launch<__half>(G, a, st);
         TRY(cudaGetLastError());
-        cudaError_t e = G.cg == 1 ? (h->split ? products_launch<1, true>(a, G.grid, st) : products_launch<1, false>(a, G.grid, st))
-                                  : (h->split ? products_launch<2, true>(a, G.grid, st) : products_launch<2, false>(a, G.grid, st));
+        cudaError_t e;
+        if (G.mode == kNarrow) e = h->split ? products_launch<kNarrow, true>(a, G.grid, st) : products_launch<kNarrow, false>(a, G.grid, st);
+        else if (G.mode == kSingle) e = h->split ? products_launch<kSingle, true>(a, G.grid, st) : products_launch<kSingle, false>(a, G.grid, st);
+        else e = h->split ? products_launch<kPaired, true>(a, G.grid, st) : products_launch<kPaired, false>(a, G.grid, st);
         TRY(e);
         h->launches += 3;
+    }
+    if (both) {
+        TRY(cudaEventRecord(h->join, small_st));
+        TRY(cudaStreamWaitEvent(st, h->join, 0));
     }
     return CSER_OK;
 }
 
 void cser_orth_destroy(cser_orth_handle h) {
     if (!h) return;
+    if (h->side) cudaStreamSynchronize(h->side), cudaStreamDestroy(h->side);
+    if (h->fork) cudaEventDestroy(h->fork);
+    if (h->join) cudaEventDestroy(h->join);
     for (cser_orth::Group &G : h->groups)
         if (G.tables) cudaFree(G.tables);
     if (h->small.tables) cudaFree(h->small.tables);

@@ -79,15 +79,15 @@ class Orthogonalizer:
     def apply(self, grad, out=None, momentum=None, mu=0.0, stream=None):
         """grad [n, ld] -> out [n, ld] (made if not given: zeros outside the matrices); momentum is updated in place."""
         size = (self.n, self.ld)
-        _want(grad.is_cuda and grad.dtype == self.in_dtype and grad.shape == size and grad.is_contiguous(),
-              f"Orthogonalizer: grad must be a contiguous CUDA {self.in_dtype} tensor of shape {size}")
+        if not (grad.is_cuda and grad.dtype == self.in_dtype and grad.shape == size and grad.is_contiguous()):
+            raise CSERError(f"Orthogonalizer: grad must be a contiguous CUDA {self.in_dtype} tensor of shape {size}")
         if out is None:
             out = torch.zeros(size, dtype=self.out_dtype, device=grad.device)
-        _want(out.is_cuda and out.dtype == self.out_dtype and out.shape == size and out.is_contiguous(),
-              f"Orthogonalizer: out must be a contiguous CUDA {self.out_dtype} tensor of shape {size}")
-        if momentum is not None:
-            _want(momentum.is_cuda and momentum.dtype == torch.float32 and momentum.shape == size and
-                  momentum.is_contiguous(), f"Orthogonalizer: momentum must be a contiguous CUDA float32 tensor of shape {size}")
+        if not (out.is_cuda and out.dtype == self.out_dtype and out.shape == size and out.is_contiguous()):
+            raise CSERError(f"Orthogonalizer: out must be a contiguous CUDA {self.out_dtype} tensor of shape {size}")
+        if momentum is not None and not (momentum.is_cuda and momentum.dtype == torch.float32 and momentum.shape == size and
+                                         momentum.is_contiguous()):
+            raise CSERError(f"Orthogonalizer: momentum must be a contiguous CUDA float32 tensor of shape {size}")
         _check(_lib.cser_orth_apply(self.h, grad.data_ptr(), None if momentum is None else momentum.data_ptr(), mu,
                                     out.data_ptr(), _stream(stream)), "cser_orth_apply")
         return out
@@ -128,44 +128,47 @@ class LinearCrossEntropy:
         self.h = ctypes.c_void_p(h)
 
     def _inputs(self, hidden, weight, target, ignore_index):
-        t = target.shape[1] if target.dim() == 2 else -1
-        for name, a, shape in (("hidden", hidden, (self.n, t, self.dim)), ("weight", weight, (self.n, self.vocab, self.dim))):
-            _want(a.is_cuda and a.dtype == self.dtype and a.shape == shape and (a.stride(2) == 1 or self.dim == 1) and
-                  min(a.stride()) >= 0, f"LinearCrossEntropy: {name} must be a CUDA {self.dtype} tensor of shape {shape} "
-                  "with a contiguous last dimension")
-        _want(target.is_cuda and target.dtype == torch.int64 and target.shape == (self.n, t) and target.is_contiguous() and
-              0 <= t <= self.max_tokens, f"LinearCrossEntropy: target must be a contiguous CUDA int64 tensor "
-              f"[{self.n}, at most {self.max_tokens}]")
-        return _XentInputs(hidden.data_ptr(), hidden.stride(1), hidden.stride(0), weight.data_ptr(), weight.stride(1),
-                           weight.stride(0), target.data_ptr(), ignore_index, t)
+        n, dim = self.n, self.dim
+        if not (target.is_cuda and target.dtype == torch.int64 and target.dim() == 2 and target.shape[0] == n and
+                target.shape[1] <= self.max_tokens and target.is_contiguous()):
+            raise CSERError(f"LinearCrossEntropy: target must be a contiguous CUDA int64 tensor [{n}, at most {self.max_tokens}]")
+        t = target.shape[1]
+        hs, ws = hidden.stride(), weight.stride()
+        if not (hidden.is_cuda and hidden.dtype == self.dtype and hidden.shape == (n, t, dim) and (hs[2] == 1 or dim == 1)):
+            raise CSERError(f"LinearCrossEntropy: hidden must be a CUDA {self.dtype} tensor of shape {(n, t, dim)} with a contiguous "
+                            "last dimension")
+        if not (weight.is_cuda and weight.dtype == self.dtype and weight.shape == (n, self.vocab, dim) and (ws[2] == 1 or dim == 1)):
+            raise CSERError(f"LinearCrossEntropy: weight must be a CUDA {self.dtype} tensor of shape {(n, self.vocab, dim)} with a "
+                            "contiguous last dimension")
+        return _XentInputs(hidden.data_ptr(), hs[1], hs[0], weight.data_ptr(), ws[1], ws[0], target.data_ptr(), ignore_index, t)
 
     def loss(self, hidden, weight, target, ignore_index=-100, stream=None):
         """(loss, lse), each fp32 [n, tokens]; lse is what grad takes."""
         args = self._inputs(hidden, weight, target, ignore_index)
         both = torch.empty((2, *target.shape), dtype=torch.float32, device=target.device)
-        _check(_lib.cser_xent_loss(self.h, ctypes.byref(args), both[0].data_ptr(), both[1].data_ptr(), _stream(stream)),
-               "cser_xent_loss")
-        return both[0], both[1]
+        loss, lse = both.unbind(0)
+        _check(_lib.cser_xent_loss(self.h, ctypes.byref(args), loss.data_ptr(), lse.data_ptr(), _stream(stream)), "cser_xent_loss")
+        return loss, lse
 
     def grad(self, hidden, weight, target, lse, dloss, ignore_index=-100, dhidden=None, dweight=None, need_dhidden=True,
              need_dweight=True, stream=None):
         """(dhidden, dweight) of sum(dloss * loss); dweight may be a [n, vocab, dim] view of a larger [n, d] array."""
         args = self._inputs(hidden, weight, target, ignore_index)
-        for name, a in (("lse", lse), ("dloss", dloss)):
-            _want(a.is_cuda and a.dtype == torch.float32 and a.shape == target.shape and a.is_contiguous(),
-                  f"LinearCrossEntropy: {name} must be a contiguous CUDA float32 tensor of target's shape")
+        for a in (lse, dloss):
+            if not (a.is_cuda and a.dtype == torch.float32 and a.shape == target.shape and a.is_contiguous()):
+                raise CSERError("LinearCrossEntropy: lse and dloss must be contiguous CUDA float32 tensors of target's shape")
         if need_dhidden:
             if dhidden is None:
                 dhidden = torch.empty(hidden.shape, dtype=self.dtype, device=hidden.device)
-            _want(dhidden.is_cuda and dhidden.dtype == self.dtype and dhidden.shape == hidden.shape and dhidden.is_contiguous(),
-                  f"LinearCrossEntropy: dhidden must be a contiguous CUDA {self.dtype} tensor of hidden's shape")
+            elif not (dhidden.is_cuda and dhidden.dtype == self.dtype and dhidden.shape == hidden.shape and dhidden.is_contiguous()):
+                raise CSERError(f"LinearCrossEntropy: dhidden must be a contiguous CUDA {self.dtype} tensor of hidden's shape")
         if need_dweight:
             if dweight is None:
                 dweight = torch.empty(weight.shape, dtype=self.dtype, device=weight.device)
-            _want(dweight.is_cuda and dweight.dtype == self.dtype and dweight.shape == weight.shape and
-                  (self.dim == 1 or dweight.stride(2) == 1) and (self.vocab == 1 or dweight.stride(1) == self.dim) and
-                  (self.n == 1 or dweight.stride(0) >= self.vocab * self.dim),
-                  f"LinearCrossEntropy: dweight must be a CUDA {self.dtype} tensor of weight's shape, dense for each worker")
+            elif not (dweight.is_cuda and dweight.dtype == self.dtype and dweight.shape == weight.shape and
+                      (self.dim == 1 or dweight.stride(2) == 1) and (self.vocab == 1 or dweight.stride(1) == self.dim) and
+                      (self.n == 1 or dweight.stride(0) >= self.vocab * self.dim)):
+                raise CSERError(f"LinearCrossEntropy: dweight must be a CUDA {self.dtype} tensor of weight's shape, dense for each worker")
         _check(_lib.cser_xent_grad(self.h, ctypes.byref(args), lse.data_ptr(), dloss.data_ptr(),
                                    dhidden.data_ptr() if need_dhidden else None,
                                    dweight.data_ptr() if need_dweight else None,

@@ -193,6 +193,22 @@ def test_results_do_not_depend_on_what_else_the_plan_holds():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("out_t", [BF, F32], ids=str)
+@pytest.mark.parametrize("shapes", [[(500, 1000), (1000, 500)] * 7, [(130, 200), (200, 130)] * 20, [(129, 65)] * 3], ids=lambda s: f"{len(s)}")
+def test_plans_of_different_sizes(shapes, out_t):
+    """Many large matrices, many small ones, few: tiles are cut differently."""
+    gen, mats, at = generator(8), [], 0
+    for r, c in shapes:
+        mats.append((at, r, c))
+        at += r * c
+    u = torch.cat([matrix(gen, r, c).reshape(-1) for r, c in shapes] * 2).reshape(2, -1)
+    got = train.Orthogonalizer(mats, 2, at, F32, out_t).apply(u)
+    for o, r, c in mats:
+        for i in range(2):
+            assert far(got[i, o:o + r * c].view(r, c), exact(u[i, o:o + r * c].view(r, c))) < OUT[out_t], (r, c)
+
+
+@pytest.mark.gpu
 def test_refusals():
     ok = dict(matrices=[(0, 4, 5)], n_workers=1, ld=20)
     train.Orthogonalizer(**ok)
