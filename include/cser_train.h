@@ -96,8 +96,8 @@ typedef struct cser_xent_inputs {
  * Workspace for up to max_tokens tokens per worker.  piece: vocabulary entries per piece of the gradient (rounded up to
  * a multiple of 256), 0 = chosen so that a piece of dz takes at most 256 MB.  1 <= vocab <= 2^24, 1 <= dim <= 65536,
  * 1 <= n_workers * max_tokens <= 2^24, n_workers * vocab and n_workers * ceil(max_tokens / 128) * ceil(vocab / 256) at most 2^30.
- * hidden or weights whose rows are not 16 bytes apart (or not 16-byte aligned) are first copied: the buffer for that is
- * allocated on the first such call, which must not be under stream capture.  Returns NULL on failure.
+ * hidden or weights whose rows are not a multiple of 16 bytes apart (or not 16-byte aligned) are first copied: the buffer for that is
+ * allocated with the handle where dim is no multiple of 8, else on the first such call, which must not be under stream capture.  Returns NULL on failure.
  */
 cser_xent_handle cser_xent_create(int32_t n_workers, int64_t max_tokens, int64_t vocab, int64_t dim, int32_t type,
                                   int64_t piece);

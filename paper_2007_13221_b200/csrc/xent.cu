@@ -33,6 +33,10 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLowest = -1e30f;                  // below every logit, and finite times log2(e)
 constexpr size_t kPieceBytes = 256ull << 20;
+// The tensor cores truncate every partial sum: 1.2e-6 of a logit over an inner dimension of 1024 (2.5e-6 of a small loss), 3e-6
+// over 4096.  Above 256 the loss's accumulators are taken out and added up, rounded, after this many stages (an inner dimension of 256).
+constexpr int kLossChunk = 4;
+constexpr int kJoinRows = kThreads / 32;           // rows that the last CTA joins itself, one per warp
 
 // 2^x, flushing: the instruction.
 __device__ __forceinline__ float exp2_fast(float x) {
@@ -55,6 +59,7 @@ struct XentArgs {
     const int64_t *target;
     int64_t ignore;
     float *loss, *lse_out;
+    unsigned *ticket;                              // of the CTAs of a loss whose last one joins the parts
     // gradient
     const float *lse, *dloss;
     float *ratio;                                  // [n * tokens] dloss relative to the largest, times the type's scale
@@ -69,8 +74,11 @@ struct XentArgs {
 };
 
 // ------------------------------------------------------------------ logits, tile by tile
-template <int CG, bool GRAD>
+// What the tiles of z are for: a loss, a loss over a long inner dimension (chunks), dz.
+enum { kLoss = 0, kLongLoss = 1, kGrad = 2 };
+template <int CG, int WHAT>
 struct LogitsJob {
+    static constexpr bool GRAD = WHAT == kGrad, LONG = WHAT == kLongLoss;
     const XentArgs &a;
     int first, every, vocab_tiles;
     static constexpr bool kCopier = false;
@@ -87,7 +95,9 @@ struct LogitsJob {
         t.n = 256, t.stages = (a.dim + 63) / 64, t.a_lim = t.b_lim = t.stages;
     }
     __device__ __forceinline__ bool ready(Pipe<CG> &, const Tile &) const { return true; }
-    __device__ __forceinline__ bool chunk_ends(const Tile &t, int k) const { return k + 1 == t.stages; }
+    __device__ __forceinline__ bool chunk_ends(const Tile &t, int k) const {
+        return k + 1 == t.stages || (LONG && (k + 1) % kLossChunk == 0);
+    }
     __device__ __forceinline__ int bf16() const { return a.bf16; }
     struct Loader {
         const CUtensorMap *h, *w;
@@ -115,32 +125,50 @@ struct LogitsJob {
         }
         uint32_t tmem;
         if constexpr (!GRAD) {
-            if (!p.take(turn, tmem)) return false;
+            float v[LONG ? 2 : 1][32];                               // all 64 columns, or 32 at a time
+            const int chunks = LONG ? (t.stages + kLossChunk - 1) / kLossChunk : 1;
+            for (int c = 0; c < chunks; ++c) {
+                if (!p.take(turn, tmem)) return false;
+                if (!LONG) break;
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    float x[16];
+                    tmem_load(tmem + c0 + b * 16, x);
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) {
+                        float &sum = v[LONG ? b / 2 : 0][b % 2 * 16 + k];
+                        sum = __fadd_rn(c ? sum : 0.f, x[k]);
+                    }
+                }
+                p.release(turn, lane);
+            }
             float m = kLowest, s = 0.f;
-#pragma unroll 1
+#pragma unroll(LONG ? 2 : 1)
             for (int b = 0; b < 64; b += 32) {
                 const int col = t.j * 256 + c0 + b;
-                float v[32];
-                tmem_load(tmem + c0 + b, v);
-                if (b == 32) p.release(turn, lane);
+                float(&z)[32] = v[LONG ? b / 32 : 0];
+                if (!LONG) {
+                    tmem_load(tmem + c0 + b, z);
+                    if (b == 32) p.release(turn, lane);
+                }
                 if (col + 32 > a.vocab) {
 #pragma unroll
                     for (int k = 0; k < 32; ++k)
-                        if (col + k >= a.vocab) v[k] = -INFINITY;
+                        if (col + k >= a.vocab) z[k] = -INFINITY;
                 }
                 float top = m;
 #pragma unroll
-                for (int k = 0; k < 32; ++k) top = fmaxf(top, v[k]);
-                float sum[4] = {0.f, 0.f, 0.f, 0.f};
+                for (int k = 0; k < 32; ++k) top = fmaxf(top, z[k]);
+                float e[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int k = 0; k < 32; ++k) sum[k % 4] += exp2_fast((v[k] - top) * kLog2e);
-                s = __fmaf_rn(s, exp2_fast((m - top) * kLog2e), (sum[0] + sum[1]) + (sum[2] + sum[3]));
+                for (int k = 0; k < 32; ++k) e[k % 4] += exp2_fast((z[k] - top) * kLog2e);
+                s = __fmaf_rn(s, exp2_fast((m - top) * kLog2e), (e[0] + e[1]) + (e[2] + e[3]));
                 m = top;
                 const unsigned off = (unsigned)(target - col);
                 if (off < 32u) {
 #pragma unroll
                     for (int k = 0; k < 32; ++k)
-                        if (off == (unsigned)k) a.z_target[at] = v[k];
+                        if (off == (unsigned)k) a.z_target[at] = z[k];
                 }
             }
             if (live) a.part[(size_t)(t.j * 4 + warp / 4) * a.n * a.tokens + at] = make_float2(m, s);
@@ -184,15 +212,10 @@ struct LogitsJob {
     }
 };
 
-template <int CG, bool GRAD>
-__global__ void __launch_bounds__(kThreads, 1) xent_logits_kernel(const __grid_constant__ XentArgs a) {
-    extern __shared__ unsigned char raw[];
-    if (threadIdx.x == 0) prefetch_tensor_map(&a.h), prefetch_tensor_map(&a.w);
-    Pipe<CG> p;
-    p.template setup<LogitsJob<CG, GRAD>>(raw, a.err);
-    LogitsJob<CG, GRAD> job{a, (int)blockIdx.x / CG, (int)gridDim.x / CG, (a.piece_n + 255) / 256};
-    p.run(job);
-    p.teardown();
+__device__ __forceinline__ void row_loss(const XentArgs &a, size_t at, float lse) {
+    const int64_t y = a.target[at];
+    a.lse_out[at] = lse;
+    if (a.loss) a.loss[at] = y == a.ignore ? 0.f : y >= 0 && y < a.vocab ? lse - __ldcg(a.z_target + at) : NAN;
 }
 
 // The parts of 32 rows joined by 32 warps: a lane takes a row, a warp every 32nd part, four of them at a time.
@@ -221,10 +244,47 @@ __global__ void __launch_bounds__(1024) xent_join_kernel(const __grid_constant__
             s = s * exp2_fast((m - top) * kLog2e) + q.y * exp2_fast((q.x - top) * kLog2e);
             m = top;
         }
-        const float lse = m + logf(s);
-        const int64_t y = a.target[at];
-        a.lse_out[at] = lse;
-        if (a.loss) a.loss[at] = y == a.ignore ? 0.f : y >= 0 && y < a.vocab ? lse - a.z_target[at] : NAN;
+        row_loss(a, at, m + logf(s));
+    }
+}
+
+template <int CG, int WHAT>
+__global__ void __launch_bounds__(kThreads, 1) xent_logits_kernel(const __grid_constant__ XentArgs a) {
+    extern __shared__ unsigned char raw[];
+    if (threadIdx.x == 0) prefetch_tensor_map(&a.h), prefetch_tensor_map(&a.w);
+    Pipe<CG> p;
+    p.template setup<LogitsJob<CG, WHAT>>(raw, a.err);
+    LogitsJob<CG, WHAT> job{a, (int)blockIdx.x / CG, (int)gridDim.x / CG, (a.piece_n + 255) / 256};
+    p.run(job);
+    p.teardown();
+    if constexpr (WHAT != kGrad) {
+        // Few rows: the last CTA to finish joins their parts, a warp each (a kernel of its own: 5 us after 14).
+        if (a.n * a.tokens > kJoinRows) return;
+        __shared__ bool last;
+        if (threadIdx.x == 0) {
+            __threadfence();
+            last = atomicAdd(a.ticket, 1u) == gridDim.x - 1;
+            __threadfence();
+            if (last) *a.ticket = 0;                                 // for the next call
+        }
+        __syncthreads();
+        const int row = threadIdx.x / 32, lane = threadIdx.x % 32, rows = a.n * a.tokens;
+        if (!last || row >= rows) return;
+        float m = kLowest, s = 0.f;
+#pragma unroll 4
+        for (int k = lane; k < a.parts; k += 32) {
+            const float2 q = __ldcg(a.part + (size_t)k * rows + row);
+            const float top = fmaxf(m, q.x);
+            s = s * exp2_fast((m - top) * kLog2e) + q.y * exp2_fast((q.x - top) * kLog2e);
+            m = top;
+        }
+        for (int k = 16; k; k >>= 1) {
+            const float qm = __shfl_xor_sync(~0u, m, k), qs = __shfl_xor_sync(~0u, s, k);
+            const float top = fmaxf(m, qm);
+            s = s * exp2_fast((m - top) * kLog2e) + qs * exp2_fast((qm - top) * kLog2e);
+            m = top;
+        }
+        if (lane == 0) row_loss(a, row, m + logf(s));
     }
 }
 
@@ -441,12 +501,19 @@ __global__ void __launch_bounds__(256) xent_join_dh_kernel(const __grid_constant
     }
 }
 
-// Rows that no tensor copy can start at, as rows padded to a multiple of 8.
-__global__ void __launch_bounds__(256) xent_pack_kernel(const uint16_t *src, long long row_stride, long long worker_stride, int rows,
-                                                        int dim, int padded, uint16_t *dst) {
-    const long long row = blockIdx.x;
-    const uint16_t *s = src + (row / rows) * worker_stride + (row % rows) * row_stride;
-    uint16_t *d = dst + row * padded;
+// Rows that no tensor copy can start at, as rows padded to a multiple of 8; of up to two arrays.
+struct PackSource {
+    const uint16_t *src;
+    long long row_stride, worker_stride;
+    int rows, all;                                 // of a worker, of all
+    uint16_t *dst;
+};
+__global__ void __launch_bounds__(256) xent_pack_kernel(const PackSource x, const PackSource y, int dim, int padded) {
+    const bool second = (int)blockIdx.x >= x.all;
+    const PackSource &p = second ? y : x;
+    const long long row = (int)blockIdx.x - (second ? x.all : 0);
+    const uint16_t *s = p.src + (row / p.rows) * p.worker_stride + (row % p.rows) * p.row_stride;
+    uint16_t *d = p.dst + row * padded;
     for (int c = threadIdx.x; c < padded; c += 256) d[c] = c < dim ? s[c] : 0;
 }
 
@@ -472,6 +539,7 @@ struct cser_xent {
     void *work = nullptr;
     float2 *part = nullptr;
     float *z_target = nullptr, *ratio = nullptr, *unscale = nullptr, *acc = nullptr;
+    unsigned *ticket = nullptr;
     char *dz = nullptr;
     void *pack_h = nullptr, *pack_w = nullptr;     // made on the first call that needs them
     encode_fn encode = nullptr;
@@ -505,9 +573,9 @@ bool tensor_map(const cser_xent *h, CUtensorMap &m, const void *p, long long row
                      CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// The map of an operand, of a packed copy where its rows cannot be read in place.
+// The map of an operand, of a packed copy (then `job` says of what) where its rows cannot be read in place.
 int operand(cser_xent *h, CUtensorMap &m, int &workers, const void *p, long long rows, long long row_stride, long long worker_stride,
-            void *&pack, long long pack_rows, const char *what, cudaStream_t st) {
+            void *&pack, long long pack_rows, PackSource &job, const char *what, cudaStream_t st) {
     workers = h->n == 1 || worker_stride == 0 ? 1 : h->n;
     if (rows == 1) row_stride = up(h->dim, 8);                      // no second row: its distance says nothing
     const bool direct = (uintptr_t)p % 16 == 0 && row_stride % 8 == 0 && row_stride > 0 && (workers == 1 || worker_stride % 8 == 0);
@@ -520,10 +588,7 @@ int operand(cser_xent *h, CUtensorMap &m, int &workers, const void *p, long long
                 return cser_internal_fail(CSER_ERR_INVALID, "%s needs a packing buffer: make the first such call outside a capture", what);
             TRY(cudaMalloc(&pack, (size_t)h->n * pack_rows * padded * 2));
         }
-        xent_pack_kernel<<<(unsigned)(workers * rows), 256, 0, st>>>(static_cast<const uint16_t *>(p), row_stride, worker_stride, (int)rows,
-                                                                     (int)h->dim, (int)padded, static_cast<uint16_t *>(pack));
-        TRY(cudaGetLastError());
-        h->launches++;
+        job = {static_cast<const uint16_t *>(p), row_stride, worker_stride, (int)rows, (int)(workers * rows), static_cast<uint16_t *>(pack)};
         p = pack, row_stride = padded, worker_stride = padded * rows;
     }
     if (!tensor_map(h, m, p, rows, row_stride, worker_stride, workers, h->dim))
@@ -552,16 +617,22 @@ int prepare_call(cser_xent *h, const cser_xent_inputs *in, const char *what, Xen
     if (int rc = cser_internal_check_ptr(in->target, "target")) return rc;
     if ((uintptr_t)in->hidden % 2 || (uintptr_t)in->weight % 2 || (uintptr_t)in->target % 8)
         return cser_internal_fail(CSER_ERR_INVALID, "%s: a pointer is not aligned to its element type", what);
+    PackSource pack[2] = {};
     if (int rc = operand(h, a.h, a.h_workers, in->hidden, in->tokens, in->hidden_row_stride, in->hidden_worker_stride, h->pack_h,
-                         h->max_tokens, "hidden", st))
+                         h->max_tokens, pack[0], "hidden", st))
         return rc;
     if (int rc = operand(h, a.w, a.w_workers, in->weight, h->vocab, in->weight_row_stride, in->weight_worker_stride, h->pack_w, h->vocab,
-                         "weight", st))
+                         pack[1], "weight", st))
         return rc;
+    if (pack[0].all + pack[1].all) {
+        xent_pack_kernel<<<(unsigned)(pack[0].all + pack[1].all), 256, 0, st>>>(pack[0], pack[1], (int)h->dim, (int)up(h->dim, 8));
+        TRY(cudaGetLastError());
+        h->launches++;
+    }
     a.bf16 = h->type == CSER_TYPE_BF16;
     a.tp = h->tp, a.part = h->part, a.parts = h->parts, a.z_target = h->z_target, a.target = in->target, a.ignore = in->ignore_index;
     a.ratio = h->ratio, a.unscale = h->unscale, a.dz = h->dz, a.dz_worker = (size_t)(h->piece / 64) * h->tp * 128;
-    a.acc = h->acc, a.acc_rows = (int)up(a.tokens, 256), a.acc_cols = h->acc_cols, a.err = h->err_dev;
+    a.ticket = h->ticket, a.acc = h->acc, a.acc_rows = (int)up(a.tokens, 256), a.acc_cols = h->acc_cols, a.err = h->err_dev;
     return CSER_OK;
 }
 
@@ -585,8 +656,9 @@ cudaError_t tiles_launch(cser_xent *h, K kernel, size_t shared, long long tiles,
 template <int CG>
 cudaError_t kernels_setup() {
     const int b = (int)Pipe<CG>::kSharedBytes;
-    cudaError_t e = cudaFuncSetAttribute(xent_logits_kernel<CG, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, b);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(xent_logits_kernel<CG, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, b);
+    cudaError_t e = cudaFuncSetAttribute(xent_logits_kernel<CG, kLoss>, cudaFuncAttributeMaxDynamicSharedMemorySize, b);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(xent_logits_kernel<CG, kLongLoss>, cudaFuncAttributeMaxDynamicSharedMemorySize, b);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(xent_logits_kernel<CG, kGrad>, cudaFuncAttributeMaxDynamicSharedMemorySize, b);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(xent_grad_kernel<CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)GradPipe<CG>::kSharedBytes);
     return e;
 }
@@ -594,10 +666,13 @@ cudaError_t kernels_setup() {
 template <int CG>
 int loss_launch(cser_xent *h, XentArgs &a, cudaStream_t st) {
     a.token_tiles = (int)(up(a.tokens, 128 * CG) / (128 * CG)), a.piece0 = 0, a.piece_n = a.vocab;
-    TRY((tiles_launch<CG>(h, xent_logits_kernel<CG, false>, Pipe<CG>::kSharedBytes, (long long)a.n * a.token_tiles * ((a.vocab + 255) / 256), st, a)));
-    xent_join_kernel<<<(unsigned)(((long long)a.n * a.tokens + 31) / 32), 1024, 0, st>>>(a);
-    TRY(cudaGetLastError());
-    h->launches++;
+    const auto kernel = a.dim > kLossChunk * kStageK ? xent_logits_kernel<CG, kLongLoss> : xent_logits_kernel<CG, kLoss>;
+    TRY((tiles_launch<CG>(h, kernel, Pipe<CG>::kSharedBytes, (long long)a.n * a.token_tiles * ((a.vocab + 255) / 256), st, a)));
+    if ((long long)a.n * a.tokens > kJoinRows) {
+        xent_join_kernel<<<(unsigned)(((long long)a.n * a.tokens + 31) / 32), 1024, 0, st>>>(a);
+        TRY(cudaGetLastError());
+        h->launches++;
+    }
     return CSER_OK;
 }
 
@@ -613,7 +688,7 @@ int grad_launch(cser_xent *h, XentArgs &a, cudaStream_t st) {
         a.piece0 = (int)v, a.piece_n = (int)(h->vocab - v < h->piece ? h->vocab - v : h->piece);
         a.first_piece = v == 0, a.last_piece = v + h->piece >= h->vocab;
         const long long vt = up(a.piece_n, 128 * CG) / (128 * CG);
-        TRY((tiles_launch<CG>(h, xent_logits_kernel<CG, true>, Pipe<CG>::kSharedBytes, (long long)a.n * a.token_tiles * ((a.piece_n + 255) / 256), st, a)));
+        TRY((tiles_launch<CG>(h, xent_logits_kernel<CG, kGrad>, Pipe<CG>::kSharedBytes, (long long)a.n * a.token_tiles * ((a.piece_n + 255) / 256), st, a)));
         const long long n_dh = a.dh ? (long long)a.n * a.token_tiles * a.splits * dim_tiles : 0, n_dw = a.dw ? a.n * vt * dim_tiles : 0;
         TRY((tiles_launch<CG>(h, xent_grad_kernel<CG>, GradPipe<CG>::kSharedBytes, n_dh + n_dw, st, a, (int)n_dh, (int)n_dw)));
     }
@@ -672,13 +747,20 @@ cser_xent_handle cser_xent_create(int32_t n_workers, int64_t max_tokens, int64_t
     size_t at = 0;
     auto place = [&](size_t b) { const size_t p = at; at += (b + 1023) / 1024 * 1024; return p; };
     const size_t o_part = place((size_t)rows * h->parts * 8), o_zt = place((size_t)rows * 4), o_ratio = place((size_t)rows * 4),
-                 o_un = place((size_t)n_workers * 4), o_dz = place((size_t)n_workers * (h->piece / 64) * h->tp * 128),
+                 o_un = place((size_t)n_workers * 4), o_tick = place(4), o_dz = place((size_t)n_workers * (h->piece / 64) * h->tp * 128),
                  o_acc = place((size_t)n_workers * acc_rows * h->acc_cols * 4);
     e = cudaMalloc(&h->work, at);
+    if (dim % 8) {                                 // dense rows of this length need packing
+        if (e == cudaSuccess) e = cudaMalloc(&h->pack_h, (size_t)rows * up(dim, 8) * 2);
+        if (e == cudaSuccess) e = cudaMalloc(&h->pack_w, (size_t)n_workers * vocab * up(dim, 8) * 2);
+    }
     if (e == cudaSuccess) e = cudaHostAlloc(reinterpret_cast<void **>(&h->err_host), 64, cudaHostAllocMapped | cudaHostAllocPortable);
     if (e == cudaSuccess) *h->err_host = 0, e = cudaHostGetDevicePointer(reinterpret_cast<void **>(&h->err_dev), h->err_host, 0);
     if (e != cudaSuccess) return drop(e);
     char *w = static_cast<char *>(h->work);
+    h->ticket = reinterpret_cast<unsigned *>(w + o_tick);
+    e = cudaMemset(h->ticket, 0, 4);
+    if (e != cudaSuccess) return drop(e);
     h->part = reinterpret_cast<float2 *>(w + o_part), h->z_target = reinterpret_cast<float *>(w + o_zt);
     h->ratio = reinterpret_cast<float *>(w + o_ratio), h->unscale = reinterpret_cast<float *>(w + o_un);
     h->dz = w + o_dz, h->acc = reinterpret_cast<float *>(w + o_acc);

@@ -266,6 +266,17 @@ def test_many_tiles(size):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("size", [(1, 40, 700, 2112), (1, 150, 520, 4104), (1, 3, 1000, 8192)], ids=str)
+def test_long_inner_dimensions(size):
+    """Losses as exact as for short ones: 2e-6 of 1 + |lse| whatever the dimension (partial sums taken out of the tensor cores)."""
+    n, t, v, d = size
+    h, w, y, dloss = inputs(n, t, v, d, BF)
+    loss, lse, _, _ = check(train.LinearCrossEntropy(n, t, v, d, BF), h, w, y, dloss, BF)
+    e_loss, e_lse = exact(h, w, y, dloss)[:2]
+    assert bool(((lse.double() - e_lse).abs() <= 2e-6 * (1 + e_lse.abs())).all())
+
+
+@pytest.mark.gpu
 def test_refusals():
     ok = dict(n_workers=2, max_tokens=8, vocab=30, dim=16, dtype=BF)
     op = train.LinearCrossEntropy(**ok)
