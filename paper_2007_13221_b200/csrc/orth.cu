@@ -296,12 +296,14 @@ template <typename T>
 __global__ void __launch_bounds__(256) orth_norm_kernel(const OrthArgs a) {
     __shared__ float red[8];
     __shared__ int last;
+    let_next_start();
     const uint2 c = a.chunk[blockIdx.x];
     norm_chunk<T>(a, c.x, c.y, red, last);
 }
 template <typename T>
 __global__ void __launch_bounds__(256) orth_convert_kernel(const OrthArgs a) {
     const PanelUnit u = a.unit[blockIdx.x];
+    earlier_done();
     make_panels<T>(a, u.q, (int)u.r0, (int)u.c0);
 }
 
@@ -943,20 +945,20 @@ cudaError_t small_setup(const cser_orth::Small &S) {
     return e;
 }
 template <typename T>
-void small_launch(const cser_orth::Small &S, const SmallArgs &a, cudaStream_t st) {
+cudaError_t small_launch(const cser_orth::Small &S, const SmallArgs &a, cudaStream_t st) {
     if (S.n_resident) {
-        if (S.side <= 32) orth_resident_kernel<T, 4><<<S.n_resident, 256, S.resident_shared, st>>>(a);
-        else orth_resident_kernel<T, 8><<<S.n_resident, 256, S.resident_shared, st>>>(a);
-    } else {
-        orth_gram_kernel<T><<<S.n_part, 256, S.gram_shared, st>>>(a);
-        orth_apply_kernel<T><<<S.n_piece, 256, S.apply_shared, st>>>(a);
+        return launch_kernel(S.side <= 32 ? orth_resident_kernel<T, 4> : orth_resident_kernel<T, 8>, (unsigned)S.n_resident, 256, S.resident_shared,
+                             1, false, st, a);
     }
+    cudaError_t e = launch_kernel(orth_gram_kernel<T>, (unsigned)S.n_part, 256, S.gram_shared, 1, false, st, a);
+    return e == cudaSuccess ? launch_kernel(orth_apply_kernel<T>, (unsigned)S.n_piece, 256, S.apply_shared, 1, true, st, a) : e;
 }
 
 template <typename T>
-void prologue_launch(const cser_orth::Group &G, const OrthArgs &a, cudaStream_t st) {
-    orth_norm_kernel<T><<<G.n_chunk, 256, 0, st>>>(a);
-    orth_convert_kernel<T><<<G.n_unit, 256, 0, st>>>(a);
+cudaError_t prologue_launch(const cser_orth::Group &G, const OrthArgs &a, cudaStream_t st) {
+    // The norm kernel follows the group before it (or another call), whose products read what it writes: no overlap there.
+    cudaError_t e = launch_kernel(orth_norm_kernel<T>, (unsigned)G.n_chunk, 256, 0, 1, false, st, a);
+    return e == cudaSuccess ? launch_kernel(orth_convert_kernel<T>, (unsigned)G.n_unit, 256, 0, 1, true, st, a) : e;
 }
 
 }  // namespace
@@ -1099,20 +1101,19 @@ int cser_orth_apply(cser_orth_handle h, const void *grad, float *m, float mu, vo
         if (!S->tables) continue;
         SmallArgs a = S->args;
         a.grad = grad, a.m = m, a.mu = mu, a.out = out;
-        if (h->in_type == CSER_TYPE_F32) small_launch<float>(*S, a, small_st);
-        else if (h->in_type == CSER_TYPE_BF16) small_launch<__nv_bfloat16>(*S, a, small_st);
-        else small_launch<__half>(*S, a, small_st);
-        TRY(cudaGetLastError());
+        const cudaError_t e = h->in_type == CSER_TYPE_F32    ? small_launch<float>(*S, a, small_st)
+                              : h->in_type == CSER_TYPE_BF16 ? small_launch<__nv_bfloat16>(*S, a, small_st)
+                                                             : small_launch<__half>(*S, a, small_st);
+        TRY(e);
         h->launches += S->n_resident ? 1 : 2;
     }
     for (cser_orth::Group &G : h->groups) {
         OrthArgs a = G.args;
         a.grad = grad, a.m = m, a.mu = mu, a.out = out;
-        if (h->in_type == CSER_TYPE_F32) prologue_launch<float>(G, a, st);
-        else if (h->in_type == CSER_TYPE_BF16) prologue_launch<__nv_bfloat16>(G, a, st);
-        else prologue_launch<__half>(G, a, st);
-        TRY(cudaGetLastError());
-        cudaError_t e;
+        cudaError_t e = h->in_type == CSER_TYPE_F32    ? prologue_launch<float>(G, a, st)
+                        : h->in_type == CSER_TYPE_BF16 ? prologue_launch<__nv_bfloat16>(G, a, st)
+                                                       : prologue_launch<__half>(G, a, st);
+        TRY(e);
         if (G.mode == kNarrow) e = h->split ? products_launch<kNarrow, true>(a, G.grid, st) : products_launch<kNarrow, false>(a, G.grid, st);
         else if (G.mode == kSingle) e = h->split ? products_launch<kSingle, true>(a, G.grid, st) : products_launch<kSingle, false>(a, G.grid, st);
         else e = h->split ? products_launch<kPaired, true>(a, G.grid, st) : products_launch<kPaired, false>(a, G.grid, st);

@@ -157,6 +157,7 @@ template <typename T>
 __global__ void __launch_bounds__(256) orth_gram_kernel(const SmallArgs a) {
     extern __shared__ __align__(16) double sh[];
     __shared__ int last;
+    let_next_start();
     const uint2 pt = a.part[blockIdx.x];
     const SmallMat M = a.mats[pt.x];
     const int sp = M.sp, side = sp / 8, tiles = side * (side + 1) / 2, ld = gram_ld(sp), cols = kGramDoubles / ld / 4 * 4;
@@ -253,6 +254,7 @@ __global__ void __launch_bounds__(256) orth_apply_kernel(const SmallArgs a) {
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     double *q = sh, *u = sh + sp * sq;                               // [sp][sq], [sp][kApplyLd]
     const T *g = static_cast<const T *>(a.grad);
+    earlier_done();
     for (int e = threadIdx.x; e < sp * sp; e += 256) q[e / sp * sq + e % sp] = __ldcg(a.work + M.q + e);
 #pragma unroll 4
     for (int e = threadIdx.x; e < n * sp; e += 256) {

@@ -27,6 +27,11 @@ constexpr int kEpiWarp0 = 4, kEpiWarps = 16;
 constexpr int kThreads = (kEpiWarp0 + kEpiWarps) * 32;
 
 // ------------------------------------------------------------------ small PTX
+// Kernels of one call are launched to overlap: the next one's CTAs may set up (barriers, tensor memory) while this one's
+// last ones run.  let_next_start() allows it, earlier_done() waits until all earlier kernels are complete and their writes
+// visible; nothing that they write, or read and we write, is touched before it.
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void earlier_done() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
@@ -546,3 +551,26 @@ struct Pipe {
         if (threadIdx.x / 32 == 2) tmem_free<CG>(sh->tmem, 512);
     }
 };
+
+// ------------------------------------------------------------------ launches
+// `after`: an earlier kernel of the same call is in the stream, whose end this one may overlap (it calls earlier_done()).
+template <typename... P, typename... A>
+cudaError_t launch_kernel(void (*kernel)(P...), unsigned grid, unsigned block, size_t shared, unsigned cluster, bool after, cudaStream_t st,
+                          A... args) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(grid), cfg.blockDim = dim3(block), cfg.dynamicSmemBytes = shared, cfg.stream = st;
+    cudaLaunchAttribute at[2];
+    unsigned n = 0;
+    if (cluster > 1) {
+        at[n].id = cudaLaunchAttributeClusterDimension;
+        at[n].val.clusterDim.x = cluster, at[n].val.clusterDim.y = 1, at[n].val.clusterDim.z = 1;
+        ++n;
+    }
+    if (after) {
+        at[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        at[n].val.programmaticStreamSerializationAllowed = 1;
+        ++n;
+    }
+    cfg.attrs = at, cfg.numAttrs = n;
+    return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
+}

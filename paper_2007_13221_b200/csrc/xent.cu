@@ -36,6 +36,7 @@ constexpr size_t kPieceBytes = 256ull << 20;
 // The tensor cores truncate every partial sum: 1.2e-6 of a logit over an inner dimension of 1024 (2.5e-6 of a small loss), 3e-6
 // over 4096.  Above 256 the loss's accumulators are taken out and added up, rounded, after this many stages (an inner dimension of 256).
 constexpr int kLossChunk = 4;
+constexpr int kOwnRatio = 256;                     // tokens of a worker up to which every warp finds the largest |dloss| itself
 constexpr int kJoinRows = kThreads / 32;           // rows that the last CTA joins itself, one per warp
 
 // 2^x, flushing: the instruction.
@@ -72,6 +73,39 @@ struct XentArgs {
     long long dw_stride;
     unsigned *err;
 };
+
+// ------------------------------------------------------------------ dloss, relative to the largest
+__device__ __forceinline__ float type_scale(const XentArgs &a) { return a.bf16 ? 1.f : 4096.f; }
+__device__ __forceinline__ float row_ratio(const XentArgs &a, size_t at, float top) {
+    const int64_t y = a.target[at];
+    if (y == a.ignore) return 0.f;
+    if (y < 0 || y >= a.vocab) return NAN;
+    const float d = a.dloss[at];
+    return d == 0.f ? 0.f : d / top * type_scale(a);                 // NaN stays NaN
+}
+// The largest |dloss| of a worker's tokens that count, by `n` threads of which this is `k`; not yet joined between them.
+__device__ __forceinline__ float largest(const XentArgs &a, int worker, int k, int n) {
+    const size_t base = (size_t)worker * a.tokens;
+    float top = 0.f;
+    for (int t = k; t < a.tokens; t += n)
+        if (a.target[base + t] != a.ignore) top = fmaxf(top, fabsf(a.dloss[base + t]));
+    for (int m = 16; m; m >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, m));
+    return top;
+}
+// One CTA per worker.
+__global__ void __launch_bounds__(1024) xent_ratio_kernel(const __grid_constant__ XentArgs a) {
+    __shared__ float red[32];
+    let_next_start();
+    earlier_done();
+    float top = largest(a, blockIdx.x, threadIdx.x, 1024);
+    if (threadIdx.x % 32 == 0) red[threadIdx.x / 32] = top;
+    __syncthreads();
+    top = red[threadIdx.x % 32];
+    for (int k = 16; k; k >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, k));
+    if (threadIdx.x == 0) a.unscale[blockIdx.x] = top / type_scale(a);
+    const size_t base = (size_t)blockIdx.x * a.tokens;
+    for (int t = threadIdx.x; t < a.tokens; t += 1024) a.ratio[base + t] = row_ratio(a, base + t, top);
+}
 
 // ------------------------------------------------------------------ logits, tile by tile
 // What the tiles of z are for: a loss, a loss over a long inner dimension (chunks), dz.
@@ -130,6 +164,10 @@ struct LogitsJob {
             for (int c = 0; c < chunks; ++c) {
                 if (!p.take(turn, tmem)) return false;
                 if (!LONG) break;
+                if (c == 0) {
+#pragma unroll
+                    for (int b = 0; b < (LONG ? 2 : 0); ++b) tmem_load(tmem + c0 + b * 32, v[b]);
+                } else
 #pragma unroll
                 for (int b = 0; b < 4; ++b) {
                     float x[16];
@@ -137,7 +175,7 @@ struct LogitsJob {
 #pragma unroll
                     for (int k = 0; k < 16; ++k) {
                         float &sum = v[LONG ? b / 2 : 0][b % 2 * 16 + k];
-                        sum = __fadd_rn(c ? sum : 0.f, x[k]);
+                        sum = __fadd_rn(sum, x[k]);
                     }
                 }
                 p.release(turn, lane);
@@ -174,7 +212,14 @@ struct LogitsJob {
             if (live) a.part[(size_t)(t.j * 4 + warp / 4) * a.n * a.tokens + at] = make_float2(m, s);
         } else {
             float ratio = 0.f, lse = 0.f;
-            if (live) ratio = a.ratio[at], lse = a.lse[at];
+            if (a.tokens <= kOwnRatio) {                             // no kernel came before that worked the ratios out
+                const float top = largest(a, t.w, lane, 32);
+                if (live) ratio = row_ratio(a, at, top);
+                if (warp == 0 && lane == 0) a.unscale[t.w] = top / type_scale(a);
+            } else if (live) {
+                ratio = a.ratio[at];
+            }
+            if (live) lse = a.lse[at];
             if (!p.take(turn, tmem)) return false;
             char *dz = a.dz + (size_t)t.w * a.dz_worker;
 #pragma unroll 1
@@ -221,6 +266,8 @@ __device__ __forceinline__ void row_loss(const XentArgs &a, size_t at, float lse
 // The parts of 32 rows joined by 32 warps: a lane takes a row, a warp every 32nd part, four of them at a time.
 __global__ void __launch_bounds__(1024) xent_join_kernel(const __grid_constant__ XentArgs a) {
     __shared__ float2 red[32][32];
+    let_next_start();
+    earlier_done();
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const size_t rows = (size_t)a.n * a.tokens, at = (size_t)blockIdx.x * 32 + lane;
     float m = kLowest, s = 0.f;
@@ -251,10 +298,12 @@ __global__ void __launch_bounds__(1024) xent_join_kernel(const __grid_constant__
 template <int CG, int WHAT>
 __global__ void __launch_bounds__(kThreads, 1) xent_logits_kernel(const __grid_constant__ XentArgs a) {
     extern __shared__ unsigned char raw[];
+    let_next_start();
     if (threadIdx.x == 0) prefetch_tensor_map(&a.h), prefetch_tensor_map(&a.w);
     Pipe<CG> p;
     p.template setup<LogitsJob<CG, WHAT>>(raw, a.err);
     LogitsJob<CG, WHAT> job{a, (int)blockIdx.x / CG, (int)gridDim.x / CG, (a.piece_n + 255) / 256};
+    earlier_done();
     p.run(job);
     p.teardown();
     if constexpr (WHAT != kGrad) {
@@ -285,32 +334,6 @@ __global__ void __launch_bounds__(kThreads, 1) xent_logits_kernel(const __grid_c
             m = top;
         }
         if (lane == 0) row_loss(a, row, m + logf(s));
-    }
-}
-
-// One CTA per worker: the largest |dloss| of the tokens that count, and every token's dloss relative to it.
-__global__ void __launch_bounds__(1024) xent_ratio_kernel(const __grid_constant__ XentArgs a) {
-    __shared__ float red[32];
-    const size_t base = (size_t)blockIdx.x * a.tokens;
-    float top = 0.f;
-    for (int t = threadIdx.x; t < a.tokens; t += 1024)
-        if (a.target[base + t] != a.ignore) top = fmaxf(top, fabsf(a.dloss[base + t]));
-    for (int k = 16; k; k >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, k));
-    if (threadIdx.x % 32 == 0) red[threadIdx.x / 32] = top;
-    __syncthreads();
-    top = red[threadIdx.x % 32];
-    for (int k = 16; k; k >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, k));
-    const float scale = a.bf16 ? 1.f : 4096.f;
-    if (threadIdx.x == 0) a.unscale[blockIdx.x] = top / scale;
-    for (int t = threadIdx.x; t < a.tokens; t += 1024) {
-        const int64_t y = a.target[base + t];
-        float r = 0.f;
-        if (y != a.ignore) {
-            const float d = a.dloss[base + t];
-            if (d != 0.f) r = d / top * scale;                       // NaN stays NaN
-            if (y < 0 || y >= a.vocab) r = NAN;
-        }
-        a.ratio[base + t] = r;
     }
 }
 
@@ -461,6 +484,7 @@ struct GradJob {
 template <int CG>
 __global__ void __launch_bounds__(kThreads, 1) xent_grad_kernel(const __grid_constant__ XentArgs a, int n_dh, int n_dw) {
     extern __shared__ unsigned char raw[];
+    let_next_start();
     if (threadIdx.x == 0) prefetch_tensor_map(&a.h), prefetch_tensor_map(&a.w);
     GradPipe<CG> p;
     p.template setup<GradJob<CG>>(raw, a.err);
@@ -474,12 +498,15 @@ __global__ void __launch_bounds__(kThreads, 1) xent_grad_kernel(const __grid_con
         job.early = stages / (each < 12 ? 12 : each);
         if (job.early > fits) job.early = fits;
     }
+    earlier_done();
     p.run(job);
     p.teardown();
 }
 
 // Where the inner dimension was split: the shares of dh added in their order, four columns a thread.
 __global__ void __launch_bounds__(256) xent_join_dh_kernel(const __grid_constant__ XentArgs a) {
+    let_next_start();
+    earlier_done();
     const int groups = (a.dim + 3) / 4;
     const long long e = (long long)blockIdx.x * 256 + threadIdx.x, row_at = e / groups;
     const int col = (int)(e - row_at * groups) * 4;
@@ -509,6 +536,8 @@ struct PackSource {
     uint16_t *dst;
 };
 __global__ void __launch_bounds__(256) xent_pack_kernel(const PackSource x, const PackSource y, int dim, int padded) {
+    let_next_start();
+    earlier_done();
     const bool second = (int)blockIdx.x >= x.all;
     const PackSource &p = second ? y : x;
     const long long row = (int)blockIdx.x - (second ? x.all : 0);
@@ -596,7 +625,7 @@ int operand(cser_xent *h, CUtensorMap &m, int &workers, const void *p, long long
     return CSER_OK;
 }
 
-int prepare_call(cser_xent *h, const cser_xent_inputs *in, const char *what, XentArgs &a, cudaStream_t st) {
+int prepare_call(cser_xent *h, const cser_xent_inputs *in, const char *what, XentArgs &a, bool &packed, cudaStream_t st) {
     if (!h) return cser_internal_fail(CSER_ERR_INVALID, "%s: NULL handle", what);
     if (!in) return cser_internal_fail(CSER_ERR_INVALID, "%s: NULL inputs", what);
     int dev = -1;
@@ -607,7 +636,7 @@ int prepare_call(cser_xent *h, const cser_xent_inputs *in, const char *what, Xen
         return cser_internal_fail(CSER_ERR_CUDA, "a device-side wait ran out in an earlier call: its results are incomplete");
     if (in->tokens < 0 || in->tokens > h->max_tokens)
         return cser_internal_fail(CSER_ERR_INVALID, "%s: tokens must be in 0..%lld", what, h->max_tokens);
-    a = XentArgs{};
+    a = XentArgs{}, packed = false;
     a.n = h->n, a.tokens = (int)in->tokens, a.vocab = (int)h->vocab, a.dim = (int)h->dim;
     if (in->tokens == 0) return CSER_OK;
     if (in->hidden_row_stride < 0 || in->hidden_worker_stride < 0 || in->weight_row_stride < 0 || in->weight_worker_stride < 0)
@@ -624,7 +653,8 @@ int prepare_call(cser_xent *h, const cser_xent_inputs *in, const char *what, Xen
     if (int rc = operand(h, a.w, a.w_workers, in->weight, h->vocab, in->weight_row_stride, in->weight_worker_stride, h->pack_w, h->vocab,
                          pack[1], "weight", st))
         return rc;
-    if (pack[0].all + pack[1].all) {
+    packed = pack[0].all + pack[1].all > 0;
+    if (packed) {
         xent_pack_kernel<<<(unsigned)(pack[0].all + pack[1].all), 256, 0, st>>>(pack[0], pack[1], (int)h->dim, (int)up(h->dim, 8));
         TRY(cudaGetLastError());
         h->launches++;
@@ -637,20 +667,10 @@ int prepare_call(cser_xent *h, const cser_xent_inputs *in, const char *what, Xen
 }
 
 template <int CG, typename K, typename... Args>
-cudaError_t tiles_launch(cser_xent *h, K kernel, size_t shared, long long tiles, cudaStream_t st, Args... args) {
+cudaError_t tiles_launch(cser_xent *h, K kernel, size_t shared, long long tiles, bool after, cudaStream_t st, Args... args) {
     const long long most = h->sms / CG;
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)((tiles < most ? tiles : most) * CG));
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = shared;
-    cfg.stream = st;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = CG, at[0].val.clusterDim.y = 1, at[0].val.clusterDim.z = 1;
-    cfg.attrs = at;
-    cfg.numAttrs = CG == 1 ? 0 : 1;
     h->launches++;
-    return cudaLaunchKernelEx(&cfg, kernel, args...);
+    return launch_kernel(kernel, (unsigned)((tiles < most ? tiles : most) * CG), kThreads, shared, CG, after, st, args...);
 }
 
 template <int CG>
@@ -664,38 +684,40 @@ cudaError_t kernels_setup() {
 }
 
 template <int CG>
-int loss_launch(cser_xent *h, XentArgs &a, cudaStream_t st) {
+int loss_launch(cser_xent *h, XentArgs &a, bool packed, cudaStream_t st) {
     a.token_tiles = (int)(up(a.tokens, 128 * CG) / (128 * CG)), a.piece0 = 0, a.piece_n = a.vocab;
     const auto kernel = a.dim > kLossChunk * kStageK ? xent_logits_kernel<CG, kLongLoss> : xent_logits_kernel<CG, kLoss>;
-    TRY((tiles_launch<CG>(h, kernel, Pipe<CG>::kSharedBytes, (long long)a.n * a.token_tiles * ((a.vocab + 255) / 256), st, a)));
+    TRY((tiles_launch<CG>(h, kernel, Pipe<CG>::kSharedBytes, (long long)a.n * a.token_tiles * ((a.vocab + 255) / 256), packed, st, a)));
     if ((long long)a.n * a.tokens > kJoinRows) {
-        xent_join_kernel<<<(unsigned)(((long long)a.n * a.tokens + 31) / 32), 1024, 0, st>>>(a);
-        TRY(cudaGetLastError());
+        TRY(launch_kernel(xent_join_kernel, (unsigned)(((long long)a.n * a.tokens + 31) / 32), 1024, 0, 1, true, st, a));
         h->launches++;
     }
     return CSER_OK;
 }
 
 template <int CG>
-int grad_launch(cser_xent *h, XentArgs &a, cudaStream_t st) {
+int grad_launch(cser_xent *h, XentArgs &a, bool packed, cudaStream_t st) {
     a.token_tiles = (int)(up(a.tokens, 128 * CG) / (128 * CG));
     a.splits = splits_of(h, a.tokens);
-    xent_ratio_kernel<<<(unsigned)a.n, 1024, 0, st>>>(a);
-    TRY(cudaGetLastError());
-    h->launches++;
+    bool after = packed;
+    if (a.tokens > kOwnRatio) {
+        TRY(launch_kernel(xent_ratio_kernel, (unsigned)a.n, 1024, 0, 1, after, st, a));
+        h->launches++;
+        after = true;
+    }
     const long long dim_tiles = up(a.dim, 256) / 256;
     for (long long v = 0; v < h->vocab; v += h->piece) {
         a.piece0 = (int)v, a.piece_n = (int)(h->vocab - v < h->piece ? h->vocab - v : h->piece);
         a.first_piece = v == 0, a.last_piece = v + h->piece >= h->vocab;
         const long long vt = up(a.piece_n, 128 * CG) / (128 * CG);
-        TRY((tiles_launch<CG>(h, xent_logits_kernel<CG, kGrad>, Pipe<CG>::kSharedBytes, (long long)a.n * a.token_tiles * ((a.piece_n + 255) / 256), st, a)));
+        TRY((tiles_launch<CG>(h, xent_logits_kernel<CG, kGrad>, Pipe<CG>::kSharedBytes, (long long)a.n * a.token_tiles * ((a.piece_n + 255) / 256), after, st, a)));
+        after = true;
         const long long n_dh = a.dh ? (long long)a.n * a.token_tiles * a.splits * dim_tiles : 0, n_dw = a.dw ? a.n * vt * dim_tiles : 0;
-        TRY((tiles_launch<CG>(h, xent_grad_kernel<CG>, GradPipe<CG>::kSharedBytes, n_dh + n_dw, st, a, (int)n_dh, (int)n_dw)));
+        TRY((tiles_launch<CG>(h, xent_grad_kernel<CG>, GradPipe<CG>::kSharedBytes, n_dh + n_dw, true, st, a, (int)n_dh, (int)n_dw)));
     }
     if (a.dh && a.splits > 1) {
         const long long e = (long long)a.n * a.tokens * ((a.dim + 3) / 4);
-        xent_join_dh_kernel<<<(unsigned)((e + 255) / 256), 256, 0, st>>>(a);
-        TRY(cudaGetLastError());
+        TRY(launch_kernel(xent_join_dh_kernel, (unsigned)((e + 255) / 256), 256, 0, 1, true, st, a));
         h->launches++;
     }
     return CSER_OK;
@@ -770,7 +792,8 @@ cser_xent_handle cser_xent_create(int32_t n_workers, int64_t max_tokens, int64_t
 int cser_xent_loss(cser_xent_handle h, const cser_xent_inputs *in, float *loss, float *lse, void *stream) {
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     XentArgs a;
-    if (int rc = prepare_call(h, in, "cser_xent_loss", a, st)) return rc;
+    bool packed = false;
+    if (int rc = prepare_call(h, in, "cser_xent_loss", a, packed, st)) return rc;
     if (a.tokens == 0) return CSER_OK;
     if (int rc = cser_internal_check_ptr(lse, "cser_xent_loss: lse")) return rc;
     if (loss)
@@ -778,14 +801,15 @@ int cser_xent_loss(cser_xent_handle h, const cser_xent_inputs *in, float *loss, 
     if ((uintptr_t)lse % 4 || (uintptr_t)loss % 4)
         return cser_internal_fail(CSER_ERR_INVALID, "cser_xent_loss: a pointer is not aligned to its element type");
     a.loss = loss, a.lse_out = lse;
-    return wide_tiles(a.tokens) ? loss_launch<2>(h, a, st) : loss_launch<1>(h, a, st);
+    return wide_tiles(a.tokens) ? loss_launch<2>(h, a, packed, st) : loss_launch<1>(h, a, packed, st);
 }
 
 int cser_xent_grad(cser_xent_handle h, const cser_xent_inputs *in, const float *lse, const float *dloss, void *dhidden,
                    void *dweight, int64_t dweight_stride, void *stream) {
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     XentArgs a;
-    if (int rc = prepare_call(h, in, "cser_xent_grad", a, st)) return rc;
+    bool packed = false;
+    if (int rc = prepare_call(h, in, "cser_xent_grad", a, packed, st)) return rc;
     if (!dhidden && !dweight) return CSER_OK;
     if (dweight) {
         if (int rc = cser_internal_check_ptr(dweight, "cser_xent_grad: dweight")) return rc;
@@ -807,7 +831,7 @@ int cser_xent_grad(cser_xent_handle h, const cser_xent_inputs *in, const float *
     if ((uintptr_t)lse % 4 || (uintptr_t)dloss % 4)
         return cser_internal_fail(CSER_ERR_INVALID, "cser_xent_grad: a pointer is not aligned to its element type");
     a.lse = lse, a.dloss = dloss, a.dh = dhidden, a.dw = dweight, a.dw_stride = dweight_stride;
-    return wide_tiles(a.tokens) ? grad_launch<2>(h, a, st) : grad_launch<1>(h, a, st);
+    return wide_tiles(a.tokens) ? grad_launch<2>(h, a, packed, st) : grad_launch<1>(h, a, packed, st);
 }
 
 void cser_xent_destroy(cser_xent_handle h) {

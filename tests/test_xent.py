@@ -89,7 +89,7 @@ def test_against_the_formula(size, dtype):
     h, w, y, dloss = inputs(n, t, v, d, dtype)
     op = train.LinearCrossEntropy(n, t, v, d, dtype)
     check(op, h, w, y, dloss, dtype)
-    assert op.launches >= 4
+    assert op.launches >= 3                           # loss, dz, the gradients
 
 
 @pytest.mark.gpu
