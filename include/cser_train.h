@@ -39,7 +39,8 @@ extern "C" {
  * its singular vectors.  A matrix of zeros gives zeros.  Infinities and NaN spoil their own matrix only.
  * Momenta and outputs outside the listed matrices are neither read nor written.
  *
- * Arithmetic.  in_type F32, BF16 or F16; momentum fp32; norms and sums fp32.  out_type BF16 or F16: the products take
+ * Arithmetic.  in_type F32, BF16 or F16; momentum fp32.  Matrices with a short side of at most 64 go through their Gram
+ * matrix in 64 bits.  Others: norms and sums fp32; out_type BF16 or F16: the products take
  * fp16 operands (11 bits), with the remainder of X and the diagonals of A and b A + c A A carried in addition, which
  * leaves about 1e-3 relative error at most before the rounding of the result.  out_type F32: the operands are pairs of
  * fp16 (22 bits) and each product is three, about 1e-6.  Results are the same from call to call, bit for bit.
@@ -62,6 +63,13 @@ cser_orth_handle cser_orth_create(int32_t n_workers, int64_t ld, int32_t n_matri
  */
 int cser_orth_apply(cser_orth_handle h, const void *grad, float *m, float mu, void *out, void *stream);
 void cser_orth_destroy(cser_orth_handle h);
+/*
+ * Test hook for the bounded waits.  In the NEXT cser_orth_apply the tiled kernel waits for something that does not happen, and every wait is
+ * limited to wait_mcycles million SM clock cycles (1 .. 2000; the normal limit is 2000, about a second).  The wait runs out, the
+ * kernel ends, and every later cser_orth_apply on the plan returns CSER_ERR_CUDA.  Nothing traps and the CUDA context stays
+ * usable.  CSER_ERR_INVALID where all matrices have a short side of at most 64: no kernel waits then.
+ */
+int cser_orth_debug_stall_next(cser_orth_handle h, unsigned wait_mcycles);
 /* Number of kernels launched on behalf of the plan. */
 int64_t cser_orth_launch_count(cser_orth_handle h);
 

@@ -91,6 +91,8 @@ struct OrthArgs {
     void *out;
     int out_type;
     unsigned *err;
+    long long wait_cycles;
+    unsigned stall;                                // test hook: added to what the second phase of each matrix waits for
 };
 
 // ------------------------------------------------------------------ element access
@@ -359,6 +361,7 @@ struct OrthJob {
         t.phase = phase, t.tall = M.tall, t.last = phase == kPhaseX && step == a.steps - 1;
         t.row0 = t.row_a = e.i * 128 * CG + rank * 128, t.row_b = e.j * TN + rank * (t.n / CG), t.panel0 = e.j * (TN / 64);
         t.need = (unsigned)step * (2 * M.tiles_sym + M.tiles_x) + (unsigned)phase * M.tiles_sym, t.done = a.done + e.q;
+        if (phase == kPhaseB) t.need += a.stall;
         __half *sym_hi = phase == kPhaseB ? M.ah : M.bh, *sym_lo = phase == kPhaseB ? M.al : M.bl;
         t.a_hi = (const char *)(sym_a ? sym_hi : M.xh[from]), t.a_lo = (const char *)(sym_a ? sym_lo : M.xl[from]);
         t.b_hi = (const char *)(sym_b ? sym_hi : M.xh[from]), t.b_lo = (const char *)(sym_b ? sym_lo : M.xl[from]);
@@ -533,7 +536,7 @@ struct OrthJob {
                 t0 = clock64();
             } else {
                 if (p.sh->dead) return false;
-                if (clock64() - t0 > kWaitCycles) {
+                if (clock64() - t0 > p.limit) {
                     p.fail();
                     return false;
                 }
@@ -687,7 +690,7 @@ __global__ void __launch_bounds__(kThreads, 1) orth_products_kernel(const __grid
     extern __shared__ unsigned char raw[];
     constexpr int CG = mode_cg(MODE);
     OrthPipe<MODE, SPLIT> p;
-    p.template setup<OrthJob<MODE, SPLIT>>(raw, a.err);
+    p.template setup<OrthJob<MODE, SPLIT>>(raw, a.err, a.wait_cycles);
     OrthJob<MODE, SPLIT> job{a, (int)blockIdx.x / CG, (int)gridDim.x / CG};
     p.run(job);
     p.teardown();
@@ -724,6 +727,7 @@ struct cser_orth {
     cudaEvent_t fork = nullptr, join = nullptr;
     void *work = nullptr;                          // shared by the groups, which run one after the other
     unsigned *err_host = nullptr;
+    unsigned stall_mcycles = 0;                    // cser_orth_debug_stall_next
     long long launches = 0;
 };
 
@@ -1078,7 +1082,8 @@ int cser_orth_apply(cser_orth_handle h, const void *grad, float *m, float mu, vo
     if (dev != h->device)
         return cser_internal_fail(CSER_ERR_INVALID, "handle belongs to device %d, current device is %d", h->device, dev);
     if (*reinterpret_cast<volatile unsigned *>(h->err_host))
-        return cser_internal_fail(CSER_ERR_CUDA, "a device-side wait ran out in an earlier cser_orth_apply: its results are incomplete");
+        return cser_internal_fail(CSER_ERR_CUDA, "a device-side wait ran out in an earlier cser_orth_apply: its results are incomplete, "
+                                                 "make a new plan");
     if (int rc = cser_internal_check_ptr(grad, "cser_orth_apply: grad")) return rc;
     if (int rc = cser_internal_check_ptr(out, "cser_orth_apply: out")) return rc;
     if (m)
@@ -1110,6 +1115,8 @@ int cser_orth_apply(cser_orth_handle h, const void *grad, float *m, float mu, vo
     for (cser_orth::Group &G : h->groups) {
         OrthArgs a = G.args;
         a.grad = grad, a.m = m, a.mu = mu, a.out = out;
+        a.wait_cycles = h->stall_mcycles ? h->stall_mcycles * 1000000ll : kWaitCycles;
+        a.stall = h->stall_mcycles ? 1u << 30 : 0;
         cudaError_t e = h->in_type == CSER_TYPE_F32    ? prologue_launch<float>(G, a, st)
                         : h->in_type == CSER_TYPE_BF16 ? prologue_launch<__nv_bfloat16>(G, a, st)
                                                        : prologue_launch<__half>(G, a, st);
@@ -1120,6 +1127,7 @@ int cser_orth_apply(cser_orth_handle h, const void *grad, float *m, float mu, vo
         TRY(e);
         h->launches += 3;
     }
+    h->stall_mcycles = 0;
     if (both) {
         TRY(cudaEventRecord(h->join, small_st));
         TRY(cudaStreamWaitEvent(st, h->join, 0));
@@ -1139,6 +1147,15 @@ void cser_orth_destroy(cser_orth_handle h) {
     if (h->work) cudaFree(h->work);
     if (h->err_host) cudaFreeHost(h->err_host);
     delete h;
+}
+
+int cser_orth_debug_stall_next(cser_orth_handle h, unsigned wait_mcycles) {
+    if (!h) return cser_internal_fail(CSER_ERR_INVALID, "cser_orth_debug_stall_next: NULL handle");
+    if (wait_mcycles < 1 || wait_mcycles > 2000)
+        return cser_internal_fail(CSER_ERR_INVALID, "cser_orth_debug_stall_next: wait_mcycles must be in 1..2000");
+    if (h->groups.empty()) return cser_internal_fail(CSER_ERR_INVALID, "cser_orth_debug_stall_next: the plan has no kernel that waits");
+    h->stall_mcycles = wait_mcycles;
+    return CSER_OK;
 }
 
 int64_t cser_orth_launch_count(cser_orth_handle h) { return h ? h->launches : 0; }

@@ -252,6 +252,7 @@ struct Pipe {
     Shared *sh;
     unsigned *err;                                                  // the handle's word, mapped host memory
     uint32_t rank;
+    long long limit;                                                // of a wait, in cycles
 
     __device__ __forceinline__ void fail() {
         sh->dead = 1;
@@ -268,7 +269,7 @@ struct Pipe {
             for (int k = 0; k < 64; ++k)
                 if (mbar_try_wait(bar, parity)) return true;
             if (sh->dead) return false;
-            if (clock64() - t0 > kWaitCycles) {
+            if (clock64() - t0 > limit) {
                 fail();
                 return false;
             }
@@ -282,7 +283,7 @@ struct Pipe {
             asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(counter) : "memory");
             if (v >= target) return true;
             if (sh->dead) return false;
-            if ((k & 63) == 63 && clock64() - t0 > kWaitCycles) {
+            if ((k & 63) == 63 && clock64() - t0 > limit) {
                 fail();
                 return false;
             }
@@ -290,12 +291,12 @@ struct Pipe {
     }
 
     template <class Job>
-    __device__ __forceinline__ void setup(unsigned char *raw, unsigned *err_word) {
+    __device__ __forceinline__ void setup(unsigned char *raw, unsigned *err_word, long long wait_cycles = kWaitCycles) {
         static_assert(sizeof(typename Job::Tile) <= kTileBytes && alignof(typename Job::Tile) <= 16, "a tile in shared memory");
         stage0 = (smem_addr(raw) + 1023u) & ~1023u;
         extra = stage0 + kStages * kStageBytes;
         sh = reinterpret_cast<Shared *>(raw + (extra - smem_addr(raw)) + EXTRA);
-        err = err_word;
+        err = err_word, limit = wait_cycles;
         rank = CG == 1 ? 0 : cluster_rank();
         if (threadIdx.x == 0) {
             for (int s = 0; s < kStages; ++s) {
@@ -394,7 +395,7 @@ struct Pipe {
                 for (int k = 0; k < pending; ++k) {
                     s = s == 0 ? kStages - 1 : s - 1;
                     if (s == kStages - 1) ph ^= 1;
-                    while (!(CG == 2 && rank == 0) && !mbar_try_wait(&sh->full[s], ph) && clock64() - t0 < kWaitCycles) {}
+                    while (!(CG == 2 && rank == 0) && !mbar_try_wait(&sh->full[s], ph) && clock64() - t0 < limit) {}
                 }
                 if (CG == 2 && rank == 0)               // its barriers also count the peer's arrivals: allow time instead
                     while (clock64() - t0 < 2000000ll) {}
@@ -456,7 +457,7 @@ struct Pipe {
             if (!ok) {                                  // products in flight end before tensor memory is given back
                 mma_commit<CG>(&sh->drain);
                 const long long t0 = clock64();
-                while (!mbar_try_wait(&sh->drain, 0) && clock64() - t0 < kWaitCycles) {}
+                while (!mbar_try_wait(&sh->drain, 0) && clock64() - t0 < limit) {}
             }
         } else if (CG == 2 && warp == 1 && lane == 0) {
             // The pair's second CTA passes "this stage has landed" on to the first one's barrier.

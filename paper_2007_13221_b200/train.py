@@ -34,6 +34,7 @@ def lib():
             ("cser_orth_create", p, [i32, i64, i32, p, p, p, p, p, i32, i32, i32]),
             ("cser_orth_apply", c.c_int, [p, p, p, f32, p, p]),
             ("cser_orth_destroy", None, [p]),
+            ("cser_orth_debug_stall_next", c.c_int, [p, c.c_uint]),
             ("cser_orth_launch_count", i64, [p]),
             ("cser_xent_create", p, [i32, i64, i64, i64, i32, i64]),
             ("cser_xent_loss", c.c_int, [p, c.POINTER(_XentInputs), p, p, p]),

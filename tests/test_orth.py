@@ -234,6 +234,34 @@ def test_refusals():
     assert torch.equal(o.apply(g), o.apply(g))
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("shapes", [[(200, 300)], [(200, 300), (16, 16)], [(512, 1024)] * 12], ids=lambda s: f"{len(s)}")
+@pytest.mark.parametrize("out_t", [BF, F32], ids=str)
+def test_a_wait_that_runs_out_ends_the_kernel_and_is_reported(shapes, out_t):
+    """Single CTAs and pairs, both results: the context and other plans stay usable."""
+    mats, at = [], 0
+    for r, c in shapes:
+        mats.append((at, r, c))
+        at += r * c
+    g = torch.randn((1, at), device="cuda")
+    o, other = (train.Orthogonalizer(mats, 1, at, F32, out_t) for _ in range(2))
+    want = other.apply(g)
+    assert torch.equal(o.apply(g), want)
+    L = train.lib()
+    for bad in (0, 2001):
+        assert L.cser_orth_debug_stall_next(o.h, bad) == -1
+    assert L.cser_orth_debug_stall_next(o.h, 20) == 0
+    o.apply(g)
+    torch.cuda.synchronize()
+    for _ in range(2):
+        with pytest.raises(CSERError, match="wait ran out"):
+            o.apply(g)
+    assert torch.equal(other.apply(g), want)
+    o.close()
+    small = train.Orthogonalizer([(0, 8, 8)], 1, 64)
+    assert L.cser_orth_debug_stall_next(small.h, 20) == -1 and L.cser_orth_debug_stall_next(None, 20) == -1
+
+
 def test_refusals_need_no_gpu():
     """Arguments are checked before the first CUDA call."""
     for bad in (dict(n_workers=0), dict(ld=0), dict(matrices=[(0, 4, 6)]), dict(matrices=[(0, 4, 0)]), dict(steps=0)):
