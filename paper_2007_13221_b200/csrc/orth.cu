@@ -501,7 +501,7 @@ struct OrthJob {
                         end = true;
                         break;
                     }
-                    fence_async_proxy();                             // what the tile's phase reads, for the copy engine
+                    fence_async_global();                            // what the tile's phase reads, for the copy engine
                 }
                 const Tile &t = *p.template tile_at<Tile>(ahead);
                 bulk_out_read<0>();
@@ -511,8 +511,7 @@ struct OrthJob {
             }
             if (signal) {
                 const Tile &t = *p.template tile_at<Tile>(behind);
-                bulk_out_done();
-                fence_async_proxy();                                 // the next phase reads through the copy engine
+                bulk_out_done();                                     // written; the next phase's readers fence their own copies
                 asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(t.done) : "memory");
                 signal = false, moved = true;
                 p.tile_done(behind);
@@ -669,13 +668,13 @@ struct OrthJob {
                                    make_uint4(__float_as_uint(v[4 * k]), __float_as_uint(v[4 * k + 1]), __float_as_uint(v[4 * k + 2]),
                                               __float_as_uint(v[4 * k + 3])));
             }
-            fence_async_proxy();
+            fence_async_shared();
             __syncwarp();
             if (lane == 0) mbar_arrive(&p.sh->extra_done[ring.buf]);
             if (last) {
                 if (!p.warp_wait(&p.sh->extra_done[ring.buf], ring.parity())) return false;
                 store_result(p, t, panel, tid);
-                fence_async_proxy();                                 // read before the copy engine writes here again
+                fence_async_shared();                                // read before the copy engine writes here again
                 __syncwarp();
             }
             if (lane == 0) mbar_arrive(&p.sh->extra_free[ring.buf]);

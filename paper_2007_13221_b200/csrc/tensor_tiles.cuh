@@ -92,7 +92,10 @@ __device__ __forceinline__ void tensor_copy_in(uint32_t dst, const CUtensorMap *
 __device__ __forceinline__ void prefetch_tensor_map(const CUtensorMap *map) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
 }
-__device__ __forceinline__ void fence_async_proxy() { asm volatile("fence.proxy.async;" ::: "memory"); }
+// Between ordinary accesses to shared memory and the copy engine's, and to global memory.  (The fence over both takes about 1100
+// cycles: in the epilogue of every panel that was a third of its time.)
+__device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void fence_async_global() { asm volatile("fence.proxy.async.global;" ::: "memory"); }
 
 template <int CG>
 __device__ __forceinline__ void tmem_alloc(uint32_t *dst, uint32_t cols) {
@@ -374,7 +377,7 @@ struct Pipe {
                 ok = wait(&sh->tile_full[walk.slot], walk.ph);
                 const Tile &t = *tile_at<Tile>(walk);
                 if (!ok || t.n == 0) break;
-                fence_async_proxy();                    // what ready() saw written, for the copy engine
+                fence_async_global();                   // what ready() saw written, for the copy engine
                 typename Job::Loader from(job, t);
                 const uint32_t bytes = from.bytes();
                 const int stages = t.stages;
