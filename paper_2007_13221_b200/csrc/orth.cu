@@ -493,6 +493,13 @@ struct OrthJob {
         long long t0 = clock64();
         for (;;) {
             bool moved = false;
+            if (signal) {                                            // before anything else: the next phase waits for it
+                const Tile &t = *p.template tile_at<Tile>(behind);
+                bulk_out_done();                                     // written; the next phase's readers fence their own copies
+                asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(t.done) : "memory");
+                signal = false, moved = true;
+                p.tile_done(behind);
+            }
             while (!end && used < kBufs) {
                 if (!known) {
                     if (!mbar_test(&p.sh->tile_full[ahead.slot], ahead.ph)) break;
@@ -508,13 +515,6 @@ struct OrthJob {
                 load_panel(p, t, b_in);
                 ++used, moved = true;
                 if (++b_in == t.n / 64) b_in = 0, known = false, ahead.step();
-            }
-            if (signal) {
-                const Tile &t = *p.template tile_at<Tile>(behind);
-                bulk_out_done();                                     // written; the next phase's readers fence their own copies
-                asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(t.done) : "memory");
-                signal = false, moved = true;
-                p.tile_done(behind);
             }
             if (used > 0) {
                 const Tile &t = *p.template tile_at<Tile>(behind);
@@ -545,12 +545,16 @@ struct OrthJob {
 
     __device__ __forceinline__ bool epilogue(P &p, const Tile &t, typename P::Turn &turn, int warp, int lane) {
         const int tid = warp * 32 + lane, side = warp / 4, r = warp % 4 * 32 + lane, row = t.row0 + r, panels = t.n / 64;
-        const bool last = t.last;
-        const float d_row = t.phase == kPhaseB ? __ldcg(t.da + row) : t.phase == kPhaseX && !t.tall ? __ldcg(t.db + row) : 0.f;
+        const bool last = t.last, tall = t.tall;
+        const int phase = t.phase;
+        float *da = t.da, *db = t.db;
+        // What of the diagonals a column needs: of A for B, of B for the X of a tall matrix.
+        const float *d_cols = phase == kPhaseB ? da : phase == kPhaseX && tall ? db : nullptr;
+        const float d_row = phase == kPhaseB ? __ldcg(da + row) : phase == kPhaseX && !tall ? __ldcg(db + row) : 0.f;
         uint32_t tmem;
         float sum[kSums][16];                                        // of a 32-bit result's chunks
         if (SPLIT) {
-            const int each = t.phase == kPhaseX ? kChunkX : kChunkAB, chunks = (t.stages + each - 1) / each;
+            const int each = phase == kPhaseX ? kChunkX : kChunkAB, chunks = (t.stages + each - 1) / each;
             for (int c = 0; c <= chunks; ++c) {                      // hi hi, then the small products
                 if (c < chunks ? !p.take(turn, tmem) : !p.take_small(turn, tmem)) return false;
 #pragma unroll
@@ -569,6 +573,10 @@ struct OrthJob {
 #pragma unroll kSums
         for (int b = 0; b < (SPLIT ? kSums : panels); ++b) {
             const int panel = t.panel0 + b, col = panel * 64 + side * 16;
+            float4 d_col[4];                                         // asked for before the waits
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                d_col[k] = d_cols ? __ldcg(reinterpret_cast<const float4 *>(d_cols + col) + k) : make_float4(0.f, 0.f, 0.f, 0.f);
             if (!p.warp_wait(&p.sh->extra_full[ring.buf], ring.parity())) return false;
             const uint32_t at = p.extra + ring.buf * kBufBytes;
             float v[16];
@@ -580,18 +588,18 @@ struct OrthJob {
                 if (b + 1 == panels) p.release(turn, lane);
             }
             const unsigned on = (unsigned)(row - col);               // the diagonal is at column `on` of the 16, if below 16
-            if (t.phase == kPhaseA) {
+            if (phase == kPhaseA) {
                 if (on < 16u) {
 #pragma unroll
                     for (int k = 0; k < 16; ++k)
-                        if (on == (unsigned)k) t.da[row] = v[k] * kUnscale2, v[k] = 0.f;
+                        if (on == (unsigned)k) da[row] = v[k] * kUnscale2, v[k] = 0.f;
                     __threadfence();
                 }
 #pragma unroll
                 for (int k = 0; k < 16; ++k) v[k] *= kUnscale;
             } else {
                 float x[16];
-                if (SPLIT && t.phase == kPhaseX) {
+                if (SPLIT && phase == kPhaseX) {
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         const uint4 f = shared_load16(at + kWide + wide_chunk(r, side * 4 + k));
@@ -602,7 +610,7 @@ struct OrthJob {
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
                         unpack8(shared_load16(at + panel_chunk(r, side * 2 + k)), x + 8 * k);
-                        if (SPLIT || t.phase == kPhaseX) {
+                        if (SPLIT || phase == kPhaseX) {
                             float l[8];
                             unpack8(shared_load16(at + kLo + panel_chunk(r, side * 2 + k)), l);
 #pragma unroll
@@ -610,18 +618,18 @@ struct OrthJob {
                         }
                     }
                 }
-                if (t.phase == kPhaseB) {
+                if (phase == kPhaseB) {
                     // x is A without its diagonal, times 2^12
                     if (on < 16u) {
 #pragma unroll
                         for (int k = 0; k < 16; ++k)
                             if (on == (unsigned)k)
-                                t.db[row] = __fmaf_rn(kC, __fmaf_rn(d_row, d_row, v[k] * kUnscale2), kB * d_row), v[k] = 0.f;
+                                db[row] = __fmaf_rn(kC, __fmaf_rn(d_row, d_row, v[k] * kUnscale2), kB * d_row), v[k] = 0.f;
                         __threadfence();
                     }
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
-                        const float4 dc = __ldcg(reinterpret_cast<const float4 *>(t.da + col) + k);
+                        const float4 dc = d_col[k];
                         const float d[4] = {dc.x, dc.y, dc.z, dc.w};
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
@@ -630,10 +638,10 @@ struct OrthJob {
                             v[i] = on == (unsigned)i ? 0.f : __fmaf_rn(kC, sq, kB * x[i]);
                         }
                     }
-                } else if (t.tall) {
+                } else if (tall) {
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
-                        const float4 dc = __ldcg(reinterpret_cast<const float4 *>(t.db + col) + k);
+                        const float4 dc = d_col[k];
                         const float d[4] = {dc.x, dc.y, dc.z, dc.w};
 #pragma unroll
                         for (int e = 0; e < 4; ++e) v[4 * k + e] = __fmaf_rn(kA + d[e], x[4 * k + e], v[4 * k + e] * kUnscale);
@@ -658,10 +666,10 @@ struct OrthJob {
                     if (last && a.out_type == CSER_TYPE_BF16)
                         hi = make_uint4(pack_bf162(e[0], e[1]), pack_bf162(e[2], e[3]), pack_bf162(e[4], e[5]), pack_bf162(e[6], e[7]));
                     shared_store16(at + panel_chunk(r, side * 2 + k), hi);
-                    if (SPLIT || t.phase == kPhaseX) shared_store16(at + kLo + panel_chunk(r, side * 2 + k), lo);
+                    if (SPLIT || phase == kPhaseX) shared_store16(at + kLo + panel_chunk(r, side * 2 + k), lo);
                 }
             }
-            if (SPLIT && t.phase == kPhaseX) {
+            if (SPLIT && phase == kPhaseX) {
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
                     shared_store16(at + kWide + wide_chunk(r, side * 4 + k),

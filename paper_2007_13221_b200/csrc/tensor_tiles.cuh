@@ -3,7 +3,8 @@
 // an epilogue of the operator's own.  Device code; included by orth.cu and xent.cu inside their unnamed namespaces.
 //
 // Roles.  A CTA is 20 warps: warp 0 issues the copies, warp 1 issues the matrix instructions, warp 2 works out what the next
-// tiles are and leaves that in shared memory, warp 3 may copy for the epilogue, warps 4-19 are the epilogue (warp w reads
+// tiles are, waits for what they read and leaves them in shared memory, warp 3 may copy for the epilogue, warps 4-19 are the
+// epilogue (warp w reads
 // the tensor-memory lanes 32*(w%4)..+31, the quarter (w-4)/4 of the columns; with 8 epilogue warps, two to a scheduler, the
 // latencies of their arithmetic showed: 3000 cycles for 128 x 64 values).  Two
 // accumulators of 256 columns take turns, so the epilogue of one tile runs under the products of the next.  With
@@ -312,7 +313,8 @@ struct Pipe {
             }
             for (int k = 0; k < 3; ++k)
                 mbar_init(&sh->extra_full[k], 1), mbar_init(&sh->extra_done[k], kEpiWarps), mbar_init(&sh->extra_free[k], kEpiWarps);
-            for (int k = 0; k < kTiles; ++k) mbar_init(&sh->tile_full[k], 1), mbar_init(&sh->tile_empty[k], 2 + kEpiWarps + Job::kCopier);
+            for (int k = 0; k < kTiles; ++k)
+                mbar_init(&sh->tile_full[k], 1), mbar_init(&sh->tile_empty[k], 2 + kEpiWarps + Job::kCopier);
             mbar_init(&sh->drain, 1);
             sh->dead = 0;
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -484,6 +486,8 @@ struct Pipe {
             for (int i = lane; ok; i += kTiles) {
                 job.tile(t, i, (int)rank);
                 ok = wait(&sh->tile_empty[lane], (uint32_t)(i / kTiles & 1) ^ 1);
+                // One at a time looks at memory: the lane of the tile before has done with it.
+                if (ok && i) ok = wait(&sh->tile_full[(i - 1) % kTiles], (uint32_t)((i - 1) / kTiles & 1));
                 if (ok && t.n) ok = job.ready(*this, t);
                 if (!ok) break;
                 *reinterpret_cast<Tile *>(sh->tile[lane]) = t;

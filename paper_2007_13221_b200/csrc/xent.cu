@@ -37,7 +37,7 @@ constexpr size_t kPieceBytes = 256ull << 20;
 // over 4096.  Above 256 the loss's accumulators are taken out and added up, rounded, after this many stages (an inner dimension of 256).
 constexpr int kLossChunk = 4;
 constexpr int kOwnRatio = 256;                     // tokens of a worker up to which every warp finds the largest |dloss| itself
-constexpr int kJoinRows = kThreads / 32;           // rows that the last CTA joins itself, one per warp
+constexpr int kJoinRows = 20;                     // rows that the last CTA joins itself, one per warp
 
 // 2^x, flushing: the instruction.
 __device__ __forceinline__ float exp2_fast(float x) {
