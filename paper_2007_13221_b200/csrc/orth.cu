@@ -883,7 +883,10 @@ int build_group(cser_orth *h, cser_orth::Group &G, const std::vector<HostMat> &m
     A.out_type = h->out_type;
     G.n_chunk = (int)chunk.size(), G.n_unit = (int)unit.size(), G.mode = mode;
     const int widest = A.n_sym > A.n_x ? A.n_sym : A.n_x;
-    G.grid = (widest < ctas ? widest : ctas) * cg;
+    // Kernels of small matrices beside this one need SMs of their own: it starts when all of its CTAs fit.
+    const int beside = h->small.n_part + h->resident.n_resident, spare = beside * 4 < ctas ? beside : ctas / 4;
+    const int most = ctas - (spare + cg - 1) / cg;
+    G.grid = (widest < most ? widest : most) * cg;
     return CSER_OK;
 }
 
@@ -1105,20 +1108,6 @@ int cser_orth_apply(cser_orth_handle h, const void *grad, float *m, float mu, vo
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const bool both = !h->groups.empty() && (h->resident.tables || h->small.tables);
     cudaStream_t small_st = both ? h->side : st;
-    if (both) {
-        TRY(cudaEventRecord(h->fork, st));
-        TRY(cudaStreamWaitEvent(small_st, h->fork, 0));
-    }
-    for (const cser_orth::Small *S : {&h->resident, &h->small}) {
-        if (!S->tables) continue;
-        SmallArgs a = S->args;
-        a.grad = grad, a.m = m, a.mu = mu, a.out = out;
-        const cudaError_t e = h->in_type == CSER_TYPE_F32    ? small_launch<float>(*S, a, small_st)
-                              : h->in_type == CSER_TYPE_BF16 ? small_launch<__nv_bfloat16>(*S, a, small_st)
-                                                             : small_launch<__half>(*S, a, small_st);
-        TRY(e);
-        h->launches += S->n_resident ? 1 : 2;
-    }
     for (cser_orth::Group &G : h->groups) {
         OrthArgs a = G.args;
         a.grad = grad, a.m = m, a.mu = mu, a.out = out;
@@ -1128,11 +1117,26 @@ int cser_orth_apply(cser_orth_handle h, const void *grad, float *m, float mu, vo
                         : h->in_type == CSER_TYPE_BF16 ? prologue_launch<__nv_bfloat16>(G, a, st)
                                                        : prologue_launch<__half>(G, a, st);
         TRY(e);
+        // The small matrices' kernels follow the last group's products in time, onto the SMs that those leave: the other way round the
+        // products, whose CTAs start together or not at all, waited for them.
+        const bool fork = both && &G == &h->groups.back();
+        if (fork) TRY(cudaEventRecord(h->fork, st));
         if (G.mode == kNarrow) e = h->split ? products_launch<kNarrow, true>(a, G.grid, st) : products_launch<kNarrow, false>(a, G.grid, st);
         else if (G.mode == kSingle) e = h->split ? products_launch<kSingle, true>(a, G.grid, st) : products_launch<kSingle, false>(a, G.grid, st);
         else e = h->split ? products_launch<kPaired, true>(a, G.grid, st) : products_launch<kPaired, false>(a, G.grid, st);
         TRY(e);
         h->launches += 3;
+    }
+    if (both) TRY(cudaStreamWaitEvent(small_st, h->fork, 0));
+    for (const cser_orth::Small *S : {&h->resident, &h->small}) {
+        if (!S->tables) continue;
+        SmallArgs a = S->args;
+        a.grad = grad, a.m = m, a.mu = mu, a.out = out;
+        const cudaError_t e = h->in_type == CSER_TYPE_F32    ? small_launch<float>(*S, a, small_st)
+                              : h->in_type == CSER_TYPE_BF16 ? small_launch<__nv_bfloat16>(*S, a, small_st)
+                                                             : small_launch<__half>(*S, a, small_st);
+        TRY(e);
+        h->launches += S->n_resident ? 1 : 2;
     }
     h->stall_mcycles = 0;
     if (both) {
