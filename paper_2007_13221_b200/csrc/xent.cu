@@ -34,8 +34,10 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLowest = -1e30f;                  // below every logit, and finite times log2(e)
 constexpr size_t kPieceBytes = 256ull << 20;
 // The tensor cores truncate every partial sum: 1.2e-6 of a logit over an inner dimension of 1024 (2.5e-6 of a small loss), 3e-6
-// over 4096.  Above 256 the loss's accumulators are taken out and added up, rounded, after this many stages (an inner dimension of 256).
-constexpr int kLossChunk = 4;
+// over 4096.  So the loss's accumulators are taken out and added up, rounded, after this many stages: an inner dimension of 256
+// for few tokens, where memory is the bound, of 512 for many (of 256 the epilogue cannot keep up: tensor cores 73 % busy
+// instead of 85 % at 2048 tokens x 16384 x 4096).
+__host__ __device__ constexpr int loss_chunk(int cg) { return cg == 1 ? 4 : 8; }
 constexpr int kOwnRatio = 256;                     // tokens of a worker up to which every warp finds the largest |dloss| itself
 constexpr int kJoinRows = 20;                     // rows that the last CTA joins itself, one per warp
 
@@ -130,7 +132,7 @@ struct LogitsJob {
     }
     __device__ __forceinline__ bool ready(Pipe<CG> &, const Tile &) const { return true; }
     __device__ __forceinline__ bool chunk_ends(const Tile &t, int k) const {
-        return k + 1 == t.stages || (LONG && (k + 1) % kLossChunk == 0);
+        return k + 1 == t.stages || (LONG && (k + 1) % loss_chunk(CG) == 0);
     }
     __device__ __forceinline__ int bf16() const { return a.bf16; }
     struct Loader {
@@ -160,7 +162,7 @@ struct LogitsJob {
         uint32_t tmem;
         if constexpr (!GRAD) {
             float v[LONG ? 2 : 1][32];                               // all 64 columns, or 32 at a time
-            const int chunks = LONG ? (t.stages + kLossChunk - 1) / kLossChunk : 1;
+            const int chunks = LONG ? (t.stages + loss_chunk(CG) - 1) / loss_chunk(CG) : 1;
             for (int c = 0; c < chunks; ++c) {
                 if (!p.take(turn, tmem)) return false;
                 if (!LONG) break;
@@ -686,7 +688,7 @@ cudaError_t kernels_setup() {
 template <int CG>
 int loss_launch(cser_xent *h, XentArgs &a, bool packed, cudaStream_t st) {
     a.token_tiles = (int)(up(a.tokens, 128 * CG) / (128 * CG)), a.piece0 = 0, a.piece_n = a.vocab;
-    const auto kernel = a.dim > kLossChunk * kStageK ? xent_logits_kernel<CG, kLongLoss> : xent_logits_kernel<CG, kLoss>;
+    const auto kernel = a.dim > loss_chunk(CG) * kStageK ? xent_logits_kernel<CG, kLongLoss> : xent_logits_kernel<CG, kLoss>;
     TRY((tiles_launch<CG>(h, kernel, Pipe<CG>::kSharedBytes, (long long)a.n * a.token_tiles * ((a.vocab + 255) / 256), packed, st, a)));
     if ((long long)a.n * a.tokens > kJoinRows) {
         TRY(launch_kernel(xent_join_kernel, (unsigned)(((long long)a.n * a.tokens + 31) / 32), 1024, 0, 1, true, st, a));
