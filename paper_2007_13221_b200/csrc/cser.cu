@@ -22,6 +22,7 @@
 #include <stdarg.h>
 #include <string.h>
 #include <math.h>
+#include <mutex>
 #include <new>
 
 #include "cser.h"
@@ -658,6 +659,49 @@ int cser_internal_fail(int code, const char *fmt, ...) {
     return code;
 }
 int cser_internal_check_ptr(const void *p, const char *what) { return check_device_ptr(p, what); }
+
+namespace {
+// Pages of words for kernels to report in, 64 bytes apart; kept for the life of the process.
+constexpr int kWordsPerPage = 64, kWordStep = 16;
+struct WordPage {
+    unsigned *base;
+    uint64_t taken;
+    WordPage *next;
+};
+WordPage *g_pages = nullptr;
+std::mutex g_pages_lock;
+}  // namespace
+
+cudaError_t cser_internal_take_word(unsigned **host, unsigned **device) {
+    std::lock_guard<std::mutex> hold(g_pages_lock);
+    WordPage *p = g_pages;
+    while (p && p->taken == ~0ull) p = p->next;
+    if (!p) {
+        p = new (std::nothrow) WordPage{nullptr, 0, g_pages};
+        if (!p) return cudaErrorMemoryAllocation;
+        const cudaError_t e = cudaHostAlloc(reinterpret_cast<void **>(&p->base), kWordsPerPage * kWordStep * sizeof(unsigned),
+                                            cudaHostAllocMapped | cudaHostAllocPortable);
+        if (e != cudaSuccess) {
+            delete p;
+            return e;
+        }
+        g_pages = p;
+    }
+    int k = 0;
+    while (p->taken >> k & 1) ++k;
+    unsigned *w = p->base + k * kWordStep;
+    *w = 0;
+    const cudaError_t e = cudaHostGetDevicePointer(reinterpret_cast<void **>(device), w, 0);
+    if (e != cudaSuccess) return e;
+    p->taken |= 1ull << k;
+    *host = w;
+    return cudaSuccess;
+}
+void cser_internal_give_word(unsigned *host) {
+    std::lock_guard<std::mutex> hold(g_pages_lock);
+    for (WordPage *p = g_pages; p; p = p->next)
+        if (host >= p->base && host < p->base + kWordsPerPage * kWordStep) p->taken &= ~(1ull << ((host - p->base) / kWordStep));
+}
 
 extern "C" {
 

@@ -787,7 +787,6 @@ int orth_fail(cser_orth *h, int code, const char *what) {
 struct HostMat {
     long long offset, rows, cols, stride;
     float scale;
-    int worker;
 };
 
 // Padded dimensions and workspace of one matrix.
@@ -954,6 +953,7 @@ template <typename T>
 cudaError_t small_setup(const cser_orth::Small &S) {
     cudaError_t e = cudaFuncSetAttribute(orth_gram_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S.gram_shared);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(orth_apply_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S.apply_shared);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(orth_resident_kernel<T, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S.resident_shared);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(orth_resident_kernel<T, 4>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S.resident_shared);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(orth_resident_kernel<T, 8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S.resident_shared);
     return e;
@@ -961,7 +961,7 @@ cudaError_t small_setup(const cser_orth::Small &S) {
 template <typename T>
 cudaError_t small_launch(const cser_orth::Small &S, const SmallArgs &a, cudaStream_t st) {
     if (S.n_resident) {
-        return launch_kernel(S.side <= 32 ? orth_resident_kernel<T, 4> : orth_resident_kernel<T, 8>, (unsigned)S.n_resident, 256, S.resident_shared,
+        return launch_kernel(S.side <= 16 ? orth_resident_kernel<T, 2> : S.side <= 32 ? orth_resident_kernel<T, 4> : orth_resident_kernel<T, 8>, (unsigned)S.n_resident, 256, S.resident_shared,
                              1, false, st, a);
     }
     cudaError_t e = launch_kernel(orth_gram_kernel<T>, (unsigned)S.n_part, 256, S.gram_shared, 1, false, st, a);
@@ -991,7 +991,6 @@ cser_orth_handle cser_orth_create(int32_t n_workers, int64_t ld, int32_t n_matri
     std::vector<HostMat> all, small;
     cser_orth *h = nullptr;
     try {
-        std::vector<std::pair<long long, long long>> span;
         for (int k = 0; k < n_matrices; ++k) {
             const long long st = row_stride ? row_stride[k] : cols[k];
             if (rows[k] < 1 || cols[k] < 1 || rows[k] > 65536 || cols[k] > 65536) return bad("rows and cols must be in 1..65536");
@@ -1003,7 +1002,7 @@ cser_orth_handle cser_orth_create(int32_t n_workers, int64_t ld, int32_t n_matri
         for (int w = 0; w < n_workers; ++w)
             for (int k = 0; k < n_matrices; ++k)
                 (rows[k] <= kSmallSide || cols[k] <= kSmallSide ? small : all).push_back({(long long)w * ld + offset[k], rows[k], cols[k], row_stride ? row_stride[k] : cols[k],
-                               scale ? scale[k] : 1.f, w});
+                               scale ? scale[k] : 1.f});
         h = new cser_orth;
         h->in_type = in_type, h->out_type = out_type, h->split = out_type == CSER_TYPE_F32;
         if (cudaGetDevice(&h->device) != cudaSuccess) {
@@ -1061,9 +1060,8 @@ cser_orth_handle cser_orth_create(int32_t n_workers, int64_t ld, int32_t n_matri
             if (er == cudaSuccess) er = cudaEventCreateWithFlags(&h->fork, cudaEventDisableTiming);
             if (er == cudaSuccess) er = cudaEventCreateWithFlags(&h->join, cudaEventDisableTiming);
         }
-        if (er == cudaSuccess) er = cudaHostAlloc(reinterpret_cast<void **>(&h->err_host), 64, cudaHostAllocMapped | cudaHostAllocPortable);
         unsigned *err_dev = nullptr;
-        if (er == cudaSuccess) *h->err_host = 0, er = cudaHostGetDevicePointer(reinterpret_cast<void **>(&err_dev), h->err_host, 0);
+        if (er == cudaSuccess) er = cser_internal_take_word(&h->err_host, &err_dev);
         if (er != cudaSuccess) {
             orth_fail(h, er == cudaErrorMemoryAllocation ? CSER_ERR_NOMEM : CSER_ERR_CUDA, cudaGetErrorString(er));
             return nullptr;
@@ -1156,7 +1154,7 @@ void cser_orth_destroy(cser_orth_handle h) {
     if (h->small.tables) cudaFree(h->small.tables);
     if (h->resident.tables) cudaFree(h->resident.tables);
     if (h->work) cudaFree(h->work);
-    if (h->err_host) cudaFreeHost(h->err_host);
+    if (h->err_host) cser_internal_give_word(h->err_host);
     delete h;
 }
 

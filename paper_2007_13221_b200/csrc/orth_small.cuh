@@ -314,9 +314,9 @@ __host__ __device__ constexpr size_t resident_bytes(int sp, long long l) {
 }
 constexpr size_t kResidentMost = 224 * 1024;
 
-// MOST: eighths of the short side at most.
+// MOST: eighths of the short side at most (2, 4, 8).
 template <typename T, int MOST>
-__global__ void __launch_bounds__(256, MOST == 4 ? 3 : 2) orth_resident_kernel(const SmallArgs a) {
+__global__ void __launch_bounds__(256, MOST == 8 ? 2 : 3) orth_resident_kernel(const SmallArgs a) {
     extern __shared__ __align__(16) double sh[];
     const SmallMat M = a.mats[blockIdx.x];
     const int sp = M.sp, sq = square_ld(sp), ld = resident_ld(sp), cols = (M.l + 15) / 16 * 16, eighths = sp / 8;
@@ -383,21 +383,24 @@ __global__ void __launch_bounds__(256, MOST == 4 ? 3 : 2) orth_resident_kernel(c
         if (j <= i) A[i * sq + j] = A[j * sq + i] = s;
     }
     __syncthreads();
-    Q = small_steps<MOST == 4 ? 2 : 5>(A, P, Q, W, sp, a.steps);
-    // out = scale Q u: a warp takes 16 columns and puts the results where they were.
-    for (int c = warp * 16; c < cols; c += 128) {
-        double acc[MOST][2][2] = {};
+    Q = small_steps<MOST == 8 ? 5 : MOST == 4 ? 2 : 1>(A, P, Q, W, sp, a.steps);
+    // out = scale Q u: a warp takes 16 columns (32 for the shortest sides: more chains at once) and puts the results where they were.
+    constexpr int kCols = MOST == 2 ? 4 : 2;
+    for (int c = warp * kCols * 8; c < cols; c += kCols * 64) {
+        double acc[MOST][kCols][2] = {};
 #pragma unroll 2
         for (int k = 0; k < sp; k += 4) {
             const float *row = u + (c + lane / 4) * ld + k + lane % 4;
-            const double b0 = (double)row[0], b1 = (double)row[8 * ld];
+            double f[kCols];
+#pragma unroll
+            for (int h = 0; h < kCols; ++h) f[h] = c + h * 8 < cols ? (double)row[h * 8 * ld] : 0.0;
             const double *col = Q + lane / 4 * sq + k + lane % 4;
 #pragma unroll
             for (int t = 0; t < MOST; ++t)
                 if (t * 8 < sp) {
                     const double v = col[t * 8 * sq];
-                    mma_f64(acc[t][0], v, b0);
-                    mma_f64(acc[t][1], v, b1);
+#pragma unroll
+                    for (int h = 0; h < kCols; ++h) mma_f64(acc[t][h], v, f[h]);
                 }
         }
         __syncwarp();
@@ -405,10 +408,11 @@ __global__ void __launch_bounds__(256, MOST == 4 ? 3 : 2) orth_resident_kernel(c
         for (int t = 0; t < MOST; ++t)
             if (t * 8 < sp)
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
+                for (int h = 0; h < kCols; ++h)
 #pragma unroll
                     for (int p = 0; p < 2; ++p)
-                        u[(c + h * 8 + lane % 4 * 2 + p) * ld + t * 8 + lane / 4] = (float)(acc[t][h][p] * (double)M.scale);
+                        if (c + h * 8 < cols)
+                            u[(c + h * 8 + lane % 4 * 2 + p) * ld + t * 8 + lane / 4] = (float)(acc[t][h][p] * (double)M.scale);
     }
     __syncthreads();
 #pragma unroll 2

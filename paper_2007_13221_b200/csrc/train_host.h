@@ -1,5 +1,6 @@
 // train_host.h - what the translation units of libcser.so share on the host (defined in cser.cu).
 #pragma once
+#include <cuda_runtime.h>
 #include <stdint.h>
 #include "cser.h"
 
@@ -8,3 +9,8 @@ __attribute__((visibility("hidden"))) int cser_internal_fail(int code, const cha
     __attribute__((format(printf, 2, 3)));
 // CSER_OK if p is memory of the current device.
 __attribute__((visibility("hidden"))) int cser_internal_check_ptr(const void *p, const char *what);
+
+// A word of mapped pinned memory, 0, for kernels to report a wait that ran out in: its host and its device address.  From a page that
+// the process keeps (pinning one per handle took 2 ms of a handle's 2.8).
+__attribute__((visibility("hidden"))) cudaError_t cser_internal_take_word(unsigned **host, unsigned **device);
+__attribute__((visibility("hidden"))) void cser_internal_give_word(unsigned *host);

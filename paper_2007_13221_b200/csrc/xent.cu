@@ -778,8 +778,7 @@ cser_xent_handle cser_xent_create(int32_t n_workers, int64_t max_tokens, int64_t
         if (e == cudaSuccess) e = cudaMalloc(&h->pack_h, (size_t)rows * up(dim, 8) * 2);
         if (e == cudaSuccess) e = cudaMalloc(&h->pack_w, (size_t)n_workers * vocab * up(dim, 8) * 2);
     }
-    if (e == cudaSuccess) e = cudaHostAlloc(reinterpret_cast<void **>(&h->err_host), 64, cudaHostAllocMapped | cudaHostAllocPortable);
-    if (e == cudaSuccess) *h->err_host = 0, e = cudaHostGetDevicePointer(reinterpret_cast<void **>(&h->err_dev), h->err_host, 0);
+    if (e == cudaSuccess) e = cser_internal_take_word(&h->err_host, &h->err_dev);
     if (e != cudaSuccess) return drop(e);
     char *w = static_cast<char *>(h->work);
     h->ticket = reinterpret_cast<unsigned *>(w + o_tick);
@@ -840,7 +839,7 @@ void cser_xent_destroy(cser_xent_handle h) {
     if (!h) return;
     for (void *p : {h->work, h->pack_h, h->pack_w})
         if (p) cudaFree(p);
-    if (h->err_host) cudaFreeHost(h->err_host);
+    if (h->err_host) cser_internal_give_word(h->err_host);
     delete h;
 }
 
