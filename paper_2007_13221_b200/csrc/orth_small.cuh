@@ -76,20 +76,22 @@ __device__ __forceinline__ void triangle(int k, int &i, int &j) {
     while (i * (i + 1) / 2 > k) --i;
     j = k - i * (i + 1) / 2;
 }
-// A warp's 8 x 8 tiles of one triangle of an s x s matrix: every eighth one, at most N.
+// A warp's 8 x 8 tiles of one triangle of an s x s matrix, at most N: a run of them row by row, so that most share the fragment
+// of the row with the one before.
 template <int N>
 struct WarpTiles {
     int i[N], j[N], n = 0;                                           // this lane's row of either operand's fragment
+    bool fresh[N];                                                   // another row of tiles than the one before
     __device__ __forceinline__ explicit WarpTiles(int sp) {
         const int side = sp / 8, tiles = side * (side + 1) / 2, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+        const int each = tiles / 8, more = tiles % 8, first = warp * each + (warp < more ? warp : more);
+        n = each + (warp < more);
 #pragma unroll
         for (int b = 0; b < N; ++b) {
             i[b] = j[b] = 0;
-            if (warp + 8 * b < tiles) {
-                triangle(warp + 8 * b, i[b], j[b]);
-                ++n;
-            }
+            if (b < n) triangle(first + b, i[b], j[b]);
             i[b] = i[b] * 8 + lane / 4, j[b] = j[b] * 8 + lane / 4;
+            fresh[b] = b == 0 || i[b] != i[b > 0 ? b - 1 : 0];
         }
     }
 };
@@ -101,12 +103,17 @@ __device__ __forceinline__ void sym_product(double *out, const double *x, const 
     const int ld = square_ld(sp), k = threadIdx.x % 4;
     double c[N][2][2] = {};
 #pragma unroll 2
-    for (int e = 0; e < sp; e += 8)
+    for (int e = 0; e < sp; e += 8) {
+        double u[2] = {};
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int b = 0; b < N; ++b)
-                if (b < w.n) mma_f64(c[b][h], x[w.i[b] * ld + k + e + 4 * h], y[w.j[b] * ld + k + e + 4 * h]);
+        for (int b = 0; b < N; ++b)
+            if (b < w.n) {
+                if (w.fresh[b]) u[0] = x[w.i[b] * ld + k + e], u[1] = x[w.i[b] * ld + k + e + 4];
+                const double v0 = y[w.j[b] * ld + k + e], v1 = y[w.j[b] * ld + k + e + 4];
+                mma_f64(c[b][0], u[0], v0);
+                mma_f64(c[b][1], u[1], v1);
+            }
+    }
 #pragma unroll
     for (int b = 0; b < N; ++b)
         if (b < w.n)
@@ -354,33 +361,53 @@ __global__ void __launch_bounds__(256, MOST == 8 ? 2 : 3) orth_resident_kernel(c
         for (int k = 0; k < 8; ++k) o[M.tall ? k : k * ld] = v[k];
     }
     __syncthreads();
-    // Gram matrix: few tiles are shared out among the warps by columns, in `groups`; of many a warp has every eighth one.
-    const int room = 3 * sp * sq / (tiles * 64), groups = tiles >= 8 ? 1 : 8 / tiles < room ? 8 / tiles : room, group = tiles >= 8 ? 0 : warp / tiles, tile0 = tiles >= 8 ? warp : warp % tiles;
-    for (int b = tile0; b < tiles && group < groups; b += 8) {
-        int ti, tj;
-        triangle(b, ti, tj);
-        double acc[4][2] = {};
-        const float *row = u + (group * 4 + lane % 4) * ld + lane / 4;
-        const int step = groups * 4 * ld;
-        int c = group * 4;
-        for (; c + groups * 12 < cols; c += groups * 16, row += 4 * step)
+    if (tiles >= 8) {                                                // Gram matrix: a warp's tiles side by side, each a chain
+        constexpr int kMost = MOST == 8 ? 5 : 2;
+        const WarpTiles<kMost> w(sp);
+        double acc[kMost][2] = {};
+        const float *row = u + lane % 4 * ld;
+#pragma unroll 4
+        for (int c = 0; c < cols; c += 4, row += 4 * ld)
 #pragma unroll
-            for (int h = 0; h < 4; ++h) mma_f64(acc[h], (double)row[h * step + ti * 8], (double)row[h * step + tj * 8]);
-        for (; c < cols; c += groups * 4, row += step) mma_f64(acc[0], (double)row[ti * 8], (double)row[tj * 8]);
-        // over P, Q and W: the groups' sums one after the other
-        double *o = P + (group * tiles + b) * 64 + lane * 2;
+            for (int b = 0; b < kMost; ++b)
+                if (b < w.n) mma_f64(acc[b], (double)row[w.i[b]], (double)row[w.j[b]]);
 #pragma unroll
-        for (int q = 0; q < 2; ++q) o[q] = (acc[0][q] + acc[1][q]) + (acc[2][q] + acc[3][q]);
-    }
-    __syncthreads();
-    for (int e = threadIdx.x; e < tiles * 64; e += 256) {
-        const int k = e / 64, w = e - k * 64;
-        int bi, bj;
-        triangle(k, bi, bj);
-        double s = 0.0;
-        for (int q = 0; q < groups; ++q) s += P[q * tiles * 64 + e];
-        const int i = bi * 8 + w / 8, j = bj * 8 + w % 8;
-        if (j <= i) A[i * sq + j] = A[j * sq + i] = s;
+        for (int b = 0; b < kMost; ++b)
+            if (b < w.n) {
+                const int i = w.i[b], j = w.j[b] / 8 * 8 + lane % 4 * 2;
+#pragma unroll
+                for (int q = 0; q < 2; ++q)
+                    if (j + q <= i) A[i * sq + j + q] = A[(j + q) * sq + i] = acc[b][q];
+            }
+    } else {                                                         // few tiles: shared out by columns too, in `groups`, four chains
+        const int room = 3 * sp * sq / (tiles * 64), groups = 8 / tiles < room ? 8 / tiles : room;
+        if (warp / tiles < groups) {
+            const int b = warp % tiles, group = warp / tiles;
+            int ti, tj;
+            triangle(b, ti, tj);
+            double acc[4][2] = {};
+            const float *row = u + (group * 4 + lane % 4) * ld + lane / 4;
+            const int step = groups * 4 * ld;
+            int c = group * 4;
+            for (; c + groups * 12 < cols; c += groups * 16, row += 4 * step)
+#pragma unroll
+                for (int h = 0; h < 4; ++h) mma_f64(acc[h], (double)row[h * step + ti * 8], (double)row[h * step + tj * 8]);
+            for (; c < cols; c += groups * 4, row += step) mma_f64(acc[0], (double)row[ti * 8], (double)row[tj * 8]);
+            // over P, Q and W: the groups' sums one after the other
+            double *o = P + (group * tiles + b) * 64 + lane * 2;
+#pragma unroll
+            for (int q = 0; q < 2; ++q) o[q] = (acc[0][q] + acc[1][q]) + (acc[2][q] + acc[3][q]);
+        }
+        __syncthreads();
+        for (int e = threadIdx.x; e < tiles * 64; e += 256) {
+            const int k = e / 64, w = e - k * 64;
+            int bi, bj;
+            triangle(k, bi, bj);
+            double s = 0.0;
+            for (int q = 0; q < groups; ++q) s += P[q * tiles * 64 + e];
+            const int i = bi * 8 + w / 8, j = bj * 8 + w % 8;
+            if (j <= i) A[i * sq + j] = A[j * sq + i] = s;
+        }
     }
     __syncthreads();
     Q = small_steps<MOST == 8 ? 5 : MOST == 4 ? 2 : 1>(A, P, Q, W, sp, a.steps);

@@ -46,7 +46,8 @@ def far(got, want):
 
 
 SHAPES = [(1, 1), (1, 77), (77, 1), (2, 3), (16, 1024), (1024, 16), (64, 64), (63, 65), (127, 129), (128, 128), (129, 127),
-          (128, 256), (256, 128), (257, 640), (640, 257), (300, 1500), (1100, 513), (1, 5000)]
+          (128, 256), (256, 128), (257, 640), (640, 257), (300, 1500), (1100, 513), (1, 5000),
+          (8, 200), (9, 40), (24, 24), (200, 25), (32, 33), (40, 500), (48, 48), (56, 300), (64, 4000)]
 
 
 @pytest.mark.gpu
