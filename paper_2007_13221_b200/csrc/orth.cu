@@ -321,7 +321,7 @@ struct OrthJob {
     static constexpr int CG = mode_cg(MODE), TN = tile_n(MODE, SPLIT), kSums = SPLIT ? TN / 64 : 1;
     const OrthArgs &a;
     int first, every;
-    static constexpr bool kCopier = true;
+    static constexpr bool kCopier = true, kRemainders = false;
 
     struct Tile {
         int n, stages, a_lim, b_lim;

@@ -364,6 +364,8 @@ struct Pipe {
     //   int bf16()
     //   bool epilogue(pipe, tile, turn, warp, lane)   warp 0..15: for each chunk take(), read its columns, release();
     //                              false once a wait was.  Its warps do not wait for one another but on bounded barriers
+    //   kRemainders; bool remainders()   whether rows 32..63 of the first operand are what rounding left of its rows 0..31, which are all
+    //              there are: they meet the second operand's same 16 bits, with no copy and no stage of their own
     //   kCopier; bool copier(pipe)  a thread of its own for what the epilogue brings and takes away through shared memory; walks the
     //                              tiles itself
     template <class Job>
@@ -435,9 +437,21 @@ struct Pipe {
                     const uint64_t db = (b_mn ? operand_desc(true) : operand_desc(false)) + at + (kABytes >> 4);
                     const uint32_t sa = operand_step(a_mn), sb = operand_step(b_mn);
                     const uint32_t di = id | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16);
+                    bool lows = false;
+                    if constexpr (Job::kRemainders) lows = job.remainders();
+                    if (lows) {
+                        const uint32_t lo = a_mn ? 2 * sa : 32 * 128 / 16;   // MN-major: 32 on in the inner dimension; K-major: 32 rows on
 #pragma unroll
-                    for (int e = 0; e < kStageK / 16; ++e)
-                        mma_f16<CG>(d, da + e * sa, db + e * sb, di, e == 0 ? !fresh : 1);
+                        for (int e = 0; e < kStageK / 16; ++e) {
+                            if (a_mn && e >= 2) break;
+                            mma_f16<CG>(d, da + e * sa, db + e * sb, di, e == 0 ? !fresh : 1);
+                            mma_f16<CG>(d, da + lo + e * sa, db + e * sb, di, 1);
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < kStageK / 16; ++e)
+                            mma_f16<CG>(d, da + e * sa, db + e * sb, di, e == 0 ? !fresh : 1);
+                    }
                     if (PAIR) {
                         constexpr uint32_t lo = kLoOffset >> 4;
 #pragma unroll

@@ -14,6 +14,8 @@
 // Rounding.  dz is rounded to the operands' type, 8 (bf16) or 11 (fp16) bits, as any product on these inputs has to.
 // It is held relative to the worker's largest |dloss| (times 2^12 for fp16, whose smallest normal number is above 1 / V for a
 // large vocabulary) and the factor is put back in fp32 at the end: for a mean over tokens dz is p - [target] itself, not p / T rounded.
+// Up to 32 tokens, where a single rounding (of p - 1 at the target) can be most of a result's error, what it left is kept too, in
+// rows that are padding otherwise: no more bytes, no more stages.
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <cuda_bf16.h>
@@ -109,6 +111,24 @@ __global__ void __launch_bounds__(1024) xent_ratio_kernel(const __grid_constant_
     for (int t = threadIdx.x; t < a.tokens; t += 1024) a.ratio[base + t] = row_ratio(a, base + t, top);
 }
 
+constexpr int kLowRows = 32;                       // tokens of a worker up to which dz keeps what its rounding left
+// What 8 values have beyond their 16-bit forms `o`, in 16 bits.
+__device__ __forceinline__ uint4 remainder8(const float *v, const uint4 &o, int bf16) {
+    const uint32_t w[4] = {o.x, o.y, o.z, o.w};
+    uint32_t r[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        if (bf16) {
+            const float2 b = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(&w[k]));
+            r[k] = pack_bf162(v[2 * k] - b.x, v[2 * k + 1] - b.y);
+        } else {
+            const float2 b = __half22float2(*reinterpret_cast<const __half2 *>(&w[k]));
+            r[k] = pack_half2(v[2 * k] - b.x, v[2 * k + 1] - b.y);
+        }
+    }
+    return make_uint4(r[0], r[1], r[2], r[3]);
+}
+
 // ------------------------------------------------------------------ logits, tile by tile
 // What the tiles of z are for: a loss, a loss over a long inner dimension (chunks), dz.
 enum { kLoss = 0, kLongLoss = 1, kGrad = 2 };
@@ -117,7 +137,7 @@ struct LogitsJob {
     static constexpr bool GRAD = WHAT == kGrad, LONG = WHAT == kLongLoss;
     const XentArgs &a;
     int first, every, vocab_tiles;
-    static constexpr bool kCopier = false;
+    static constexpr bool kCopier = false, kRemainders = false;
 
     struct Tile {
         int w, i, j, n, stages, a_lim, b_lim;
@@ -224,6 +244,7 @@ struct LogitsJob {
             if (live) lse = a.lse[at];
             if (!p.take(turn, tmem)) return false;
             char *dz = a.dz + (size_t)t.w * a.dz_worker;
+            const bool lows = CG == 1 && a.tokens <= kLowRows;
 #pragma unroll 1
             for (int b = 0; b < 64; b += 32) {
                 const int in = t.j * 256 + c0 + b, col = a.piece0 + in;
@@ -251,7 +272,13 @@ struct LogitsJob {
                         o = make_uint4(pack_bf162(e[0], e[1]), pack_bf162(e[2], e[3]), pack_bf162(e[4], e[5]), pack_bf162(e[6], e[7]));
                     else
                         o = make_uint4(pack_half2(e[0], e[1]), pack_half2(e[2], e[3]), pack_half2(e[4], e[5]), pack_half2(e[6], e[7]));
-                    *reinterpret_cast<uint4 *>(dz + (size_t)(in / 64) * a.tp * 128 + panel_chunk(row, in % 64 / 8 + k)) = o;
+                    char *to = dz + (size_t)(in / 64) * a.tp * 128 + panel_chunk(row, in % 64 / 8 + k);
+                    if (!lows || row >= 64) {
+                        *reinterpret_cast<uint4 *>(to) = o;
+                    } else if (row < 32) {
+                        *reinterpret_cast<uint4 *>(to) = o;
+                        *reinterpret_cast<uint4 *>(to + 32 * 128) = remainder8(e, o, a.bf16);
+                    }
                 }
             }
         }
@@ -350,7 +377,8 @@ struct GradJob {
     using P = GradPipe<CG>;
     const XentArgs &a;
     int first, every, n_dh, n_dw, dim_tiles, vocab_tiles, early;
-    static constexpr bool kCopier = false;
+    static constexpr bool kCopier = false, kRemainders = CG == 1;
+    __device__ __forceinline__ bool remainders() const { return a.tokens <= kLowRows; }
 
     struct Tile {
         int w, i, j, n, stages, a_lim, b_lim, k0, split, dw;

@@ -94,6 +94,35 @@ def test_against_the_formula(size, dtype):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [BF, HF], ids=str)
+@pytest.mark.parametrize("size", [(1, 1, 134, 279), (4, 1, 1000, 64), (1, 17, 700, 520), (2, 31, 2000, 136), (1, 32, 5000, 264)], ids=str)
+def test_few_tokens_round_once(size, dtype):
+    """Up to 32 tokens dz keeps what its rounding left: u^2 |dz| in place of u |dz|, and the truncation of the products'
+    partial sums, 2^-23 of the sum of magnitudes for each of two per 16 of the inner dimension, no longer vanishes beside it."""
+    n, t, v, d = size
+    h, w, y, dloss = inputs(n, t, v, d, dtype)
+    op = train.LinearCrossEntropy(n, 40, v, d, dtype)
+    loss, lse, dh, dw = check(op, h, w, y, dloss, dtype)
+    u, tiny = (2.0 ** -8, 0.0) if dtype == BF else (2.0 ** -11, 2.0 ** -25)
+    for i in range(n):
+        hi, wi = h[i].double(), w[i].double()
+        ok = y[i] != IGN
+        z = hi @ wi.t()
+        l = torch.logsumexp(z, 1)[:, None]
+        p = torch.exp(z - l)
+        dz = p.clone()
+        dz[torch.arange(t, device="cuda"), torch.where(ok, y[i], 0)] -= 1
+        g = (dloss[i].double() * ok)[:, None]
+        dz *= g
+        off = 2e-5 * (1 + l.abs()) * p * g.abs() + 2.0 ** -37 * g.abs().max()
+        for got, mine, other, of in ((dh[i], dz, wi, off), (dw[i], dz.t(), hi, off.t())):
+            sums = 2.0 ** -23 * 2 * (mine.shape[1] // 16 + 1)
+            want = mine @ other
+            bound = 1.1 * ((of + (u * u + sums) * mine.abs()) @ other.abs() + u * want.abs() + tiny)
+            assert bool(((got.double() - want).abs() <= bound).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, HF], ids=str)
 @pytest.mark.parametrize("piece", [1, 256, 512, 1024])
 def test_pieces_of_the_vocabulary(piece, dtype):
     n, t, v, d = 2, 200, 1700, 136
