@@ -90,6 +90,12 @@ __device__ __forceinline__ void tensor_copy_in(uint32_t dst, const CUtensorMap *
         "l"(map), "r"(smem_addr(bar)), "r"(col), "r"(row), "r"(worker)
         : "memory");
 }
+// The same from shared memory, what lies outside the tensor left out; counted in the thread's groups of copies.
+__device__ __forceinline__ void tensor_copy_out(const CUtensorMap *map, uint32_t src, int col, int row, int worker) {
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map), "r"(src), "r"(col),
+                 "r"(row), "r"(worker)
+                 : "memory");
+}
 __device__ __forceinline__ void prefetch_tensor_map(const CUtensorMap *map) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
 }

@@ -75,6 +75,8 @@ struct XentArgs {
     int acc_rows, acc_cols, splits, first_piece, last_piece;
     void *dh, *dw;
     long long dw_stride;
+    CUtensorMap dh_map, dw_map;                    // of the results, boxes of 64 x 32, where
+    int dh_boxes, dw_boxes;                        // these say that their address and rows allow it
     unsigned *err;
 };
 
@@ -359,11 +361,17 @@ __global__ void __launch_bounds__(kThreads, 1) xent_logits_kernel(const __grid_c
         const int row = threadIdx.x / 32, lane = threadIdx.x % 32, rows = a.n * a.tokens;
         if (!last || row >= rows) return;
         float m = kLowest, s = 0.f;
-#pragma unroll 4
-        for (int k = lane; k < a.parts; k += 32) {
-            const float2 q = __ldcg(a.part + (size_t)k * rows + row);
-            const float top = fmaxf(m, q.x);
-            s = s * exp2_fast((m - top) * kLog2e) + q.y * exp2_fast((q.x - top) * kLog2e);
+        for (int k = lane; k < a.parts; k += 32 * 8) {               // 8 on their way at a time: of one row 2048 parts take 5 us, 4 at a time 11
+            float2 q[8];
+            float top = m;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                q[e] = k + 32 * e < a.parts ? __ldcg(a.part + (size_t)(k + 32 * e) * rows + row) : make_float2(kLowest, 0.f);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = fmaxf(top, q[e].x);
+            s *= exp2_fast((m - top) * kLog2e);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s += q[e].y * exp2_fast((q[e].x - top) * kLog2e);
             m = top;
         }
         for (int k = 16; k; k >>= 1) {
@@ -458,6 +466,37 @@ struct GradJob {
                 if (p < boxes) tensor_copy_in(sb + p * 8192, b, col + p * 64, row0 + k * 64, worker, bar);
         }
     };
+    // N columns of a row: dh's share of a piece is added to the earlier ones', what is complete goes, in 16 bits, into the warp's
+    // 4 KB of shared memory, a panel of 32 rows.
+    template <int N>
+    __device__ __forceinline__ void columns(const Tile &t, float (&v)[N], int row, int col, bool live, bool leaves, float f, uint32_t at,
+                                            int lane, int chunk) const {
+        if (!t.dw && (!a.first_piece || !leaves)) {
+            float4 *acc = reinterpret_cast<float4 *>(a.acc + (((size_t)t.w * a.splits + t.split) * a.acc_rows + row) * a.acc_cols + col);
+            if (!a.first_piece && live) {
+#pragma unroll
+                for (int k = 0; k < N / 4; ++k) {
+                    const float4 q = acc[k];
+                    v[4 * k] += q.x, v[4 * k + 1] += q.y, v[4 * k + 2] += q.z, v[4 * k + 3] += q.w;
+                }
+            }
+            if (!leaves) {
+#pragma unroll
+                for (int k = 0; k < N / 4; ++k)
+                    if (live) acc[k] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+                return;
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] *= f;
+#pragma unroll
+        for (int k = 0; k < N / 8; ++k) {
+            const float *e = v + 8 * k;
+            shared_store16(at + panel_chunk(lane, chunk + k),
+                           a.bf16 ? make_uint4(pack_bf162(e[0], e[1]), pack_bf162(e[2], e[3]), pack_bf162(e[4], e[5]), pack_bf162(e[6], e[7]))
+                                  : make_uint4(pack_half2(e[0], e[1]), pack_half2(e[2], e[3]), pack_half2(e[4], e[5]), pack_half2(e[6], e[7])));
+        }
+    }
     __device__ __forceinline__ bool epilogue(P &p, const Tile &t, typename P::Turn &turn, int warp, int lane) const {
         uint32_t tmem;
         const int row0 = t.i * 128 * CG + (int)p.rank * 128 + warp % 4 * 32, row = row0 + lane;
@@ -471,38 +510,40 @@ struct GradJob {
             p.release(turn, lane);
             return true;
         }
+        if (CG == 1) {
+            if (lane == 0) bulk_out_read<0>();                       // the last tile's rows have left the buffer
+            __syncwarp();
+        }
+        if (CG == 1 && quarter == 64) {
 #pragma unroll 1
-        for (int b = 0; b < quarter; b += 16) {
-            float v[16];
-            tmem_load(tmem + c0 + b, v);
-            if (b + 16 >= quarter) p.release(turn, lane);
-            if (!t.dw && (!a.first_piece || !leaves)) {
-                float4 *acc = reinterpret_cast<float4 *>(
-                    a.acc + (((size_t)t.w * a.splits + t.split) * a.acc_rows + row) * a.acc_cols + col0 + b);
-                if (!a.first_piece && lane < rows) {
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const float4 q = acc[k];
-                        v[4 * k] += q.x, v[4 * k + 1] += q.y, v[4 * k + 2] += q.z, v[4 * k + 3] += q.w;
-                    }
-                }
-                if (!leaves) {
-#pragma unroll
-                    for (int k = 0; k < 4 && lane < rows; ++k) acc[k] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
-                    continue;
-                }
+            for (int b = 0; b < 64; b += 32) {
+                float v[32];
+                tmem_load(tmem + c0 + b, v);
+                if (b == 32) p.release(turn, lane);
+                columns(t, v, row, col0 + b, lane < rows, leaves, f, at, lane, b / 8);
             }
-#pragma unroll
-            for (int k = 0; k < 16; ++k) v[k] *= f;
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const float *e = v + 8 * k;
-                shared_store16(at + panel_chunk(lane, b / 8 + k),
-                               a.bf16 ? make_uint4(pack_bf162(e[0], e[1]), pack_bf162(e[2], e[3]), pack_bf162(e[4], e[5]), pack_bf162(e[6], e[7]))
-                                      : make_uint4(pack_half2(e[0], e[1]), pack_half2(e[2], e[3]), pack_half2(e[4], e[5]), pack_half2(e[6], e[7])));
+        } else {
+#pragma unroll 1
+            for (int b = 0; b < quarter; b += 16) {
+                float v[16];
+                tmem_load(tmem + c0 + b, v);
+                if (b + 16 >= quarter) p.release(turn, lane);
+                columns(t, v, row, col0 + b, lane < rows, leaves, f, at, lane, b / 8);
             }
         }
         if (!leaves) return true;
+        // Tiles of dW by single CTAs are one or two stages long, and this is their bound: rows sent off by the copy engine, and 32 columns
+        // at a time, 8 x 16 tokens x 30522 x 1024, gradients 327 -> 293 us.  By pairs, where a tile's products take
+        // longer, it made no difference (8 x 512 tokens 735 us either way), and what follows needs no maps.
+        if (CG == 1 && quarter == 64 && (t.dw ? a.dw_boxes : a.dh_boxes)) {
+            fence_async_shared();
+            __syncwarp();
+            if (lane == 0) {
+                tensor_copy_out(t.dw ? &a.dw_map : &a.dh_map, at, col0, t.dw ? a.piece0 + row0 : row0, t.w);
+                bulk_out_commit();
+            }
+            return true;
+        }
         __syncwarp();
         const int cols = a.dim - col0 < quarter ? a.dim - col0 : quarter;
         uint16_t *o = t.dw ? static_cast<uint16_t *>(a.dw) + t.w * a.dw_stride + (long long)(a.piece0 + row0) * a.dim + col0
@@ -514,12 +555,14 @@ struct GradJob {
                 if (r < rows) *reinterpret_cast<uint4 *>(o + (long long)r * a.dim + c * 8) = shared_load16(at + panel_chunk(r, c));
             }
         } else {
-            for (int r = 0; r < 32 && r < rows; ++r)
-                for (int c = lane; c < cols; c += 32) {
+            for (int c = lane; c < cols; c += 32) {
+#pragma unroll 8
+                for (int r = 0; r < 32; ++r) {
                     uint16_t v;
-                    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(at + panel_chunk(r, c / 8) + c % 8 * 2) : "memory");
-                    o[(long long)r * a.dim + c] = v;
+                    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(at + panel_chunk(r, c / 8) + c % 8 * 2));
+                    if (r < rows) o[(long long)r * a.dim + c] = v;
                 }
+            }
         }
         __syncwarp();
         return true;
@@ -545,6 +588,7 @@ __global__ void __launch_bounds__(kThreads, 1) xent_grad_kernel(const __grid_con
     }
     earlier_done();
     p.run(job);
+    if (CG == 1) bulk_out_done();                  // of the threads that sent results off
     p.teardown();
 }
 
@@ -625,10 +669,12 @@ namespace {
 
 long long up(long long v, long long to) { return (v + to - 1) / to * to; }
 int splits_of(const cser_xent *h, long long tokens) {
-    // Few tiles of dh and a long inner dimension: the vocabulary is split so that every SM has a share, each of 16 stages at least.
+    // Few tiles of dh and a long inner dimension: the vocabulary is split so that every SM has a share, each of 8 stages at least;
+    // fewer than 24 are left whole: joining takes 3 us, as much as 8 stages (2 x 5 tokens x 3000 x 2000, gradients: 40 us by 16, 35 by 8;
+    // 3 x 77 x 1003 x 201, 16 stages: 27 whole, 30 in two).
     const long long tiles = h->n * (up(tokens, 128) / 128) * (up(h->dim, 256) / 256), stages = up(h->piece < h->vocab ? h->piece : h->vocab, 64) / 64;
     long long s = tiles >= h->sms ? 1 : h->sms / tiles;
-    if (s > stages / 16) s = stages / 16;
+    if (s > stages / 8) s = stages < 24 ? 1 : stages / 8;
     return s < 1 ? 1 : (int)s;
 }
 
@@ -738,6 +784,17 @@ int loss_launch(cser_xent *h, XentArgs &a, bool packed, cudaStream_t st) {
         h->launches++;
     }
     return CSER_OK;
+}
+
+// The map of a result that lies dense for each worker; 0: its address or rows do not allow one.
+int result_map(const cser_xent *h, CUtensorMap &m, void *p, long long rows, long long worker_stride) {
+    if (!p || (uintptr_t)p % 16 || h->dim % 8 || (h->n > 1 && worker_stride % 8)) return 0;
+    const cuuint64_t size[3] = {(cuuint64_t)h->dim, (cuuint64_t)rows, (cuuint64_t)h->n};
+    const cuuint64_t stride[2] = {(cuuint64_t)h->dim * 2, (cuuint64_t)(h->n > 1 ? worker_stride : rows * h->dim) * 2};
+    const cuuint32_t box[3] = {64, 32, 1}, step[3] = {1, 1, 1};
+    return h->encode(&m, h->type == CSER_TYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, p, size, stride,
+                     box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <int CG>
@@ -875,7 +932,10 @@ int cser_xent_grad(cser_xent_handle h, const cser_xent_inputs *in, const float *
     if ((uintptr_t)lse % 4 || (uintptr_t)dloss % 4)
         return cser_internal_fail(CSER_ERR_INVALID, "cser_xent_grad: a pointer is not aligned to its element type");
     a.lse = lse, a.dloss = dloss, a.dh = dhidden, a.dw = dweight, a.dw_stride = dweight_stride;
-    return wide_tiles(a.tokens) ? grad_launch<2>(h, a, packed, st) : grad_launch<1>(h, a, packed, st);
+    if (wide_tiles(a.tokens)) return grad_launch<2>(h, a, packed, st);
+    a.dh_boxes = result_map(h, a.dh_map, dhidden, a.tokens, (long long)a.tokens * h->dim);
+    a.dw_boxes = result_map(h, a.dw_map, dweight, h->vocab, dweight_stride);
+    return grad_launch<1>(h, a, packed, st);
 }
 
 void cser_xent_destroy(cser_xent_handle h) {
