@@ -581,7 +581,7 @@ struct Pipe {
 };
 
 // ------------------------------------------------------------------ launches
-// `after`: an earlier kernel of the same call is in the stream, whose end this one may overlap (it calls earlier_done()).
+// `after`: this kernel may be set up while the one before it in the stream, whichever that is, ends (it calls earlier_done()).
 template <typename... P, typename... A>
 cudaError_t launch_kernel(void (*kernel)(P...), unsigned grid, unsigned block, size_t shared, unsigned cluster, bool after, cudaStream_t st,
                           A... args) {

@@ -716,7 +716,7 @@ int operand(cser_xent *h, CUtensorMap &m, int &workers, const void *p, long long
     return CSER_OK;
 }
 
-int prepare_call(cser_xent *h, const cser_xent_inputs *in, const char *what, XentArgs &a, bool &packed, cudaStream_t st) {
+int prepare_call(cser_xent *h, const cser_xent_inputs *in, const char *what, XentArgs &a, cudaStream_t st) {
     if (!h) return cser_internal_fail(CSER_ERR_INVALID, "%s: NULL handle", what);
     if (!in) return cser_internal_fail(CSER_ERR_INVALID, "%s: NULL inputs", what);
     int dev = -1;
@@ -727,7 +727,7 @@ int prepare_call(cser_xent *h, const cser_xent_inputs *in, const char *what, Xen
         return cser_internal_fail(CSER_ERR_CUDA, "a device-side wait ran out in an earlier call: its results are incomplete");
     if (in->tokens < 0 || in->tokens > h->max_tokens)
         return cser_internal_fail(CSER_ERR_INVALID, "%s: tokens must be in 0..%lld", what, h->max_tokens);
-    a = XentArgs{}, packed = false;
+    a = XentArgs{};
     a.n = h->n, a.tokens = (int)in->tokens, a.vocab = (int)h->vocab, a.dim = (int)h->dim;
     if (in->tokens == 0) return CSER_OK;
     if (in->hidden_row_stride < 0 || in->hidden_worker_stride < 0 || in->weight_row_stride < 0 || in->weight_worker_stride < 0)
@@ -744,10 +744,9 @@ int prepare_call(cser_xent *h, const cser_xent_inputs *in, const char *what, Xen
     if (int rc = operand(h, a.w, a.w_workers, in->weight, h->vocab, in->weight_row_stride, in->weight_worker_stride, h->pack_w, h->vocab,
                          pack[1], "weight", st))
         return rc;
-    packed = pack[0].all + pack[1].all > 0;
-    if (packed) {
-        xent_pack_kernel<<<(unsigned)(pack[0].all + pack[1].all), 256, 0, st>>>(pack[0], pack[1], (int)h->dim, (int)up(h->dim, 8));
-        TRY(cudaGetLastError());
+    if (pack[0].all + pack[1].all > 0) {
+        TRY(launch_kernel(xent_pack_kernel, (unsigned)(pack[0].all + pack[1].all), 256, 0, 1, true, st, pack[0], pack[1], (int)h->dim,
+                          (int)up(h->dim, 8)));
         h->launches++;
     }
     a.bf16 = h->type == CSER_TYPE_BF16;
@@ -758,10 +757,10 @@ int prepare_call(cser_xent *h, const cser_xent_inputs *in, const char *what, Xen
 }
 
 template <int CG, typename K, typename... Args>
-cudaError_t tiles_launch(cser_xent *h, K kernel, size_t shared, long long tiles, bool after, cudaStream_t st, Args... args) {
+cudaError_t tiles_launch(cser_xent *h, K kernel, size_t shared, long long tiles, cudaStream_t st, Args... args) {
     const long long most = h->sms / CG;
     h->launches++;
-    return launch_kernel(kernel, (unsigned)((tiles < most ? tiles : most) * CG), kThreads, shared, CG, after, st, args...);
+    return launch_kernel(kernel, (unsigned)((tiles < most ? tiles : most) * CG), kThreads, shared, CG, true, st, args...);
 }
 
 template <int CG>
@@ -775,10 +774,10 @@ cudaError_t kernels_setup() {
 }
 
 template <int CG>
-int loss_launch(cser_xent *h, XentArgs &a, bool packed, cudaStream_t st) {
+int loss_launch(cser_xent *h, XentArgs &a, cudaStream_t st) {
     a.token_tiles = (int)(up(a.tokens, 128 * CG) / (128 * CG)), a.piece0 = 0, a.piece_n = a.vocab;
     const auto kernel = a.dim > loss_chunk(CG) * kStageK ? xent_logits_kernel<CG, kLongLoss> : xent_logits_kernel<CG, kLoss>;
-    TRY((tiles_launch<CG>(h, kernel, Pipe<CG>::kSharedBytes, (long long)a.n * a.token_tiles * ((a.vocab + 255) / 256), packed, st, a)));
+    TRY((tiles_launch<CG>(h, kernel, Pipe<CG>::kSharedBytes, (long long)a.n * a.token_tiles * ((a.vocab + 255) / 256), st, a)));
     if ((long long)a.n * a.tokens > kJoinRows) {
         TRY(launch_kernel(xent_join_kernel, (unsigned)(((long long)a.n * a.tokens + 31) / 32), 1024, 0, 1, true, st, a));
         h->launches++;
@@ -798,24 +797,21 @@ int result_map(const cser_xent *h, CUtensorMap &m, void *p, long long rows, long
 }
 
 template <int CG>
-int grad_launch(cser_xent *h, XentArgs &a, bool packed, cudaStream_t st) {
+int grad_launch(cser_xent *h, XentArgs &a, cudaStream_t st) {
     a.token_tiles = (int)(up(a.tokens, 128 * CG) / (128 * CG));
     a.splits = splits_of(h, a.tokens);
-    bool after = packed;
     if (a.tokens > kOwnRatio) {
-        TRY(launch_kernel(xent_ratio_kernel, (unsigned)a.n, 1024, 0, 1, after, st, a));
+        TRY(launch_kernel(xent_ratio_kernel, (unsigned)a.n, 1024, 0, 1, true, st, a));
         h->launches++;
-        after = true;
     }
     const long long dim_tiles = up(a.dim, 256) / 256;
     for (long long v = 0; v < h->vocab; v += h->piece) {
         a.piece0 = (int)v, a.piece_n = (int)(h->vocab - v < h->piece ? h->vocab - v : h->piece);
         a.first_piece = v == 0, a.last_piece = v + h->piece >= h->vocab;
         const long long vt = up(a.piece_n, 128 * CG) / (128 * CG);
-        TRY((tiles_launch<CG>(h, xent_logits_kernel<CG, kGrad>, Pipe<CG>::kSharedBytes, (long long)a.n * a.token_tiles * ((a.piece_n + 255) / 256), after, st, a)));
-        after = true;
+        TRY((tiles_launch<CG>(h, xent_logits_kernel<CG, kGrad>, Pipe<CG>::kSharedBytes, (long long)a.n * a.token_tiles * ((a.piece_n + 255) / 256), st, a)));
         const long long n_dh = a.dh ? (long long)a.n * a.token_tiles * a.splits * dim_tiles : 0, n_dw = a.dw ? a.n * vt * dim_tiles : 0;
-        TRY((tiles_launch<CG>(h, xent_grad_kernel<CG>, GradPipe<CG>::kSharedBytes, n_dh + n_dw, true, st, a, (int)n_dh, (int)n_dw)));
+        TRY((tiles_launch<CG>(h, xent_grad_kernel<CG>, GradPipe<CG>::kSharedBytes, n_dh + n_dw, st, a, (int)n_dh, (int)n_dw)));
     }
     if (a.dh && a.splits > 1) {
         const long long e = (long long)a.n * a.tokens * ((a.dim + 3) / 4);
@@ -893,8 +889,7 @@ cser_xent_handle cser_xent_create(int32_t n_workers, int64_t max_tokens, int64_t
 int cser_xent_loss(cser_xent_handle h, const cser_xent_inputs *in, float *loss, float *lse, void *stream) {
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     XentArgs a;
-    bool packed = false;
-    if (int rc = prepare_call(h, in, "cser_xent_loss", a, packed, st)) return rc;
+    if (int rc = prepare_call(h, in, "cser_xent_loss", a, st)) return rc;
     if (a.tokens == 0) return CSER_OK;
     if (int rc = cser_internal_check_ptr(lse, "cser_xent_loss: lse")) return rc;
     if (loss)
@@ -902,15 +897,14 @@ int cser_xent_loss(cser_xent_handle h, const cser_xent_inputs *in, float *loss, 
     if ((uintptr_t)lse % 4 || (uintptr_t)loss % 4)
         return cser_internal_fail(CSER_ERR_INVALID, "cser_xent_loss: a pointer is not aligned to its element type");
     a.loss = loss, a.lse_out = lse;
-    return wide_tiles(a.tokens) ? loss_launch<2>(h, a, packed, st) : loss_launch<1>(h, a, packed, st);
+    return wide_tiles(a.tokens) ? loss_launch<2>(h, a, st) : loss_launch<1>(h, a, st);
 }
 
 int cser_xent_grad(cser_xent_handle h, const cser_xent_inputs *in, const float *lse, const float *dloss, void *dhidden,
                    void *dweight, int64_t dweight_stride, void *stream) {
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     XentArgs a;
-    bool packed = false;
-    if (int rc = prepare_call(h, in, "cser_xent_grad", a, packed, st)) return rc;
+    if (int rc = prepare_call(h, in, "cser_xent_grad", a, st)) return rc;
     if (!dhidden && !dweight) return CSER_OK;
     if (dweight) {
         if (int rc = cser_internal_check_ptr(dweight, "cser_xent_grad: dweight")) return rc;
@@ -932,10 +926,10 @@ int cser_xent_grad(cser_xent_handle h, const cser_xent_inputs *in, const float *
     if ((uintptr_t)lse % 4 || (uintptr_t)dloss % 4)
         return cser_internal_fail(CSER_ERR_INVALID, "cser_xent_grad: a pointer is not aligned to its element type");
     a.lse = lse, a.dloss = dloss, a.dh = dhidden, a.dw = dweight, a.dw_stride = dweight_stride;
-    if (wide_tiles(a.tokens)) return grad_launch<2>(h, a, packed, st);
+    if (wide_tiles(a.tokens)) return grad_launch<2>(h, a, st);
     a.dh_boxes = result_map(h, a.dh_map, dhidden, a.tokens, (long long)a.tokens * h->dim);
     a.dw_boxes = result_map(h, a.dw_map, dweight, h->vocab, dweight_stride);
-    return grad_launch<1>(h, a, packed, st);
+    return grad_launch<1>(h, a, st);
 }
 
 void cser_xent_destroy(cser_xent_handle h) {
