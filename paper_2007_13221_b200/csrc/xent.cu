@@ -41,7 +41,7 @@ constexpr size_t kPieceBytes = 256ull << 20;
 // instead of 85 % at 2048 tokens x 16384 x 4096).
 __host__ __device__ constexpr int loss_chunk(int cg) { return cg == 1 ? 4 : 8; }
 constexpr int kOwnRatio = 256;                     // tokens of a worker up to which every warp finds the largest |dloss| itself
-constexpr int kJoinRows = 20;                     // rows that the last CTA joins itself, one per warp
+constexpr int kJoinRows = 20;                     // rows that the last CTA joins itself, a warp or more for each
 
 // 2^x, flushing: the instruction.
 __device__ __forceinline__ float exp2_fast(float x) {
@@ -348,7 +348,7 @@ __global__ void __launch_bounds__(kThreads, 1) xent_logits_kernel(const __grid_c
     p.run(job);
     p.teardown();
     if constexpr (WHAT != kGrad) {
-        // Few rows: the last CTA to finish joins their parts, a warp each (a kernel of its own: 5 us after 14).
+        // Few rows: the last CTA to finish joins their parts (a kernel of its own: 5 us after 14).
         if (a.n * a.tokens > kJoinRows) return;
         __shared__ bool last;
         if (threadIdx.x == 0) {
@@ -358,29 +358,46 @@ __global__ void __launch_bounds__(kThreads, 1) xent_logits_kernel(const __grid_c
             if (last) *a.ticket = 0;                                 // for the next call
         }
         __syncthreads();
-        const int row = threadIdx.x / 32, lane = threadIdx.x % 32, rows = a.n * a.tokens;
-        if (!last || row >= rows) return;
+        if (!last) return;
+        // A warp for each 256 parts of a row: what more of them would save, their joining costs.
+        const int rows = a.n * a.tokens, most = kThreads / 32 / rows, share = min(most, (a.parts + 255) / 256);
+        const int warp = threadIdx.x / 32, row = warp / share, lane = threadIdx.x % 32;
+        __shared__ float2 red[kThreads / 32];
         float m = kLowest, s = 0.f;
-        for (int k = lane; k < a.parts; k += 32 * 8) {               // 8 on their way at a time: of one row 2048 parts take 5 us, 4 at a time 11
-            float2 q[8];
-            float top = m;
+        if (row < rows)
+            for (int k = warp % share * 32 + lane; k < a.parts; k += 32 * share * 8) {   // 8 on their way at a time
+                float2 q[8];
+                float top = m;
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                q[e] = k + 32 * e < a.parts ? __ldcg(a.part + (size_t)(k + 32 * e) * rows + row) : make_float2(kLowest, 0.f);
+                for (int e = 0; e < 8; ++e) {
+                    const int at = k + 32 * share * e;
+                    q[e] = at < a.parts ? __ldcg(a.part + (size_t)at * rows + row) : make_float2(kLowest, 0.f);
+                }
 #pragma unroll
-            for (int e = 0; e < 8; ++e) top = fmaxf(top, q[e].x);
-            s *= exp2_fast((m - top) * kLog2e);
+                for (int e = 0; e < 8; ++e) top = fmaxf(top, q[e].x);
+                s *= exp2_fast((m - top) * kLog2e);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s += q[e].y * exp2_fast((q[e].x - top) * kLog2e);
-            m = top;
-        }
+                for (int e = 0; e < 8; ++e) s += q[e].y * exp2_fast((q[e].x - top) * kLog2e);
+                m = top;
+            }
         for (int k = 16; k; k >>= 1) {
             const float qm = __shfl_xor_sync(~0u, m, k), qs = __shfl_xor_sync(~0u, s, k);
             const float top = fmaxf(m, qm);
             s = s * exp2_fast((m - top) * kLog2e) + qs * exp2_fast((qm - top) * kLog2e);
             m = top;
         }
-        if (lane == 0) row_loss(a, row, m + logf(s));
+        if (lane == 0) red[warp] = make_float2(m, s);
+        __syncthreads();
+        if (threadIdx.x < rows) {
+            m = kLowest, s = 0.f;
+            for (int k = 0; k < share; ++k) {
+                const float2 q = red[threadIdx.x * share + k];
+                const float top = fmaxf(m, q.x);
+                s = s * exp2_fast((m - top) * kLog2e) + q.y * exp2_fast((q.x - top) * kLog2e);
+                m = top;
+            }
+            row_loss(a, threadIdx.x, m + logf(s));
+        }
     }
 }
 
@@ -592,24 +609,40 @@ __global__ void __launch_bounds__(kThreads, 1) xent_grad_kernel(const __grid_con
     p.teardown();
 }
 
-// Where the inner dimension was split: the shares of dh added in their order, four columns a thread.
+// Where the inner dimension was split: the shares of dh added up, four columns a thread, by eight threads that take an eighth of the
+// shares each (by one, the 148 shares of 1 token x 102595 x 40 took as long as the rest).
+constexpr int kJoinWays = 8;
 __global__ void __launch_bounds__(256) xent_join_dh_kernel(const __grid_constant__ XentArgs a) {
+    __shared__ float4 red[kJoinWays][32];
     let_next_start();
     earlier_done();
-    const int groups = (a.dim + 3) / 4;
-    const long long e = (long long)blockIdx.x * 256 + threadIdx.x, row_at = e / groups;
+    const int groups = (a.dim + 3) / 4, way = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const long long e = (long long)blockIdx.x * 32 + lane, row_at = e / groups;
     const int col = (int)(e - row_at * groups) * 4;
-    if (row_at >= (long long)a.n * a.tokens) return;
+    const bool live = row_at < (long long)a.n * a.tokens;
     const int w = (int)(row_at / a.tokens), row = (int)(row_at - (long long)w * a.tokens);
-    float v[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < a.splits; ++s) {
-        const float4 q = *reinterpret_cast<const float4 *>(a.acc + (((size_t)w * a.splits + s) * a.acc_rows + row) * a.acc_cols + col);
-        v[0] += q.x, v[1] += q.y, v[2] += q.z, v[3] += q.w;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (live) {
+        const float4 *from = reinterpret_cast<const float4 *>(a.acc + ((size_t)w * a.splits * a.acc_rows + row) * a.acc_cols + col);
+        const size_t next = (size_t)a.acc_rows * a.acc_cols / 4;
+        const int end = a.splits * (way + 1) / kJoinWays;
+#pragma unroll 4
+        for (int s = a.splits * way / kJoinWays; s < end; ++s) {
+            const float4 q = from[s * next];
+            v.x += q.x, v.y += q.y, v.z += q.z, v.w += q.w;
+        }
+    }
+    red[way][lane] = v;
+    __syncthreads();
+    if (way || !live) return;
+    for (int k = 1; k < kJoinWays; ++k) {
+        const float4 q = red[k][lane];
+        v.x += q.x, v.y += q.y, v.z += q.z, v.w += q.w;
     }
     const float f = a.unscale[w];
     uint16_t *o = static_cast<uint16_t *>(a.dh) + row_at * a.dim + col;
-    const uint32_t lo = a.bf16 ? pack_bf162(v[0] * f, v[1] * f) : pack_half2(v[0] * f, v[1] * f);
-    const uint32_t hi = a.bf16 ? pack_bf162(v[2] * f, v[3] * f) : pack_half2(v[2] * f, v[3] * f);
+    const uint32_t lo = a.bf16 ? pack_bf162(v.x * f, v.y * f) : pack_half2(v.x * f, v.y * f);
+    const uint32_t hi = a.bf16 ? pack_bf162(v.z * f, v.w * f) : pack_half2(v.z * f, v.w * f);
     if (col + 4 <= a.dim && (reinterpret_cast<uintptr_t>(o) & 7) == 0) {
         *reinterpret_cast<uint2 *>(o) = make_uint2(lo, hi);
     } else {
@@ -617,22 +650,32 @@ __global__ void __launch_bounds__(256) xent_join_dh_kernel(const __grid_constant
     }
 }
 
-// Rows that no tensor copy can start at, as rows padded to a multiple of 8; of up to two arrays.
+// Rows that no tensor copy can start at, as rows padded to a multiple of 8; of up to two arrays.  8 columns a thread, `per` threads a
+// row (a CTA per row took 200 us for 246016 rows of 37).
 struct PackSource {
     const uint16_t *src;
     long long row_stride, worker_stride;
     int rows, all;                                 // of a worker, of all
     uint16_t *dst;
 };
-__global__ void __launch_bounds__(256) xent_pack_kernel(const PackSource x, const PackSource y, int dim, int padded) {
+__global__ void __launch_bounds__(256) xent_pack_kernel(const PackSource x, const PackSource y, int dim, int padded, int per) {
     let_next_start();
     earlier_done();
-    const bool second = (int)blockIdx.x >= x.all;
+    const unsigned slot = threadIdx.x / per;
+    const int at = (int)(blockIdx.x * (256u / per) + slot), k = threadIdx.x - slot * per;
+    if (slot >= 256u / per || at >= x.all + y.all) return;
+    const bool second = at >= x.all;
     const PackSource &p = second ? y : x;
-    const long long row = (int)blockIdx.x - (second ? x.all : 0);
-    const uint16_t *s = p.src + (row / p.rows) * p.worker_stride + (row % p.rows) * p.row_stride;
-    uint16_t *d = p.dst + row * padded;
-    for (int c = threadIdx.x; c < padded; c += 256) d[c] = c < dim ? s[c] : 0;
+    const int row = at - (second ? x.all : 0), worker = row / p.rows;
+    const uint16_t *s = p.src + worker * p.worker_stride + (row - worker * p.rows) * p.row_stride;
+    uint16_t *d = p.dst + (long long)row * padded;
+    for (int c = k * 8; c < padded; c += per * 8) {
+        uint32_t v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            v[e] = (c + 2 * e < dim ? (uint32_t)s[c + 2 * e] : 0u) | (c + 2 * e + 1 < dim ? (uint32_t)s[c + 2 * e + 1] << 16 : 0u);
+        *reinterpret_cast<uint4 *>(d + c) = make_uint4(v[0], v[1], v[2], v[3]);
+    }
 }
 
 }  // namespace
@@ -745,8 +788,9 @@ int prepare_call(cser_xent *h, const cser_xent_inputs *in, const char *what, Xen
                          pack[1], "weight", st))
         return rc;
     if (pack[0].all + pack[1].all > 0) {
-        TRY(launch_kernel(xent_pack_kernel, (unsigned)(pack[0].all + pack[1].all), 256, 0, 1, true, st, pack[0], pack[1], (int)h->dim,
-                          (int)up(h->dim, 8)));
+        const int chunks = (int)(up(h->dim, 8) / 8), per = chunks < 256 ? chunks : 256, rows = 256 / per;
+        TRY(launch_kernel(xent_pack_kernel, (unsigned)(((long long)pack[0].all + pack[1].all + rows - 1) / rows), 256, 0, 1, true, st, pack[0],
+                          pack[1], (int)h->dim, (int)up(h->dim, 8), per));
         h->launches++;
     }
     a.bf16 = h->type == CSER_TYPE_BF16;
@@ -815,7 +859,7 @@ int grad_launch(cser_xent *h, XentArgs &a, cudaStream_t st) {
     }
     if (a.dh && a.splits > 1) {
         const long long e = (long long)a.n * a.tokens * ((a.dim + 3) / 4);
-        TRY(launch_kernel(xent_join_dh_kernel, (unsigned)((e + 255) / 256), 256, 0, 1, true, st, a));
+        TRY(launch_kernel(xent_join_dh_kernel, (unsigned)((e + 31) / 32), 256, 0, 1, true, st, a));
         h->launches++;
     }
     return CSER_OK;
