@@ -67,10 +67,14 @@ struct OrthMat {
     unsigned tiles_sym, tiles_x;                   // signals that complete a phase
     float scale;
     int chunk0, chunks;                            // of the norm kernel
+    float *part;                                   // sums of A's tiles over shares of the inner dimension, see choose_shares
+    unsigned *joined;                              // [its tiles of A][CTAs][epilogue warps] how often one has left such sums
+    int n_joined, shares;
 };
 struct OrthTile {
     uint32_t q;
     uint16_t i, j;
+    uint16_t share, slot;                          // of A's tiles: the last share is the one that adds them up; which of its matrix's
 };
 struct PanelUnit {
     uint32_t q, r0, c0;                            // 32 rows, up to 4 panels
@@ -78,8 +82,8 @@ struct PanelUnit {
 
 struct OrthArgs {
     const OrthMat *mats;
-    const OrthTile *sym, *x;
-    int n_sym, n_x, steps;
+    const OrthTile *a_tiles, *sym, *x;
+    int n_a, n_sym, n_x, steps;
     unsigned *done;                                // [matrices] finished tiles
     unsigned *ticket;                              // [matrices] norm kernel
     float *partial, *inv;                          // [chunks], [matrices] 1 / (norm + eps)
@@ -245,6 +249,7 @@ __device__ __forceinline__ void norm_chunk(const OrthArgs &a, uint32_t q, uint32
         a.ticket[q] = 0;                           // for the next call
         a.done[q] = 0;
     }
+    for (int k = threadIdx.x; k < M.n_joined; k += 256) M.joined[k] = 0;
 }
 
 // 32 rows of up to 4 panels: a thread makes one chunk of 8 columns per panel; the padding becomes 0.
@@ -315,10 +320,12 @@ enum { kPhaseA = 0, kPhaseB = 1, kPhaseX = 2 };
 template <int MODE, bool SPLIT>
 using OrthPipe = Pipe<mode_cg(MODE), tile_n(MODE, SPLIT), SPLIT ? 65536 : 98304, SPLIT>;
 
-template <int MODE, bool SPLIT>
+// SHARES: some of A's tiles are summed in shares (a kernel of its own: with that code in it, 32 matrices of 1024 x 1024 with 32-bit
+// results, which have none, took 3160 us instead of 2710).
+template <int MODE, bool SPLIT, bool SHARES>
 struct OrthJob {
     using P = OrthPipe<MODE, SPLIT>;
-    static constexpr int CG = mode_cg(MODE), TN = tile_n(MODE, SPLIT), kSums = SPLIT ? TN / 64 : 1;
+    static constexpr int CG = mode_cg(MODE), TN = tile_n(MODE, SPLIT), kSums = SPLIT ? TN / 64 : 1, kPartFloats = 128 * TN;
     const OrthArgs &a;
     int first, every;
     static constexpr bool kCopier = true, kRemainders = false;
@@ -336,23 +343,29 @@ struct OrthJob {
         long long offset, stride;
         int rows, cols;
         float scale;
+        int share, shares;
+        float *part;                                                 // of this CTA's tile, shares 0, 1, ... one after the other
+        unsigned *joined;
+        unsigned joins;                                              // what it has counted when all of this step's are there
     };
 
     __device__ __forceinline__ void tile(Tile &t, int k, int rank) const {
         t.n = 0;
         const long long at = first + (long long)k * every;
-        const int per_step = 2 * a.n_sym + a.n_x;
+        const int per_step = a.n_a + a.n_sym + a.n_x;
         if (at >= (long long)per_step * a.steps) return;
         const int in = (int)at, step = in / per_step;
         int r = in - step * per_step, phase = kPhaseA;
-        const OrthTile *list = a.sym;
-        if (r >= a.n_sym) r -= a.n_sym, phase = kPhaseB;
+        const OrthTile *list = a.a_tiles;
+        if (r >= a.n_a) r -= a.n_a, phase = kPhaseB, list = a.sym;
         if (phase == kPhaseB && r >= a.n_sym) r -= a.n_sym, phase = kPhaseX, list = a.x;
         const OrthTile e = list[r];
         const OrthMat &M = a.mats[e.q];
         const int width = phase == kPhaseX ? M.cp : M.sp, from = step & 1, to = from ^ 1;
         t.n = width - e.j * TN < TN ? width - e.j * TN : TN;
-        t.stages = phase == kPhaseA ? M.k_long : M.k_short;
+        t.share = e.share, t.shares = phase == kPhaseA ? M.shares : 1;
+        const int k0 = SHARES && phase == kPhaseA ? M.k_long * e.share / t.shares : 0;
+        t.stages = phase != kPhaseA ? M.k_short : SHARES ? M.k_long * (e.share + 1) / t.shares - k0 : M.k_long;
         // Of a symmetric matrix the stages of the panels up to the row's own 256 are stored, the others as their mirror image.
         const int tri_a = (e.i * 128 * CG / 256 + 1) * 4, tri_b = (e.j * TN / 256 + 1) * 4;
         const bool sym_a = phase == kPhaseB || (phase == kPhaseX && !M.tall), sym_b = phase == kPhaseB || (phase == kPhaseX && M.tall);
@@ -365,6 +378,13 @@ struct OrthJob {
         __half *sym_hi = phase == kPhaseB ? M.ah : M.bh, *sym_lo = phase == kPhaseB ? M.al : M.bl;
         t.a_hi = (const char *)(sym_a ? sym_hi : M.xh[from]), t.a_lo = (const char *)(sym_a ? sym_lo : M.xl[from]);
         t.b_hi = (const char *)(sym_b ? sym_hi : M.xh[from]), t.b_lo = (const char *)(sym_b ? sym_lo : M.xl[from]);
+        if (SHARES) {
+            const size_t on = (size_t)k0 * (M.tall ? 8192 : (size_t)M.rp * 128);   // to the share's first stage
+            t.a_hi += on, t.a_lo += on, t.b_hi += on, t.b_lo += on;
+            const size_t tile_at = (size_t)e.slot * CG + rank;
+            t.part = M.part + tile_at * (t.shares - 1) * kPartFloats, t.joined = M.joined + tile_at * kEpiWarps;
+            t.joins = (unsigned)(step + 1) * (t.shares - 1);
+        }
         t.a_panel = (size_t)(sym_a ? M.sp : M.rp) * 128, t.b_panel = (size_t)(sym_b ? M.sp : M.rp) * 128;
         t.rp = phase == kPhaseX ? M.rp : M.sp;
         t.dst_hi = (char *)(phase == kPhaseA ? M.ah : phase == kPhaseB ? M.bh : M.xh[to]);
@@ -519,12 +539,13 @@ struct OrthJob {
             if (used > 0) {
                 const Tile &t = *p.template tile_at<Tile>(behind);
                 if (mbar_test(t.last ? &p.sh->extra_free[ring.buf] : &p.sh->extra_done[ring.buf], ring.parity())) {
-                    if (!t.last) store_panel(p, t, b_out);
+                    const bool leaves = SHARES && t.share + 1 < t.shares;   // only sums, which are not a panel's
+                    if (!t.last && !leaves) store_panel(p, t, b_out);
                     ring.step();
                     --used, moved = true;
                     if (++b_out == t.n / 64) {
                         b_out = 0;
-                        if (t.last) p.tile_done(behind);
+                        if (t.last || leaves) p.tile_done(behind);
                         else signal = true;
                     }
                 }
@@ -570,6 +591,12 @@ struct OrthJob {
         } else if (!p.take(turn, tmem)) {
             return false;
         }
+        const bool leaves = SHARES && t.share + 1 < t.shares;
+        if (SHARES && t.shares > 1 && !leaves) {                               // the other shares' sums are there
+            bool there = true;
+            if (lane == 0) there = p.wait_counter(t.joined + warp, t.joins);
+            if (!__shfl_sync(~0u, (int)there, 0)) return false;
+        }
 #pragma unroll kSums
         for (int b = 0; b < (SPLIT ? kSums : panels); ++b) {
             const int panel = t.panel0 + b, col = panel * 64 + side * 16;
@@ -586,6 +613,26 @@ struct OrthJob {
             } else {
                 tmem_load(tmem + b * 64 + side * 16, v);
                 if (b + 1 == panels) p.release(turn, lane);
+            }
+            if (SHARES && t.shares > 1) {
+                float4 *part = reinterpret_cast<float4 *>(t.part) + (size_t)b * 4 * (kEpiWarps * 32) + tid;
+                if (leaves) {
+                    part += (size_t)t.share * (kPartFloats / 4);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        part[k * kEpiWarps * 32] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+                    if (lane == 0) mbar_arrive(&p.sh->extra_done[ring.buf]), mbar_arrive(&p.sh->extra_free[ring.buf]);
+                    ring.step();
+                    continue;
+                }
+#pragma unroll 1
+                for (int e = 0; e + 1 < t.shares; ++e, part += kPartFloats / 4) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const float4 q = __ldcg(part + k * kEpiWarps * 32);
+                        v[4 * k] += q.x, v[4 * k + 1] += q.y, v[4 * k + 2] += q.z, v[4 * k + 3] += q.w;
+                    }
+                }
             }
             const unsigned on = (unsigned)(row - col);               // the diagonal is at column `on` of the 16, if below 16
             if (phase == kPhaseA) {
@@ -688,17 +735,24 @@ struct OrthJob {
             if (lane == 0) mbar_arrive(&p.sh->extra_free[ring.buf]);
             ring.step();
         }
+        if (leaves) {
+            __syncwarp();
+            if (lane == 0) {
+                __threadfence();
+                asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(t.joined + warp) : "memory");
+            }
+        }
         return true;
     }
 };
 
-template <int MODE, bool SPLIT>
+template <int MODE, bool SPLIT, bool SHARES>
 __global__ void __launch_bounds__(kThreads, 1) orth_products_kernel(const __grid_constant__ OrthArgs a) {
     extern __shared__ unsigned char raw[];
     constexpr int CG = mode_cg(MODE);
     OrthPipe<MODE, SPLIT> p;
-    p.template setup<OrthJob<MODE, SPLIT>>(raw, a.err, a.wait_cycles);
-    OrthJob<MODE, SPLIT> job{a, (int)blockIdx.x / CG, (int)gridDim.x / CG};
+    p.template setup<OrthJob<MODE, SPLIT, SHARES>>(raw, a.err, a.wait_cycles);
+    OrthJob<MODE, SPLIT, SHARES> job{a, (int)blockIdx.x / CG, (int)gridDim.x / CG};
     p.run(job);
     p.teardown();
 }
@@ -717,6 +771,7 @@ __global__ void __launch_bounds__(kThreads, 1) orth_products_kernel(const __grid
 struct cser_orth {
     struct Group {
         int mode = kSingle, grid = 0, n_chunk = 0, n_unit = 0;
+        bool shares = false;
         OrthArgs args{};
         void *tables = nullptr;                    // one allocation for the lists and matrices
     };
@@ -744,7 +799,7 @@ int type_size(int t) { return t == CSER_TYPE_F32 ? 4 : 2; }
 long long up(long long v, long long to) { return (v + to - 1) / to * to; }
 
 template <int MODE, bool SPLIT>
-cudaError_t products_launch(const OrthArgs &a, int grid, cudaStream_t st) {
+cudaError_t products_launch(const OrthArgs &a, bool shares, int grid, cudaStream_t st) {
     constexpr int CG = mode_cg(MODE);
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)grid);
@@ -758,13 +813,16 @@ cudaError_t products_launch(const OrthArgs &a, int grid, cudaStream_t st) {
     at[1].val.clusterDim.x = CG, at[1].val.clusterDim.y = 1, at[1].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = CG == 1 ? 1 : 2;
-    return cudaLaunchKernelEx(&cfg, orth_products_kernel<MODE, SPLIT>, a);
+    return cudaLaunchKernelEx(&cfg, shares ? orth_products_kernel<MODE, SPLIT, true> : orth_products_kernel<MODE, SPLIT, false>, a);
 }
 template <int MODE, bool SPLIT>
 cudaError_t products_setup(int &pairs) {
     constexpr int CG = mode_cg(MODE);
-    cudaError_t e = cudaFuncSetAttribute(orth_products_kernel<MODE, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+    cudaError_t e = cudaFuncSetAttribute(orth_products_kernel<MODE, SPLIT, false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                          (int)OrthPipe<MODE, SPLIT>::kSharedBytes);
+    if (e == cudaSuccess)
+        e = cudaFuncSetAttribute(orth_products_kernel<MODE, SPLIT, true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                 (int)OrthPipe<MODE, SPLIT>::kSharedBytes);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(CG);
@@ -775,7 +833,11 @@ cudaError_t products_setup(int &pairs) {
     at[0].val.clusterDim.x = CG, at[0].val.clusterDim.y = 1, at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    return cudaOccupancyMaxActiveClusters(&pairs, orth_products_kernel<MODE, SPLIT>, &cfg);
+    int with_shares = 0;
+    e = cudaOccupancyMaxActiveClusters(&pairs, orth_products_kernel<MODE, SPLIT, false>, &cfg);
+    if (e == cudaSuccess) e = cudaOccupancyMaxActiveClusters(&with_shares, orth_products_kernel<MODE, SPLIT, true>, &cfg);
+    if (with_shares < pairs) pairs = with_shares;
+    return e;
 }
 
 int orth_fail(cser_orth *h, int code, const char *what) {
@@ -818,10 +880,24 @@ int choose_mode(const std::vector<HostMat> &all, bool split, int pairs, int sms)
     return area[1] < 1.5 * 16384.0 * sms ? kNarrow : kSingle;
 }
 
+// In how many shares a matrix's tiles of A sum their inner dimension, where there are idle CTAs for them: so that the stages of
+// one, and what joining costs in their time, are fewest.  Joining: 8 stages' time, and 2.5 for each share's sums (22 and 4
+// where they are of 128 x 256 for each of a pair).  One of 100 x 60000 1560 us -> 300 (16-bit; 32-bit 3450 -> 590), two of
+// 256 x 16384 580 -> 285 (1150 -> 555), 1024 x 4096 276 -> 239; with a share for every 8 stages 8 of 512 x 2048 went from 223 to 241.
+int choose_shares(int tiles, int ctas, int k_long, bool wide) {
+    int best = 1;
+    double least = k_long;
+    for (int s = 2; s <= ctas / tiles && s <= k_long; ++s) {
+        const double cost = (double)k_long / s + (wide ? 22 + 4 * s : 8 + 2.5 * s);
+        if (cost < least) best = s, least = cost;
+    }
+    return best;
+}
+
 int build_group(cser_orth *h, cser_orth::Group &G, const std::vector<HostMat> &ms, int mode, int steps, int ctas) {
     const int cg = mode_cg(mode);
     std::vector<OrthMat> mats(ms.size());
-    std::vector<OrthTile> sym, xs;
+    std::vector<OrthTile> as, sym, xs;
     std::vector<uint2> chunk;
     std::vector<PanelUnit> unit;
     size_t at = 0;
@@ -846,34 +922,57 @@ int build_group(cser_orth *h, cser_orth::Group &G, const std::vector<HostMat> &m
         const int tm = 128 * cg, tn = tile_n(mode, h->split);
         for (int j = 0; j * tn < M.sp; ++j)
             for (int i = 0; i * tm < M.sp; ++i)
-                if (i * tm / 256 >= j * tn / 256) sym.push_back({(uint32_t)q, (uint16_t)i, (uint16_t)j}), M.tiles_sym += cg;
+                if (i * tm / 256 >= j * tn / 256) sym.push_back({(uint32_t)q, (uint16_t)i, (uint16_t)j, 0, 0}), M.tiles_sym += cg;
         if (M.tall) {
             for (int i = 0; i * tm < M.rp; ++i)
-                for (int j = 0; j * tn < M.cp; ++j) xs.push_back({(uint32_t)q, (uint16_t)i, (uint16_t)j}), M.tiles_x += cg;
+                for (int j = 0; j * tn < M.cp; ++j) xs.push_back({(uint32_t)q, (uint16_t)i, (uint16_t)j, 0, 0}), M.tiles_x += cg;
         } else {
             for (int j = 0; j * tn < M.cp; ++j)
-                for (int i = 0; i * tm < M.rp; ++i) xs.push_back({(uint32_t)q, (uint16_t)i, (uint16_t)j}), M.tiles_x += cg;
+                for (int i = 0; i * tm < M.rp; ++i) xs.push_back({(uint32_t)q, (uint16_t)i, (uint16_t)j, 0, 0}), M.tiles_x += cg;
         }
+    }
+    // Kernels of small matrices beside this one need SMs of their own: it starts when all of its CTAs fit.
+    const int beside = h->small.n_part + h->resident.n_resident, spare = beside * 4 < ctas ? beside : ctas / 4;
+    const int most = ctas - (spare + cg - 1) / cg;
+    size_t part_floats = 0, joins = 0;             // of the matrices' `part` and `joined`, at first as offsets
+    std::vector<size_t> part_at(ms.size()), join_at(ms.size());
+    for (size_t k = 0; k < sym.size();) {
+        const uint32_t q = sym[k].q;
+        OrthMat &M = mats[q];
+        M.shares = choose_shares((int)sym.size(), most, M.k_long, tile_n(mode, h->split) == 256);
+        part_at[q] = part_floats, join_at[q] = joins;
+        const size_t k1 = k;
+        for (; k < sym.size() && sym[k].q == q; ++k)
+            for (int e = 0; e < M.shares; ++e) as.push_back({q, sym[k].i, sym[k].j, (uint16_t)e, (uint16_t)(k - k1)});
+        G.shares |= M.shares > 1;
+        M.n_joined = M.shares > 1 ? (int)(k - k1) * cg * kEpiWarps : 0;
+        part_floats += (k - k1) * cg * (M.shares - 1) * 128 * tile_n(mode, h->split), joins += M.n_joined;
     }
     const size_t n = ms.size();
     size_t bytes = 0;
     auto place = [&](size_t b) { const size_t p = bytes; bytes += (b + 255) / 256 * 256; return p; };
-    const size_t o_mat = place(n * sizeof(OrthMat)), o_sym = place(sym.size() * sizeof(OrthTile)),
-                 o_x = place(xs.size() * sizeof(OrthTile)), o_ck = place(chunk.size() * sizeof(uint2)),
+    const size_t o_mat = place(n * sizeof(OrthMat)), o_as = place(as.size() * sizeof(OrthTile)), o_sym = place(sym.size() * sizeof(OrthTile)),
+                 o_pt = place(part_floats * 4), o_join = place(joins * 4), o_x = place(xs.size() * sizeof(OrthTile)), o_ck = place(chunk.size() * sizeof(uint2)),
                  o_un = place(unit.size() * sizeof(PanelUnit)),
                  o_done = place(n * 4), o_tick = place(n * 4),
                  o_inv = place(n * 4), o_part = place((size_t)chunk0 * 4);
     TRY(cudaMalloc(&G.tables, bytes));
     char *t = static_cast<char *>(G.tables);
     TRY(cudaMemset(t + o_done, 0, bytes - o_done));
+    for (size_t q = 0; q < n; ++q) {
+        mats[q].part = reinterpret_cast<float *>(t + o_pt) + part_at[q];
+        mats[q].joined = reinterpret_cast<unsigned *>(t + o_join) + join_at[q];
+    }
     TRY(cudaMemcpy(t + o_mat, mats.data(), n * sizeof(OrthMat), cudaMemcpyHostToDevice));
+    TRY(cudaMemcpy(t + o_as, as.data(), as.size() * sizeof(OrthTile), cudaMemcpyHostToDevice));
     TRY(cudaMemcpy(t + o_sym, sym.data(), sym.size() * sizeof(OrthTile), cudaMemcpyHostToDevice));
     TRY(cudaMemcpy(t + o_x, xs.data(), xs.size() * sizeof(OrthTile), cudaMemcpyHostToDevice));
     TRY(cudaMemcpy(t + o_un, unit.data(), unit.size() * sizeof(PanelUnit), cudaMemcpyHostToDevice));
     TRY(cudaMemcpy(t + o_ck, chunk.data(), chunk.size() * sizeof(uint2), cudaMemcpyHostToDevice));
     OrthArgs &A = G.args;
-    A.n_sym = (int)sym.size(), A.n_x = (int)xs.size(), A.steps = steps;
+    A.n_a = (int)as.size(), A.n_sym = (int)sym.size(), A.n_x = (int)xs.size(), A.steps = steps;
     A.mats = reinterpret_cast<OrthMat *>(t + o_mat);
+    A.a_tiles = reinterpret_cast<OrthTile *>(t + o_as);
     A.sym = reinterpret_cast<OrthTile *>(t + o_sym);
     A.x = reinterpret_cast<OrthTile *>(t + o_x);
     A.chunk = reinterpret_cast<uint2 *>(t + o_ck), A.unit = reinterpret_cast<PanelUnit *>(t + o_un);
@@ -881,10 +980,7 @@ int build_group(cser_orth *h, cser_orth::Group &G, const std::vector<HostMat> &m
     A.inv = reinterpret_cast<float *>(t + o_inv), A.partial = reinterpret_cast<float *>(t + o_part);
     A.out_type = h->out_type;
     G.n_chunk = (int)chunk.size(), G.n_unit = (int)unit.size(), G.mode = mode;
-    const int widest = A.n_sym > A.n_x ? A.n_sym : A.n_x;
-    // Kernels of small matrices beside this one need SMs of their own: it starts when all of its CTAs fit.
-    const int beside = h->small.n_part + h->resident.n_resident, spare = beside * 4 < ctas ? beside : ctas / 4;
-    const int most = ctas - (spare + cg - 1) / cg;
+    const int widest = A.n_a > A.n_x ? A.n_a : A.n_x;               // there are at least as many tiles of A as of B
     G.grid = (widest < most ? widest : most) * cg;
     return CSER_OK;
 }
@@ -1119,9 +1215,9 @@ int cser_orth_apply(cser_orth_handle h, const void *grad, float *m, float mu, vo
         // products, whose CTAs start together or not at all, waited for them.
         const bool fork = both && &G == &h->groups.back();
         if (fork) TRY(cudaEventRecord(h->fork, st));
-        if (G.mode == kNarrow) e = h->split ? products_launch<kNarrow, true>(a, G.grid, st) : products_launch<kNarrow, false>(a, G.grid, st);
-        else if (G.mode == kSingle) e = h->split ? products_launch<kSingle, true>(a, G.grid, st) : products_launch<kSingle, false>(a, G.grid, st);
-        else e = h->split ? products_launch<kPaired, true>(a, G.grid, st) : products_launch<kPaired, false>(a, G.grid, st);
+        if (G.mode == kNarrow) e = h->split ? products_launch<kNarrow, true>(a, G.shares, G.grid, st) : products_launch<kNarrow, false>(a, G.shares, G.grid, st);
+        else if (G.mode == kSingle) e = h->split ? products_launch<kSingle, true>(a, G.shares, G.grid, st) : products_launch<kSingle, false>(a, G.shares, G.grid, st);
+        else e = h->split ? products_launch<kPaired, true>(a, G.shares, G.grid, st) : products_launch<kPaired, false>(a, G.shares, G.grid, st);
         TRY(e);
         h->launches += 3;
     }

@@ -210,6 +210,27 @@ def test_plans_of_different_sizes(shapes, out_t):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("types", [(BF, BF), (F32, F32), (F32, HF)], ids=str)
+@pytest.mark.parametrize("shapes", [[(100, 6000)], [(6000, 100), (70, 1025)], [(300, 5003)] * 2, [(512, 16384)] * 2, [(8192, 700), (65, 65)]],
+                         ids=lambda s: f"{len(s)}x{s[0]}")
+def test_long_sides_in_shares(shapes, types):
+    """Few and long: the inner dimension of A is summed in shares by several CTAs.  The same bits every time."""
+    gen = generator(17)
+    ms = [matrix(gen, r, c).to(types[0]) for r, c in shapes]
+    at, mats = 0, []
+    for r, c in shapes:
+        mats.append((at, r, c))
+        at += r * c
+    flat = torch.cat([m.reshape(-1) for m in ms]).reshape(1, -1)
+    o = train.Orthogonalizer(mats, 1, at, *types)
+    first = o.apply(flat).clone()
+    for (off, r, c), m in zip(mats, ms):
+        assert far(first[0, off:off + r * c].view(r, c), exact(m)) < OUT[types[1]]
+    for _ in range(3):
+        assert torch.equal(o.apply(flat), first)
+
+
+@pytest.mark.gpu
 def test_refusals():
     ok = dict(matrices=[(0, 4, 5)], n_workers=1, ld=20)
     train.Orthogonalizer(**ok)
