@@ -985,7 +985,8 @@ int build_group(cser_orth *h, cser_orth::Group &G, const std::vector<HostMat> &m
     return CSER_OK;
 }
 
-int build_small(cser_orth *h, const std::vector<HostMat> &ms, int steps) {
+// `ctas`: SMs for these alone.
+int build_small(cser_orth *h, const std::vector<HostMat> &ms, int steps, int ctas) {
     std::vector<SmallMat> mats(ms.size());
     std::vector<uint2> part, piece;
     size_t work = 0;
@@ -995,9 +996,11 @@ int build_small(cser_orth *h, const std::vector<HostMat> &ms, int steps) {
         M.tall = ms[q].rows > ms[q].cols;
         M.s = (int)(M.tall ? ms[q].cols : ms[q].rows), M.l = (int)(M.tall ? ms[q].rows : ms[q].cols), M.sp = (int)up(M.s, 8);
         M.offset = ms[q].offset, M.stride = ms[q].stride, M.scale = ms[q].scale;
-        // Parts of at least one piece of u in shared memory and 16 at most: the last CTA adds them up alone.
+        // Parts of at least one piece of u in shared memory, and 16 at most, since the last CTA adds them up alone, or as many as there
+        // are SMs that would be idle (one of 64 x 60000: 640 us by 16, 215 by 148).
         const long long cols = kGramDoubles / gram_ld(M.sp) / 4 * 4, fit = up(M.l, cols) / cols;
-        M.parts = fit < 16 ? (int)fit : 16;
+        const int idle = ctas / (int)ms.size(), top = idle < 16 ? 16 : idle;
+        M.parts = fit < top ? (int)fit : top;
         M.per = (int)(up(up(M.l, M.parts) / M.parts, cols));
         M.parts = (int)(up(M.l, M.per) / M.per);
         const int side = M.sp / 8;
@@ -1138,7 +1141,7 @@ cser_orth_handle cser_orth_create(int32_t n_workers, int64_t ld, int32_t n_matri
             (pays && resident_bytes((int)up(side, 8), longer) <= kResidentMost ? fit : rest).push_back(m);
         }
         if (er == cudaSuccess && !small.empty()) {
-            if ((!rest.empty() && build_small(h, rest, steps) != CSER_OK) || (!fit.empty() && build_resident(h, fit, steps) != CSER_OK)) {
+            if ((!rest.empty() && build_small(h, rest, steps, all.empty() ? fit_ctas[kSingle] : 0) != CSER_OK) || (!fit.empty() && build_resident(h, fit, steps) != CSER_OK)) {
                 cser_orth_destroy(h);
                 return nullptr;
             }

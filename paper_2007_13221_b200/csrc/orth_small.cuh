@@ -237,14 +237,21 @@ __global__ void __launch_bounds__(256) orth_gram_kernel(const SmallArgs a) {
     const int sq = square_ld(sp), all_size = sp * sq;
     double *A = sh, *P = sh + all_size, *Q = P + all_size, *W = Q + all_size;
     const double *all = a.work + M.partial;
-    for (int e = threadIdx.x; e < tiles * 64; e += 256) {
-        const int k = e / 64, w = e - k * 64;
+    constexpr int kOwn = 9;                                          // 36 tiles' elements by 256 threads
+    double sum[kOwn] = {};
+#pragma unroll 2
+    for (int p = 0; p < M.parts; ++p)
+#pragma unroll
+        for (int b = 0; b < kOwn; ++b)
+            if (threadIdx.x + 256 * b < tiles * 64) sum[b] += __ldcg(all + (size_t)p * tiles * 64 + threadIdx.x + 256 * b);
+#pragma unroll
+    for (int b = 0; b < kOwn; ++b) {
+        const int e = threadIdx.x + 256 * b, k = e / 64, w = e - k * 64;
+        if (k >= tiles) break;
         int bi, bj;
         triangle(k, bi, bj);
-        double s = 0.0;
-        for (int p = 0; p < M.parts; ++p) s += __ldcg(all + (size_t)p * tiles * 64 + e);
         const int i = bi * 8 + w / 8, j = bj * 8 + w % 8;
-        if (j <= i) A[i * sq + j] = A[j * sq + i] = s;
+        if (j <= i) A[i * sq + j] = A[j * sq + i] = sum[b];
     }
     __syncthreads();
     Q = sp <= 32 ? small_steps<2>(A, P, Q, W, sp, a.steps) : small_steps<5>(A, P, Q, W, sp, a.steps);

@@ -211,7 +211,8 @@ def test_plans_of_different_sizes(shapes, out_t):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("types", [(BF, BF), (F32, F32), (F32, HF)], ids=str)
-@pytest.mark.parametrize("shapes", [[(100, 6000)], [(6000, 100), (70, 1025)], [(300, 5003)] * 2, [(512, 16384)] * 2, [(8192, 700), (65, 65)]],
+@pytest.mark.parametrize("shapes", [[(100, 6000)], [(6000, 100), (70, 1025)], [(300, 5003)] * 2, [(512, 16384)] * 2, [(8192, 700), (65, 65)],
+                                    [(64, 20000)], [(30001, 7), (40, 9000)], [(33, 9000), (200, 300)]],
                          ids=lambda s: f"{len(s)}x{s[0]}")
 def test_long_sides_in_shares(shapes, types):
     """Few and long: the inner dimension of A is summed in shares by several CTAs.  The same bits every time."""
