@@ -671,9 +671,18 @@ __global__ void __launch_bounds__(256) xent_pack_kernel(const PackSource x, cons
     uint16_t *d = p.dst + (long long)row * padded;
     for (int c = k * 8; c < padded; c += per * 8) {
         uint32_t v[4];
+        if (c + 8 > dim) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            v[e] = (c + 2 * e < dim ? (uint32_t)s[c + 2 * e] : 0u) | (c + 2 * e + 1 < dim ? (uint32_t)s[c + 2 * e + 1] << 16 : 0u);
+            for (int e = 0; e < 4; ++e)
+                v[e] = (c + 2 * e < dim ? (uint32_t)s[c + 2 * e] : 0u) | (c + 2 * e + 1 < dim ? (uint32_t)s[c + 2 * e + 1] << 16 : 0u);
+        } else if ((reinterpret_cast<uintptr_t>(s) & 2) == 0) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = reinterpret_cast<const uint32_t *>(s + c)[e];
+        } else {
+            const uint32_t *between = reinterpret_cast<const uint32_t *>(s + c + 1);
+            const uint32_t x = between[0], y = between[1], z = between[2];
+            v[0] = (uint32_t)s[c] | x << 16, v[1] = x >> 16 | y << 16, v[2] = y >> 16 | z << 16, v[3] = z >> 16 | (uint32_t)s[c + 7] << 16;
+        }
         *reinterpret_cast<uint4 *>(d + c) = make_uint4(v[0], v[1], v[2], v[3]);
     }
 }
