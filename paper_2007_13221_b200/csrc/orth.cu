@@ -328,7 +328,7 @@ struct OrthJob {
     static constexpr int CG = mode_cg(MODE), TN = tile_n(MODE, SPLIT), kSums = SPLIT ? TN / 64 : 1, kPartFloats = 128 * TN;
     const OrthArgs &a;
     int first, every;
-    static constexpr bool kCopier = true, kRemainders = false;
+    static constexpr bool kCopier = true, kRemainders = false, kWaits = true;
 
     struct Tile {
         int n, stages, a_lim, b_lim;

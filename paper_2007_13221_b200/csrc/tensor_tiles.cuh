@@ -364,7 +364,8 @@ struct Pipe {
     //                              dimension; a_lim, b_lim: from which stage on that operand is MN-major
     //   void tile(Tile &, int i, int rank)   the i-th tile of this CTA (pair); each lane asks for growing i only
     //   bool chunk_ends(tile, k)   after this stage the epilogue takes the accumulator (always after the last)
-    //   bool ready(pipe, tile)     waits until what the tile reads is in memory (before any role hears of the tile)
+    //   kWaits; bool ready(pipe, tile)   whether tiles read what this launch writes; then waits until that is in memory (before any role
+    //                              hears of the tile)
     //   Loader                     made from a tile; uint32_t bytes(); void load(k, a, b, bar): copies of bytes() bytes into a and b (shared
     //                              addresses; the lo halves of pairs kLoOffset behind)
     //   int bf16()
@@ -383,11 +384,12 @@ struct Pipe {
         if (warp == 0 && lane == 0) {
             int s = 0, issued = 0;
             uint32_t ph = 0;
+            if (!Job::kWaits) fence_async_global();     // what earlier kernels wrote; beside the search for the first tile
             while (ok) {
                 ok = wait(&sh->tile_full[walk.slot], walk.ph);
                 const Tile &t = *tile_at<Tile>(walk);
                 if (!ok || t.n == 0) break;
-                fence_async_global();                   // what ready() saw written, for the copy engine
+                if (Job::kWaits) fence_async_global();  // what ready() saw written, for the copy engine
                 typename Job::Loader from(job, t);
                 const uint32_t bytes = from.bytes();
                 const int stages = t.stages;

@@ -143,7 +143,7 @@ struct LogitsJob {
     static constexpr bool GRAD = WHAT == kGrad, LONG = WHAT == kLongLoss;
     const XentArgs &a;
     int first, every, vocab_tiles;
-    static constexpr bool kCopier = false, kRemainders = false;
+    static constexpr bool kCopier = false, kRemainders = false, kWaits = false;
 
     struct Tile {
         int w, i, j, n, stages, a_lim, b_lim;
@@ -298,11 +298,16 @@ struct LogitsJob {
     }
 };
 
-__device__ __forceinline__ void row_loss(const XentArgs &a, size_t at, float lse) {
-    const int64_t y = a.target[at];
-    a.lse_out[at] = lse;
-    if (a.loss) a.loss[at] = y == a.ignore ? 0.f : y >= 0 && y < a.vocab ? lse - __ldcg(a.z_target + at) : NAN;
-}
+// z[target] of a row, or what makes its loss 0 or NaN; asked for before its parts are joined.
+struct RowTarget {
+    int64_t y;
+    float z;
+    __device__ __forceinline__ RowTarget(const XentArgs &a, size_t at, bool live) : y(live ? a.target[at] : 0), z(live ? __ldcg(a.z_target + at) : 0.f) {}
+    __device__ __forceinline__ void loss(const XentArgs &a, size_t at, float lse) const {
+        a.lse_out[at] = lse;
+        if (a.loss) a.loss[at] = y == a.ignore ? 0.f : y >= 0 && y < a.vocab ? lse - z : NAN;
+    }
+};
 
 // The parts of 32 rows joined by 32 warps: a lane takes a row, a warp every 32nd part, four of them at a time.
 __global__ void __launch_bounds__(1024) xent_join_kernel(const __grid_constant__ XentArgs a) {
@@ -311,6 +316,7 @@ __global__ void __launch_bounds__(1024) xent_join_kernel(const __grid_constant__
     earlier_done();
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const size_t rows = (size_t)a.n * a.tokens, at = (size_t)blockIdx.x * 32 + lane;
+    const RowTarget of(a, at, warp == 0 && at < rows);
     float m = kLowest, s = 0.f;
     if (at < rows)
         for (int k = warp; k < a.parts; k += 128) {
@@ -332,7 +338,7 @@ __global__ void __launch_bounds__(1024) xent_join_kernel(const __grid_constant__
             s = s * exp2_fast((m - top) * kLog2e) + q.y * exp2_fast((q.x - top) * kLog2e);
             m = top;
         }
-        row_loss(a, at, m + logf(s));
+        of.loss(a, at, m + logf(s));
     }
 }
 
@@ -351,10 +357,10 @@ __global__ void __launch_bounds__(kThreads, 1) xent_logits_kernel(const __grid_c
         // Few rows: the last CTA to finish joins their parts (a kernel of its own: 5 us after 14).
         if (a.n * a.tokens > kJoinRows) return;
         __shared__ bool last;
-        if (threadIdx.x == 0) {
-            __threadfence();
-            last = atomicAdd(a.ticket, 1u) == gridDim.x - 1;
-            __threadfence();
+        if (threadIdx.x == 0) {                                      // after the CTA's barrier in teardown()
+            unsigned before;
+            asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(before) : "l"(a.ticket) : "memory");
+            last = before == gridDim.x - 1;
             if (last) *a.ticket = 0;                                 // for the next call
         }
         __syncthreads();
@@ -362,6 +368,7 @@ __global__ void __launch_bounds__(kThreads, 1) xent_logits_kernel(const __grid_c
         // A warp for each 256 parts of a row: what more of them would save, their joining costs.
         const int rows = a.n * a.tokens, most = kThreads / 32 / rows, share = min(most, (a.parts + 255) / 256);
         const int warp = threadIdx.x / 32, row = warp / share, lane = threadIdx.x % 32;
+        const RowTarget of(a, threadIdx.x, threadIdx.x < rows);
         __shared__ float2 red[kThreads / 32];
         float m = kLowest, s = 0.f;
         if (row < rows)
@@ -396,7 +403,7 @@ __global__ void __launch_bounds__(kThreads, 1) xent_logits_kernel(const __grid_c
                 s = s * exp2_fast((m - top) * kLog2e) + q.y * exp2_fast((q.x - top) * kLog2e);
                 m = top;
             }
-            row_loss(a, threadIdx.x, m + logf(s));
+            of.loss(a, threadIdx.x, m + logf(s));
         }
     }
 }
@@ -412,7 +419,7 @@ struct GradJob {
     using P = GradPipe<CG>;
     const XentArgs &a;
     int first, every, n_dh, n_dw, dim_tiles, vocab_tiles, early;
-    static constexpr bool kCopier = false, kRemainders = CG == 1;
+    static constexpr bool kCopier = false, kRemainders = CG == 1, kWaits = false;
     __device__ __forceinline__ bool remainders() const { return a.tokens <= kLowRows; }
 
     struct Tile {
