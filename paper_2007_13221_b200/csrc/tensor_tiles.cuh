@@ -365,7 +365,8 @@ struct Pipe {
     //   void tile(Tile &, int i, int rank)   the i-th tile of this CTA (pair); each lane asks for growing i only
     //   bool chunk_ends(tile, k)   after this stage the epilogue takes the accumulator (always after the last)
     //   kWaits; bool ready(pipe, tile)   whether tiles read what this launch writes; then waits until that is in memory (before any role
-    //                              hears of the tile)
+    //                              hears of the tile).  If not, the launch may overlap the end of the kernel before it: tiles are worked
+    //                              out from the kernel's arguments alone, copies and epilogue begin with earlier_done()
     //   Loader                     made from a tile; uint32_t bytes(); void load(k, a, b, bar): copies of bytes() bytes into a and b (shared
     //                              addresses; the lo halves of pairs kLoOffset behind)
     //   int bf16()
@@ -384,7 +385,7 @@ struct Pipe {
         if (warp == 0 && lane == 0) {
             int s = 0, issued = 0;
             uint32_t ph = 0;
-            if (!Job::kWaits) fence_async_global();     // what earlier kernels wrote; beside the search for the first tile
+            bool first = !Job::kWaits;
             while (ok) {
                 ok = wait(&sh->tile_full[walk.slot], walk.ph);
                 const Tile &t = *tile_at<Tile>(walk);
@@ -394,6 +395,7 @@ struct Pipe {
                 const uint32_t bytes = from.bytes();
                 const int stages = t.stages;
                 tile_done(walk);
+                if (first) earlier_done(), fence_async_global(), first = false;
                 for (int k = 0; k < stages; ++k) {
                     ok = wait(&sh->empty[s], ph ^ 1);
                     if (!ok) break;
@@ -526,6 +528,7 @@ struct Pipe {
             }
         } else if (warp >= kEpiWarp0) {
             Turn turn;
+            if (!Job::kWaits) earlier_done();
             while (ok) {
                 ok = warp_wait(&sh->tile_full[walk.slot], walk.ph);
                 const Tile &t = *tile_at<Tile>(walk);

@@ -350,7 +350,6 @@ __global__ void __launch_bounds__(kThreads, 1) xent_logits_kernel(const __grid_c
     Pipe<CG> p;
     p.template setup<LogitsJob<CG, WHAT>>(raw, a.err);
     LogitsJob<CG, WHAT> job{a, (int)blockIdx.x / CG, (int)gridDim.x / CG, (a.piece_n + 255) / 256};
-    earlier_done();
     p.run(job);
     p.teardown();
     if constexpr (WHAT != kGrad) {
@@ -610,7 +609,6 @@ __global__ void __launch_bounds__(kThreads, 1) xent_grad_kernel(const __grid_con
         job.early = stages / (each < 12 ? 12 : each);
         if (job.early > fits) job.early = fits;
     }
-    earlier_done();
     p.run(job);
     if (CG == 1) bulk_out_done();                  // of the threads that sent results off
     p.teardown();
