@@ -52,7 +52,7 @@ typedef struct cser_orth *cser_orth_handle;
  * <= 65536.  row_stride[k] >= cols[k]: elements from one row to the next (NULL: cols[k]).  scale[k]: finite factor of the
  * result (NULL: 1).  Matrices must lie inside the vector and not overlap.  steps: 1..16.  The arrays are host memory
  * and are copied.  The plan owns a workspace of about 8 bytes per element (16 for a 32-bit result) for all matrices of all workers or 2 GB,
- * whichever is less (more only where one matrix needs more).  Returns NULL on failure.
+ * whichever is less (more only where one matrix needs more), and at most 20 MB for sums that CTAs share.  Returns NULL on failure.
  */
 cser_orth_handle cser_orth_create(int32_t n_workers, int64_t ld, int32_t n_matrices, const int64_t *offset,
                                   const int64_t *rows, const int64_t *cols, const int64_t *row_stride,

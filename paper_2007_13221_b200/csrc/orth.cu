@@ -24,7 +24,8 @@
 //
 // Order of work.  The list of all tiles of all phases of all steps is dealt out to the CTAs in order; a tile waits for
 // the tiles of its own matrix's earlier phases by a counter, so the phases of different matrices overlap.  The launch is cooperative:
-// every CTA is resident, a wait always has someone to end it.
+// every CTA is resident, a wait always has someone to end it.  Where A's tiles are fewer than the CTAs and the long side is long, a tile is
+// several entries of the list, each a share of the inner dimension: the last one waits for the others' sums and adds them up in order.
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <cuda_bf16.h>
