@@ -231,6 +231,29 @@ def test_strides_alignment_and_shared_weights(dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, HF], ids=str)
+@pytest.mark.parametrize("size", [(3, 20, 1700, 264), (2, 100, 900, 328), (1, 300, 700, 264), (2, 33, 515, 201)], ids=str)
+@pytest.mark.parametrize("piece", [0, 256])
+def test_gradients_inside_larger_arrays(size, piece, dtype):
+    """Gradients in the middle of larger arrays, as parts of a flat gradient are: what lies around them stays."""
+    n, t, v, d = size
+    h, w, y, dloss = inputs(n, t, v, d, dtype)
+    op = train.LinearCrossEntropy(n, t, v, d, dtype, piece=piece)
+    loss, lse = op.loss(h, w, y)
+    gap = 64
+    flat = torch.full((n, gap + v * d + gap), 7.0, dtype=dtype, device="cuda")
+    around = torch.full((gap + n * t * d + gap,), 7.0, dtype=dtype, device="cuda")
+    dw = flat[:, gap:gap + v * d].view(n, v, d)
+    dh = around[gap:gap + n * t * d].view(n, t, d)
+    op.grad(h, w, y, lse, dloss, dhidden=dh, dweight=dw)
+    plain_dh, plain_dw = op.grad(h, w, y, lse, dloss)
+    assert torch.equal(dw, plain_dw) and torch.equal(dh, plain_dh)
+    assert bool((flat[:, :gap] == 7).all()) and bool((flat[:, gap + v * d:] == 7).all())
+    assert bool((around[:gap] == 7).all()) and bool((around[-gap:] == 7).all())
+    check(op, h, w, y, dloss, dtype)
+
+
+@pytest.mark.gpu
 def test_gradient_against_differences():
     """Central differences of the op's own loss along random directions: fp16 inputs moved by amounts they hold exactly."""
     n, t, v, d = 1, 40, 120, 32
