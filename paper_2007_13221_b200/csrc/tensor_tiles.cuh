@@ -547,8 +547,12 @@ struct Pipe {
     __device__ __forceinline__ bool take(Turn &t, uint32_t &at) {
         if (!warp_wait(&sh->acc_full[t.acc], t.ph)) return false;
         tmem_fence_after();
-        at = sh->tmem + (uint32_t)t.acc * kAccCols + ((uint32_t)(threadIdx.x / 32 % 4) << 21);
+        at = acc_at(t);
         return true;
+    }
+    // Where the accumulator taken last is.
+    __device__ __forceinline__ uint32_t acc_at(const Turn &t) const {
+        return sh->tmem + (uint32_t)t.acc * kAccCols + ((uint32_t)(threadIdx.x / 32 % 4) << 21);
     }
     // The same for the tile's small products, after its last chunk.
     __device__ __forceinline__ bool take_small(Turn &t, uint32_t &at) {

@@ -38,7 +38,9 @@ constexpr size_t kPieceBytes = 256ull << 20;
 // The tensor cores truncate every partial sum: 1.2e-6 of a logit over an inner dimension of 1024 (2.5e-6 of a small loss), 3e-6
 // over 4096.  So the loss's accumulators are taken out and added up, rounded, after this many stages: an inner dimension of 256
 // for few tokens, where memory is the bound, of 512 for many (of 256 the epilogue cannot keep up: tensor cores 73 % busy
-// instead of 85 % at 2048 tokens x 16384 x 4096).
+// instead of 85 % at 2048 tokens x 16384 x 4096).  The gradient's logits are summed in
+// the same chunks, so that p is of the logits that lse is of: 1 - p = 8e-4 of a nearly certain token came out 3 % off without
+// (4096 x 32768 x 4096, gradient 2.55 ms without, 2.62 with).
 __host__ __device__ constexpr int loss_chunk(int cg) { return cg == 1 ? 4 : 8; }
 constexpr int kOwnRatio = 256;                     // tokens of a worker up to which every warp finds the largest |dloss| itself
 constexpr int kJoinRows = 20;                     // rows that the last CTA joins itself, a warp or more for each
@@ -136,11 +138,12 @@ __device__ __forceinline__ uint4 remainder8(const float *v, const uint4 &o, int 
 }
 
 // ------------------------------------------------------------------ logits, tile by tile
-// What the tiles of z are for: a loss, a loss over a long inner dimension (chunks), dz.
-enum { kLoss = 0, kLongLoss = 1, kGrad = 2 };
+// What the tiles of z are for: a loss, or dz; over a long inner dimension in chunks, the same ones for both: a loss near 0 is
+// the difference of lse and z, and so is p - 1.
+enum { kLoss = 0, kLongLoss = 1, kGrad = 2, kLongGrad = 3 };
 template <int CG, int WHAT>
 struct LogitsJob {
-    static constexpr bool GRAD = WHAT == kGrad, LONG = WHAT == kLongLoss;
+    static constexpr bool GRAD = WHAT >= kGrad, LONG = WHAT == kLongLoss || WHAT == kLongGrad;
     const XentArgs &a;
     int first, every, vocab_tiles;
     static constexpr bool kCopier = false, kRemainders = false, kWaits = false;
@@ -176,6 +179,28 @@ struct LogitsJob {
             for (int p = 0; p < 4 / CG; ++p) tensor_copy_in(sb + p * 8192, w, k * 64, row_b + p * 64, wb, bar);
         }
     };
+    // The accumulator's turn, or all chunks added up, rounded: the warp's 64 columns.
+    template <int N>
+    __device__ __forceinline__ bool sums(Pipe<CG> &p, typename Pipe<CG>::Turn &turn, int chunks, int c0, int lane, float (&v)[N][32]) const {
+        uint32_t tmem;
+        for (int c = 0; c < chunks; ++c) {
+            if (!p.take(turn, tmem)) return false;
+            if (!LONG) break;
+            if (c == 0) {
+#pragma unroll
+                for (int b = 0; b < N; ++b) tmem_load(tmem + c0 + b * 32, v[b]);
+            } else
+#pragma unroll
+            for (int b = 0; b < 2 * N; ++b) {
+                float x[16];
+                tmem_load(tmem + c0 + b * 16, x);
+#pragma unroll
+                for (int k = 0; k < 16; ++k) v[b / 2][b % 2 * 16 + k] = __fadd_rn(v[b / 2][b % 2 * 16 + k], x[k]);
+            }
+            p.release(turn, lane);
+        }
+        return true;
+    }
     __device__ __forceinline__ bool epilogue(Pipe<CG> &p, const Tile &t, typename Pipe<CG>::Turn &turn, int warp, int lane) const {
         const int row = t.i * 128 * CG + (int)p.rank * 128 + warp % 4 * 32 + lane;
         const int c0 = warp / 4 * 64;
@@ -197,35 +222,16 @@ struct LogitsJob {
             const int64_t y = a.target[at];
             if (y >= 0 && y < a.vocab && y != a.ignore) target = (int)y;
         }
-        uint32_t tmem;
+        float v[LONG ? 2 : 1][32];                                   // all 64 columns, or 32 at a time
         if constexpr (!GRAD) {
-            float v[LONG ? 2 : 1][32];                               // all 64 columns, or 32 at a time
-            for (int c = 0; c < chunks; ++c) {
-                if (!p.take(turn, tmem)) return false;
-                if (!LONG) break;
-                if (c == 0) {
-#pragma unroll
-                    for (int b = 0; b < (LONG ? 2 : 0); ++b) tmem_load(tmem + c0 + b * 32, v[b]);
-                } else
-#pragma unroll
-                for (int b = 0; b < 4; ++b) {
-                    float x[16];
-                    tmem_load(tmem + c0 + b * 16, x);
-#pragma unroll
-                    for (int k = 0; k < 16; ++k) {
-                        float &sum = v[LONG ? b / 2 : 0][b % 2 * 16 + k];
-                        sum = __fadd_rn(sum, x[k]);
-                    }
-                }
-                p.release(turn, lane);
-            }
+            if (!sums(p, turn, chunks, c0, lane, v)) return false;
             float m = kLowest, s = 0.f;
 #pragma unroll(LONG ? 2 : 1)
             for (int b = 0; b < 64; b += 32) {
                 const int col = t.j * 256 + c0 + b;
                 float(&z)[32] = v[LONG ? b / 32 : 0];
                 if (!LONG) {
-                    tmem_load(tmem + c0 + b, z);
+                    tmem_load(p.acc_at(turn) + c0 + b, z);
                     if (b == 32) p.release(turn, lane);
                 }
                 if (col + 32 > a.vocab) {
@@ -259,30 +265,32 @@ struct LogitsJob {
                 ratio = a.ratio[at];
             }
             if (live) lse = a.lse[at];
-            if (!p.take(turn, tmem)) return false;
+            if (!sums(p, turn, chunks, c0, lane, v)) return false;
             char *dz = a.dz + (size_t)t.w * a.dz_worker;
-#pragma unroll 1
+#pragma unroll(LONG ? 2 : 1)
             for (int b = 0; b < 64; b += 32) {
                 const int in = t.j * 256 + c0 + b, col = a.piece0 + in;
-                float v[32];
-                tmem_load(tmem + c0 + b, v);
-                if (b == 32) p.release(turn, lane);
+                float(&x)[32] = v[LONG ? b / 32 : 0];
+                if (!LONG) {
+                    tmem_load(p.acc_at(turn) + c0 + b, x);
+                    if (b == 32) p.release(turn, lane);
+                }
 #pragma unroll
-                for (int k = 0; k < 32; ++k) v[k] = ratio * exp2_fast((v[k] - lse) * kLog2e);   // the difference first: it is exact where p is near 1
+                for (int k = 0; k < 32; ++k) x[k] = ratio * exp2_fast((x[k] - lse) * kLog2e);   // the difference first: it is exact where p is near 1
                 const unsigned off = (unsigned)(target - col);
                 if (off < 32u) {
 #pragma unroll
                     for (int k = 0; k < 32; ++k)
-                        if (off == (unsigned)k) v[k] -= ratio;
+                        if (off == (unsigned)k) x[k] -= ratio;
                 }
                 if (col + 32 > a.vocab || !(ratio != 0.f)) {        // padding, and tokens that do not count
 #pragma unroll
                     for (int k = 0; k < 32; ++k)
-                        if (col + k >= a.vocab || ratio == 0.f) v[k] = 0.f;
+                        if (col + k >= a.vocab || ratio == 0.f) x[k] = 0.f;
                 }
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    const float *e = v + 8 * k;
+                    const float *e = x + 8 * k;
                     uint4 o;
                     if (a.bf16)
                         o = make_uint4(pack_bf162(e[0], e[1]), pack_bf162(e[2], e[3]), pack_bf162(e[4], e[5]), pack_bf162(e[6], e[7]));
@@ -303,9 +311,11 @@ struct RowTarget {
     int64_t y;
     float z;
     __device__ __forceinline__ RowTarget(const XentArgs &a, size_t at, bool live) : y(live ? a.target[at] : 0), z(live ? __ldcg(a.z_target + at) : 0.f) {}
-    __device__ __forceinline__ void loss(const XentArgs &a, size_t at, float lse) const {
-        a.lse_out[at] = lse;
-        if (a.loss) a.loss[at] = y == a.ignore ? 0.f : y >= 0 && y < a.vocab ? lse - z : NAN;
+    // From the largest logit and the sum of exponentials relative to it; the logits' difference first: it is exact where the loss is small.
+    __device__ __forceinline__ void loss(const XentArgs &a, size_t at, float m, float s) const {
+        const float l = logf(s);
+        a.lse_out[at] = m + l;
+        if (a.loss) a.loss[at] = y == a.ignore ? 0.f : y >= 0 && y < a.vocab ? (m - z) + l : NAN;
     }
 };
 
@@ -338,7 +348,7 @@ __global__ void __launch_bounds__(1024) xent_join_kernel(const __grid_constant__
             s = s * exp2_fast((m - top) * kLog2e) + q.y * exp2_fast((q.x - top) * kLog2e);
             m = top;
         }
-        of.loss(a, at, m + logf(s));
+        of.loss(a, at, m, s);
     }
 }
 
@@ -352,7 +362,7 @@ __global__ void __launch_bounds__(kThreads, 1) xent_logits_kernel(const __grid_c
     LogitsJob<CG, WHAT> job{a, (int)blockIdx.x / CG, (int)gridDim.x / CG, (a.piece_n + 255) / 256};
     p.run(job);
     p.teardown();
-    if constexpr (WHAT != kGrad) {
+    if constexpr (WHAT < kGrad) {
         // Few rows: the last CTA to finish joins their parts (a kernel of its own: 5 us after 14).
         if (a.n * a.tokens > kJoinRows) return;
         __shared__ bool last;
@@ -402,7 +412,7 @@ __global__ void __launch_bounds__(kThreads, 1) xent_logits_kernel(const __grid_c
                 s = s * exp2_fast((m - top) * kLog2e) + q.y * exp2_fast((q.x - top) * kLog2e);
                 m = top;
             }
-            of.loss(a, threadIdx.x, m + logf(s));
+            of.loss(a, threadIdx.x, m, s);
         }
     }
 }
@@ -827,6 +837,7 @@ cudaError_t kernels_setup() {
     cudaError_t e = cudaFuncSetAttribute(xent_logits_kernel<CG, kLoss>, cudaFuncAttributeMaxDynamicSharedMemorySize, b);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(xent_logits_kernel<CG, kLongLoss>, cudaFuncAttributeMaxDynamicSharedMemorySize, b);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(xent_logits_kernel<CG, kGrad>, cudaFuncAttributeMaxDynamicSharedMemorySize, b);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(xent_logits_kernel<CG, kLongGrad>, cudaFuncAttributeMaxDynamicSharedMemorySize, b);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(xent_grad_kernel<CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)GradPipe<CG>::kSharedBytes);
     return e;
 }
@@ -867,7 +878,8 @@ int grad_launch(cser_xent *h, XentArgs &a, cudaStream_t st) {
         a.piece0 = (int)v, a.piece_n = (int)(h->vocab - v < h->piece ? h->vocab - v : h->piece);
         a.first_piece = v == 0, a.last_piece = v + h->piece >= h->vocab;
         const long long vt = up(a.piece_n, 128 * CG) / (128 * CG);
-        TRY((tiles_launch<CG>(h, xent_logits_kernel<CG, kGrad>, Pipe<CG>::kSharedBytes, (long long)a.n * a.token_tiles * ((a.piece_n + 255) / 256), st, a)));
+        const auto kernel = a.dim > loss_chunk(CG) * kStageK ? xent_logits_kernel<CG, kLongGrad> : xent_logits_kernel<CG, kGrad>;
+        TRY((tiles_launch<CG>(h, kernel, Pipe<CG>::kSharedBytes, (long long)a.n * a.token_tiles * ((a.piece_n + 255) / 256), st, a)));
         const long long n_dh = a.dh ? (long long)a.n * a.token_tiles * a.splits * dim_tiles : 0, n_dw = a.dw ? a.n * vt * dim_tiles : 0;
         TRY((tiles_launch<CG>(h, xent_grad_kernel<CG>, GradPipe<CG>::kSharedBytes, n_dh + n_dw, st, a, (int)n_dh, (int)n_dw)));
     }

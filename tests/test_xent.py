@@ -254,6 +254,31 @@ def test_gradients_inside_larger_arrays(size, piece, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, HF], ids=str)
+@pytest.mark.parametrize("size", [(1, 2, 2933), (1, 3, 4096), (150, 4, 2048), (2, 500, 1024)], ids=str)
+def test_tokens_that_are_nearly_certain(size, dtype):
+    """A loss near 0 and p - 1 are small differences of large logits.  z is the same in loss and gradient, so that what is off in
+    it (1e-5 of 1 + |lse|) moves 1 - p, and the loss, by its share of them only; beside that there is the rounding of lse and the
+    exponential's, 2^-24 |lse| + 2^-22 at most, of which a 1e-6 of 1 + |lse| is allowed."""
+    t, v, d = size
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(d)
+    w = (torch.randn((1, v, d), generator=gen, device="cuda") * 2 / d ** 0.5).to(dtype)
+    y = torch.randint(0, v, (1, t), generator=gen, device="cuda")
+    h = (0.4 * torch.randn((1, t, d), generator=gen, device="cuda") + 2.2 * w[0][y[0]].float()).to(dtype)
+    dloss = torch.ones((1, t), device="cuda")
+    op = train.LinearCrossEntropy(1, t, v, d, dtype)
+    loss, lse = op.loss(h, w, y)
+    dh, dw = op.grad(h, w, y, lse, dloss)
+    e_loss, e_lse, e_dh, e_dw, _, _ = exact(h, w, y, dloss)
+    size_of = 1 + float(e_lse.abs().max())
+    left = -torch.expm1(-e_loss)                                     # 1 - p
+    assert bool(((loss.double() - e_loss).abs() <= (1e-5 * left + 2.0 ** -22) * size_of).all())
+    off = GRAD[dtype] + 1e-5 * size_of + 1e-6 * size_of * t ** 0.5 / float(left.norm())
+    assert far(dh, e_dh) < off and far(dw, e_dw) < off
+
+
+@pytest.mark.gpu
 def test_gradient_against_differences():
     """Central differences of the op's own loss along random directions: fp16 inputs moved by amounts they hold exactly."""
     n, t, v, d = 1, 40, 120, 32
