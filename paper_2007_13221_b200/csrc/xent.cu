@@ -74,7 +74,8 @@ struct XentArgs {
     char *dz;                                      // [n][piece / 64 panels][tp rows][128 bytes]
     size_t dz_worker;
     float *acc;                                    // [n][splits][acc_rows][acc_cols] dh of the pieces so far
-    int acc_rows, acc_cols, splits, first_piece, last_piece;
+    int acc_rows, acc_cols, first_piece, last_piece;
+    int splits, shares;                            // of dh's inner dimension: kept in acc; of this piece, 1 .. splits, each of a stage at least
     void *dh, *dw;
     long long dw_stride;
     CUtensorMap dh_map, dw_map;                    // of the results, boxes of 64 x 32, where
@@ -461,11 +462,11 @@ struct GradJob {
             t.i = at % vocab_tiles, t.w = at / vocab_tiles;
             t.k0 = 0, t.stages = (a.tokens + 63) / 64, t.split = 0, t.a_lim = 0;
         } else {
-            t.split = at % a.splits, at /= a.splits;
+            t.split = at % a.shares, at /= a.shares;
             t.i = at % a.token_tiles, t.w = at / a.token_tiles;
             const int all = (a.piece_n + 63) / 64;
-            t.k0 = (int)((long long)all * t.split / a.splits);
-            t.stages = (int)((long long)all * (t.split + 1) / a.splits) - t.k0, t.a_lim = t.stages;
+            t.k0 = (int)((long long)all * t.split / a.shares);
+            t.stages = (int)((long long)all * (t.split + 1) / a.shares) - t.k0, t.a_lim = t.stages;
         }
         t.b_lim = 0;
     }
@@ -614,7 +615,7 @@ __global__ void __launch_bounds__(kThreads, 1) xent_grad_kernel(const __grid_con
                     (a.piece_n + 128 * CG - 1) / (128 * CG), 0};
     if (n_dh && n_dw) {
         // A tile of dh in tiles of dW, whose epilogue takes as long as 12 stages, and of which there may not be that many.
-        const int stages = ((a.piece_n + 63) / 64 + a.splits - 1) / a.splits, less = job.every - n_dh % job.every;
+        const int stages = ((a.piece_n + 63) / 64 + a.shares - 1) / a.shares, less = job.every - n_dh % job.every;
         const int each = (a.tokens + 63) / 64, fits = n_dw / less;
         job.early = stages / (each < 12 ? 12 : each);
         if (job.early > fits) job.early = fits;
@@ -877,10 +878,14 @@ int grad_launch(cser_xent *h, XentArgs &a, cudaStream_t st) {
     for (long long v = 0; v < h->vocab; v += h->piece) {
         a.piece0 = (int)v, a.piece_n = (int)(h->vocab - v < h->piece ? h->vocab - v : h->piece);
         a.first_piece = v == 0, a.last_piece = v + h->piece >= h->vocab;
+        // The last piece can have fewer stages than there are shares: a tile without a stage would have no accumulator.  The
+        // sums of the shares that it leaves out are complete with the pieces before.
+        const int stages = (a.piece_n + 63) / 64;
+        a.shares = a.splits < stages ? a.splits : stages;
         const long long vt = up(a.piece_n, 128 * CG) / (128 * CG);
         const auto kernel = a.dim > loss_chunk(CG) * kStageK ? xent_logits_kernel<CG, kLongGrad> : xent_logits_kernel<CG, kGrad>;
         TRY((tiles_launch<CG>(h, kernel, Pipe<CG>::kSharedBytes, (long long)a.n * a.token_tiles * ((a.piece_n + 255) / 256), st, a)));
-        const long long n_dh = a.dh ? (long long)a.n * a.token_tiles * a.splits * dim_tiles : 0, n_dw = a.dw ? a.n * vt * dim_tiles : 0;
+        const long long n_dh = a.dh ? (long long)a.n * a.token_tiles * a.shares * dim_tiles : 0, n_dw = a.dw ? a.n * vt * dim_tiles : 0;
         TRY((tiles_launch<CG>(h, xent_grad_kernel<CG>, GradPipe<CG>::kSharedBytes, n_dh + n_dw, st, a, (int)n_dh, (int)n_dw)));
     }
     if (a.dh && a.splits > 1) {

@@ -131,6 +131,21 @@ def test_pieces_of_the_vocabulary(piece, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, HF], ids=str)
+@pytest.mark.parametrize("size", [  # n, tokens, vocab, dim, piece: the last piece has 1, 2, 3, 4 stages of 64 or one more than shares
+    (1, 10, 2049, 64, 2048), (1, 10, 2100, 64, 2048), (1, 10, 2048 + 65, 72, 2048), (2, 40, 4096 + 129, 64, 2048), (1, 10, 2048 + 256, 64, 2048),
+    (1, 10, 2048 + 257, 64, 2048), (1, 200, 2049, 64, 2048), (2, 300, 2048 + 129, 264, 2048), (1, 130, 4096 + 193, 201, 2048),
+    (8, 16, 65600, 64, 0), (1, 1200, 104800, 200, 0)], ids=str)
+def test_a_last_piece_shorter_than_the_shares_of_the_others(size, dtype):
+    """dh's inner dimension is summed in shares where it has few tiles; every share has a stage, in the last piece too."""
+    n, t, v, d, piece = size
+    h, w, y, dloss = inputs(n, t, v, d, dtype)
+    op = train.LinearCrossEntropy(n, t, v, d, dtype, piece=piece)
+    loss, lse, dh, _ = check(op, h, w, y, dloss, dtype)
+    assert torch.equal(op.grad(h, w, y, lse, dloss, need_dweight=False)[0], dh)
+
+
+@pytest.mark.gpu
 def test_fewer_tokens_than_the_handle_was_made_for():
     n, v, d = 2, 900, 160
     op = train.LinearCrossEntropy(n, 700, v, d, BF)
