@@ -3,6 +3,9 @@
 They live in the same ``libcser.so`` as the optimizer step (``binding``) and surround it in a training step:
 ``LinearCrossEntropy`` gives the loss of a language model's head and its gradient, ``Orthogonalizer`` turns the
 matrices inside the flat [n_workers, d] gradient into orthogonalised updates that ``binding.CSER.step`` takes.
+
+``stream``: where a call runs (default: torch's current stream).  What it reads has to be ready there; results that it makes
+are made there, and the caller orders their use elsewhere.  Memory is safe without that: tensors may be dropped after the call.
 """
 import ctypes
 
@@ -52,6 +55,21 @@ def _want(ok, what):
         raise CSERError(what)
 
 
+def _on(stream, call, *args):
+    """call(...) with `stream` as the current one.  The allocator does not give out the arguments' memory again before `stream` has
+    passed this point, nor the results' before the caller's stream has passed the place where they are dropped."""
+    here = torch.cuda.current_stream()
+    for t in args:
+        if torch.is_tensor(t) and t.is_cuda:
+            t.record_stream(stream)
+    with torch.cuda.stream(stream):
+        got = call(*args)
+    for t in got if isinstance(got, tuple) else (got,):
+        if t is not None:
+            t.record_stream(here)
+    return got
+
+
 class Orthogonalizer:
     """Plan for the matrices ``[(offset, rows, cols), ...]`` inside each row of an [n_workers, ld] array.
 
@@ -79,6 +97,8 @@ class Orthogonalizer:
 
     def apply(self, grad, out=None, momentum=None, mu=0.0, stream=None):
         """grad [n, ld] -> out [n, ld] (made if not given: zeros outside the matrices); momentum is updated in place."""
+        if stream is not None:
+            return _on(stream, self.apply, grad, out, momentum, mu)
         size = (self.n, self.ld)
         if not (grad.is_cuda and grad.dtype == self.in_dtype and grad.shape == size and grad.is_contiguous()):
             raise CSERError(f"Orthogonalizer: grad must be a contiguous CUDA {self.in_dtype} tensor of shape {size}")
@@ -90,7 +110,7 @@ class Orthogonalizer:
                                          momentum.is_contiguous()):
             raise CSERError(f"Orthogonalizer: momentum must be a contiguous CUDA float32 tensor of shape {size}")
         _check(_lib.cser_orth_apply(self.h, grad.data_ptr(), None if momentum is None else momentum.data_ptr(), mu,
-                                    out.data_ptr(), _stream(stream)), "cser_orth_apply")
+                                    out.data_ptr(), _stream()), "cser_orth_apply")
         return out
 
     @property
@@ -145,14 +165,18 @@ class LinearCrossEntropy:
 
     def loss(self, hidden, weight, target, ignore_index=-100, stream=None):
         """(loss, lse), each fp32 [n, tokens]; lse is what grad takes."""
+        if stream is not None:
+            return _on(stream, self.loss, hidden, weight, target, ignore_index)
         args = self._inputs(hidden, weight, target, ignore_index)
         loss, lse = torch.empty_like(target, dtype=torch.float32), torch.empty_like(target, dtype=torch.float32)
-        _check(_lib.cser_xent_loss(self.h, ctypes.byref(args), loss.data_ptr(), lse.data_ptr(), _stream(stream)), "cser_xent_loss")
+        _check(_lib.cser_xent_loss(self.h, ctypes.byref(args), loss.data_ptr(), lse.data_ptr(), _stream()), "cser_xent_loss")
         return loss, lse
 
     def grad(self, hidden, weight, target, lse, dloss, ignore_index=-100, dhidden=None, dweight=None, need_dhidden=True,
              need_dweight=True, stream=None):
         """(dhidden, dweight) of sum(dloss * loss); dweight may be a [n, vocab, dim] view of a larger [n, d] array."""
+        if stream is not None:
+            return _on(stream, self.grad, hidden, weight, target, lse, dloss, ignore_index, dhidden, dweight, need_dhidden, need_dweight)
         args = self._inputs(hidden, weight, target, ignore_index)
         for a in (lse, dloss):
             if not (a.is_cuda and a.dtype == torch.float32 and a.shape == target.shape and a.is_contiguous()):
@@ -172,7 +196,7 @@ class LinearCrossEntropy:
         _check(_lib.cser_xent_grad(self.h, ctypes.byref(args), lse.data_ptr(), dloss.data_ptr(),
                                    dhidden.data_ptr() if need_dhidden else None,
                                    dweight.data_ptr() if need_dweight else None,
-                                   max(dweight.stride(0), self.vocab * self.dim) if need_dweight else 0, _stream(stream)),
+                                   max(dweight.stride(0), self.vocab * self.dim) if need_dweight else 0, _stream()),
                "cser_xent_grad")
         return dhidden if need_dhidden else None, dweight if need_dweight else None
 
