@@ -80,10 +80,11 @@ int64_t cser_orth_launch_count(cser_orth_handle h);
  * and for the upstream gradients dloss[i,t]:
  *     dz_v = (exp(z_v - lse) - [v = target]) * dloss ,   dhidden = sum_v dz_v weight[v] ,   dweight[v] = sum_t dz_v hidden[t]
  * A token whose target is ignore_index has loss 0 and adds nothing to the gradients.  A target outside 0..vocab-1 that
- * is not ignore_index makes that token's loss NaN, its row of dhidden NaN and its worker's dweight NaN.
+ * is not ignore_index makes that token's loss NaN, its row of dhidden NaN and its worker's dweight NaN; so does, for the gradients, a
+ * dloss that is not finite of a token that counts.
  *
  * Arithmetic.  hidden, weight, dhidden and dweight are of one type, BF16 or F16.  Logits, sums, lse and loss are fp32.  dz is
- * held in the operands' type between the products, relative to the worker's largest |dloss|, so a uniform dloss (the mean
+ * held in the operands' type between the products, relative to the worker's largest finite |dloss|, so a uniform dloss (the mean
  * over the tokens) adds no rounding.  Sums over pieces are fp32, in a fixed order: results are the same from call to call.
  */
 typedef struct cser_xent *cser_xent_handle;

@@ -90,14 +90,14 @@ __device__ __forceinline__ float row_ratio(const XentArgs &a, size_t at, float t
     if (y == a.ignore) return 0.f;
     if (y < 0 || y >= a.vocab) return NAN;
     const float d = a.dloss[at];
-    return d == 0.f ? 0.f : d / top * type_scale(a);                 // NaN stays NaN
+    return d == 0.f ? 0.f : isfinite(d) ? d / top * type_scale(a) : NAN;
 }
-// The largest |dloss| of a worker's tokens that count, by `n` threads of which this is `k`; not yet joined between them.
+// The largest finite |dloss| of a worker's tokens that count (one that is not finite spoils its own row of dh, not all), by `n` threads of which this is `k`; not yet joined between them.
 __device__ __forceinline__ float largest(const XentArgs &a, int worker, int k, int n) {
     const size_t base = (size_t)worker * a.tokens;
     float top = 0.f;
     for (int t = k; t < a.tokens; t += n)
-        if (a.target[base + t] != a.ignore) top = fmaxf(top, fabsf(a.dloss[base + t]));
+        if (a.target[base + t] != a.ignore && isfinite(a.dloss[base + t])) top = fmaxf(top, fabsf(a.dloss[base + t]));
     for (int m = 16; m; m >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, m));
     return top;
 }

@@ -198,6 +198,32 @@ def test_ignored_tokens_other_indices_and_targets_out_of_range(dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, HF], ids=str)
+@pytest.mark.parametrize("size", [(2, 20, 300, 64), (2, 90, 700, 72), (2, 300, 700, 201)], ids=str)
+def test_a_dloss_that_is_not_finite_stays_in_its_row(size, dtype):
+    """Its token's row of dhidden and its worker's dweight; tokens that do not count have no dloss."""
+    n, t, v, d = size
+    h, w, y, dloss = inputs(n, t, v, d, dtype)
+    op = train.LinearCrossEntropy(n, t, v, d, dtype)
+    loss, lse = op.loss(h, w, y)
+    y[:, 4:8] = 1
+    y[:, 9], y[:, 12] = IGN, IGN
+    loss, lse = op.loss(h, w, y)
+    hurt = dloss.clone()
+    hurt[0, 5], hurt[0, 6], hurt[0, 7] = float("inf"), -float("inf"), float("nan")
+    hurt[:, 9], hurt[:, 12] = float("inf"), float("nan")
+    dh, dw = op.grad(h, w, y, lse, hurt)
+    zero = torch.where(hurt.isfinite(), hurt, 0.0)
+    _, _, e_dh, e_dw, b_dh, b_dw = exact(h, w, y, zero)
+    rows = torch.ones_like(y, dtype=torch.bool)
+    rows[0, 5:8] = False
+    assert bool(((dh.double() - e_dh).abs() <= b_dh)[rows].all())
+    assert not bool(dh[0, 5:8].isfinite().all(1).any())
+    assert not bool(dw[0].isfinite().all(1).any())
+    assert bool(((dw.double() - e_dw).abs() <= b_dw)[1].all())
+
+
+@pytest.mark.gpu
 def test_large_logits_and_values_that_are_not_finite():
     n, t, v, d = 1, 70, 500, 64
     h, w, y, dloss = inputs(n, t, v, d, BF, spread=60.0)
