@@ -85,7 +85,8 @@ int64_t cser_orth_launch_count(cser_orth_handle h);
  *
  * Arithmetic.  hidden, weight, dhidden and dweight are of one type, BF16 or F16.  Logits, sums, lse and loss are fp32.  dz is
  * held in the operands' type between the products, relative to the worker's largest finite |dloss|, so a uniform dloss (the mean
- * over the tokens) adds no rounding.  Sums over pieces are fp32, in a fixed order: results are the same from call to call.
+ * over the tokens) adds no rounding; F16: where the |dloss| of a worker's tokens are more than 2^6 apart, a second time relative to each
+ * token's own for dhidden, so that its rows are as exact whatever their weight.  Sums over pieces are fp32, in a fixed order: results are the same from call to call.
  */
 typedef struct cser_xent *cser_xent_handle;
 
@@ -103,7 +104,7 @@ typedef struct cser_xent_inputs {
 
 /*
  * Workspace for up to max_tokens tokens per worker.  piece: vocabulary entries per piece of the gradient (rounded up to
- * a multiple of 256), 0 = chosen so that a piece of dz takes at most 256 MB.  1 <= vocab <= 2^24, 1 <= dim <= 65536,
+ * a multiple of 256), 0 = chosen so that a piece of dz takes at most 256 MB (twice that for F16).  1 <= vocab <= 2^24, 1 <= dim <= 65536,
  * 1 <= n_workers * max_tokens <= 2^24, n_workers * vocab and n_workers * ceil(max_tokens / 128) * ceil(vocab / 256) at most 2^30.
  * hidden or weights whose rows are not a multiple of 16 bytes apart (or not 16-byte aligned) are first copied: the buffer for that is
  * allocated with the handle where dim is no multiple of 8, else on the first such call, which must not be under stream capture.  Returns NULL on failure.

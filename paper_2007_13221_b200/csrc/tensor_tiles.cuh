@@ -367,8 +367,9 @@ struct Pipe {
     //   kWaits; bool ready(pipe, tile)   whether tiles read what this launch writes; then waits until that is in memory (before any role
     //                              hears of the tile).  If not, the launch may overlap the end of the kernel before it: tiles are worked
     //                              out from the kernel's arguments alone, copies and epilogue begin with earlier_done()
-    //   Loader                     made from a tile; uint32_t bytes(); void load(k, a, b, bar): copies of bytes() bytes into a and b (shared
-    //                              addresses; the lo halves of pairs kLoOffset behind)
+    //   Loader                     made from a tile; uint32_t bytes(); settle(job, tile), unless kWaits: what it reads that earlier kernels
+    //                              wrote; void load(k, a, b, bar): copies of bytes() bytes into a and b (shared addresses; the lo halves
+    //                              of pairs kLoOffset behind)
     //   int bf16()
     //   bool epilogue(pipe, tile, turn, warp, lane)   warp 0..15: for each chunk take(), read its columns, release();
     //                              false once a wait was.  Its warps do not wait for one another but on bounded barriers
@@ -394,8 +395,9 @@ struct Pipe {
                 typename Job::Loader from(job, t);
                 const uint32_t bytes = from.bytes();
                 const int stages = t.stages;
-                tile_done(walk);
                 if (first) earlier_done(), fence_async_global(), first = false;
+                if constexpr (!Job::kWaits) from.settle(job, t);
+                tile_done(walk);
                 for (int k = 0; k < stages; ++k) {
                     ok = wait(&sh->empty[s], ph ^ 1);
                     if (!ok) break;

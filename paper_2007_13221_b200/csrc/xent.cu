@@ -14,6 +14,9 @@
 // Rounding.  dz is rounded to the operands' type, 8 (bf16) or 11 (fp16) bits, as any product on these inputs has to.
 // It is held relative to the worker's largest |dloss| (times 2^12 for fp16, whose smallest normal number is above 1 / V for a
 // large vocabulary) and the factor is put back in fp32 at the end: for a mean over tokens dz is p - [target] itself, not p / T rounded.
+// fp16's range ends 2^-37 below the largest |dloss| that way, and a token of little weight would have its row of dh made from what is left of
+// it: p = 1e-5 under a weight of 2^-20 is nothing.  So where a worker's weights are more than 2^6 apart, dz is left a second time for dh, each row
+// relative to its own |dloss| (dW's rows add tokens up, and there 2^-37 of the largest is little).
 // Up to 32 tokens, where a single rounding (of p - 1 at the target) can be most of a result's error, what it left is kept too, in
 // rows that are padding otherwise: no more bytes, no more stages.
 #include <cuda.h>
@@ -52,6 +55,11 @@ __device__ __forceinline__ float exp2_fast(float x) {
     return y;
 }
 
+struct WorkerScale {
+    float unscale;
+    int by_row;                                    // dh is made from dz_rows
+};
+
 struct XentArgs {
     CUtensorMap h, w;                              // (dim, row, worker), boxes of 64 x 64
     int n, tokens, vocab, dim;
@@ -70,8 +78,10 @@ struct XentArgs {
     // gradient
     const float *lse, *dloss;
     float *ratio;                                  // [n * tokens] dloss relative to the largest, times the type's scale
-    float *unscale;                                // [n] what takes that back
+    WorkerScale *scale;                            // [n] what takes that back
+    float *row_unscale;                            // [n * tokens] the same for a row of dh
     char *dz;                                      // [n][piece / 64 panels][tp rows][128 bytes]
+    char *dz_rows;                                 // the same with a factor for each row; fp16 only
     size_t dz_worker;
     float *acc;                                    // [n][splits][acc_rows][acc_cols] dh of the pieces so far
     int acc_rows, acc_cols, first_piece, last_piece;
@@ -84,36 +94,59 @@ struct XentArgs {
 };
 
 // ------------------------------------------------------------------ dloss, relative to the largest
+// How far apart the weights of a worker's tokens are beyond which dh's rows have factors of their own: up to there every p above 1e-6
+// keeps all of fp16's bits.  Gradients with and without, fp16: 8 x 512 x 30522 x 1024 793 us and 675, 8 x 16 394 and 371, 4096 x 32768 x 4096
+// 2.84 ms and 2.68.
+constexpr float kApart = 64.f;
 __device__ __forceinline__ float type_scale(const XentArgs &a) { return a.bf16 ? 1.f : 4096.f; }
-__device__ __forceinline__ float row_ratio(const XentArgs &a, size_t at, float top) {
+// The largest and the smallest finite |dloss| but 0 of a worker's tokens that count.  (One that is not finite spoils its own row
+// of dh, not all.)
+struct Weights {
+    float top, low;
+    // By `n` threads of which this is `k`; not yet joined between warps.
+    __device__ __forceinline__ Weights(const XentArgs &a, int worker, int k, int n) : top(0.f), low(INFINITY) {
+        const size_t base = (size_t)worker * a.tokens;
+        for (int t = k; t < a.tokens; t += n) {
+            const float d = fabsf(a.dloss[base + t]);
+            if (a.target[base + t] != a.ignore && isfinite(d) && d != 0.f) top = fmaxf(top, d), low = fminf(low, d);
+        }
+        join();
+    }
+    __device__ __forceinline__ void join() {
+#pragma unroll
+        for (int m = 16; m; m >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, m)), low = fminf(low, __shfl_xor_sync(~0u, low, m));
+    }
+    __device__ __forceinline__ WorkerScale scale(const XentArgs &a) const { return {top / type_scale(a), !a.bf16 && low * kApart < top}; }
+};
+// A row's factor of dz relative to the largest dloss, and what takes its factor of dh back.
+__device__ __forceinline__ float row_ratio(const XentArgs &a, size_t at, float top, const WorkerScale &of, float &unscale) {
     const int64_t y = a.target[at];
+    unscale = of.unscale;
     if (y == a.ignore) return 0.f;
     if (y < 0 || y >= a.vocab) return NAN;
     const float d = a.dloss[at];
-    return d == 0.f ? 0.f : isfinite(d) ? d / top * type_scale(a) : NAN;
-}
-// The largest finite |dloss| of a worker's tokens that count (one that is not finite spoils its own row of dh, not all), by `n` threads of which this is `k`; not yet joined between them.
-__device__ __forceinline__ float largest(const XentArgs &a, int worker, int k, int n) {
-    const size_t base = (size_t)worker * a.tokens;
-    float top = 0.f;
-    for (int t = k; t < a.tokens; t += n)
-        if (a.target[base + t] != a.ignore && isfinite(a.dloss[base + t])) top = fmaxf(top, fabsf(a.dloss[base + t]));
-    for (int m = 16; m; m >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, m));
-    return top;
+    if (d == 0.f) return 0.f;
+    if (!isfinite(d)) return NAN;
+    if (of.by_row) unscale = fabsf(d) / type_scale(a);
+    return d / top * type_scale(a);
 }
 // One CTA per worker.
 __global__ void __launch_bounds__(1024) xent_ratio_kernel(const __grid_constant__ XentArgs a) {
-    __shared__ float red[32];
+    __shared__ float red[2][32];
     let_next_start();
     earlier_done();
-    float top = largest(a, blockIdx.x, threadIdx.x, 1024);
-    if (threadIdx.x % 32 == 0) red[threadIdx.x / 32] = top;
+    Weights w(a, blockIdx.x, threadIdx.x, 1024);
+    if (threadIdx.x % 32 == 0) red[0][threadIdx.x / 32] = w.top, red[1][threadIdx.x / 32] = w.low;
     __syncthreads();
-    top = red[threadIdx.x % 32];
-    for (int k = 16; k; k >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, k));
-    if (threadIdx.x == 0) a.unscale[blockIdx.x] = top / type_scale(a);
+    w.top = red[0][threadIdx.x % 32], w.low = red[1][threadIdx.x % 32];
+    w.join();
+    const WorkerScale of = w.scale(a);
+    if (threadIdx.x == 0) a.scale[blockIdx.x] = of;
     const size_t base = (size_t)blockIdx.x * a.tokens;
-    for (int t = threadIdx.x; t < a.tokens; t += 1024) a.ratio[base + t] = row_ratio(a, base + t, top);
+    for (int t = threadIdx.x; t < a.tokens; t += 1024) {
+        float unscale;
+        a.ratio[base + t] = row_ratio(a, base + t, w.top, of, unscale), a.row_unscale[base + t] = unscale;
+    }
 }
 
 // Boxes of 64 rows that a CTA's 128 tokens take, `left` of which there are: what the second one's place holds instead reaches
@@ -171,6 +204,7 @@ struct LogitsJob {
         __device__ __forceinline__ Loader(const LogitsJob &job, const Tile &t, int rank = CG == 1 ? 0 : (int)cluster_rank())
             : h(&job.a.h), w(&job.a.w), row_a(t.i * 128 * CG + rank * 128), row_b(job.a.piece0 + t.j * 256 + rank * 128),
               wa(job.a.h_workers == 1 ? 0 : t.w), wb(job.a.w_workers == 1 ? 0 : t.w), boxes(row_boxes(job.a.tokens - row_a)) {}
+        __device__ __forceinline__ void settle(const LogitsJob &, const Tile &) const {}
         __device__ __forceinline__ uint32_t bytes() const { return Pipe<CG>::kStageBytes - 16384 + (uint32_t)boxes * 8192; }
         __device__ __forceinline__ void load(int k, uint32_t sa, uint32_t sb, uint64_t *bar) const {
 #pragma unroll
@@ -201,6 +235,29 @@ struct LogitsJob {
             p.release(turn, lane);
         }
         return true;
+    }
+    // 32 columns of a row, of which `left` are not 0, times `factor` into the panels at `base`; `in`: the first one's place in the piece.
+    __device__ __forceinline__ void leave(float (&x)[32], float factor, int left, char *base, int worker, int in, int row, bool lows) const {
+#pragma unroll
+        for (int k = 0; k < 32; ++k) x[k] *= factor;
+        if (left < 32) {
+#pragma unroll
+            for (int k = 0; k < 32; ++k)
+                if (k >= left) x[k] = 0.f;
+        }
+        char *dz = base + (size_t)worker * a.dz_worker + (size_t)(in / 64) * a.tp * 128;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float *e = x + 8 * k;
+            uint4 o;
+            if (a.bf16)
+                o = make_uint4(pack_bf162(e[0], e[1]), pack_bf162(e[2], e[3]), pack_bf162(e[4], e[5]), pack_bf162(e[6], e[7]));
+            else
+                o = make_uint4(pack_half2(e[0], e[1]), pack_half2(e[2], e[3]), pack_half2(e[4], e[5]), pack_half2(e[6], e[7]));
+            char *to = dz + panel_chunk(row, in % 64 / 8 + k);
+            *reinterpret_cast<uint4 *>(to) = o;
+            if (lows) *reinterpret_cast<uint4 *>(to + 32 * 128) = remainder8(e, o, a.bf16);
+        }
     }
     __device__ __forceinline__ bool epilogue(Pipe<CG> &p, const Tile &t, typename Pipe<CG>::Turn &turn, int warp, int lane) const {
         const int row = t.i * 128 * CG + (int)p.rank * 128 + warp % 4 * 32 + lane;
@@ -258,16 +315,21 @@ struct LogitsJob {
             if (live) a.part[(size_t)(t.j * 4 + warp / 4) * a.n * a.tokens + at] = make_float2(m, s);
         } else {
             float ratio = 0.f, lse = 0.f;
+            int by_row;
             if (a.tokens <= kOwnRatio) {                             // no kernel came before that worked the ratios out
-                const float top = largest(a, t.w, lane, 32);
-                if (live) ratio = row_ratio(a, at, top);
-                if (warp == 0 && lane == 0) a.unscale[t.w] = top / type_scale(a);
-            } else if (live) {
-                ratio = a.ratio[at];
+                const Weights weights(a, t.w, lane, 32);
+                const WorkerScale of = weights.scale(a);
+                float unscale = 0.f;
+                if (live) ratio = row_ratio(a, at, weights.top, of, unscale);
+                if (t.j == 0 && warp < 4 && live) a.row_unscale[at] = unscale;
+                if (warp == 0 && lane == 0) a.scale[t.w] = of;
+                by_row = of.by_row;
+            } else {
+                if (live) ratio = a.ratio[at];
+                by_row = a.dz_rows && a.scale[t.w].by_row;
             }
             if (live) lse = a.lse[at];
             if (!sums(p, turn, chunks, c0, lane, v)) return false;
-            char *dz = a.dz + (size_t)t.w * a.dz_worker;
 #pragma unroll(LONG ? 2 : 1)
             for (int b = 0; b < 64; b += 32) {
                 const int in = t.j * 256 + c0 + b, col = a.piece0 + in;
@@ -277,30 +339,16 @@ struct LogitsJob {
                     if (b == 32) p.release(turn, lane);
                 }
 #pragma unroll
-                for (int k = 0; k < 32; ++k) x[k] = ratio * exp2_fast((x[k] - lse) * kLog2e);   // the difference first: it is exact where p is near 1
+                for (int k = 0; k < 32; ++k) x[k] = exp2_fast((x[k] - lse) * kLog2e);   // the difference first: it is exact where p is near 1
                 const unsigned off = (unsigned)(target - col);
                 if (off < 32u) {
 #pragma unroll
                     for (int k = 0; k < 32; ++k)
-                        if (off == (unsigned)k) x[k] -= ratio;
+                        if (off == (unsigned)k) x[k] -= 1.f;
                 }
-                if (col + 32 > a.vocab || !(ratio != 0.f)) {        // padding, and tokens that do not count
-#pragma unroll
-                    for (int k = 0; k < 32; ++k)
-                        if (col + k >= a.vocab || ratio == 0.f) x[k] = 0.f;
-                }
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const float *e = x + 8 * k;
-                    uint4 o;
-                    if (a.bf16)
-                        o = make_uint4(pack_bf162(e[0], e[1]), pack_bf162(e[2], e[3]), pack_bf162(e[4], e[5]), pack_bf162(e[6], e[7]));
-                    else
-                        o = make_uint4(pack_half2(e[0], e[1]), pack_half2(e[2], e[3]), pack_half2(e[4], e[5]), pack_half2(e[6], e[7]));
-                    char *to = dz + (size_t)(in / 64) * a.tp * 128 + panel_chunk(row, in % 64 / 8 + k);
-                    *reinterpret_cast<uint4 *>(to) = o;
-                    if (lows) *reinterpret_cast<uint4 *>(to + 32 * 128) = remainder8(e, o, a.bf16);
-                }
+                const int left = ratio == 0.f ? 0 : a.vocab - col;   // padding, and tokens that do not count, are 0 whatever x is
+                leave(x, ratio, left, a.dz, t.w, in, row, lows);
+                if (by_row) leave(x, ratio == 0.f ? 0.f : type_scale(a) / fabsf(ratio), left, a.dz_rows, t.w, in, row, lows);
             }
         }
         return true;
@@ -487,6 +535,9 @@ struct GradJob {
             col = t.j * 256 + rank * (t.n / CG), row0 = dw ? 0 : a.piece0 + t.k0 * 64;
             worker = (dw ? a.h_workers : a.w_workers) == 1 ? 0 : t.w, rows = dw ? 2 : row_boxes(a.tokens - row);
         }
+        __device__ __forceinline__ void settle(const GradJob &job, const Tile &t) {
+            if (!dw && job.a.dz_rows && job.a.scale[t.w].by_row) dz += job.a.dz_rows - job.a.dz;
+        }
         __device__ __forceinline__ uint32_t bytes() const { return (uint32_t)(rows + boxes) * 8192; }
         __device__ __forceinline__ void load(int k, uint32_t sa, uint32_t sb, uint64_t *bar) const {
             if (dw) {
@@ -537,8 +588,8 @@ struct GradJob {
         const int quarter = t.n / 4, c0 = warp / 4 * quarter, col0 = t.j * 256 + c0;
         const bool leaves = t.dw || (a.last_piece && a.splits == 1);
         const uint32_t at = p.extra + (uint32_t)warp * 4096;
-        const float f = a.unscale[t.w];
         const int rows = (t.dw ? a.piece_n : a.tokens) - row0;
+        const float f = t.dw ? a.scale[t.w].unscale : lane < rows ? a.row_unscale[(size_t)t.w * a.tokens + row] : 0.f;
         if (!p.take(turn, tmem)) return false;
         if (rows <= 0) {
             p.release(turn, lane);
@@ -655,7 +706,7 @@ __global__ void __launch_bounds__(256) xent_join_dh_kernel(const __grid_constant
         const float4 q = red[k][lane];
         v.x += q.x, v.y += q.y, v.z += q.z, v.w += q.w;
     }
-    const float f = a.unscale[w];
+    const float f = a.row_unscale[row_at];
     uint16_t *o = static_cast<uint16_t *>(a.dh) + row_at * a.dim + col;
     const uint32_t lo = a.bf16 ? pack_bf162(v.x * f, v.y * f) : pack_half2(v.x * f, v.y * f);
     const uint32_t hi = a.bf16 ? pack_bf162(v.z * f, v.w * f) : pack_half2(v.z * f, v.w * f);
@@ -724,9 +775,10 @@ struct cser_xent {
     int parts = 0, tp = 0, acc_cols = 0;
     void *work = nullptr;
     float2 *part = nullptr;
-    float *z_target = nullptr, *ratio = nullptr, *unscale = nullptr, *acc = nullptr;
+    float *z_target = nullptr, *ratio = nullptr, *row_unscale = nullptr, *acc = nullptr;
+    WorkerScale *scale = nullptr;
     unsigned *ticket = nullptr;
-    char *dz = nullptr;
+    char *dz = nullptr, *dz_rows = nullptr;
     void *pack_h = nullptr, *pack_w = nullptr;     // made on the first call that needs them
     encode_fn encode = nullptr;
     unsigned *err_host = nullptr, *err_dev = nullptr;
@@ -820,7 +872,7 @@ int prepare_call(cser_xent *h, const cser_xent_inputs *in, const char *what, Xen
     }
     a.bf16 = h->type == CSER_TYPE_BF16;
     a.tp = h->tp, a.part = h->part, a.parts = h->parts, a.z_target = h->z_target, a.target = in->target, a.ignore = in->ignore_index;
-    a.ratio = h->ratio, a.unscale = h->unscale, a.dz = h->dz, a.dz_worker = (size_t)(h->piece / 64) * h->tp * 128;
+    a.ratio = h->ratio, a.scale = h->scale, a.row_unscale = h->row_unscale, a.dz = h->dz, a.dz_rows = h->dz_rows, a.dz_worker = (size_t)(h->piece / 64) * h->tp * 128;
     a.ticket = h->ticket, a.acc = h->acc, a.acc_rows = (int)up(a.tokens, 256), a.acc_cols = h->acc_cols, a.err = h->err_dev;
     return CSER_OK;
 }
@@ -942,7 +994,9 @@ cser_xent_handle cser_xent_create(int32_t n_workers, int64_t max_tokens, int64_t
     size_t at = 0;
     auto place = [&](size_t b) { const size_t p = at; at += (b + 1023) / 1024 * 1024; return p; };
     const size_t o_part = place((size_t)rows * h->parts * 8), o_zt = place((size_t)rows * 4), o_ratio = place((size_t)rows * 4),
-                 o_un = place((size_t)n_workers * 4), o_tick = place(4), o_dz = place((size_t)n_workers * (h->piece / 64) * h->tp * 128),
+                 o_un = place((size_t)n_workers * sizeof(WorkerScale)), o_run = place((size_t)rows * 4), o_tick = place(4),
+                 o_dz = place((size_t)n_workers * (h->piece / 64) * h->tp * 128), dz_bytes = at - o_dz,
+                 o_dzr = place(type == CSER_TYPE_F16 ? dz_bytes : 0),
                  o_acc = place((size_t)n_workers * acc_rows * h->acc_cols * 4);
     e = cudaMalloc(&h->work, at);
     if (dim % 8) {                                 // dense rows of this length need packing
@@ -956,8 +1010,9 @@ cser_xent_handle cser_xent_create(int32_t n_workers, int64_t max_tokens, int64_t
     e = cudaMemset(h->ticket, 0, 4);
     if (e != cudaSuccess) return drop(e);
     h->part = reinterpret_cast<float2 *>(w + o_part), h->z_target = reinterpret_cast<float *>(w + o_zt);
-    h->ratio = reinterpret_cast<float *>(w + o_ratio), h->unscale = reinterpret_cast<float *>(w + o_un);
-    h->dz = w + o_dz, h->acc = reinterpret_cast<float *>(w + o_acc);
+    h->ratio = reinterpret_cast<float *>(w + o_ratio), h->row_unscale = reinterpret_cast<float *>(w + o_run);
+    h->scale = reinterpret_cast<WorkerScale *>(w + o_un);
+    h->dz = w + o_dz, h->dz_rows = type == CSER_TYPE_F16 ? w + o_dzr : nullptr, h->acc = reinterpret_cast<float *>(w + o_acc);
     return h;
 }
 

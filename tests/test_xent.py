@@ -224,6 +224,47 @@ def test_a_dloss_that_is_not_finite_stays_in_its_row(size, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("size", [(1, 20, 20000, 64), (1, 70, 20000, 72), (2, 300, 20000, 64), (1, 100, 9000, 1032), (1, 9, 60000, 64)], ids=str)
+@pytest.mark.parametrize("dtype", [BF, HF], ids=str)
+def test_rows_of_tokens_with_little_weight(size, dtype):
+    """dloss of 1 to 2^-20 of the largest: a row of dhidden is as exact relative to its own dloss.  The weights have a common
+    part, so that the many small p of a row add up.  Every entry: u |dz| |W| + 2e-5 (1 + |lse|) p |dloss| |W| + the result's
+    rounding as elsewhere, and the spacing of the smallest dz, 2^-37 of the largest dloss of which the token's is 1/64 at
+    least, or of the token's own: 2^-31 |dloss|."""
+    n, t, v, d = size
+    h, w, y, _ = inputs(n, t, v, d, dtype, spread=0.5)
+    w = (w.float() + 0.5).to(dtype)
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(t)
+    dloss = 4096 * torch.exp2(-20 * torch.rand((n, t), generator=gen, device="cuda")) * torch.randint(0, 2, (n, t), generator=gen, device="cuda").mul(2).sub(1)
+    dloss[:, 0], dloss[:, 1], dloss[:, 2] = 4096, 4096 * 2.0 ** -20, 0
+    op = train.LinearCrossEntropy(n, t, v, d, dtype)
+    _, lse = op.loss(h, w, y)
+    dh, dw = op.grad(h, w, y, lse, dloss)
+    u, tiny = (2.0 ** -8, 0.0) if dtype == BF else (2.0 ** -11, 2.0 ** -25)
+    for i in range(n):
+        hi, wi = h[i].double(), w[i].double()
+        ok = y[i] != IGN
+        z = hi @ wi.t()
+        l = torch.logsumexp(z, 1)[:, None]
+        p = torch.exp(z - l)
+        g = (dloss[i].double() * ok)[:, None]
+        off = 2e-5 * (1 + l.abs()) * p * g.abs() + 2.0 ** -31 * g.abs()
+        p[torch.arange(t, device="cuda"), torch.where(ok, y[i], 0)] -= 1
+        dz = p * g
+        want = dz @ wi
+        bound = 1.1 * ((off + u * dz.abs()) @ wi.abs() + u * want.abs() + tiny)
+        assert bool(((dh[i].double() - want).abs() <= bound).all())
+        # and as a whole, row by row: roundings of dz and of the result are independent of one another
+        live = ok & (dloss[i].abs() > 0)
+        err = (dh[i].double() - want)[live].norm(dim=1)
+        size_of = u * (dz[live].square() @ wi.square()).sum(1).sqrt() + u * want[live].norm(dim=1) + (off[live] @ wi.abs()).norm(dim=1) + tiny * d ** 0.5
+        assert bool((err <= 1.1 * size_of).all())
+    _, _, _, e_dw, _, b_dw = exact(h, w, y, dloss)
+    assert bool(((dw.double() - e_dw).abs() <= b_dw).all())
+
+
+@pytest.mark.gpu
 def test_large_logits_and_values_that_are_not_finite():
     n, t, v, d = 1, 70, 500, 64
     h, w, y, dloss = inputs(n, t, v, d, BF, spread=60.0)
