@@ -23,6 +23,7 @@
 #include <cuda_runtime.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
+#include <float.h>
 #include <math.h>
 #include <stdint.h>
 #include <stdio.h>
@@ -36,7 +37,7 @@ namespace {
 #include "tensor_tiles.cuh"
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLowest = -1e30f;                  // below every logit, and finite times log2(e)
+constexpr float kLowest = -FLT_MAX;                // a maximum of nothing: no finite logit is lower, and differences from it are not NaN
 constexpr size_t kPieceBytes = 256ull << 20;
 // The tensor cores truncate every partial sum: 1.2e-6 of a logit over an inner dimension of 1024 (2.5e-6 of a small loss), 3e-6
 // over 4096.  So the loss's accumulators are taken out and added up, rounded, after this many stages: an inner dimension of 256

@@ -265,6 +265,23 @@ def test_rows_of_tokens_with_little_weight(size, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("t", [3, 50, 200])
+def test_logits_of_any_finite_size(t):
+    """Rows whose logits all lie near the type's lowest value, beside ordinary ones."""
+    n, v, d = 1, 300, 16
+    h, w, y, dloss = inputs(n, t, v, d, BF)
+    w = w.float()
+    w[..., 0] = 1 + torch.arange(v, device="cuda") / 64.0
+    h = h.float()
+    h[0, 1, :], h[0, 1, 0] = 0, -1e35
+    h[0, 2, :], h[0, 2, 0] = 0, -1e38 / 4
+    h, w = h.bfloat16(), w.bfloat16()
+    y[0, 1], y[0, 2] = 0, 5
+    op = train.LinearCrossEntropy(n, t, v, d, BF)
+    check(op, h, w, y, dloss, BF)
+
+
+@pytest.mark.gpu
 def test_large_logits_and_values_that_are_not_finite():
     n, t, v, d = 1, 70, 500, 64
     h, w, y, dloss = inputs(n, t, v, d, BF, spread=60.0)
