@@ -79,7 +79,8 @@ int64_t cser_orth_launch_count(cser_orth_handle h);
  *     z_v = <hidden[i,t,:], weight[i,v,:]> ,   lse = log sum_v exp z_v ,   loss = lse - z_target
  * and for the upstream gradients dloss[i,t]:
  *     dz_v = (exp(z_v - lse) - [v = target]) * dloss ,   dhidden = sum_v dz_v weight[v] ,   dweight[v] = sum_t dz_v hidden[t]
- * A token whose target is ignore_index has loss 0 and adds nothing to the gradients.  A target outside 0..vocab-1 that
+ * A token whose target is ignore_index has loss 0 and adds nothing to the gradients, even where its hidden state is not finite; nor does
+ * one whose dloss is 0.  A target outside 0..vocab-1 that
  * is not ignore_index makes that token's loss NaN, its row of dhidden NaN and its worker's dweight NaN; so does, for the gradients, a
  * dloss that is not finite of a token that counts.
  *

@@ -58,8 +58,10 @@ __device__ __forceinline__ float exp2_fast(float x) {
 
 struct WorkerScale {
     float unscale;
-    int by_row;                                    // dh is made from dz_rows
+    int flags;
 };
+// dh is made from dz_rows; dW is made from h_clean.
+enum { kByRow = 1, kCleaned = 2 };
 
 struct XentArgs {
     CUtensorMap h, w;                              // (dim, row, worker), boxes of 64 x 64
@@ -83,6 +85,11 @@ struct XentArgs {
     float *row_unscale;                            // [n * tokens] the same for a row of dh
     char *dz;                                      // [n][piece / 64 panels][tp rows][128 bytes]
     char *dz_rows;                                 // the same with a factor for each row; fp16 only
+    const uint16_t *h_at;                          // what the map `h` is of
+    long long h_row, h_worker;
+    uint16_t *h_clean;                             // [n][clean_rows][dim, rounded up to 8] see clean_rows()
+    int clean_rows;
+    const CUtensorMap *h_clean_map;                // in the workspace: arguments of a launch take time on the host
     size_t dz_worker;
     float *acc;                                    // [n][splits][acc_rows][acc_cols] dh of the pieces so far
     int acc_rows, acc_cols, first_piece, last_piece;
@@ -101,24 +108,46 @@ struct XentArgs {
 constexpr float kApart = 64.f;
 __device__ __forceinline__ float type_scale(const XentArgs &a) { return a.bf16 ? 1.f : 4096.f; }
 // The largest and the smallest finite |dloss| but 0 of a worker's tokens that count.  (One that is not finite spoils its own row
-// of dh, not all.)
+// of dh, not all.)  And whether a token that does not count, or whose dloss is 0, has a hidden state that is not finite: no logit, and so no
+// lse, is finite then.
 struct Weights {
     float top, low;
+    int dirty;
     // By `n` threads of which this is `k`; not yet joined between warps.
-    __device__ __forceinline__ Weights(const XentArgs &a, int worker, int k, int n) : top(0.f), low(INFINITY) {
+    __device__ __forceinline__ Weights(const XentArgs &a, int worker, int k, int n) : top(0.f), low(INFINITY), dirty(0) {
         const size_t base = (size_t)worker * a.tokens;
         for (int t = k; t < a.tokens; t += n) {
-            const float d = fabsf(a.dloss[base + t]);
-            if (a.target[base + t] != a.ignore && isfinite(d) && d != 0.f) top = fmaxf(top, d), low = fminf(low, d);
+            const float d = fabsf(a.dloss[base + t]), lse = a.lse[base + t];
+            const bool counts = a.target[base + t] != a.ignore && d != 0.f;
+            if (counts && isfinite(d)) top = fmaxf(top, d), low = fminf(low, d);
+            dirty |= !counts && !isfinite(lse);
         }
         join();
     }
     __device__ __forceinline__ void join() {
 #pragma unroll
         for (int m = 16; m; m >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, m)), low = fminf(low, __shfl_xor_sync(~0u, low, m));
+        dirty = __any_sync(~0u, dirty);
     }
-    __device__ __forceinline__ WorkerScale scale(const XentArgs &a) const { return {top / type_scale(a), !a.bf16 && low * kApart < top}; }
+    __device__ __forceinline__ WorkerScale scale(const XentArgs &a) const {
+        return {top / type_scale(a), (!a.bf16 && low * kApart < top ? kByRow : 0) | (dirty ? kCleaned : 0)};
+    }
 };
+// 32 rows of hidden states by a warp, as dW takes them where a worker has such tokens: theirs as zeros (dz is 0 there, but 0 x NaN is
+// not), and zeros up to the products' 64.
+__device__ __forceinline__ void clean_rows(const XentArgs &a, int worker, int row0, int lane) {
+    const size_t at = (size_t)worker * a.tokens + row0 + lane;
+    const bool zero = row0 + lane >= a.tokens || ((a.target[at] == a.ignore || a.dloss[at] == 0.f) && !isfinite(a.lse[at]));
+    const unsigned zeros = __ballot_sync(~0u, zero);
+    const int padded = (a.dim + 7) / 8 * 8;
+#pragma unroll 1
+    for (int r = 0; r < 32; ++r) {
+        const uint16_t *from = a.h_at + worker * a.h_worker + (row0 + r) * a.h_row;
+        uint16_t *to = a.h_clean + ((size_t)worker * a.clean_rows + row0 + r) * padded;
+#pragma unroll 1
+        for (int c = lane; c < padded; c += 32) to[c] = zeros >> r & 1 || c >= a.dim ? (uint16_t)0 : from[c];
+    }
+}
 // A row's factor of dz relative to the largest dloss, and what takes its factor of dh back.
 __device__ __forceinline__ float row_ratio(const XentArgs &a, size_t at, float top, const WorkerScale &of, float &unscale) {
     const int64_t y = a.target[at];
@@ -128,7 +157,7 @@ __device__ __forceinline__ float row_ratio(const XentArgs &a, size_t at, float t
     const float d = a.dloss[at];
     if (d == 0.f) return 0.f;
     if (!isfinite(d)) return NAN;
-    if (of.by_row) unscale = fabsf(d) / type_scale(a);
+    if (of.flags & kByRow) unscale = fabsf(d) / type_scale(a);
     return d / top * type_scale(a);
 }
 // One CTA per worker.
@@ -141,6 +170,7 @@ __global__ void __launch_bounds__(1024) xent_ratio_kernel(const __grid_constant_
     __syncthreads();
     w.top = red[0][threadIdx.x % 32], w.low = red[1][threadIdx.x % 32];
     w.join();
+    w.dirty = __syncthreads_or(w.dirty);
     const WorkerScale of = w.scale(a);
     if (threadIdx.x == 0) a.scale[blockIdx.x] = of;
     const size_t base = (size_t)blockIdx.x * a.tokens;
@@ -316,7 +346,7 @@ struct LogitsJob {
             if (live) a.part[(size_t)(t.j * 4 + warp / 4) * a.n * a.tokens + at] = make_float2(m, s);
         } else {
             float ratio = 0.f, lse = 0.f;
-            int by_row;
+            int flags;
             if (a.tokens <= kOwnRatio) {                             // no kernel came before that worked the ratios out
                 const Weights weights(a, t.w, lane, 32);
                 const WorkerScale of = weights.scale(a);
@@ -324,11 +354,12 @@ struct LogitsJob {
                 if (live) ratio = row_ratio(a, at, weights.top, of, unscale);
                 if (t.j == 0 && warp < 4 && live) a.row_unscale[at] = unscale;
                 if (warp == 0 && lane == 0) a.scale[t.w] = of;
-                by_row = of.by_row;
+                flags = of.flags;
             } else {
                 if (live) ratio = a.ratio[at];
-                by_row = a.dz_rows && a.scale[t.w].by_row;
+                flags = a.scale[t.w].flags;
             }
+            if (flags & kCleaned && t.j == 0 && a.first_piece && warp < 4) clean_rows(a, t.w, row - lane, lane);
             if (live) lse = a.lse[at];
             if (!sums(p, turn, chunks, c0, lane, v)) return false;
 #pragma unroll(LONG ? 2 : 1)
@@ -349,7 +380,7 @@ struct LogitsJob {
                 }
                 const int left = ratio == 0.f ? 0 : a.vocab - col;   // padding, and tokens that do not count, are 0 whatever x is
                 leave(x, ratio, left, a.dz, t.w, in, row, lows);
-                if (by_row) leave(x, ratio == 0.f ? 0.f : type_scale(a) / fabsf(ratio), left, a.dz_rows, t.w, in, row, lows);
+                if (flags & kByRow) leave(x, ratio == 0.f ? 0.f : type_scale(a) / fabsf(ratio), left, a.dz_rows, t.w, in, row, lows);
             }
         }
         return true;
@@ -478,6 +509,7 @@ struct GradJob {
     using P = GradPipe<CG>;
     const XentArgs &a;
     int first, every, n_dh, n_dw, dim_tiles, vocab_tiles, early;
+    int known = -1, flags = 0;                     // of the worker of the copying thread's last tile
     static constexpr bool kCopier = false, kRemainders = CG == 1, kWaits = false;
     __device__ __forceinline__ bool remainders() const { return a.tokens <= kLowRows; }
 
@@ -536,8 +568,10 @@ struct GradJob {
             col = t.j * 256 + rank * (t.n / CG), row0 = dw ? 0 : a.piece0 + t.k0 * 64;
             worker = (dw ? a.h_workers : a.w_workers) == 1 ? 0 : t.w, rows = dw ? 2 : row_boxes(a.tokens - row);
         }
-        __device__ __forceinline__ void settle(const GradJob &job, const Tile &t) {
-            if (!dw && job.a.dz_rows && job.a.scale[t.w].by_row) dz += job.a.dz_rows - job.a.dz;
+        __device__ __forceinline__ void settle(GradJob &job, const Tile &t) {
+            if (job.known != t.w) job.known = t.w, job.flags = __ldcg(&job.a.scale[t.w].flags);
+            if (!dw && job.flags & kByRow) dz += job.a.dz_rows - job.a.dz;
+            if (dw && job.flags & kCleaned) b = job.a.h_clean_map, worker = t.w;
         }
         __device__ __forceinline__ uint32_t bytes() const { return (uint32_t)(rows + boxes) * 8192; }
         __device__ __forceinline__ void load(int k, uint32_t sa, uint32_t sb, uint64_t *bar) const {
@@ -780,6 +814,8 @@ struct cser_xent {
     WorkerScale *scale = nullptr;
     unsigned *ticket = nullptr;
     char *dz = nullptr, *dz_rows = nullptr;
+    uint16_t *h_clean = nullptr;
+    CUtensorMap *h_clean_map = nullptr;
     void *pack_h = nullptr, *pack_w = nullptr;     // made on the first call that needs them
     encode_fn encode = nullptr;
     unsigned *err_host = nullptr, *err_dev = nullptr;
@@ -814,8 +850,9 @@ bool tensor_map(const cser_xent *h, CUtensorMap &m, const void *p, long long row
                      CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// The map of an operand, of a packed copy (then `job` says of what) where its rows cannot be read in place.
-int operand(cser_xent *h, CUtensorMap &m, int &workers, const void *p, long long rows, long long row_stride, long long worker_stride,
+// The map of an operand, of a packed copy (then `job` says of what, and the address and strides become its) where its rows cannot
+// be read in place.
+int operand(cser_xent *h, CUtensorMap &m, int &workers, const void *&p, long long rows, long long &row_stride, long long &worker_stride,
             void *&pack, long long pack_rows, PackSource &job, const char *what, cudaStream_t st) {
     workers = h->n == 1 || worker_stride == 0 ? 1 : h->n;
     if (rows == 1) row_stride = up(h->dim, 8);                      // no second row: its distance says nothing
@@ -859,12 +896,12 @@ int prepare_call(cser_xent *h, const cser_xent_inputs *in, const char *what, Xen
     if ((uintptr_t)in->hidden % 2 || (uintptr_t)in->weight % 2 || (uintptr_t)in->target % 8)
         return cser_internal_fail(CSER_ERR_INVALID, "%s: a pointer is not aligned to its element type", what);
     PackSource pack[2] = {};
-    if (int rc = operand(h, a.h, a.h_workers, in->hidden, in->tokens, in->hidden_row_stride, in->hidden_worker_stride, h->pack_h,
-                         h->max_tokens, pack[0], "hidden", st))
-        return rc;
-    if (int rc = operand(h, a.w, a.w_workers, in->weight, h->vocab, in->weight_row_stride, in->weight_worker_stride, h->pack_w, h->vocab,
-                         pack[1], "weight", st))
-        return rc;
+    const void *hid = in->hidden, *wei = in->weight;
+    long long h_row = in->hidden_row_stride, h_worker = in->hidden_worker_stride, w_row = in->weight_row_stride, w_worker = in->weight_worker_stride;
+    if (int rc = operand(h, a.h, a.h_workers, hid, in->tokens, h_row, h_worker, h->pack_h, h->max_tokens, pack[0], "hidden", st)) return rc;
+    if (int rc = operand(h, a.w, a.w_workers, wei, h->vocab, w_row, w_worker, h->pack_w, h->vocab, pack[1], "weight", st)) return rc;
+    a.h_at = static_cast<const uint16_t *>(hid), a.h_row = h_row, a.h_worker = a.h_workers == 1 ? 0 : h_worker;
+    a.h_clean = h->h_clean, a.h_clean_map = h->h_clean_map, a.clean_rows = (int)up(h->max_tokens, 64);
     if (pack[0].all + pack[1].all > 0) {
         const int chunks = (int)(up(h->dim, 8) / 8), per = chunks < 256 ? chunks : 256, rows = 256 / per;
         TRY(launch_kernel(xent_pack_kernel, (unsigned)(((long long)pack[0].all + pack[1].all + rows - 1) / rows), 256, 0, 1, true, st, pack[0],
@@ -998,6 +1035,7 @@ cser_xent_handle cser_xent_create(int32_t n_workers, int64_t max_tokens, int64_t
                  o_un = place((size_t)n_workers * sizeof(WorkerScale)), o_run = place((size_t)rows * 4), o_tick = place(4),
                  o_dz = place((size_t)n_workers * (h->piece / 64) * h->tp * 128), dz_bytes = at - o_dz,
                  o_dzr = place(type == CSER_TYPE_F16 ? dz_bytes : 0),
+                 o_map = place(sizeof(CUtensorMap)), o_clean = place((size_t)n_workers * up(max_tokens, 64) * up(dim, 8) * 2),
                  o_acc = place((size_t)n_workers * acc_rows * h->acc_cols * 4);
     e = cudaMalloc(&h->work, at);
     if (dim % 8) {                                 // dense rows of this length need packing
@@ -1013,6 +1051,12 @@ cser_xent_handle cser_xent_create(int32_t n_workers, int64_t max_tokens, int64_t
     h->part = reinterpret_cast<float2 *>(w + o_part), h->z_target = reinterpret_cast<float *>(w + o_zt);
     h->ratio = reinterpret_cast<float *>(w + o_ratio), h->row_unscale = reinterpret_cast<float *>(w + o_run);
     h->scale = reinterpret_cast<WorkerScale *>(w + o_un);
+    h->h_clean = reinterpret_cast<uint16_t *>(w + o_clean);
+    h->h_clean_map = reinterpret_cast<CUtensorMap *>(w + o_map);
+    CUtensorMap map;
+    const bool made = tensor_map(h, map, h->h_clean, up(max_tokens, 64), up(dim, 8), up(max_tokens, 64) * up(dim, 8), n_workers, dim);
+    e = made ? cudaMemcpy(h->h_clean_map, &map, sizeof(map), cudaMemcpyHostToDevice) : cudaErrorInvalidValue;
+    if (e != cudaSuccess) return drop(e);
     h->dz = w + o_dz, h->dz_rows = type == CSER_TYPE_F16 ? w + o_dzr : nullptr, h->acc = reinterpret_cast<float *>(w + o_acc);
     return h;
 }

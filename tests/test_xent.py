@@ -282,6 +282,51 @@ def test_logits_of_any_finite_size(t):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, HF], ids=str)
+@pytest.mark.parametrize("size", [(2, 20, 300, 64, 0), (2, 32, 300, 72, 0), (3, 90, 700, 201, 256), (2, 300, 700, 136, 0), (2, 333, 3000, 264, 1024),
+                                  (1, 70, 50, 1, 0)], ids=str)
+def test_hidden_states_of_tokens_that_do_not_count_may_be_anything(size, dtype):
+    """The same gradients, bit for bit, as with zeros there."""
+    n, t, v, d, piece = size
+    h, w, y, dloss = inputs(n, t, v, d, dtype)
+    y[:, :8] = 1
+    y[:, 3], y[0, 5], y[:, t - 1] = IGN, IGN, IGN
+    dloss[:, 6] = 0
+    op = train.LinearCrossEntropy(n, t, v, d, dtype, piece=piece)
+    blank = h.clone()
+    blank[:, 3], blank[0, 5], blank[:, t - 1], blank[:, 6] = 0, 0, 0, 0
+    odd = blank.clone()
+    odd[:, 3], odd[0, 5, 0], odd[:, t - 1], odd[:, 6] = float("nan"), float("inf"), -float("inf"), float("nan")
+    if d > 1:
+        odd[:, t - 1, 1] = float("inf")
+    loss, lse = op.loss(blank, w, y)
+    want = op.grad(blank, w, y, lse, dloss)
+    check(op, blank, w, y, dloss, dtype)
+    loss2, lse2 = op.loss(odd, w, y)
+    counted = torch.ones_like(y, dtype=torch.bool)
+    counted[:, 6] = False
+    assert torch.equal(loss2[counted], loss[counted])
+    got = op.grad(odd, w, y, lse2, dloss)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    got = op.grad(odd, w, y, lse2, dloss, need_dhidden=False)
+    assert torch.equal(got[1], want[1])
+    again = op.grad(blank, w, y, lse, dloss)
+    assert torch.equal(again[0], want[0]) and torch.equal(again[1], want[1])
+    # one array of hidden states for all workers: where another worker counts the token, its gradient is spoiled, and only its
+    if n > 1:
+        shared = odd[:1].expand(n, -1, -1)
+        y2 = y.clone()
+        y2[1, 3] = 2
+        _, lse3 = op.loss(shared, w, y2)
+        got = op.grad(shared, w, y2, lse3, dloss)
+        base = blank[:1].expand(n, -1, -1)
+        _, lse4 = op.loss(base, w, y2)
+        want = op.grad(base, w, y2, lse4, dloss)
+        assert torch.equal(got[0][0], want[0][0]) and torch.equal(got[1][0], want[1][0])
+        assert bool(got[1][1].isnan().any()) and bool(got[0][1, 3].isnan().any())
+
+
+@pytest.mark.gpu
 def test_large_logits_and_values_that_are_not_finite():
     n, t, v, d = 1, 70, 500, 64
     h, w, y, dloss = inputs(n, t, v, d, BF, spread=60.0)
