@@ -232,6 +232,20 @@ def cser_wshard_apply(h, msg, stream=None):
     _check(lib().cser_wshard_apply(h, _ptr(msg), _stream(stream)), "cser_wshard_apply")
 
 
+_waiting = []       # (destroy, handle): dropped while a graph was captured
+
+
+def _release(destroy, h):
+    """Destroys a handle once the GPU is done with it.  That takes calls which end a capture, so while the current stream is
+    captured (by a handle's close(), or because it is collected just then) it waits for the next handle that goes."""
+    _waiting.append((destroy, h))
+    if not torch.cuda.is_current_stream_capturing():
+        torch.cuda.synchronize()
+        while _waiting:
+            d, k = _waiting.pop()
+            d(k)
+
+
 class CSER:
     """Convenience owner of one handle (still only marshalling)."""
 
@@ -242,9 +256,8 @@ class CSER:
 
     def close(self):
         if self.h is not None:
-            torch.cuda.synchronize()
-            cser_destroy(self.h)
-            self.h = None
+            h, self.h = self.h, None
+            _release(cser_destroy, h)
 
     def __del__(self):
         try:

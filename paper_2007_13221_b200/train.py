@@ -11,7 +11,7 @@ import ctypes
 
 import torch
 
-from .binding import CSERError, _check, _ptr, _stream, cser_last_error
+from .binding import CSERError, _check, _ptr, _release, _stream, cser_last_error
 from .binding import lib as _base_lib
 
 TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
@@ -119,9 +119,8 @@ class Orthogonalizer:
 
     def close(self):
         if self.h is not None:
-            torch.cuda.synchronize()
-            lib().cser_orth_destroy(self.h)
-            self.h = None
+            h, self.h = self.h, None
+            _release(lib().cser_orth_destroy, h)
 
     def __del__(self):
         try:
@@ -206,9 +205,8 @@ class LinearCrossEntropy:
 
     def close(self):
         if self.h is not None:
-            torch.cuda.synchronize()
-            lib().cser_xent_destroy(self.h)
-            self.h = None
+            h, self.h = self.h, None
+            _release(lib().cser_xent_destroy, h)
 
     def __del__(self):
         try:

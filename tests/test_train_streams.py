@@ -6,7 +6,7 @@ again while either stream may still use it.
 import pytest
 import torch
 
-from paper_2007_13221_b200 import train
+from paper_2007_13221_b200 import binding, train
 
 pytestmark = pytest.mark.gpu
 LONG = 200_000_000                                    # cycles, about a tenth of a second: what is queued behind it runs late
@@ -130,3 +130,22 @@ def test_the_current_stream_by_name():
         b = op.grad(*x, a[1], dloss, stream=side)
     torch.cuda.synchronize()
     assert torch.equal(a[0], loss) and all(torch.equal(p, q) for p, q in zip(b, grads))
+
+
+def test_a_handle_may_go_while_a_graph_is_captured():
+    """Closed or collected; it is destroyed with the next one that goes."""
+    op, g, want = orth()
+    closed, dropped = (train.Orthogonalizer([(0, 40, 70), (3000, 30, 30)], 2, 4096) for _ in range(2))
+    head, step, after = train.LinearCrossEntropy(2, 8, 30, 16), binding.CSER(1000, 2, 100, 2, 2, 2, 0.1, 0.9), train.LinearCrossEntropy(1, 8, 30, 16)
+    out = torch.zeros_like(g)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        closed.close()
+        op.apply(g, out)
+        del dropped, head
+        step.close()
+    graph.replay()
+    assert torch.equal(out, want) and closed.h is None and step.h is None and len(binding._waiting) >= 4
+    after.close()
+    assert binding._waiting == []
