@@ -1022,7 +1022,7 @@ cser_xent_handle cser_xent_create(int32_t n_workers, int64_t max_tokens, int64_t
     const long long rows = (long long)n_workers * max_tokens;
     h->tp = (int)up(max_tokens, 256), h->acc_cols = (int)up(dim, 128), h->parts = (int)(4 * (up(vocab, 256) / 256));
     const long long fit = (long long)(kPieceBytes / ((size_t)h->n * h->tp * 2)) / 256 * 256;
-    h->piece = piece ? up(piece, 256) : fit < 2048 ? 2048 : fit;
+    h->piece = piece ? up(piece < vocab ? piece : vocab, 256) : fit < 2048 ? 2048 : fit;
     if (h->piece > up(vocab, 256)) h->piece = up(vocab, 256);
     long long acc_rows = 0;                        // the most that any number of tokens asks for
     for (long long t = 128; t < max_tokens + 128; t += 128) {

@@ -131,6 +131,16 @@ def test_pieces_of_the_vocabulary(piece, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("piece", [1700, 1701, 2 ** 40, 2 ** 63 - 1])
+def test_pieces_longer_than_the_vocabulary(piece):
+    n, t, v, d = 2, 200, 1700, 136
+    h, w, y, dloss = inputs(n, t, v, d, BF)
+    got = check(train.LinearCrossEntropy(n, t, v, d, BF, piece=piece), h, w, y, dloss, BF)
+    want = check(train.LinearCrossEntropy(n, t, v, d, BF), h, w, y, dloss, BF)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [BF, HF], ids=str)
 @pytest.mark.parametrize("size", [  # n, tokens, vocab, dim, piece: the last piece has 1, 2, 3, 4 stages of 64 or one more than shares
     (1, 10, 2049, 64, 2048), (1, 10, 2100, 64, 2048), (1, 10, 2048 + 65, 72, 2048), (2, 40, 4096 + 129, 64, 2048), (1, 10, 2048 + 256, 64, 2048),
