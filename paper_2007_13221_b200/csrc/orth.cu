@@ -1088,6 +1088,7 @@ cser_orth_handle cser_orth_create(int32_t n_workers, int64_t ld, int32_t n_matri
     if (steps < 1 || steps > 16) return bad("steps must be in 1..16");
     if (in_type < 0 || in_type > 2 || out_type < 0 || out_type > 2) return bad("unknown element type");
     if ((long long)n_workers * n_matrices > (1 << 20)) return bad("more than 2^20 matrices");
+    if (ld > (1ll << 46) / n_workers) return bad("n_workers * ld must be at most 2^46");   // and no sum below overflows
     std::vector<HostMat> all, small;
     cser_orth *h = nullptr;
     try {

@@ -302,3 +302,10 @@ def test_formula_of_the_exact_form():
     for _ in range(5):
         s = 3.4445 * s - 4.7750 * s ** 3 + 2.0315 * s ** 5
     assert torch.allclose(exact(x), u @ torch.diag(s) @ v, rtol=1e-10, atol=1e-10)
+
+
+def test_sizes_whose_sums_would_overflow_are_refused():
+    for bad in (dict(matrices=[(0, 3, 1)], ld=2 ** 62, row_strides=[2 ** 62]), dict(ld=2 ** 62, n_workers=4), dict(ld=2 ** 44, n_workers=5),
+                dict(matrices=[(2 ** 46 - 1, 4, 5)], ld=2 ** 46), dict(matrices=[(2 ** 63 - 1, 4, 5)])):
+        with pytest.raises(CSERError, match="2\\^46|reaches outside"):
+            train.Orthogonalizer(**{**dict(matrices=[(0, 4, 5)], n_workers=1, ld=20), **bad})
