@@ -50,7 +50,7 @@ typedef struct cser_orth *cser_orth_handle;
 /*
  * n_workers * ld at most 2^46.  offset[k], rows[k], cols[k]: where matrix k begins in a worker's vector and its shape (row-major),
  * 1 <= rows, cols <= 65536.  row_stride[k] >= cols[k]: elements from one row to the next (NULL: cols[k]).  scale[k]: finite factor of the
- * result (NULL: 1).  Matrices must lie inside the vector and not overlap.  steps: 1..16.  The arrays are host memory
+ * result (NULL: 1).  Matrices must lie inside the vector and share no element.  steps: 1..16.  The arrays are host memory
  * and are copied.  The plan owns a workspace of about 8 bytes per element (16 for a 32-bit result) for all matrices of all workers or 2 GB,
  * whichever is less (more only where one matrix needs more), and at most 20 MB for sums that CTAs share.  Returns NULL on failure.
  */

@@ -33,6 +33,7 @@
 #include <math.h>
 #include <stdint.h>
 #include <stdio.h>
+#include <algorithm>
 #include <new>
 #include <vector>
 
@@ -796,6 +797,11 @@ struct cser_orth {
 
 namespace {
 
+struct HostMat {
+    long long offset, rows, cols, stride;
+    float scale;
+};
+
 int type_size(int t) { return t == CSER_TYPE_F32 ? 4 : 2; }
 long long up(long long v, long long to) { return (v + to - 1) / to * to; }
 
@@ -841,16 +847,38 @@ cudaError_t products_setup(int &pairs) {
     return e;
 }
 
+// Whether two matrices of one worker's vector share an element.  Those whose spans meet (columns of one array) row by row.
+bool any_overlap(std::vector<HostMat> ms) {
+    auto span_end = [](const HostMat &m) { return m.offset + (m.rows - 1) * m.stride + m.cols; };
+    std::sort(ms.begin(), ms.end(), [](const HostMat &x, const HostMat &y) { return x.offset < y.offset; });
+    std::vector<std::pair<long long, long long>> run;
+    for (size_t k = 0; k < ms.size();) {
+        long long end = span_end(ms[k]);
+        size_t to = k + 1;
+        for (; to < ms.size() && ms[to].offset < end; ++to) end = std::max(end, span_end(ms[to]));
+        if (to > k + 1) {
+            run.clear();
+            for (; k < to; ++k) {
+                const bool dense = ms[k].stride == ms[k].cols;
+                for (long long r = 0; r < (dense ? 1 : ms[k].rows); ++r) {
+                    const long long at = ms[k].offset + r * ms[k].stride;
+                    run.emplace_back(at, dense ? span_end(ms[k]) : at + ms[k].cols);
+                }
+            }
+            std::sort(run.begin(), run.end());
+            for (size_t e = 1; e < run.size(); ++e)
+                if (run[e].first < run[e - 1].second) return true;
+        }
+        k = to;
+    }
+    return false;
+}
+
 int orth_fail(cser_orth *h, int code, const char *what) {
     cser_internal_fail(code, "cser_orth_create: %s", what);
     cser_orth_destroy(h);
     return code;
 }
-
-struct HostMat {
-    long long offset, rows, cols, stride;
-    float scale;
-};
 
 // Padded dimensions and workspace of one matrix.
 void shape_of(const HostMat &m, int cg, OrthMat &M) {
@@ -1089,7 +1117,7 @@ cser_orth_handle cser_orth_create(int32_t n_workers, int64_t ld, int32_t n_matri
     if (in_type < 0 || in_type > 2 || out_type < 0 || out_type > 2) return bad("unknown element type");
     if ((long long)n_workers * n_matrices > (1 << 20)) return bad("more than 2^20 matrices");
     if (ld > (1ll << 46) / n_workers) return bad("n_workers * ld must be at most 2^46");   // and no sum below overflows
-    std::vector<HostMat> all, small;
+    std::vector<HostMat> one, all, small;          // of one worker; of all of them
     cser_orth *h = nullptr;
     try {
         for (int k = 0; k < n_matrices; ++k) {
@@ -1099,11 +1127,14 @@ cser_orth_handle cser_orth_create(int32_t n_workers, int64_t ld, int32_t n_matri
             if (offset[k] < 0 || offset[k] > ld || offset[k] + (rows[k] - 1) * st + cols[k] > ld)
                 return bad("a matrix reaches outside the vector");
             if (scale && !isfinite(scale[k])) return bad("scale must be finite");
+            one.push_back({offset[k], rows[k], cols[k], st, scale ? scale[k] : 1.f});
         }
+        if (any_overlap(one)) return bad("two matrices overlap");
         for (int w = 0; w < n_workers; ++w)
-            for (int k = 0; k < n_matrices; ++k)
-                (rows[k] <= kSmallSide || cols[k] <= kSmallSide ? small : all).push_back({(long long)w * ld + offset[k], rows[k], cols[k], row_stride ? row_stride[k] : cols[k],
-                               scale ? scale[k] : 1.f});
+            for (HostMat m : one) {
+                m.offset += (long long)w * ld;
+                (m.rows <= kSmallSide || m.cols <= kSmallSide ? small : all).push_back(m);
+            }
         h = new cser_orth;
         h->in_type = in_type, h->out_type = out_type, h->split = out_type == CSER_TYPE_F32;
         if (cudaGetDevice(&h->device) != cudaSuccess) {

@@ -309,3 +309,21 @@ def test_sizes_whose_sums_would_overflow_are_refused():
                 dict(matrices=[(2 ** 46 - 1, 4, 5)], ld=2 ** 46), dict(matrices=[(2 ** 63 - 1, 4, 5)])):
         with pytest.raises(CSERError, match="2\\^46|reaches outside"):
             train.Orthogonalizer(**{**dict(matrices=[(0, 4, 5)], n_workers=1, ld=20), **bad})
+
+
+def test_matrices_that_share_an_element_are_refused():
+    for ms, strides in (([(0, 4, 5), (19, 1, 1)], None), ([(0, 4, 5), (0, 4, 5)], None), ([(10, 2, 5), (0, 2, 6)], None),
+                        ([(0, 3, 2), (3, 3, 2)], [4, 4]), ([(0, 3, 2), (2, 3, 2), (9, 1, 1)], [4, 4, 1]), ([(0, 100, 1), (99, 1, 1)], [1, 1]),
+                        ([(0, 5, 2), (2, 3, 2)], [4, 5])):
+        with pytest.raises(CSERError, match="two matrices overlap"):
+            train.Orthogonalizer(ms, 2, 100, row_strides=strides)
+
+
+@pytest.mark.gpu
+def test_columns_of_one_array_are_matrices_of_their_own():
+    """Interleaved rows, which share no element."""
+    gen = generator(21)
+    u = torch.stack([matrix(gen, 90, 100 + 70) for _ in range(2)])
+    got = train.Orthogonalizer([(0, 90, 100), (100, 90, 70)], 2, 90 * 170, row_strides=[170, 170]).apply(u.reshape(2, -1)).view(2, 90, 170)
+    for i in range(2):
+        assert far(got[i, :, :100], exact(u[i, :, :100])) < OUT[F32] and far(got[i, :, 100:], exact(u[i, :, 100:])) < OUT[F32]
