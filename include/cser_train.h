@@ -59,7 +59,8 @@ cser_orth_handle cser_orth_create(int32_t n_workers, int64_t ld, int32_t n_matri
                                   const float *scale, int32_t steps, int32_t in_type, int32_t out_type);
 /*
  * grad: [n_workers, ld] of in_type.  m: fp32 [n_workers, ld], updated in place, or NULL (then mu is ignored).  0 <= mu < 1.
- * out: [n_workers, ld] of out_type; may be grad itself where the types are the same.
+ * out: [n_workers, ld] of out_type; may be grad itself where the types are the same.  Otherwise the three arrays must not overlap from the
+ * first matrix's beginning to the last one's end.
  */
 int cser_orth_apply(cser_orth_handle h, const void *grad, float *m, float mu, void *out, void *stream);
 void cser_orth_destroy(cser_orth_handle h);

@@ -778,6 +778,7 @@ struct cser_orth {
         void *tables = nullptr;                    // one allocation for the lists and matrices
     };
     int device = 0, in_type = 0, out_type = 0;
+    long long first = 0, last = 0;                 // elements of the [n, ld] arrays that the matrices begin and end at
     bool split = false;
     std::vector<Group> groups;
     struct Small {                                 // matrices with a short side of at most kSmallSide
@@ -1137,6 +1138,11 @@ cser_orth_handle cser_orth_create(int32_t n_workers, int64_t ld, int32_t n_matri
             }
         h = new cser_orth;
         h->in_type = in_type, h->out_type = out_type, h->split = out_type == CSER_TYPE_F32;
+        h->first = ld;
+        for (const HostMat &m : one) {
+            h->first = std::min(h->first, m.offset);
+            h->last = std::max(h->last, (n_workers - 1) * (long long)ld + m.offset + (m.rows - 1) * m.stride + m.cols);
+        }
         if (cudaGetDevice(&h->device) != cudaSuccess) {
             orth_fail(h, CSER_ERR_CUDA, "no CUDA device");
             return nullptr;
@@ -1233,7 +1239,15 @@ int cser_orth_apply(cser_orth_handle h, const void *grad, float *m, float mu, vo
         return cser_internal_fail(CSER_ERR_INVALID, "cser_orth_apply: a pointer is not aligned to its element type");
     if (grad == out && h->in_type != h->out_type)
         return cser_internal_fail(CSER_ERR_INVALID, "cser_orth_apply: out may be grad only where the types are the same");
-    if (m && (static_cast<const void *>(m) == grad || static_cast<const void *>(m) == out))
+    // From the first matrix's beginning to the last one's end.
+    auto apart = [&](const void *x, int size_x, const void *y, int size_y) {
+        const uintptr_t p = (uintptr_t)x, q = (uintptr_t)y;
+        return p + h->last * size_x <= q + h->first * size_y || q + h->last * size_y <= p + h->first * size_x;
+    };
+    const int size_in = type_size(h->in_type), size_out = type_size(h->out_type);
+    if (grad != out && !apart(grad, size_in, out, size_out))
+        return cser_internal_fail(CSER_ERR_INVALID, "cser_orth_apply: out must be grad itself or apart from it");
+    if (m && (!apart(m, 4, grad, size_in) || !apart(m, 4, out, size_out)))
         return cser_internal_fail(CSER_ERR_INVALID, "cser_orth_apply: m must be an array of its own");
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const bool both = !h->groups.empty() && (h->resident.tables || h->small.tables);

@@ -285,6 +285,35 @@ def test_a_wait_that_runs_out_ends_the_kernel_and_is_reported(shapes, out_t):
     assert L.cser_orth_debug_stall_next(small.h, 20) == -1 and L.cser_orth_debug_stall_next(None, 20) == -1
 
 
+@pytest.mark.gpu
+def test_arrays_that_overlap_are_refused():
+    """From the first matrix's beginning to the last one's end; what lies outside may."""
+    n, ld = 2, 400
+    o, wide = (train.Orthogonalizer([(40, 10, 12), (200, 8, 9)], n, ld, F32, t) for t in (F32, BF))
+    buf = torch.randn(8 * n * ld, generator=generator(1), device="cuda")
+
+    def at(k, t=F32):
+        return buf.view(t)[k * 4 // (4 if t == F32 else 2):][:n * ld].view(n, ld)
+
+    grad, size = at(2000), (n - 1) * ld + 200 + 72 - 40             # touched elements
+    want = o.apply(grad.clone(), momentum=torch.ones_like(grad), mu=0.5)
+    for k in (2000 - size, 2000 + size):                             # just apart
+        keep = buf.clone()
+        assert torch.equal(o.apply(grad, at(k), momentum=torch.ones_like(grad), mu=0.5)[:, 40:160], want[:, 40:160])
+        buf.copy_(keep)
+    for k in (2000 - size + 1, 1999, 2001, 2000 + size - 1):
+        with pytest.raises(CSERError, match="apart"):
+            o.apply(grad, at(k))
+        with pytest.raises(CSERError, match="its own"):
+            o.apply(grad, momentum=at(k))
+        with pytest.raises(CSERError, match="its own"):
+            o.apply(grad, at(4800), momentum=at(4800 + k - 2000))
+    with pytest.raises(CSERError, match="apart"):
+        wide.apply(grad, at(2100, BF))
+    with pytest.raises(CSERError):
+        wide.apply(grad, at(2000, BF))
+
+
 def test_refusals_need_no_gpu():
     """Arguments are checked before the first CUDA call."""
     for bad in (dict(n_workers=0), dict(ld=0), dict(matrices=[(0, 4, 6)]), dict(matrices=[(0, 4, 0)]), dict(steps=0)):
