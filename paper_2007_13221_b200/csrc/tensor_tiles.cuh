@@ -366,7 +366,8 @@ struct Pipe {
     //   bool chunk_ends(tile, k)   after this stage the epilogue takes the accumulator (always after the last)
     //   kWaits; bool ready(pipe, tile)   whether tiles read what this launch writes; then waits until that is in memory (before any role
     //                              hears of the tile).  If not, the launch may overlap the end of the kernel before it: tiles are worked
-    //                              out from the kernel's arguments alone, copies and epilogue begin with earlier_done()
+    //                              out from the kernel's arguments alone, and every role calls earlier_done() before its first wait for
+    //                              another role's work: however long the kernel before it takes, that is no wait of this one
     //   Loader                     made from a tile; uint32_t bytes(); settle(job, tile), unless kWaits: what it reads that earlier kernels
     //                              wrote; void load(k, a, b, bar): copies of bytes() bytes into a and b (shared addresses; the lo halves
     //                              of pairs kLoOffset behind)
@@ -424,6 +425,7 @@ struct Pipe {
             uint32_t ph = 0;
             Turn turn;
             const uint32_t tmem = sh->tmem;
+            if (!Job::kWaits) earlier_done();
             while (ok) {
                 ok = wait(&sh->tile_full[walk.slot], walk.ph);
                 if (!ok || tile_at<Tile>(walk)->n == 0) break;
@@ -494,6 +496,7 @@ struct Pipe {
             // The pair's second CTA passes "this stage has landed" on to the first one's barrier.
             int s = 0;
             uint32_t ph = 0;
+            if (!Job::kWaits) earlier_done();
             while (ok) {
                 ok = wait(&sh->tile_full[walk.slot], walk.ph);
                 const Tile &t = *tile_at<Tile>(walk);
@@ -511,6 +514,7 @@ struct Pipe {
             Tile t;
             for (int i = lane; ok; i += kTiles) {
                 job.tile(t, i, (int)rank);
+                if (!Job::kWaits && i == lane + kTiles) earlier_done();
                 ok = wait(&sh->tile_empty[lane], (uint32_t)(i / kTiles & 1) ^ 1);
                 // One at a time looks at memory: the lane of the tile before has done with it.
                 if (ok && i) ok = wait(&sh->tile_full[(i - 1) % kTiles], (uint32_t)((i - 1) / kTiles & 1));

@@ -489,6 +489,29 @@ def test_calls_are_repeatable_on_any_stream_and_in_a_graph():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("size", [(1, 40, 50000, 64), (2, 300, 30000, 72)], ids=str)
+def test_a_long_kernel_ahead_that_lets_the_next_one_be_set_up(size):
+    """The time that the kernel ahead takes, about 1.6 s here, is no wait that could run out (those may take about one)."""
+    import ctypes
+    import __graft_entry__
+    ahead = ctypes.CDLL(f"{__graft_entry__.ROOT}/tests/libearly_trigger.so")
+    ahead.early_trigger.argtypes = [ctypes.c_longlong, ctypes.c_void_p]
+    n, t, v, d = size
+    h, w, y, dloss = inputs(n, t, v, d, BF)
+    op = train.LinearCrossEntropy(n, t, v, d, BF)
+    loss, lse = op.loss(h, w, y)
+    want = op.grad(h, w, y, lse, dloss)
+    stream = torch.cuda.current_stream().cuda_stream
+    assert ahead.early_trigger(3_000_000_000, stream) == 0
+    got = op.loss(h, w, y)
+    assert ahead.early_trigger(3_000_000_000, stream) == 0
+    got += op.grad(h, w, y, lse, dloss)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, (loss, lse, *want)))
+    op.loss(h, w, y)                                  # and nothing was reported
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("size", [(1, 600, 40000, 256), (8, 130, 3001, 128)], ids=str)
 def test_many_tiles(size):
     n, t, v, d = size
