@@ -828,10 +828,11 @@ long long up(long long v, long long to) { return (v + to - 1) / to * to; }
 int splits_of(const cser_xent *h, long long tokens) {
     // Few tiles of dh and a long inner dimension: the vocabulary is split so that every SM has a share, each of 8 stages at least;
     // fewer than 24 are left whole: joining takes 3 us, as much as 8 stages (2 x 5 tokens x 3000 x 2000, gradients: 40 us by 16, 35 by 8;
-    // 3 x 77 x 1003 x 201, 16 stages: 27 whole, 30 in two).
+    // 3 x 77 x 1003 x 201, 16 stages: 27 whole, 30 in two; 50 x 100 x 1200 x 256, 19 stages: 34 and 50; 8 x 100 x 1200 x 2048: 40 and 60).
     const long long tiles = h->n * (up(tokens, 128) / 128) * (up(h->dim, 256) / 256), stages = up(h->piece < h->vocab ? h->piece : h->vocab, 64) / 64;
     long long s = tiles >= h->sms ? 1 : h->sms / tiles;
-    if (s > stages / 8) s = stages < 24 ? 1 : stages / 8;
+    if (stages < 24) s = 1;
+    else if (s > stages / 8) s = stages / 8;
     return s < 1 ? 1 : (int)s;
 }
 

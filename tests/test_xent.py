@@ -489,6 +489,19 @@ def test_calls_are_repeatable_on_any_stream_and_in_a_graph():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("size", [(60, 20, 1100, 200), (8, 100, 1200, 2048), (1, 100, 1535, 16384), (1, 5, 1500, 64), (2, 5, 1000, 520)], ids=str)
+def test_inner_dimensions_of_fewer_than_24_stages_are_left_whole(size):
+    """However many SMs that leaves idle: the gradients are two kernels, with none that joins shares.  (1535 entries are 24.)"""
+    n, t, v, d = size
+    h, w, y, dloss = inputs(n, t, v, d, BF)
+    op = train.LinearCrossEntropy(n, t, v, d, BF)
+    _, lse, _, _ = check(op, h, w, y, dloss, BF)
+    before = op.launches
+    op.grad(h, w, y, lse, dloss)
+    assert op.launches - before == (2 if (v + 63) // 64 < 24 else 3)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("size", [(1, 40, 50000, 64), (2, 300, 30000, 72)], ids=str)
 def test_a_long_kernel_ahead_that_lets_the_next_one_be_set_up(size):
     """The time that the kernel ahead takes, about 1.6 s here, is no wait that could run out (those may take about one)."""
