@@ -74,6 +74,19 @@ def test_other_spectra(kind, out):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("out", [BF, HF], ids=str)
+@pytest.mark.parametrize("kind", ["mixed", "noise", "low rank"])
+@pytest.mark.parametrize("shape", [(384, 512), (1000, 300), (1024, 1024), (2048, 512)], ids=str)
+def test_products_of_16_bit_results_leave_a_thousandth(shape, kind, out):
+    """1e-3 before the rounding of the result, whose 2-norm is 2^-p / sqrt(7) of the result's for p bits (half an ulp, uniform, of values
+    spread evenly over a binade), the two independent; a tenth for how values really lie in their binades."""
+    u = matrix(generator(sum(shape)), *shape, kind)
+    got = train.Orthogonalizer([(0, *shape)], 1, u.numel(), F32, out).apply(u.reshape(1, -1)).view(shape)
+    rounding = 2.0 ** (-8 if out == BF else -11) / 7 ** 0.5
+    assert far(got, exact(u)) < 1.1 * (1e-6 + rounding ** 2) ** 0.5
+
+
+@pytest.mark.gpu
 def test_singular_values_come_near_one():
     u = matrix(generator(1), 192, 384, "noise")
     got = train.Orthogonalizer([(0, 192, 384)], 1, u.numel(), F32, F32).apply(u.reshape(1, -1)).view(192, 384)

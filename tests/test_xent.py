@@ -185,6 +185,24 @@ def test_a_mean_over_the_tokens_is_not_rounded_twice():
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [BF, HF], ids=str)
+@pytest.mark.parametrize("size", [(1, 150, 600, 128), (2, 300, 700, 264), (1, 4096, 1000, 64)], ids=str)
+def test_a_uniform_dloss_adds_no_rounding(size, dtype):
+    """dz is that of dloss = 1 whatever dloss is: three times the result for 1/3 differs from the result for 1 by the roundings of
+    these two results, u each, alone.  Were p / 3 rounded itself, entries whose terms cancel would be off by u of the terms."""
+    n, t, v, d = size
+    h, w, y, _ = inputs(n, t, v, d, dtype)
+    op = train.LinearCrossEntropy(n, t, v, d, dtype)
+    _, lse = op.loss(h, w, y)
+    ones = torch.ones((n, t), device="cuda")
+    third, whole = op.grad(h, w, y, lse, ones / 3), op.grad(h, w, y, lse, ones)
+    u, tiny = (2.0 ** -8, 0.0) if dtype == BF else (2.0 ** -11, 2.0 ** -25)
+    for a, b in zip(third, whole):
+        a, b = a.double(), b.double()
+        assert bool(((3 * a - b).abs() <= 2.02 * u * b.abs() + 4 * tiny).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, HF], ids=str)
 def test_ignored_tokens_other_indices_and_targets_out_of_range(dtype):
     n, t, v, d = 2, 90, 400, 64
     h, w, y, dloss = inputs(n, t, v, d, dtype, ignored=0.0)
