@@ -762,14 +762,6 @@ __global__ void __launch_bounds__(kThreads, 1) orth_products_kernel(const __grid
 }  // namespace
 
 // ------------------------------------------------------------------ host
-#define TRY(expr)                                                                                              \
-    do {                                                                                                       \
-        cudaError_t _e = (expr);                                                                               \
-        if (_e != cudaSuccess)                                                                                 \
-            return cser_internal_fail(_e == cudaErrorMemoryAllocation ? CSER_ERR_NOMEM : CSER_ERR_CUDA, "%s: %s", #expr, \
-                                      cudaGetErrorString(_e));                                                 \
-    } while (0)
-
 struct cser_orth {
     struct Group {
         int mode = kSingle, grid = 0, n_chunk = 0, n_unit = 0;
@@ -804,7 +796,6 @@ struct HostMat {
 };
 
 int type_size(int t) { return t == CSER_TYPE_F32 ? 4 : 2; }
-long long up(long long v, long long to) { return (v + to - 1) / to * to; }
 
 template <int MODE, bool SPLIT>
 cudaError_t products_launch(const OrthArgs &a, bool shares, int grid, cudaStream_t st) {

@@ -23,7 +23,7 @@
 struct SmallMat {
     long long offset, stride;
     int s, l, sp, tall;                            // sp: s rounded up to 8
-    int part0, parts, per;                         // parts of the long side, columns of each
+    int parts, per;                                // of the long side, columns of each
     size_t partial, q;                             // places in the 64-bit workspace: [parts][tiles][64], [sp][sp]
     float scale;
 };

@@ -792,14 +792,6 @@ __global__ void __launch_bounds__(256) xent_pack_kernel(const PackSource x, cons
 }  // namespace
 
 // ------------------------------------------------------------------ host
-#define TRY(expr)                                                                                              \
-    do {                                                                                                       \
-        cudaError_t _e = (expr);                                                                               \
-        if (_e != cudaSuccess)                                                                                 \
-            return cser_internal_fail(_e == cudaErrorMemoryAllocation ? CSER_ERR_NOMEM : CSER_ERR_CUDA, "%s: %s", #expr, \
-                                      cudaGetErrorString(_e));                                                 \
-    } while (0)
-
 typedef CUresult (*encode_fn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
                               const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
                               CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -824,7 +816,6 @@ struct cser_xent {
 
 namespace {
 
-long long up(long long v, long long to) { return (v + to - 1) / to * to; }
 int splits_of(const cser_xent *h, long long tokens) {
     // Few tiles of dh and a long inner dimension: the vocabulary is split so that every SM has a share, each of 8 stages at least;
     // fewer than 24 are left whole: joining takes 3 us, as much as 8 stages (2 x 5 tokens x 3000 x 2000, gradients: 40 us by 16, 35 by 8;

@@ -11,7 +11,7 @@ import ctypes
 
 import torch
 
-from .binding import CSERError, _check, _ptr, _release, _stream, cser_last_error
+from .binding import CSERError, _check, _release, _stream, cser_last_error
 from .binding import lib as _base_lib
 
 TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
