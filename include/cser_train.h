@@ -7,9 +7,13 @@
  * the GPU that was current when the handle was created; `stream` is a cudaStream_t as void* (NULL = legacy default
  * stream); a call only enqueues work and returns; calls on one handle must not overlap, on the host or on the GPU (a
  * handle's workspace serves one call at a time).  Calls may be captured in a CUDA
- * graph and replayed (but see cser_xent_create for unaligned inputs).  No call aborts, throws or traps on the device.  Every wait inside a kernel is bounded to about a
- * second; one that ran out (the GPU withheld from part of a launch, say) ends the kernel and every later call on the
- * handle returns CSER_ERR_CUDA, the results of that call being incomplete.
+ * graph and replayed (but see cser_xent_create for unaligned inputs).  No call aborts, throws or traps on the device.  Every wait inside a
+ * kernel is bounded to about a second; one that ran out (the GPU withheld from part of a launch, say) ends the kernel and every
+ * later call on the handle returns CSER_ERR_CUDA, the results of that call being incomplete.
+ *
+ * A handle is made once for many calls: creation allocates, copies its tables and asks the driver about kernels, and destruction waits for
+ * the GPU.  On a B200 0.4 to 1 ms for the cross entropy and 0.8 to 2.8 ms for a plan, up to 17 ms for a process's first (its kernels
+ * are loaded), 0.3 to 3.3 ms to destroy: more than many a call takes.
  */
 #ifndef CSER_TRAIN_H_
 #define CSER_TRAIN_H_
@@ -40,7 +44,8 @@ extern "C" {
  * Momenta and outputs outside the listed matrices are neither read nor written.
  *
  * Arithmetic.  in_type F32, BF16 or F16; momentum fp32.  Matrices with a short side of at most 64 go through their Gram
- * matrix in 64 bits.  Others: norms and sums fp32; out_type BF16 or F16: the products take
+ * matrix in 64 bits.  Others: norms and sums fp32, so |u|_F below 2^64 (from there on the result is 0), and X in fp16's range: a matrix with |u|_F
+ * below about 1e-15 sqrt(rows cols), of which 1e-7 leaves next to nothing, keeps fewer bits in a 16-bit result; out_type BF16 or F16: the products take
  * fp16 operands (11 bits), with the remainder of X and the diagonals of A and b A + c A A carried in addition, which
  * leaves about 1e-3 relative error at most before the rounding of the result.  out_type F32: the operands are pairs of
  * fp16 (22 bits) and each product is three, about 1e-6.  Results are the same from call to call, bit for bit.
@@ -52,7 +57,9 @@ typedef struct cser_orth *cser_orth_handle;
  * 1 <= rows, cols <= 65536.  row_stride[k] >= cols[k]: elements from one row to the next (NULL: cols[k]).  scale[k]: finite factor of the
  * result (NULL: 1).  Matrices must lie inside the vector and share no element.  steps: 1..16.  The arrays are host memory
  * and are copied.  The plan owns a workspace of about 8 bytes per element (16 for a 32-bit result) for all matrices of all workers or 2 GB,
- * whichever is less (more only where one matrix needs more), and at most 20 MB for sums that CTAs share.  Returns NULL on failure.
+ * whichever is less (more only where one matrix needs more), and at most 20 MB for sums that CTAs share.  Matrices that do not fit
+ * these 2 GB together go through it in groups, of three kernels each; those with a short side of at most 64 take up to three more.  Returns
+ * NULL on failure.
  */
 cser_orth_handle cser_orth_create(int32_t n_workers, int64_t ld, int32_t n_matrices, const int64_t *offset,
                                   const int64_t *rows, const int64_t *cols, const int64_t *row_stride,
@@ -81,14 +88,14 @@ int64_t cser_orth_launch_count(cser_orth_handle h);
  * and for the upstream gradients dloss[i,t]:
  *     dz_v = (exp(z_v - lse) - [v = target]) * dloss ,   dhidden = sum_v dz_v weight[v] ,   dweight[v] = sum_t dz_v hidden[t]
  * A token whose target is ignore_index has loss 0 and adds nothing to the gradients, even where its hidden state is not finite; nor does
- * one whose dloss is 0.  A target outside 0..vocab-1 that
- * is not ignore_index makes that token's loss NaN, its row of dhidden NaN and its worker's dweight NaN; so does, for the gradients, a
- * dloss that is not finite of a token that counts.
+ * one whose dloss is 0.  A target outside 0..vocab-1 that is not ignore_index makes that token's loss NaN, its row of dhidden NaN and its
+ * worker's dweight NaN; so does, for the gradients, a dloss that is not finite of a token that counts.
  *
  * Arithmetic.  hidden, weight, dhidden and dweight are of one type, BF16 or F16.  Logits, sums, lse and loss are fp32.  dz is
- * held in the operands' type between the products, relative to the worker's largest finite |dloss|, so a uniform dloss (the mean
+ * held in the operands' type between the products (up to 32 tokens with what that rounding leaves), relative to the worker's largest finite |dloss|, so a uniform dloss (the mean
  * over the tokens) adds no rounding; F16: where the |dloss| of a worker's tokens are more than 2^6 apart, a second time relative to each
- * token's own for dhidden, so that its rows are as exact whatever their weight.  Sums over pieces are fp32, in a fixed order: results are the same from call to call.
+ * token's own for dhidden, so that its rows are as exact whatever their weight.  Sums over pieces are fp32, in
+ * a fixed order: results are the same from call to call.
  */
 typedef struct cser_xent *cser_xent_handle;
 
@@ -105,11 +112,14 @@ typedef struct cser_xent_inputs {
 } cser_xent_inputs;
 
 /*
- * Workspace for up to max_tokens tokens per worker.  piece: vocabulary entries per piece of the gradient (rounded up to
- * a multiple of 256), 0 = chosen so that a piece of dz takes at most 256 MB (twice that for F16).  1 <= vocab <= 2^24, 1 <= dim <= 65536,
+ * Handle for up to max_tokens tokens per worker.  piece: vocabulary entries per piece of the gradient (rounded up to a multiple of
+ * 256), 0 = as many as 256 MB of dz hold, but 2048 at least.  The workspace, all of it allocated here, with T = max_tokens rounded up to
+ * 256: dz, n_workers * T * piece * 2 bytes (twice for F16); parts of the losses, n_workers * max_tokens * vocab / 8; a copy of the
+ * hidden states; and, where the vocabulary is gone through in several pieces or dhidden has few tiles, its fp32 sums.  1 <= vocab <= 2^24, 1 <= dim <= 65536,
  * 1 <= n_workers * max_tokens <= 2^24, n_workers * vocab and n_workers * ceil(max_tokens / 128) * ceil(vocab / 256) at most 2^30.
  * hidden or weights whose rows are not a multiple of 16 bytes apart (or not 16-byte aligned) are first copied: the buffer for that is
- * allocated with the handle where dim is no multiple of 8, else on the first such call, which must not be under stream capture.  Returns NULL on failure.
+ * allocated with the handle where dim is no multiple of 8, else on the first such call, which must not be under stream capture.  Returns
+ * NULL on failure.
  */
 cser_xent_handle cser_xent_create(int32_t n_workers, int64_t max_tokens, int64_t vocab, int64_t dim, int32_t type,
                                   int64_t piece);
@@ -118,7 +128,8 @@ int cser_xent_loss(cser_xent_handle h, const cser_xent_inputs *in, float *loss, 
 /*
  * lse: as cser_xent_loss gave it for the same inputs.  dloss: fp32 [n_workers, tokens], dense.
  * dhidden: [n_workers, tokens, dim], dense, or NULL.  dweight: [n_workers][vocab, dim], each worker's dense, dweight_stride
- * elements (>= vocab*dim) from one worker to the next, or NULL.  With tokens = 0, dweight becomes 0.
+ * elements (>= vocab*dim) from one worker to the next, or NULL.  With tokens = 0, dweight becomes 0.  What is written must not overlap
+ * what is read.
  */
 int cser_xent_grad(cser_xent_handle h, const cser_xent_inputs *in, const float *lse, const float *dloss, void *dhidden,
                    void *dweight, int64_t dweight_stride, void *stream);

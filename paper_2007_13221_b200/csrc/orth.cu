@@ -1,5 +1,6 @@
 // Orthogonalised updates (cser_orth_* of include/cser_train.h): Newton-Schulz products on the matrices inside the flat
-// gradients of n workers, grouped: one call is three kernels, whatever the number of matrices.
+// gradients of n workers, grouped: three kernels for as many matrices as fit a workspace of 2 GB (and up to three for those with a short
+// side of at most 64, orth_small.cuh).
 //
 //   orth_norm_kernel     one pass over g (and m, which it updates): |u|_F per matrix
 //   orth_convert_kernel  X = u / (|u|_F + 1e-7) as 16-bit panels (tensor_tiles.cuh)

@@ -6,7 +6,8 @@
 // maximum and a sum of exponentials per row and quarter tile, and one that joins them.  cser_xent_grad: for each piece of
 // the vocabulary a kernel computes the tiles of z again and leaves dz in 16 bits, as panels (tensor_tiles.cuh), and
 // one kernel makes from them the piece's rows of dW (inner dimension: tokens) and the piece's share of dh (inner dimension: the piece).
-// Every operand is read where it lies: the products that need dz, h or W the other way round take the same tiles with the other majorness.
+// The products that need dz, h or W the other way round take the same tiles with the other majorness.  Operands are read where they lie, but for
+// rows that no tensor copy can start at (not 16 bytes apart, or at another address), which each call packs first.
 //
 // Bound.  6 T V D multiply-adds' flops (8 with z computed again) against 2 V D elements of W and dW moved: the tensor cores for
 // T above about 500, the read of W (and the write of dW) below.
@@ -17,8 +18,9 @@
 // fp16's range ends 2^-37 below the largest |dloss| that way, and a token of little weight would have its row of dh made from what is left of
 // it: p = 1e-5 under a weight of 2^-20 is nothing.  So where a worker's weights are more than 2^6 apart, dz is left a second time for dh, each row
 // relative to its own |dloss| (dW's rows add tokens up, and there 2^-37 of the largest is little).
-// Up to 32 tokens, where a single rounding (of p - 1 at the target) can be most of a result's error, what it left is kept too, in
-// rows that are padding otherwise: no more bytes, no more stages.
+// That rounding and the result's are all there is: 1.9e-3 of a bf16 gradient in the 2-norm, where products of unrounded dz leave the result's
+// own, 1.7e-3 (fp16 2.6e-4 and 2.1e-4).  Up to 32 tokens what it left is kept too, in rows that are padding otherwise: no more bytes, no more
+// stages, and 1.7e-3.  Above, the same would take both gradients' products twice, half as much time again.
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <cuda_bf16.h>
@@ -103,8 +105,8 @@ struct XentArgs {
 
 // ------------------------------------------------------------------ dloss, relative to the largest
 // How far apart the weights of a worker's tokens are beyond which dh's rows have factors of their own: up to there every p above 1e-6
-// keeps all of fp16's bits.  Gradients with and without, fp16: 8 x 512 x 30522 x 1024 793 us and 675, 8 x 16 394 and 371, 4096 x 32768 x 4096
-// 2.84 ms and 2.68.
+// keeps all of fp16's bits.  Gradients with and without, fp16: 8 x 512 x 30522 x 1024 750 to 860 us and 680, 8 x 16 394 and 371, 4096 x 32768 x
+// 4096 2.8 ms and 2.6.
 constexpr float kApart = 64.f;
 __device__ __forceinline__ float type_scale(const XentArgs &a) { return a.bf16 ? 1.f : 4096.f; }
 // The largest and the smallest finite |dloss| but 0 of a worker's tokens that count.  (One that is not finite spoils its own row
