@@ -59,6 +59,8 @@ def _on(stream, call, *args):
     """call(...) with `stream` as the current one.  The allocator does not give out the arguments' memory again before `stream` has
     passed this point, nor the results' before the caller's stream has passed the place where they are dropped."""
     here = torch.cuda.current_stream()
+    if not isinstance(stream, torch.cuda.Stream):    # another package's, known by its cuda_stream
+        stream = torch.cuda.ExternalStream(stream.cuda_stream)
     for t in args:
         if torch.is_tensor(t) and t.is_cuda:
             t.record_stream(stream)

@@ -118,6 +118,22 @@ def test_results_may_be_dropped_while_the_current_stream_reads_them():
     assert all(torch.equal(a, b) for a, b in zip(read, (loss, lse, *grads)))
 
 
+def test_streams_of_other_packages():
+    """Anything with a cuda_stream, as the optimizer's calls take."""
+    class Stream:
+        def __init__(self, raw):
+            self.cuda_stream = raw
+
+    op, g, want = orth()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for s in (Stream(side.cuda_stream), torch.cuda.ExternalStream(side.cuda_stream)):
+        torch.cuda._sleep(LONG)
+        got = op.apply(g, stream=s)
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
+
+
 def test_the_current_stream_by_name():
     """The stream that is current anyway, given or not."""
     op, g, want = orth()
