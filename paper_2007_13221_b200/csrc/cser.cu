@@ -1,7 +1,7 @@
 // CSER / M-CSER optimizer step for B200 (sm_100a): host side of the C ABI declared in
 // include/cser.h.  The kernels live in grbs_kernels.cuh (block selection),
 // step_kernels.cuh (streaming and selected-block kernels) and wshard_kernels.cuh
-// (worker-sharded pack / apply).
+// (worker-sharded pack / apply).  layers.cuh at the end adds the ABI of include/cser_layers.h.
 //
 // Layout: g, x, e, m are fp32 [n, d] row-major (worker-major).  The step is bound
 // by HBM traffic (about 28 bytes per element and worker against 7 flops), so the
@@ -22,8 +22,10 @@
 #include <stdarg.h>
 #include <string.h>
 #include <math.h>
+#include <algorithm>
 #include <mutex>
 #include <new>
+#include <type_traits>
 
 #include "cser.h"
 #include "train_host.h"
@@ -1454,3 +1456,5 @@ extern "C" int cser_step_noalloc(int64_t d, int32_t n_workers, int32_t block_siz
     if (rc) return rc;
     return launch_step(&c, grad, 0, d, is_reset, s);
 }
+
+#include "layers.cuh"
