@@ -25,6 +25,7 @@
 #include <algorithm>
 #include <mutex>
 #include <new>
+#include <numeric>
 #include <type_traits>
 
 #include "cser.h"

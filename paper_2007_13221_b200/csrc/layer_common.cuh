@@ -69,27 +69,55 @@ struct Draw {
     const unsigned long long *step_at = nullptr;
 };
 
-__device__ __forceinline__ unsigned long long step_of(const Draw &d) { return d.step_at ? d.step + *d.step_at : d.step; }
+// A worker's generator.  Of a call's four counter words only the first differs from call to call, so the first round's second product and
+// the second round's first are the same for all: they are made once a thread.
+struct Words {
+    uint32_t k0, k1, a, b, c, d;
 
-// Keep bits of the V elements from element e of a worker's array on, bit j for e + j.  V a multiple of 4 with e too: V / 4 draws.
-// Otherwise one draw more, and the words are shifted into place.
-template <int V, bool ALIGNED>
-__device__ __forceinline__ uint32_t keep_bits(const Draw &d, unsigned long long step, uint32_t c3, long long e) {
-    constexpr int kDraws = ALIGNED ? V / 4 : (V + 2) / 4 + 1;
-    uint32_t w[kDraws * 4];
-    const uint32_t q = (uint32_t)(e >> 2);
-#pragma unroll
-    for (int k = 0; k < kDraws; ++k) {
-        uint32_t four[4];
-        philox4x32_10(four, d.k0, d.k1, q + k, (uint32_t)step, (uint32_t)(step >> 32), c3);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) w[k * 4 + j] = four[j];
+    __device__ __forceinline__ Words(const Draw &g, int worker) : k0(g.k0), k1(g.k1) {
+        const unsigned long long step = g.step_at ? g.step + *g.step_at : g.step;
+        const uint64_t p = (uint64_t)0xCD9E8D57u * (uint32_t)(step >> 32);
+        const uint64_t q = (uint64_t)0xD2511F53u * ((uint32_t)(p >> 32) ^ (uint32_t)step ^ k0);
+        a = (g.c3 + worker) ^ k1;
+        b = (uint32_t)p ^ (k0 + 0x9E3779B9u);
+        c = (uint32_t)(q >> 32) ^ (k1 + 0xBB67AE85u);
+        d = (uint32_t)q;
     }
-    uint32_t bits = 0;
+
+    // Draws 4 * quad .. 4 * quad + 3 of the worker.
+    __device__ __forceinline__ void four(uint32_t *w, uint32_t quad) const {
+        const uint64_t p = (uint64_t)0xD2511F53u * quad;
+        const uint64_t q = (uint64_t)0xCD9E8D57u * ((uint32_t)(p >> 32) ^ a);
+        uint32_t c0 = (uint32_t)(q >> 32) ^ b, c1 = (uint32_t)q, c2 = (uint32_t)p ^ c, c3 = d;
+        philox4x32_rounds<8>(c0, c1, c2, c3, k0 + 2 * 0x9E3779B9u, k1 + 2 * 0xBB67AE85u);
+        w[0] = c0, w[1] = c1, w[2] = c2, w[3] = c3;
+    }
+};
+
+// w[j] <- w[j + by], by in 0..3.
+template <int N> __device__ __forceinline__ void shift_words(uint32_t (&w)[N], uint32_t by) {
+    if (by & 1) {
 #pragma unroll
-    for (int j = 0; j < kDraws * 4; ++j) bits |= (w[j] >= d.threshold ? 1u : 0u) << j;
-    return ALIGNED ? bits : bits >> ((uint32_t)e & 3);
+        for (int j = 0; j + 1 < N; ++j) w[j] = w[j + 1];
+    }
+    if (by & 2) {
+#pragma unroll
+        for (int j = 0; j + 2 < N; ++j) w[j] = w[j + 2];
+    }
 }
+
+// The draws of the V elements from element e of a worker's array on.  ALIGNED: e is a multiple of 4, as V is.  Otherwise a call more,
+// and the words are shifted into place.
+template <int V, bool ALIGNED> struct Drawn {
+    static constexpr int kCalls = ALIGNED ? V / 4 : (V + 2) / 4 + 1;
+    uint32_t w[kCalls * 4];
+    __device__ __forceinline__ Drawn(const Words &words, long long e) {
+        const uint32_t quad = (uint32_t)(e >> 2);
+#pragma unroll
+        for (int k = 0; k < kCalls; ++k) words.four(w + 4 * k, quad + k);
+        if (!ALIGNED) shift_words(w, (uint32_t)e & 3);
+    }
+};
 
 // ------------------------------------------------------------------ sums over rows
 // out[k][i][c] = sum over r of part[k][i][r][c], in an order of its own for each (k, i, c): 32 lanes of rows each take every 32nd, and

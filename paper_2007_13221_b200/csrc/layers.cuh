@@ -109,15 +109,39 @@ void column_blocks(long long cols, int v, int &tx, int &blocks) {
     blocks = (int)ceil_div(vectors, tx);
 }
 
-// Chunks of rows for sums: as many as keep the GPU busy, of no fewer rows than a block takes four times.
-long long row_chunks(long long rows, long long others, int tx) {
-    const long long most = ceil_div(rows, 4 * (256 / tx)), want = ceil_div(kBusy, others);
-    return most < want ? most : want;
-}
-
 int check_rows(const cser_rows *a, const cser_drop *h, int64_t rows, bool written, const char *what) {
     const Axis axes[2] = {{rows, a->row_stride}, {h->n, a->worker_stride}};
     return check_array(a->data, h->type, h->cols, axes, written, what);
+}
+
+// Rows of cols elements to a walked row: as many as make whole vectors, and as fill a block's 32 of them.
+long long rows_walked_as_one(long long cols, int v) {
+    const long long least = v / std::gcd(cols, (long long)v);
+    return least * std::max(1ll, ceil_div(32 * v, least * cols));
+}
+
+// How the rows of a call are walked.
+struct Walk {
+    long long width, rows, chunk_rows, most_chunks;    // most_chunks: of this many rows or fewer
+    int tx, col_blocks, chunks;
+};
+Walk walk_of(long long rows, long long cols, int n, int v, bool dense) {
+    Walk k;
+    const long long fold = dense ? rows_walked_as_one(cols, v) : 1;
+    k.width = fold * cols, k.rows = dense ? ceil_div(rows * cols + v - 1, k.width) : rows;
+    column_blocks(k.width, v, k.tx, k.col_blocks);
+    const long long most = ceil_div(k.rows, 4 * (256 / k.tx)), want = ceil_div(kBusy, (long long)k.col_blocks * n);
+    k.most_chunks = std::min(most, want);
+    k.chunk_rows = ceil_div(k.rows, k.most_chunks);
+    k.chunks = (int)ceil_div(k.rows, k.chunk_rows);
+    return k;
+}
+
+template <typename T, int MODE, bool SHIFTED> void drop_rows_launch(const DropArgs<T> &a, unsigned grid, bool sums, cudaStream_t st) {
+    if (sums)
+        drop_rows_kernel<T, MODE, SHIFTED, true><<<grid, 256, 0, st>>>(a);
+    else
+        drop_rows_kernel<T, MODE, SHIFTED, false><<<grid, 256, 0, st>>>(a);
 }
 
 template <typename T>
@@ -126,59 +150,49 @@ int drop_launch(cser_drop *h, int64_t rows, const Draw &draw, const cser_rows *x
     constexpr int V = 16 / sizeof(T);
     DropArgs<T> a{};
     a.rows = rows, a.cols = h->cols, a.draw = draw, a.bias = bias, a.bias_worker = bias_stride;
-    bool dense = true, vector = h->cols % V == 0, same = true;
-    const int ahead = (int)((uintptr_t)x->data % 16 / sizeof(T));
+    a.ahead = (int)((uintptr_t)x->data % 16 / sizeof(T)), a.ahead_worker = h->n == 1 ? 0 : (int)(x->worker_stride % V);
+    bool dense = true, plain = h->cols % V == 0;
     auto take = [&](const cser_rows *r) {
-        const int at = (int)((uintptr_t)r->data % 16 / sizeof(T));
-        dense = dense && (rows == 1 || r->row_stride == h->cols);
-        same = same && at == ahead && (h->n == 1 || r->worker_stride % V == 0);
-        vector = vector && at == 0 && (rows == 1 || r->row_stride % V == 0) && (h->n == 1 || r->worker_stride % V == 0);
+        const int at = (int)((uintptr_t)r->data % 16 / sizeof(T)), more = h->n == 1 ? 0 : (int)(r->worker_stride % V);
+        dense = dense && (rows == 1 || r->row_stride == h->cols) && at == a.ahead && more == a.ahead_worker;
+        plain = plain && at == 0 && more == 0 && (rows == 1 || r->row_stride % V == 0);
     };
     a.x = static_cast<const T *>(x->data), a.x_row = x->row_stride, a.x_worker = x->worker_stride;
     take(x);
     if (residual) a.r = static_cast<const T *>(residual->data), a.r_row = residual->row_stride, a.r_worker = residual->worker_stride, take(residual);
     if (y) a.y = static_cast<T *>(y->data), a.y_row = y->row_stride, a.y_worker = y->worker_stride, take(y);
-    if (!dbias && dense && same && !(bias && vector)) {
-        a.ahead = ahead;
-        const long long blocks = ceil_div(rows * h->cols + ahead, 256 * V);
-        if (blocks > kMostBlocks) return fail(CSER_ERR_INVALID, "dropout: too many elements");
+    const bool shifted = a.ahead || a.ahead_worker;
+    h->launches++;
+    if (dense && !bias && !dbias) {
+        const long long blocks = ceil_div(rows * h->cols + V - 1, 256 * V * kFlat);
         const dim3 grid((unsigned)blocks, (unsigned)h->n);
-        if (ahead)
+        if (shifted)
             drop_flat_kernel<T, true><<<grid, 256, 0, st>>>(a);
         else
             drop_flat_kernel<T, false><<<grid, 256, 0, st>>>(a);
-        h->launches++;
         TRY(cudaGetLastError());
         return CSER_OK;
     }
-    column_blocks(h->cols, V, a.tx, a.col_blocks);
-    const long long others = (long long)a.col_blocks * h->n;
-    a.chunks = (int)row_chunks(rows, others, a.tx);
-    a.chunk_rows = ceil_div(rows, a.chunks);
-    a.chunks = (int)ceil_div(rows, a.chunk_rows);
-    if (others * a.chunks > kMostBlocks) return fail(CSER_ERR_INVALID, "dropout: too many elements");
-    const unsigned grid = (unsigned)(others * a.chunks);
-    if (dbias) {
-        const bool one = a.chunks == 1;
-        a.part = one ? dbias : h->part, a.part_worker = one ? dbias_stride : a.chunks * h->cols;
-        if (vector)
-            drop_rows_kernel<T, true, true><<<grid, 256, 0, st>>>(a);
-        else
-            drop_rows_kernel<T, false, true><<<grid, 256, 0, st>>>(a);
-        h->launches++;
-        TRY(cudaGetLastError());
-        if (one) return CSER_OK;
-        RowSums s{};
-        s.part = h->part, s.out[0] = dbias, s.out_stride[0] = dbias_stride, s.rows = a.chunks, s.cols = h->cols;
-        return launch_row_sums(s, h->n, 1, h->launches, st);
-    }
-    if (vector)
-        drop_rows_kernel<T, true, false><<<grid, 256, 0, st>>>(a);
+    dense = dense && !(plain && h->cols >= 32 * V);    // wide rows of whole vectors: the simpler walk
+    const Walk k = walk_of(rows, h->cols, h->n, V, dense);
+    a.width = k.width, a.chunk_rows = k.chunk_rows, a.tx = k.tx, a.col_blocks = k.col_blocks, a.chunks = k.chunks;
+    const long long blocks = (long long)k.col_blocks * k.chunks * h->n;
+    if (blocks > kMostBlocks) return fail(CSER_ERR_INVALID, "dropout: too many elements");
+    const bool direct = k.chunks == 1 && k.width == h->cols;
+    if (dbias) a.part = direct ? dbias : h->part, a.part_worker = direct ? dbias_stride : k.chunks * k.width;
+    if (dense && shifted)
+        drop_rows_launch<T, kDense, true>(a, (unsigned)blocks, dbias, st);
+    else if (dense)
+        drop_rows_launch<T, kDense, false>(a, (unsigned)blocks, dbias, st);
+    else if (plain)
+        drop_rows_launch<T, kPlain, false>(a, (unsigned)blocks, dbias, st);
     else
-        drop_rows_kernel<T, false, false><<<grid, 256, 0, st>>>(a);
-    h->launches++;
+        drop_rows_launch<T, kOdd, true>(a, (unsigned)blocks, dbias, st);
     TRY(cudaGetLastError());
-    return CSER_OK;
+    if (!dbias || direct) return CSER_OK;
+    RowSums s{};
+    s.part = h->part, s.out[0] = dbias, s.out_stride[0] = dbias_stride, s.rows = k.chunks * (k.width / h->cols), s.cols = h->cols;
+    return launch_row_sums(s, h->n, 1, h->launches, st);
 }
 
 int drop_call(cser_drop *h, int64_t rows, uint64_t step, const uint64_t *step_at, const cser_rows *x, const float *bias, int64_t bias_stride,
@@ -209,11 +223,14 @@ cser_drop_handle cser_drop_create(int32_t n_workers, int64_t max_rows, int64_t c
     if (!h) return bad(CSER_ERR_NOMEM, "host allocation failed");
     h->n = n_workers, h->max_rows = max_rows, h->cols = cols, h->p = p, h->seed = seed, h->site = site, h->first_worker = first_worker,
     h->type = type;
-    int tx, blocks;
-    layers::column_blocks(cols, 16 / layers::size_of(type), tx, blocks);
-    const long long chunks = layers::row_chunks(max_rows, (long long)blocks * n_workers, tx);
+    // Walked either way.
+    long long sums = 0;
+    for (bool dense : {false, true}) {
+        const layers::Walk k = layers::walk_of(max_rows, cols, n_workers, 16 / layers::size_of(type), dense);
+        sums = std::max(sums, k.most_chunks * k.width);
+    }
     cudaError_t e = cudaGetDevice(&h->device);
-    if (e == cudaSuccess) e = cudaMalloc(&h->part, (size_t)(n_workers * chunks * cols) * 4);
+    if (e == cudaSuccess) e = cudaMalloc(&h->part, (size_t)(n_workers * sums) * 4);
     if (e != cudaSuccess) {
         fail(e == cudaErrorMemoryAllocation ? CSER_ERR_NOMEM : CSER_ERR_CUDA, "cser_drop_create: %s", cudaGetErrorString(e));
         delete h;

@@ -59,13 +59,18 @@ __device__ __forceinline__ void join_moments(float &n, float &mean, float &m2, f
     n = total;
 }
 
-// V elements of x as they count: dropped out or not.
-template <typename T, int V, bool DROP>
-__device__ __forceinline__ uint32_t counted(float (&f)[V], const Draw &d, unsigned long long step, uint32_t c3, long long e) {
+// V elements of x as they count, dropped out or not, from element e of the worker's array on; their keep bits.
+template <int V, bool DROP>
+__device__ __forceinline__ uint32_t counted(float (&f)[V], const Draw &d, const Words &words, long long e) {
     if (!DROP) return ~0u;
-    const uint32_t keep = keep_bits<V, V % 4 == 0>(d, step, c3, e);
+    const Drawn<V, V % 4 == 0> drawn(words, e);
+    uint32_t keep = 0;
 #pragma unroll
-    for (int j = 0; j < V; ++j) f[j] = keep >> j & 1 ? f[j] * d.factor : 0.f;
+    for (int j = 0; j < V; ++j) {
+        const bool k = drawn.w[j] >= d.threshold;
+        f[j] = k ? f[j] * d.factor : 0.f;
+        keep |= (uint32_t)k << j;
+    }
     return keep;
 }
 
@@ -108,7 +113,7 @@ template <typename T, int V> __device__ __forceinline__ void channels_of(Channel
 template <typename T, int V, bool DROP>
 __global__ void __launch_bounds__(256) norm_moments_kernel(NormArgs<T> a) {
     const Place p = place<T, V>(a);
-    const unsigned long long step = DROP ? step_of(a.draw) : 0;
+    const Words words(a.draw, p.w);
     float n = 0.f, mean[V], m2[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) mean[j] = m2[j] = 0.f;
@@ -127,7 +132,7 @@ __global__ void __launch_bounds__(256) norm_moments_kernel(NormArgs<T> a) {
             for (int u = 0; u < U; ++u)
                 if (i + u * p.rows < p.last) {
                     v[u].floats(f[u]);
-                    counted<T, V, DROP>(f[u], a.draw, step, a.draw.c3 + p.w, e0 + (i + u * p.rows) * a.channels);
+                    counted<V, DROP>(f[u], a.draw, words, e0 + (i + u * p.rows) * a.channels);
                     ++got;
                 }
             const float part = 1.f / got, share = got / (n + got);
@@ -212,7 +217,7 @@ template <typename T, int V, bool DROP>
 __global__ void __launch_bounds__(256) norm_apply_kernel(NormArgs<T> a) {
     const Place p = place<T, V>(a);
     if (!p.in) return;
-    const unsigned long long step = DROP ? step_of(a.draw) : 0;
+    const Words words(a.draw, p.w);
     Channels<V> k;
     channels_of(k, a, p.w, p.b, p.c, true);
     const T *x = a.x + p.w * a.xs.worker + p.b * a.xs.sample + p.c;
@@ -224,7 +229,7 @@ __global__ void __launch_bounds__(256) norm_apply_kernel(NormArgs<T> a) {
         float f[V];
         Vec<T, V> v(x + i * a.xs.pixel);
         v.floats(f);
-        counted<T, V, DROP>(f, a.draw, step, a.draw.c3 + p.w, e0 + i * a.channels);
+        counted<V, DROP>(f, a.draw, words, e0 + i * a.channels);
 #pragma unroll
         for (int j = 0; j < V; ++j) f[j] = activate(fmaf(f[j] - k.mean[j], k.weight[j], k.bias[j]), a.act);
         v.round(f);
@@ -236,7 +241,7 @@ __global__ void __launch_bounds__(256) norm_apply_kernel(NormArgs<T> a) {
 template <typename T, int V, bool DROP>
 __global__ void __launch_bounds__(256) norm_grad_sums_kernel(NormArgs<T> a) {
     const Place p = place<T, V>(a);
-    const unsigned long long step = DROP ? step_of(a.draw) : 0;
+    const Words words(a.draw, p.w);
     float s0[V], s1[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) s0[j] = s1[j] = 0.f;
@@ -249,7 +254,7 @@ __global__ void __launch_bounds__(256) norm_grad_sums_kernel(NormArgs<T> a) {
             float f[V], d[V];
             Vec<T, V> vx(x + i * a.xs.pixel), vd(dy + i * a.dys.pixel);
             vx.floats(f), vd.floats(d);
-            counted<T, V, DROP>(f, a.draw, step, a.draw.c3 + p.w, e0 + i * a.channels);
+            counted<V, DROP>(f, a.draw, words, e0 + i * a.channels);
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 const float h = (f[j] - k.mean[j]) * k.rstd[j], dz = slope_times(d[j], fmaf(h, k.weight[j], k.bias[j]), a.act);
@@ -301,7 +306,7 @@ template <typename T, int V, bool DROP>
 __global__ void __launch_bounds__(256) norm_grad_apply_kernel(NormArgs<T> a) {
     const Place p = place<T, V>(a);
     if (!p.in) return;
-    const unsigned long long step = DROP ? step_of(a.draw) : 0;
+    const Words words(a.draw, p.w);
     Channels<V> k;
     channels_of(k, a, p.w, p.b, p.c, true);
     float m1[V], m2[V];
@@ -317,7 +322,7 @@ __global__ void __launch_bounds__(256) norm_grad_apply_kernel(NormArgs<T> a) {
         float f[V], d[V];
         Vec<T, V> vx(x + i * a.xs.pixel), vd(dy + i * a.dys.pixel);
         vx.floats(f), vd.floats(d);
-        const uint32_t keep = counted<T, V, DROP>(f, a.draw, step, a.draw.c3 + p.w, e0 + i * a.channels);
+        const uint32_t keep = counted<V, DROP>(f, a.draw, words, e0 + i * a.channels);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             const float h = (f[j] - k.mean[j]) * k.rstd[j], dz = slope_times(d[j], fmaf(h, k.weight[j], k.bias[j]), a.act);

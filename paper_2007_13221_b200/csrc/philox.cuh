@@ -22,20 +22,17 @@ __device__ __forceinline__ uint32_t philox4x32_10_word0(uint32_t k0, uint32_t k1
 }
 
 
-// All four words of the same draw.
-__device__ __forceinline__ void philox4x32_10(uint32_t (&w)[4], uint32_t k0, uint32_t k1, uint32_t c0, uint32_t c1, uint32_t c2,
-                                              uint32_t c3) {
-    const uint32_t M0 = 0xD2511F53u, M1 = 0xCD9E8D57u;
-    const uint32_t W0 = 0x9E3779B9u, W1 = 0xBB67AE85u;
+// Rounds on all four words, with the key of the first of them.
+template <int ROUNDS>
+__device__ __forceinline__ void philox4x32_rounds(uint32_t &c0, uint32_t &c1, uint32_t &c2, uint32_t &c3, uint32_t k0, uint32_t k1) {
 #pragma unroll
-    for (int r = 0; r < 10; ++r) {
-        const uint64_t p0 = (uint64_t)M0 * c0, p1 = (uint64_t)M1 * c2;      // one wide multiply each
+    for (int r = 0; r < ROUNDS; ++r) {
+        const uint64_t p0 = (uint64_t)0xD2511F53u * c0, p1 = (uint64_t)0xCD9E8D57u * c2;      // one wide multiply each
         c0 = (uint32_t)(p1 >> 32) ^ c1 ^ k0;
         c1 = (uint32_t)p1;
         c2 = (uint32_t)(p0 >> 32) ^ c3 ^ k1;
         c3 = (uint32_t)p0;
-        k0 += W0;
-        k1 += W1;
+        k0 += 0x9E3779B9u;
+        k1 += 0xBB67AE85u;
     }
-    w[0] = c0, w[1] = c1, w[2] = c2, w[3] = c3;
 }
