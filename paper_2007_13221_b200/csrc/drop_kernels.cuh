@@ -18,7 +18,8 @@ template <typename T> struct DropArgs {
     long long rows, cols, part_worker;                 // part_worker: from one worker's sums to the next
     long long width;                                   // elements of a row as it is walked
     long long chunk_rows;
-    int tx, col_blocks, chunks;
+    long long walked, last_row;                        // such rows, and elements of the last, with nothing ahead
+    int tx, log_rows, col_blocks, chunks;              // log_rows: of 256 / tx
     int ahead, ahead_worker;                           // elements between a 16-byte boundary and the first worker's first element; more for each worker
     Draw draw;
 };
@@ -41,46 +42,40 @@ template <typename T, int V> __device__ __forceinline__ void store_some(const Ve
         if (j >= first && j < end) p[j] = v.at[j];
 }
 
-// Arrays that are dense for each worker and lie alike: all at the same distance from a 16-byte boundary.  Without bias and sums
-// columns do not matter: a warp takes kFlat * 32 vectors of the worker's array, 32 at a time.  SHIFTED: for some worker that distance is not
-// 0, so vectors start in the middle of four draws; what a lane lacks is its neighbour's, or, for the last lane, the first's of the 32
-// vectors behind, which are drawn first.  Grid (vectors / (256 kFlat), workers).
 constexpr int kFlat = 4;
-template <typename T, bool SHIFTED>
-__global__ void __launch_bounds__(256) drop_flat_kernel(DropArgs<T> a) {
+
+// The kFlat * 32 vectors of a warp, from its lane's element e0 on.  CHECKED: some of their elements may not exist.
+template <typename T, bool SHIFTED, bool RESIDUAL, bool CHECKED>
+__device__ __forceinline__ void drop_flat_warp(const DropArgs<T> &a, int w, int lane, long long e0, long long count) {
     constexpr int V = 16 / sizeof(T);
-    const long long count = a.rows * a.cols;
-    const int w = blockIdx.y, lane = threadIdx.x & 31;
-    const int ahead = SHIFTED ? (a.ahead + w * a.ahead_worker) % V : 0;
-    const long long e0 = (((long long)blockIdx.x * 8 + (threadIdx.x >> 5)) * (kFlat * 32) + lane) * V - ahead;
-    if (e0 - lane * V >= count) return;                // the whole warp
-    const T *x = a.x + w * a.x_worker + e0, *r = a.r ? a.r + w * a.r_worker + e0 : nullptr;
+    const T *x = a.x + w * a.x_worker + e0, *r = RESIDUAL ? a.r + w * a.r_worker + e0 : nullptr;
     T *y = a.y + w * a.y_worker + e0;
     Vec<T, V> vx[kFlat], vr[kFlat];
+    auto whole = [&](int u) { return !CHECKED || (e0 + u * 32 * V >= 0 && e0 + (u * 32 + 1) * V <= count); };
 #pragma unroll
     for (int u = 0; u < kFlat; ++u) {
         const long long e = e0 + u * 32 * V;
-        if (e >= 0 && e + V <= count) {
+        if (whole(u)) {
             vx[u] = Vec<T, V>(x + u * 32 * V);
-            if (r) vr[u] = Vec<T, V>(r + u * 32 * V);
+            if (RESIDUAL) vr[u] = Vec<T, V>(r + u * 32 * V);
         } else {
             load_some<T, V>(vx[u], x + u * 32 * V, -e, count - e);
-            if (r) load_some<T, V>(vr[u], r + u * 32 * V, -e, count - e);
+            if (RESIDUAL) load_some<T, V>(vr[u], r + u * 32 * V, -e, count - e);
         }
     }
     const Words words(a.draw, w);
+    const uint32_t quad = (uint32_t)(e0 >> 2), by = (uint32_t)e0 & 3;
     uint32_t next[3];                                  // the first draws of the 32 vectors behind
     if (SHIFTED) {
         uint32_t four[4];
-        words.four(four, (uint32_t)((e0 + (kFlat * 32 - lane) * V) >> 2));
+        words.four(four, quad + (kFlat * 32 - lane) * (V / 4));
         next[0] = four[0], next[1] = four[1], next[2] = four[2];
     }
 #pragma unroll
     for (int u = kFlat - 1; u >= 0; --u) {
-        const long long e = e0 + u * 32 * V;
         uint32_t d[V + 3];
 #pragma unroll
-        for (int k = 0; k < V / 4; ++k) words.four(d + 4 * k, (uint32_t)(e >> 2) + k);
+        for (int k = 0; k < V / 4; ++k) words.four(d + 4 * k, quad + u * 8 * V + k);
         if (SHIFTED) {
 #pragma unroll
             for (int j = 0; j < 3; ++j) {
@@ -88,19 +83,39 @@ __global__ void __launch_bounds__(256) drop_flat_kernel(DropArgs<T> a) {
                 d[V + j] = lane == 31 ? next[j] : neighbour;
                 next[j] = first;
             }
-            shift_words(d, (uint32_t)e & 3);
+            shift_words(d, by);
         }
         float f[V], g[V];
         vx[u].floats(f);
-        if (r) vr[u].floats(g);
+        if (RESIDUAL) vr[u].floats(g);
 #pragma unroll
-        for (int j = 0; j < V; ++j) f[j] = dropped_out(f[j], d[j] >= a.draw.threshold, a.draw.factor, r != nullptr, g[j]);
+        for (int j = 0; j < V; ++j) f[j] = dropped_out(f[j], d[j] >= a.draw.threshold, a.draw.factor, RESIDUAL, RESIDUAL ? g[j] : 0.f);
         vx[u].round(f);
-        if (e >= 0 && e + V <= count)
+        if (whole(u))
             vx[u].to(y + u * 32 * V);
         else
-            store_some<T, V>(vx[u], y + u * 32 * V, -e, count - e);
+            store_some<T, V>(vx[u], y + u * 32 * V, -(e0 + u * 32 * V), count - (e0 + u * 32 * V));
     }
+}
+
+// Arrays that are dense for each worker and lie alike: all at the same distance from a 16-byte boundary.  Without bias and sums
+// columns do not matter: a warp takes kFlat * 32 vectors of the worker's array, 32 at a time.  SHIFTED: for some worker that distance is not
+// 0, so vectors start in the middle of four draws; what a lane lacks is its neighbour's, or, for the last lane, the first's of the 32
+// vectors behind, which are drawn first.  Grid (vectors / (256 kFlat), workers).
+template <typename T, bool SHIFTED, bool RESIDUAL>
+__global__ void __launch_bounds__(256) drop_flat_kernel(DropArgs<T> a) {
+    constexpr int V = 16 / sizeof(T);
+    after_previous();
+    let_next();
+    const long long count = a.rows * a.cols;
+    const int w = blockIdx.y, lane = threadIdx.x & 31;
+    const int ahead = SHIFTED ? (a.ahead + w * a.ahead_worker) % V : 0;
+    const long long first = (long long)blockIdx.x * (256 * kFlat * V) - ahead;          // of the block
+    const long long e0 = first + ((threadIdx.x >> 5) * (kFlat * 32) + lane) * V;
+    if (first >= 0 && first + 256 * kFlat * V <= count)
+        drop_flat_warp<T, SHIFTED, RESIDUAL, false>(a, w, lane, e0, count);
+    else if (e0 - lane * V < count)                    // the whole warp
+        drop_flat_warp<T, SHIFTED, RESIDUAL, true>(a, w, lane, e0, count);
 }
 
 // With a bias or sums over rows, and for any strides: a thread keeps V neighbouring columns and walks down the rows of its chunk.  256
@@ -111,15 +126,19 @@ __global__ void __launch_bounds__(256) drop_flat_kernel(DropArgs<T> a) {
 //   PLAIN  rows that begin on 16-byte boundaries and hold whole vectors (width = cols).
 //   ODD    any rows, element by element.
 enum DropRows { kDense, kPlain, kOdd };
-template <typename T, int MODE, bool SHIFTED, bool SUMS>
-__global__ void __launch_bounds__(256) drop_rows_kernel(DropArgs<T> a) {
+enum DropKind { kSums, kForward, kResidual };       // the gradient with sums; the forward pass without and with a residual
+template <typename T, int MODE, bool SHIFTED, int KIND>
+__global__ void __launch_bounds__(256, 4) drop_rows_kernel(DropArgs<T> a) {
     constexpr int V = 16 / sizeof(T);
+    constexpr bool SUMS = KIND == kSums, residual = KIND == kResidual;
+    after_previous();
+    let_next();
     const int col_block = blockIdx.x % a.col_blocks, rest = blockIdx.x / a.col_blocks, chunk = rest % a.chunks, w = rest / a.chunks;
-    const int tx = threadIdx.x & (a.tx - 1), ty = threadIdx.x / a.tx, step_rows = 256 / a.tx;
+    const int tx = threadIdx.x & (a.tx - 1), step_rows = 1 << a.log_rows, ty = threadIdx.x >> (8 - a.log_rows);
     const long long count = a.rows * a.cols;
     const int ahead = MODE == kDense && SHIFTED ? (a.ahead + w * a.ahead_worker) % V : 0;
     const long long c = ((long long)col_block * a.tx + tx) * V;                    // of the row as it is walked
-    const long long walked = MODE == kDense ? (count + ahead + a.width - 1) / a.width : a.rows;
+    const long long walked = a.walked + (MODE == kDense && a.last_row + ahead > a.width);
     const long long first = chunk * a.chunk_rows, last = first + a.chunk_rows < walked ? first + a.chunk_rows : walked;
     const bool in = c < a.width;
     const Words words(a.draw, w);
@@ -132,51 +151,84 @@ __global__ void __launch_bounds__(256) drop_rows_kernel(DropArgs<T> a) {
 #pragma unroll
     for (int j = 0; j < V; ++j) {
         b[j] = sum[j] = 0.f;
-        if (a.bias && in && col < a.cols) b[j] = a.bias[w * a.bias_worker + col];
+        if (!SUMS && a.bias && in && col < a.cols) b[j] = a.bias[w * a.bias_worker + col];
         if (++col == a.cols && MODE == kDense) col = 0;
     }
-    if (in)
-        for (long long row = first + ty; row < last; row += step_rows) {
-            const long long e = MODE == kDense ? row * a.width + c - ahead : row * a.cols + c;
-            const T *x, *r = nullptr;
-            T *y = nullptr;
-            if (MODE == kDense) {
-                x = a.x + w * a.x_worker + e;
-                if (a.r) r = a.r + w * a.r_worker + e;
-                if (a.y) y = a.y + w * a.y_worker + e;
-            } else {
-                x = a.x + w * a.x_worker + row * a.x_row + c;
-                if (a.r) r = a.r + w * a.r_worker + row * a.r_row + c;
-                if (a.y) y = a.y + w * a.y_worker + row * a.y_row + c;
-            }
-            const long long begin = MODE == kDense ? -e : 0, end = MODE == kDense ? count - e : a.cols - c;
-            const bool whole = MODE == kPlain || (MODE == kDense && begin <= 0 && end >= V);
-            Vec<T, V> vx, vr;
-            if (whole) {
-                vx = Vec<T, V>(x);
-                if (r) vr = Vec<T, V>(r);
-            } else {
-                load_some<T, V>(vx, x, begin, end);
-                if (r) load_some<T, V>(vr, r, begin, end);
-            }
-            const Drawn<V, !SHIFTED> d(words, e);
+    if (in && first + ty < last) {
+        // Places of the thread's first row, and how far its next is.
+        const long long row0 = first + ty, e_row = MODE == kDense ? a.width : a.cols, e = row0 * e_row + c - ahead;
+        const long long x_step = (MODE == kDense ? a.width : a.x_row) << a.log_rows, r_step = (MODE == kDense ? a.width : a.r_row) << a.log_rows,
+                        y_step = (MODE == kDense ? a.width : a.y_row) << a.log_rows, e_step = e_row << a.log_rows;
+        const bool store = !SUMS || a.y;
+        uint32_t quad = (uint32_t)(e >> 2);
+        const uint32_t by = (uint32_t)e & 3, quad_step = (uint32_t)(e_step >> 2);          // (not odd: rows are whole fours)
+        const T *x = a.x + w * a.x_worker + (e - (MODE == kDense ? 0 : row0 * (e_row - a.x_row))), *r = nullptr;
+        T *y = nullptr;
+        if (residual) r = a.r + w * a.r_worker + (e - (MODE == kDense ? 0 : row0 * (e_row - a.r_row)));
+        if (store) y = a.y + w * a.y_worker + (e - (MODE == kDense ? 0 : row0 * (e_row - a.y_row)));
+        const int steps = (int)((last - row0 + step_rows - 1) >> a.log_rows);
+
+        auto finish = [&](Vec<T, V> &vx, const Vec<T, V> &vr, const Drawn<V, !SHIFTED> &d) {
             float f[V], g[V];
             vx.floats(f);
-            if (r) vr.floats(g);
+            if (residual) vr.floats(g);
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                const bool keep = d.w[j] >= a.draw.threshold && (whole || (j >= begin && j < end));
-                const float v = f[j] + b[j];
-                if (SUMS) sum[j] += keep ? v * a.draw.factor : 0.f;
-                f[j] = dropped_out(v, keep, a.draw.factor, r != nullptr, g[j]);
+                f[j] = dropped_out(SUMS ? f[j] : f[j] + b[j], d.w[j] >= a.draw.threshold, a.draw.factor, residual, residual ? g[j] : 0.f);
+                if (SUMS) sum[j] += f[j];
             }
-            if (!y) continue;
             vx.round(f);
-            if (whole)
-                vx.to(y);
-            else
-                store_some<T, V>(vx, y, begin, end);
+        };
+        auto next = [&](int rows) {
+            x += rows * x_step, quad += rows * quad_step;
+            if (residual) r += rows * r_step;
+            if (store) y += rows * y_step;
+        };
+        // A row of which some elements may not exist, or that begins anywhere.
+        auto some = [&](int i) {
+            const long long at = e + i * e_step, begin = MODE == kDense ? -at : 0, end = MODE == kDense ? count - at : a.cols - c;
+            Vec<T, V> vx, vr;
+#pragma unroll
+            for (int j = 0; j < V; ++j) vx.at[j] = vr.at[j] = from_float<T>(0.f);
+            load_some<T, V>(vx, x, begin, end);
+            if (residual) load_some<T, V>(vr, r, begin, end);
+            finish(vx, vr, Drawn<V, !SHIFTED>(words, at));
+            if (store) store_some<T, V>(vx, y, begin, end);
+            next(1);
+        };
+        int i = 0;
+        if (MODE == kOdd) {
+            for (; i < steps; ++i) some(i);
+        } else {
+            // Of the dense rows only the first and the last can be short.
+            const bool short_last = MODE == kDense && row0 + ((long long)(steps - 1) << a.log_rows) == walked - 1;
+            const int whole = short_last ? steps - 1 : steps;
+            if (MODE == kDense && row0 == 0 && whole) some(i++);
+            constexpr int U = residual || V == 8 ? 2 : 4;       // rows whose loads are under way together
+            for (; i + U <= whole; i += U) {
+                Vec<T, V> vx[U], vr[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    vx[u] = Vec<T, V>(x + u * x_step);
+                    if (residual) vr[u] = Vec<T, V>(r + u * r_step);
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    finish(vx[u], vr[u], Drawn<V, !SHIFTED>(words, quad + u * quad_step, by));
+                    if (store) vx[u].to(y + u * y_step);
+                }
+                next(U);
+            }
+            for (; i < whole; ++i) {
+                Vec<T, V> vx(x), vr;
+                if (residual) vr = Vec<T, V>(r);
+                finish(vx, vr, Drawn<V, !SHIFTED>(words, quad, by));
+                if (store) vx.to(y);
+                next(1);
+            }
+            if (i < steps) some(i);
         }
+    }
     if (!SUMS) return;
     // Rows of a warp first, then the eight warps.
     __shared__ float sums[8][32 * V];

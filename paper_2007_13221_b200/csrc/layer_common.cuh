@@ -2,6 +2,11 @@
 // Device code; included by layers.cuh inside its unnamed namespace.
 #pragma once
 
+// Every kernel is set up while the one before it in the stream ends, and touches no memory before that end.
+__device__ __forceinline__ void after_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// The next kernel may be set up from here on.
+__device__ __forceinline__ void let_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 // ------------------------------------------------------------------ elements
 template <int BYTES> struct Raw;
 template <> struct Raw<16> { typedef uint4 type; };
@@ -111,12 +116,12 @@ template <int N> __device__ __forceinline__ void shift_words(uint32_t (&w)[N], u
 template <int V, bool ALIGNED> struct Drawn {
     static constexpr int kCalls = ALIGNED ? V / 4 : (V + 2) / 4 + 1;
     uint32_t w[kCalls * 4];
-    __device__ __forceinline__ Drawn(const Words &words, long long e) {
-        const uint32_t quad = (uint32_t)(e >> 2);
+    __device__ __forceinline__ Drawn(const Words &words, uint32_t quad, uint32_t by) {
 #pragma unroll
         for (int k = 0; k < kCalls; ++k) words.four(w + 4 * k, quad + k);
-        if (!ALIGNED) shift_words(w, (uint32_t)e & 3);
+        if (!ALIGNED) shift_words(w, by);
     }
+    __device__ __forceinline__ Drawn(const Words &words, long long e) : Drawn(words, (uint32_t)(e >> 2), (uint32_t)e & 3) {}
 };
 
 // ------------------------------------------------------------------ sums over rows
@@ -130,6 +135,7 @@ struct RowSums {
 };
 __global__ void __launch_bounds__(1024) sum_rows_kernel(RowSums a) {
     __shared__ float sums[32][33];
+    after_previous();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const long long c = (long long)blockIdx.x * 32 + lane;
     float *out = a.out[blockIdx.z];

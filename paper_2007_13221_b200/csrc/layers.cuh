@@ -71,10 +71,22 @@ Draw draw_of(double p, uint64_t seed, uint32_t site, int first_worker, uint64_t 
     return d;
 }
 
+// A launch that may be set up while the kernel before it ends; `cluster` blocks form one.
+template <typename... P, typename... A>
+cudaError_t launch(void (*kernel)(P...), dim3 grid, unsigned block, size_t shared, unsigned cluster, cudaStream_t st, const A &...args) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid, cfg.blockDim = dim3(block), cfg.dynamicSmemBytes = shared, cfg.stream = st;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization, at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = cluster, at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+    cfg.attrs = at, cfg.numAttrs = cluster > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
+}
+
 int launch_row_sums(const RowSums &s, long long n, int planes, int64_t &launches, cudaStream_t st) {
-    sum_rows_kernel<<<dim3((unsigned)ceil_div(s.cols, 32), (unsigned)n, (unsigned)planes), 1024, 0, st>>>(s);
+    TRY(launch(sum_rows_kernel, dim3((unsigned)ceil_div(s.cols, 32), (unsigned)n, (unsigned)planes), 1024, 0, 1, st, s));
     launches++;
-    TRY(cudaGetLastError());
     return CSER_OK;
 }
 
@@ -120,28 +132,29 @@ long long rows_walked_as_one(long long cols, int v) {
     return least * std::max(1ll, ceil_div(32 * v, least * cols));
 }
 
+constexpr int kSteps = 8, kSumSteps = 16;
 // How the rows of a call are walked.
 struct Walk {
     long long width, rows, chunk_rows, most_chunks;    // most_chunks: of this many rows or fewer
     int tx, col_blocks, chunks;
 };
-Walk walk_of(long long rows, long long cols, int n, int v, bool dense) {
+Walk walk_of(long long rows, long long cols, int n, int v, bool dense, bool sums) {
     Walk k;
     const long long fold = dense ? rows_walked_as_one(cols, v) : 1;
     k.width = fold * cols, k.rows = dense ? ceil_div(rows * cols + v - 1, k.width) : rows;
     column_blocks(k.width, v, k.tx, k.col_blocks);
-    const long long most = ceil_div(k.rows, 4 * (256 / k.tx)), want = ceil_div(kBusy, (long long)k.col_blocks * n);
-    k.most_chunks = std::min(most, want);
+    // Each thread kSteps rows, or fewer, but four, where that leaves the GPU idle.
+    const long long step = 256 / k.tx, most = ceil_div(k.rows, 4 * step), want = ceil_div(kBusy, (long long)k.col_blocks * n);
+    k.most_chunks = std::min(most, std::max(want, ceil_div(k.rows, (sums ? kSumSteps : kSteps) * step)));
     k.chunk_rows = ceil_div(k.rows, k.most_chunks);
     k.chunks = (int)ceil_div(k.rows, k.chunk_rows);
     return k;
 }
 
-template <typename T, int MODE, bool SHIFTED> void drop_rows_launch(const DropArgs<T> &a, unsigned grid, bool sums, cudaStream_t st) {
-    if (sums)
-        drop_rows_kernel<T, MODE, SHIFTED, true><<<grid, 256, 0, st>>>(a);
-    else
-        drop_rows_kernel<T, MODE, SHIFTED, false><<<grid, 256, 0, st>>>(a);
+template <typename T, int MODE, bool SHIFTED> cudaError_t drop_rows_launch(const DropArgs<T> &a, unsigned grid, bool sums, cudaStream_t st) {
+    const auto kernel = sums ? drop_rows_kernel<T, MODE, SHIFTED, kSums>
+                             : a.r ? drop_rows_kernel<T, MODE, SHIFTED, kResidual> : drop_rows_kernel<T, MODE, SHIFTED, kForward>;
+    return launch(kernel, dim3(grid), 256, 0, 1, st, a);
 }
 
 template <typename T>
@@ -162,33 +175,29 @@ int drop_launch(cser_drop *h, int64_t rows, const Draw &draw, const cser_rows *x
     if (residual) a.r = static_cast<const T *>(residual->data), a.r_row = residual->row_stride, a.r_worker = residual->worker_stride, take(residual);
     if (y) a.y = static_cast<T *>(y->data), a.y_row = y->row_stride, a.y_worker = y->worker_stride, take(y);
     const bool shifted = a.ahead || a.ahead_worker;
-    h->launches++;
     if (dense && !bias && !dbias) {
         const long long blocks = ceil_div(rows * h->cols + V - 1, 256 * V * kFlat);
         const dim3 grid((unsigned)blocks, (unsigned)h->n);
-        if (shifted)
-            drop_flat_kernel<T, true><<<grid, 256, 0, st>>>(a);
-        else
-            drop_flat_kernel<T, false><<<grid, 256, 0, st>>>(a);
-        TRY(cudaGetLastError());
+        const auto kernel = shifted ? (a.r ? drop_flat_kernel<T, true, true> : drop_flat_kernel<T, true, false>)
+                                    : (a.r ? drop_flat_kernel<T, false, true> : drop_flat_kernel<T, false, false>);
+        TRY(launch(kernel, grid, 256, 0, 1, st, a));
+        h->launches++;
         return CSER_OK;
     }
     dense = dense && !(plain && h->cols >= 32 * V);    // wide rows of whole vectors: the simpler walk
-    const Walk k = walk_of(rows, h->cols, h->n, V, dense);
-    a.width = k.width, a.chunk_rows = k.chunk_rows, a.tx = k.tx, a.col_blocks = k.col_blocks, a.chunks = k.chunks;
+    const Walk k = walk_of(rows, h->cols, h->n, V, dense, dbias);
+    a.width = k.width, a.chunk_rows = k.chunk_rows, a.tx = k.tx, a.log_rows = 8 - (int)std::log2(k.tx);
+    a.walked = dense ? ceil_div(rows * h->cols, k.width) : rows, a.last_row = rows * h->cols - (a.walked - 1) * k.width;
+    a.col_blocks = k.col_blocks, a.chunks = k.chunks;
     const long long blocks = (long long)k.col_blocks * k.chunks * h->n;
     if (blocks > kMostBlocks) return fail(CSER_ERR_INVALID, "dropout: too many elements");
     const bool direct = k.chunks == 1 && k.width == h->cols;
     if (dbias) a.part = direct ? dbias : h->part, a.part_worker = direct ? dbias_stride : k.chunks * k.width;
-    if (dense && shifted)
-        drop_rows_launch<T, kDense, true>(a, (unsigned)blocks, dbias, st);
-    else if (dense)
-        drop_rows_launch<T, kDense, false>(a, (unsigned)blocks, dbias, st);
-    else if (plain)
-        drop_rows_launch<T, kPlain, false>(a, (unsigned)blocks, dbias, st);
-    else
-        drop_rows_launch<T, kOdd, true>(a, (unsigned)blocks, dbias, st);
-    TRY(cudaGetLastError());
+    TRY((dense && shifted ? drop_rows_launch<T, kDense, true>(a, (unsigned)blocks, dbias, st)
+         : dense          ? drop_rows_launch<T, kDense, false>(a, (unsigned)blocks, dbias, st)
+         : plain          ? drop_rows_launch<T, kPlain, false>(a, (unsigned)blocks, dbias, st)
+                          : drop_rows_launch<T, kOdd, true>(a, (unsigned)blocks, dbias, st)));
+    h->launches++;
     if (!dbias || direct) return CSER_OK;
     RowSums s{};
     s.part = h->part, s.out[0] = dbias, s.out_stride[0] = dbias_stride, s.rows = k.chunks * (k.width / h->cols), s.cols = h->cols;
@@ -226,7 +235,7 @@ cser_drop_handle cser_drop_create(int32_t n_workers, int64_t max_rows, int64_t c
     // Walked either way.
     long long sums = 0;
     for (bool dense : {false, true}) {
-        const layers::Walk k = layers::walk_of(max_rows, cols, n_workers, 16 / layers::size_of(type), dense);
+        const layers::Walk k = layers::walk_of(max_rows, cols, n_workers, 16 / layers::size_of(type), dense, true);
         sums = std::max(sums, k.most_chunks * k.width);
     }
     cudaError_t e = cudaGetDevice(&h->device);
@@ -356,18 +365,11 @@ template <typename T> int norm_apply(cser_norm *h, const cser_norm_inputs *in, c
         constexpr int V = decltype(vector)::value;
         unsigned grid;
         if (!cut(a, V, true, grid)) return fail(CSER_ERR_INVALID, "cser_norm_apply: too many elements");
-        if (h->drop)
-            norm_moments_kernel<T, V, true><<<grid, 256, 0, st>>>(a);
-        else
-            norm_moments_kernel<T, V, false><<<grid, 256, 0, st>>>(a);
-        norm_join_moments_kernel<T><<<(unsigned)ceil_div((long long)a.n * a.samples * a.groups, 8), 256, 0, st>>>(a);
+        TRY(launch(h->drop ? norm_moments_kernel<T, V, true> : norm_moments_kernel<T, V, false>, dim3(grid), 256, 0, 1, st, a));
+        TRY(launch(norm_join_moments_kernel<T>, dim3((unsigned)ceil_div((long long)a.n * a.samples * a.groups, 8)), 256, 0, 1, st, a));
         if (!cut(a, V, false, grid)) return fail(CSER_ERR_INVALID, "cser_norm_apply: too many elements");
-        if (h->drop)
-            norm_apply_kernel<T, V, true><<<grid, 256, 0, st>>>(a);
-        else
-            norm_apply_kernel<T, V, false><<<grid, 256, 0, st>>>(a);
+        TRY(launch(h->drop ? norm_apply_kernel<T, V, true> : norm_apply_kernel<T, V, false>, dim3(grid), 256, 0, 1, st, a));
         h->launches += 3;
-        TRY(cudaGetLastError());
         return CSER_OK;
     });
 }
@@ -383,12 +385,8 @@ int norm_grad(cser_norm *h, const cser_norm_inputs *in, const float *stats, cons
         constexpr int V = decltype(vector)::value;
         unsigned grid;
         if (!cut(a, V, true, grid)) return fail(CSER_ERR_INVALID, "cser_norm_grad: too many elements");
-        if (h->drop)
-            norm_grad_sums_kernel<T, V, true><<<grid, 256, 0, st>>>(a);
-        else
-            norm_grad_sums_kernel<T, V, false><<<grid, 256, 0, st>>>(a);
+        TRY(launch(h->drop ? norm_grad_sums_kernel<T, V, true> : norm_grad_sums_kernel<T, V, false>, dim3(grid), 256, 0, 1, st, a));
         h->launches++;
-        TRY(cudaGetLastError());
         if (dweight || dbias) {
             RowSums s{};
             s.part = a.part, s.plane = a.plane, s.rows = (long long)a.samples * a.chunks, s.cols = a.channels;
@@ -396,14 +394,10 @@ int norm_grad(cser_norm *h, const cser_norm_inputs *in, const float *stats, cons
             if (int rc = launch_row_sums(s, a.n, 2, h->launches, st)) return rc;
         }
         if (!dx) return CSER_OK;
-        norm_join_sums_kernel<T><<<(unsigned)ceil_div((long long)a.n * a.samples * a.groups, 8), 256, 0, st>>>(a);
+        TRY(launch(norm_join_sums_kernel<T>, dim3((unsigned)ceil_div((long long)a.n * a.samples * a.groups, 8)), 256, 0, 1, st, a));
         if (!cut(a, V, false, grid)) return fail(CSER_ERR_INVALID, "cser_norm_grad: too many elements");
-        if (h->drop)
-            norm_grad_apply_kernel<T, V, true><<<grid, 256, 0, st>>>(a);
-        else
-            norm_grad_apply_kernel<T, V, false><<<grid, 256, 0, st>>>(a);
+        TRY(launch(h->drop ? norm_grad_apply_kernel<T, V, true> : norm_grad_apply_kernel<T, V, false>, dim3(grid), 256, 0, 1, st, a));
         h->launches += 2;
-        TRY(cudaGetLastError());
         return CSER_OK;
     });
 }

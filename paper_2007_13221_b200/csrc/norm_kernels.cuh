@@ -112,6 +112,8 @@ template <typename T, int V> __device__ __forceinline__ void channels_of(Channel
 // Moments of each channel over a chunk of a sample's pixels: plane 0 the mean, plane 1 the sum of squares about it.
 template <typename T, int V, bool DROP>
 __global__ void __launch_bounds__(256) norm_moments_kernel(NormArgs<T> a) {
+    after_previous();
+    let_next();
     const Place p = place<T, V>(a);
     const Words words(a.draw, p.w);
     float n = 0.f, mean[V], m2[V];
@@ -192,6 +194,8 @@ __global__ void __launch_bounds__(256) norm_moments_kernel(NormArgs<T> a) {
 
 // Mean and rstd of each group from its channels' moments: a warp a group.
 template <typename T> __global__ void __launch_bounds__(256) norm_join_moments_kernel(NormArgs<T> a) {
+    after_previous();
+    let_next();
     const long long g = (long long)blockIdx.x * 8 + (threadIdx.x >> 5), all = (long long)a.n * a.samples * a.groups;
     if (g >= all) return;
     const int lane = threadIdx.x & 31;
@@ -215,6 +219,8 @@ template <typename T> __global__ void __launch_bounds__(256) norm_join_moments_k
 
 template <typename T, int V, bool DROP>
 __global__ void __launch_bounds__(256) norm_apply_kernel(NormArgs<T> a) {
+    after_previous();
+    let_next();
     const Place p = place<T, V>(a);
     if (!p.in) return;
     const Words words(a.draw, p.w);
@@ -240,6 +246,8 @@ __global__ void __launch_bounds__(256) norm_apply_kernel(NormArgs<T> a) {
 // Sums of dz (plane 0) and dz * xhat (plane 1) of each channel over a chunk of a sample's pixels.
 template <typename T, int V, bool DROP>
 __global__ void __launch_bounds__(256) norm_grad_sums_kernel(NormArgs<T> a) {
+    after_previous();
+    let_next();
     const Place p = place<T, V>(a);
     const Words words(a.draw, p.w);
     float s0[V], s1[V];
@@ -283,6 +291,8 @@ __global__ void __launch_bounds__(256) norm_grad_sums_kernel(NormArgs<T> a) {
 
 // s1 / N and s2 / N of each group: a warp a group.
 template <typename T> __global__ void __launch_bounds__(256) norm_join_sums_kernel(NormArgs<T> a) {
+    after_previous();
+    let_next();
     const long long g = (long long)blockIdx.x * 8 + (threadIdx.x >> 5), all = (long long)a.n * a.samples * a.groups;
     if (g >= all) return;
     const int lane = threadIdx.x & 31;
@@ -304,6 +314,8 @@ template <typename T> __global__ void __launch_bounds__(256) norm_join_sums_kern
 
 template <typename T, int V, bool DROP>
 __global__ void __launch_bounds__(256) norm_grad_apply_kernel(NormArgs<T> a) {
+    after_previous();
+    let_next();
     const Place p = place<T, V>(a);
     if (!p.in) return;
     const Words words(a.draw, p.w);
