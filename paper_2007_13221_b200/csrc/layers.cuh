@@ -1,6 +1,6 @@
 // layers.cuh - host side of the layers between the models' products (include/cser_layers.h); included by cser.cu.
 //
-// Kernels: drop_kernels.cuh (dropout), norm_kernels.cuh (group norm), layer_common.cuh (what both use).
+// Kernels: drop_kernels.cuh (dropout), norm_resident.cuh and norm_kernels.cuh (group norm), layer_common.cuh (what both use).
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -13,6 +13,7 @@ namespace layers {
 #include "layer_common.cuh"
 #include "drop_kernels.cuh"
 #include "norm_kernels.cuh"
+#include "norm_resident.cuh"
 
 constexpr long long kBusy = 148 * 8;                   // blocks of 256 threads that fill the GPU; a constant, so that sums do not depend on the GPU
 constexpr long long kMostBlocks = 0x7fffffff;
@@ -357,6 +358,42 @@ template <typename T, typename F> int with_vector(int v, F f) {
     return v == 2 ? f(std::integral_constant<int, 2>()) : f(std::integral_constant<int, 1>());
 }
 
+// How a call is made in one walk, with v elements a vector; false: it does not fit, or vectors are too short for asynchronous copies.
+// Slices of 128 bytes of a pixel, or of 64 or 32 where wider ones do not fit a cluster or would leave SMs idle.  Of the numbers of blocks to an SM
+// that shared memory can be cut for, three where that fits, then two, then one.
+bool plan_resident(const cser_norm *h, const cser_norm_inputs *in, int v, bool two, Resident &r, size_t &shared) {
+    const int size = size_of(h->type), per_group = (int)(h->channels / h->groups);
+    if (v * size < 4) return false;
+    const long long least = std::lcm(per_group, v) / v, all = h->channels / v, samples = (long long)h->n * in->samples;
+    if (least > 256) return false;
+    bool found = false;
+    for (size_t most : {size_t(74) << 10, size_t(112) << 10, size_t(220) << 10}) {
+        for (int bytes : {128, 64, 32}) {
+            Resident k{};
+            k.sv = (int)std::min(all, least * ceil_div(bytes, least * v * size));
+            if (k.sv > 256) continue;
+            while (1 << k.log_tx < k.sv) ++k.log_tx;
+            const int rows = 256 >> k.log_tx;
+            k.slices = (int)ceil_div(all, k.sv);
+            auto cut = [&](int cluster) {
+                k.cluster = cluster, k.per = ceil_div(in->pixels, cluster);
+                const long long slots = ceil_div(k.per, rows);
+                k.slots = (int)std::min(slots, 1ll << 16);
+                return resident_shared(k, v, size, two, two && h->drop) <= most;
+            };
+            int c = 1;
+            while (!cut(c) && c < 8) c *= 2;
+            if (!cut(c) || samples * k.slices * c > kMostBlocks) continue;
+            while (samples * k.slices * k.cluster < kBusy / 4 && c < 8 && k.per >= 4 * rows) cut(c *= 2);
+            r = k, found = true;
+            if (samples * k.slices * 8 >= kBusy / 4) break;
+        }
+        if (found) break;
+    }
+    if (found) shared = resident_shared(r, v, size, two, two && h->drop);
+    return found;
+}
+
 template <typename T> int norm_apply(cser_norm *h, const cser_norm_inputs *in, const cser_pixels *y, float *stats, cudaStream_t st) {
     NormArgs<T> a = norm_args<T>(h, in, stats);
     a.y = static_cast<T *>(y->data), a.ys = view_of(y);
@@ -364,6 +401,16 @@ template <typename T> int norm_apply(cser_norm *h, const cser_norm_inputs *in, c
     return with_vector<T>(v, [&](auto vector) -> int {
         constexpr int V = decltype(vector)::value;
         unsigned grid;
+        if constexpr (V * sizeof(T) >= 4) {
+            Resident r;
+            size_t shared;
+            if (plan_resident(h, in, V, false, r, shared)) {
+                grid = (unsigned)((long long)a.n * a.samples * r.slices * r.cluster);
+                TRY(launch(h->drop ? norm_resident_kernel<T, V, true> : norm_resident_kernel<T, V, false>, dim3(grid), 256, shared, r.cluster, st, a, r));
+                h->launches++;
+                return CSER_OK;
+            }
+        }
         if (!cut(a, V, true, grid)) return fail(CSER_ERR_INVALID, "cser_norm_apply: too many elements");
         TRY(launch(h->drop ? norm_moments_kernel<T, V, true> : norm_moments_kernel<T, V, false>, dim3(grid), 256, 0, 1, st, a));
         TRY(launch(norm_join_moments_kernel<T>, dim3((unsigned)ceil_div((long long)a.n * a.samples * a.groups, 8)), 256, 0, 1, st, a));
@@ -384,8 +431,21 @@ int norm_grad(cser_norm *h, const cser_norm_inputs *in, const float *stats, cons
     return with_vector<T>(v, [&](auto vector) -> int {
         constexpr int V = decltype(vector)::value;
         unsigned grid;
-        if (!cut(a, V, true, grid)) return fail(CSER_ERR_INVALID, "cser_norm_grad: too many elements");
-        TRY(launch(h->drop ? norm_grad_sums_kernel<T, V, true> : norm_grad_sums_kernel<T, V, false>, dim3(grid), 256, 0, 1, st, a));
+        bool done = false;
+        if constexpr (V * sizeof(T) >= 4) {
+            Resident r;
+            size_t shared;
+            if (plan_resident(h, in, V, true, r, shared)) {
+                grid = (unsigned)((long long)a.n * a.samples * r.slices * r.cluster);
+                a.part = dweight || dbias ? h->part : nullptr, a.chunks = 1, done = true;
+                TRY(launch(h->drop ? norm_grad_resident_kernel<T, V, true> : norm_grad_resident_kernel<T, V, false>, dim3(grid), 256, shared, r.cluster,
+                           st, a, r));
+            }
+        }
+        if (!done) {
+            if (!cut(a, V, true, grid)) return fail(CSER_ERR_INVALID, "cser_norm_grad: too many elements");
+            TRY(launch(h->drop ? norm_grad_sums_kernel<T, V, true> : norm_grad_sums_kernel<T, V, false>, dim3(grid), 256, 0, 1, st, a));
+        }
         h->launches++;
         if (dweight || dbias) {
             RowSums s{};
@@ -393,13 +453,28 @@ int norm_grad(cser_norm *h, const cser_norm_inputs *in, const float *stats, cons
             s.out[0] = dbias, s.out_stride[0] = dbias_stride, s.out[1] = dweight, s.out_stride[1] = dweight_stride;
             if (int rc = launch_row_sums(s, a.n, 2, h->launches, st)) return rc;
         }
-        if (!dx) return CSER_OK;
+        if (!dx || done) return CSER_OK;
         TRY(launch(norm_join_sums_kernel<T>, dim3((unsigned)ceil_div((long long)a.n * a.samples * a.groups, 8)), 256, 0, 1, st, a));
         if (!cut(a, V, false, grid)) return fail(CSER_ERR_INVALID, "cser_norm_grad: too many elements");
         TRY(launch(h->drop ? norm_grad_apply_kernel<T, V, true> : norm_grad_apply_kernel<T, V, false>, dim3(grid), 256, 0, 1, st, a));
         h->launches += 2;
         return CSER_OK;
     });
+}
+
+// The one-walk kernels of a type may use all of an SM's shared memory.
+template <typename T, int V> cudaError_t allow_shared_of() {
+    if constexpr (V * sizeof(T) >= 4) {
+        for (auto k : {norm_resident_kernel<T, V, false>, norm_resident_kernel<T, V, true>, norm_grad_resident_kernel<T, V, false>,
+                       norm_grad_resident_kernel<T, V, true>})
+            if (cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 << 10)) return e;
+    }
+    return cudaSuccess;
+}
+template <typename T> cudaError_t allow_shared() {
+    cudaError_t e = allow_shared_of<T, 16 / sizeof(T)>();
+    if (e == cudaSuccess) e = allow_shared_of<T, 8 / sizeof(T)>();
+    return e == cudaSuccess ? allow_shared_of<T, 4 / sizeof(T)>() : e;
 }
 
 // Checks that both calls make; *empty: nothing to compute.
@@ -453,6 +528,9 @@ cser_norm_handle cser_norm_create(int32_t n_workers, int64_t max_samples, int64_
     const long long all = (long long)n_workers * max_samples;
     h->plane = (all + layers::kBusy) * channels;
     cudaError_t e = cudaGetDevice(&h->device);
+    if (e == cudaSuccess)
+        e = type == CSER_TYPE_F32 ? layers::allow_shared<float>() : type == CSER_TYPE_BF16 ? layers::allow_shared<__nv_bfloat16>()
+                                                                                          : layers::allow_shared<__half>();
     if (e == cudaSuccess) e = cudaMalloc(&h->part, (size_t)h->plane * 2 * 4);
     if (e == cudaSuccess) e = cudaMalloc(&h->group_sums, (size_t)(all * groups) * sizeof(float2));
     if (e != cudaSuccess) {
