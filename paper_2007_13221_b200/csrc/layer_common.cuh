@@ -66,6 +66,53 @@ template <> __device__ __forceinline__ void Vec<__half, 8>::round(const float (&
     bits = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// Two floats that one instruction works on: half the issue slots of the layers whose arithmetic would otherwise bound them.
+struct F2 {
+    float x, y;
+};
+__device__ __forceinline__ unsigned long long bits_of(F2 a) {
+    unsigned long long r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a.x), "f"(a.y));
+    return r;
+}
+__device__ __forceinline__ F2 pair_of(unsigned long long r) {
+    F2 a;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(a.x), "=f"(a.y) : "l"(r));
+    return a;
+}
+__device__ __forceinline__ F2 two(float v) { return {v, v}; }
+__device__ __forceinline__ F2 operator+(F2 a, F2 b) {
+    unsigned long long r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits_of(a)), "l"(bits_of(b)));
+    return pair_of(r);
+}
+__device__ __forceinline__ F2 operator*(F2 a, F2 b) {
+    unsigned long long r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits_of(a)), "l"(bits_of(b)));
+    return pair_of(r);
+}
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+    unsigned long long r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(bits_of(a)), "l"(bits_of(b)), "l"(bits_of(c)));
+    return pair_of(r);
+}
+__device__ __forceinline__ F2 operator-(F2 a, F2 b) { return fma2(b, two(-1.f), a); }
+
+// V elements as pairs; of a single one the other half is 0.
+template <int V> constexpr int kPairs = (V + 1) / 2;
+template <typename T, int V> __device__ __forceinline__ void pairs_of(const Vec<T, V> &v, F2 (&p)[kPairs<V>]) {
+    float f[V];
+    v.floats(f);
+#pragma unroll
+    for (int j = 0; j < kPairs<V>; ++j) p[j] = {f[2 * j], 2 * j + 1 < V ? f[(2 * j + 1) % V] : 0.f};
+}
+template <typename T, int V> __device__ __forceinline__ void round_pairs(Vec<T, V> &v, const F2 (&p)[kPairs<V>]) {
+    float f[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) f[j] = j & 1 ? p[j / 2].y : p[j / 2].x;
+    v.round(f);
+}
+
 // ------------------------------------------------------------------ draws
 struct Draw {
     uint32_t k0 = 0, k1 = 0, c3 = 0, threshold = 0;    // c3: of the first worker

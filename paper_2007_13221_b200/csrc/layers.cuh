@@ -358,40 +358,47 @@ template <typename T, typename F> int with_vector(int v, F f) {
     return v == 2 ? f(std::integral_constant<int, 2>()) : f(std::integral_constant<int, 1>());
 }
 
+constexpr int kSharedAimed = 36 << 10;
 // How a call is made in one walk, with v elements a vector; false: it does not fit, or vectors are too short for asynchronous copies.
-// Slices of 128 bytes of a pixel, or of 64 or 32 where wider ones do not fit a cluster or would leave SMs idle.  Of the numbers of blocks to an SM
-// that shared memory can be cut for, three where that fits, then two, then one.
+// Slices of 128 bytes of a pixel, or of 64 or 32 where wider ones do not fit a cluster or would leave SMs idle.
 bool plan_resident(const cser_norm *h, const cser_norm_inputs *in, int v, bool two, Resident &r, size_t &shared) {
     const int size = size_of(h->type), per_group = (int)(h->channels / h->groups);
     if (v * size < 4) return false;
     const long long least = std::lcm(per_group, v) / v, all = h->channels / v, samples = (long long)h->n * in->samples;
-    if (least > 256) return false;
+    if (least > kBlock) return false;
     bool found = false;
-    for (size_t most : {size_t(74) << 10, size_t(112) << 10, size_t(220) << 10}) {
+    for (bool last : {false, true}) {
         for (int bytes : {128, 64, 32}) {
             Resident k{};
             k.sv = (int)std::min(all, least * ceil_div(bytes, least * v * size));
-            if (k.sv > 256) continue;
+            if (k.sv > kBlock) continue;
             while (1 << k.log_tx < k.sv) ++k.log_tx;
-            const int rows = 256 >> k.log_tx;
-            k.slices = (int)ceil_div(all, k.sv);
-            auto cut = [&](int cluster) {
-                k.cluster = cluster, k.per = ceil_div(in->pixels, cluster);
-                const long long slots = ceil_div(k.per, rows);
-                k.slots = (int)std::min(slots, 1ll << 16);
-                return resident_shared(k, v, size, two, two && h->drop) <= most;
+            const int rows = kBlock >> k.log_tx;
+            const long long slices = ceil_div(all, k.sv);
+            auto cut = [&](int log_cluster) {
+                k.log_cluster = log_cluster, k.per = (int)ceil_div(in->pixels, 1 << log_cluster);
+                k.slots = (int)std::min(ceil_div(k.per, rows), 1ll << 16);
+                return resident_shared(k, v, size, two, two && h->drop);
             };
-            int c = 1;
-            while (!cut(c) && c < 8) c *= 2;
-            if (!cut(c) || samples * k.slices * c > kMostBlocks) continue;
-            while (samples * k.slices * k.cluster < kBusy / 4 && c < 8 && k.per >= 4 * rows) cut(c *= 2);
+            int c = 0;
+            while (c < 3 && cut(c) > (size_t)kSharedAimed) ++c;
+            if (cut(c) > (size_t)(last ? 220 << 10 : 112 << 10) || samples << c > kMostBlocks || slices > 65535) continue;
+            while ((samples * slices << k.log_cluster) < kBusy / 4 && c < 3 && k.per >= 4 * rows) cut(++c);
             r = k, found = true;
-            if (samples * k.slices * 8 >= kBusy / 4) break;
+            if (samples * slices * 8 >= kBusy / 4) break;
         }
         if (found) break;
     }
-    if (found) shared = resident_shared(r, v, size, two, two && h->drop);
-    return found;
+    if (!found) return false;
+    r.fold = std::gcd(per_group, v), r.log_sub = 0;
+    const int entries = two ? per_group : (per_group / r.fold) << r.log_cluster;
+    while (r.log_sub < 5 && 1 << r.log_sub < entries) ++r.log_sub;
+    r.group_magic = per_group == 1 ? 0 : (uint32_t)(((1ull << 32) + per_group - 1) / per_group);
+    shared = resident_shared(r, v, size, two, two && h->drop);
+    return true;
+}
+template <typename T> dim3 resident_grid(const NormArgs<T> &a, const Resident &r, int v) {
+    return dim3((unsigned)(a.n * a.samples) << r.log_cluster, (unsigned)ceil_div(a.channels / v, r.sv));
 }
 
 template <typename T> int norm_apply(cser_norm *h, const cser_norm_inputs *in, const cser_pixels *y, float *stats, cudaStream_t st) {
@@ -405,8 +412,8 @@ template <typename T> int norm_apply(cser_norm *h, const cser_norm_inputs *in, c
             Resident r;
             size_t shared;
             if (plan_resident(h, in, V, false, r, shared)) {
-                grid = (unsigned)((long long)a.n * a.samples * r.slices * r.cluster);
-                TRY(launch(h->drop ? norm_resident_kernel<T, V, true> : norm_resident_kernel<T, V, false>, dim3(grid), 256, shared, r.cluster, st, a, r));
+                TRY(launch(h->drop ? norm_resident_kernel<T, V, true> : norm_resident_kernel<T, V, false>, resident_grid(a, r, V), kBlock, shared,
+                           1 << r.log_cluster, st, a, r));
                 h->launches++;
                 return CSER_OK;
             }
@@ -436,10 +443,9 @@ int norm_grad(cser_norm *h, const cser_norm_inputs *in, const float *stats, cons
             Resident r;
             size_t shared;
             if (plan_resident(h, in, V, true, r, shared)) {
-                grid = (unsigned)((long long)a.n * a.samples * r.slices * r.cluster);
                 a.part = dweight || dbias ? h->part : nullptr, a.chunks = 1, done = true;
-                TRY(launch(h->drop ? norm_grad_resident_kernel<T, V, true> : norm_grad_resident_kernel<T, V, false>, dim3(grid), 256, shared, r.cluster,
-                           st, a, r));
+                TRY(launch(h->drop ? norm_grad_resident_kernel<T, V, true> : norm_grad_resident_kernel<T, V, false>, resident_grid(a, r, V), kBlock,
+                           shared, 1 << r.log_cluster, st, a, r));
             }
         }
         if (!done) {

@@ -1,11 +1,14 @@
-// norm_kernels.cuh - group norm with an activation, channels last, forward and gradient.
+// norm_kernels.cuh - group norm with an activation, channels last, forward and gradient: arithmetic, and kernels for samples that do not
+// fit a cluster's shared memory (norm_resident.cuh) or rows that begin anywhere.
 // Device code; included by layers.cuh inside its unnamed namespace.
 //
 //   xhat = (x - mean) rstd,  z = xhat weight + bias,  y = act(z)
 //   dz = dy act'(z),  dx = rstd (dz weight - (s1 + xhat s2) / N),  s1 = sum dz weight,  s2 = sum dz weight xhat  over the group
 //
 // Everything that is summed is summed for each channel first, then over the channels of a group: one walk over the pixels serves any
-// number of channels a group, and the gradient's channel sums are dbias and dweight.  Bound: memory.
+// number of channels a group, and the gradient's channel sums are dbias and dweight.  Bound: memory, with the issue of instructions close
+// behind (eight bf16 elements of a silu gradient are 190 of the 264 slots that an SM's quarter has for them at the copy rate, and
+// their 32 exponentials and reciprocals 256 of its cycles): two floats an instruction, and approximations by single instructions.
 #pragma once
 
 enum { kActNone = CSER_ACT_NONE, kActRelu = CSER_ACT_RELU, kActSilu = CSER_ACT_SILU };
@@ -30,22 +33,42 @@ template <typename T> struct NormArgs {
     Draw draw;
 };
 
-// Exponential and reciprocal by the hardware's approximations, about 2^-22 each: below the rounding of fp32 results' own sums by little,
-// of 16-bit ones by far.
-__device__ __forceinline__ float sigmoid(float z) { return __fdividef(1.f, 1.f + __expf(-z)); }
+// f(act as a constant): loops with the activation inside are compiled once for each.
+template <typename F> __device__ __forceinline__ void with_act(int act, F f) {
+    if (act == kActSilu)
+        f(std::integral_constant<int, kActSilu>());
+    else if (act == kActRelu)
+        f(std::integral_constant<int, kActRelu>());
+    else
+        f(std::integral_constant<int, kActNone>());
+}
 
-__device__ __forceinline__ float activate(float z, int act) {
-    if (act == kActSilu) return z * sigmoid(z);
-    if (act == kActRelu) return z > 0.f || z != z ? z : 0.f;
+// 1 / (1 + exp(-z)) by the exponential and the reciprocal that are instructions, each good to about 2^-22: as good as the rounding of
+// z in 32 bits lets it be, and far below that of 16-bit results.
+__device__ __forceinline__ F2 sigmoid(F2 z) {
+    F2 t = z * two(-1.4426950408889634f);
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(t.x));
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(t.y));
+    t = t + two(1.f);
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(t.x));
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(t.y));
+    return t;
+}
+// NaN stays NaN.
+__device__ __forceinline__ float relu(float v, float z) { return z <= 0.f ? 0.f : v; }
+
+template <int ACT> __device__ __forceinline__ F2 activate(F2 z) {
+    if (ACT == kActSilu) return z * sigmoid(z);
+    if (ACT == kActRelu) return {relu(z.x, z.x), relu(z.y, z.y)};
     return z;
 }
 // dy * act'(z)
-__device__ __forceinline__ float slope_times(float dy, float z, int act) {
-    if (act == kActSilu) {
-        const float g = sigmoid(z);
-        return dy * (g * fmaf(z, 1.f - g, 1.f));
+template <int ACT> __device__ __forceinline__ F2 slope_times(F2 dy, F2 z) {
+    if (ACT == kActSilu) {
+        const F2 g = sigmoid(z);
+        return dy * (g * fma2(z, two(1.f) - g, two(1.f)));
     }
-    if (act == kActRelu) return z > 0.f || z != z ? dy : 0.f;
+    if (ACT == kActRelu) return {relu(dy.x, z.x), relu(dy.y, z.y)};
     return dy;
 }
 
@@ -59,21 +82,131 @@ __device__ __forceinline__ void join_moments(float &n, float &mean, float &m2, f
     n = total;
 }
 
-// V elements of x as they count, dropped out or not, from element e of the worker's array on; their keep bits.
-template <int V, bool DROP>
-__device__ __forceinline__ uint32_t counted(float (&f)[V], const Draw &d, const Words &words, long long e) {
-    if (!DROP) return ~0u;
-    const Drawn<V, V % 4 == 0> drawn(words, e);
+// Moments of a thread's V channels.  Values are taken kBatch at a time relative to the first of them, which keeps sums of squares from
+// cancelling: that value is one of the set, so what is subtracted is at most kBatch times what is left, wherever the mean is.
+constexpr int kBatch = 32;
+template <int V> struct Moments {
+    float n = 0.f;
+    F2 mean[kPairs<V>], m2[kPairs<V>];
+    F2 first[kPairs<V>], sum[kPairs<V>], squares[kPairs<V>];
+
+    __device__ __forceinline__ Moments() {
+#pragma unroll
+        for (int j = 0; j < kPairs<V>; ++j) mean[j] = m2[j] = two(0.f);
+    }
+    __device__ __forceinline__ void begin(const F2 (&f)[kPairs<V>]) {
+#pragma unroll
+        for (int j = 0; j < kPairs<V>; ++j) first[j] = f[j], sum[j] = squares[j] = two(0.f);
+    }
+    __device__ __forceinline__ void add(const F2 (&f)[kPairs<V>]) {
+#pragma unroll
+        for (int j = 0; j < kPairs<V>; ++j) {
+            const F2 d = f[j] - first[j];
+            sum[j] = sum[j] + d, squares[j] = fma2(d, d, squares[j]);
+        }
+    }
+    // The batch had `count` values, the first among them.
+    __device__ __forceinline__ void end(int count) {
+        const float total = n + count, share = count / total, part = 1.f / count;
+#pragma unroll
+        for (int j = 0; j < kPairs<V>; ++j) {
+            const F2 s = sum[j] * two(part), d = first[j] + s - mean[j], q = fma2(sum[j], s * two(-1.f), squares[j]);
+            mean[j] = fma2(d, two(share), mean[j]);
+            m2[j] = m2[j] + q + d * d * two(n * share);
+        }
+        n = total;
+    }
+    // Joins the sets of the threads of a warp whose lanes differ in bits `span` and above; all end with the same bits.
+    __device__ __forceinline__ void join_lanes(int span) {
+        for (int o = span; o < 32; o <<= 1) {
+            const float n2 = __shfl_xor_sync(~0u, n, o), total = n + n2;
+            const bool upper = threadIdx.x & o;                                     // the lower lane's set comes first in both
+            const float share = total == 0.f ? 0.f : (upper ? n : n2) / total, weight = (upper ? n2 : n) * share;
+#pragma unroll
+            for (int j = 0; j < kPairs<V>; ++j) {
+                const F2 other = {__shfl_xor_sync(~0u, mean[j].x, o), __shfl_xor_sync(~0u, mean[j].y, o)};
+                const F2 q = {__shfl_xor_sync(~0u, m2[j].x, o), __shfl_xor_sync(~0u, m2[j].y, o)};
+                const F2 low = upper ? other : mean[j], d = (upper ? mean[j] : other) - low;
+                mean[j] = fma2(d, two(share), low);
+                m2[j] = m2[j] + q + d * d * two(weight);
+            }
+            n = total;
+        }
+    }
+};
+
+// Drops out what a worker's array has from element e on: dropped elements become 0, others stay (times the factor later); keep bits.
+template <typename T, int V> __device__ __forceinline__ uint32_t drop_out(Vec<T, V> &v, const Draw &draw, const Words &words, long long e) {
+    const Drawn<V, V % 4 == 0> d(words, e);
     uint32_t keep = 0;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-        const bool k = drawn.w[j] >= d.threshold;
-        f[j] = k ? f[j] * d.factor : 0.f;
-        keep |= (uint32_t)k << j;
+        const bool kept = d.w[j] >= draw.threshold;
+        if (!kept) v.at[j] = from_float<T>(0.f);
+        keep |= (uint32_t)kept << j;
     }
     return keep;
 }
+// Values as they count.
+template <typename T, int V, bool DROP> __device__ __forceinline__ void counted(F2 (&f)[kPairs<V>], const Vec<T, V> &v, float factor) {
+    pairs_of(v, f);
+    if (DROP) {
+#pragma unroll
+        for (int j = 0; j < kPairs<V>; ++j) f[j] = f[j] * two(factor);
+    }
+}
 
+// A thread's channels.  xhat = x * rstd + offset: one rounding more than (x - mean) rstd, of the size of that of the mean.
+template <int V> struct Channels {
+    F2 rstd[kPairs<V>], offset[kPairs<V>], weight[kPairs<V>], bias[kPairs<V>];
+};
+template <typename T, int V> __device__ __forceinline__ void channels_of(Channels<V> &k, const NormArgs<T> &a, int w, int b, int c) {
+    const float *means = a.stats + ((long long)w * a.samples + b) * a.groups, *rstds = means + (long long)a.n * a.samples * a.groups;
+    float v[4][2 * kPairs<V>] = {};
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        const int g = (c + j) / a.per_group;
+        v[0][j] = rstds[g], v[1][j] = -means[g] * v[0][j];
+        v[2][j] = a.weight ? a.weight[w * a.weight_worker + c + j] : 1.f;
+        v[3][j] = a.bias ? a.bias[w * a.bias_worker + c + j] : 0.f;
+    }
+#pragma unroll
+    for (int j = 0; j < kPairs<V>; ++j) {
+        k.rstd[j] = {v[0][2 * j], v[0][2 * j + 1]}, k.offset[j] = {v[1][2 * j], v[1][2 * j + 1]};
+        k.weight[j] = {v[2][2 * j], v[2][2 * j + 1]}, k.bias[j] = {v[3][2 * j], v[3][2 * j + 1]};
+    }
+}
+
+// Sums dz and dz * xhat of a vector.
+template <typename T, int V, bool DROP, int ACT>
+__device__ __forceinline__ void add_grad(F2 (&s0)[kPairs<V>], F2 (&s1)[kPairs<V>], const Channels<V> &k, const Vec<T, V> &vx, const Vec<T, V> &vd,
+                                         float factor) {
+    F2 f[kPairs<V>], d[kPairs<V>];
+    counted<T, V, DROP>(f, vx, factor);
+    pairs_of(vd, d);
+#pragma unroll
+    for (int j = 0; j < kPairs<V>; ++j) {
+        const F2 h = fma2(f[j], k.rstd[j], k.offset[j]), dz = slope_times<ACT>(d[j], fma2(h, k.weight[j], k.bias[j]));
+        s0[j] = s0[j] + dz, s1[j] = fma2(dz, h, s1[j]);
+    }
+}
+// dx of a vector, into vx.  scale = rstd * weight, m1 = -rstd s1 / N, m2 = -rstd s2 / N.
+template <typename T, int V, bool DROP, int ACT>
+__device__ __forceinline__ void make_grad(Vec<T, V> &vx, const Channels<V> &k, const F2 (&scale)[kPairs<V>], const F2 (&m1)[kPairs<V>],
+                                          const F2 (&m2)[kPairs<V>], const Vec<T, V> &vd, float factor, uint32_t keep) {
+    F2 f[kPairs<V>], d[kPairs<V>];
+    counted<T, V, DROP>(f, vx, factor);
+    pairs_of(vd, d);
+#pragma unroll
+    for (int j = 0; j < kPairs<V>; ++j) {
+        const F2 h = fma2(f[j], k.rstd[j], k.offset[j]), dz = slope_times<ACT>(d[j], fma2(h, k.weight[j], k.bias[j]));
+        f[j] = fma2(h, m2[j], fma2(dz, scale[j], m1[j]));
+        if (DROP) f[j] = {keep >> 2 * j & 1 ? f[j].x * factor : 0.f, keep >> (2 * j + 1) & 1 ? f[j].y * factor : 0.f};
+    }
+    round_pairs(vx, f);
+}
+
+// ------------------------------------------------------------------ in several walks
 // Where a thread of the walking kernels stands.  256 threads are tx column vectors (a power of two up to 32) x 256 / tx pixels.
 struct Place {
     int w, b, chunk, c, ty, rows;                      // rows: pixels that the block takes at a time
@@ -94,20 +227,15 @@ template <typename T, int V> __device__ __forceinline__ Place place(const NormAr
     p.in = p.c < a.channels;
     return p;
 }
-
-template <int V> struct Channels {                     // a thread's channels
-    float mean[V], rstd[V], weight[V], bias[V];
-};
-template <typename T, int V> __device__ __forceinline__ void channels_of(Channels<V> &k, const NormArgs<T> &a, int w, int b, int c, bool with_stats) {
-    const float *mean = a.stats + ((long long)w * a.samples + b) * a.groups, *rstd = mean + (long long)a.n * a.samples * a.groups;
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-        const int g = (c + j) / a.per_group;
-        k.mean[j] = with_stats ? mean[g] : 0.f, k.rstd[j] = with_stats ? rstd[g] : 0.f;
-        k.weight[j] = a.weight ? a.weight[w * a.weight_worker + c + j] : 1.f;
-        k.bias[j] = a.bias ? a.bias[w * a.bias_worker + c + j] : 0.f;
-    }
+// The thread's element of pixel i.
+template <typename T> __device__ __forceinline__ T *at_pixel(T *p, const View &v, const Place &s, long long i) {
+    return p + s.w * v.worker + s.b * v.sample + i * v.pixel + s.c;
 }
+// Its place in the worker's array, as the dropout counts.
+template <typename T> __device__ __forceinline__ long long element(const NormArgs<T> &a, const Place &s, long long i) {
+    return (s.b * a.pixels + i) * a.channels + s.c;
+}
+constexpr int kTogether = 4;                           // pixels whose loads are under way together
 
 // Moments of each channel over a chunk of a sample's pixels: plane 0 the mean, plane 1 the sum of squares about it.
 template <typename T, int V, bool DROP>
@@ -116,70 +244,40 @@ __global__ void __launch_bounds__(256) norm_moments_kernel(NormArgs<T> a) {
     let_next();
     const Place p = place<T, V>(a);
     const Words words(a.draw, p.w);
-    float n = 0.f, mean[V], m2[V];
-#pragma unroll
-    for (int j = 0; j < V; ++j) mean[j] = m2[j] = 0.f;
+    Moments<V> m;
     if (p.in) {
-        const T *x = a.x + p.w * a.xs.worker + p.b * a.xs.sample + p.c;
-        const long long e0 = (long long)p.b * a.pixels * a.channels + p.c;
-        constexpr int U = 4;                           // pixels whose moments are taken about their own mean, then joined
-        for (long long i = p.first + p.ty; i < p.last; i += U * p.rows) {
-            float f[U][V];
-            Vec<T, V> v[U];
+        const T *x = at_pixel(a.x, a.xs, p, p.first + p.ty);
+        int got = 0;                                   // of the batch
+        for (long long i = p.first + p.ty; i < p.last; i += kTogether * p.rows, x += kTogether * p.rows * a.xs.pixel) {
+            Vec<T, V> v[kTogether];
 #pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (i + u * p.rows < p.last) v[u] = Vec<T, V>(x + (i + u * p.rows) * a.xs.pixel);
-            int got = 0;
+            for (int u = 0; u < kTogether; ++u)
+                if (i + u * p.rows < p.last) v[u] = Vec<T, V>(x + u * p.rows * a.xs.pixel);
 #pragma unroll
-            for (int u = 0; u < U; ++u)
+            for (int u = 0; u < kTogether; ++u)
                 if (i + u * p.rows < p.last) {
-                    v[u].floats(f[u]);
-                    counted<V, DROP>(f[u], a.draw, words, e0 + (i + u * p.rows) * a.channels);
+                    if (DROP) drop_out(v[u], a.draw, words, element(a, p, i + u * p.rows));
+                    F2 f[kPairs<V>];
+                    counted<T, V, DROP>(f, v[u], a.draw.factor);
+                    if (got == 0) m.begin(f);
+                    m.add(f);
                     ++got;
                 }
-            const float part = 1.f / got, share = got / (n + got);
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                float s = f[0][j];
-#pragma unroll
-                for (int u = 1; u < U; ++u) s += u < got ? f[u][j] : 0.f;
-                s *= part;
-                float q = 0.f;
-#pragma unroll
-                for (int u = 0; u < U; ++u)
-                    if (u < got) q = fmaf(f[u][j] - s, f[u][j] - s, q);
-                const float d = s - mean[j];
-                mean[j] = fmaf(d, share, mean[j]);
-                m2[j] += q + d * d * (n * share);
-            }
-            n += got;
+            if (got + kTogether > kBatch) m.end(got), got = 0;
         }
+        if (got) m.end(got);
     }
     // Threads of the same channels: those of a warp, then the eight warps.
+    m.join_lanes(a.tx);
     __shared__ float count[8][32], means[8][32 * V], squares[8][32 * V];
-    for (int o = a.tx; o < 32; o <<= 1) {
-        const float n2 = __shfl_xor_sync(~0u, n, o);
-        float total = n;
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const float mean2 = __shfl_xor_sync(~0u, mean[j], o), m22 = __shfl_xor_sync(~0u, m2[j], o);
-            total = n;
-            // The lower lane's set comes first in both, so that both end with the same bits.
-            if (threadIdx.x & o) {
-                float nn = n2, mm = mean2, qq = m22;
-                join_moments(nn, mm, qq, n, mean[j], m2[j]);
-                mean[j] = mm, m2[j] = qq, total = nn;
-            } else {
-                join_moments(total, mean[j], m2[j], n2, mean2, m22);
-            }
-        }
-        n = n + n2;
-    }
     const int warp = threadIdx.x >> 5, tx = threadIdx.x & (a.tx - 1);
     if ((threadIdx.x & 31) < a.tx) {
-        count[warp][tx] = n;
+        count[warp][tx] = m.n;
 #pragma unroll
-        for (int j = 0; j < V; ++j) means[warp][tx * V + j] = mean[j], squares[warp][tx * V + j] = m2[j];
+        for (int j = 0; j < V; ++j) {
+            means[warp][tx * V + j] = j & 1 ? m.mean[j / 2].y : m.mean[j / 2].x;
+            squares[warp][tx * V + j] = j & 1 ? m.m2[j / 2].y : m.m2[j / 2].x;
+        }
     }
     __syncthreads();
     const int k = threadIdx.x, c = (blockIdx.x % a.col_blocks) * a.tx * V + k;
@@ -225,22 +323,31 @@ __global__ void __launch_bounds__(256) norm_apply_kernel(NormArgs<T> a) {
     if (!p.in) return;
     const Words words(a.draw, p.w);
     Channels<V> k;
-    channels_of(k, a, p.w, p.b, p.c, true);
-    const T *x = a.x + p.w * a.xs.worker + p.b * a.xs.sample + p.c;
-    T *y = a.y + p.w * a.ys.worker + p.b * a.ys.sample + p.c;
-    const long long e0 = (long long)p.b * a.pixels * a.channels + p.c;
+    channels_of(k, a, p.w, p.b, p.c);
+    F2 scale[kPairs<V>], shift[kPairs<V>];
 #pragma unroll
-    for (int j = 0; j < V; ++j) k.weight[j] *= k.rstd[j];
-    for (long long i = p.first + p.ty; i < p.last; i += p.rows) {
-        float f[V];
-        Vec<T, V> v(x + i * a.xs.pixel);
-        v.floats(f);
-        counted<V, DROP>(f, a.draw, words, e0 + i * a.channels);
+    for (int j = 0; j < kPairs<V>; ++j) scale[j] = k.rstd[j] * k.weight[j], shift[j] = fma2(k.offset[j], k.weight[j], k.bias[j]);
+    const T *x = at_pixel(a.x, a.xs, p, p.first + p.ty);
+    T *y = at_pixel(a.y, a.ys, p, p.first + p.ty);
+    with_act(a.act, [&](auto act) {
+        for (long long i = p.first + p.ty; i < p.last; i += kTogether * p.rows, x += kTogether * p.rows * a.xs.pixel, y += kTogether * p.rows * a.ys.pixel) {
+            Vec<T, V> v[kTogether];
 #pragma unroll
-        for (int j = 0; j < V; ++j) f[j] = activate(fmaf(f[j] - k.mean[j], k.weight[j], k.bias[j]), a.act);
-        v.round(f);
-        v.to(y + i * a.ys.pixel);
-    }
+            for (int u = 0; u < kTogether; ++u)
+                if (i + u * p.rows < p.last) v[u] = Vec<T, V>(x + u * p.rows * a.xs.pixel);
+#pragma unroll
+            for (int u = 0; u < kTogether; ++u)
+                if (i + u * p.rows < p.last) {
+                    if (DROP) drop_out(v[u], a.draw, words, element(a, p, i + u * p.rows));
+                    F2 f[kPairs<V>];
+                    counted<T, V, DROP>(f, v[u], a.draw.factor);
+#pragma unroll
+                    for (int j = 0; j < kPairs<V>; ++j) f[j] = activate<decltype(act)::value>(fma2(f[j], scale[j], shift[j]));
+                    round_pairs(v[u], f);
+                    v[u].to(y + u * p.rows * a.ys.pixel);
+                }
+        }
+    });
 }
 
 // Sums of dz (plane 0) and dz * xhat (plane 1) of each channel over a chunk of a sample's pixels.
@@ -250,42 +357,48 @@ __global__ void __launch_bounds__(256) norm_grad_sums_kernel(NormArgs<T> a) {
     let_next();
     const Place p = place<T, V>(a);
     const Words words(a.draw, p.w);
-    float s0[V], s1[V];
+    F2 s0[kPairs<V>], s1[kPairs<V>];
 #pragma unroll
-    for (int j = 0; j < V; ++j) s0[j] = s1[j] = 0.f;
+    for (int j = 0; j < kPairs<V>; ++j) s0[j] = s1[j] = two(0.f);
     if (p.in) {
         Channels<V> k;
-        channels_of(k, a, p.w, p.b, p.c, true);
-        const T *x = a.x + p.w * a.xs.worker + p.b * a.xs.sample + p.c, *dy = a.dy + p.w * a.dys.worker + p.b * a.dys.sample + p.c;
-        const long long e0 = (long long)p.b * a.pixels * a.channels + p.c;
-        for (long long i = p.first + p.ty; i < p.last; i += p.rows) {
-            float f[V], d[V];
-            Vec<T, V> vx(x + i * a.xs.pixel), vd(dy + i * a.dys.pixel);
-            vx.floats(f), vd.floats(d);
-            counted<V, DROP>(f, a.draw, words, e0 + i * a.channels);
+        channels_of(k, a, p.w, p.b, p.c);
+        const T *x = at_pixel(a.x, a.xs, p, p.first + p.ty), *dy = at_pixel(a.dy, a.dys, p, p.first + p.ty);
+        constexpr int U = 2;
+        with_act(a.act, [&](auto act) {
+            for (long long i = p.first + p.ty; i < p.last; i += U * p.rows, x += U * p.rows * a.xs.pixel, dy += U * p.rows * a.dys.pixel) {
+                Vec<T, V> vx[U], vd[U];
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const float h = (f[j] - k.mean[j]) * k.rstd[j], dz = slope_times(d[j], fmaf(h, k.weight[j], k.bias[j]), a.act);
-                s0[j] += dz, s1[j] = fmaf(dz, h, s1[j]);
+                for (int u = 0; u < U; ++u)
+                    if (i + u * p.rows < p.last) vx[u] = Vec<T, V>(x + u * p.rows * a.xs.pixel), vd[u] = Vec<T, V>(dy + u * p.rows * a.dys.pixel);
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (i + u * p.rows < p.last) {
+                        if (DROP) drop_out(vx[u], a.draw, words, element(a, p, i + u * p.rows));
+                        add_grad<T, V, DROP, decltype(act)::value>(s0, s1, k, vx[u], vd[u], a.draw.factor);
+                    }
             }
-        }
+        });
     }
+    float t0[2 * kPairs<V>], t1[2 * kPairs<V>];
+#pragma unroll
+    for (int j = 0; j < kPairs<V>; ++j) t0[2 * j] = s0[j].x, t0[2 * j + 1] = s0[j].y, t1[2 * j] = s1[j].x, t1[2 * j + 1] = s1[j].y;
     __shared__ float sums[2][8][32 * V];
     for (int o = a.tx; o < 32; o <<= 1)
 #pragma unroll
-        for (int j = 0; j < V; ++j) s0[j] += __shfl_xor_sync(~0u, s0[j], o), s1[j] += __shfl_xor_sync(~0u, s1[j], o);
+        for (int j = 0; j < V; ++j) t0[j] += __shfl_xor_sync(~0u, t0[j], o), t1[j] += __shfl_xor_sync(~0u, t1[j], o);
     const int warp = threadIdx.x >> 5, tx = threadIdx.x & (a.tx - 1);
     if ((threadIdx.x & 31) < a.tx)
 #pragma unroll
-        for (int j = 0; j < V; ++j) sums[0][warp][tx * V + j] = s0[j], sums[1][warp][tx * V + j] = s1[j];
+        for (int j = 0; j < V; ++j) sums[0][warp][tx * V + j] = t0[j], sums[1][warp][tx * V + j] = t1[j];
     __syncthreads();
     const int k = threadIdx.x, c = (blockIdx.x % a.col_blocks) * a.tx * V + k;
     if (k < a.tx * V && c < a.channels) {
-        float t0 = 0.f, t1 = 0.f;
+        float u0 = 0.f, u1 = 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) t0 += sums[0][i][k], t1 += sums[1][i][k];
+        for (int i = 0; i < 8; ++i) u0 += sums[0][i][k], u1 += sums[1][i][k];
         const long long at = (((long long)p.w * a.samples + p.b) * a.chunks + p.chunk) * a.channels + c;
-        a.part[at] = t0, a.part[a.plane + at] = t1;
+        a.part[at] = u0, a.part[a.plane + at] = u1;
     }
 }
 
@@ -312,6 +425,17 @@ template <typename T> __global__ void __launch_bounds__(256) norm_join_sums_kern
     if (lane == 0) a.group_sums[g] = make_float2(s0 * of, s1 * of);
 }
 
+// Factors of make_grad for a thread's channels, from its groups' s1 / N and s2 / N.
+template <int V, typename F>
+__device__ __forceinline__ void grad_factors(F2 (&scale)[kPairs<V>], F2 (&m1)[kPairs<V>], F2 (&m2)[kPairs<V>], const Channels<V> &k, F sums) {
+#pragma unroll
+    for (int j = 0; j < kPairs<V>; ++j) {
+        const float2 a = sums(2 * j), b = 2 * j + 1 < V ? sums(2 * j + 1) : make_float2(0.f, 0.f);
+        scale[j] = k.rstd[j] * k.weight[j];
+        m1[j] = k.rstd[j] * F2{-a.x, -b.x}, m2[j] = k.rstd[j] * F2{-a.y, -b.y};
+    }
+}
+
 template <typename T, int V, bool DROP>
 __global__ void __launch_bounds__(256) norm_grad_apply_kernel(NormArgs<T> a) {
     after_previous();
@@ -320,28 +444,26 @@ __global__ void __launch_bounds__(256) norm_grad_apply_kernel(NormArgs<T> a) {
     if (!p.in) return;
     const Words words(a.draw, p.w);
     Channels<V> k;
-    channels_of(k, a, p.w, p.b, p.c, true);
-    float m1[V], m2[V];
+    channels_of(k, a, p.w, p.b, p.c);
+    F2 scale[kPairs<V>], m1[kPairs<V>], m2[kPairs<V>];
+    grad_factors<V>(scale, m1, m2, k, [&](int j) { return a.group_sums[((long long)p.w * a.samples + p.b) * a.groups + (p.c + j) / a.per_group]; });
+    const T *x = at_pixel(a.x, a.xs, p, p.first + p.ty), *dy = at_pixel(a.dy, a.dys, p, p.first + p.ty);
+    T *y = at_pixel(a.y, a.ys, p, p.first + p.ty);
+    constexpr int U = 2;
+    with_act(a.act, [&](auto act) {
+        for (long long i = p.first + p.ty; i < p.last;
+             i += U * p.rows, x += U * p.rows * a.xs.pixel, dy += U * p.rows * a.dys.pixel, y += U * p.rows * a.ys.pixel) {
+            Vec<T, V> vx[U], vd[U];
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-        const float2 m = a.group_sums[((long long)p.w * a.samples + p.b) * a.groups + (p.c + j) / a.per_group];
-        m1[j] = m.x, m2[j] = m.y;
-    }
-    const T *x = a.x + p.w * a.xs.worker + p.b * a.xs.sample + p.c, *dy = a.dy + p.w * a.dys.worker + p.b * a.dys.sample + p.c;
-    T *y = a.y + p.w * a.ys.worker + p.b * a.ys.sample + p.c;
-    const long long e0 = (long long)p.b * a.pixels * a.channels + p.c;
-    for (long long i = p.first + p.ty; i < p.last; i += p.rows) {
-        float f[V], d[V];
-        Vec<T, V> vx(x + i * a.xs.pixel), vd(dy + i * a.dys.pixel);
-        vx.floats(f), vd.floats(d);
-        const uint32_t keep = counted<V, DROP>(f, a.draw, words, e0 + i * a.channels);
+            for (int u = 0; u < U; ++u)
+                if (i + u * p.rows < p.last) vx[u] = Vec<T, V>(x + u * p.rows * a.xs.pixel), vd[u] = Vec<T, V>(dy + u * p.rows * a.dys.pixel);
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const float h = (f[j] - k.mean[j]) * k.rstd[j], dz = slope_times(d[j], fmaf(h, k.weight[j], k.bias[j]), a.act);
-            f[j] = k.rstd[j] * (fmaf(dz, k.weight[j], -m1[j]) - h * m2[j]);
-            if (DROP) f[j] = keep >> j & 1 ? f[j] * a.draw.factor : 0.f;
+            for (int u = 0; u < U; ++u)
+                if (i + u * p.rows < p.last) {
+                    const uint32_t keep = DROP ? drop_out(vx[u], a.draw, words, element(a, p, i + u * p.rows)) : 0;
+                    make_grad<T, V, DROP, decltype(act)::value>(vx[u], k, scale, m1, m2, vd[u], a.draw.factor, keep);
+                    vx[u].to(y + u * p.rows * a.ys.pixel);
+                }
         }
-        vx.round(f);
-        vx.to(y + i * a.ys.pixel);
-    }
+    });
 }
