@@ -305,6 +305,12 @@ struct cser_norm {
     float *part = nullptr;                             // two planes of channels' sums
     float2 *group_sums = nullptr;
     long long plane = 0;
+    struct Fit {                                       // clusters that the GPU holds at a time
+        const void *kernel = nullptr;
+        int log_cluster = 0, log_block = 0, clusters = 0;
+        size_t shared = 0;
+    } fits[4];
+    unsigned next_fit = 0;
 };
 
 namespace {
@@ -358,47 +364,71 @@ template <typename T, typename F> int with_vector(int v, F f) {
     return v == 2 ? f(std::integral_constant<int, 2>()) : f(std::integral_constant<int, 1>());
 }
 
-constexpr int kSharedAimed = 36 << 10;
 // How a call is made in one walk, with v elements a vector; false: it does not fit, or vectors are too short for asynchronous copies.
-// Slices of 128 bytes of a pixel, or of 64 or 32 where wider ones do not fit a cluster or would leave SMs idle.
+// Clusters cost more than narrow slices: the fewest blocks that hold a slice of 64 bytes of a pixel at two blocks to an SM, then of 32, then at
+// one to an SM (8 x 16 x 56 x 56 x 256 in bf16, forward: 64 bytes by 2 blocks 86 us, 128 by 4 96, 128 by 8 at four to an SM 100, 32 by one
+// 106; gradient 133 by 4 and 156 of 128 bytes by 8).  Blocks of 256 threads, or of 128 where four fit an SM (28 x 28 x 256 forward 89 and
+// 115 us).  Few units are spread over more blocks, at four pixels a thread and more.
 bool plan_resident(const cser_norm *h, const cser_norm_inputs *in, int v, bool two, Resident &r, size_t &shared) {
     const int size = size_of(h->type), per_group = (int)(h->channels / h->groups);
     if (v * size < 4) return false;
     const long long least = std::lcm(per_group, v) / v, all = h->channels / v, samples = (long long)h->n * in->samples;
-    if (least > kBlock) return false;
     bool found = false;
-    for (bool last : {false, true}) {
-        for (int bytes : {128, 64, 32}) {
-            Resident k{};
-            k.sv = (int)std::min(all, least * ceil_div(bytes, least * v * size));
-            if (k.sv > kBlock) continue;
-            while (1 << k.log_tx < k.sv) ++k.log_tx;
-            const int rows = kBlock >> k.log_tx;
-            const long long slices = ceil_div(all, k.sv);
-            auto cut = [&](int log_cluster) {
-                k.log_cluster = log_cluster, k.per = (int)ceil_div(in->pixels, 1 << log_cluster);
-                k.slots = (int)std::min(ceil_div(k.per, rows), 1ll << 16);
-                return resident_shared(k, v, size, two, two && h->drop);
+    for (size_t most : {size_t(112) << 10, size_t(220) << 10}) {
+        for (int bytes : {64, 32}) {
+            r = Resident{};
+            r.fold = std::gcd(per_group, v);
+            const long long vectors = std::min(all, least * ceil_div(bytes, least * v * size)), slices = ceil_div(all, vectors);
+            if (vectors > 128 || samples * slices > kMostBlocks / 8) continue;
+            r.sv = (int)vectors, r.slices = (uint32_t)slices, r.units = (uint32_t)(samples * slices);
+            while (1 << r.log_tx < r.sv) ++r.log_tx;
+            auto cut = [&](int log_cluster) {          // by so many blocks: bytes of shared memory of one
+                r.log_cluster = log_cluster, r.per = (int)ceil_div(in->pixels, 1 << log_cluster);
+                for (r.log_block = 7;; ++r.log_block) {
+                    const long long slots = ceil_div(r.per, (1 << r.log_block) >> r.log_tx);
+                    if (slots > 1 << 16) return ~size_t(0);
+                    r.slots = (int)slots, shared = resident_shared(r, v, size, two, two && h->drop);
+                    if (r.log_block == 8 || shared <= size_t(55) << 10) return shared;
+                }
             };
             int c = 0;
-            while (c < 3 && cut(c) > (size_t)kSharedAimed) ++c;
-            if (cut(c) > (size_t)(last ? 220 << 10 : 112 << 10) || samples << c > kMostBlocks || slices > 65535) continue;
-            while ((samples * slices << k.log_cluster) < kBusy / 4 && c < 3 && k.per >= 4 * rows) cut(++c);
-            r = k, found = true;
-            if (samples * slices * 8 >= kBusy / 4) break;
+            while (cut(c) > most && c < 3) ++c;
+            if (shared > most) continue;
+            while (r.units << r.log_cluster < kBusy / 4 && c < 3 && r.per >= 4 * ((1 << r.log_block) >> r.log_tx)) cut(++c);
+            found = true;
+            break;
         }
         if (found) break;
     }
     if (!found) return false;
-    r.fold = std::gcd(per_group, v), r.log_sub = 0;
     const int entries = two ? per_group : (per_group / r.fold) << r.log_cluster;
     while (r.log_sub < 5 && 1 << r.log_sub < entries) ++r.log_sub;
     r.group_magic = per_group == 1 ? 0 : (uint32_t)(((1ull << 32) + per_group - 1) / per_group);
-    shared = resident_shared(r, v, size, two, two && h->drop);
     return true;
 }
-template <typename T> dim3 resident_grid(const NormArgs<T> &a, const Resident &r, int v) {
-    return dim3((unsigned)(a.n * a.samples) << r.log_cluster, (unsigned)ceil_div(a.channels / v, r.sv));
+// The call's launch: as many clusters as the GPU holds at a time, or as there are units.  How many that is is asked once for a kernel and a
+// shape.
+template <typename T>
+int resident_launch(cser_norm *h, void (*kernel)(NormArgs<T>, Resident), const NormArgs<T> &a, const Resident &r, size_t shared, cudaStream_t st) {
+    cser_norm::Fit *fit = nullptr;
+    for (auto &f : h->fits)
+        if (f.kernel == (const void *)kernel && f.log_cluster == r.log_cluster && f.log_block == r.log_block && f.shared == shared) fit = &f;
+    if (!fit) {
+        fit = &h->fits[h->next_fit++ % 4];
+        cudaLaunchConfig_t cfg{};
+        cfg.gridDim = dim3(1u << r.log_cluster), cfg.blockDim = dim3(1u << r.log_block), cfg.dynamicSmemBytes = shared;
+        cudaLaunchAttribute at[1];
+        at[0].id = cudaLaunchAttributeClusterDimension;
+        at[0].val.clusterDim.x = 1u << r.log_cluster, at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+        cfg.attrs = at, cfg.numAttrs = 1;
+        fit->kernel = nullptr;
+        TRY(cudaOccupancyMaxActiveClusters(&fit->clusters, kernel, &cfg));
+        fit->kernel = (const void *)kernel, fit->log_cluster = r.log_cluster, fit->log_block = r.log_block, fit->shared = shared;
+    }
+    const uint32_t clusters = std::min<uint32_t>(r.units, std::max(fit->clusters, 1));
+    TRY(launch(kernel, dim3(clusters << r.log_cluster), 1u << r.log_block, shared, 1u << r.log_cluster, st, a, r));
+    h->launches++;
+    return CSER_OK;
 }
 
 template <typename T> int norm_apply(cser_norm *h, const cser_norm_inputs *in, const cser_pixels *y, float *stats, cudaStream_t st) {
@@ -412,10 +442,7 @@ template <typename T> int norm_apply(cser_norm *h, const cser_norm_inputs *in, c
             Resident r;
             size_t shared;
             if (plan_resident(h, in, V, false, r, shared)) {
-                TRY(launch(h->drop ? norm_resident_kernel<T, V, true> : norm_resident_kernel<T, V, false>, resident_grid(a, r, V), kBlock, shared,
-                           1 << r.log_cluster, st, a, r));
-                h->launches++;
-                return CSER_OK;
+                return resident_launch<T>(h, h->drop ? norm_resident_kernel<T, V, true> : norm_resident_kernel<T, V, false>, a, r, shared, st);
             }
         }
         if (!cut(a, V, true, grid)) return fail(CSER_ERR_INVALID, "cser_norm_apply: too many elements");
@@ -444,15 +471,15 @@ int norm_grad(cser_norm *h, const cser_norm_inputs *in, const float *stats, cons
             size_t shared;
             if (plan_resident(h, in, V, true, r, shared)) {
                 a.part = dweight || dbias ? h->part : nullptr, a.chunks = 1, done = true;
-                TRY(launch(h->drop ? norm_grad_resident_kernel<T, V, true> : norm_grad_resident_kernel<T, V, false>, resident_grid(a, r, V), kBlock,
-                           shared, 1 << r.log_cluster, st, a, r));
+                if (int rc = resident_launch<T>(h, h->drop ? norm_grad_resident_kernel<T, V, true> : norm_grad_resident_kernel<T, V, false>, a, r, shared, st))
+                    return rc;
             }
         }
         if (!done) {
             if (!cut(a, V, true, grid)) return fail(CSER_ERR_INVALID, "cser_norm_grad: too many elements");
             TRY(launch(h->drop ? norm_grad_sums_kernel<T, V, true> : norm_grad_sums_kernel<T, V, false>, dim3(grid), 256, 0, 1, st, a));
+            h->launches++;
         }
-        h->launches++;
         if (dweight || dbias) {
             RowSums s{};
             s.part = a.part, s.plane = a.plane, s.rows = (long long)a.samples * a.chunks, s.cols = a.channels;

@@ -82,17 +82,14 @@ __device__ __forceinline__ void join_moments(float &n, float &mean, float &m2, f
     n = total;
 }
 
-// Moments of a thread's V channels.  Values are taken kBatch at a time relative to the first of them, which keeps sums of squares from
-// cancelling: that value is one of the set, so what is subtracted is at most kBatch times what is left, wherever the mean is.
-constexpr int kBatch = 32;
-template <int V> struct Moments {
-    float n = 0.f;
-    F2 mean[kPairs<V>], m2[kPairs<V>];
+// Sums of a few values of each of V channels, relative to the first of them, which keeps sums of squares from cancelling: that value is one of
+// the set, so what is subtracted is at most as many times what is left as there are values, wherever the mean is.
+template <int V> struct Batch {
     F2 first[kPairs<V>], sum[kPairs<V>], squares[kPairs<V>];
 
-    __device__ __forceinline__ Moments() {
+    __device__ __forceinline__ Batch() {
 #pragma unroll
-        for (int j = 0; j < kPairs<V>; ++j) mean[j] = m2[j] = two(0.f);
+        for (int j = 0; j < kPairs<V>; ++j) first[j] = sum[j] = squares[j] = two(0.f);
     }
     __device__ __forceinline__ void begin(const F2 (&f)[kPairs<V>]) {
 #pragma unroll
@@ -105,35 +102,32 @@ template <int V> struct Moments {
             sum[j] = sum[j] + d, squares[j] = fma2(d, d, squares[j]);
         }
     }
-    // The batch had `count` values, the first among them.
+    // Mean and sum of squares about it of `count` values, in the places of first and squares.
     __device__ __forceinline__ void end(int count) {
-        const float total = n + count, share = count / total, part = 1.f / count;
+        const float part = count ? 1.f / count : 0.f;
 #pragma unroll
         for (int j = 0; j < kPairs<V>; ++j) {
-            const F2 s = sum[j] * two(part), d = first[j] + s - mean[j], q = fma2(sum[j], s * two(-1.f), squares[j]);
-            mean[j] = fma2(d, two(share), mean[j]);
-            m2[j] = m2[j] + q + d * d * two(n * share);
-        }
-        n = total;
-    }
-    // Joins the sets of the threads of a warp whose lanes differ in bits `span` and above; all end with the same bits.
-    __device__ __forceinline__ void join_lanes(int span) {
-        for (int o = span; o < 32; o <<= 1) {
-            const float n2 = __shfl_xor_sync(~0u, n, o), total = n + n2;
-            const bool upper = threadIdx.x & o;                                     // the lower lane's set comes first in both
-            const float share = total == 0.f ? 0.f : (upper ? n : n2) / total, weight = (upper ? n2 : n) * share;
-#pragma unroll
-            for (int j = 0; j < kPairs<V>; ++j) {
-                const F2 other = {__shfl_xor_sync(~0u, mean[j].x, o), __shfl_xor_sync(~0u, mean[j].y, o)};
-                const F2 q = {__shfl_xor_sync(~0u, m2[j].x, o), __shfl_xor_sync(~0u, m2[j].y, o)};
-                const F2 low = upper ? other : mean[j], d = (upper ? mean[j] : other) - low;
-                mean[j] = fma2(d, two(share), low);
-                m2[j] = m2[j] + q + d * d * two(weight);
-            }
-            n = total;
+            const F2 s = sum[j] * two(part);
+            first[j] = first[j] + s, squares[j] = fma2(sum[j], s * two(-1.f), squares[j]);
         }
     }
 };
+
+// Joins sets of N means and sums of squares, n * fold values behind each, of the threads of a warp whose lanes differ in bits `span` and above.
+template <int N> __device__ __forceinline__ void join_lanes(float &n, float (&mean)[N], float (&m2)[N], int fold, int span) {
+    for (int o = span; o < 32; o <<= 1) {
+        const float n2 = __shfl_xor_sync(~0u, n, o), total = n + n2;
+        const bool upper = threadIdx.x & o;                                         // the lower lane's set comes first in both
+        const float share = total == 0.f ? 0.f : __fdividef(upper ? n : n2, total), weight = fold * (upper ? n2 : n) * share;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const float other = __shfl_xor_sync(~0u, mean[j], o), q = __shfl_xor_sync(~0u, m2[j], o);
+            const float low = upper ? other : mean[j], d = (upper ? mean[j] : other) - low;
+            mean[j] = fmaf(d, share, low), m2[j] = fmaf(d * d, weight, m2[j] + q);
+        }
+        n = total;
+    }
+}
 
 // Drops out what a worker's array has from element e on: dropped elements become 0, others stay (times the factor later); keep bits.
 template <typename T, int V> __device__ __forceinline__ uint32_t drop_out(Vec<T, V> &v, const Draw &draw, const Words &words, long long e) {
@@ -156,28 +150,28 @@ template <typename T, int V, bool DROP> __device__ __forceinline__ void counted(
     }
 }
 
-// A thread's channels.  xhat = x * rstd + offset: one rounding more than (x - mean) rstd, of the size of that of the mean.
+// A thread's channels: z = x * scale + shift.  (One rounding more than (x - mean) rstd weight + bias has, of the size of that of the mean.)
 template <int V> struct Channels {
-    F2 rstd[kPairs<V>], offset[kPairs<V>], weight[kPairs<V>], bias[kPairs<V>];
+    F2 scale[kPairs<V>], shift[kPairs<V>], minus_mean[kPairs<V>];
 };
 template <typename T, int V> __device__ __forceinline__ void channels_of(Channels<V> &k, const NormArgs<T> &a, int w, int b, int c) {
     const float *means = a.stats + ((long long)w * a.samples + b) * a.groups, *rstds = means + (long long)a.n * a.samples * a.groups;
-    float v[4][2 * kPairs<V>] = {};
+    float v[3][2 * kPairs<V>] = {};
 #pragma unroll
     for (int j = 0; j < V; ++j) {
         const int g = (c + j) / a.per_group;
-        v[0][j] = rstds[g], v[1][j] = -means[g] * v[0][j];
-        v[2][j] = a.weight ? a.weight[w * a.weight_worker + c + j] : 1.f;
-        v[3][j] = a.bias ? a.bias[w * a.bias_worker + c + j] : 0.f;
+        v[2][j] = -means[g];
+        v[0][j] = rstds[g] * (a.weight ? a.weight[w * a.weight_worker + c + j] : 1.f);
+        v[1][j] = fmaf(v[2][j], v[0][j], a.bias ? a.bias[w * a.bias_worker + c + j] : 0.f);
     }
 #pragma unroll
     for (int j = 0; j < kPairs<V>; ++j) {
-        k.rstd[j] = {v[0][2 * j], v[0][2 * j + 1]}, k.offset[j] = {v[1][2 * j], v[1][2 * j + 1]};
-        k.weight[j] = {v[2][2 * j], v[2][2 * j + 1]}, k.bias[j] = {v[3][2 * j], v[3][2 * j + 1]};
+        k.scale[j] = {v[0][2 * j], v[0][2 * j + 1]}, k.shift[j] = {v[1][2 * j], v[1][2 * j + 1]};
+        k.minus_mean[j] = {v[2][2 * j], v[2][2 * j + 1]};
     }
 }
 
-// Sums dz and dz * xhat of a vector.
+// Sums dz and dz * (x - mean) of a vector.
 template <typename T, int V, bool DROP, int ACT>
 __device__ __forceinline__ void add_grad(F2 (&s0)[kPairs<V>], F2 (&s1)[kPairs<V>], const Channels<V> &k, const Vec<T, V> &vx, const Vec<T, V> &vd,
                                          float factor) {
@@ -186,21 +180,21 @@ __device__ __forceinline__ void add_grad(F2 (&s0)[kPairs<V>], F2 (&s1)[kPairs<V>
     pairs_of(vd, d);
 #pragma unroll
     for (int j = 0; j < kPairs<V>; ++j) {
-        const F2 h = fma2(f[j], k.rstd[j], k.offset[j]), dz = slope_times<ACT>(d[j], fma2(h, k.weight[j], k.bias[j]));
-        s0[j] = s0[j] + dz, s1[j] = fma2(dz, h, s1[j]);
+        const F2 dz = slope_times<ACT>(d[j], fma2(f[j], k.scale[j], k.shift[j]));
+        s0[j] = s0[j] + dz, s1[j] = fma2(dz, f[j] + k.minus_mean[j], s1[j]);
     }
 }
-// dx of a vector, into vx.  scale = rstd * weight, m1 = -rstd s1 / N, m2 = -rstd s2 / N.
+// dx of a vector, into vx: dz * scale + x * m2 + m1, with m2 = -rstd^2 s2 / N and m1 = -rstd s1 / N - mean m2.
 template <typename T, int V, bool DROP, int ACT>
-__device__ __forceinline__ void make_grad(Vec<T, V> &vx, const Channels<V> &k, const F2 (&scale)[kPairs<V>], const F2 (&m1)[kPairs<V>],
+__device__ __forceinline__ void make_grad(Vec<T, V> &vx, const F2 (&scale)[kPairs<V>], const F2 (&shift)[kPairs<V>], const F2 (&m1)[kPairs<V>],
                                           const F2 (&m2)[kPairs<V>], const Vec<T, V> &vd, float factor, uint32_t keep) {
     F2 f[kPairs<V>], d[kPairs<V>];
     counted<T, V, DROP>(f, vx, factor);
     pairs_of(vd, d);
 #pragma unroll
     for (int j = 0; j < kPairs<V>; ++j) {
-        const F2 h = fma2(f[j], k.rstd[j], k.offset[j]), dz = slope_times<ACT>(d[j], fma2(h, k.weight[j], k.bias[j]));
-        f[j] = fma2(h, m2[j], fma2(dz, scale[j], m1[j]));
+        const F2 dz = slope_times<ACT>(d[j], fma2(f[j], scale[j], shift[j]));
+        f[j] = fma2(dz, scale[j], fma2(f[j], m2[j], m1[j]));
         if (DROP) f[j] = {keep >> 2 * j & 1 ? f[j].x * factor : 0.f, keep >> (2 * j + 1) & 1 ? f[j].y * factor : 0.f};
     }
     round_pairs(vx, f);
@@ -235,7 +229,7 @@ template <typename T> __device__ __forceinline__ T *at_pixel(T *p, const View &v
 template <typename T> __device__ __forceinline__ long long element(const NormArgs<T> &a, const Place &s, long long i) {
     return (s.b * a.pixels + i) * a.channels + s.c;
 }
-constexpr int kTogether = 4;                           // pixels whose loads are under way together
+constexpr int kTogether = 4, kBatch = 32;              // pixels whose loads are under way together; and whose moments are taken together
 
 // Moments of each channel over a chunk of a sample's pixels: plane 0 the mean, plane 1 the sum of squares about it.
 template <typename T, int V, bool DROP>
@@ -244,10 +238,23 @@ __global__ void __launch_bounds__(256) norm_moments_kernel(NormArgs<T> a) {
     let_next();
     const Place p = place<T, V>(a);
     const Words words(a.draw, p.w);
-    Moments<V> m;
+    float n = 0.f, mean[V], m2[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) mean[j] = m2[j] = 0.f;
     if (p.in) {
         const T *x = at_pixel(a.x, a.xs, p, p.first + p.ty);
-        int got = 0;                                   // of the batch
+        Batch<V> m;
+        int got = 0;
+        auto join = [&] {
+            m.end(got);
+            const float total = n + got, share = got / total;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const float d = (j & 1 ? m.first[j / 2].y : m.first[j / 2].x) - mean[j];
+                mean[j] = fmaf(d, share, mean[j]), m2[j] = fmaf(d * d, n * share, m2[j] + (j & 1 ? m.squares[j / 2].y : m.squares[j / 2].x));
+            }
+            n = total, got = 0;
+        };
         for (long long i = p.first + p.ty; i < p.last; i += kTogether * p.rows, x += kTogether * p.rows * a.xs.pixel) {
             Vec<T, V> v[kTogether];
 #pragma unroll
@@ -263,21 +270,18 @@ __global__ void __launch_bounds__(256) norm_moments_kernel(NormArgs<T> a) {
                     m.add(f);
                     ++got;
                 }
-            if (got + kTogether > kBatch) m.end(got), got = 0;
+            if (got == kBatch) join();
         }
-        if (got) m.end(got);
+        if (got) join();
     }
     // Threads of the same channels: those of a warp, then the eight warps.
-    m.join_lanes(a.tx);
+    join_lanes(n, mean, m2, 1, a.tx);
     __shared__ float count[8][32], means[8][32 * V], squares[8][32 * V];
     const int warp = threadIdx.x >> 5, tx = threadIdx.x & (a.tx - 1);
     if ((threadIdx.x & 31) < a.tx) {
-        count[warp][tx] = m.n;
+        count[warp][tx] = n;
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            means[warp][tx * V + j] = j & 1 ? m.mean[j / 2].y : m.mean[j / 2].x;
-            squares[warp][tx * V + j] = j & 1 ? m.m2[j / 2].y : m.m2[j / 2].x;
-        }
+        for (int j = 0; j < V; ++j) means[warp][tx * V + j] = mean[j], squares[warp][tx * V + j] = m2[j];
     }
     __syncthreads();
     const int k = threadIdx.x, c = (blockIdx.x % a.col_blocks) * a.tx * V + k;
@@ -324,9 +328,6 @@ __global__ void __launch_bounds__(256) norm_apply_kernel(NormArgs<T> a) {
     const Words words(a.draw, p.w);
     Channels<V> k;
     channels_of(k, a, p.w, p.b, p.c);
-    F2 scale[kPairs<V>], shift[kPairs<V>];
-#pragma unroll
-    for (int j = 0; j < kPairs<V>; ++j) scale[j] = k.rstd[j] * k.weight[j], shift[j] = fma2(k.offset[j], k.weight[j], k.bias[j]);
     const T *x = at_pixel(a.x, a.xs, p, p.first + p.ty);
     T *y = at_pixel(a.y, a.ys, p, p.first + p.ty);
     with_act(a.act, [&](auto act) {
@@ -342,7 +343,7 @@ __global__ void __launch_bounds__(256) norm_apply_kernel(NormArgs<T> a) {
                     F2 f[kPairs<V>];
                     counted<T, V, DROP>(f, v[u], a.draw.factor);
 #pragma unroll
-                    for (int j = 0; j < kPairs<V>; ++j) f[j] = activate<decltype(act)::value>(fma2(f[j], scale[j], shift[j]));
+                    for (int j = 0; j < kPairs<V>; ++j) f[j] = activate<decltype(act)::value>(fma2(f[j], k.scale[j], k.shift[j]));
                     round_pairs(v[u], f);
                     v[u].to(y + u * p.rows * a.ys.pixel);
                 }
@@ -397,8 +398,8 @@ __global__ void __launch_bounds__(256) norm_grad_sums_kernel(NormArgs<T> a) {
         float u0 = 0.f, u1 = 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) u0 += sums[0][i][k], u1 += sums[1][i][k];
-        const long long at = (((long long)p.w * a.samples + p.b) * a.chunks + p.chunk) * a.channels + c;
-        a.part[at] = u0, a.part[a.plane + at] = u1;
+        const long long sample = (long long)p.w * a.samples + p.b, at = (sample * a.chunks + p.chunk) * a.channels + c;
+        a.part[at] = u0, a.part[a.plane + at] = u1 * a.stats[((long long)a.n * a.samples + sample) * a.groups + c / a.per_group];
     }
 }
 
@@ -425,17 +426,6 @@ template <typename T> __global__ void __launch_bounds__(256) norm_join_sums_kern
     if (lane == 0) a.group_sums[g] = make_float2(s0 * of, s1 * of);
 }
 
-// Factors of make_grad for a thread's channels, from its groups' s1 / N and s2 / N.
-template <int V, typename F>
-__device__ __forceinline__ void grad_factors(F2 (&scale)[kPairs<V>], F2 (&m1)[kPairs<V>], F2 (&m2)[kPairs<V>], const Channels<V> &k, F sums) {
-#pragma unroll
-    for (int j = 0; j < kPairs<V>; ++j) {
-        const float2 a = sums(2 * j), b = 2 * j + 1 < V ? sums(2 * j + 1) : make_float2(0.f, 0.f);
-        scale[j] = k.rstd[j] * k.weight[j];
-        m1[j] = k.rstd[j] * F2{-a.x, -b.x}, m2[j] = k.rstd[j] * F2{-a.y, -b.y};
-    }
-}
-
 template <typename T, int V, bool DROP>
 __global__ void __launch_bounds__(256) norm_grad_apply_kernel(NormArgs<T> a) {
     after_previous();
@@ -445,8 +435,20 @@ __global__ void __launch_bounds__(256) norm_grad_apply_kernel(NormArgs<T> a) {
     const Words words(a.draw, p.w);
     Channels<V> k;
     channels_of(k, a, p.w, p.b, p.c);
-    F2 scale[kPairs<V>], m1[kPairs<V>], m2[kPairs<V>];
-    grad_factors<V>(scale, m1, m2, k, [&](int j) { return a.group_sums[((long long)p.w * a.samples + p.b) * a.groups + (p.c + j) / a.per_group]; });
+    F2 m1[kPairs<V>], m2[kPairs<V>];
+    {
+        const long long group0 = ((long long)p.w * a.samples + p.b) * a.groups;
+        float v[2][2 * kPairs<V>] = {};
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const int g = (p.c + j) / a.per_group;
+            const float rstd = a.stats[(long long)a.n * a.samples * a.groups + group0 + g];
+            const float2 sums = a.group_sums[group0 + g];
+            v[1][j] = -rstd * rstd * sums.y, v[0][j] = fmaf(-a.stats[group0 + g], v[1][j], -rstd * sums.x);
+        }
+#pragma unroll
+        for (int j = 0; j < kPairs<V>; ++j) m1[j] = {v[0][2 * j], v[0][2 * j + 1]}, m2[j] = {v[1][2 * j], v[1][2 * j + 1]};
+    }
     const T *x = at_pixel(a.x, a.xs, p, p.first + p.ty), *dy = at_pixel(a.dy, a.dys, p, p.first + p.ty);
     T *y = at_pixel(a.y, a.ys, p, p.first + p.ty);
     constexpr int U = 2;
@@ -461,7 +463,7 @@ __global__ void __launch_bounds__(256) norm_grad_apply_kernel(NormArgs<T> a) {
             for (int u = 0; u < U; ++u)
                 if (i + u * p.rows < p.last) {
                     const uint32_t keep = DROP ? drop_out(vx[u], a.draw, words, element(a, p, i + u * p.rows)) : 0;
-                    make_grad<T, V, DROP, decltype(act)::value>(vx[u], k, scale, m1, m2, vd[u], a.draw.factor, keep);
+                    make_grad<T, V, DROP, decltype(act)::value>(vx[u], k.scale, k.shift, m1, m2, vd[u], a.draw.factor, keep);
                     vx[u].to(y + u * p.rows * a.ys.pixel);
                 }
         }

@@ -8,14 +8,14 @@
 // are made from the slots.  Each element crosses HBM once in each direction, where separate kernels for sums and results read twice.
 #pragma once
 
-constexpr int kBlock = 128, kLogBlock = 7;           // threads
+constexpr int kMostThreads = 256;
 struct Resident {
-    int sv, log_tx, log_cluster, slots;                // sv: vectors of a slice; slots: of a thread and array
+    int sv, log_tx, log_block, log_cluster, slots;     // sv: vectors of a slice; log_block: threads; slots: of a thread and array
     int fold, log_sub;                                 // neighbouring channels of a vector that share a group; lanes of a group's sums
     uint32_t group_magic;                              // 2^32 / channels of a group, rounded up; 0 for one
     int per;                                           // pixels of a block
+    uint32_t slices, units;                            // of a sample, and of all
 };
-// Grid: x: blocks of a cluster for each sample, y: slices.
 
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
@@ -34,39 +34,41 @@ template <int BYTES> __device__ __forceinline__ void copy_async(void *to, const 
 }
 __device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
-// Where a thread stands, and its parts of the block's shared memory.
+// Where a thread stands, and its parts of the block's shared memory.  `here` and what comes before it change with the unit.
 template <typename T, int V> struct Stand {
     typedef typename Vec<T, V>::raw raw;
-    int w, b, sample, rank, c0, tx, ty, log_rows, here, mine;        // c0: the slice's first channel; here: its channels; mine: pixels of this thread
-    int first, last;
-    bool in;
-    raw *x, *dy;                                       // its slots, kBlock apart
-    uint8_t *keep;                                     // keep bits of its slots, kBlock apart
-    float *coef, *red, *all;                           // six planes for channels, rows of sums of two planes, two planes of each block of the cluster
+    int w, b, sample, c0, mine, here;                  // c0: the slice's first channel; mine: pixels of this thread; here: channels of the slice
+    int rank, tx, ty, log_rows, warps, first, last, pixels;          // pixels: of this thread, where its channels exist
+    raw *x, *dy;                                       // its slots, as far apart as there are threads
+    uint8_t *keep;                                     // keep bits of its slots, likewise
+    float *coef, *red, *all;                           // six planes for channels, rows of sums of two planes, twice two planes of each block of the cluster
 
     __device__ __forceinline__ Stand(const NormArgs<T> &a, const Resident &r, unsigned char *shared, bool two, bool bits) {
-        rank = blockIdx.x & ((1 << r.log_cluster) - 1), sample = blockIdx.x >> r.log_cluster;
-        w = (unsigned)sample / (unsigned)a.samples, b = sample - w * a.samples;
-        c0 = blockIdx.y * r.sv * V;
-        here = a.channels - c0 < r.sv * V ? a.channels - c0 : r.sv * V;
-        log_rows = kLogBlock - r.log_tx;
+        rank = blockIdx.x & ((1 << r.log_cluster) - 1);
+        log_rows = r.log_block - r.log_tx, warps = 1 << (r.log_block - 5);
         tx = threadIdx.x & ((1 << r.log_tx) - 1), ty = threadIdx.x >> r.log_tx;
-        in = tx * V < here;
         const long long begin = (long long)rank * r.per;
         first = begin < a.pixels ? (int)begin : (int)a.pixels, last = begin + r.per < a.pixels ? (int)begin + r.per : (int)a.pixels;
         const int left = last - first - ty;
-        mine = in && left > 0 ? (left + (1 << log_rows) - 1) >> log_rows : 0;
+        pixels = left > 0 ? (left + (1 << log_rows) - 1) >> log_rows : 0;
         x = reinterpret_cast<raw *>(shared) + threadIdx.x;
-        dy = x + (two ? r.slots * kBlock : 0);
-        unsigned char *rest = shared + (size_t)r.slots * kBlock * sizeof(raw) * (two ? 2 : 1);
+        dy = x + (two ? r.slots << r.log_block : 0);
+        unsigned char *rest = shared + ((size_t)r.slots << r.log_block) * sizeof(raw) * (two ? 2 : 1);
         keep = rest + threadIdx.x;
-        if (bits) rest += r.slots * kBlock;
+        if (bits) rest += r.slots << r.log_block;
         coef = reinterpret_cast<float *>(rest);
         red = coef + 6 * width();
         all = red + 2 * sum_rows() * width();
     }
-    __device__ __forceinline__ int width() const { return (kBlock >> log_rows) * V; }        // channels of a row of sums
-    __device__ __forceinline__ int sum_rows() const { return log_rows < kLogBlock - 5 ? 1 << log_rows : kBlock / 32; }
+    __device__ __forceinline__ void go(const NormArgs<T> &a, const Resident &r, uint32_t unit) {
+        sample = unit / r.slices;
+        c0 = (unit - sample * r.slices) * r.sv * V;
+        w = (uint32_t)sample / (uint32_t)a.samples, b = sample - w * a.samples;
+        here = min(a.channels - c0, r.sv * V);
+        mine = tx * V < here ? pixels : 0;
+    }
+    __device__ __forceinline__ int width() const { return (warps * 32 >> log_rows) * V; }        // channels of a row of sums
+    __device__ __forceinline__ int sum_rows() const { return min(1 << log_rows, warps); }
     __device__ __forceinline__ long long step(const View &v) const { return v.pixel << log_rows; }
     template <typename U> __device__ __forceinline__ U *at(U *p, const View &v) const {
         return p + w * v.worker + b * v.sample + (first + ty) * v.pixel + c0 + tx * V;
@@ -84,13 +86,14 @@ template <typename T, int V> struct Stand {
 };
 // Bytes of shared memory of the above.
 inline size_t resident_shared(const Resident &r, int v, int size, bool two, bool bits) {
-    const int width = (1 << r.log_tx) * v, rows = std::min(kBlock >> r.log_tx, kBlock / 32);
-    return (size_t)r.slots * kBlock * (v * size * (two ? 2 : 1) + (bits ? 1 : 0)) + (size_t)(6 + 2 * rows + (2 << r.log_cluster)) * width * 4;
+    const int width = (1 << r.log_tx) * v, rows = std::min(1 << (r.log_block - r.log_tx), 1 << (r.log_block - 5));
+    const size_t sums = width / (two ? 1 : r.fold);
+    return ((size_t)r.slots << r.log_block) * (v * size * (two ? 2 : 1) + (bits ? 1 : 0)) + (size_t)(6 + 2 * rows) * width * 4 + (4 << r.log_cluster) * sums * 4;
 }
 
 // Leaves a thread's N sums (lanes joined already) for the block: row of sums, two planes.
-template <int N> __device__ __forceinline__ void leave_row(float *red, int log_tx, int log_rows, const float (&p)[N], const float (&q)[N]) {
-    const int sums = N << log_tx, rows = min(kBlock >> log_tx, kBlock / 32), row = log_tx > 5 ? threadIdx.x >> log_tx : threadIdx.x >> 5;
+template <int N> __device__ __forceinline__ void leave_row(float *red, int log_tx, const float (&p)[N], const float (&q)[N]) {
+    const int sums = N << log_tx, rows = min((int)blockDim.x >> log_tx, (int)blockDim.x / 32), row = log_tx > 5 ? threadIdx.x >> log_tx : threadIdx.x >> 5;
     if (log_tx >= 5 || (threadIdx.x & 31) < 1 << log_tx) {
         float *a = red + row * sums + (threadIdx.x & ((1 << log_tx) - 1)) * N, *b = a + rows * sums;
 #pragma unroll
@@ -135,8 +138,8 @@ template <int U, int V, typename T, typename L, typename F> __device__ __forcein
     }
 }
 
-// Forward: moments of the parts of a group that a thread's vector holds, FOLD channels each, over the lanes, the block and the cluster.
-template <int FOLD, int V> __device__ __forceinline__ void fold_moments(float (&mean)[V / FOLD], float (&m2)[V / FOLD], const Moments<V> &m) {
+// Forward: moments of the parts of a group that a thread's vector holds, FOLD channels each of n values.
+template <int FOLD, int V> __device__ __forceinline__ void fold_moments(float (&mean)[V / FOLD], float (&m2)[V / FOLD], const Batch<V> &m, float n) {
     constexpr float kOf = 1.f / FOLD;
 #pragma unroll
     for (int i = 0; i < V / FOLD; ++i) {
@@ -144,27 +147,13 @@ template <int FOLD, int V> __device__ __forceinline__ void fold_moments(float (&
 #pragma unroll
         for (int j = 0; j < FOLD; ++j) {
             const int c = i * FOLD + j;
-            f[j] = c & 1 ? m.mean[c / 2].y : m.mean[c / 2].x;
-            sum += f[j], squares += c & 1 ? m.m2[c / 2].y : m.m2[c / 2].x;
+            f[j] = c & 1 ? m.first[c / 2].y : m.first[c / 2].x;
+            sum += f[j], squares += c & 1 ? m.squares[c / 2].y : m.squares[c / 2].x;
         }
         mean[i] = sum * kOf;
 #pragma unroll
         for (int j = 0; j < FOLD; ++j) off = fmaf(f[j] - mean[i], f[j] - mean[i], off);
-        m2[i] = fmaf(m.n, off, squares);
-    }
-}
-template <int N> __device__ __forceinline__ void join_lanes(float &n, float (&mean)[N], float (&m2)[N], int fold, int span) {
-    for (int o = span; o < 32; o <<= 1) {
-        const float n2 = __shfl_xor_sync(~0u, n, o), total = n + n2;
-        const bool upper = threadIdx.x & o;                                         // the lower lane's set comes first in both
-        const float share = total == 0.f ? 0.f : __fdividef(upper ? n : n2, total), weight = fold * (upper ? n2 : n) * share;
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-            const float other = __shfl_xor_sync(~0u, mean[j], o), q = __shfl_xor_sync(~0u, m2[j], o);
-            const float low = upper ? other : mean[j], d = (upper ? mean[j] : other) - low;
-            mean[j] = fmaf(d, share, low), m2[j] = fmaf(d * d, weight, m2[j] + q);
-        }
-        n = total;
+        m2[i] = fmaf(n, off, squares);
     }
 }
 // f(FOLD as a constant), for the powers of two up to V.
@@ -180,54 +169,57 @@ template <int V, typename F> __device__ __forceinline__ void with_fold(int fold,
 }
 
 template <typename T, int V, bool DROP>
-__global__ void __launch_bounds__(kBlock) norm_resident_kernel(NormArgs<T> a, Resident r) {
+__global__ void __launch_bounds__(kMostThreads) norm_resident_kernel(NormArgs<T> a, Resident r) {
     extern __shared__ __align__(16) unsigned char shared[];
     if (r.log_cluster) cluster_arrive();
     after_previous();
     let_next();
-    const Stand<T, V> s(a, r, shared, false, false);
+    Stand<T, V> s(a, r, shared, false, false);
     const int width = s.width(), lane = threadIdx.x & 31;
+    const uint32_t clusters = gridDim.x >> r.log_cluster;
+    uint32_t unit = blockIdx.x >> r.log_cluster;
+    s.go(a, r, unit);
     {
         const T *x = s.at(a.x, a.xs);
         const long long step = s.step(a.xs);
-        for (int u = 0; u < s.mine; ++u, x += step) copy_async<V * sizeof(T)>(s.x + u * kBlock, x);
+        for (int u = 0; u < s.mine; ++u, x += step) copy_async<V * sizeof(T)>(s.x + (u << r.log_block), x);
     }
-    for (int c = threadIdx.x; c < s.here; c += kBlock) {               // planes 2 and 3: weight and bias
+    if (r.log_cluster) cluster_wait();                 // all blocks are there
+    float *all = s.all;
+    for (;;) {
+    for (int c = threadIdx.x; c < s.here; c += s.warps * 32) {               // planes 2 and 3: weight and bias
         s.coef[2 * width + c] = a.weight ? a.weight[s.w * a.weight_worker + s.c0 + c] : 1.f;
         s.coef[3 * width + c] = a.bias ? a.bias[s.w * a.bias_worker + s.c0 + c] : 0.f;
     }
     const Words words(a.draw, s.w);
-    Moments<V> m;
+    Batch<V> m;
     const long long e0 = ((long long)s.b * a.pixels + s.first + s.ty) * a.channels + s.c0 + s.tx * V, e_step = (long long)a.channels << s.log_rows;
     copies_done();
-    for (int u0 = 0; u0 < s.mine; u0 += kBatch) {
-        const int u1 = u0 + kBatch < s.mine ? u0 + kBatch : s.mine;
-        walk_slots<DROP ? 2 : 4, V, T>(u0, u1, [&](int u) { return s.x[u * kBlock]; }, [&](int u, Vec<T, V> &v) {
-            if (DROP) {                                // dropped elements become 0 in their slot
-                drop_out(v, a.draw, words, e0 + u * e_step);
-                s.x[u * kBlock] = v.bits;
-            }
-            F2 f[kPairs<V>];
-            counted<T, V, DROP>(f, v, a.draw.factor);
-            if (u == u0) m.begin(f);
-            m.add(f);
-        });
-        m.end(u1 - u0);
-    }
+    walk_slots<DROP ? 2 : 4, V, T>(0, s.mine, [&](int u) { return s.x[(u << r.log_block)]; }, [&](int u, Vec<T, V> &v) {
+        if (DROP) {                                    // dropped elements become 0 in their slot
+            drop_out(v, a.draw, words, e0 + u * e_step);
+            s.x[(u << r.log_block)] = v.bits;
+        }
+        F2 f[kPairs<V>];
+        counted<T, V, DROP>(f, v, a.draw.factor);
+        if (u == 0) m.begin(f);
+        m.add(f);
+    });
+    m.end(s.mine);
     // Threads of the same channels: those of a warp, then rows of the block, of which each warp (or part of one) has left one, ...
     with_fold<V>(r.fold, [&](auto fold) {
         constexpr int kFold = decltype(fold)::value;
         float mean[V / kFold], m2[V / kFold];
-        fold_moments<kFold, V>(mean, m2, m);
-        join_lanes(m.n, mean, m2, kFold, 1 << r.log_tx);
-        leave_row(s.red, r.log_tx, s.log_rows, mean, m2);
+        float n = (float)s.mine;
+        fold_moments<kFold, V>(mean, m2, m, n);
+        join_lanes(n, mean, m2, kFold, 1 << r.log_tx);
+        leave_row(s.red, r.log_tx, mean, m2);
     });
     __syncthreads();
     const int sums = width / r.fold, sum_rows = s.sum_rows(), block_pixels = s.last - s.first, each = (1 << s.log_rows) / sum_rows;
     const int whole = (block_pixels >> s.log_rows) * each, rest = block_pixels & ((1 << s.log_rows) - 1), mine = s.here / r.fold;
     const float of_block = block_pixels ? 1.f / block_pixels : 0.f;
-    if (r.log_cluster) cluster_wait();                 // all blocks are there
-    for (int k = threadIdx.x; k < mine; k += kBlock) {
+    for (int k = threadIdx.x; k < mine; k += s.warps * 32) {
         // Pixels of the threads i * each .. i * each + each - 1 of a column: each of them takes every rows-th.
         auto count = [&](int i) { return (float)(whole + min(max(rest - i * each, 0), each)); };
         float sum = 0.f, squares = 0.f, off = 0.f;
@@ -237,18 +229,18 @@ __global__ void __launch_bounds__(kBlock) norm_resident_kernel(NormArgs<T> a, Re
             const float d = s.red[i * sums + k] - mean;
             off = fmaf(count(i) * d, d, off), squares += s.red[(sum_rows + i) * sums + k];
         }
-        tell_all(r, s.all, s.rank, sums, k, mean, fmaf((float)r.fold, off, squares));
+        tell_all(r, all, s.rank, sums, k, mean, fmaf((float)r.fold, off, squares));
     }
     meet(r);
     // ... then the blocks of the cluster and the parts of a group, by 2^log_sub lanes a group.
     const int parts = a.per_group / r.fold, groups = s.here / a.per_group, g0 = s.c0 / a.per_group;
     const float of_group = 1.f / ((float)a.pixels * a.per_group);
-    for (int base = threadIdx.x >> 5 << (5 - r.log_sub); base < groups; base += kBlock >> r.log_sub) {
+    for (int base = threadIdx.x >> 5 << (5 - r.log_sub); base < groups; base += (s.warps * 32) >> r.log_sub) {
         const int g = base + (lane >> r.log_sub), sub = lane & ((1 << r.log_sub) - 1), entries = g < groups ? parts << r.log_cluster : 0;
         auto values = [&](int i, float &pixels, float &mean, float &m2) {
             const int rank = i & ((1 << r.log_cluster) - 1), k = g * parts + (i >> r.log_cluster);
             pixels = (float)(r.fold * min(max((int)a.pixels - rank * r.per, 0), r.per));
-            mean = s.all[2 * rank * sums + k], m2 = s.all[(2 * rank + 1) * sums + k];
+            mean = all[2 * rank * sums + k], m2 = all[(2 * rank + 1) * sums + k];
         };
         float sum = 0.f, squares = 0.f, p, q, v;
         for (int i = sub; i < entries; i += 1 << r.log_sub) values(i, p, q, v), sum = fmaf(p, q, sum);
@@ -267,13 +259,21 @@ __global__ void __launch_bounds__(kBlock) norm_resident_kernel(NormArgs<T> a, Re
         }
     }
     __syncthreads();
+    // The next unit's vectors take the places of this one's as soon as these have been used.
+    Stand<T, V> next = s;
+    unit += clusters;
+    const bool more = unit < r.units;
+    if (more) next.go(a, r, unit);
+    const int coming = more ? next.mine : 0;
+    const T *x = next.at(a.x, a.xs);
+    const long long x_step = s.step(a.xs);
     if (s.mine) {
         F2 scale[kPairs<V>], shift[kPairs<V>];
         s.channels(scale, 0), s.channels(shift, 1);
         T *y = s.at(a.y, a.ys);
         const long long step = s.step(a.ys);
         with_act(a.act, [&](auto act) {
-            walk_slots<4, V, T>(0, s.mine, [&](int u) { return s.x[u * kBlock]; }, [&](int, Vec<T, V> &v) {
+            walk_slots<4, V, T>(0, s.mine, [&](int u) { return s.x[(u << r.log_block)]; }, [&](int u, Vec<T, V> &v) {
                 F2 f[kPairs<V>];
                 pairs_of(v, f);
 #pragma unroll
@@ -281,35 +281,50 @@ __global__ void __launch_bounds__(kBlock) norm_resident_kernel(NormArgs<T> a, Re
                 round_pairs(v, f);
                 v.to(y);
                 y += step;
+                if (u < coming) copy_async<V * sizeof(T)>(s.x + (u << r.log_block), x);
+                x += x_step;
             });
         });
+    }
+    if (!more) return;
+    for (int u = s.mine; u < coming; ++u, x += x_step) copy_async<V * sizeof(T)>(s.x + (u << r.log_block), x);
+    s = next;
+    // The block that is behind may still read the sums of this unit, but not those of the one before: they are two.
+    all = all == s.all ? s.all + (2 << r.log_cluster) * sums : s.all;
     }
 }
 
 template <typename T, int V, bool DROP>
-__global__ void __launch_bounds__(kBlock) norm_grad_resident_kernel(NormArgs<T> a, Resident r) {
+__global__ void __launch_bounds__(kMostThreads) norm_grad_resident_kernel(NormArgs<T> a, Resident r) {
     extern __shared__ __align__(16) unsigned char shared[];
     if (r.log_cluster) cluster_arrive();
     after_previous();
     let_next();
-    const Stand<T, V> s(a, r, shared, true, DROP);
+    Stand<T, V> s(a, r, shared, true, DROP);
     const int width = s.width(), lane = threadIdx.x & 31;
+    const uint32_t clusters = gridDim.x >> r.log_cluster;
+    uint32_t unit = blockIdx.x >> r.log_cluster;
+    s.go(a, r, unit);
     {
         const T *x = s.at(a.x, a.xs), *dy = s.at(a.dy, a.dys);
         const long long x_step = s.step(a.xs), dy_step = s.step(a.dys);
         for (int u = 0; u < s.mine; ++u, x += x_step, dy += dy_step) {
-            copy_async<V * sizeof(T)>(s.x + u * kBlock, x);
-            copy_async<V * sizeof(T)>(s.dy + u * kBlock, dy);
+            copy_async<V * sizeof(T)>(s.x + (u << r.log_block), x);
+            copy_async<V * sizeof(T)>(s.dy + (u << r.log_block), dy);
         }
     }
-    // Planes: xhat = x * [0] + [1], z = xhat * [2] + [3].  With a dropout [0] carries its factor.
-    for (int c = threadIdx.x; c < s.here; c += kBlock) {
+    if (r.log_cluster) cluster_wait();                 // all blocks are there
+    float *all = s.all;
+    for (;;) {
+    // Planes: z = x * [0] + [1], [2] = -mean, [3] = rstd.
+    for (int c = threadIdx.x; c < s.here; c += s.warps * 32) {
         const int g = r.group_magic ? __umulhi(s.c0 + c, r.group_magic) : s.c0 + c;
         const long long at = (long long)s.sample * a.groups + g;
         const float mean = a.stats[at], rstd = a.stats[(long long)a.n * a.samples * a.groups + at];
-        s.coef[c] = DROP ? rstd * a.draw.factor : rstd, s.coef[width + c] = -mean * rstd;
-        s.coef[2 * width + c] = a.weight ? a.weight[s.w * a.weight_worker + s.c0 + c] : 1.f;
-        s.coef[3 * width + c] = a.bias ? a.bias[s.w * a.bias_worker + s.c0 + c] : 0.f;
+        const float scale = a.weight ? rstd * a.weight[s.w * a.weight_worker + s.c0 + c] : rstd;
+        s.coef[c] = scale;
+        s.coef[width + c] = fmaf(-mean, scale, a.bias ? a.bias[s.w * a.bias_worker + s.c0 + c] : 0.f);
+        s.coef[2 * width + c] = -mean, s.coef[3 * width + c] = rstd;
     }
     const Words words(a.draw, s.w);
     Channels<V> k;
@@ -318,17 +333,17 @@ __global__ void __launch_bounds__(kBlock) norm_grad_resident_kernel(NormArgs<T> 
     for (int j = 0; j < kPairs<V>; ++j) s0[j] = s1[j] = two(0.f);
     copies_done();
     __syncthreads();
-    s.channels(k.rstd, 0), s.channels(k.offset, 1), s.channels(k.weight, 2), s.channels(k.bias, 3);
+    s.channels(k.scale, 0), s.channels(k.shift, 1), s.channels(k.minus_mean, 2);
     const long long e0 = ((long long)s.b * a.pixels + s.first + s.ty) * a.channels + s.c0 + s.tx * V, e_step = (long long)a.channels << s.log_rows;
     with_act(a.act, [&](auto act) {
-        walk_slots<2, V, T>(0, s.mine, [&](int u) { return s.x[u * kBlock]; }, [&](int u, Vec<T, V> &vx) {
+        walk_slots<2, V, T>(0, s.mine, [&](int u) { return s.x[(u << r.log_block)]; }, [&](int u, Vec<T, V> &vx) {
             Vec<T, V> vd;
-            vd.bits = s.dy[u * kBlock];
+            vd.bits = s.dy[(u << r.log_block)];
             if (DROP) {
-                s.keep[u * kBlock] = (uint8_t)drop_out(vx, a.draw, words, e0 + u * e_step);
-                s.x[u * kBlock] = vx.bits;
+                s.keep[(u << r.log_block)] = (uint8_t)drop_out(vx, a.draw, words, e0 + u * e_step);
+                s.x[(u << r.log_block)] = vx.bits;
             }
-            add_grad<T, V, false, decltype(act)::value>(s0, s1, k, vx, vd, 1.f);
+            add_grad<T, V, DROP, decltype(act)::value>(s0, s1, k, vx, vd, a.draw.factor);
         });
     });
     float t0[V], t1[V];
@@ -337,61 +352,76 @@ __global__ void __launch_bounds__(kBlock) norm_grad_resident_kernel(NormArgs<T> 
     for (int o = 1 << r.log_tx; o < 32; o <<= 1)
 #pragma unroll
         for (int j = 0; j < V; ++j) t0[j] += __shfl_xor_sync(~0u, t0[j], o), t1[j] += __shfl_xor_sync(~0u, t1[j], o);
-    leave_row(s.red, r.log_tx, s.log_rows, t0, t1);
+    leave_row(s.red, r.log_tx, t0, t1);
     __syncthreads();
     const int sum_rows = s.sum_rows();
-    if (r.log_cluster) cluster_wait();                 // all blocks are there
-    for (int c = threadIdx.x; c < s.here; c += kBlock) {
+    for (int c = threadIdx.x; c < s.here; c += s.warps * 32) {
         float p = 0.f, q = 0.f;
         for (int i = 0; i < sum_rows; ++i) p += s.red[i * width + c], q += s.red[(sum_rows + i) * width + c];
-        tell_all(r, s.all, s.rank, width, c, p, q);
+        tell_all(r, all, s.rank, width, c, p, q);
     }
     meet(r);
-    // Sums over the cluster; of a channel they are the sample's share of dbias and dweight (each block writes some channels'), times the weight
-    // of its group's s1 and s2, which planes 4 and 5 take.
-    for (int c = threadIdx.x; c < s.here; c += kBlock) {
+    // Sums over the cluster; of a channel they are the sample's share of dbias and dweight (each block writes some channels').  Times the
+    // channel's rstd and weight, planes 4 and 5 take them for its group's s1 and s2.
+    for (int c = threadIdx.x; c < s.here; c += s.warps * 32) {
         float p = 0.f, q = 0.f;
-        for (int i = 0; i < 1 << r.log_cluster; ++i) p += s.all[2 * i * width + c], q += s.all[(2 * i + 1) * width + c];
+        for (int i = 0; i < 1 << r.log_cluster; ++i) p += all[2 * i * width + c], q += all[(2 * i + 1) * width + c];
+        q *= s.coef[3 * width + c];
         if (a.part && (c & ((1 << r.log_cluster) - 1)) == s.rank) {
             const long long at = (long long)s.sample * a.channels + s.c0 + c;
             a.part[at] = p, a.part[a.plane + at] = q;
         }
-        s.coef[4 * width + c] = p * s.coef[2 * width + c], s.coef[5 * width + c] = q * s.coef[2 * width + c];
+        s.coef[4 * width + c] = p * s.coef[c], s.coef[5 * width + c] = q * s.coef[c];
     }
-    if (!a.y) return;
+    // The next unit's vectors take the places of this one's as soon as these have been used.
+    Stand<T, V> next = s;
+    unit += clusters;
+    const bool more = unit < r.units;
+    if (more) next.go(a, r, unit);
+    const int coming = more ? next.mine : 0;
+    const T *x = next.at(a.x, a.xs), *dy = next.at(a.dy, a.dys);
+    const long long x_step = s.step(a.xs), dy_step = s.step(a.dys);
+    int used = 0;                                      // slots that are on their way
     __syncthreads();
-    // The first two rows of sums, which all have read, become planes for -rstd s1 / N and -rstd s2 / N, with dx's own factor of a dropout in rstd.
-    const int groups = s.here / a.per_group;
-    const float of = -1.f / ((float)a.pixels * a.per_group);
-    for (int base = threadIdx.x >> 5 << (5 - r.log_sub); base < groups; base += kBlock >> r.log_sub) {
-        const int g = base + (lane >> r.log_sub), sub = lane & ((1 << r.log_sub) - 1), end = g < groups ? (g + 1) * a.per_group : 0;
-        float p = 0.f, q = 0.f;
-        for (int c = g * a.per_group + sub; c < end; c += 1 << r.log_sub) p += s.coef[4 * width + c], q += s.coef[5 * width + c];
-        p = lanes_sum(p, r.log_sub) * of, q = lanes_sum(q, r.log_sub) * of;
-        for (int c = g * a.per_group + sub; c < end; c += 1 << r.log_sub) s.red[c] = s.coef[c] * p, s.red[width + c] = s.coef[c] * q;
-    }
-    __syncthreads();
-    if (s.mine) {
-        F2 scale[kPairs<V>], m1[kPairs<V>], m2[kPairs<V>];
+    if (a.y) {
+        // The first two rows of sums, which all have read, become planes for make_grad's m1 and m2.
+        const int groups = s.here / a.per_group;
+        const float of = -1.f / ((float)a.pixels * a.per_group);
+        for (int base = threadIdx.x >> 5 << (5 - r.log_sub); base < groups; base += (s.warps * 32) >> r.log_sub) {
+            const int g = base + (lane >> r.log_sub), sub = lane & ((1 << r.log_sub) - 1), end = g < groups ? (g + 1) * a.per_group : 0;
+            float p = 0.f, q = 0.f;
+            for (int c = g * a.per_group + sub; c < end; c += 1 << r.log_sub) p += s.coef[4 * width + c], q += s.coef[5 * width + c];
+            p = lanes_sum(p, r.log_sub) * of, q = lanes_sum(q, r.log_sub) * of;
+            for (int c = g * a.per_group + sub; c < end; c += 1 << r.log_sub) {
+                const float m2 = q * s.coef[3 * width + c];
+                s.red[c] = fmaf(s.coef[2 * width + c], m2, p), s.red[width + c] = m2;
+            }
+        }
+        __syncthreads();
+        F2 m1[kPairs<V>], m2[kPairs<V>];
         s.channels(m1, 6), s.channels(m2, 7);
-#pragma unroll
-        for (int j = 0; j < kPairs<V>; ++j) scale[j] = k.rstd[j] * k.weight[j];
         T *y = s.at(a.y, a.ys);
         const long long step = s.step(a.ys);
         with_act(a.act, [&](auto act) {
-            walk_slots<2, V, T>(0, s.mine, [&](int u) { return s.x[u * kBlock]; }, [&](int u, Vec<T, V> &vx) {
+            walk_slots<2, V, T>(0, s.mine, [&](int u) { return s.x[(u << r.log_block)]; }, [&](int u, Vec<T, V> &vx) {
                 Vec<T, V> vd;
-                vd.bits = s.dy[u * kBlock];
-                make_grad<T, V, false, decltype(act)::value>(vx, k, scale, m1, m2, vd, 1.f, 0);
-                if (DROP) {
-                    const uint32_t keep = s.keep[u * kBlock];
-#pragma unroll
-                    for (int j = 0; j < V; ++j)
-                        if (!(keep >> j & 1)) vx.at[j] = from_float<T>(0.f);
-                }
+                vd.bits = s.dy[(u << r.log_block)];
+                make_grad<T, V, DROP, decltype(act)::value>(vx, k.scale, k.shift, m1, m2, vd, a.draw.factor, DROP ? s.keep[(u << r.log_block)] : 0);
                 vx.to(y);
                 y += step;
+                if (u < coming) copy_async<V * sizeof(T)>(s.x + (u << r.log_block), x), copy_async<V * sizeof(T)>(s.dy + (u << r.log_block), dy);
+                x += x_step, dy += dy_step;
             });
         });
+        used = s.mine;
+    }
+    if (!more) return;
+    for (int u = used; u < coming; ++u, x += x_step, dy += dy_step) {
+        copy_async<V * sizeof(T)>(s.x + (u << r.log_block), x);
+        copy_async<V * sizeof(T)>(s.dy + (u << r.log_block), dy);
+    }
+    s = next;
+    // The block that is behind may still read the sums of this unit, but not those of the one before: they are two.
+    all = all == s.all ? s.all + (2 << r.log_cluster) * width : s.all;
     }
 }
