@@ -357,6 +357,13 @@ template <typename T> bool cut(NormArgs<T> &a, int v, bool sums, unsigned &grid)
     return others * a.chunks <= kMostBlocks;
 }
 
+// Threads that join the parts of a group: eight parts each, if that many are.
+template <typename T> unsigned join_threads(const NormArgs<T> &a) {
+    unsigned k = 32;
+    while (k < 1024 && k * 8ll < (long long)a.chunks * a.per_group) k *= 2;
+    return k;
+}
+
 // Calls f with the kernel's vector length as a constant.
 template <typename T, typename F> int with_vector(int v, F f) {
     if (sizeof(T) == 2 && v == 8) return f(std::integral_constant<int, 16 / sizeof(T)>());
@@ -374,8 +381,11 @@ bool plan_resident(const cser_norm *h, const cser_norm_inputs *in, int v, bool t
     if (v * size < 4) return false;
     const long long least = std::lcm(per_group, v) / v, all = h->channels / v, samples = (long long)h->n * in->samples;
     bool found = false;
+    // 64 bytes, or more where a unit would be less than 16 KB and there are enough.
+    long long widest = 64;
+    while (widest < 4096 && widest * in->pixels < 16 << 10 && samples * ceil_div(h->channels * size, 2 * widest) >= kBusy / 2) widest *= 2;
     for (size_t most : {size_t(112) << 10, size_t(220) << 10}) {
-        for (int bytes : {64, 32}) {
+        for (long long bytes : {widest, 32ll}) {
             r = Resident{};
             r.fold = std::gcd(per_group, v);
             const long long vectors = std::min(all, least * ceil_div(bytes, least * v * size)), slices = ceil_div(all, vectors);
@@ -447,7 +457,7 @@ template <typename T> int norm_apply(cser_norm *h, const cser_norm_inputs *in, c
         }
         if (!cut(a, V, true, grid)) return fail(CSER_ERR_INVALID, "cser_norm_apply: too many elements");
         TRY(launch(h->drop ? norm_moments_kernel<T, V, true> : norm_moments_kernel<T, V, false>, dim3(grid), 256, 0, 1, st, a));
-        TRY(launch(norm_join_moments_kernel<T>, dim3((unsigned)ceil_div((long long)a.n * a.samples * a.groups, 8)), 256, 0, 1, st, a));
+        TRY(launch(norm_join_moments_kernel<T>, dim3((unsigned)(a.n * a.samples * a.groups)), join_threads(a), 0, 1, st, a));
         if (!cut(a, V, false, grid)) return fail(CSER_ERR_INVALID, "cser_norm_apply: too many elements");
         TRY(launch(h->drop ? norm_apply_kernel<T, V, true> : norm_apply_kernel<T, V, false>, dim3(grid), 256, 0, 1, st, a));
         h->launches += 3;
@@ -487,7 +497,7 @@ int norm_grad(cser_norm *h, const cser_norm_inputs *in, const float *stats, cons
             if (int rc = launch_row_sums(s, a.n, 2, h->launches, st)) return rc;
         }
         if (!dx || done) return CSER_OK;
-        TRY(launch(norm_join_sums_kernel<T>, dim3((unsigned)ceil_div((long long)a.n * a.samples * a.groups, 8)), 256, 0, 1, st, a));
+        TRY(launch(norm_join_sums_kernel<T>, dim3((unsigned)(a.n * a.samples * a.groups)), join_threads(a), 0, 1, st, a));
         if (!cut(a, V, false, grid)) return fail(CSER_ERR_INVALID, "cser_norm_grad: too many elements");
         TRY(launch(h->drop ? norm_grad_apply_kernel<T, V, true> : norm_grad_apply_kernel<T, V, false>, dim3(grid), 256, 0, 1, st, a));
         h->launches += 2;

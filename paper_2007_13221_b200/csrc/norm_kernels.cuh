@@ -294,29 +294,48 @@ __global__ void __launch_bounds__(256) norm_moments_kernel(NormArgs<T> a) {
     }
 }
 
-// Mean and rstd of each group from its channels' moments: a warp a group.
-template <typename T> __global__ void __launch_bounds__(256) norm_join_moments_kernel(NormArgs<T> a) {
+// Sum over a block of whole warps, for all of its threads.
+__device__ __forceinline__ float block_sum(float v) {
+    __shared__ float sums[32];
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(~0u, v, o);
+    if (blockDim.x == 32) return v;
+    if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = (threadIdx.x & 31) < blockDim.x / 32 ? sums[threadIdx.x & 31] : 0.f;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(~0u, v, o);
+    __syncthreads();
+    return v;
+}
+// What a group's parts are: f(where, chunk, channel of the group) for a thread's share of them.
+template <typename T, typename F> __device__ __forceinline__ void group_parts(const NormArgs<T> &a, long long group, F f) {
+    const long long base = group / a.groups * a.chunks * a.channels + (group % a.groups) * a.per_group;
+    for (int i = threadIdx.x; i < a.chunks * a.per_group; i += blockDim.x) {
+        const int chunk = i / a.per_group, c = i - chunk * a.per_group;
+        f(base + (long long)chunk * a.channels + c, chunk, c);
+    }
+}
+
+// Mean and rstd of each group from its channels' moments: a block a group.
+template <typename T> __global__ void __launch_bounds__(1024) norm_join_moments_kernel(NormArgs<T> a) {
     after_previous();
     let_next();
-    const long long g = (long long)blockIdx.x * 8 + (threadIdx.x >> 5), all = (long long)a.n * a.samples * a.groups;
-    if (g >= all) return;
-    const int lane = threadIdx.x & 31;
-    const long long sample = g / a.groups;
-    const float *part = a.part + sample * a.chunks * a.channels + (g % a.groups) * a.per_group;
-    const int entries = a.chunks * a.per_group;
-    float n = 0.f, mean = 0.f, m2 = 0.f;
-    for (int i = lane; i < entries; i += 32) {
-        const int chunk = i / a.per_group, c = i % a.per_group;
+    const long long g = blockIdx.x;
+    auto pixels = [&](int chunk) {
         const long long left = a.pixels - chunk * a.chunk_pixels;
-        const float count = (float)(left < a.chunk_pixels ? left : a.chunk_pixels);
-        const long long at = (long long)chunk * a.channels + c;
-        join_moments(n, mean, m2, count, part[at], part[a.plane + at]);
-    }
-    for (int o = 1; o < 32; o <<= 1) {
-        const float n2 = __shfl_down_sync(~0u, n, o), mean2 = __shfl_down_sync(~0u, mean, o), m22 = __shfl_down_sync(~0u, m2, o);
-        join_moments(n, mean, m2, n2, mean2, m22);     // lane 0 joins disjoint sets: what it adds has not been added by others
-    }
-    if (lane == 0) a.stats[g] = mean, a.stats[all + g] = 1.f / sqrtf(m2 / n + a.eps);
+        return (float)(left < a.chunk_pixels ? left : a.chunk_pixels);
+    };
+    float sum = 0.f, squares = 0.f;
+    const float of = 1.f / ((float)a.pixels * a.per_group);
+    group_parts(a, g, [&](long long at, int chunk, int) { sum = fmaf(pixels(chunk), a.part[at], sum); });
+    const float mean = block_sum(sum) * of;
+    group_parts(a, g, [&](long long at, int chunk, int) {
+        const float d = a.part[at] - mean;
+        squares = fmaf(pixels(chunk) * d, d, squares + a.part[a.plane + at]);
+    });
+    squares = block_sum(squares) * of;
+    if (threadIdx.x == 0) a.stats[g] = mean, a.stats[(long long)a.n * a.samples * a.groups + g] = 1.f / sqrtf(squares + a.eps);
 }
 
 template <typename T, int V, bool DROP>
@@ -403,27 +422,20 @@ __global__ void __launch_bounds__(256) norm_grad_sums_kernel(NormArgs<T> a) {
     }
 }
 
-// s1 / N and s2 / N of each group: a warp a group.
-template <typename T> __global__ void __launch_bounds__(256) norm_join_sums_kernel(NormArgs<T> a) {
+// s1 / N and s2 / N of each group: a block a group.
+template <typename T> __global__ void __launch_bounds__(1024) norm_join_sums_kernel(NormArgs<T> a) {
     after_previous();
     let_next();
-    const long long g = (long long)blockIdx.x * 8 + (threadIdx.x >> 5), all = (long long)a.n * a.samples * a.groups;
-    if (g >= all) return;
-    const int lane = threadIdx.x & 31;
-    const long long sample = g / a.groups;
-    const int c0 = (int)(g % a.groups) * a.per_group, w = (int)(sample / a.samples);
-    const float *part = a.part + sample * a.chunks * a.channels + c0;
-    const int entries = a.chunks * a.per_group;
+    const long long g = blockIdx.x;
+    const int w = (int)(g / a.groups / a.samples), c0 = (int)(g % a.groups) * a.per_group;
     float s0 = 0.f, s1 = 0.f;
-    for (int i = lane; i < entries; i += 32) {
-        const int chunk = i / a.per_group, c = i % a.per_group;
+    group_parts(a, g, [&](long long at, int, int c) {
         const float k = a.weight ? a.weight[w * a.weight_worker + c0 + c] : 1.f;
-        const long long at = (long long)chunk * a.channels + c;
-        s0 = fmaf(part[at], k, s0), s1 = fmaf(part[a.plane + at], k, s1);
-    }
-    for (int o = 16; o; o >>= 1) s0 += __shfl_xor_sync(~0u, s0, o), s1 += __shfl_xor_sync(~0u, s1, o);
+        s0 = fmaf(a.part[at], k, s0), s1 = fmaf(a.part[a.plane + at], k, s1);
+    });
+    s0 = block_sum(s0), s1 = block_sum(s1);
     const float of = 1.f / ((float)a.pixels * a.per_group);
-    if (lane == 0) a.group_sums[g] = make_float2(s0 * of, s1 * of);
+    if (threadIdx.x == 0) a.group_sums[g] = make_float2(s0 * of, s1 * of);
 }
 
 template <typename T, int V, bool DROP>
