@@ -349,7 +349,7 @@ template <typename T> NormArgs<T> norm_args(const cser_norm *h, const cser_norm_
 template <typename T> bool cut(NormArgs<T> &a, int v, bool sums, unsigned &grid) {
     column_blocks(a.channels, v, a.tx, a.col_blocks);
     const long long others = (long long)a.n * a.samples * a.col_blocks;
-    const long long most = ceil_div(a.pixels, 4 * (256 / a.tx)), want = sums ? ceil_div(kBusy, (long long)a.n * a.samples) : ceil_div(4 * kBusy, others);
+    const long long most = ceil_div(a.pixels, 4 * (256 / a.tx)), want = sums ? ceil_div(kBusy / 2, (long long)a.n * a.samples) : ceil_div(kBusy, others);
     const long long chunks = most < want ? most : want;
     a.chunk_pixels = ceil_div(a.pixels, chunks);
     a.chunks = (int)ceil_div(a.pixels, a.chunk_pixels);

@@ -11,7 +11,7 @@ import ctypes
 
 import torch
 
-from .binding import CSERError, _check, _release, _stream, cser_last_error
+from .binding import CSERError, _check, _release, cser_last_error
 from .binding import lib as _base_lib
 from .train import TYPES, _on, _want
 
@@ -86,9 +86,20 @@ def _params(name, t, n, cols):
     """(pointer, worker stride) of an fp32 [n, cols] tensor or None."""
     if t is None:
         return None, 0
-    if not (t.is_cuda and t.dtype == torch.float32 and t.dim() == 2 and t.shape[0] == n and t.shape[1] == cols and (t.stride(1) == 1 or cols == 1)):
+    stride = t.stride()
+    if not (t.dtype is torch.float32 and t.shape == (n, cols) and (stride[1] == 1 or cols == 1) and t.is_cuda):
         raise CSERError(f"{name} must be a CUDA float32 tensor of shape {(n, cols)} with a contiguous last dimension")
-    return t.data_ptr(), t.stride(0)
+    return t.data_ptr(), stride[0]
+
+
+def _like(t):
+    """A dense tensor of t's shape and type."""
+    return torch.empty_like(t) if t.is_contiguous() else torch.empty_like(t, memory_format=torch.contiguous_format)
+
+
+def _raw_stream(t):
+    """The current stream of t's device."""
+    return torch._C._cuda_getCurrentRawStream(t.get_device())
 
 
 class _Handle:
@@ -131,6 +142,10 @@ class Dropout(_Handle):
 
     def _array(self, name, t, like=None):
         shape = t.shape
+        if (t.dtype is self.dtype and t.is_contiguous() and t.is_cuda and
+                (shape == like.shape if like is not None else len(shape) >= 2 and shape[0] == self.n and shape[-1] == self.cols)):
+            each = t.numel() // self.n                    # the ordinary case, without its strides
+            return each // self.cols, _Rows(t.data_ptr(), self.cols, each)
         if not (t.is_cuda and t.dtype == self.dtype and t.dim() >= 2 and shape[0] == self.n and shape[-1] == self.cols and
                 (like is None or shape == like.shape)):
             raise CSERError(f"Dropout: {name} must be a CUDA {self.dtype} tensor of shape " +
@@ -152,9 +167,11 @@ class Dropout(_Handle):
         b, b_stride = _params("Dropout: bias", bias, self.n, self.cols)
         rs = None if residual is None else self._array("residual", residual, x)[1]
         if out is None:
-            out = torch.empty_like(x, memory_format=torch.contiguous_format)
+            out = _like(x)
         ys = self._array("out", out, x)[1]
-        _check(_lib.cser_drop_apply(self.h, rows, step, step_at, xs, b, b_stride, rs, ys, _stream()), "cser_drop_apply")
+        rc = _lib.cser_drop_apply(self.h, rows, step, step_at, xs, b, b_stride, rs, ys, _raw_stream(x))
+        if rc:
+            _check(rc, "cser_drop_apply")
         return out
 
     def grad(self, dy, step, dx=None, dbias=None, need_dx=True, need_dbias=False, stream=None):
@@ -167,12 +184,12 @@ class Dropout(_Handle):
         xs = None
         if need_dx:
             if dx is None:
-                dx = torch.empty_like(dy, memory_format=torch.contiguous_format)
+                dx = _like(dy)
             xs = self._array("dx", dx, dy)[1]
         if dbias is None and need_dbias:
             dbias = torch.empty((self.n, self.cols), dtype=torch.float32, device=dy.device)
         b, b_stride = _params("Dropout: dbias", dbias, self.n, self.cols)
-        _check(_lib.cser_drop_grad(self.h, rows, step, step_at, ds, xs, b, b_stride, _stream()), "cser_drop_grad")
+        _check(_lib.cser_drop_grad(self.h, rows, step, step_at, ds, xs, b, b_stride, _raw_stream(dy)), "cser_drop_grad")
         return dx if need_dx else None, dbias
 
 
@@ -199,6 +216,12 @@ class GroupNorm(_Handle):
 
     def _array(self, name, t, like=None):
         shape = t.shape
+        if (t.dtype is self.dtype and t.is_contiguous() and t.is_cuda and
+                (shape == like.shape if like is not None else len(shape) >= 3 and shape[0] == self.n and shape[-1] == self.channels)):
+            each = t.numel() // self.n                    # the ordinary case, without its strides
+            sample = each // shape[1] if each else 0
+            if each or shape[1] == 0:
+                return sample // self.channels, _Pixels(t.data_ptr(), self.channels, sample, each)
         if not (t.is_cuda and t.dtype == self.dtype and t.dim() >= 3 and shape[0] == self.n and shape[-1] == self.channels and
                 (like is None or shape == like.shape)):
             raise CSERError(f"GroupNorm: {name} must be a CUDA {self.dtype} tensor of shape " +
@@ -222,10 +245,10 @@ class GroupNorm(_Handle):
             return _on(stream, self.apply, x, weight, bias, step, out)
         args = self._inputs(x, weight, bias, step)
         if out is None:
-            out = torch.empty_like(x, memory_format=torch.contiguous_format)
+            out = _like(x)
         ys = self._array("out", out, x)[1]
         stats = torch.empty((2, self.n, x.shape[1], self.groups), dtype=torch.float32, device=x.device)
-        _check(_lib.cser_norm_apply(self.h, args, ys, stats.data_ptr(), _stream()), "cser_norm_apply")
+        _check(_lib.cser_norm_apply(self.h, args, ys, stats.data_ptr(), _raw_stream(x)), "cser_norm_apply")
         return out, stats
 
     def grad(self, x, dy, stats, weight=None, bias=None, step=0, dx=None, dweight=None, dbias=None, need_dx=True, need_params=True,
@@ -242,7 +265,7 @@ class GroupNorm(_Handle):
         xs = None
         if need_dx:
             if dx is None:
-                dx = torch.empty_like(x, memory_format=torch.contiguous_format)
+                dx = _like(x)
             xs = self._array("dx", dx, x)[1]
         if need_params:
             if dweight is None:
@@ -253,5 +276,5 @@ class GroupNorm(_Handle):
             b, b_stride = _params("GroupNorm: dbias", dbias, self.n, self.channels)
         else:
             dweight, dbias, w, w_stride, b, b_stride = None, None, None, 0, None, 0
-        _check(_lib.cser_norm_grad(self.h, args, stats.data_ptr(), ds, xs, w, w_stride, b, b_stride, _stream()), "cser_norm_grad")
+        _check(_lib.cser_norm_grad(self.h, args, stats.data_ptr(), ds, xs, w, w_stride, b, b_stride, _raw_stream(x)), "cser_norm_grad")
         return dx if need_dx else None, dweight, dbias
