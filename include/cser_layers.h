@@ -42,8 +42,8 @@ typedef struct cser_rows {
 
 /*
  * Handle for up to max_rows rows a worker.  0 <= p < 1 (and floor(p * 2^32) < 2^32); 1 <= site < 2^20: one number for each place of the
- * model that drops; first_worker >= 0 and first_worker + n_workers <= 4096; max_rows * cols <= 2^34; n_workers * max_rows <= 2^40.
- * The workspace, for sums of dbias, is at most 16 KB a column block of 256: (n_workers * blocks + 1184) * 1 KB.  Returns NULL on failure.
+ * model that drops; first_worker >= 0 and first_worker + n_workers <= 4096; max_rows * cols <= 2^34.
+ * The workspace, for sums of dbias, is 4 bytes for every 128 elements or so, and 5 MB at least where there are many.  Returns NULL on failure.
  */
 cser_drop_handle cser_drop_create(int32_t n_workers, int64_t max_rows, int64_t cols, double p, uint64_t seed, uint32_t site,
                                   int32_t first_worker, int32_t type);
@@ -100,10 +100,10 @@ typedef struct cser_norm_inputs {
 } cser_norm_inputs;
 
 /*
- * 1 <= channels <= 65536, a multiple of groups; n_workers <= 4096, n_workers * max_samples <= 2^24; eps >= 0 and finite.  drop: NULL, or a dropout for the
- * same number of workers, of the same type and with `channels` columns; it is copied, and n times its own limit of rows does not
- * apply, but samples * pixels * channels <= 2^34 does.  The workspace is 8 bytes for each channel of n_workers * max_samples + 1184 samples
- * and 8 for each group of n_workers * max_samples.  Returns NULL on failure.
+ * 1 <= channels <= 65536, a multiple of groups; n_workers <= 4096, n_workers * max_samples <= 2^24, and times groups below 2^31; eps >= 0 and
+ * finite.  drop: NULL, or a dropout for the same number of workers, of the same type and with `channels` columns; it is copied and may be
+ * destroyed.  Its limit of rows does not matter here, but samples * pixels * channels <= 2^34 does.  The workspace is 8 bytes for each channel of
+ * n_workers * max_samples + 1184 samples and 8 for each group of n_workers * max_samples.  Returns NULL on failure.
  */
 cser_norm_handle cser_norm_create(int32_t n_workers, int64_t max_samples, int64_t channels, int64_t groups, int32_t act, float eps,
                                   int32_t type, cser_drop_handle drop);

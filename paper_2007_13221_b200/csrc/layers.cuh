@@ -557,6 +557,8 @@ cser_norm_handle cser_norm_create(int32_t n_workers, int64_t max_samples, int64_
         return bad(CSER_ERR_INVALID, "n_workers must be in 1..4096, max_samples positive and their product at most 2^24");
     if (channels < 1 || channels > 65536 || groups < 1 || channels % groups)
         return bad(CSER_ERR_INVALID, "channels must be in 1..65536 and a multiple of groups");
+    if ((long long)n_workers * max_samples > 0x7fffffff / groups)
+        return bad(CSER_ERR_INVALID, "n_workers * max_samples * groups must be below 2^31");
     if (act != CSER_ACT_NONE && act != CSER_ACT_RELU && act != CSER_ACT_SILU)
         return bad(CSER_ERR_INVALID, "act must be CSER_ACT_NONE, CSER_ACT_RELU or CSER_ACT_SILU");
     if (!(eps >= 0.f) || !isfinite(eps)) return bad(CSER_ERR_INVALID, "eps must be finite and not negative");

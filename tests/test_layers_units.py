@@ -1,0 +1,221 @@
+"""Group norm where there are more units of work than the GPU holds at a time, and the layers' streams, large offsets and use together.
+
+The one-walk kernels keep their blocks and fetch the next unit into the places of this one: sizes here give every block several units, of
+equal and of unequal length, for clusters of one block and more, and the results are those of the same samples alone.
+"""
+import pytest
+import torch
+
+from paper_2007_13221_b200 import layers
+
+pytestmark = pytest.mark.gpu
+BF, HF, F32 = torch.bfloat16, torch.float16, torch.float32
+LONG = 200_000_000                                    # cycles, about a tenth of a second: what is queued behind it runs late
+
+
+def inputs(n, b, pixels, c, dtype, seed=0):
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+    x = (torch.randn((n, b, pixels, c), generator=gen, device="cuda") * 1.5 + torch.randn(c, generator=gen, device="cuda")).to(dtype)
+    dy = torch.randn((n, b, pixels, c), generator=gen, device="cuda").to(dtype)
+    return x, dy, torch.rand((n, c), generator=gen, device="cuda") + 0.5, torch.randn((n, c), generator=gen, device="cuda") * 0.3
+
+
+# n, samples, pixels, channels, groups, type: clusters of 1, of 2, of 4 and of 8, slices whose last is narrower, groups wider than a slice's 64
+# bytes, vectors of 8 and of 4 bytes
+MANY = [(8, 60, 64, 256, 32, BF), (2, 200, 1024, 128, 32, BF), (4, 50, 1200, 192, 4, HF), (3, 60, 3136, 64, 32, BF), (2, 40, 5000, 36, 3, HF),
+        (1, 40, 12544, 64, 32, HF), (2, 300, 77, 104, 13, F32), (8, 200, 1, 512, 32, BF), (4, 300, 9, 100, 25, BF), (1, 700, 400, 60, 2, F32)]
+
+
+@pytest.mark.parametrize("act", ["none", "silu"])
+@pytest.mark.parametrize("size", MANY, ids=str)
+def test_many_units_equal_the_samples_alone(size, act):
+    """A sample's result does not depend on what else the call has: bit for bit where it is cut alike, within rounding else."""
+    n, b, pixels, c, groups, dtype = size
+    x, dy, w, s = inputs(n, b, pixels, c, dtype)
+    op = layers.GroupNorm(n, b, c, groups, act, dtype=dtype)
+    y, stats = op.apply(x, w, s)
+    dx, dw, db = op.grad(x, dy, stats, w, s)
+    u = {BF: 2.0 ** -8, HF: 2.0 ** -11, F32: 2.0 ** -24}[dtype]
+    hat = (x.double().view(n, b, pixels, groups, -1))
+    mean = hat.mean((2, 4), keepdim=True)
+    rstd = 1 / (hat.var((2, 4), keepdim=True, correction=0) + 1e-5).sqrt()
+    hat = ((hat - mean) * rstd).view(x.shape)
+    z = hat * w.double().view(n, 1, 1, c) + s.double().view(n, 1, 1, c)
+    gate = torch.sigmoid(z)
+    want = z * gate if act == "silu" else z
+    # 64 roundings of values of up to 16 deviations before the result's own
+    slack = 64 * 16 * 2.0 ** -24
+    assert bool(((y.double() - want).abs() <= 1.01 * u * want.abs() + slack * (1 + want.abs()) + 2.0 ** -25).all())
+    dz = dy.double() * (gate * (1 + z * (1 - gate)) if act == "silu" else 1)
+    t = (dz * w.double().view(n, 1, 1, c)).view(n, b, pixels, groups, -1)
+    h5 = hat.view(t.shape)
+    wanted = ((t - t.mean((2, 4), keepdim=True) - h5 * (t * h5).mean((2, 4), keepdim=True)) * rstd).view(x.shape)
+    size_dx = (rstd * (1 + h5.abs())).expand(t.shape).reshape(x.shape) * (1 + dy.double().abs()) * 4
+    assert bool(((dx.double() - wanted).abs() <= 1.01 * u * wanted.abs() + slack * size_dx + 2.0 ** -25).all())
+    for got, terms, size in ((db, dz, 1 + dy.double().abs()), (dw, dz * hat, (1 + dy.double().abs()) * (1 + hat.abs()))):
+        assert bool(((got.double() - terms.sum((1, 2))).abs() <= (slack + 64 * 2.0 ** -24) * size.sum((1, 2))).all())
+    again = op.apply(x, w, s)
+    assert torch.equal(again[0], y) and torch.equal(again[1], stats)
+    more = op.grad(x, dy, stats, w, s)
+    assert all(torch.equal(p, q) for p, q in zip(more, (dx, dw, db)))
+    few = layers.GroupNorm(n, 1, c, groups, act, dtype=dtype)
+    for k in (0, b // 2, b - 1):
+        one, st = few.apply(x[:, k:k + 1], w, s)
+        assert bool(((one.double() - y[:, k:k + 1].double()).abs() <= 2.02 * u * one.double().abs() + 2 * slack * (1 + one.double().abs())).all())
+
+
+@pytest.mark.parametrize("size", MANY[:7], ids=str)
+def test_many_units_of_a_dropout(size):
+    """The same as norm(dropout(x)) with the dropped array rounded to no fewer bits than it has: a factor of 2 rounds nothing."""
+    n, b, pixels, c, groups, dtype = size
+    x, dy, w, s = inputs(n, b, pixels, c, dtype, seed=1)
+    drop = layers.Dropout(n, b * pixels, c, 0.5, 77, 9, dtype)
+    dropped = drop.apply(x, 3)
+    fused = layers.GroupNorm(n, b, c, groups, "silu", dtype=dtype, dropout=drop)
+    plain = layers.GroupNorm(n, b, c, groups, "silu", dtype=dtype)
+    y, stats = fused.apply(x, w, s, step=3)
+    y2, stats2 = plain.apply(dropped, w, s)
+    u = {BF: 2.0 ** -8, HF: 2.0 ** -11, F32: 2.0 ** -24}[dtype]
+    slack = 128 * 16 * 2.0 ** -24
+    assert bool(((stats - stats2).abs() <= slack * (1 + stats2.abs())).all())
+    assert bool(((y.double() - y2.double()).abs() <= 2.02 * u * y2.double().abs() + slack * (1 + y2.double().abs())).all())
+    got = fused.grad(x, dy, stats, w, s, step=3)
+    want = plain.grad(dropped, dy, stats2, w, s)
+    through = drop.grad(want[0], 3)[0]
+    size_dx = 2 * (1 + dy.double().abs()) * (1 + through.double().abs()) * 8
+    assert bool(((got[0].double() - through.double()).abs() <= 3.03 * u * through.double().abs() + slack * size_dx).all())
+    for g, p in zip(got[1:], want[1:]):
+        assert bool(((g - p).abs() <= slack * pixels * b).all())
+
+
+def test_more_than_2_31_elements():
+    """Offsets beyond 32 bits, at both ends of arrays of 2^31 + 2^20 elements, against the same places in small calls."""
+    n, rows, cols = 1, 2 ** 21 + 2 ** 10, 1024
+    x = torch.zeros((n, rows, cols), dtype=BF, device="cuda")
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(3)
+    head, tail = torch.randn((64, cols), generator=gen, device="cuda").to(BF), torch.randn((64, cols), generator=gen, device="cuda").to(BF)
+    x[0, :64], x[0, -64:] = head, tail
+    op = layers.Dropout(n, rows, cols, 0.25, 5, 6)
+    y = op.apply(x, 11)
+    kept = y[0, -64:] != 0
+    assert torch.equal(y[0, :64], layers.Dropout(1, 64, cols, 0.25, 5, 6).apply(head[None], 11)[0])
+    assert bool((y[0, 64:-64] == 0).all())
+    dx, db = op.grad(x, 11, need_dbias=True)
+    assert torch.equal(dx, y)
+    want = y[0, :64].double().sum(0) + y[0, -64:].double().sum(0)
+    size = y[0, :64].double().abs().sum(0) + y[0, -64:].double().abs().sum(0)
+    assert bool(((db[0].double() - want).abs() <= size * (2.0 ** -8 + 1e-5)).all())
+    import numpy as np
+    from oracle.philox import philox4x32_10
+    first = (rows - 64) * cols
+    q = np.arange(first // 4, rows * cols // 4, dtype=np.uint64)
+    words = np.stack(philox4x32_10(5, 0, q, 11, 0, 4096 * 6), 1).reshape(64, cols)
+    assert torch.equal(kept, torch.from_numpy(words >= 2 ** 30).cuda() & (tail != 0))
+    del y, dx
+    norm = layers.GroupNorm(1, rows // 2, cols, 8, "silu")
+    z, stats = norm.apply(x.view(1, rows // 2, 2, cols))
+    part = layers.GroupNorm(1, 32, cols, 8, "silu").apply(x.view(1, rows // 2, 2, cols)[:, -32:])
+    assert bool(((z[:, -32:].double() - part[0].double()).abs() <= 2.0 ** -7 * part[0].double().abs() + 1e-4).all())
+    assert bool((z[:, 32:-32] == 0).all())
+    grads = norm.grad(x.view(1, rows // 2, 2, cols), z, stats)
+    assert bool(grads[0][:, 32:-32].isfinite().all()) and bool((grads[0][:, 32:-32] == 0).all())
+
+
+def test_calls_on_another_stream():
+    """Results are made on the stream; inputs may be dropped after the call, results while the current stream reads them."""
+    x, dy, w, s = inputs(2, 6, 300, 64, BF)
+    drop = layers.Dropout(2, 6 * 300, 64, 0.3, 1, 2)
+    norm = layers.GroupNorm(2, 6, 64, 8, "silu", dropout=drop)
+    xs, dys = x.view(2, 1800, 64), dy.view(2, 1800, 64)
+
+    def calls(x, dy, w, s, stream=None):
+        y, stats = norm.apply(x, w, s, step=4, stream=stream)
+        a = drop.apply(x.view(2, 1800, 64), 4, bias=w, residual=dy.view(2, 1800, 64), stream=stream)
+        return (y, stats, a, *norm.grad(x, dy, stats, w, s, step=4, stream=stream),
+                *drop.grad(dy.view(2, 1800, 64), 4, need_dbias=True, stream=stream))
+
+    want = calls(x, dy, w, s)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    old = [torch.empty_like(a) for a in want]
+    torch.cuda._sleep(LONG)
+    for a in old:
+        a.fill_(7)
+    del old                                             # memory that the current stream writes late and its pool gives out at once
+    got = calls(x, dy, w, s, stream=side)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    args = [a.clone() for a in (x, dy, w, s)]
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(LONG)
+    got = calls(*args, stream=side)
+    shapes = [torch.empty_like(a) for a in args]
+    del args
+    junk = [torch.full_like(a, 3) for a in shapes for _ in range(3)]
+    torch.cuda.synchronize()
+    del junk
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    torch.cuda._sleep(LONG)
+    read = [a.clone() for a in got]
+    del got
+    with torch.cuda.stream(side):
+        junk = [torch.full_like(a, 3) for a in read for _ in range(3)]
+    torch.cuda.synchronize()
+    del junk
+    assert all(torch.equal(a, b) for a, b in zip(read, want))
+    assert xs.data_ptr() == x.data_ptr() and dys.data_ptr() == dy.data_ptr()
+
+
+def test_calls_behind_one_another_and_captured():
+    """Kernels are set up while the ones before them end: a chain of calls on the same buffers, replayed and not, gives the same bits."""
+    n, b, pixels, c = 2, 40, 49, 96
+    x, dy, w, s = inputs(n, b, pixels, c, BF, seed=5)
+    drop = layers.Dropout(n, b * pixels, c, 0.3, 1, 2)
+    norm = layers.GroupNorm(n, b, c, 12, "silu")
+    flat, grads = torch.zeros((n, 500), device="cuda"), torch.zeros((n, 500), device="cuda")
+    flat[:, 3:3 + c], flat[:, 200:200 + c] = w, s
+    weight, bias, dweight, dbias = flat[:, 3:3 + c], flat[:, 200:200 + c], grads[:, 3:3 + c], grads[:, 200:200 + c]
+    h, out, dx = torch.empty_like(x), torch.empty_like(x), torch.empty_like(x)
+
+    def chain():
+        drop.apply(x, 8, out=h)
+        for _ in range(3):
+            _, stats = norm.apply(h, weight, bias, out=out)
+            norm.grad(h, dy, stats, weight, bias, dx=dx, dweight=dweight, dbias=dbias)
+            drop.apply(dx, 9, residual=out, out=h)
+        drop.grad(h, 10, dx=dx, dbias=grads[:, 400:400 + c])
+
+    chain()
+    torch.cuda.synchronize()
+    want = [a.clone() for a in (h, out, dx, grads)]
+    for _ in range(5):
+        chain()
+    assert all(torch.equal(a, b) for a, b in zip((h, out, dx, grads), want))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        chain()
+    for a in (h, out, dx, grads):
+        a.zero_()
+    for _ in range(3):
+        graph.replay()
+    assert all(torch.equal(a, b) for a, b in zip((h, out, dx, grads), want))
+
+
+def test_a_handle_may_go_while_a_graph_is_captured():
+    x, dy, w, s = inputs(1, 2, 9, 16, BF)
+    norm, other, drop = layers.GroupNorm(1, 2, 16, 4), layers.GroupNorm(1, 2, 16, 4), layers.Dropout(1, 18, 16, 0.5, 1, 1)
+    want = norm.apply(x, w, s)[0]
+    out = torch.zeros_like(x)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        other.close()
+        norm.apply(x, w, s, out=out)
+        del drop
+    graph.replay()
+    assert torch.equal(out, want) and other.h is None
