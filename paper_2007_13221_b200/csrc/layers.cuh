@@ -475,12 +475,16 @@ int norm_grad(cser_norm *h, const cser_norm_inputs *in, const float *stats, cons
     return with_vector<T>(v, [&](auto vector) -> int {
         constexpr int V = decltype(vector)::value;
         unsigned grid;
-        bool done = false;
+        bool done = false, direct = false;
         if constexpr (V * sizeof(T) >= 4) {
             Resident r;
             size_t shared;
             if (plan_resident(h, in, V, true, r, shared)) {
-                a.part = dweight || dbias ? h->part : nullptr, a.chunks = 1, done = true;
+                // A worker's only sample's sums are its gradients; those of several are added up behind.
+                a.chunks = 1, done = true, direct = a.samples == 1;
+                a.sums[0] = direct ? dbias : h->part, a.sums_sample[0] = direct ? dbias_stride : a.channels;
+                a.sums[1] = direct ? dweight : h->part + h->plane, a.sums_sample[1] = direct ? dweight_stride : a.channels;
+                if (!dbias && !dweight) a.sums[0] = a.sums[1] = nullptr;
                 if (int rc = resident_launch<T>(h, h->drop ? norm_grad_resident_kernel<T, V, true> : norm_grad_resident_kernel<T, V, false>, a, r, shared, st))
                     return rc;
             }
@@ -490,7 +494,7 @@ int norm_grad(cser_norm *h, const cser_norm_inputs *in, const float *stats, cons
             TRY(launch(h->drop ? norm_grad_sums_kernel<T, V, true> : norm_grad_sums_kernel<T, V, false>, dim3(grid), 256, 0, 1, st, a));
             h->launches++;
         }
-        if (dweight || dbias) {
+        if ((dweight || dbias) && !direct) {
             RowSums s{};
             s.part = a.part, s.plane = a.plane, s.rows = (long long)a.samples * a.chunks, s.cols = a.channels;
             s.out[0] = dbias, s.out_stride[0] = dbias_stride, s.out[1] = dweight, s.out_stride[1] = dweight_stride;

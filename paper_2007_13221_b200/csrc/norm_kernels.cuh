@@ -25,6 +25,8 @@ template <typename T> struct NormArgs {
     float2 *group_sums;                                // s1 / N, s2 / N of each sample's groups
     float *part;                                       // two planes of [n * samples][chunks][channels]
     long long plane;
+    float *sums[2];                                    // of dz and dz * xhat of each sample, or null
+    long long sums_sample[2];                          // from one sample's to the next's
     int n, samples, channels, groups, per_group, act;
     long long pixels;
     float eps;
@@ -242,6 +244,7 @@ __global__ void __launch_bounds__(256) norm_moments_kernel(NormArgs<T> a) {
     let_next();
     const Place p = place<T, V>(a);
     const Words words(a.draw, p.w);
+    constexpr int U = 2 * kTogether;
     float n = 0.f, mean[V], m2[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) mean[j] = m2[j] = 0.f;
@@ -259,13 +262,13 @@ __global__ void __launch_bounds__(256) norm_moments_kernel(NormArgs<T> a) {
             }
             n = total, got = 0;
         };
-        for (long long i = p.first + p.ty; i < p.last; i += kTogether * p.rows, x += kTogether * p.rows * a.xs.pixel) {
-            Vec<T, V> v[kTogether];
+        for (long long i = p.first + p.ty; i < p.last; i += U * p.rows, x += U * p.rows * a.xs.pixel) {
+            Vec<T, V> v[U];
 #pragma unroll
-            for (int u = 0; u < kTogether; ++u)
+            for (int u = 0; u < U; ++u)
                 if (i + u * p.rows < p.last) v[u] = Vec<T, V>(x + u * p.rows * a.xs.pixel);
 #pragma unroll
-            for (int u = 0; u < kTogether; ++u)
+            for (int u = 0; u < U; ++u)
                 if (i + u * p.rows < p.last) {
                     if (DROP) drop_out(v[u], a.draw, words, element(a, p, i + u * p.rows));
                     F2 f[kPairs<V>];
@@ -388,7 +391,7 @@ __global__ void __launch_bounds__(256) norm_grad_sums_kernel(NormArgs<T> a) {
         Channels<V> k;
         channels_of(k, a, p.w, p.b, p.c);
         const T *x = at_pixel(a.x, a.xs, p, p.first + p.ty), *dy = at_pixel(a.dy, a.dys, p, p.first + p.ty);
-        constexpr int U = 2;
+        constexpr int U = kTogether;
         with_act(a.act, [&](auto act) {
             for (long long i = p.first + p.ty; i < p.last; i += U * p.rows, x += U * p.rows * a.xs.pixel, dy += U * p.rows * a.dys.pixel) {
                 Vec<T, V> vx[U], vd[U];

@@ -367,9 +367,9 @@ __global__ void __launch_bounds__(kMostThreads) norm_grad_resident_kernel(NormAr
         float p = 0.f, q = 0.f;
         for (int i = 0; i < 1 << r.log_cluster; ++i) p += all[2 * i * width + c], q += all[(2 * i + 1) * width + c];
         q *= s.coef[3 * width + c];
-        if (a.part && (c & ((1 << r.log_cluster) - 1)) == s.rank) {
-            const long long at = (long long)s.sample * a.channels + s.c0 + c;
-            a.part[at] = p, a.part[a.plane + at] = q;
+        if ((c & ((1 << r.log_cluster) - 1)) == s.rank) {
+            if (a.sums[0]) a.sums[0][s.sample * a.sums_sample[0] + s.c0 + c] = p;
+            if (a.sums[1]) a.sums[1][s.sample * a.sums_sample[1] + s.c0 + c] = q;
         }
         s.coef[4 * width + c] = p * s.coef[c], s.coef[5 * width + c] = q * s.coef[c];
     }

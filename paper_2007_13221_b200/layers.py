@@ -168,7 +168,9 @@ class Dropout(_Handle):
         rs = None if residual is None else self._array("residual", residual, x)[1]
         if out is None:
             out = _like(x)
-        ys = self._array("out", out, x)[1]
+            ys = _Rows(out.data_ptr(), self.cols, rows * self.cols)
+        else:
+            ys = self._array("out", out, x)[1]
         rc = _lib.cser_drop_apply(self.h, rows, step, step_at, xs, b, b_stride, rs, ys, _raw_stream(x))
         if rc:
             _check(rc, "cser_drop_apply")
@@ -185,7 +187,9 @@ class Dropout(_Handle):
         if need_dx:
             if dx is None:
                 dx = _like(dy)
-            xs = self._array("dx", dx, dy)[1]
+                xs = _Rows(dx.data_ptr(), self.cols, rows * self.cols)
+            else:
+                xs = self._array("dx", dx, dy)[1]
         if dbias is None and need_dbias:
             dbias = torch.empty((self.n, self.cols), dtype=torch.float32, device=dy.device)
         b, b_stride = _params("Dropout: dbias", dbias, self.n, self.cols)
@@ -231,6 +235,16 @@ class GroupNorm(_Handle):
         pixels, step = _merged(f"GroupNorm: {name}", shape, stride, 2, t.dim() - 1)
         return pixels, _Pixels(t.data_ptr(), step, stride[1], stride[0])
 
+    def _dense(self, t, args):
+        """A dense array of x's shape, as just made."""
+        sample = args.pixels * self.channels
+        return _Pixels(t.data_ptr(), self.channels, sample, sample * args.samples)
+
+    def _new_params(self, like, x):
+        if like is not None and like.is_contiguous():
+            return torch.empty_like(like)                 # half the time of empty()
+        return torch.empty((self.n, self.channels), dtype=torch.float32, device=x.device)
+
     def _inputs(self, x, weight, bias, step):
         pixels, xs = self._array("x", x)
         step, step_at = _step(step)
@@ -246,8 +260,10 @@ class GroupNorm(_Handle):
         args = self._inputs(x, weight, bias, step)
         if out is None:
             out = _like(x)
-        ys = self._array("out", out, x)[1]
-        stats = torch.empty((2, self.n, x.shape[1], self.groups), dtype=torch.float32, device=x.device)
+            ys = self._dense(out, args)
+        else:
+            ys = self._array("out", out, x)[1]
+        stats = torch.empty((2, self.n, args.samples, self.groups), dtype=torch.float32, device=x.device)
         _check(_lib.cser_norm_apply(self.h, args, ys, stats.data_ptr(), _raw_stream(x)), "cser_norm_apply")
         return out, stats
 
@@ -266,12 +282,14 @@ class GroupNorm(_Handle):
         if need_dx:
             if dx is None:
                 dx = _like(x)
-            xs = self._array("dx", dx, x)[1]
+                xs = self._dense(dx, args)
+            else:
+                xs = self._array("dx", dx, x)[1]
         if need_params:
             if dweight is None:
-                dweight = torch.empty((self.n, self.channels), dtype=torch.float32, device=x.device)
+                dweight = self._new_params(weight, x)
             if dbias is None:
-                dbias = torch.empty((self.n, self.channels), dtype=torch.float32, device=x.device)
+                dbias = self._new_params(bias, x)
             w, w_stride = _params("GroupNorm: dweight", dweight, self.n, self.channels)
             b, b_stride = _params("GroupNorm: dbias", dbias, self.n, self.channels)
         else:
