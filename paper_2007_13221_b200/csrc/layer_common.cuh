@@ -172,8 +172,8 @@ template <int V, bool ALIGNED> struct Drawn {
 };
 
 // ------------------------------------------------------------------ sums over rows
-// out[k][i][c] = sum over r of part[k][i][r][c], in an order of its own for each (k, i, c): 32 lanes of rows each take every 32nd, and
-// their sums are added in order.  Grid (ceil(cols / 32), n, planes), 1024 threads: a warp reads 32 columns of a row.
+// out[k][i][c] = sum over r of part[k][i][r][c]: a block's warps take every so many rows each, and their sums are added in order.  Grid
+// (ceil(cols / 32), n, planes): a warp reads 32 columns of a row.
 struct RowSums {
     const float *part;
     float *out[2];
@@ -181,27 +181,31 @@ struct RowSums {
     long long rows, cols, plane;                       // plane: elements from one plane of parts to the next
 };
 __global__ void __launch_bounds__(1024) sum_rows_kernel(RowSums a) {
-    __shared__ float sums[32][33];
+    __shared__ float sums[32][32];
     after_previous();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     const long long c = (long long)blockIdx.x * 32 + lane;
     float *out = a.out[blockIdx.z];
     if (!out) return;
-    const float *p = a.part + blockIdx.z * a.plane + (long long)blockIdx.y * a.rows * a.cols;
+    const float *p = a.part + blockIdx.z * a.plane + (long long)blockIdx.y * a.rows * a.cols + c;
     float s = 0.f;
     if (c < a.cols) {
+        constexpr int U = 8;                           // rows whose loads are under way together
         long long r = warp;
-        for (; r + 96 < a.rows; r += 128) {
-            const float v0 = p[r * a.cols + c], v1 = p[(r + 32) * a.cols + c], v2 = p[(r + 64) * a.cols + c], v3 = p[(r + 96) * a.cols + c];
-            s = ((s + v0) + v1) + (v2 + v3);
+        for (; r + (U - 1) * warps < a.rows; r += U * warps) {
+            float v[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] = p[(r + u * warps) * a.cols];
+#pragma unroll
+            for (int u = 0; u < U; ++u) s += v[u];
         }
-        for (; r < a.rows; r += 32) s += p[r * a.cols + c];
+#pragma unroll 4
+        for (; r < a.rows; r += warps) s += p[r * a.cols];
     }
     sums[warp][lane] = s;
     __syncthreads();
-    s = sums[lane][warp];                              // warp now stands for the column
-#pragma unroll
-    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(~0u, s, o);
-    const long long col = (long long)blockIdx.x * 32 + warp;
-    if (lane == 0 && col < a.cols) out[blockIdx.y * a.out_stride[blockIdx.z] + col] = s;
+    if (warp == 0 && c < a.cols) {
+        for (int k = 1; k < warps; ++k) s += sums[k][lane];
+        out[blockIdx.y * a.out_stride[blockIdx.z] + c] = s;
+    }
 }

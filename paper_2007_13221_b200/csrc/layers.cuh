@@ -86,7 +86,7 @@ cudaError_t launch(void (*kernel)(P...), dim3 grid, unsigned block, size_t share
 }
 
 int launch_row_sums(const RowSums &s, long long n, int planes, int64_t &launches, cudaStream_t st) {
-    TRY(launch(sum_rows_kernel, dim3((unsigned)ceil_div(s.cols, 32), (unsigned)n, (unsigned)planes), 1024, 0, 1, st, s));
+    TRY(launch(sum_rows_kernel, dim3((unsigned)ceil_div(s.cols, 32), (unsigned)n, (unsigned)planes), s.rows > 64 ? 1024 : 256, 0, 1, st, s));
     launches++;
     return CSER_OK;
 }
