@@ -64,18 +64,19 @@ __device__ __forceinline__ void drop_flat_warp(const DropArgs<T> &a, int w, int 
         }
     }
     const Words words(a.draw, w);
-    const uint32_t quad = (uint32_t)(e0 >> 2), by = (uint32_t)e0 & 3;
+    const uint64_t call = Words::call(e0 >> 2);
+    const uint32_t by = (uint32_t)e0 & 3;
     uint32_t next[3];                                  // the first draws of the 32 vectors behind
     if (SHIFTED) {
         uint32_t four[4];
-        words.four(four, quad + (kFlat * 32 - lane) * (V / 4));
+        words.four(four, call + (uint64_t)((kFlat * 32 - lane) * (V / 4)) * Words::kCall);
         next[0] = four[0], next[1] = four[1], next[2] = four[2];
     }
 #pragma unroll
     for (int u = kFlat - 1; u >= 0; --u) {
         uint32_t d[V + 3];
 #pragma unroll
-        for (int k = 0; k < V / 4; ++k) words.four(d + 4 * k, quad + u * 8 * V + k);
+        for (int k = 0; k < V / 4; ++k) words.four(d + 4 * k, call + (u * 8 * V + k) * Words::kCall);
         if (SHIFTED) {
 #pragma unroll
             for (int j = 0; j < 3; ++j) {
@@ -160,8 +161,9 @@ __global__ void __launch_bounds__(256, 4) drop_rows_kernel(DropArgs<T> a) {
         const long long x_step = (MODE == kDense ? a.width : a.x_row) << a.log_rows, r_step = (MODE == kDense ? a.width : a.r_row) << a.log_rows,
                         y_step = (MODE == kDense ? a.width : a.y_row) << a.log_rows, e_step = e_row << a.log_rows;
         const bool store = !SUMS || a.y;
-        uint32_t quad = (uint32_t)(e >> 2);
-        const uint32_t by = (uint32_t)e & 3, quad_step = (uint32_t)(e_step >> 2);          // (not odd: rows are whole fours)
+        uint64_t call = Words::call(e >> 2);
+        const uint64_t call_step = Words::call(e_step >> 2);                               // (not odd: rows are whole fours)
+        const uint32_t by = (uint32_t)e & 3;
         const T *x = a.x + w * a.x_worker + (e - (MODE == kDense ? 0 : row0 * (e_row - a.x_row))), *r = nullptr;
         T *y = nullptr;
         if (residual) r = a.r + w * a.r_worker + (e - (MODE == kDense ? 0 : row0 * (e_row - a.r_row)));
@@ -180,7 +182,7 @@ __global__ void __launch_bounds__(256, 4) drop_rows_kernel(DropArgs<T> a) {
             vx.round(f);
         };
         auto next = [&](int rows) {
-            x += rows * x_step, quad += rows * quad_step;
+            x += rows * x_step, call += rows * call_step;
             if (residual) r += rows * r_step;
             if (store) y += rows * y_step;
         };
@@ -214,7 +216,7 @@ __global__ void __launch_bounds__(256, 4) drop_rows_kernel(DropArgs<T> a) {
                 }
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
-                    finish(vx[u], vr[u], Drawn<V, !SHIFTED>(words, quad + u * quad_step, by));
+                    finish(vx[u], vr[u], Drawn<V, !SHIFTED>(words, call + u * call_step, by));
                     if (store) vx[u].to(y + u * y_step);
                 }
                 next(U);
@@ -222,7 +224,7 @@ __global__ void __launch_bounds__(256, 4) drop_rows_kernel(DropArgs<T> a) {
             for (; i < whole; ++i) {
                 Vec<T, V> vx(x), vr;
                 if (residual) vr = Vec<T, V>(r);
-                finish(vx, vr, Drawn<V, !SHIFTED>(words, quad, by));
+                finish(vx, vr, Drawn<V, !SHIFTED>(words, call, by));
                 if (store) vx.to(y);
                 next(1);
             }

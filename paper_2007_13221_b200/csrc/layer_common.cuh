@@ -136,9 +136,12 @@ struct Words {
         d = (uint32_t)q;
     }
 
-    // Draws 4 * quad .. 4 * quad + 3 of the worker.
-    __device__ __forceinline__ void four(uint32_t *w, uint32_t quad) const {
-        const uint64_t p = (uint64_t)0xD2511F53u * quad;
+    // The first round's first product, of the call number itself: from call to call it grows by kCall, so it is multiplied out once.
+    static constexpr uint64_t kCall = 0xD2511F53u;
+    __device__ __forceinline__ static uint64_t call(long long number) { return kCall * (uint64_t)number; }
+
+    // The draws of the call with this product.
+    __device__ __forceinline__ void four(uint32_t *w, uint64_t p) const {
         const uint64_t q = (uint64_t)0xCD9E8D57u * ((uint32_t)(p >> 32) ^ a);
         uint32_t c0 = (uint32_t)(q >> 32) ^ b, c1 = (uint32_t)q, c2 = (uint32_t)p ^ c, c3 = d;
         philox4x32_rounds<8>(c0, c1, c2, c3, k0 + 2 * 0x9E3779B9u, k1 + 2 * 0xBB67AE85u);
@@ -163,12 +166,12 @@ template <int N> __device__ __forceinline__ void shift_words(uint32_t (&w)[N], u
 template <int V, bool ALIGNED> struct Drawn {
     static constexpr int kCalls = ALIGNED ? V / 4 : (V + 2) / 4 + 1;
     uint32_t w[kCalls * 4];
-    __device__ __forceinline__ Drawn(const Words &words, uint32_t quad, uint32_t by) {
+    __device__ __forceinline__ Drawn(const Words &words, uint64_t call, uint32_t by) {
 #pragma unroll
-        for (int k = 0; k < kCalls; ++k) words.four(w + 4 * k, quad + k);
+        for (int k = 0; k < kCalls; ++k) words.four(w + 4 * k, call + k * Words::kCall);
         if (!ALIGNED) shift_words(w, by);
     }
-    __device__ __forceinline__ Drawn(const Words &words, long long e) : Drawn(words, (uint32_t)(e >> 2), (uint32_t)e & 3) {}
+    __device__ __forceinline__ Drawn(const Words &words, long long e) : Drawn(words, Words::call(e >> 2), (uint32_t)e & 3) {}
 };
 
 // ------------------------------------------------------------------ sums over rows
