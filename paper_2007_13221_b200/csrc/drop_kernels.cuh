@@ -4,9 +4,12 @@
 //   y = residual + keep * (x + bias) / (1 - p),   dx = keep * dy / (1 - p),   dbias = sum over rows of dx
 //
 // A call of the generator makes four draws: its number is the element's place in the worker's array, so a thread draws what it needs
-// wherever it stands and nothing is stored.  Bound: memory, with the generator close behind for 16-bit elements (a call's 18 wide
-// multiplies occupy their pipe for four cycles each: eight elements take 144 of the 176 cycles that an SM's quarter has for them
-// at the copy rate), so nothing is drawn twice that a neighbour has and what all calls share is made once a thread.
+// wherever it stands and nothing is stored.  Bound: memory for 32-bit elements (8 x 4096 x 1024 with bias and residual 6.7 TB/s), the generator for
+// 16-bit ones: of the 176 cycles that an SM's quarter has for eight of them at the copy rate, two calls' wide multiplies occupy their pipe
+// for 140 (four cycles each) and all instructions about 140 slots, and the two overlap to 225 (8 x 8192 x 4096 5.2 TB/s, 206 us; floor 164).  So what
+// all calls share is made once a thread (the round that differs in one word, the first product, which grows by addition from call to call:
+// 379 -> 206 us together with whole vectors), and nothing is drawn twice that a neighbour has.  Tried: products from the FP64 pipe (106 cycles a
+// call for 88), high and low halves apart (90).
 #pragma once
 
 template <typename T> struct DropArgs {
