@@ -263,7 +263,8 @@ class GroupNorm(_Handle):
             ys = self._dense(out, args)
         else:
             ys = self._array("out", out, x)[1]
-        stats = torch.empty((2, self.n, args.samples, self.groups), dtype=torch.float32, device=x.device)
+        size = (2, self.n, args.samples, self.groups)
+        stats = torch.empty(size, dtype=torch.float32, device=x.device) if weight is None else weight.new_empty(size)
         _check(_lib.cser_norm_apply(self.h, args, ys, stats.data_ptr(), _raw_stream(x)), "cser_norm_apply")
         return out, stats
 
