@@ -26,7 +26,8 @@ extern "C" {
  * division of the workers over handles.
  *     y = residual + keep * (x + bias) / (1 - p)          bias, residual: none, one or both
  *     dx = keep * dy / (1 - p) ,   dbias = sum over rows of dx ,   (dresidual = dy)
- * A dropped element counts as 0 whatever its value, an infinity or NaN too.
+ * A dropped element counts as 0 whatever its value, an infinity or NaN too.  Where workers share an array (a worker stride of 0), gradients are
+ * still each worker's own.
  *
  * Arithmetic.  x, residual, y, dy and dx are of one type, F32, BF16 or F16; computed in fp32 and rounded once.  bias and dbias are
  * fp32; the sums are fp32, of values before their rounding, in a fixed order.

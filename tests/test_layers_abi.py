@@ -52,3 +52,12 @@ def test_stamp_covers_the_layers_sources(tmp_path):
         after = g.source_id(str(copy / "cser.cu"))
         assert after != before, name
         before = after
+
+
+def test_norms_of_too_many_groups_are_refused():
+    """Before anything is allocated: the groups of all samples are numbered with 31 bits."""
+    import pytest
+    from paper_2007_13221_b200 import layers
+    from paper_2007_13221_b200.binding import CSERError
+    with pytest.raises(CSERError, match="2\\^31"):
+        layers.GroupNorm(2, 2 ** 23, 256, 128)

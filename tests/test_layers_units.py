@@ -219,3 +219,37 @@ def test_a_handle_may_go_while_a_graph_is_captured():
         del drop
     graph.replay()
     assert torch.equal(out, want) and other.h is None
+
+
+def test_between_the_other_operators():
+    """Behind and before the cross entropy, whose kernels too are set up while the ones before them end: the same bits as one after the other."""
+    from paper_2007_13221_b200 import train
+    n, t, v, d = 2, 96, 700, 128
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(9)
+    x = torch.randn((n, t, d), generator=gen, device="cuda").to(BF)
+    w = (torch.randn((n, v, d), generator=gen, device="cuda") * 0.1).to(BF)
+    y = torch.randint(0, v, (n, t), generator=gen, device="cuda")
+    mean = torch.full((n, t), 1.0 / t, device="cuda")
+    drop, head = layers.Dropout(n, t, d, 0.2, 3, 1), train.LinearCrossEntropy(n, t, v, d)
+    norm = layers.GroupNorm(n, t, d, 4, "silu")
+
+    def step(wait):
+        out = []
+        h, stats = norm.apply(x.view(n, t, 1, d))
+        wait()
+        h = drop.apply(h.view(n, t, d), 6, residual=x)
+        wait()
+        loss, lse = head.loss(h, w, y)
+        wait()
+        dh, dw = head.grad(h, w, y, lse, mean)
+        wait()
+        dz, db = drop.grad(dh, 6, need_dbias=True)
+        wait()
+        out += [loss, dw, dz, db, *norm.grad(x.view(n, t, 1, d), dz.view(n, t, 1, d), stats)]
+        return out
+
+    want = step(torch.cuda.synchronize)
+    for _ in range(20):
+        got = step(lambda: None)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
