@@ -8,6 +8,9 @@
  * stream); a call only enqueues work and returns; calls on one handle must not overlap, on the host or on the GPU (a handle's
  * workspace serves one call at a time).  Calls may be captured in a CUDA graph and replayed.  No call aborts, throws or
  * traps on the device, and no kernel waits for another.  Results are the same from call to call, bit for bit.
+ *
+ * A handle is made once for many calls: on a B200 0.03 to 0.35 ms for a workspace of more than 1 MB, and as much to
+ * destroy.  The first call of a kind loads its kernel, 2 to 4 ms once in a process.
  */
 #ifndef CSER_LAYERS_H_
 #define CSER_LAYERS_H_

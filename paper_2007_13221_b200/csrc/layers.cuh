@@ -416,8 +416,8 @@ bool plan_resident(const cser_norm *h, const cser_norm_inputs *in, int v, bool t
     r.group_magic = per_group == 1 ? 0 : (uint32_t)(((1ull << 32) + per_group - 1) / per_group);
     return true;
 }
-// The call's launch: as many clusters as the GPU holds at a time, or as there are units.  How many that is is asked once for a kernel and a
-// shape.
+// The call's launch: as many clusters as the GPU holds at a time, or as there are units.  How many it holds is asked once for a kernel and a
+// shape, and the kernel allowed its shared memory then (for all kernels when a handle is made, loading them took 40 ms of a process).
 template <typename T>
 int resident_launch(cser_norm *h, void (*kernel)(NormArgs<T>, Resident), const NormArgs<T> &a, const Resident &r, size_t shared, cudaStream_t st) {
     cser_norm::Fit *fit = nullptr;
@@ -432,6 +432,7 @@ int resident_launch(cser_norm *h, void (*kernel)(NormArgs<T>, Resident), const N
         at[0].val.clusterDim.x = 1u << r.log_cluster, at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
         cfg.attrs = at, cfg.numAttrs = 1;
         fit->kernel = nullptr;
+        TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 << 10));
         TRY(cudaOccupancyMaxActiveClusters(&fit->clusters, kernel, &cfg));
         fit->kernel = (const void *)kernel, fit->log_cluster = r.log_cluster, fit->log_block = r.log_block, fit->shared = shared;
     }
@@ -509,21 +510,6 @@ int norm_grad(cser_norm *h, const cser_norm_inputs *in, const float *stats, cons
     });
 }
 
-// The one-walk kernels of a type may use all of an SM's shared memory.
-template <typename T, int V> cudaError_t allow_shared_of() {
-    if constexpr (V * sizeof(T) >= 4) {
-        for (auto k : {norm_resident_kernel<T, V, false>, norm_resident_kernel<T, V, true>, norm_grad_resident_kernel<T, V, false>,
-                       norm_grad_resident_kernel<T, V, true>})
-            if (cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 << 10)) return e;
-    }
-    return cudaSuccess;
-}
-template <typename T> cudaError_t allow_shared() {
-    cudaError_t e = allow_shared_of<T, 16 / sizeof(T)>();
-    if (e == cudaSuccess) e = allow_shared_of<T, 8 / sizeof(T)>();
-    return e == cudaSuccess ? allow_shared_of<T, 4 / sizeof(T)>() : e;
-}
-
 // Checks that both calls make; *empty: nothing to compute.
 int check_norm(const cser_norm *h, const cser_norm_inputs *in, const char *what, bool *empty) {
     if (!h) return fail(CSER_ERR_INVALID, "%s: NULL handle", what);
@@ -577,9 +563,6 @@ cser_norm_handle cser_norm_create(int32_t n_workers, int64_t max_samples, int64_
     const long long all = (long long)n_workers * max_samples;
     h->plane = (all + layers::kBusy) * channels;
     cudaError_t e = cudaGetDevice(&h->device);
-    if (e == cudaSuccess)
-        e = type == CSER_TYPE_F32 ? layers::allow_shared<float>() : type == CSER_TYPE_BF16 ? layers::allow_shared<__nv_bfloat16>()
-                                                                                          : layers::allow_shared<__half>();
     if (e == cudaSuccess) e = cudaMalloc(&h->part, (size_t)h->plane * 2 * 4);
     if (e == cudaSuccess) e = cudaMalloc(&h->group_sums, (size_t)(all * groups) * sizeof(float2));
     if (e != cudaSuccess) {
