@@ -1,6 +1,6 @@
 // layers.cuh - host side of the layers between the models' products (include/cser_layers.h); included by cser.cu.
 //
-// Kernels: drop_kernels.cuh (dropout), norm_resident.cuh and norm_kernels.cuh (group norm), layer_common.cuh (what both use).
+// Launches are cut by the rules of layer_plan.h.  Kernels: drop_kernels.cuh (dropout), norm_resident.cuh and norm_kernels.cuh (group norm), layer_common.cuh (what both use).
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -10,15 +10,12 @@
 namespace {
 namespace layers {
 
+#include "layer_plan.h"
 #include "layer_common.cuh"
 #include "drop_kernels.cuh"
 #include "norm_kernels.cuh"
 #include "norm_resident.cuh"
 
-constexpr long long kBusy = 148 * 8;                   // blocks of 256 threads that fill the GPU; a constant, so that sums do not depend on the GPU
-constexpr long long kMostBlocks = 0x7fffffff;
-
-long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
 int size_of(int type) { return type == CSER_TYPE_F32 ? 4 : 2; }
 bool aligned(const void *p, int to) { return (uintptr_t)p % to == 0; }
 
@@ -114,42 +111,9 @@ struct cser_drop {
 namespace {
 namespace layers {
 
-// Column vectors of a block and column blocks, for rows of `cols` elements in vectors of v.
-void column_blocks(long long cols, int v, int &tx, int &blocks) {
-    const long long vectors = ceil_div(cols, v);
-    tx = 1;
-    while (tx < 32 && tx < vectors) tx *= 2;
-    blocks = (int)ceil_div(vectors, tx);
-}
-
 int check_rows(const cser_rows *a, const cser_drop *h, int64_t rows, bool written, const char *what) {
     const Axis axes[2] = {{rows, a->row_stride}, {h->n, a->worker_stride}};
     return check_array(a->data, h->type, h->cols, axes, written, what);
-}
-
-// Rows of cols elements to a walked row: as many as make whole vectors, and as fill a block's 32 of them.
-long long rows_walked_as_one(long long cols, int v) {
-    const long long least = v / std::gcd(cols, (long long)v);
-    return least * std::max(1ll, ceil_div(32 * v, least * cols));
-}
-
-constexpr int kSteps = 8, kSumSteps = 16;
-// How the rows of a call are walked.
-struct Walk {
-    long long width, rows, chunk_rows, most_chunks;    // most_chunks: of this many rows or fewer
-    int tx, col_blocks, chunks;
-};
-Walk walk_of(long long rows, long long cols, int n, int v, bool dense, bool sums) {
-    Walk k;
-    const long long fold = dense ? rows_walked_as_one(cols, v) : 1;
-    k.width = fold * cols, k.rows = dense ? ceil_div(rows * cols + v - 1, k.width) : rows;
-    column_blocks(k.width, v, k.tx, k.col_blocks);
-    // Each thread kSteps rows, or fewer, but four, where that leaves the GPU idle.
-    const long long step = 256 / k.tx, most = ceil_div(k.rows, 4 * step), want = ceil_div(kBusy, (long long)k.col_blocks * n);
-    k.most_chunks = std::min(most, std::max(want, ceil_div(k.rows, (sums ? kSumSteps : kSteps) * step)));
-    k.chunk_rows = ceil_div(k.rows, k.most_chunks);
-    k.chunks = (int)ceil_div(k.rows, k.chunk_rows);
-    return k;
 }
 
 template <typename T, int MODE, bool SHIFTED> cudaError_t drop_rows_launch(const DropArgs<T> &a, unsigned grid, bool sums, cudaStream_t st) {
@@ -332,6 +296,9 @@ int vector_of(const cser_norm *h, const cser_norm_inputs *in, const cser_pixels 
     return v;
 }
 
+NormSizes sizes_of(const cser_norm *h, const cser_norm_inputs *in) {
+    return {size_of(h->type), h->n, in->samples, in->pixels, h->channels, h->groups, h->drop};
+}
 View view_of(const cser_pixels *a) { return {(long long)a->pixel_stride, (long long)a->sample_stride, (long long)a->worker_stride}; }
 
 template <typename T> NormArgs<T> norm_args(const cser_norm *h, const cser_norm_inputs *in, float *stats) {
@@ -371,51 +338,6 @@ template <typename T, typename F> int with_vector(int v, F f) {
     return v == 2 ? f(std::integral_constant<int, 2>()) : f(std::integral_constant<int, 1>());
 }
 
-// How a call is made in one walk, with v elements a vector; false: it does not fit, or vectors are too short for asynchronous copies.
-// Clusters cost more than narrow slices: the fewest blocks that hold a slice of 64 bytes of a pixel at two blocks to an SM, then of 32, then at
-// one to an SM (8 x 16 x 56 x 56 x 256 in bf16, forward: 64 bytes by 2 blocks 86 us, 128 by 4 96, 128 by 8 at four to an SM 100, 32 by one
-// 106; gradient 133 by 4 and 156 of 128 bytes by 8).  Blocks of 256 threads, or of 128 where four fit an SM (28 x 28 x 256 forward 89 and
-// 115 us).  Few units are spread over more blocks, at four pixels a thread and more.
-bool plan_resident(const cser_norm *h, const cser_norm_inputs *in, int v, bool two, Resident &r, size_t &shared) {
-    const int size = size_of(h->type), per_group = (int)(h->channels / h->groups);
-    if (v * size < 4) return false;
-    const long long least = std::lcm(per_group, v) / v, all = h->channels / v, samples = (long long)h->n * in->samples;
-    bool found = false;
-    // 64 bytes, or more where a unit would be less than 16 KB and there are enough.
-    long long widest = 64;
-    while (widest < 4096 && widest * in->pixels < 16 << 10 && samples * ceil_div(h->channels * size, 2 * widest) >= kBusy / 2) widest *= 2;
-    for (size_t most : {size_t(112) << 10, size_t(220) << 10}) {
-        for (long long bytes : {widest, 32ll}) {
-            r = Resident{};
-            r.fold = std::gcd(per_group, v);
-            const long long vectors = std::min(all, least * ceil_div(bytes, least * v * size)), slices = ceil_div(all, vectors);
-            if (vectors > 128 || samples * slices > kMostBlocks / 8) continue;
-            r.sv = (int)vectors, r.slices = (uint32_t)slices, r.units = (uint32_t)(samples * slices);
-            while (1 << r.log_tx < r.sv) ++r.log_tx;
-            auto cut = [&](int log_cluster) {          // by so many blocks: bytes of shared memory of one
-                r.log_cluster = log_cluster, r.per = (int)ceil_div(in->pixels, 1 << log_cluster);
-                for (r.log_block = 7;; ++r.log_block) {
-                    const long long slots = ceil_div(r.per, (1 << r.log_block) >> r.log_tx);
-                    if (slots > 1 << 16) return ~size_t(0);
-                    r.slots = (int)slots, shared = resident_shared(r, v, size, two, two && h->drop);
-                    if (r.log_block == 8 || shared <= size_t(55) << 10) return shared;
-                }
-            };
-            int c = 0;
-            while (cut(c) > most && c < 3) ++c;
-            if (shared > most) continue;
-            while (r.units << r.log_cluster < kBusy / 4 && c < 3 && r.per >= 4 * ((1 << r.log_block) >> r.log_tx)) cut(++c);
-            found = true;
-            break;
-        }
-        if (found) break;
-    }
-    if (!found) return false;
-    const int entries = two ? per_group : (per_group / r.fold) << r.log_cluster;
-    while (r.log_sub < 5 && 1 << r.log_sub < entries) ++r.log_sub;
-    r.group_magic = per_group == 1 ? 0 : (uint32_t)(((1ull << 32) + per_group - 1) / per_group);
-    return true;
-}
 // The call's launch: as many clusters as the GPU holds at a time, or as there are units.  How many it holds is asked once for a kernel and a
 // shape, and the kernel allowed its shared memory then (for all kernels when a handle is made, loading them took 40 ms of a process).
 template <typename T>
@@ -432,7 +354,7 @@ int resident_launch(cser_norm *h, void (*kernel)(NormArgs<T>, Resident), const N
         at[0].val.clusterDim.x = 1u << r.log_cluster, at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
         cfg.attrs = at, cfg.numAttrs = 1;
         fit->kernel = nullptr;
-        TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 << 10));
+        TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostShared));
         TRY(cudaOccupancyMaxActiveClusters(&fit->clusters, kernel, &cfg));
         fit->kernel = (const void *)kernel, fit->log_cluster = r.log_cluster, fit->log_block = r.log_block, fit->shared = shared;
     }
@@ -452,7 +374,7 @@ template <typename T> int norm_apply(cser_norm *h, const cser_norm_inputs *in, c
         if constexpr (V * sizeof(T) >= 4) {
             Resident r;
             size_t shared;
-            if (plan_resident(h, in, V, false, r, shared)) {
+            if (plan_resident(sizes_of(h, in), V, false, r, shared)) {
                 return resident_launch<T>(h, h->drop ? norm_resident_kernel<T, V, true> : norm_resident_kernel<T, V, false>, a, r, shared, st);
             }
         }
@@ -480,7 +402,7 @@ int norm_grad(cser_norm *h, const cser_norm_inputs *in, const float *stats, cons
         if constexpr (V * sizeof(T) >= 4) {
             Resident r;
             size_t shared;
-            if (plan_resident(h, in, V, true, r, shared)) {
+            if (plan_resident(sizes_of(h, in), V, true, r, shared)) {
                 // A worker's only sample's sums are its gradients; those of several are added up behind.
                 a.chunks = 1, done = true, direct = a.samples == 1;
                 a.sums[0] = direct ? dbias : h->part, a.sums_sample[0] = direct ? dbias_stride : a.channels;

@@ -16,13 +16,6 @@
 #pragma once
 
 constexpr int kMostThreads = 256;
-struct Resident {
-    int sv, log_tx, log_block, log_cluster, slots;     // sv: vectors of a slice; log_block: threads; slots: of a thread and array
-    int fold, log_sub;                                 // neighbouring channels of a vector that share a group; lanes of a group's sums
-    uint32_t group_magic;                              // 2^32 / channels of a group, rounded up; 0 for one
-    int per;                                           // pixels of a block
-    uint32_t slices, units;                            // of a sample, and of all
-};
 
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
@@ -91,13 +84,6 @@ template <typename T, int V> struct Stand {
         }
     }
 };
-// Bytes of shared memory of the above.
-inline size_t resident_shared(const Resident &r, int v, int size, bool two, bool bits) {
-    const int width = (1 << r.log_tx) * v, rows = std::min(1 << (r.log_block - r.log_tx), 1 << (r.log_block - 5));
-    const size_t sums = width / (two ? 1 : r.fold);
-    return ((size_t)r.slots << r.log_block) * (v * size * (two ? 2 : 1) + (bits ? 1 : 0)) + (size_t)(6 + 2 * rows) * width * 4 + (4 << r.log_cluster) * sums * 4;
-}
-
 // Leaves a thread's N sums (lanes joined already) for the block: row of sums, two planes.
 template <int N> __device__ __forceinline__ void leave_row(float *red, int log_tx, const float (&p)[N], const float (&q)[N]) {
     const int sums = N << log_tx, rows = min((int)blockDim.x >> log_tx, (int)blockDim.x / 32), row = log_tx > 5 ? threadIdx.x >> log_tx : threadIdx.x >> 5;

@@ -1,0 +1,57 @@
+"""How the layers' launches are cut (layer_plan.h), checked on the host for sizes that no test could hold on a GPU."""
+import ctypes
+import os
+import subprocess
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+class Resident(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_int) for k in ("sv", "log_tx", "log_block", "log_cluster", "slots", "fold", "log_sub")] + \
+               [("group_magic", ctypes.c_uint32), ("per", ctypes.c_int), ("slices", ctypes.c_uint32), ("units", ctypes.c_uint32)]
+
+
+@pytest.fixture(scope="module")
+def rules(tmp_path_factory):
+    out = str(tmp_path_factory.mktemp("plan") / "plan.so")
+    res = subprocess.run(["g++", "-std=c++17", "-O2", "-Wall", "-Wno-unused-function", "-shared", "-fPIC", "-I",
+                          os.path.join(ROOT, "paper_2007_13221_b200", "csrc"), os.path.join(ROOT, "tests", "layer_plan_check.cpp"), "-o", out],
+                         capture_output=True, text=True)
+    assert res.returncode == 0, res.stderr
+    return ctypes.CDLL(out)
+
+
+def plan(rules, size, n, samples, pixels, channels, groups, drop, v, two, preset=0):
+    """(plan, bytes of shared memory) or None."""
+    r, shared = Resident(), ctypes.c_uint64()
+    found = rules.plan_norm((ctypes.c_int64 * 7)(size, n, samples, pixels, channels, groups, drop), v, int(two), ctypes.c_uint64(preset),
+                            ctypes.byref(shared), ctypes.byref(r))
+    return (r, shared.value) if found else None
+
+
+@pytest.mark.parametrize("preset", [0, 1000, 2 ** 64 - 1])
+@pytest.mark.parametrize("size,pixels,channels,groups", [(4, 4_300_000, 64, 1), (2, 640_000, 1024, 1), (2, 25_000_000, 32, 1), (4, 2 ** 31 - 1, 4, 1)])
+def test_samples_of_too_many_pixels_are_refused_whatever_memory_held_before(rules, size, pixels, channels, groups, preset):
+    for two in (False, True):
+        for drop in (False, True):
+            assert plan(rules, size, 1, 1, pixels, channels, groups, drop, 16 // size, two, preset) is None
+
+
+def test_a_plan_holds_what_it_is_for(rules):
+    """Slots for every pixel of a block, blocks for every pixel of a sample, slices of whole groups for every channel."""
+    for size, v in ((2, 8), (2, 4), (2, 2), (4, 4), (4, 2), (4, 1)):
+        for channels, groups in ((64, 32), (64, 1), (96, 3), (1000, 125), (2048, 64), (120, 120), (24, 24)):
+            if channels % v:
+                continue
+            for pixels in (1, 2, 31, 64, 100, 784, 3136, 12544, 70000, 10 ** 7):
+                for n, samples, two, drop in ((1, 1, True, True), (8, 16, False, False), (8, 16, True, False), (2, 700, True, True)):
+                    got = plan(rules, size, n, samples, pixels, channels, groups, drop, v, two)
+                    if got is None:
+                        continue
+                    r, _ = got
+                    assert r.log_block in (7, 8) and 0 <= r.log_cluster <= 3 and r.sv <= 1 << r.log_tx <= 128
+                    assert r.per << r.log_cluster >= pixels and r.slots << (r.log_block - r.log_tx) >= r.per
+                    assert r.slices * r.sv * v >= channels and r.units == n * samples * r.slices
+                    assert r.sv * v % (channels // groups) == 0

@@ -253,3 +253,12 @@ def test_between_the_other_operators():
     for _ in range(20):
         got = step(lambda: None)
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_a_sample_of_so_many_pixels_that_no_thread_has_slots_for_its_own():
+    """More than 2^16 pixels a thread of a cluster: three kernels forward.  A thread of theirs has about 112 pixels, then 600 parts are joined."""
+    from test_layers import check_norm, norm_inputs
+    x, weight, bias, dy = norm_inputs(11, 1, 1, (530000,), 127, F32)
+    op = layers.GroupNorm(1, 1, 127, 1, "silu", dtype=F32)
+    check_norm(op, x, weight, bias, dy, 1, "silu", chain=256)
+    assert op.launches == 3 + 4
