@@ -85,7 +85,7 @@ bool plan_resident(const NormSizes &k, int v, bool two, Resident &r, size_t &sha
             if (vectors > 128 || samples * slices > kMostBlocks / 8) continue;
             r.sv = (int)vectors, r.slices = (uint32_t)slices, r.units = (uint32_t)(samples * slices);
             while (1 << r.log_tx < r.sv) ++r.log_tx;
-            auto cut = [&](int log_cluster) -> size_t {          // by so many blocks: bytes of shared memory of one
+            auto cut = [&](Resident &r, int log_cluster) -> size_t {          // by so many blocks: bytes of shared memory of one
                 r.log_cluster = log_cluster, r.per = (int)ceil_div(k.pixels, 1 << log_cluster);
                 for (r.log_block = 7;; ++r.log_block) {
                     const long long slots = ceil_div(r.per, (1 << r.log_block) >> r.log_tx);
@@ -96,9 +96,14 @@ bool plan_resident(const NormSizes &k, int v, bool two, Resident &r, size_t &sha
                 }
             };
             int c = 0;
-            for (shared = cut(c); shared > most && c < 3;) shared = cut(++c);
+            for (shared = cut(r, c); shared > most && c < 3;) shared = cut(r, ++c);
             if (shared > most) continue;
-            while (r.units << r.log_cluster < kBusy / 4 && c < 3 && r.per >= 4 * ((1 << r.log_block) >> r.log_tx)) shared = cut(++c);
+            while (r.units << r.log_cluster < kBusy / 4 && c < 3 && r.per >= 4 * ((1 << r.log_block) >> r.log_tx)) {
+                Resident more = r;
+                const size_t bytes = cut(more, ++c);
+                if (bytes > kMostShared) break;        // (the sums that more blocks exchange can outweigh the pixels that each has less)
+                r = more, shared = bytes;
+            }
             found = true;
             break;
         }

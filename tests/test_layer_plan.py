@@ -55,3 +55,19 @@ def test_a_plan_holds_what_it_is_for(rules):
                     assert r.per << r.log_cluster >= pixels and r.slots << (r.log_block - r.log_tx) >= r.per
                     assert r.slices * r.sv * v >= channels and r.units == n * samples * r.slices
                     assert r.sv * v % (channels // groups) == 0
+
+
+def test_no_plan_needs_more_shared_memory_than_a_block_has(rules):
+    """220 KB, which is what the kernels are allowed; few units of wide slices are spread over more blocks, whose exchanged sums take more."""
+    for size in (2, 4):
+        for v in [k for k in (1, 2, 4, 8) if 4 <= k * size <= 16]:
+            for drop in (False, True):
+                for two in (False, True):
+                    for per_group in (1, 3, 8, 12, 64, 100, 128, 256, 300, 512, 1000, 1024):
+                        for groups in (1, 2, 4, 32):
+                            if per_group * groups % v:
+                                continue
+                            for samples in (1, 8, 74, 1000):
+                                for pixels in (1, 7, 20, 49, 64, 97, 100, 104, 108, 112, 120, 196, 400, 784, 1000, 3136):
+                                    got = plan(rules, size, 1, samples, pixels, per_group * groups, groups, drop, v, two)
+                                    assert got is None or got[1] <= 220 * 1024, (size, v, drop, two, per_group, groups, samples, pixels)

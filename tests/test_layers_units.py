@@ -262,3 +262,12 @@ def test_a_sample_of_so_many_pixels_that_no_thread_has_slots_for_its_own():
     op = layers.GroupNorm(1, 1, 127, 1, "silu", dtype=F32)
     check_norm(op, x, weight, bias, dy, 1, "silu", chain=256)
     assert op.launches == 3 + 4
+
+
+@pytest.mark.parametrize("size", [(1, 1, 100, 1024, 1, BF), (1, 2, 104, 600, 2, HF), (1, 1, 101, 512, 1, F32)], ids=str)
+def test_few_samples_of_wide_groups(size):
+    """Gradients whose blocks' shared memory is nearly used up."""
+    from test_layers import check_norm, norm_inputs
+    n, b, pixels, c, groups, dtype = size
+    x, weight, bias, dy = norm_inputs(12, n, b, (pixels,), c, dtype)
+    check_norm(layers.GroupNorm(n, b, c, groups, "silu", dtype=dtype), x, weight, bias, dy, groups, "silu")
