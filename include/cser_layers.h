@@ -47,7 +47,9 @@ typedef struct cser_rows {
 /*
  * Handle for up to max_rows rows a worker.  0 <= p < 1 (and floor(p * 2^32) < 2^32); 1 <= site < 2^20: one number for each place of the
  * model that drops; first_worker >= 0 and first_worker + n_workers <= 4096; max_rows * cols <= 2^34.
- * The workspace, for sums of dbias, is 4 bytes for every 128 elements or so, and 5 MB at least where there are many.  Returns NULL on failure.
+ * The workspace, for sums of dbias, is none for a single row a worker, else 4 bytes for every 128 elements, up to 1.3 MB more where there are few, and
+ * for each worker 1 KB and 4 bytes for each element of two of its rows, or of nine (five in 32 bits) where it has that many and 16 bytes do
+ * not divide them.  Returns NULL on failure.
  */
 cser_drop_handle cser_drop_create(int32_t n_workers, int64_t max_rows, int64_t cols, double p, uint64_t seed, uint32_t site,
                                   int32_t first_worker, int32_t type);

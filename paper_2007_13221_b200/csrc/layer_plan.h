@@ -21,6 +21,8 @@ long long rows_walked_as_one(long long cols, int v) {
     const long long least = v / std::gcd(cols, (long long)v);
     return least * std::max(1ll, ceil_div(32 * v, least * cols));
 }
+// Whether a call of this many rows has one such row.  Fewer are walked as they are: most of a longer row would not exist.
+bool walked_as_one(long long rows, long long cols, int v) { return rows >= rows_walked_as_one(cols, v); }
 
 constexpr int kSteps = 8, kSumSteps = 16;
 // How the rows of a call are walked.
@@ -39,6 +41,17 @@ Walk walk_of(long long rows, long long cols, int n, int v, bool dense, bool sums
     k.chunk_rows = ceil_div(k.rows, k.most_chunks);
     k.chunks = (int)ceil_div(k.rows, k.chunk_rows);
     return k;
+}
+
+// Floats a worker for the sums of up to max_rows rows, of which any call may have fewer; 0 where one chunk's sums are the result.
+long long sums_of(long long max_rows, long long cols, int n, int v) {
+    long long sums = 0;
+    for (bool dense : {false, true}) {                 // walked either way
+        if (dense && !walked_as_one(max_rows, cols, v)) continue;
+        const Walk k = walk_of(max_rows, cols, n, v, dense, true);
+        if (k.most_chunks > 1 || k.width != cols) sums = std::max(sums, k.most_chunks * k.width);
+    }
+    return sums;
 }
 
 // ------------------------------------------------------------------ group norm in one walk

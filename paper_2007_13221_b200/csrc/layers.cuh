@@ -149,7 +149,7 @@ int drop_launch(cser_drop *h, int64_t rows, const Draw &draw, const cser_rows *x
         h->launches++;
         return CSER_OK;
     }
-    dense = dense && !(plain && h->cols >= 32 * V);    // wide rows of whole vectors: the simpler walk
+    dense = dense && !(plain && h->cols >= 32 * V) && walked_as_one(rows, h->cols, V);         // wide rows of whole vectors: the simpler walk
     const Walk k = walk_of(rows, h->cols, h->n, V, dense, dbias);
     a.width = k.width, a.chunk_rows = k.chunk_rows, a.tx = k.tx, a.log_rows = 8 - (int)std::log2(k.tx);
     a.walked = dense ? ceil_div(rows * h->cols, k.width) : rows, a.last_row = rows * h->cols - (a.walked - 1) * k.width;
@@ -197,12 +197,7 @@ cser_drop_handle cser_drop_create(int32_t n_workers, int64_t max_rows, int64_t c
     if (!h) return bad(CSER_ERR_NOMEM, "host allocation failed");
     h->n = n_workers, h->max_rows = max_rows, h->cols = cols, h->p = p, h->seed = seed, h->site = site, h->first_worker = first_worker,
     h->type = type;
-    // Walked either way.
-    long long sums = 0;
-    for (bool dense : {false, true}) {
-        const layers::Walk k = layers::walk_of(max_rows, cols, n_workers, 16 / layers::size_of(type), dense, true);
-        sums = std::max(sums, k.most_chunks * k.width);
-    }
+    const long long sums = layers::sums_of(max_rows, cols, n_workers, 16 / layers::size_of(type));
     cudaError_t e = cudaGetDevice(&h->device);
     if (e == cudaSuccess) e = cudaMalloc(&h->part, (size_t)(n_workers * sums) * 4);
     if (e != cudaSuccess) {

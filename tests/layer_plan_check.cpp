@@ -17,3 +17,10 @@ extern "C" int plan_norm(const int64_t *sizes, int v, int two, uint64_t preset, 
     *shared = bytes;
     return found;
 }
+
+// Floats a worker of a dropout's workspace, and of its sums for one call.
+extern "C" int64_t drop_sums(int64_t max_rows, int64_t cols, int n, int v) { return sums_of(max_rows, cols, n, v); }
+extern "C" int64_t drop_used(int64_t rows, int64_t cols, int n, int v, int dense) {
+    const Walk k = walk_of(rows, cols, n, v, dense && walked_as_one(rows, cols, v), true);
+    return k.chunks == 1 && k.width == cols ? 0 : k.chunks * k.width;
+}

@@ -20,7 +20,11 @@ def rules(tmp_path_factory):
                           os.path.join(ROOT, "paper_2007_13221_b200", "csrc"), os.path.join(ROOT, "tests", "layer_plan_check.cpp"), "-o", out],
                          capture_output=True, text=True)
     assert res.returncode == 0, res.stderr
-    return ctypes.CDLL(out)
+    lib = ctypes.CDLL(out)
+    i64, i32 = ctypes.c_int64, ctypes.c_int
+    lib.drop_sums.restype, lib.drop_sums.argtypes = i64, [i64, i64, i32, i32]
+    lib.drop_used.restype, lib.drop_used.argtypes = i64, [i64, i64, i32, i32, i32]
+    return lib
 
 
 def plan(rules, size, n, samples, pixels, channels, groups, drop, v, two, preset=0):
@@ -71,3 +75,31 @@ def test_no_plan_needs_more_shared_memory_than_a_block_has(rules):
                                 for pixels in (1, 7, 20, 49, 64, 97, 100, 104, 108, 112, 120, 196, 400, 784, 1000, 3136):
                                     got = plan(rules, size, 1, samples, pixels, per_group * groups, groups, drop, v, two)
                                     assert got is None or got[1] <= 220 * 1024, (size, v, drop, two, per_group, groups, samples, pixels)
+
+
+SUMS = [(1, 1), (1, 1001), (1, 2 ** 20 + 1), (1, 2 ** 30 + 1), (2, 1001), (7, 10001), (8, 10001), (9, 1001), (100, 10001), (33, 64), (1000, 1), (65536, 3),
+        (10 ** 6, 7), (4096, 1024), (8192, 4096), (77, 201), (9999, 1111), (2 ** 20, 16384), (2 ** 34, 1), (5, 2 ** 31 + 5)]
+
+
+@pytest.mark.parametrize("n", [1, 8, 300])
+@pytest.mark.parametrize("v", [4, 8])
+def test_a_dropout_s_workspace_is_as_small_as_stated(rules, n, v):
+    """4 bytes for every 128 elements, 1.3 MB at most where there are few, and a walked row (v rows, or 32 vectors and a row of them) a worker."""
+    for rows, cols in SUMS:
+        if rows * cols * n > 2 ** 34:
+            continue
+        got, folded = 4 * n * rules.drop_sums(rows, cols, n, v), v * cols if rows >= v else cols
+        assert got <= 4 * n * rows * cols / 128 + 1.3e6 + 4 * n * (folded + 32 * v + cols), (rows, cols, got)
+        if rows == 1:
+            assert got == 0
+
+
+@pytest.mark.parametrize("v", [4, 8])
+def test_a_dropout_s_workspace_holds_any_call(rules, v):
+    for n in (1, 3, 64):
+        for most, cols in SUMS:
+            room = rules.drop_sums(most, cols, n, v)
+            for rows in {1, 2, 3, 7, 8, 9, 31, 32, 33, 100, 129, most // 3, most // 2, most - 1, most}:
+                if 1 <= rows <= most:
+                    for dense in (0, 1):
+                        assert rules.drop_used(rows, cols, n, v, dense) <= room, (n, most, cols, rows, dense)

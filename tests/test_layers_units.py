@@ -271,3 +271,24 @@ def test_few_samples_of_wide_groups(size):
     n, b, pixels, c, groups, dtype = size
     x, weight, bias, dy = norm_inputs(12, n, b, (pixels,), c, dtype)
     check_norm(layers.GroupNorm(n, b, c, groups, "silu", dtype=dtype), x, weight, bias, dy, groups, "silu")
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=str)
+@pytest.mark.parametrize("size", [(1, 1, 2 ** 20 + 1), (8, 1, 1001), (2, 5, 4099), (3, 7, 1001), (3, 8, 1001), (1, 100, 10001)], ids=str)
+def test_few_rows_of_columns_that_no_vector_divides(size, dtype):
+    """Against the formula; a call with fewer rows than the handle is for sums as many."""
+    from test_layers import SEED, check_drop, gen_of, mask, normal
+    n, rows, cols = size
+    gen = gen_of(13)
+    x, r, dy = (normal(gen, *size).to(dtype) for _ in range(3))
+    bias = normal(gen, n, cols)
+    for most in (rows, 9 * rows):
+        check_drop(layers.Dropout(n, most, cols, 0.3, SEED, 3, dtype), x, bias, r, dy, 0.3, mask(n, rows * cols, 0.3))
+
+
+def test_a_handle_for_one_wide_row_takes_no_memory():
+    torch.cuda.synchronize()
+    before = torch.cuda.mem_get_info()[0]
+    op = layers.Dropout(1, 1, 2 ** 25 + 1, 0.1, 0, 1)
+    assert before - torch.cuda.mem_get_info()[0] < 2 ** 23          # (another process's share of the card may move a little)
+    op.close()
