@@ -200,8 +200,8 @@ class Dropout(_Handle):
 class GroupNorm(_Handle):
     """Group norm with an activation ("none", "relu" or "silu") of [n, samples, ..., channels] arrays, up to ``max_samples`` a worker.
 
-    dropout: a ``Dropout`` for the same workers, channels and type; x then counts as dropout(x), and step is the dropout's.  It is
-    copied.  See cser_norm_create.
+    dropout: a ``Dropout`` for the same workers, channels and type; x then counts as dropout(x), and every call needs the dropout's step.
+    It is copied.  See cser_norm_create.
     """
     _kind = "norm"
 
@@ -211,7 +211,7 @@ class GroupNorm(_Handle):
         _want(activation in ACTIVATIONS, 'GroupNorm: activations are "none", "relu" and "silu"')
         _want(dropout is None or dropout.h is not None, "GroupNorm: the dropout is closed")
         self.n, self.max_samples, self.channels, self.groups = int(n_workers), int(max_samples), int(channels), int(groups)
-        self.dtype = dtype
+        self.dtype, self.drops = dtype, dropout is not None
         h = lib().cser_norm_create(self.n, self.max_samples, self.channels, self.groups, ACTIVATIONS[activation], float(eps), TYPES[dtype],
                                    None if dropout is None else dropout.h)
         if not h:
@@ -246,15 +246,18 @@ class GroupNorm(_Handle):
         return torch.empty((self.n, self.channels), dtype=torch.float32, device=x.device)
 
     def _inputs(self, x, weight, bias, step):
+        if step is None:                                  # (one left out would mean one mask for ever, or another one in the gradient)
+            _want(not self.drops, "GroupNorm: with a dropout each call needs its step")
+            step = 0
         pixels, xs = self._array("x", x)
         step, step_at = _step(step)
         w, w_stride = _params("GroupNorm: weight", weight, self.n, self.channels)
         b, b_stride = _params("GroupNorm: bias", bias, self.n, self.channels)
         return _NormInputs(xs, w, b, w_stride, b_stride, x.shape[1], pixels, step, step_at)
 
-    def apply(self, x, weight=None, bias=None, step=0, out=None, stream=None):
+    def apply(self, x, weight=None, bias=None, step=None, out=None, stream=None):
         """(act(norm(x) * weight + bias), stats); weight and bias fp32 [n, channels] or None.  stats, fp32 [2, n, samples, groups] (mean and
-        1 / deviation), is what grad takes.  out may be x."""
+        1 / deviation), is what grad takes.  step: of the dropout, where there is one.  out may be x."""
         if stream is not None:
             return _on(stream, self.apply, x, weight, bias, step, out)
         args = self._inputs(x, weight, bias, step)
@@ -268,7 +271,7 @@ class GroupNorm(_Handle):
         _check(_lib.cser_norm_apply(self.h, args, ys, stats.data_ptr(), _raw_stream(x)), "cser_norm_apply")
         return out, stats
 
-    def grad(self, x, dy, stats, weight=None, bias=None, step=0, dx=None, dweight=None, dbias=None, need_dx=True, need_params=True,
+    def grad(self, x, dy, stats, weight=None, bias=None, step=None, dx=None, dweight=None, dbias=None, need_dx=True, need_params=True,
              stream=None):
         """(dx, dweight, dbias) of sum(dy * apply(x, weight, bias, step)[0]).  dx may be x or dy; dweight and dbias may be views of a flat
         [n, d] gradient."""

@@ -61,3 +61,20 @@ def test_norms_of_too_many_groups_are_refused():
     from paper_2007_13221_b200.binding import CSERError
     with pytest.raises(CSERError, match="2\\^31"):
         layers.GroupNorm(2, 2 ** 23, 256, 128)
+
+
+def test_a_norm_with_a_dropout_needs_the_step():
+    """Refused before anything else of a call is looked at; a norm without a dropout goes on to its arrays."""
+    import pytest
+    import torch
+    from paper_2007_13221_b200 import layers
+    from paper_2007_13221_b200.binding import CSERError
+    op = object.__new__(layers.GroupNorm)
+    op.h, op.n, op.max_samples, op.channels, op.groups, op.dtype = None, 1, 2, 8, 2, torch.float32
+    x = torch.zeros((1, 2, 3, 8))
+    for drops, match in ((True, "step"), (False, "CUDA")):
+        op.drops = drops
+        with pytest.raises(CSERError, match=match):
+            op.apply(x)
+        with pytest.raises(CSERError, match=match):
+            op.grad(x, x, torch.zeros((2, 1, 2, 2)))
