@@ -74,6 +74,13 @@ def _merged(name, shape, stride, first, last):
     return size, step
 
 
+def _number(what, v, bits=64):
+    """v as a signed number of so many bits, which ctypes would cut without a word."""
+    v = int(v)
+    _want(-1 << bits - 1 <= v < 1 << bits - 1, f"{what} is out of range")
+    return v
+
+
 def _step(step):
     """(64 bits of the number, device pointer) of a step given as a number or as an int64 CUDA tensor of one element."""
     if torch.is_tensor(step):
@@ -133,9 +140,10 @@ class Dropout(_Handle):
         self.h = None
         _want(dtype in TYPES, "Dropout: types are float32, bfloat16 and float16")
         _want(0 <= site < 2 ** 32, "Dropout: site must be in 1..2^20-1")
-        self.n, self.max_rows, self.cols, self.p, self.dtype = int(n_workers), int(max_rows), int(cols), float(p), dtype
-        h = lib().cser_drop_create(self.n, self.max_rows, self.cols, self.p, int(seed) & 0xFFFFFFFFFFFFFFFF, int(site), int(first_worker),
-                                   TYPES[dtype])
+        self.n, self.max_rows, self.cols = _number("Dropout: n_workers", n_workers, 32), _number("Dropout: max_rows", max_rows), _number("Dropout: cols", cols)
+        self.p, self.dtype = float(p), dtype
+        h = lib().cser_drop_create(self.n, self.max_rows, self.cols, self.p, int(seed) & 0xFFFFFFFFFFFFFFFF, int(site),
+                                   _number("Dropout: first_worker", first_worker, 32), TYPES[dtype])
         if not h:
             raise CSERError(f"cser_drop_create failed: {cser_last_error()}")
         self.h = ctypes.c_void_p(h)
@@ -210,7 +218,8 @@ class GroupNorm(_Handle):
         _want(dtype in TYPES, "GroupNorm: types are float32, bfloat16 and float16")
         _want(activation in ACTIVATIONS, 'GroupNorm: activations are "none", "relu" and "silu"')
         _want(dropout is None or dropout.h is not None, "GroupNorm: the dropout is closed")
-        self.n, self.max_samples, self.channels, self.groups = int(n_workers), int(max_samples), int(channels), int(groups)
+        self.n, self.max_samples = _number("GroupNorm: n_workers", n_workers, 32), _number("GroupNorm: max_samples", max_samples)
+        self.channels, self.groups = _number("GroupNorm: channels", channels), _number("GroupNorm: groups", groups)
         self.dtype, self.drops = dtype, dropout is not None
         h = lib().cser_norm_create(self.n, self.max_samples, self.channels, self.groups, ACTIVATIONS[activation], float(eps), TYPES[dtype],
                                    None if dropout is None else dropout.h)

@@ -78,3 +78,16 @@ def test_a_norm_with_a_dropout_needs_the_step():
             op.apply(x)
         with pytest.raises(CSERError, match=match):
             op.grad(x, x, torch.zeros((2, 1, 2, 2)))
+
+
+def test_numbers_that_the_c_types_would_cut_are_refused():
+    """2^32 as an int32 is 0: another worker's mask, silently."""
+    import pytest
+    from paper_2007_13221_b200 import layers
+    from paper_2007_13221_b200.binding import CSERError
+    for kw in (dict(n_workers=2 ** 32 + 1), dict(max_rows=2 ** 64 + 1), dict(cols=2 ** 64 + 1), dict(first_worker=2 ** 32), dict(first_worker=-2 ** 32)):
+        with pytest.raises(CSERError, match=next(iter(kw))):
+            layers.Dropout(**{**dict(n_workers=1, max_rows=1, cols=1, p=0.5, seed=0, site=1), **kw})
+    for kw in (dict(n_workers=2 ** 32 + 1), dict(max_samples=2 ** 64 + 1), dict(channels=2 ** 64 + 8), dict(groups=2 ** 64 + 2)):
+        with pytest.raises(CSERError, match=next(iter(kw))):
+            layers.GroupNorm(**{**dict(n_workers=1, max_samples=1, channels=8, groups=2), **kw})
