@@ -56,8 +56,8 @@ cser_drop_handle cser_drop_create(int32_t n_workers, int64_t max_rows, int64_t c
 /*
  * step: 64 bits, any; step_at: NULL, or device memory holding a number that is added to step (modulo 2^64) when the call runs, so that a
  * replayed graph draws anew.  bias: fp32 [n_workers][cols], bias_stride elements from one worker's to the next (a part of the flat
- * state, say), or NULL.  residual: or NULL.  y may be x or residual itself (same pointer and strides); otherwise what is written must not
- * share elements with what is read.
+ * state, say), or NULL.  residual: or NULL.  y may be x or residual itself (same pointer and strides); otherwise what a call writes must not
+ * share memory with its other arrays (here and below).  Refused where the two have the same strides or one has no gaps.
  */
 int cser_drop_apply(cser_drop_handle h, int64_t rows, uint64_t step, const uint64_t *step_at, const cser_rows *x,
                     const float *bias, int64_t bias_stride, const cser_rows *residual, const cser_rows *y, void *stream);
@@ -114,7 +114,7 @@ typedef struct cser_norm_inputs {
 cser_norm_handle cser_norm_create(int32_t n_workers, int64_t max_samples, int64_t channels, int64_t groups, int32_t act, float eps,
                                   int32_t type, cser_drop_handle drop);
 /* stats: fp32 [2, n_workers, samples, groups], dense: mean, then rstd; what cser_norm_grad takes.  y may be x itself (same pointer and
- * strides); otherwise what is written must not share elements with what is read.  With pixels = 0 the stats become 0. */
+ * strides).  With pixels = 0 the stats become 0. */
 int cser_norm_apply(cser_norm_handle h, const cser_norm_inputs *in, const cser_pixels *y, float *stats, void *stream);
 /* stats: as cser_norm_apply gave them for the same inputs.  dx: or NULL; may be x or dy itself.  dweight, dbias: fp32 [n_workers][channels],
  * dweight_stride and dbias_stride (>= channels) elements from one worker's to the next, or NULL; 0 where samples or pixels are 0. */

@@ -1,6 +1,6 @@
 // layers.cuh - host side of the layers between the models' products (include/cser_layers.h); included by cser.cu.
 //
-// Launches are cut by the rules of layer_plan.h.  Kernels: drop_kernels.cuh (dropout), norm_resident.cuh and norm_kernels.cuh (group norm), layer_common.cuh (what both use).
+// Launches are cut by the rules of layer_plan.h, arrays told apart by layer_arrays.h.  Kernels: drop_kernels.cuh (dropout), norm_resident.cuh and norm_kernels.cuh (group norm), layer_common.cuh (what both use).
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -10,6 +10,7 @@
 namespace {
 namespace layers {
 
+#include "layer_arrays.h"
 #include "layer_plan.h"
 #include "layer_common.cuh"
 #include "drop_kernels.cuh"
@@ -36,7 +37,6 @@ int check_params(const float *p, int64_t stride, int64_t least, int n, const cha
 
 // An array whose innermost `run` elements are contiguous, with these axes around them.  What is written must not lie on itself: from the
 // closest axis to the widest, each has to step over all that is inside.
-struct Axis { int64_t size, stride; };
 template <int N> int check_array(const void *data, int type, int64_t run, const Axis (&given)[N], bool written, const char *what) {
     if (int rc = check_device_ptr(data, what)) return rc;
     if (!aligned(data, size_of(type))) return fail(CSER_ERR_INVALID, "%s: a pointer is not aligned to its element type", what);
@@ -53,6 +53,24 @@ template <int N> int check_array(const void *data, int type, int64_t run, const 
             span += (__int128)(a.size - 1) * a.stride;
         }
     return span <= (1ll << 60) ? CSER_OK : fail(CSER_ERR_INVALID, "%s: its strides are too large", what);
+}
+
+// What a call writes shares no memory with its other arrays, but a result may take the place of an input: all of it.
+struct Given {
+    const char *name;
+    Array array;
+    bool written, replaces;                            // replaces: a result, or an input that one may replace
+};
+template <int N> int check_apart(const Given (&all)[N], const char *what) {
+    for (const Given &w : all)
+        for (const Given &o : all)
+            if (w.written && w.array.at && o.array.at && &w != &o && shares(w.array, o.array) && !(w.replaces && o.replaces && same(w.array, o.array)))
+                return fail(CSER_ERR_INVALID, "%s: %s and %s share memory", what, w.name, o.name);
+    return CSER_OK;
+}
+Array params_of(const float *p, int64_t stride, int64_t count, int n) {
+    const Axis axes[1] = {{n, stride}};
+    return p ? array_of(p, count, axes, 4) : Array();
 }
 
 int check_step_at(const uint64_t *p) {
@@ -114,6 +132,11 @@ namespace layers {
 int check_rows(const cser_rows *a, const cser_drop *h, int64_t rows, bool written, const char *what) {
     const Axis axes[2] = {{rows, a->row_stride}, {h->n, a->worker_stride}};
     return check_array(a->data, h->type, h->cols, axes, written, what);
+}
+Array rows_of(const cser_rows *a, const cser_drop *h, int64_t rows) {
+    if (!a) return Array();
+    const Axis axes[2] = {{rows, a->row_stride}, {h->n, a->worker_stride}};
+    return array_of(a->data, h->cols, axes, size_of(h->type));
 }
 
 template <typename T, int MODE, bool SHIFTED> cudaError_t drop_rows_launch(const DropArgs<T> &a, unsigned grid, bool sums, cudaStream_t st) {
@@ -223,6 +246,11 @@ int cser_drop_apply(cser_drop_handle h, int64_t rows, uint64_t step, const uint6
     if (bias)
         if (int rc = check_params(bias, bias_stride, 0, h->n, "cser_drop_apply: bias")) return rc;
     if (int rc = check_step_at(step_at)) return rc;
+    const Given all[] = {{"y", rows_of(y, h, rows), true, true},
+                         {"x", rows_of(x, h, rows), false, true},
+                         {"residual", rows_of(residual, h, rows), false, true},
+                         {"bias", params_of(bias, bias_stride, h->cols, h->n), false, false}};
+    if (int rc = check_apart(all, "cser_drop_apply")) return rc;
     return drop_call(h, rows, step, step_at, x, bias, bias_stride, residual, y, nullptr, 0, (cudaStream_t)stream);
 }
 
@@ -241,6 +269,10 @@ int cser_drop_grad(cser_drop_handle h, int64_t rows, uint64_t step, const uint64
     if (dx)
         if (int rc = check_rows(dx, h, rows, true, "cser_drop_grad: dx")) return rc;
     if (int rc = check_step_at(step_at)) return rc;
+    const Given all[] = {{"dx", rows_of(dx, h, rows), true, true},
+                         {"dy", rows_of(dy, h, rows), false, true},
+                         {"dbias", params_of(dbias, dbias_stride, h->cols, h->n), true, false}};
+    if (int rc = check_apart(all, "cser_drop_grad")) return rc;
     return drop_call(h, rows, step, step_at, dy, nullptr, 0, nullptr, dx, dbias, dbias_stride, (cudaStream_t)stream);
 }
 
@@ -278,6 +310,15 @@ namespace layers {
 int check_pixels(const cser_pixels *a, const cser_norm *h, const cser_norm_inputs *in, bool written, const char *what) {
     const Axis axes[3] = {{in->pixels, a->pixel_stride}, {in->samples, a->sample_stride}, {h->n, a->worker_stride}};
     return check_array(a->data, h->type, h->channels, axes, written, what);
+}
+
+Array pixels_of(const cser_pixels *a, const cser_norm *h, const cser_norm_inputs *in) {
+    if (!a) return Array();
+    const Axis axes[3] = {{in->pixels, a->pixel_stride}, {in->samples, a->sample_stride}, {h->n, a->worker_stride}};
+    return array_of(a->data, h->channels, axes, size_of(h->type));
+}
+Array stats_of(const float *stats, const cser_norm *h, const cser_norm_inputs *in) {
+    return params_of(stats, 0, 2 * h->n * in->samples * h->groups, 1);
 }
 
 // Elements that one load or store can take from an array: the largest power of two up to 16 bytes' worth that all of its starts allow.
@@ -503,6 +544,12 @@ int cser_norm_apply(cser_norm_handle h, const cser_norm_inputs *in, const cser_p
     }
     if (!y) return fail(CSER_ERR_INVALID, "cser_norm_apply: NULL array");
     if (int rc = check_pixels(y, h, in, true, "cser_norm_apply: y")) return rc;
+    const Given all[] = {{"y", pixels_of(y, h, in), true, true},
+                         {"x", pixels_of(&in->x, h, in), false, true},
+                         {"stats", stats_of(stats, h, in), true, false},
+                         {"weight", params_of(in->weight, in->weight_stride, h->channels, h->n), false, false},
+                         {"bias", params_of(in->bias, in->bias_stride, h->channels, h->n), false, false}};
+    if (int rc = check_apart(all, "cser_norm_apply")) return rc;
     if (h->type == CSER_TYPE_F32) return norm_apply<float>(h, in, y, stats, st);
     return h->type == CSER_TYPE_BF16 ? norm_apply<__nv_bfloat16>(h, in, y, stats, st) : norm_apply<__half>(h, in, y, stats, st);
 }
@@ -527,6 +574,15 @@ int cser_norm_grad(cser_norm_handle h, const cser_norm_inputs *in, const float *
     if (int rc = check_pixels(dy, h, in, false, "cser_norm_grad: dy")) return rc;
     if (dx)
         if (int rc = check_pixels(dx, h, in, true, "cser_norm_grad: dx")) return rc;
+    const Given all[] = {{"dx", pixels_of(dx, h, in), true, true},
+                         {"x", pixels_of(&in->x, h, in), false, true},
+                         {"dy", pixels_of(dy, h, in), false, true},
+                         {"stats", stats_of(stats, h, in), false, false},
+                         {"weight", params_of(in->weight, in->weight_stride, h->channels, h->n), false, false},
+                         {"bias", params_of(in->bias, in->bias_stride, h->channels, h->n), false, false},
+                         {"dweight", params_of(dweight, dweight_stride, h->channels, h->n), true, false},
+                         {"dbias", params_of(dbias, dbias_stride, h->channels, h->n), true, false}};
+    if (int rc = check_apart(all, "cser_norm_grad")) return rc;
     if (h->type == CSER_TYPE_F32) return norm_grad<float>(h, in, stats, dy, dx, dweight, dweight_stride, dbias, dbias_stride, st);
     return h->type == CSER_TYPE_BF16 ? norm_grad<__nv_bfloat16>(h, in, stats, dy, dx, dweight, dweight_stride, dbias, dbias_stride, st)
                                      : norm_grad<__half>(h, in, stats, dy, dx, dweight, dweight_stride, dbias, dbias_stride, st);

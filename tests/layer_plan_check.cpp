@@ -6,6 +6,7 @@
 #include <numeric>
 
 namespace {
+#include "layer_arrays.h"
 #include "layer_plan.h"
 }
 
@@ -23,4 +24,14 @@ extern "C" int64_t drop_sums(int64_t max_rows, int64_t cols, int n, int v) { ret
 extern "C" int64_t drop_used(int64_t rows, int64_t cols, int n, int v, int dense) {
     const Walk k = walk_of(rows, cols, n, v, dense && walked_as_one(rows, cols, v), true);
     return k.chunks == 1 && k.width == cols ? 0 : k.chunks * k.width;
+}
+
+// Whether a written array shares memory with another; each is {place, run, three times size and stride}, in elements of 2 bytes.
+extern "C" int arrays_share(const int64_t *a, const int64_t *b, int *is_same) {
+    auto of = [](const int64_t *v) {
+        const Axis axes[3] = {{v[2], v[3]}, {v[4], v[5]}, {v[6], v[7]}};
+        return array_of(reinterpret_cast<const void *>((uintptr_t)(4096 + 2 * v[0])), v[1], axes, 2);
+    };
+    *is_same = same(of(a), of(b));
+    return shares(of(a), of(b));
 }

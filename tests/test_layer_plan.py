@@ -103,3 +103,48 @@ def test_a_dropout_s_workspace_holds_any_call(rules, v):
                 if 1 <= rows <= most:
                     for dense in (0, 1):
                         assert rules.drop_used(rows, cols, n, v, dense) <= room, (n, most, cols, rows, dense)
+
+
+def places(a):
+    at, run, sizes, strides = a
+    got = set()
+    for i in range(sizes[0]):
+        for j in range(sizes[1]):
+            for k in range(sizes[2]):
+                first = at + i * strides[0] + j * strides[1] + k * strides[2]
+                got.update(range(first, first + run))
+    return got
+
+
+def test_whether_arrays_share_memory_is_known(rules):
+    """Against every element: exact where arrays are alike or one has no gaps, and never wrong where it says that they share."""
+    import random
+    rng = random.Random(5)
+    counts = {}
+    for _ in range(20000):
+        sizes, run = [rng.choice([1, 1, 2, 3, 5]) for _ in range(3)], rng.choice([1, 2, 4, 7])
+        arrays = []
+        for written in (True, False):
+            strides, inner = [0, 0, 0], run
+            for k in rng.sample(range(3), 3):
+                pad = rng.choice([0, 0, 1, run, 9])
+                strides[k] = inner + pad
+                inner = strides[k] * (sizes[k] - 1) + inner
+                if not written and rng.random() < 0.1:
+                    strides[k] = rng.choice([0, 1])
+            arrays.append((rng.randrange(0, 60), run, sizes, strides))
+        if rng.random() < 0.5:
+            arrays[1] = (arrays[1][0], run, sizes, arrays[0][3])
+        one, other = (places(a) for a in arrays)
+        raw = [(ctypes.c_int64 * 8)(a[0], a[1], *[v for pair in zip(a[2], a[3]) for v in pair]) for a in arrays]
+        is_same = ctypes.c_int()
+        got, share = bool(rules.arrays_share(*raw, ctypes.byref(is_same))), bool(one & other)
+        like = all(s == 1 or p == q for s, p, q in zip(sizes, arrays[0][3], arrays[1][3]))
+        gapless = any(max(p) - min(p) + 1 == len(p) for p in (one, other))
+        nested = len(other) == run * sizes[0] * sizes[1] * sizes[2]
+        if like or gapless and nested:
+            assert got == share, arrays
+        assert share or not got, arrays
+        assert not is_same.value or one == other
+        counts[like, gapless, share] = counts.get((like, gapless, share), 0) + 1
+    assert all(counts.get((a, b, c), 0) > 100 for a in (False, True) for b in (False, True) for c in (False, True)), counts

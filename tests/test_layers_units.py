@@ -292,3 +292,43 @@ def test_a_handle_for_one_wide_row_takes_no_memory():
     op = layers.Dropout(1, 1, 2 ** 25 + 1, 0.1, 0, 1)
     assert before - torch.cuda.mem_get_info()[0] < 2 ** 23          # (another process's share of the card may move a little)
     op.close()
+
+
+def test_arrays_that_share_memory_are_refused():
+    """But a result in an input's place; columns of one wider array lie beside each other and share nothing."""
+    from paper_2007_13221_b200.binding import CSERError
+    n, rows, cols = 2, 12, 16
+    room = torch.zeros(4 * n * rows * cols, device="cuda", dtype=F32)
+    count = n * rows * cols
+    drop, norm = layers.Dropout(n, rows, cols, 0.5, 0, 1, F32), layers.GroupNorm(n, 3, cols, 4, dtype=F32)
+
+    def array(at, shape=(n, rows, cols)):
+        return room[at:at + count].view(shape)
+
+    def image(at):
+        return array(at, (n, 3, 4, cols))
+
+    params, far = torch.zeros((n, cols), device="cuda"), array(2 * count)
+    y, stats = norm.apply(image(0))
+    inside = room[5 * cols:5 * cols + n * cols].view(n, cols)
+    wide = torch.zeros((n, rows, 3 * cols), device="cuda")
+    halves = wide[..., :cols], wide[..., cols:2 * cols], wide[..., cols - 4:2 * cols - 4]
+    calls = [lambda: drop.apply(array(0), 1, out=array(4)), lambda: drop.apply(array(cols), 1, out=array(0)),
+             lambda: drop.apply(far, 1, residual=array(0), out=array(8)), lambda: drop.apply(far, 1, bias=inside, out=array(0)),
+             lambda: drop.grad(array(0), 1, dx=array(count - 4)), lambda: drop.grad(array(0), 1, need_dx=False, dbias=inside),
+             lambda: drop.grad(far, 1, dx=array(0), dbias=inside), lambda: drop.apply(halves[0], 1, out=halves[2]),
+             lambda: norm.apply(image(0), out=image(4)), lambda: norm.apply(image(2 * count), weight=inside, out=image(0)),
+             lambda: norm.grad(image(0), image(2 * count), stats, dx=image(4)), lambda: norm.grad(image(2 * count), image(0), stats, dx=image(4)),
+             lambda: norm.grad(image(0), image(count), stats, dweight=inside), lambda: norm.grad(image(0), image(count), stats, dweight=params, dbias=params),
+             lambda: norm.grad(image(0), image(count), stats, weight=params, dweight=params),
+             lambda: norm.grad(image(0), image(count), stats, dx=image(2 * count), dbias=far.view(-1)[:n * cols].view(n, cols))]
+    for call in calls:
+        with pytest.raises(CSERError, match="share memory"):
+            call()
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(1)
+    halves[0].copy_(torch.randn((n, rows, cols), generator=gen, device="cuda"))
+    want = drop.apply(halves[0].contiguous(), 1)
+    assert torch.equal(drop.apply(halves[0], 1, out=halves[1]), want)
+    assert torch.equal(drop.apply(halves[0], 1, out=halves[0]), want)
+    assert torch.equal(drop.apply(array(0), 1, out=array(count)), drop.apply(array(0), 1))
