@@ -51,12 +51,13 @@ template <typename F> __device__ __forceinline__ void with_act(int act, F f) {
 // 1 / (1 + exp(-z)) of two numbers by the exponential and the reciprocal that are instructions, each good to about 2^-22: as good as the
 // rounding of z in 32 bits lets it be, and far below that of 16-bit results.  One reciprocal of the product serves both (of a silu gradient's
 // time the special functions' pipe was the largest part: 8 x 16 x 56 x 56 x 256 forward 96 -> 91 us), for which exponentials end at 2^60:
-// below z = -41 it stays 2^-60.
-__device__ __forceinline__ F2 sigmoid(F2 z) {
+// below z = -41 it stays 2^-60.  e: exp(-z), so that e times the result is 1 minus it, without a difference of nearly equal numbers.
+__device__ __forceinline__ F2 sigmoid(F2 z, F2 &e) {
     F2 t = z * two(-1.4426950408889634f);
     asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(t.x));
     asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(t.y));
-    t = F2{fminf(t.x, 0x1p60f), fminf(t.y, 0x1p60f)} + two(1.f);
+    e = F2{fminf(t.x, 0x1p60f), fminf(t.y, 0x1p60f)};
+    t = e + two(1.f);
     float r = t.x * t.y;
     asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(r));
     return F2{t.y, t.x} * two(r);
@@ -65,15 +66,17 @@ __device__ __forceinline__ F2 sigmoid(F2 z) {
 __device__ __forceinline__ float relu(float v, float z) { return z <= 0.f ? 0.f : v; }
 
 template <int ACT> __device__ __forceinline__ F2 activate(F2 z) {
-    if (ACT == kActSilu) return z * sigmoid(z);
+    F2 e;
+    if (ACT == kActSilu) return z * sigmoid(z, e);
     if (ACT == kActRelu) return {relu(z.x, z.x), relu(z.y, z.y)};
     return z;
 }
 // dy * act'(z)
 template <int ACT> __device__ __forceinline__ F2 slope_times(F2 dy, F2 z) {
     if (ACT == kActSilu) {
-        const F2 g = sigmoid(z);
-        return dy * (g * fma2(z, two(1.f) - g, two(1.f)));
+        F2 e;
+        const F2 g = sigmoid(z, e);
+        return dy * (g * fma2(z, e * g, two(1.f)));
     }
     if (ACT == kActRelu) return {relu(dy.x, z.x), relu(dy.y, z.y)};
     return dy;
