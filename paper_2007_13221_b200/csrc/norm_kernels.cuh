@@ -50,17 +50,23 @@ template <typename F> __device__ __forceinline__ void with_act(int act, F f) {
 
 // 1 / (1 + exp(-z)) of two numbers by the exponential and the reciprocal that are instructions, each good to about 2^-22: as good as the
 // rounding of z in 32 bits lets it be, and far below that of 16-bit results.  One reciprocal of the product serves both (of a silu gradient's
-// time the special functions' pipe was the largest part: 8 x 16 x 56 x 56 x 256 forward 96 -> 91 us), for which exponentials end at 2^60:
-// below z = -41 it stays 2^-60.  e: exp(-z), so that e times the result is 1 minus it, without a difference of nearly equal numbers.
+// time the special functions' pipe was the largest part: 8 x 16 x 56 x 56 x 256 forward 96 -> 91 us).  The factors are made 2^63 times
+// smaller, so that the product of any two that are numbers is one, and so is its reciprocal; results below 2^-126 become 0 (exponentials ended
+// at 2^60 saved a multiplication, and 2 % of that gradient's time, but left 2^-60 below z = -41; a branch for those cost 4 %).  NaN counts as
+// the largest exponential, which leaves the other number alone, and stays in z.  e: exp(-z), so that e times the result is 1 minus it,
+// without a difference of nearly equal numbers.
 __device__ __forceinline__ F2 sigmoid(F2 z, F2 &e) {
-    F2 t = z * two(-1.4426950408889634f);
-    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(t.x));
-    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(t.y));
-    e = F2{fminf(t.x, 0x1p60f), fminf(t.y, 0x1p60f)};
-    t = e + two(1.f);
-    float r = t.x * t.y;
+    const F2 t = z * two(-1.4426950408889634f);
+    float p = t.x, q = t.y;
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(p));
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(q));
+    e = F2{fminf(p, 0x1p127f), fminf(q, 0x1p127f)};
+    const F2 s = fma2(e, two(0x1p-63f), two(0x1p-63f));
+    float r = s.x * s.y;
     asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(r));
-    return F2{t.y, t.x} * two(r);
+    unsigned long long g;
+    asm("mul.rn.ftz.f32x2 %0, %1, %2;" : "=l"(g) : "l"(bits_of(F2{s.y, s.x} * two(r))), "l"(bits_of(two(0x1p-63f))));
+    return pair_of(g);
 }
 // NaN stays NaN.
 __device__ __forceinline__ float relu(float v, float z) { return z <= 0.f ? 0.f : v; }

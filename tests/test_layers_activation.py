@@ -31,8 +31,10 @@ def results(z, dtype, pixels, groups):
     return y[0, 0, 0].double(), op.grad(x, dy, stats, weight, z[None])[2][0].double()
 
 
-def check(z, dtype, pixels, groups):
-    y, slope = results(z, dtype, pixels, groups)
+def check(z, dtype, pixels, groups, of=slice(None)):
+    """The results at the channels `of` against the bounds; all results."""
+    every = results(z, dtype, pixels, groups)
+    y, slope, z = every[0][of], every[1][of], z[of]
     v = z.double()
     g, h = torch.sigmoid(v), torch.sigmoid(-v)
     d_g, d_h = h * (v.abs() + 2) * 2 * E + 8 * E, g * (v.abs() + 2) * 2 * E + 8 * E
@@ -44,6 +46,7 @@ def check(z, dtype, pixels, groups):
     want = g * (1 + v * h)
     off = (slope - want).abs() - (g * (1 + v.abs() * h) * (d_g + 4 * E) + g * v.abs() * h * d_h + flush + 2.0 ** -126)
     assert bool((off <= 0).all()), (float(z[off.argmax()]), float(slope[off.argmax()]), float(want[off.argmax()]))
+    return every
 
 
 # one walk with vectors of 16 bytes, of fewer, and several walks
@@ -58,3 +61,26 @@ def test_slopes_of_large_values(plan):
     z = torch.cat([torch.linspace(-20, 110, 2048), torch.logspace(0, 3, 2048).clamp(max=top)])
     z = z[torch.randperm(4096, generator=torch.Generator().manual_seed(1))]
     check(z.cuda(), dtype, pixels, groups)
+
+
+@pytest.mark.parametrize("plan", PLANS, ids=str)
+def test_values_far_below_zero(plan):
+    """z / (1 + exp(-z)) goes to 0 there, and so does its slope."""
+    dtype, pixels, groups = plan
+    z = -torch.cat([torch.linspace(30, 130, 2048), torch.logspace(1, 30, 2048)])
+    z = z[torch.randperm(4096, generator=torch.Generator().manual_seed(1))]
+    z[torch.arange(0, 4096, 5)] = torch.linspace(-10, 10, 820)      # and beside ordinary ones
+    check(z.cuda(), dtype, pixels, groups)
+
+
+@pytest.mark.parametrize("plan", PLANS, ids=str)
+def test_values_that_are_no_numbers_spoil_no_neighbour(plan):
+    dtype, pixels, groups = plan
+    z = torch.linspace(-60, 60, 4096)
+    bad = torch.arange(0, 4096, 5)
+    z[bad] = torch.tensor([float("nan"), float("inf"), -float("inf")]).repeat(274)[:820]
+    z = z.cuda()
+    fine = torch.ones(4096, dtype=torch.bool)
+    fine[bad] = False
+    y, slope = check(z, dtype, pixels, groups, fine.cuda())
+    assert bool(y[z == float("inf")].isposinf().all()) and bool(y[z.isnan() | z.isneginf()].isnan().all()) and bool(slope[z.isnan()].isnan().all())
