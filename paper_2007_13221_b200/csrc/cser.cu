@@ -35,10 +35,16 @@ namespace {
 
 thread_local char g_err[512] = "";
 
+int fail_v(int code, const char *fmt, va_list ap) {
+    vsnprintf(g_err, sizeof(g_err), fmt, ap);
+    // An error that is reported here is not the next call's: the runtime would give it to whoever asks for the last one after a launch.
+    if (code == CSER_ERR_CUDA || code == CSER_ERR_NOMEM) cudaGetLastError();
+    return code;
+}
 int fail(int code, const char *fmt, ...) {
     va_list ap;
     va_start(ap, fmt);
-    vsnprintf(g_err, sizeof(g_err), fmt, ap);
+    fail_v(code, fmt, ap);
     va_end(ap);
     return code;
 }
@@ -657,7 +663,7 @@ size_t g_l2_limit_before[64] = {};
 int cser_internal_fail(int code, const char *fmt, ...) {
     va_list ap;
     va_start(ap, fmt);
-    vsnprintf(g_err, sizeof(g_err), fmt, ap);
+    fail_v(code, fmt, ap);
     va_end(ap);
     return code;
 }

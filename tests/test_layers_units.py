@@ -332,3 +332,18 @@ def test_arrays_that_share_memory_are_refused():
     assert torch.equal(drop.apply(halves[0], 1, out=halves[1]), want)
     assert torch.equal(drop.apply(halves[0], 1, out=halves[0]), want)
     assert torch.equal(drop.apply(array(0), 1, out=array(count)), drop.apply(array(0), 1))
+
+
+def test_an_error_that_was_reported_stays_behind():
+    """A handle too large for the GPU is refused, and the next call of any kind does not hear of it."""
+    from paper_2007_13221_b200 import binding, train
+    from paper_2007_13221_b200.binding import CSERError
+    opt = binding.CSER(1000, 2, 16, R1=4, R2=2, H=4, eta=0.1, beta=0.9, flags=binding.FLAG_THREE_KERNELS)
+    opt.set_x0(torch.zeros(1000, device="cuda"))
+    grad = torch.ones((2, 1000), device="cuda")
+    for make in (lambda: layers.GroupNorm(4096, 4096, 65536, 1), lambda: layers.Dropout(4096, 2 ** 20, 2 ** 14, 0.1, 0, 1),
+                 lambda: train.LinearCrossEntropy(1, 2 ** 24, 2 ** 22, 64, piece=2 ** 22)):
+        with pytest.raises(CSERError):
+            make()
+        opt.step(grad)
+    opt.close()
