@@ -8,10 +8,10 @@
 // Everything that is summed is summed for each channel first, then over the channels of a group: one walk over the pixels serves any
 // number of channels a group, and the gradient's channel sums are dbias and dweight.  Bound: memory, with the issue of instructions close
 // behind (of the 176 and 264 slots that an SM's quarter has for eight bf16 elements at the copy rate, silu's forward pass takes about 130 and its
-// gradient 250, with 96 and 192 cycles of the special functions' pipe): two floats an instruction, approximations by single instructions.
+// gradient 270, with 96 and 192 cycles of the special functions' pipe): two floats an instruction, approximations by single instructions.
 //
 // The kernels in several walks: 512 x 512 x 128 in bf16 with silu, 53 us forward (moments 21, join 5, result 23; floor 20) and 85 backward (sums
-// 35, joins 8, result 42; floor 31): latency, at 16 to 32 warps an SM with four or eight loads of each thread under way.
+// 35, joins 8, result 42; floor 31): latency, at 15 to 28 warps an SM with four or eight loads of each thread under way.
 #pragma once
 
 enum { kActNone = CSER_ACT_NONE, kActRelu = CSER_ACT_RELU, kActSilu = CSER_ACT_SILU };

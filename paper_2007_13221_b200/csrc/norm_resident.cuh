@@ -11,7 +11,7 @@
 // Measured, 8 x 16 samples of 56 x 56 x 256 in bf16, without activation (4.9 TB/s forward, 4.7 backward; what bounds it is the latency of the
 // steps between a unit's last load and its first store, on the 16 warps that the registers leave an SM): 3 to 5 walks by kernels of
 // their own 638 us for both directions; clusters of eight with reads of each other's sums 368; stores instead, fewer divisions 256; blocks that
-// stay, slices of 64 bytes by two and four blocks 214.  With silu 276: 24 exponentials and reciprocals for eight elements of the gradient.
+// stay, slices of 64 bytes by two and four blocks 214.  With silu 286: 24 exponentials and reciprocals for eight elements of the gradient.
 // Tried: 512 threads at 64 registers (spills, forward 93 us for 83), slices of 128 bytes by clusters of eight (100), of 32 by one block (101).
 #pragma once
 
